@@ -217,10 +217,12 @@ def _prepare_step(s, case, gen, seed):
             values.append(v)
         s.packed, s.weight = torch.cat(s.packed), torch.cat(values)
         s.scales = torch.nn.functional.pad(torch.cat(s.scales), (0, -(H // 32) % 16)).contiguous()
-    # the token to come: one the row allows, usually the representative of its class or one near it
+    # the token to come: one the row allows
     allowed = bits[:, s.c_dev.long()]
     first = torch.rand((B, V), generator=gen, device="cuda").masked_fill_(~allowed, -1.0).argmax(dim=1)
-    s.hidden = _hidden(s.weight[first].float(), 14.0, gen)
+    # ... about as likely as all the others together
+    sure = torch.log(allowed.sum(dim=1, keepdim=True).float()) + 2.0 + torch.randn((B, 1), generator=gen, device="cuda")
+    s.hidden = _hidden(s.weight[first].float(), sure, gen)
     if case["head"] == "mxfp4":
         s.weight = None
     s.vocab_mask = torch.zeros((B, _words(V)), dtype=torch.int32, device="cuda")
@@ -318,7 +320,8 @@ def _quantize(w):
 def _dequantized(packed, scales, H):
     code = torch.stack([packed & 15, packed >> 4], dim=2).view(packed.shape[0], H)
     value = torch.tensor(_E2M1 + tuple(-v for v in _E2M1), device=packed.device)[code.int()]
-    scale = torch.ldexp(torch.ones((), device=packed.device), scales[:, : H // 32].int() - 127)
+    scales = scales[:, : H // 32].int() - 127
+    scale = torch.ldexp(torch.ones_like(scales, dtype=torch.float32), scales)
     return (value.view(-1, H // 32, 32) * scale.unsqueeze(2)).view(-1, H)
 
 
@@ -328,10 +331,10 @@ def _plain_step(s):
     w = s.weight.float() if s.weight is not None else _dequantized(s.packed, s.scales, H)
     z = (s.hidden.float() @ w.T).masked_fill(~allowed, float("-inf"))
     top, token = z.max(dim=1)
-    lse = top + torch.log(torch.exp(z - top.unsqueeze(1)).sum(dim=1))
+    log_sum = torch.log(torch.exp(z - top.unsqueeze(1)).sum(dim=1))
     rep = s.r_dev[s.c_dev[token].long()]
     logits = None if s.logits is None else z.to(s.logits.dtype)
-    return [_pack(allowed), logits, token.to(torch.int32), rep, top - lse, lse]
+    return [_pack(allowed), logits, token.to(torch.int32), rep, -log_sum, top + log_sum]
 
 
 def _plain_loss(s):
@@ -340,10 +343,10 @@ def _plain_loss(s):
     for (x, _, mask), t in zip(_row_pieces(s, 1024), s.targets.split(1024)):
         z = _masked(x.float() @ w.T, mask, V)
         top = z.amax(dim=1)
-        lse = top + torch.log(torch.exp(z - top.unsqueeze(1)).sum(dim=1))
+        log_sum = torch.log(torch.exp(z - top.unsqueeze(1)).sum(dim=1))
         of_target = z.gather(1, t.long().clamp(min=0).unsqueeze(1)).squeeze(1)
-        losses.append(torch.where(t >= 0, lse - of_target, 0.0))
-        lses.append(lse)
+        losses.append(torch.where(t >= 0, (top - of_target) + log_sum, 0.0))
+        lses.append(top + log_sum)
     return [torch.cat(losses), torch.cat(lses)]
 
 
@@ -416,7 +419,8 @@ def _exact_weights(s, lo, hi):
     for half in (0, 1):
         code = (s.packed[lo:hi] >> (4 * half)).int() & 15
         out[:, half::2] = steps[code & 7] * (1.0 - 2.0 * (code >> 3))
-    power = torch.pow(2.0, s.scales[lo:hi, : H // 32].double() - 127.0)
+    e = s.scales[lo:hi, : H // 32].int() - 127
+    power = torch.ldexp(torch.ones_like(e, dtype=torch.float64), e)
     return out * power.repeat_interleave(32, dim=1)
 
 
@@ -433,11 +437,10 @@ def _exact_step(s):
     V, K, B = s.case["V"], s.case["K"], s.case["B"]
     k = torch.arange(K, device="cuda")
     bits = (s.class_mask[:, k // 32] >> (k % 32).int()) & 1 == 1
-    token_bits = torch.zeros((B, _words(V) * 32), dtype=torch.float64, device="cuda")
-    token_bits[:, :V] = bits[:, s.c_dev.long()].double()
-    powers = torch.pow(2.0, torch.arange(32, dtype=torch.float64, device="cuda"))
-    words = (token_bits.view(B, -1, 32) * powers).sum(dim=2)
-    s.vocab_mask = torch.where(words >= 2.0 ** 31, words - 2.0 ** 32, words).to(torch.int32)
+    token_bits = torch.zeros((B, _words(V) * 32), dtype=torch.int64, device="cuda")
+    token_bits[:, :V] = bits[:, s.c_dev.long()]
+    words = sum(token_bits[:, i::32] * 2 ** i for i in range(32))
+    s.vocab_mask = torch.where(words >= 2 ** 31, words - 2 ** 32, words).to(torch.int32)
     z = _exact_scores(s, s.hidden, 0, B, V)
     lse = torch.logsumexp(z, dim=1)
     token = z.argmax(dim=1)
@@ -482,7 +485,7 @@ def _exact_quantize(s):
         blocks = w.double().view(-1, H // 32, 32)
         most = blocks.abs().amax(dim=2)
         e = torch.where(most > 0, torch.floor(torch.log2(most)) - 2.0, -127.0).clamp(min=-127.0)
-        power = torch.pow(2.0, e).unsqueeze(2)
+        power = torch.ldexp(torch.ones_like(e), e.int()).unsqueeze(2)
         a = blocks.abs() / power
         below = torch.searchsorted(edges, a.contiguous(), right=False)   # the number of edges under a
         on_edge = (below < 7) & (edges[below.clamp(max=6)] == a) & (below % 2 == 1)
