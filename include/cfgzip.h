@@ -40,14 +40,16 @@ typedef struct cfgzip_ctx cfgzip_ctx; /* opaque: device tables, scratch, sticky 
 typedef int32_t cfgzip_part_id;       /* small dense id inside one context */
 
 enum { CFGZIP_F32 = 0, CFGZIP_BF16 = 1 };                   /* logit element type */
+enum { CFGZIP_MXFP4 = 2 };                                  /* heads only: microscaled 4-bit weights, see cfgzip_head */
 enum { CFGZIP_AUTO = 0, CFGZIP_DENSE = 1, CFGZIP_SPARSE = 2 }; /* expansion strategy */
 enum {
     CFGZIP_OK = 0,
     CFGZIP_E_ARG = -1,       /* null pointer, negative size, stride too small, unknown enum */
     CFGZIP_E_RANGE = -2,     /* partition id not loaded, V mismatch, size beyond a limit */
     CFGZIP_E_PARTITION = -3, /* c / r do not describe a partition (see cfgzip_check_partition) */
-    CFGZIP_E_ALIGN = -4,     /* logits rows that must be 16-byte aligned are not (cfgzip_multi_mask_logsoftmax_argmax,
-                                cfgzip_rmw_floor); every other call takes rows that start anywhere */
+    CFGZIP_E_ALIGN = -4,     /* rows that must be 16-byte aligned are not: logits of cfgzip_multi_mask_logsoftmax_argmax and
+                                cfgzip_rmw_floor (every other call takes logits rows that start anywhere), and the weights,
+                                scales, hidden states and their gradients of the cfgzip_head calls */
     CFGZIP_E_CUDA = -5,      /* a CUDA runtime call failed (no device, launch error) */
     CFGZIP_E_NOMEM = -6      /* device allocation failed, or B exceeds the reserved rows */
 };
@@ -251,6 +253,98 @@ int cfgzip_multi_mask_logsoftmax_argmax(cfgzip_ctx* ctx, cfgzip_part_id part0, c
 int cfgzip_map_tokens(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_part,
                       const int32_t* tokens /*dev [B]*/, int32_t* reps /*dev [B]*/, int32_t B,
                       void* stream);
+
+/*
+ * ---- The head: the product of hidden states with the vocabulary, which is where the logits come from (Section 2.2: the
+ * language model's next-token scores over T), under the same masks. A decode step from hidden states reads only what the
+ * grammars of the batch allow; training on answers that a grammar allows needs the loss over the allowed tokens and its gradient.
+ *
+ * A head is a [V, H] matrix of weights on the device, described by a struct that the calls only read (the memory is the
+ * caller's, nothing of it is kept). With z[b, t] = sum_h hidden[b, h] * weight[t, h], accumulated in 32 bits:
+ *   CFGZIP_BF16  : weight [V, row_stride] bf16, row_stride in elements. H a multiple of 8.
+ *   CFGZIP_MXFP4 : two weights to a byte, the one with the lower index in the lower half, row_stride in bytes; each is e2m1
+ *                  (sign bit, then 0, 0.5, 1, 1.5, 2, 3, 4, 6) times 2^(scale - 127) with one scale byte per 32 weights of a
+ *                  row in `scales`, scale_stride bytes from row to row. H a multiple of 32. A scale of 255 is not taken (NaN).
+ * Rows of weights, scales, hidden states and gradients start on 16 bytes (CFGZIP_E_ALIGN otherwise); H at most 65536.
+ * Hidden states are bf16. They may be any values whose products stay finite; +inf and NaN scores are outside the contract.
+ */
+typedef struct cfgzip_head {
+    void* weight;         /* dev */
+    void* scales;         /* dev, CFGZIP_MXFP4 only */
+    int64_t row_stride;   /* elements (CFGZIP_BF16) or bytes (CFGZIP_MXFP4) */
+    int64_t scale_stride; /* bytes */
+    int32_t V, H;
+    int32_t dtype;        /* CFGZIP_BF16 or CFGZIP_MXFP4 */
+    int32_t reserved;     /* 0 */
+} cfgzip_head;
+
+/* Device memory that a call of the given kind wants in `workspace` for up to `rows` rows. The caller owns it; it holds nothing
+ * from one call to the next, and calls that can overlap on the GPU (graphs replayed side by side too) need one each. Calls with
+ * less give CFGZIP_E_NOMEM. Host only, touches no GPU. */
+enum { CFGZIP_HEAD_STEP = 0, CFGZIP_HEAD_LOSS = 1, CFGZIP_HEAD_LOSS_BACKWARD = 2 };
+int cfgzip_head_workspace(const cfgzip_head* head, int op, int32_t rows, int64_t* bytes);
+
+/*
+ * Weights to 4 bits: per 32 weights of a row the scale is the power of two 2^(floor(log2 max|w|) - 2), not below 2^-127, and
+ * each weight the nearest of the sixteen values times the scale (ties to the even code, above 6 to 6). A block of zeros gets
+ * scale byte 0; a block that holds an infinity or a NaN gets scale byte 255 and codes 0.
+ *   weight : dev [V, row_stride_elems] of `dtype` (CFGZIP_F32 or CFGZIP_BF16), V and H those of `head`, rows 16-byte aligned
+ *   head   : CFGZIP_MXFP4; its weight and scales are written (scale bytes behind H / 32 are left alone)
+ */
+int cfgzip_head_quantize(cfgzip_ctx* ctx, const void* weight, int dtype, int64_t row_stride_elems, const cfgzip_head* head,
+                         void* stream);
+/* The values a CFGZIP_MXFP4 head stands for, as bf16 (exact; a scale byte of 255 gives NaN): a frozen 4-bit head in the form
+ * that cfgzip_head_loss takes.   values : dev bf16 [V, row_stride_elems] (written), rows 16-byte aligned */
+int cfgzip_head_dequantize(cfgzip_ctx* ctx, const cfgzip_head* head, void* values, int64_t row_stride_elems, void* stream);
+
+/*
+ * cfgzip_masked_logsoftmax_argmax from hidden states: the scores of the tokens that some row of the batch allows are computed
+ * (weights of other tokens are not read) and reduced without being stored.
+ *   part0, row_part, class_mask : as there; the partitions' V is that of the head (CFGZIP_E_RANGE otherwise)
+ *   hidden     : dev bf16 [B, hidden_stride]
+ *   vocab_mask : nullable, as there
+ *   logits     : nullable dev [B, logits_stride] of logits_dtype (CFGZIP_F32 or CFGZIP_BF16), rows may start at any element;
+ *                receives the masked scores, -inf where a token is not allowed, for the sampling calls
+ *   argmax     : dev int32 [B]; the choice is made on the 32-bit scores, not on rounded logits
+ *   rep, logp_argmax, lse : nullable, as there
+ * Rows with nothing allowed, and rows whose partition is not loaded (all their outputs untouched), as there.
+ */
+int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_part, const uint32_t* class_mask,
+                     int64_t class_stride_words, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t B,
+                     uint32_t* vocab_mask, int64_t vocab_stride_words, void* logits, int logits_dtype, int64_t logits_stride,
+                     int32_t* argmax, int32_t* rep, float* logp_argmax, float* lse, void* workspace, int64_t workspace_bytes,
+                     void* stream);
+
+/*
+ * Cross entropy of N tokens over the tokens that each row allows, computed in pieces of the vocabulary:
+ *   lse[n] = log sum_{allowed t} exp(z[n, t]),   loss[n] = lse[n] - z[n, targets[n]]
+ *   head       : CFGZIP_BF16 (CFGZIP_E_ARG otherwise)
+ *   hidden     : dev bf16 [N, hidden_stride]
+ *   vocab_mask : NULL (everything is allowed) or dev uint32 [N, vocab_stride_words], as cfgzip_expand_mask writes them
+ *   targets    : dev int32 [N]; a negative one has no loss (loss 0). One that the row does not allow has loss +inf; one at V
+ *                or above too, and counts as a bad token.
+ *   loss, lse  : dev float [N], lse nullable; a row with nothing allowed has lse -inf (and loss +inf unless its target is negative)
+ */
+int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N,
+                     const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* targets, float* loss, float* lse,
+                     void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Its gradient. With g[n, t] = d_loss[n] * (exp(z[n, t] - lse[n]) - [t = targets[n]]) over the allowed tokens, and 0 in rows
+ * whose loss is not a finite function of z (a negative target, one that is not allowed, nothing allowed):
+ *   d_hidden[n, :] = sum_t g[n, t] * weight[t, :],    d_weight[t, :] = sum_n g[n, t] * hidden[n, :]
+ * The scores are computed again; g is rounded to bf16 (relative 2^-9) for the two products, which accumulate in 32 bits.
+ *   hidden .. targets : as given to cfgzip_head_loss, and lse as it returned it (required)
+ *   d_loss     : dev float [N]
+ *   d_hidden   : nullable dev bf16 [N, d_hidden_stride] (written)
+ *   d_weight   : nullable dev [V, d_weight_stride] of d_weight_dtype (CFGZIP_BF16 or CFGZIP_F32); written, or added to where
+ *                accumulate is not 0
+ * The results do not depend on timing (no atomic additions).
+ */
+int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N,
+                              const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* targets, const float* lse,
+                              const float* d_loss, void* d_hidden, int64_t d_hidden_stride, void* d_weight, int d_weight_dtype,
+                              int64_t d_weight_stride, int accumulate, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
  * Host-only choice between CFGZIP_DENSE and CFGZIP_SPARSE for a batch whose class masks are still in host memory,

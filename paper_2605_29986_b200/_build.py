@@ -5,6 +5,7 @@ import os
 import shutil
 import subprocess
 import sysconfig
+import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_HERE, "csrc")
@@ -14,7 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libcfgzip.so")
 CALLS_PATH = os.path.join(_HERE, "_calls" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 NVCC_FLAGS = [
-    "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo", "-shared",
+    "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
 ]
 
@@ -57,11 +58,17 @@ def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
     if not os.path.exists(nvcc):
         raise RuntimeError("nvcc not found: the CFGzip CUDA library cannot be built")
+    compile_flags = NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-I", _INCLUDE, "-I", _CSRC]
     tmp = LIB_PATH + ".%d.tmp" % os.getpid()
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + [
-        "-I", _INCLUDE, "-I", _CSRC, "-o", tmp, os.path.join(_CSRC, "cfgzip_api.cu"),
-        os.path.join(_CSRC, "cfgzip_offline.cu")]
-    subprocess.check_call(cmd)
+    with tempfile.TemporaryDirectory() as objects:  # the sources side by side: they take a minute each
+        jobs = []
+        for source in (f for f in _sources() if f.endswith(".cu")):
+            obj = os.path.join(objects, os.path.basename(source) + ".o")
+            jobs.append((obj, subprocess.Popen([nvcc] + compile_flags + ["-c", "-o", obj, source])))
+        failed = [obj for obj, job in jobs if job.wait() != 0]
+        if failed:
+            raise RuntimeError("nvcc failed for %s" % ", ".join(os.path.basename(o)[:-2] for o in failed))
+        subprocess.check_call([nvcc] + NVCC_FLAGS + ["-shared", "-o", tmp] + [obj for obj, _ in jobs])
     os.replace(tmp, LIB_PATH)
     return LIB_PATH
 

@@ -18,8 +18,9 @@ try:
 except ImportError:  # it could not be built here: the same functions through ctypes, a few microseconds slower
     _calls = None
 
-F32, BF16 = 0, 1
+F32, BF16, MXFP4 = 0, 1, 2  # (MXFP4: heads only)
 AUTO, DENSE, SPARSE = 0, 1, 2
+HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD = 0, 1, 2
 OK, E_ARG, E_RANGE, E_PARTITION, E_ALIGN, E_CUDA, E_NOMEM = 0, -1, -2, -3, -4, -5, -6
 
 _vp, _i32, _i64, _int = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_int
@@ -45,6 +46,14 @@ _SIGNATURES = {
                                                    _vp, _vp]),
     "cfgzip_plan_rows": (_int, [_vp, _i32, _vp, _i32, _vp]),
     "cfgzip_map_tokens": (_int, [_vp, _i32, _vp, _vp, _vp, _i32, _vp]),
+    "cfgzip_head_workspace": (_int, [_vp, _int, _i32, ctypes.POINTER(_i64)]),
+    "cfgzip_head_quantize": (_int, [_vp, _vp, _int, _i64, _vp, _vp]),
+    "cfgzip_head_dequantize": (_int, [_vp, _vp, _vp, _i64, _vp]),
+    "cfgzip_head_step": (_int, [_vp, _i32, _vp, _vp, _i64, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _int, _i64, _vp, _vp, _vp, _vp,
+                                _vp, _i64, _vp]),
+    "cfgzip_head_loss": (_int, [_vp, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "cfgzip_head_loss_backward": (_int, [_vp, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _int, _i64, _int,
+                                         _vp, _i64, _vp]),
     "cfgzip_choose_mode": (_int, [_vp, _i32, _vp, _vp, _i64, _i32, _int]),
     "cfgzip_decode_step_host": (_int, [_vp, _i32, _vp, _vp, _i64, _vp, _int, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _int,
                                        _vp]),
@@ -179,6 +188,16 @@ _STEP_CALLS = {
     "cfgzip_map_tokens": ("pipppis", 6, "ctx part0 row_part tokens reps B stream"),
     "cfgzip_decode_step_host": ("pippipiippppppis", 8, "ctx part0 row_part_host class_mask_host class_stride_words logits_host dtype B "
                                 "masked_logits vocab_mask_host argmax rep logp_argmax lse mode stream"),
+    "cfgzip_head_quantize": ("ppiips", 5, "ctx weight dtype row_stride_elems head stream"),
+    "cfgzip_head_dequantize": ("pppis", 4, "ctx head values row_stride_elems stream"),
+    "cfgzip_head_step": ("pippippiipipiipppppis", 20, "ctx part0 row_part class_mask class_stride_words head hidden hidden_stride B "
+                         "vocab_mask vocab_stride_words logits logits_dtype logits_stride argmax rep logp_argmax lse workspace "
+                         "workspace_bytes stream"),
+    "cfgzip_head_loss": ("pppiipippppis", 12, "ctx head hidden hidden_stride N vocab_mask vocab_stride_words targets loss lse "
+                         "workspace workspace_bytes stream"),
+    "cfgzip_head_loss_backward": ("pppiipippppipiiipis", 18, "ctx head hidden hidden_stride N vocab_mask vocab_stride_words targets "
+                                  "lse d_loss d_hidden d_hidden_stride d_weight d_weight_dtype d_weight_stride accumulate workspace "
+                                  "workspace_bytes stream"),
 }
 
 
@@ -208,6 +227,33 @@ for _name in _STEP_CALLS:
     globals()[_name] = getattr(_calls, _name) if _calls is not None else _through_ctypes(_name)
 
 ROWS_AS_PLANNED = 1  # pass as row_part after cfgzip_plan_rows: the kept grouping of that call is reused
+
+
+class cfgzip_head(ctypes.Structure):
+    """Description of a head: weights [V, H] on the device (bf16; or two 4-bit weights to a byte, with a scale byte per 32).
+
+    Strides default to dense rows. The buffers stay the caller's; this keeps a reference to those it was made from."""
+    _fields_ = [("weight", _vp), ("scales", _vp), ("row_stride", _i64), ("scale_stride", _i64), ("V", _i32), ("H", _i32),
+                ("dtype", _i32), ("reserved", _i32)]
+
+    def __init__(self, weight, dtype: int, V: int, H: int, row_stride: Optional[int] = None, scales=None,
+                 scale_stride: Optional[int] = None):
+        if row_stride is None:
+            row_stride = H // 2 if dtype == MXFP4 else H
+        if scale_stride is None:
+            scale_stride = H // 32 if scales is not None else 0
+        super().__init__(_ptr(weight), _ptr(scales), row_stride, scale_stride, V, H, dtype, 0)
+        self.buffers = (weight, scales)
+
+    def data_ptr(self) -> int:
+        return ctypes.addressof(self)
+
+
+def cfgzip_head_workspace(head: cfgzip_head, op: int, rows: int) -> int:
+    """Bytes of device memory a call of kind `op` (HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD) wants for up to `rows` rows."""
+    out = _i64(0)
+    _check(load_library().cfgzip_head_workspace(_ptr(head), op, rows, ctypes.byref(out)), "cfgzip_head_workspace")
+    return out.value
 
 
 def cfgzip_choose_mode(ctx: int, part0: int, row_part_host, class_mask_host, class_stride_words: int, B: int,

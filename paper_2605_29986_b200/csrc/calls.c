@@ -131,7 +131,8 @@ static PyObject* done(const Call* c, int status) {
     return PyObject_CallFunction(g_raise, "is", status, c->name); /* NULL: it raised */
 }
 
-enum { EXPAND_MASK, MASK_LOGITS, FUSED, SAMPLE, SAMPLE_FILTERED, MULTI_MASK, PLAN_ROWS, MAP_TOKENS, STEP_HOST, N_CALLS };
+enum { EXPAND_MASK, MASK_LOGITS, FUSED, SAMPLE, SAMPLE_FILTERED, MULTI_MASK, PLAN_ROWS, MAP_TOKENS, STEP_HOST,
+       HEAD_QUANTIZE, HEAD_DEQUANTIZE, HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD, N_CALLS };
 
 #define STEP_ARGS                                                                                                     \
     "ctx", "part0", "row_part", "class_mask", "class_stride_words", "logits", "dtype", "row_stride_elems", "B", "vocab_mask", \
@@ -157,6 +158,19 @@ static Call calls[N_CALLS] = {
     {"cfgzip_decode_step_host", "pippipiippppppis", 8,
      {"ctx", "part0", "row_part_host", "class_mask_host", "class_stride_words", "logits_host", "dtype", "B", "masked_logits",
       "vocab_mask_host", "argmax", "rep", "logp_argmax", "lse", "mode", "stream"}, NULL},
+    {"cfgzip_head_quantize", "ppiips", 5, {"ctx", "weight", "dtype", "row_stride_elems", "head", "stream"}, NULL},
+    {"cfgzip_head_dequantize", "pppis", 4, {"ctx", "head", "values", "row_stride_elems", "stream"}, NULL},
+    {"cfgzip_head_step", "pippippiipipiipppppis", 20,
+     {"ctx", "part0", "row_part", "class_mask", "class_stride_words", "head", "hidden", "hidden_stride", "B", "vocab_mask",
+      "vocab_stride_words", "logits", "logits_dtype", "logits_stride", "argmax", "rep", "logp_argmax", "lse", "workspace",
+      "workspace_bytes", "stream"}, NULL},
+    {"cfgzip_head_loss", "pppiipippppis", 12,
+     {"ctx", "head", "hidden", "hidden_stride", "N", "vocab_mask", "vocab_stride_words", "targets", "loss", "lse", "workspace",
+      "workspace_bytes", "stream"}, NULL},
+    {"cfgzip_head_loss_backward", "pppiipippppipiiipis", 18,
+     {"ctx", "head", "hidden", "hidden_stride", "N", "vocab_mask", "vocab_stride_words", "targets", "lse", "d_loss", "d_hidden",
+      "d_hidden_stride", "d_weight", "d_weight_dtype", "d_weight_stride", "accumulate", "workspace", "workspace_bytes", "stream"},
+     NULL},
 };
 
 #define I(k) ((int32_t)v[k].i)
@@ -216,6 +230,30 @@ static PyObject* py_cfgzip_decode_step_host(PyObject* self, PyObject* const* arg
          P(12), P(13), I(14), P(15));
 }
 
+#define HEAD(k) ((const cfgzip_head*)v[k].p)
+
+static PyObject* py_cfgzip_head_quantize(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    CALL(HEAD_QUANTIZE, cfgzip_head_quantize, CTX, P(1), I(2), L(3), HEAD(4), P(5));
+}
+
+static PyObject* py_cfgzip_head_dequantize(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    CALL(HEAD_DEQUANTIZE, cfgzip_head_dequantize, CTX, HEAD(1), P(2), L(3), P(4));
+}
+
+static PyObject* py_cfgzip_head_step(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    CALL(HEAD_STEP, cfgzip_head_step, CTX, I(1), P(2), P(3), L(4), HEAD(5), P(6), L(7), I(8), P(9), L(10), P(11), I(12), L(13),
+         P(14), P(15), P(16), P(17), P(18), L(19), P(20));
+}
+
+static PyObject* py_cfgzip_head_loss(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    CALL(HEAD_LOSS, cfgzip_head_loss, CTX, HEAD(1), P(2), L(3), I(4), P(5), L(6), P(7), P(8), P(9), P(10), L(11), P(12));
+}
+
+static PyObject* py_cfgzip_head_loss_backward(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    CALL(HEAD_LOSS_BACKWARD, cfgzip_head_loss_backward, CTX, HEAD(1), P(2), L(3), I(4), P(5), L(6), P(7), P(8), P(9), P(10), L(11),
+         P(12), I(13), L(14), I(15), P(16), L(17), P(18));
+}
+
 /* bind(addresses by name, raise): where the functions are, and what to call with (status, call) when one fails */
 static PyObject* py_bind(PyObject* self, PyObject* args) {
     PyObject *addresses, *raise;
@@ -247,6 +285,11 @@ static PyMethodDef methods[] = {
     METHOD(cfgzip_plan_rows),
     METHOD(cfgzip_map_tokens),
     METHOD(cfgzip_decode_step_host),
+    METHOD(cfgzip_head_quantize),
+    METHOD(cfgzip_head_dequantize),
+    METHOD(cfgzip_head_step),
+    METHOD(cfgzip_head_loss),
+    METHOD(cfgzip_head_loss_backward),
     {"bind", py_bind, METH_VARARGS, NULL},
     {NULL, NULL, 0, NULL},
 };

@@ -22,7 +22,6 @@ namespace cfgzip {
 // ---------------------------------------------------------------------------------------
 constexpr int kClusterThreads = 512, kClusterWarps = kClusterThreads / 32;
 constexpr int kClusterRows = 4;    // rows of a cluster
-constexpr int kClusterMost = 16;   // blocks of a cluster
 constexpr int kClusterChunks = 8;  // chunks of a warp's run
 constexpr int kClusterSlots = kClusterWarps + 2;  // states of a block: tokens in front of the first vector, the warps, tokens past the last one
 constexpr size_t kClusterStatic = 5 * 1024;       // most shared memory the kernel has beside the dynamic one

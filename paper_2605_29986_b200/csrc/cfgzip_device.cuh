@@ -11,6 +11,7 @@ namespace cfgzip {
 constexpr int kGroupRows = 32;        // rows that share one bit-sliced class table
 constexpr int kBatchRows = 8;         // rows a warp streams together
 constexpr int kNoPos = 0x7FFFFFFF;    // "no allowed token seen"
+constexpr int kClusterMost = 16;      // blocks of a cluster
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRefFloor = -1.7e38f; // lowest reference used for exp(z - ref)
 // Where the exponent is taken as z * scale - ref * scale (RowAcc): a logit with z * scale below this weighs nothing. The second product is
