@@ -55,31 +55,95 @@ struct Carve {
     }
 };
 
+constexpr int64_t kPieceBytes = int64_t(256) << 20;  // most of the gradient of the scores that is held at a time
+constexpr int kPairs = 74;                           // pairs of SMs that plans are made for (a plan is right for any number)
+
 struct HeadSpace {
+    // step
     float* z;
     RowState* state;
-    uint16_t *g, *weights;
-    float* d_hidden;
+    uint16_t* weights;
     uint32_t* mask;
+    // loss
+    float2* part;
+    float* of_target;
+    // gradient
+    int32_t piece, splits;  // tokens of a piece, cuts of the sum over them
+    uint16_t* g;
+    float* sums;
     int64_t bytes;
 };
+
+int up(int64_t n, int to) { return int((n + to - 1) / to * to); }
+
+// Cuts of a sum over k_blocks stages whose result has `tiles` tiles: more cuts fill the last wave of pairs better, and each is
+// one more f32 result written and read. A stage takes a pair about 0.4 us, a result's bytes 1 / 6.5 us per MB.
+int cuts(int64_t tiles, int k_blocks, int64_t result_elems) {
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= 16 && s <= std::max(1, k_blocks / 16); ++s) {
+        const double waves = double((tiles * s + kPairs - 1) / kPairs);
+        const double us = waves * ((k_blocks + s - 1) / s) * 0.4 + s * double(result_elems) * 8e-6 / 6.5;
+        if (s == 1 || us < least) {
+            least = us;
+            best = s;
+        }
+    }
+    return best;
+}
 
 HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace) {
     const uintptr_t skip = (256 - reinterpret_cast<uintptr_t>(workspace) % 256) % 256;
     Carve c(workspace ? static_cast<char*>(workspace) + skip : nullptr);
     HeadSpace s{};
-    s.z = c.take<float>(int64_t(rows) * kPiece);
-    if (op != CFGZIP_HEAD_LOSS_BACKWARD) s.state = c.take<RowState>(rows);
-    if (op == CFGZIP_HEAD_LOSS_BACKWARD) {
-        s.g = c.take<uint16_t>(int64_t(rows) * kPiece);
-        s.d_hidden = c.take<float>(int64_t(rows) * h->H);
-    }
+    const int64_t n = rows;
     if (op == CFGZIP_HEAD_STEP) {
-        s.mask = c.take<uint32_t>(int64_t(rows) * ceil_div(h->V, 32));
+        s.z = c.take<float>(n * kPiece);
+        s.state = c.take<RowState>(n);
+        s.mask = c.take<uint32_t>(n * ceil_div(h->V, 32));
         if (h->dtype == CFGZIP_MXFP4) s.weights = c.take<uint16_t>(int64_t(kPiece) * h->H);
+    } else if (op == CFGZIP_HEAD_LOSS) {
+        s.part = c.take<float2>(n * ceil_div(h->V, kMmaTile));
+        s.of_target = c.take<float>(n);
+    } else {
+        const int64_t most = kPieceBytes / 2 / std::max<int64_t>(n, 1) / kMmaTile * kMmaTile;
+        s.piece = int32_t(std::min<int64_t>(up(h->V, kMmaTile), std::max<int64_t>(most, kMmaTile)));
+        const int64_t tiles = int64_t(ceil_div(n, kMmaTile)) * ceil_div(h->H, kMmaTile);
+        s.splits = cuts(tiles, s.piece / kMmaK, n * h->H);
+        s.g = c.take<uint16_t>(n * s.piece);
+        s.sums = c.take<float>(n * h->H * s.splits);
     }
     s.bytes = c.used + 256;
     return s;
+}
+
+// Tiled copies of a bf16 matrix of `rows` rows of `cols`, boxes of 64 columns by `box` rows in the 128-byte swizzle.
+int tensor_map(cfgzip_ctx* ctx, CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t stride, int box) {
+    const cuuint64_t dims[2] = {cuuint64_t(cols), cuuint64_t(rows)};
+    const cuuint64_t strides[1] = {cuuint64_t(stride) * 2};
+    const cuuint32_t boxes[2] = {64, cuuint32_t(box)};
+    const cuuint32_t steps[2] = {1, 1};
+    if (!ctx->encode_tiled ||
+        ctx->encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, boxes, steps,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return CFGZIP_E_CUDA;
+    return CFGZIP_OK;
+}
+
+template <bool A_MN, bool B_MN, int KIND>
+int run_mma(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUtensorMap& map_b, cudaStream_t st) {
+    a.m_tiles = ceil_div(a.rows, kMmaTile);
+    a.n_tiles = ceil_div(a.cols, kMmaTile);
+    a.splits = std::max(1, a.splits);
+    a.status = ctx->d_status;
+    auto kern = k_head_mma<A_MN, B_MN, KIND>;
+    const int rc = ensure_smem(ctx, kern, kMmaSmem);
+    if (rc != CFGZIP_OK) return rc;
+    const int64_t tiles = int64_t(a.m_tiles) * a.n_tiles * a.splits;
+    if (tiles >= (int64_t(1) << 30)) return CFGZIP_E_RANGE;
+    const unsigned pairs = unsigned(std::min<int64_t>(tiles, ctx->sm_count / 2));
+    return launch(ctx, kern, dim3(2 * pairs), dim3(kMmaThreads), kMmaSmem, st, a, map_a, map_b);
 }
 
 int product(cfgzip_ctx* ctx, const ProductArgs& p, cudaStream_t st) {
@@ -221,24 +285,34 @@ int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidde
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    RowsArgs a{};
-    a.z = w.z;
-    a.ldz = kPiece;
+    CUtensorMap map_x, map_w;
+    if ((rc = tensor_map(ctx, &map_x, hidden, N, head->H, hidden_stride, 128)) != CFGZIP_OK ||
+        (rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, 128)) != CFGZIP_OK)
+        return rc;
+    MmaArgs a{};
     a.rows = N;
-    a.V = head->V;
+    a.cols = a.V = head->V;
+    a.k_blocks = ceil_div(head->H, kMmaK);
+    a.m_fast = 1;
     a.mask = vocab_mask;
     a.mask_stride = vocab_stride_words;
-    a.state = w.state;
     a.targets = targets;
-    a.lse = lse;
-    a.loss = loss;
-    a.status = ctx->d_status;
-    for (a.t0 = 0; a.t0 < a.V; a.t0 += kPiece) {
-        a.n = std::min(kPiece, a.V - a.t0);
-        if ((rc = scores(ctx, head, w, hidden, hidden_stride, N, a.t0, a.n, st)) != CFGZIP_OK) return rc;
-        if ((rc = launch(ctx, k_head_rows, dim3(unsigned(N)), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
-    }
-    return launch(ctx, k_head_finish, dim3(unsigned(ceil_div(N, 256))), dim3(256), 0, st, a);
+    a.part = w.part;
+    a.of_target = w.of_target;
+    if ((rc = run_mma<false, false, kMmaLoss>(ctx, a, map_x, map_w, st)) != CFGZIP_OK) return rc;
+    FinishArgs f{};
+    f.part = w.part;
+    f.of_target = w.of_target;
+    f.tiles = a.n_tiles;
+    f.rows = N;
+    f.V = head->V;
+    f.mask = vocab_mask;
+    f.mask_stride = vocab_stride_words;
+    f.targets = targets;
+    f.loss = loss;
+    f.lse = lse;
+    f.status = ctx->d_status;
+    return launch(ctx, k_head_loss_finish, dim3(unsigned(ceil_div(N, 32))), dim3(256), 0, st, f);
 }
 
 int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N,
@@ -264,7 +338,6 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const uint16_t* x = static_cast<const uint16_t*>(hidden);
     const int H = head->H;
     if (N == 0) {  // an empty sum
         if (!d_weight || accumulate) return CFGZIP_OK;
@@ -275,35 +348,63 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
         }
         return CFGZIP_OK;
     }
-    RowsArgs a{};
-    a.z = w.z;
-    a.ldz = kPiece;
-    a.rows = N;
-    a.V = head->V;
-    a.mask = vocab_mask;
-    a.mask_stride = vocab_stride_words;
-    a.targets = targets;
-    a.lse_in = lse;
-    a.d_loss = d_loss;
-    a.g = w.g;
-    for (a.t0 = 0; a.t0 < a.V; a.t0 += kPiece) {
-        a.n = std::min(kPiece, a.V - a.t0);
-        if ((rc = scores(ctx, head, w, hidden, hidden_stride, N, a.t0, a.n, st)) != CFGZIP_OK) return rc;
-        if ((rc = launch(ctx, k_head_gradient, dim3(unsigned(N)), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
-        const uint16_t* weights = static_cast<const uint16_t*>(head->weight) + a.t0 * head->row_stride;
-        if (d_hidden && (rc = product(ctx, ProductArgs{w.g, weights, kPiece, 1, 1, head->row_stride, w.d_hidden, H, N, H, a.n, 0, a.t0 > 0},
-                                      st)) != CFGZIP_OK)
+    CUtensorMap x_k, x_mn, w_k, w_mn, g_k, g_mn;
+    if ((rc = tensor_map(ctx, &x_k, hidden, N, H, hidden_stride, 128)) != CFGZIP_OK ||
+        (rc = tensor_map(ctx, &x_mn, hidden, N, H, hidden_stride, 64)) != CFGZIP_OK)
+        return rc;
+    for (int32_t t0 = 0; t0 < head->V; t0 += w.piece) {
+        const int32_t n = std::min(w.piece, head->V - t0);
+        const uint16_t* weights = static_cast<const uint16_t*>(head->weight) + t0 * head->row_stride;
+        // (columns of the piece behind the vocabulary are outside the maps: they come as zeros)
+        if ((rc = tensor_map(ctx, &w_k, weights, n, H, head->row_stride, 128)) != CFGZIP_OK ||
+            (rc = tensor_map(ctx, &w_mn, weights, n, H, head->row_stride, 64)) != CFGZIP_OK ||
+            (rc = tensor_map(ctx, &g_k, w.g, N, n, w.piece, 128)) != CFGZIP_OK ||
+            (rc = tensor_map(ctx, &g_mn, w.g, N, n, w.piece, 64)) != CFGZIP_OK)
             return rc;
+        MmaArgs a{};
+        a.rows = N;
+        a.cols = n;
+        a.k_blocks = ceil_div(H, kMmaK);
+        a.m_fast = 1;
+        a.t0 = t0;
+        a.V = head->V;
+        a.mask = vocab_mask;
+        a.mask_stride = vocab_stride_words;
+        a.targets = targets;
+        a.lse = lse;
+        a.d_loss = d_loss;
+        a.out = w.g;
+        a.ld = w.piece;
+        if ((rc = run_mma<false, false, kMmaGrad>(ctx, a, x_k, w_k, st)) != CFGZIP_OK) return rc;
+        if (d_hidden) {
+            MmaArgs b{};
+            b.rows = N;
+            b.cols = H;
+            b.k_blocks = ceil_div(n, kMmaK);
+            b.splits = std::min(w.splits, b.k_blocks);
+            b.out = w.sums;
+            b.ld = H;
+            b.split_elems = int64_t(N) * H;
+            b.add = t0 > 0;
+            if ((rc = run_mma<false, true, kMmaSum>(ctx, b, g_k, w_mn, st)) != CFGZIP_OK) return rc;
+        }
         if (d_weight) {
-            const size_t es = d_weight_dtype == CFGZIP_BF16 ? 2 : 4;
-            void* out = static_cast<char*>(d_weight) + size_t(a.t0) * size_t(d_weight_stride) * es;
-            if ((rc = product(ctx, ProductArgs{w.g, x, 1, kPiece, 1, hidden_stride, out, d_weight_stride, a.n, H, N,
-                                               d_weight_dtype == CFGZIP_BF16, accumulate}, st)) != CFGZIP_OK)
-                return rc;
+            MmaArgs b{};
+            b.rows = n;
+            b.cols = H;
+            b.k_blocks = ceil_div(N, kMmaK);
+            b.ld = d_weight_stride;
+            b.add = accumulate;
+            const bool half = d_weight_dtype == CFGZIP_BF16;
+            b.out = static_cast<char*>(d_weight) + int64_t(t0) * d_weight_stride * (half ? 2 : 4);
+            rc = half ? run_mma<true, true, kMmaBf16>(ctx, b, g_mn, x_mn, st) : run_mma<true, true, kMmaSum>(ctx, b, g_mn, x_mn, st);
+            if (rc != CFGZIP_OK) return rc;
         }
     }
     if (!d_hidden) return CFGZIP_OK;
-    return launch(ctx, k_head_round, dim3(unsigned(ctx->sm_count) * 8), dim3(256), 0, st, (const float*)w.d_hidden,
+    const int splits = std::min(w.splits, ceil_div(std::min(w.piece, head->V), kMmaK));
+    const int64_t blocks = std::min<int64_t>(ceil_div(int64_t(N) * (H / 8), 256), int64_t(ctx->sm_count) * 8);
+    return launch(ctx, k_head_round, dim3(unsigned(blocks)), dim3(256), 0, st, (const float*)w.sums, int64_t(N) * H, splits,
                   static_cast<uint16_t*>(d_hidden), d_hidden_stride, int(N), H);
 }
 

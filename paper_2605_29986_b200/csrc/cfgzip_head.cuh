@@ -1,12 +1,10 @@
 // The product of hidden states with a head, and what is taken from it: normaliser, greedy choice, loss, gradient.
 #pragma once
 
-#include "cfgzip_device.cuh"
-#include "cfgzip_mx.cuh"
+#include "cfgzip_head_mma.cuh"
 
 namespace cfgzip {
 
-__device__ __forceinline__ float bf16_f32(uint16_t v) { return __uint_as_float(uint32_t(v) << 16); }
 __device__ __forceinline__ uint16_t f32_bf16(float v) {  // nearest, ties to even
     uint16_t r;
     asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(r) : "f"(v));
@@ -155,24 +153,24 @@ __global__ void __launch_bounds__(256) k_head_finish(const RowsArgs a) {
     }
 }
 
-// g of a piece, bf16.
-__global__ void __launch_bounds__(256) k_head_gradient(const RowsArgs a) {
+// The sums of `splits` cuts, added up and rounded; eight to a thread, n a multiple of 8.
+__global__ void __launch_bounds__(256) k_head_round(const float* from, int64_t split_elems, int splits, uint16_t* to, int64_t to_stride,
+                                                    int rows, int n) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int row = blockIdx.x, target = a.targets[row];
-    const float lse = a.lse_in[row], d = a.d_loss[row];
-    const bool has = target >= 0 && target < a.V && lse > -INFINITY && allowed(a, row, target);
-    for (int i = threadIdx.x; i < a.n; i += 256) {
-        const int t = a.t0 + i;
-        float g = 0.f;
-        if (has && allowed(a, row, t)) g = d * (ex2f((a.z[row * a.ldz + i] - lse) * kLog2e) - (t == target ? 1.f : 0.f));
-        a.g[row * a.ldz + i] = f32_bf16(g);
+    const int vectors = n / 8;
+    const int64_t total = int64_t(rows) * vectors;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
+        float f[8] = {};
+        for (int s = 0; s < splits; ++s) {
+            const float4* p = reinterpret_cast<const float4*>(from + s * split_elems + 8 * i);
+            const float4 x = __ldcg(p), y = __ldcg(p + 1);
+            f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
+            f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+        }
+        const MxAt at = mx_at(i, vectors);
+        *reinterpret_cast<uint4*>(to + at.row * to_stride + 8 * at.col) =
+            make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
     }
-}
-
-__global__ void __launch_bounds__(256) k_head_round(const float* from, uint16_t* to, int64_t to_stride, int rows, int n) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < int64_t(rows) * n; i += int64_t(gridDim.x) * 256)
-        to[(i / n) * to_stride + i % n] = f32_bf16(from[i]);
 }
 
 }  // namespace cfgzip

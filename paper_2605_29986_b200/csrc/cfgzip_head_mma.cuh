@@ -1,0 +1,389 @@
+// Products of tall matrices for the head: scores of the loss and its gradient, and the two products of the gradient.
+#pragma once
+
+#include <cuda.h>
+
+#include "cfgzip_mma.cuh"
+#include "cfgzip_mx.cuh"
+
+namespace cfgzip {
+
+__device__ __forceinline__ float bf16_f32(uint16_t v) { return __uint_as_float(uint32_t(v) << 16); }
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {  // nearest, ties to even
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+constexpr int kMmaThreads = 384;   // a warp for the copies, one for the products, two idle, two sets of four that read the sums
+constexpr int kMmaStages = 6;
+constexpr int kMmaTile = 256;      // rows and columns of a pair's tile
+constexpr int kMmaK = 64;          // k of a stage
+constexpr uint32_t kMmaHalf = 128 * kMmaK * 2;           // bytes of one operand of a stage in one block
+constexpr size_t kMmaSmem = size_t(kMmaStages) * 2 * kMmaHalf + 1024;
+
+enum : int { kMmaLoss = 0, kMmaGrad = 1, kMmaSum = 2, kMmaBf16 = 3 };
+
+struct MmaArgs {
+    int32_t rows, cols;        // of the result (tokens x piece of the vocabulary, ...)
+    int32_t m_tiles, n_tiles;
+    int32_t k_blocks, splits;  // the k range is cut in `splits`, each with a result of its own
+    int32_t m_fast;            // neighbouring tiles go along m
+    int32_t* status;
+    // scores
+    const uint32_t* mask;
+    int64_t mask_stride;
+    int32_t t0, V;             // the piece starts at token t0
+    const int32_t* targets;
+    const float *lse, *d_loss;
+    float2* part;              // loss: [n_tiles, rows] largest score and sum
+    float* of_target;          // loss: [rows]
+    // results
+    void* out;
+    int64_t ld;                // elements
+    int64_t split_elems;
+    int32_t add;
+};
+
+__device__ __forceinline__ void st_global32(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+                 "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
+struct MmaTile {
+    int m, n, split, k0, k1;
+};
+__device__ __forceinline__ MmaTile mma_tile(const MmaArgs& a, int i) {
+    const int per = a.m_tiles * a.n_tiles, split = i / per, r = i - split * per;
+    MmaTile t;
+    t.m = a.m_fast ? r % a.m_tiles : r / a.n_tiles;
+    t.n = a.m_fast ? r / a.m_tiles : r % a.n_tiles;
+    t.split = split;
+    t.k0 = int(int64_t(a.k_blocks) * split / a.splits);
+    t.k1 = int(int64_t(a.k_blocks) * (split + 1) / a.splits);
+    return t;
+}
+
+// What a row allows of the 256 tokens from column n0 of the piece on, 32 to a word.
+__device__ __forceinline__ void tile_mask(const MmaArgs& a, int row, int n0, uint32_t (&bits)[8]) {
+    const int t = a.t0 + n0, left = min(a.cols - n0, kMmaTile);
+    const uint32_t* p = a.mask + (a.mask ? int64_t(row) * a.mask_stride + (t >> 5) : 0);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const int n = left - 32 * c;
+        uint32_t w = 0;
+        if (n > 0) w = (a.mask ? ld_after_wait(p + c) : 0xFFFFFFFFu) & (n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u);
+        bits[c] = w;
+    }
+}
+
+// Largest allowed score and the sum of exponentials, of one row and 256 tokens.
+__device__ __forceinline__ void loss_epilogue(const MmaArgs& a, const MmaTile& t, int row, uint32_t tmem, bool valid,
+                                              const uint32_t (&bits)[8]) {
+    float m = -INFINITY, s = 0.f;
+    const int n0 = t.n * kMmaTile;
+    const int asked = valid ? ld_after_wait(a.targets + row) : -1, target = asked < 0 ? -1 : asked - (a.t0 + n0);
+#pragma unroll 1
+    for (int c = 0; c < 8; ++c) {
+        uint32_t v[32];
+        tmem_ld32(tmem + 32 * c, v);
+        tmem_wait_ld();
+        if (__any_sync(0xFFFFFFFFu, (target >> 5) == c)) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (target == 32 * c + j) a.of_target[row] = __uint_as_float(v[j]);
+        }
+        uint32_t w = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w = k == c ? bits[k] : w;
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            v[j] = (w >> j) & 1u ? v[j] : 0xFF800000u;
+            top = fmaxf(top, __uint_as_float(v[j]));
+        }
+        const float next = fmaxf(m, top), ref = fmaxf(next, kRefFloor);
+        s *= ex2f((fmaxf(m, kRefFloor) - ref) * kLog2e);
+        m = next;
+        float s1 = 0.f;
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            s += ex2f((__uint_as_float(v[j]) - ref) * kLog2e);
+            s1 += ex2f((__uint_as_float(v[j + 1]) - ref) * kLog2e);
+        }
+        s += s1;
+    }
+    if (valid) a.part[int64_t(t.n) * a.rows + row] = make_float2(m, s);
+}
+
+// g = d (exp(z - lse) - [target]) of the allowed tokens, as bf16.
+__device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t, int row, uint32_t tmem, bool valid,
+                                              const uint32_t (&bits)[8]) {
+    const int n0 = t.n * kMmaTile;
+    int target = -1;
+    float d = 0.f, lse = 0.f;
+    bool has = false;
+    if (valid) {
+        target = ld_after_wait(a.targets + row);
+        lse = ld_after_wait(a.lse + row);
+        has = target >= 0 && target < a.V && lse > -INFINITY;
+        if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (target >> 5)) >> (target & 31)) & 1u;
+        if (has) d = ld_after_wait(a.d_loss + row);
+        target = has ? target - (a.t0 + n0) : -1;
+    }
+#pragma unroll 1
+    for (int c = 0; c < 8; ++c) {
+        uint32_t v[32];
+        tmem_ld32(tmem + 32 * c, v);
+        tmem_wait_ld();
+        uint32_t w = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w = k == c ? bits[k] : w;
+        if (!has) w = 0;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const float p = ex2f((__uint_as_float(v[j]) - lse) * kLog2e);
+            v[j] = __float_as_uint((w >> j) & 1u ? d * p : 0.f);
+        }
+        if (__any_sync(0xFFFFFFFFu, (target >> 5) == c)) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (has && target == 32 * c + j) v[j] = __float_as_uint(__uint_as_float(v[j]) - d);
+        }
+        if (valid) {
+            uint16_t* p = static_cast<uint16_t*>(a.out) + int64_t(row) * a.ld + n0 + 32 * c;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t o[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = bf16_pair(__uint_as_float(v[16 * h + 2 * j]), __uint_as_float(v[16 * h + 2 * j + 1]));
+                st_global32(p + 16 * h, o);
+            }
+        }
+    }
+}
+
+// Sums as they are (f32), or rounded to bf16; added to what is there where asked for. Rows start on 16 bytes, columns come in
+// multiples of 8.
+template <bool BF16>
+__device__ __forceinline__ void out_epilogue(const MmaArgs& a, const MmaTile& t, int row, uint32_t tmem, bool valid) {
+    const int n0 = t.n * kMmaTile;
+    const int64_t at = t.split * a.split_elems + int64_t(row) * a.ld + n0;
+#pragma unroll 1
+    for (int c = 0; c < 8; ++c) {
+        if (n0 + 32 * c >= a.cols) break;
+        uint32_t v[32];
+        tmem_ld32(tmem + 32 * c, v);
+        tmem_wait_ld();
+        if (!valid) continue;
+#pragma unroll
+        for (int j = 0; j < 32; j += 8) {
+            if (n0 + 32 * c + j >= a.cols) break;
+            if (BF16) {
+                uint4* p = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at + 32 * c + j);
+                if (a.add) {
+                    const uint4 b = *p;
+                    const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        v[j + k] = __float_as_uint(__uint_as_float(v[j + k]) +
+                                                   __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16));
+                }
+                *p = make_uint4(bf16_pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])),
+                                bf16_pair(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])),
+                                bf16_pair(__uint_as_float(v[j + 4]), __uint_as_float(v[j + 5])),
+                                bf16_pair(__uint_as_float(v[j + 6]), __uint_as_float(v[j + 7])));
+            } else {
+                float4* p = reinterpret_cast<float4*>(static_cast<float*>(a.out) + at + 32 * c + j);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float4 o = make_float4(__uint_as_float(v[j + 4 * k]), __uint_as_float(v[j + 4 * k + 1]),
+                                           __uint_as_float(v[j + 4 * k + 2]), __uint_as_float(v[j + 4 * k + 3]));
+                    if (a.add) {
+                        const float4 b = p[k];
+                        o = make_float4(o.x + b.x, o.y + b.y, o.z + b.z, o.w + b.w);
+                    }
+                    p[k] = o;
+                }
+            }
+        }
+    }
+}
+
+// D[rows, cols] = A B^T in tiles of 256 x 256 by pairs of blocks (each holds 128 rows of A and of B, and the sums of its 128
+// rows), persistent. Operands K-major (k contiguous) or MN-major, from tensor maps with boxes of 64 x 128 or 64 x 64.
+template <bool A_MN, bool B_MN, int KIND>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
+    k_head_mma(const __grid_constant__ MmaArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
+    extern __shared__ char smem_raw[];
+    __shared__ __align__(8) uint64_t full[kMmaStages], empty[kMmaStages], sums_full[2], sums_empty[2];
+    __shared__ uint32_t s_tmem;
+    const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int tiles = a.m_tiles * a.n_tiles * a.splits, pairs = gridDim.x / 2, pair = blockIdx.x / 2;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kMmaStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sums_full[i], 1);
+            mbar_init(&sums_empty[i], 8);  // four warps of either block
+        }
+        mbar_init_fence();
+        prefetch_tensor_map(&map_a);
+        prefetch_tensor_map(&map_b);
+    }
+    if (warp == 2) tmem_alloc<2>(&s_tmem, 512);
+    tmem_fence_before();
+    __syncthreads();
+    cluster_barrier();
+    tmem_fence_after();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const uint32_t tmem = s_tmem;
+    bool ok = true;
+    if (warp == 0) {
+        if (lane == 0) {
+            Ring r;
+            for (int i = pair; i < tiles && ok; i += pairs) {
+                const MmaTile t = mma_tile(a, i);
+                const int m = t.m * kMmaTile + int(rank) * 128, n = t.n * kMmaTile + int(rank) * 128;
+                for (int k = t.k0; k < t.k1; ++k) {
+                    if (!mbar_wait_cluster(&empty[r.stage], r.phase ^ 1)) {
+                        ok = false;
+                        break;
+                    }
+                    if (rank == 0) mbar_expect_tx(&full[r.stage], 4 * kMmaHalf);
+                    const uint32_t bar = peer_shared(&full[r.stage], 0), at = stages + uint32_t(r.stage) * 2 * kMmaHalf;
+                    if (A_MN) {
+                        tma_load_pair(at, &map_a, m, k * kMmaK, bar);
+                        tma_load_pair(at + kMmaHalf / 2, &map_a, m + 64, k * kMmaK, bar);
+                    } else {
+                        tma_load_pair(at, &map_a, k * kMmaK, m, bar);
+                    }
+                    if (B_MN) {
+                        tma_load_pair(at + kMmaHalf, &map_b, n, k * kMmaK, bar);
+                        tma_load_pair(at + kMmaHalf + kMmaHalf / 2, &map_b, n + 64, k * kMmaK, bar);
+                    } else {
+                        tma_load_pair(at + kMmaHalf, &map_b, k * kMmaK, n, bar);
+                    }
+                    r.next<kMmaStages>();
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t idesc = kMmaBf16Desc<256, 256, A_MN, B_MN>;
+            Ring r;
+            int it = 0;
+            for (int i = pair; i < tiles && ok; i += pairs, ++it) {
+                const MmaTile t = mma_tile(a, i);
+                const uint32_t d = tmem + (it & 1) * 256;
+                if (!mbar_wait_cluster(&sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
+                    ok = false;
+                    break;
+                }
+                tmem_fence_after();
+                for (int k = t.k0; k < t.k1; ++k) {
+                    if (!mbar_wait_cluster(&full[r.stage], r.phase)) {
+                        ok = false;
+                        break;
+                    }
+                    tmem_fence_after();
+                    const uint32_t at = stages + uint32_t(r.stage) * 2 * kMmaHalf;
+                    const uint64_t da = mma_desc<A_MN>(at), db = mma_desc<B_MN>(at + kMmaHalf);
+#pragma unroll
+                    for (int j = 0; j < kMmaK / 16; ++j)
+                        mma_f16<2>(d, da + j * kDescStep16<A_MN>, db + j * kDescStep16<B_MN>, idesc, k > t.k0 || j > 0);
+                    mma_commit<2>(&empty[r.stage]);
+                    r.next<kMmaStages>();
+                }
+                mma_commit<2>(&sums_full[it & 1]);
+            }
+        }
+    } else if (warp >= 4) {
+        const int set = (warp - 4) >> 2, quad = warp & 3;
+        const uint32_t empty_bar = peer_shared(&sums_empty[set], 0);
+        int it = 0;
+        for (int i = pair; i < tiles; i += pairs, ++it) {
+            if ((it & 1) != set) continue;
+            const MmaTile t = mma_tile(a, i);
+            const int row = t.m * kMmaTile + int(rank) * 128 + quad * 32 + lane;
+            const bool valid = row < a.rows;
+            uint32_t bits[8];
+            if (KIND == kMmaLoss || KIND == kMmaGrad) tile_mask(a, valid ? row : a.rows - 1, t.n * kMmaTile, bits);
+            if (!mbar_wait_cluster(&sums_full[set], (it >> 1) & 1)) {
+                ok = false;
+                break;
+            }
+            tmem_fence_after();
+            const uint32_t d = tmem + set * 256 + (uint32_t(quad * 32) << 16);
+            if (KIND == kMmaLoss) loss_epilogue(a, t, row, d, valid, bits);
+            if (KIND == kMmaGrad) grad_epilogue(a, t, row, d, valid, bits);
+            if (KIND == kMmaSum) out_epilogue<false>(a, t, row, d, valid);
+            if (KIND == kMmaBf16) out_epilogue<true>(a, t, row, d, valid);
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at_peer(empty_bar);
+        }
+    }
+    if (!ok && lane == 0) atomicExch(a.status + 3, 1);
+    __syncwarp();
+    tmem_fence_before();
+    __syncthreads();
+    cluster_barrier();
+    tmem_fence_after();
+    if (warp == 2) tmem_free<2>(tmem, 512);
+}
+
+// Partial states of a row's tiles to its results: 32 rows by a block, a warp takes every eighth tile.
+struct FinishArgs {
+    const float2* part;
+    const float* of_target;
+    int32_t tiles, rows, V;
+    const uint32_t* mask;
+    int64_t mask_stride;
+    const int32_t* targets;
+    float *loss, *lse;
+    int32_t* status;
+};
+__global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
+    float m = -INFINITY, s = 0.f;
+    if (row < a.rows)
+#pragma unroll 4
+        for (int t = warp; t < a.tiles; t += 8) {
+            const float2 p = __ldcg(a.part + int64_t(t) * a.rows + row);
+            const float next = fmaxf(m, p.x), ref = fmaxf(next, kRefFloor);
+            s = s * ex2f((fmaxf(m, kRefFloor) - ref) * kLog2e) + p.y * ex2f((fmaxf(p.x, kRefFloor) - ref) * kLog2e);
+            m = next;
+        }
+    __shared__ float2 sh[8][32];
+    sh[warp][lane] = make_float2(m, s);
+    __syncthreads();
+    if (warp || row >= a.rows) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[w][lane].x);
+    const float ref = fmaxf(top, kRefFloor);
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s += sh[w][lane].y * ex2f((fmaxf(sh[w][lane].x, kRefFloor) - ref) * kLog2e);
+    const float log_sum = logf(s);
+    if (a.lse) a.lse[row] = s > 0.f ? top + log_sum : -INFINITY;
+    const int t = ld_after_wait(a.targets + row);
+    float loss = 0.f;
+    if (t >= a.V) atomicAdd(a.status + 1, 1);
+    if (t >= 0) {
+        bool has = t < a.V;
+        if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (t >> 5)) >> (t & 31)) & 1u;
+        const float z = has ? ld_after_wait(a.of_target + row) : -INFINITY;
+        loss = z > -INFINITY ? (top - z) + log_sum : INFINITY;
+    }
+    a.loss[row] = loss;
+}
+
+}  // namespace cfgzip
