@@ -7,6 +7,7 @@
 
 #include "cfgzip.h"
 #include "cfgzip_head.cuh"
+#include "cfgzip_head_step.cuh"
 #include "context.h"
 
 using namespace cfgzip;
@@ -56,6 +57,7 @@ struct Carve {
 };
 
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // most of the gradient of the scores that is held at a time
+constexpr int kStepBlocks = 148;                     // blocks of a decode step at most
 constexpr int kPairs = 74;                           // pairs of SMs that plans are made for (a plan is right for any number)
 
 struct HeadSpace {
@@ -63,7 +65,9 @@ struct HeadSpace {
     float* z;
     RowState* state;
     uint16_t* weights;
-    uint32_t* mask;
+    uint32_t *mask, *any, *ticket;
+    int32_t* counts;
+    Partial* states;
     // loss
     float2* part;
     float* of_target;
@@ -98,10 +102,16 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
     HeadSpace s{};
     const int64_t n = rows;
     if (op == CFGZIP_HEAD_STEP) {
-        s.z = c.take<float>(n * kPiece);
-        s.state = c.take<RowState>(n);
         s.mask = c.take<uint32_t>(n * ceil_div(h->V, 32));
-        if (h->dtype == CFGZIP_MXFP4) s.weights = c.take<uint16_t>(int64_t(kPiece) * h->H);
+        s.any = c.take<uint32_t>(ceil_div(h->V, 32));
+        s.counts = c.take<int32_t>(ceil_div(h->V, 32 * kUnionWords));
+        s.ticket = c.take<uint32_t>(1);
+        s.states = c.take<Partial>(std::min<int64_t>(n, kStepRows) * kStepBlocks);
+        if (h->dtype == CFGZIP_MXFP4) {
+            s.z = c.take<float>(n * kPiece);
+            s.state = c.take<RowState>(n);
+            s.weights = c.take<uint16_t>(int64_t(kPiece) * h->H);
+        }
     } else if (op == CFGZIP_HEAD_LOSS) {
         s.part = c.take<float2>(n * ceil_div(h->V, kMmaTile));
         s.of_target = c.take<float>(n);
@@ -170,6 +180,32 @@ int scores(cfgzip_ctx* ctx, const cfgzip_head* h, const HeadSpace& w, const void
     }
     return product(ctx, ProductArgs{static_cast<const uint16_t*>(hidden), weights, stride, 1, ld, 1, w.z, kPiece, rows, n, h->H, 0, 0},
                    st);
+}
+
+// One decode step of up to kStepRows rows whose vocab masks are there.
+int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const uint16_t* hidden, int64_t hidden_stride, cudaStream_t st) {
+    CUtensorMap map_w, map_x;
+    int rc;
+    a.N = up(a.B, 32);
+    if ((rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, 1)) != CFGZIP_OK ||
+        (rc = tensor_map(ctx, &map_x, hidden, a.B, head->H, hidden_stride, a.N)) != CFGZIP_OK)
+        return rc;
+    a.n_counts = ceil_div(a.VW, kUnionWords);
+    if ((rc = launch(ctx, k_head_union, dim3(unsigned(a.n_counts)), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
+    if (a.logits) {
+        const dim3 grid(unsigned(std::max(1, std::min(ceil_div(a.V, 8192), 64))), unsigned(a.B));
+        if ((rc = launch(ctx, a.logits_dtype == CFGZIP_BF16 ? k_head_fill<kBF16> : k_head_fill<kF32>, grid, dim3(256), 0, st, a)) !=
+            CFGZIP_OK)
+            return rc;
+    }
+    const unsigned blocks = unsigned(std::min(ctx->sm_count, kStepBlocks));
+    a.k_blocks = ceil_div(a.H, 64);
+    a.rounds = ceil_div(ceil_div(a.V, blocks), kStepShare);
+    const uint32_t stage = kStepTiles * kStepTileBytes + uint32_t(a.N) * 128u;
+    a.stages = std::min(kStepStages, int((200u << 10) / stage));
+    const size_t smem = size_t(a.stages) * stage + 1024;
+    if ((rc = ensure_smem(ctx, k_head_step, smem)) != CFGZIP_OK) return rc;
+    return launch(ctx, k_head_step, dim3(blocks), dim3(kStepThreads), smem, st, a, map_w, map_x);
 }
 
 }  // namespace
@@ -241,6 +277,36 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
     if ((rc = cfgzip_expand_mask(ctx, part0, row_part, class_mask, class_stride_words, mask, mask_stride, B, CFGZIP_DENSE, stream)) !=
         CFGZIP_OK)
         return rc;
+    if (head->dtype == CFGZIP_BF16) {
+        for (int32_t b = 0; b < B; b += kStepRows) {
+            HeadStepArgs s{};
+            s.parts = ctx->d_parts;
+            s.part0 = part0;
+            s.n_parts = int32_t(ctx->parts.size());
+            s.row_part = rows ? rows + b : nullptr;
+            s.mask = mask + b * mask_stride;
+            s.mask_stride = mask_stride;
+            s.B = std::min(kStepRows, B - b);
+            s.V = head->V;
+            s.VW = ps.VW;
+            s.H = head->H;
+            s.any = w.any;
+            s.counts = w.counts;
+            s.ticket = w.ticket;
+            s.part = w.states;
+            s.logits = logits ? static_cast<char*>(logits) + b * logits_stride * (logits_dtype == CFGZIP_BF16 ? 2 : 4) : nullptr;
+            s.logits_dtype = logits_dtype;
+            s.logits_stride = logits_stride;
+            s.argmax = argmax + b;
+            s.rep = rep ? rep + b : nullptr;
+            s.logp = logp_argmax ? logp_argmax + b : nullptr;
+            s.lse = lse ? lse + b : nullptr;
+            s.status = ctx->d_status;
+            if ((rc = run_step(ctx, s, head, static_cast<const uint16_t*>(hidden) + b * hidden_stride, hidden_stride, st)) != CFGZIP_OK)
+                return rc;
+        }
+        return CFGZIP_OK;
+    }
     RowsArgs a{};
     a.parts = ctx->d_parts;
     a.part0 = part0;
