@@ -184,12 +184,12 @@ int scores(cfgzip_ctx* ctx, const cfgzip_head* h, const HeadSpace& w, const void
 
 // One decode step of up to kStepRows rows whose vocab masks are there.
 int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const uint16_t* hidden, int64_t hidden_stride, cudaStream_t st) {
-    CUtensorMap map_w, map_x;
+    CUtensorMap map_x;
     int rc;
     a.N = up(a.B, 32);
-    if ((rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, 1)) != CFGZIP_OK ||
-        (rc = tensor_map(ctx, &map_x, hidden, a.B, head->H, hidden_stride, a.N)) != CFGZIP_OK)
-        return rc;
+    a.weight = head->weight;
+    a.row_bytes = head->row_stride * 2;
+    if ((rc = tensor_map(ctx, &map_x, hidden, a.B, head->H, hidden_stride, a.N)) != CFGZIP_OK) return rc;
     a.n_counts = ceil_div(a.VW, kUnionWords);
     if ((rc = launch(ctx, k_head_union, dim3(unsigned(a.n_counts)), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
     if (a.logits) {
@@ -205,7 +205,7 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
     a.stages = std::min(kStepStages, int((200u << 10) / stage));
     const size_t smem = size_t(a.stages) * stage + 1024;
     if ((rc = ensure_smem(ctx, k_head_step, smem)) != CFGZIP_OK) return rc;
-    return launch(ctx, k_head_step, dim3(blocks), dim3(kStepThreads), smem, st, a, map_w, map_x);
+    return launch(ctx, k_head_step, dim3(blocks), dim3(kStepThreads), smem, st, a, map_x);
 }
 
 }  // namespace

@@ -13,9 +13,11 @@ namespace cfgzip {
 constexpr int kUnionWords = 32;    // mask words (1024 tokens) counted together
 constexpr int kStepRows = 128;     // rows of the batch a launch takes at most
 constexpr int kStepShare = 2048;   // tokens a block lists at a time
-constexpr int kStepThreads = 256;  // copies, products, tensor memory, idle, and four warps that read the scores
+constexpr int kStepThreads = 384;  // copies of hidden states, products, tensor memory, idle, four warps that read the scores, and
+                                   // four that fetch the weights
 constexpr int kStepTiles = 2;      // tiles of 128 tokens that share a stage, and with it the hidden states in it
 constexpr int kStepStages = 8;     // most stages
+constexpr int kStepLag = 3;        // stages whose weights are on their way while the next one is asked for
 constexpr uint32_t kStepTileBytes = 128 * 64 * 2;
 
 struct HeadStepArgs {
@@ -25,6 +27,8 @@ struct HeadStepArgs {
     const uint32_t* mask;  // [B, mask_stride] vocab masks
     int64_t mask_stride;
     int32_t B, V, VW, H;
+    const void* weight;
+    int64_t row_bytes;
     int32_t N;             // columns of a tile: B rounded up to 32
     int32_t stages, k_blocks, rounds;
     uint32_t* any;         // [VW] union of the rows' masks
@@ -88,12 +92,12 @@ __global__ void __launch_bounds__(256) k_head_fill(const HeadStepArgs a) {
     }
 }
 
-__device__ __forceinline__ void tma_gather4(uint32_t dst_smem, const void* tensor_map, int x, int4 rows, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], "
-        "[%7];" ::"r"(dst_smem),
-        "l"(tensor_map), "r"(x), "r"(rows.x), "r"(rows.y), "r"(rows.z), "r"(rows.w), "r"(bar)
-        : "memory");
+// 16 bytes to shared memory past the L1, zeros where they lie behind the row
+__device__ __forceinline__ void copy16(uint32_t dst_smem, const void* src, bool have) {
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst_smem), "l"(src), "r"(have ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
 struct StepShared {
@@ -245,7 +249,7 @@ __device__ __forceinline__ void step_scores(const HeadStepArgs& a, uint32_t tmem
 }
 
 __global__ void __launch_bounds__(kStepThreads, 1)
-    k_head_step(const __grid_constant__ HeadStepArgs a, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x) {
+    k_head_step(const __grid_constant__ HeadStepArgs a, const __grid_constant__ CUtensorMap map_x) {
     extern __shared__ char smem_raw[];
     __shared__ __align__(16) StepShared sh;
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -254,7 +258,7 @@ __global__ void __launch_bounds__(kStepThreads, 1)
     const uint32_t columns = 2 * kStepTiles * a.N <= 128 ? 128 : 2 * kStepTiles * a.N <= 256 ? 256 : 512;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStepStages; ++i) {
-            mbar_init(&sh.full[i], 1);
+            mbar_init(&sh.full[i], 5);  // hidden states, and the four warps that fetch weights
             mbar_init(&sh.empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -262,7 +266,6 @@ __global__ void __launch_bounds__(kStepThreads, 1)
             mbar_init(&sh.sums_empty[i], 4);
         }
         mbar_init_fence();
-        prefetch_tensor_map(&map_w);
         prefetch_tensor_map(&map_x);
     }
     if (warp == 2) tmem_alloc<1>(&sh.tmem, columns);
@@ -286,43 +289,69 @@ __global__ void __launch_bounds__(kStepThreads, 1)
         const int n = step_share(a, sh, round * gridDim.x + blockIdx.x, a.rounds * gridDim.x);
         const int groups = (n + 128 * kStepTiles - 1) / (128 * kStepTiles);
         if (warp == 0) {
-            for (int g = 0; g < groups && ok; ++g) {
-                int4 rows[kStepTiles];
-                uint32_t bytes = uint32_t(a.N) * 128u;
-                int have[kStepTiles];
-#pragma unroll
-                for (int t = 0; t < kStepTiles; ++t) {
-                    have[t] = min(128, n - (g * kStepTiles + t) * 128);
-                    if (have[t] > 0) bytes += uint32_t((have[t] + 3) / 4) * 512u;
-                    const int at = (g * kStepTiles + t) * 128 + 4 * lane;
-                    // (the last four rows are filled up with the last one)
-                    rows[t] = make_int4(sh.list[min(at, n - 1)], sh.list[min(at + 1, n - 1)], sh.list[min(at + 2, n - 1)],
-                                        sh.list[min(at + 3, n - 1)]);
-                }
-                for (int k = 0; k < a.k_blocks; ++k) {
+            if (lane == 0)
+                for (int i = 0; i < groups * a.k_blocks; ++i) {
                     if (!mbar_wait(&sh.empty[stage], phase ^ 1)) {
                         ok = false;
                         break;
                     }
-                    const uint32_t at = stages + uint32_t(stage) * stage_bytes, bar = smem_u32(&sh.full[stage]);
-                    if (lane == 0) {
-                        mbar_expect_tx(&sh.full[stage], bytes);
-                        asm volatile(
-                            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
-                            "[%4];" ::"r"(at + x_at),
-                            "l"(&map_x), "r"(k * 64), "r"(0), "r"(bar)
-                            : "memory");
-                    }
-                    __syncwarp();
-#pragma unroll
-                    for (int t = 0; t < kStepTiles; ++t)
-                        if (4 * lane < have[t]) tma_gather4(at + t * kStepTileBytes + lane * 512, &map_w, k * 64, rows[t], bar);
+                    mbar_expect_tx(&sh.full[stage], uint32_t(a.N) * 128u);
+                    asm volatile(
+                        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
+                        "[%4];" ::"r"(stages + uint32_t(stage) * stage_bytes + x_at),
+                        "l"(&map_x), "r"(i % a.k_blocks * 64), "r"(0), "r"(smem_u32(&sh.full[stage]))
+                        : "memory");
                     if (++stage == a.stages) {
                         stage = 0;
                         phase ^= 1;
                     }
                 }
+        } else if (warp >= 8) {
+            // eight lanes bring the 128 bytes of a row, a warp four rows at a time
+            const int chunk = lane & 7;
+            int issued = 0, done = stage;
+            auto arrive = [&] {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.full[done]);
+                if (++done == a.stages) done = 0;
+            };
+            for (int g = 0; g < groups && ok; ++g) {
+                const char* from[kStepTiles][8];
+#pragma unroll
+                for (int t = 0; t < kStepTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int at = (g * kStepTiles + t) * 128 + (warp & 3) * 32 + 4 * i + (lane >> 3);
+                        from[t][i] = at < n ? static_cast<const char*>(a.weight) + int64_t(sh.list[at]) * a.row_bytes + chunk * 16 : nullptr;
+                    }
+                for (int k = 0; k < a.k_blocks; ++k) {
+                    if (!mbar_wait(&sh.empty[stage], phase ^ 1)) {
+                        ok = false;
+                        break;
+                    }
+                    const bool have = k * 64 + chunk * 8 < a.H;
+                    const uint32_t at = stages + uint32_t(stage) * stage_bytes + uint32_t((warp & 3) * 32 + (lane >> 3)) * 128u;
+#pragma unroll
+                    for (int t = 0; t < kStepTiles; ++t)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (from[t][i])
+                                copy16(at + t * kStepTileBytes + i * 512 + uint32_t((chunk ^ ((4 * i + (lane >> 3)) & 7)) << 4),
+                                       have ? from[t][i] + k * 128 : from[t][i] - chunk * 16, have);
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    if (++stage == a.stages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                    if (++issued > kStepLag) {
+                        asm volatile("cp.async.wait_group %0;" ::"n"(kStepLag) : "memory");
+                        arrive();
+                    }
+                }
             }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            for (int i = 0; i < min(issued, kStepLag); ++i) arrive();
         } else if (warp == 1) {
             if (lane == 0) {
                 const uint32_t idesc = kMmaBf16Desc<128, 0, false, false> | uint32_t(a.N / 8) << 17;
@@ -383,7 +412,7 @@ __global__ void __launch_bounds__(kStepThreads, 1)
                                     state, lane);
                 tmem_fence_before();
                 __syncwarp();
-                if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&sh.sums_empty[it & 1])) : "memory");
+                if (lane == 0) mbar_arrive(&sh.sums_empty[it & 1]);
             }
         }
         __syncwarp();
@@ -393,7 +422,7 @@ __global__ void __launch_bounds__(kStepThreads, 1)
     if (!ok && lane == 0) atomicExch(a.status + 3, 1);
     // the four warps' states to one, out to the others' and, in the last block to come here, to the results
     Partial* mine = reinterpret_cast<Partial*>(sh.entry);
-    if (warp >= 4) {
+    if (warp >= 4 && warp < 8) {
 #pragma unroll
         for (int c = 0; c < kStepRows / 32; ++c) mine[(warp & 3) * kStepRows + 32 * c + lane] = state[c];
     }
