@@ -6,7 +6,7 @@
 #include <cstdint>
 
 #include "cfgzip.h"
-#include "cfgzip_head.cuh"
+#include "cfgzip_head_mma.cuh"
 #include "cfgzip_head_step.cuh"
 #include "context.h"
 
@@ -15,7 +15,6 @@ using namespace cfgzip;
 namespace {
 
 constexpr int kHeadMost = 65536;  // longest row of a head
-constexpr int kPiece = 8192;      // tokens whose scores are held at a time
 
 bool on16(const void* p, int64_t stride_bytes) { return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(stride_bytes)) & 15u) == 0; }
 
@@ -62,9 +61,7 @@ constexpr int kPairs = 74;                           // pairs of SMs that plans 
 
 struct HeadSpace {
     // step
-    float* z;
-    RowState* state;
-    uint16_t* weights;
+    uint16_t* swapped;
     uint32_t *mask, *any, *ticket;
     int32_t* counts;
     Partial* states;
@@ -107,11 +104,7 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
         s.counts = c.take<int32_t>(ceil_div(h->V, 32 * kUnionWords));
         s.ticket = c.take<uint32_t>(1);
         s.states = c.take<Partial>(std::min<int64_t>(n, kStepRows) * kStepBlocks);
-        if (h->dtype == CFGZIP_MXFP4) {
-            s.z = c.take<float>(n * kPiece);
-            s.state = c.take<RowState>(n);
-            s.weights = c.take<uint16_t>(int64_t(kPiece) * h->H);
-        }
+        if (h->dtype == CFGZIP_MXFP4) s.swapped = c.take<uint16_t>(std::min<int64_t>(n, kStepRowsMx) * h->H);
     } else if (op == CFGZIP_HEAD_LOSS) {
         s.part = c.take<float2>(n * ceil_div(h->V, kMmaTile));
         s.of_target = c.take<float>(n);
@@ -156,10 +149,6 @@ int run_mma(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUtenso
     return launch(ctx, kern, dim3(2 * pairs), dim3(kMmaThreads), kMmaSmem, st, a, map_a, map_b);
 }
 
-int product(cfgzip_ctx* ctx, const ProductArgs& p, cudaStream_t st) {
-    return launch(ctx, k_head_product, dim3(unsigned(ceil_div(p.N, 64)), unsigned(ceil_div(p.M, 64))), dim3(256), 0, st, p);
-}
-
 int dequantize(cfgzip_ctx* ctx, const cfgzip_head* h, int32_t t0, int32_t n, uint16_t* values, int64_t stride, cudaStream_t st) {
     const int64_t total = int64_t(n) * (h->H / 8);
     return launch(ctx, k_mx_dequantize, dim3(unsigned(ceil_div(total, 256 * kMxUnroll))), dim3(256), 0, st,
@@ -167,29 +156,25 @@ int dequantize(cfgzip_ctx* ctx, const cfgzip_head* h, int32_t t0, int32_t n, uin
                   static_cast<const uint8_t*>(h->scales) + t0 * h->scale_stride, h->scale_stride, h->H / 8, total, values, stride);
 }
 
-// Scores of a piece of the vocabulary.
-int scores(cfgzip_ctx* ctx, const cfgzip_head* h, const HeadSpace& w, const void* hidden, int64_t stride, int32_t rows, int32_t t0,
-           int32_t n, cudaStream_t st) {
-    const uint16_t* weights = static_cast<const uint16_t*>(h->weight) + t0 * h->row_stride;
-    int64_t ld = h->row_stride;
-    if (h->dtype == CFGZIP_MXFP4) {
-        const int rc = dequantize(ctx, h, t0, n, w.weights, h->H, st);
-        if (rc != CFGZIP_OK) return rc;
-        weights = w.weights;
-        ld = h->H;
-    }
-    return product(ctx, ProductArgs{static_cast<const uint16_t*>(hidden), weights, stride, 1, ld, 1, w.z, kPiece, rows, n, h->H, 0, 0},
-                   st);
-}
-
-// One decode step of up to kStepRows rows whose vocab masks are there.
-int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const uint16_t* hidden, int64_t hidden_stride, cudaStream_t st) {
+// One decode step of up to kStepRows (kStepRowsMx) rows whose vocab masks are there.
+int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const uint16_t* hidden, int64_t hidden_stride,
+             uint16_t* swapped, cudaStream_t st) {
+    const bool mx = head->dtype == CFGZIP_MXFP4;
     CUtensorMap map_x;
     int rc;
     a.N = up(a.B, 32);
     a.weight = head->weight;
-    a.row_bytes = head->row_stride * 2;
-    if ((rc = tensor_map(ctx, &map_x, hidden, a.B, head->H, hidden_stride, a.N)) != CFGZIP_OK) return rc;
+    a.row_bytes = head->row_stride * (mx ? 1 : 2);
+    a.bytes = mx ? head->H / 2 : head->H * 2;
+    a.row_atoms = ceil_div(a.bytes, kStepAtom);
+    a.scales = static_cast<const uint8_t*>(head->scales);
+    a.scale_stride = head->scale_stride;
+    if (mx) {
+        a.hidden = hidden;
+        a.hidden_stride = hidden_stride;
+        a.swapped = swapped;
+    }
+    if ((rc = tensor_map(ctx, &map_x, mx ? swapped : hidden, a.B, head->H, mx ? head->H : hidden_stride, a.N)) != CFGZIP_OK) return rc;
     a.n_counts = ceil_div(a.VW, kUnionWords);
     if ((rc = launch(ctx, k_head_union, dim3(unsigned(a.n_counts)), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
     if (a.logits) {
@@ -199,13 +184,12 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
             return rc;
     }
     const unsigned blocks = unsigned(std::min(ctx->sm_count, kStepBlocks));
-    a.k_blocks = ceil_div(a.H, 64);
     a.rounds = ceil_div(ceil_div(a.V, blocks), kStepShare);
-    const uint32_t stage = kStepTiles * kStepTileBytes + uint32_t(a.N) * 128u;
-    a.stages = std::min(kStepStages, int((200u << 10) / stage));
-    const size_t smem = size_t(a.stages) * stage + 1024;
-    if ((rc = ensure_smem(ctx, k_head_step, smem)) != CFGZIP_OK) return rc;
-    return launch(ctx, k_head_step, dim3(blocks), dim3(kStepThreads), smem, st, a, map_x);
+    a.smem = 184 << 10;
+    const size_t smem = size_t(a.smem) + 1024 + kStepTile;  // (products read 128 rows, also where fewer are there)
+    auto kern = mx ? k_head_step<true> : k_head_step<false>;
+    if ((rc = ensure_smem(ctx, kern, smem)) != CFGZIP_OK) return rc;
+    return launch(ctx, kern, dim3(blocks), dim3((mx ? kStepWarpsMx : kStepWarps) * 32), smem, st, a, map_x);
 }
 
 }  // namespace
@@ -277,62 +261,35 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
     if ((rc = cfgzip_expand_mask(ctx, part0, row_part, class_mask, class_stride_words, mask, mask_stride, B, CFGZIP_DENSE, stream)) !=
         CFGZIP_OK)
         return rc;
-    if (head->dtype == CFGZIP_BF16) {
-        for (int32_t b = 0; b < B; b += kStepRows) {
-            HeadStepArgs s{};
-            s.parts = ctx->d_parts;
-            s.part0 = part0;
-            s.n_parts = int32_t(ctx->parts.size());
-            s.row_part = rows ? rows + b : nullptr;
-            s.mask = mask + b * mask_stride;
-            s.mask_stride = mask_stride;
-            s.B = std::min(kStepRows, B - b);
-            s.V = head->V;
-            s.VW = ps.VW;
-            s.H = head->H;
-            s.any = w.any;
-            s.counts = w.counts;
-            s.ticket = w.ticket;
-            s.part = w.states;
-            s.logits = logits ? static_cast<char*>(logits) + b * logits_stride * (logits_dtype == CFGZIP_BF16 ? 2 : 4) : nullptr;
-            s.logits_dtype = logits_dtype;
-            s.logits_stride = logits_stride;
-            s.argmax = argmax + b;
-            s.rep = rep ? rep + b : nullptr;
-            s.logp = logp_argmax ? logp_argmax + b : nullptr;
-            s.lse = lse ? lse + b : nullptr;
-            s.status = ctx->d_status;
-            if ((rc = run_step(ctx, s, head, static_cast<const uint16_t*>(hidden) + b * hidden_stride, hidden_stride, st)) != CFGZIP_OK)
-                return rc;
-        }
-        return CFGZIP_OK;
+    const int32_t most = head->dtype == CFGZIP_MXFP4 ? kStepRowsMx : kStepRows;
+    for (int32_t b = 0; b < B; b += most) {
+        HeadStepArgs s{};
+        s.parts = ctx->d_parts;
+        s.part0 = part0;
+        s.n_parts = int32_t(ctx->parts.size());
+        s.row_part = rows ? rows + b : nullptr;
+        s.mask = mask + b * mask_stride;
+        s.mask_stride = mask_stride;
+        s.B = std::min(most, B - b);
+        s.V = head->V;
+        s.VW = ps.VW;
+        s.H = head->H;
+        s.any = w.any;
+        s.counts = w.counts;
+        s.ticket = w.ticket;
+        s.part = w.states;
+        s.logits = logits ? static_cast<char*>(logits) + b * logits_stride * (logits_dtype == CFGZIP_BF16 ? 2 : 4) : nullptr;
+        s.logits_dtype = logits_dtype;
+        s.logits_stride = logits_stride;
+        s.argmax = argmax + b;
+        s.rep = rep ? rep + b : nullptr;
+        s.logp = logp_argmax ? logp_argmax + b : nullptr;
+        s.lse = lse ? lse + b : nullptr;
+        s.status = ctx->d_status;
+        rc = run_step(ctx, s, head, static_cast<const uint16_t*>(hidden) + b * hidden_stride, hidden_stride, w.swapped, st);
+        if (rc != CFGZIP_OK) return rc;
     }
-    RowsArgs a{};
-    a.parts = ctx->d_parts;
-    a.part0 = part0;
-    a.n_parts = int32_t(ctx->parts.size());
-    a.row_part = rows;
-    a.z = w.z;
-    a.ldz = kPiece;
-    a.rows = B;
-    a.V = head->V;
-    a.mask = mask;
-    a.mask_stride = mask_stride;
-    a.state = w.state;
-    a.logits = logits;
-    a.logits_dtype = logits_dtype;
-    a.logits_stride = logits_stride;
-    a.argmax = argmax;
-    a.rep = rep;
-    a.logp = logp_argmax;
-    a.lse = lse;
-    a.status = ctx->d_status;
-    for (a.t0 = 0; a.t0 < a.V; a.t0 += kPiece) {
-        a.n = std::min(kPiece, a.V - a.t0);
-        if ((rc = scores(ctx, head, w, hidden, hidden_stride, B, a.t0, a.n, st)) != CFGZIP_OK) return rc;
-        if ((rc = launch(ctx, k_head_rows, dim3(unsigned(B)), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
-    }
-    return launch(ctx, k_head_finish, dim3(unsigned(ceil_div(B, 256))), dim3(256), 0, st, a);
+    return CFGZIP_OK;
 }
 
 int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N,

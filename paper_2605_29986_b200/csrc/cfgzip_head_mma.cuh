@@ -87,6 +87,7 @@ __device__ __forceinline__ void loss_epilogue(const MmaArgs& a, const MmaTile& t
 #pragma unroll 1
     for (int c = 0; c < 8; ++c) {
         uint32_t v[32];
+        __syncwarp();
         tmem_ld32(tmem + 32 * c, v);
         tmem_wait_ld();
         if (__any_sync(0xFFFFFFFFu, (target >> 5) == c)) {
@@ -135,6 +136,7 @@ __device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t
 #pragma unroll 1
     for (int c = 0; c < 8; ++c) {
         uint32_t v[32];
+        __syncwarp();
         tmem_ld32(tmem + 32 * c, v);
         tmem_wait_ld();
         uint32_t w = 0;
@@ -174,6 +176,7 @@ __device__ __forceinline__ void out_epilogue(const MmaArgs& a, const MmaTile& t,
     for (int c = 0; c < 8; ++c) {
         if (n0 + 32 * c >= a.cols) break;
         uint32_t v[32];
+        __syncwarp();
         tmem_ld32(tmem + 32 * c, v);
         tmem_wait_ld();
         if (!valid) continue;
@@ -384,6 +387,26 @@ __global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
         loss = z > -INFINITY ? (top - z) + log_sum : INFINITY;
     }
     a.loss[row] = loss;
+}
+
+// The sums of `splits` cuts, added up and rounded; eight to a thread, n a multiple of 8.
+__global__ void __launch_bounds__(256) k_head_round(const float* from, int64_t split_elems, int splits, uint16_t* to, int64_t to_stride,
+                                                    int rows, int n) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int vectors = n / 8;
+    const int64_t total = int64_t(rows) * vectors;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
+        float f[8] = {};
+        for (int s = 0; s < splits; ++s) {
+            const float4* p = reinterpret_cast<const float4*>(from + s * split_elems + 8 * i);
+            const float4 x = __ldcg(p), y = __ldcg(p + 1);
+            f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
+            f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+        }
+        const MxAt at = mx_at(i, vectors);
+        *reinterpret_cast<uint4*>(to + at.row * to_stride + 8 * at.col) =
+            make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
+    }
 }
 
 }  // namespace cfgzip

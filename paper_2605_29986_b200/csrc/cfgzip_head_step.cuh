@@ -5,20 +5,20 @@
 
 #include <cuda.h>
 
-#include "cfgzip_mma.cuh"
-#include "cfgzip_mx.cuh"
+#include "cfgzip_head_mma.cuh"
 
 namespace cfgzip {
 
 constexpr int kUnionWords = 32;    // mask words (1024 tokens) counted together
 constexpr int kStepRows = 128;     // rows of the batch a launch takes at most
+constexpr int kStepRowsMx = 64;    // ... from a 4-bit head: the hidden states are brought past four times as many weights a byte
 constexpr int kStepShare = 2048;   // tokens a block lists at a time
-constexpr int kStepThreads = 384;  // copies of hidden states, products, tensor memory, idle, four warps that read the scores, and
-                                   // four that fetch the weights
-constexpr int kStepTiles = 2;      // tiles of 128 tokens that share a stage, and with it the hidden states in it
-constexpr int kStepStages = 8;     // most stages
-constexpr int kStepLag = 3;        // stages whose weights are on their way while the next one is asked for
-constexpr uint32_t kStepTileBytes = 128 * 64 * 2;
+constexpr int kStepWarps = 12;     // copies of hidden states, products, tensor memory, idle, four that read the scores, four that
+                                   // fetch weights
+constexpr int kStepWarpsMx = 20;   // ... and two sets of four that turn 4-bit weights into bf16
+constexpr int kStepStages = 12;    // most stages
+constexpr uint32_t kStepAtom = 128;             // bytes of a weight row in an atom, the width of the swizzle
+constexpr uint32_t kStepTile = 128 * kStepAtom; // an atom of 128 tokens
 
 struct HeadStepArgs {
     const PartDev* parts;
@@ -29,8 +29,16 @@ struct HeadStepArgs {
     int32_t B, V, VW, H;
     const void* weight;
     int64_t row_bytes;
+    const uint8_t* scales;
+    int64_t scale_stride;
     int32_t N;             // columns of a tile: B rounded up to 32
-    int32_t stages, k_blocks, rounds;
+    int32_t row_atoms;     // atoms of a row of weights
+    int32_t bytes;         // of a row of weights that count
+    int32_t smem;          // shared memory for stages
+    int32_t rounds;
+    const uint16_t* hidden;  // 4-bit heads: copied to `swapped` in the order in which their weights are taken apart
+    int64_t hidden_stride;
+    uint16_t* swapped;     // [B, H]
     uint32_t* any;         // [VW] union of the rows' masks
     int32_t* counts;       // tokens of it in every kUnionWords words
     int32_t n_counts;
@@ -57,6 +65,15 @@ __global__ void __launch_bounds__(256) k_head_union(const HeadStepArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, word = blockIdx.x * kUnionWords + lane;
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
+    if (a.swapped) {  // weights 0 to 7 of a word come out as 0 4 1 5 2 6 3 7
+        const int vectors = a.H / 8;
+        for (int i = blockIdx.x * 256 + threadIdx.x; i < a.B * vectors; i += gridDim.x * 256) {
+            const int row = i / vectors, col = i - row * vectors;
+            const uint4 v = ld_after_wait(reinterpret_cast<const uint4*>(a.hidden + row * a.hidden_stride) + col);
+            reinterpret_cast<uint4*>(a.swapped)[i] = make_uint4(prmt(v.x, v.z, 0x5410), prmt(v.x, v.z, 0x7632),
+                                                                prmt(v.y, v.w, 0x5410), prmt(v.y, v.w, 0x7632));
+        }
+    }
     uint32_t any = 0;
     if (word < a.VW)
 #pragma unroll 4
@@ -101,22 +118,27 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
 }
 
 struct StepShared {
-    uint64_t full[kStepStages], empty[kStepStages], sums_full[2], sums_empty[2];
+    uint64_t full[kStepStages], empty[kStepStages], sums_full[2], sums_empty[2], w_full[4], w_empty[4];
     uint32_t tmem;
     uint32_t valid[kStepRows / 32];  // rows that have a partition
     int32_t total, entries, is_last;
-    int32_t scan[kStepThreads / 32];
+    int32_t scan[kStepWarpsMx];
     int32_t list[kStepShare];        // the block's tokens, ascending
-    alignas(16) int2 entry[kStepShare + 1];      // counted pieces that hold some of them: number, tokens in front of it
+    union alignas(16) {
+        int2 entry[kStepShare + 1];  // counted pieces that hold some of them: number, tokens in front of it
+        float turn[4][32 * 33];      // scores on their way from a lane a token to a lane a row
+        Partial state[4][kStepRows];
+    };
 };
 
 // The block's share of the union: tokens number lo .. lo + n of it, to sh.list. All threads; ends with a barrier.
+template <int THREADS>
 __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh, int share, int shares) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) sh.total = sh.entries = 0;
     __syncthreads();
     int mine = 0;
-    for (int i = tid; i < a.n_counts; i += kStepThreads) mine += __ldcg(a.counts + i);
+    for (int i = tid; i < a.n_counts; i += THREADS) mine += __ldcg(a.counts + i);
     mine = __reduce_add_sync(0xFFFFFFFFu, mine);
     if (lane == 0 && mine) atomicAdd(&sh.total, mine);
     __syncthreads();
@@ -124,7 +146,7 @@ __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh,
     const int lo = int(int64_t(total) * share / shares), hi = int(int64_t(total) * (share + 1) / shares);
     if (lo < hi) {  // (the same for every thread)
         int front = 0;
-        for (int base = 0; base < a.n_counts; base += kStepThreads) {
+        for (int base = 0; base < a.n_counts; base += THREADS) {
             const int i = base + tid, n = i < a.n_counts ? __ldcg(a.counts + i) : 0;
             int sum = n;
 #pragma unroll
@@ -136,7 +158,7 @@ __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh,
             __syncthreads();
             int before = front + sum - n;
 #pragma unroll
-            for (int w = 0; w < kStepThreads / 32; ++w) {
+            for (int w = 0; w < THREADS / 32; ++w) {
                 const int o = sh.scan[w];
                 if (w < warp) before += o;
                 front += o;
@@ -144,7 +166,7 @@ __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh,
             if (n > 0 && before < hi && before + n > lo) sh.entry[atomicAdd(&sh.entries, 1)] = make_int2(i, before);
             __syncthreads();
         }
-        for (int e = warp; e < sh.entries; e += kStepThreads / 32) {
+        for (int e = warp; e < sh.entries; e += THREADS / 32) {
             const int2 en = sh.entry[e];
             const int word = en.x * kUnionWords + lane;
             uint32_t w = word < a.VW ? __ldcg(a.any + word) : 0u;
@@ -205,65 +227,133 @@ __device__ __forceinline__ void step_bits(const HeadStepArgs& a, const StepShare
     }
 }
 
-// The scores of 128 tokens under the rows of the batch: a lane has a token, a column is a row. Lane j of a warp keeps the state
-// of the rows 32 c + j over the warp's tokens.
-__device__ __forceinline__ void step_scores(const HeadStepArgs& a, uint32_t tmem, int token, const uint32_t (&bits)[kStepRows / 32],
-                                            Partial (&state)[kStepRows / 32], int lane) {
+// The scores of 128 tokens under the rows of the batch: a lane has a token, a column is a row; by way of shared memory a lane
+// has a row (32 c + lane) and the warp's 32 tokens, and keeps that row's state.
+__device__ __forceinline__ void step_scores(const HeadStepArgs& a, float* turn, const int32_t* list, uint32_t tmem, int token,
+                                            const uint32_t (&bits)[kStepRows / 32], Partial (&state)[kStepRows / 32], int lane) {
 #pragma unroll
     for (int c = 0; c < kStepRows / 32; ++c) {
         if (32 * c >= a.B) break;
         uint32_t v[32];
         tmem_ld32(tmem + 32 * c, v);
         tmem_wait_ld();
-        float m = -INFINITY, s = 0.f;
-        int pos = kNoPos;
+        if (a.logits) {
+            const int n = min(32, a.B - 32 * c);
+            if (a.logits_dtype == kBF16) {
+                uint16_t* p = static_cast<uint16_t*>(a.logits) + 32 * c * a.logits_stride + token;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const bool has = (bits[c] >> j) & 1u;
-            const uint32_t who = __ballot_sync(0xFFFFFFFFu, has);
-            if (!who) continue;
-            const float z = has ? __uint_as_float(v[j]) : -INFINITY;
-            const float top = redux_max(z);
-            float e = has ? ex2f((z - fmaxf(top, kRefFloor)) * kLog2e) : 0.f;
+                for (int j = 0; j < 32; ++j)
+                    if (j < n && ((bits[c] >> j) & 1u)) p[j * a.logits_stride] = uint16_t(bf16_pair(__uint_as_float(v[j]), 0.f));
+            } else {
+                float* p = static_cast<float*>(a.logits) + 32 * c * a.logits_stride + token;
 #pragma unroll
-            for (int d = 16; d >= 1; d >>= 1) e += __shfl_xor_sync(0xFFFFFFFFu, e, d);
-            const int first = __shfl_sync(0xFFFFFFFFu, token, __ffs(__ballot_sync(0xFFFFFFFFu, has && z == top)) - 1);
-            if (lane == j) {
-                m = top;
-                s = e;
-                pos = first;
-            }
-            if (a.logits && has) {
-                const int64_t at = (32 * c + j) * a.logits_stride + token;
-                if (a.logits_dtype == kBF16) {
-                    uint16_t r;
-                    asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(r) : "f"(z));
-                    static_cast<uint16_t*>(a.logits)[at] = r;
-                } else {
-                    static_cast<float*>(a.logits)[at] = z;
-                }
+                for (int j = 0; j < 32; ++j)
+                    if (j < n && ((bits[c] >> j) & 1u)) p[j * a.logits_stride] = __uint_as_float(v[j]);
             }
         }
-        partial_merge(state[c].m, state[c].s, state[c].pos, m, s, pos);
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) turn[j * 33 + lane] = (bits[c] >> j) & 1u ? __uint_as_float(v[j]) : -INFINITY;
+        const uint32_t has = warp_transpose32(bits[c], lane);
+        __syncwarp();
+        float m = -INFINITY;
+        int at = __ffs(has) - 1;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const float z = turn[lane * 33 + j];
+            v[j] = __float_as_uint(z);
+            at = z > m ? j : at;
+            m = fmaxf(m, z);
+        }
+        const float ref = fmaxf(m, kRefFloor);
+        float s[2] = {};
+#pragma unroll
+        for (int j = 0; j < 32; ++j) s[j & 1] += ex2f((__uint_as_float(v[j]) - ref) * kLog2e);
+        if (has) partial_merge(state[c].m, state[c].s, state[c].pos, m, s[0] + s[1], list[at]);
+        __syncwarp();
     }
 }
 
-__global__ void __launch_bounds__(kStepThreads, 1)
+// Four 4-bit blocks of 32 weights (16 bytes each) of a token to tensor memory as bf16: sign, exponent and fraction of a weight go
+// to the top bits of a bf16 number, 2^126 below their value, and two exact products bring them up. Weights i and i + 4 of a word
+// come out side by side.
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ void mx_word(uint32_t w, uint32_t scale, uint32_t (&out)[4]) {
+    const uint32_t up = 0x7E807E80u;  // 2^126
+    const uint32_t t[4] = {((w << 12) & 0x80008000u) | ((w << 6) & 0x01C001C0u), ((w << 8) & 0x80008000u) | ((w << 2) & 0x01C001C0u),
+                           ((w << 4) & 0x80008000u) | ((w >> 2) & 0x01C001C0u), (w & 0x80008000u) | ((w >> 6) & 0x01C001C0u)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = mul_bf16x2(mul_bf16x2(t[i], up), scale);
+}
+__device__ __forceinline__ uint32_t mx_scale_pair(uint32_t byte) {  // 2^(byte - 127) twice, as bf16
+    const uint32_t b = byte == 255u ? 0x7FC0u : byte ? byte << 7 : 0x0040u;
+    return b | b << 16;
+}
+__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]),
+        "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]),
+        "r"(v[31])
+        : "memory");
+}
+__device__ __forceinline__ void mma_f16_from_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
+        : "memory");
+}
+
+// How a block's stages are laid out: `tiles` tiles of 128 tokens side by side where it has more than 128, otherwise as many rows
+// as it has tokens (rounded up to 8) and so many more atoms of them. A product takes 128 rows all the same: what it reads behind
+// the rows that are there gives sums that nobody reads.
+struct StepLayout {
+    int tiles, rows, atoms, steps, stages;
+    uint32_t x_at, bytes;
+};
+template <bool MX>
+__device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int most) {
+    constexpr int X = MX ? 4 : 1;  // atoms of hidden states to an atom of weights
+    StepLayout l;
+    l.tiles = most > 128 ? 2 : 1;
+    l.rows = most > 128 ? 256 : (max(most, 1) + 7) & ~7;
+    l.atoms = 1;
+    while (l.atoms < 8 && l.atoms < a.row_atoms && 2 * l.atoms * (l.rows + X * a.N) * kStepAtom <= (24u << 10)) l.atoms *= 2;
+    l.steps = (a.row_atoms + l.atoms - 1) / l.atoms;
+    l.x_at = uint32_t(l.atoms) * l.rows * kStepAtom;
+    l.bytes = l.x_at + uint32_t(l.atoms) * X * a.N * kStepAtom;
+    l.stages = min(kStepStages, int(uint32_t(a.smem) / l.bytes));
+    return l;
+}
+
+template <bool MX>
+__global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     k_head_step(const __grid_constant__ HeadStepArgs a, const __grid_constant__ CUtensorMap map_x) {
+    constexpr int kThreads = (MX ? kStepWarpsMx : kStepWarps) * 32, X = MX ? 4 : 1;
     extern __shared__ char smem_raw[];
     __shared__ __align__(16) StepShared sh;
-    const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t x_at = kStepTiles * kStepTileBytes, stage_bytes = x_at + uint32_t(a.N) * 128u;
-    const uint32_t columns = 2 * kStepTiles * a.N <= 128 ? 128 : 2 * kStepTiles * a.N <= 256 ? 256 : 512;
+    const uint32_t columns = MX ? 512 : 4 * a.N <= 128 ? 128 : 4 * a.N <= 256 ? 256 : 512;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStepStages; ++i) {
-            mbar_init(&sh.full[i], 5);  // hidden states, and the four warps that fetch weights
-            mbar_init(&sh.empty[i], 1);
+            mbar_init(&sh.full[i], 1 + 128);        // hidden states, and every thread that fetches weights
+            mbar_init(&sh.empty[i], MX ? 1 + 8 : 1);  // the products, and the warps that take weights apart
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.sums_full[i], 1);
             mbar_init(&sh.sums_empty[i], 4);
+        }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&sh.w_full[i], 4);
+            mbar_init(&sh.w_empty[i], 1);
         }
         mbar_init_fence();
         prefetch_tensor_map(&map_x);
@@ -280,125 +370,203 @@ __global__ void __launch_bounds__(kStepThreads, 1)
     tmem_fence_after();
     const uint32_t tmem = sh.tmem;
     bool ok = true;
-    int stage = 0, group_at = 0;
-    uint32_t phase = 0;
+    int stage = 0, groups_done = 0;
+    uint32_t phase = 0, unit = 0;
     Partial state[kStepRows / 32];
 #pragma unroll
     for (int c = 0; c < kStepRows / 32; ++c) state[c] = partial_empty();
     for (int round = 0; round < a.rounds; ++round) {
-        const int n = step_share(a, sh, round * gridDim.x + blockIdx.x, a.rounds * gridDim.x);
-        const int groups = (n + 128 * kStepTiles - 1) / (128 * kStepTiles);
+        const int shares = a.rounds * gridDim.x;
+        const int n = step_share<kThreads>(a, sh, round * gridDim.x + blockIdx.x, shares);
+        const StepLayout l = step_layout<MX>(a, (sh.total + shares - 1) / shares);  // (the same in every round)
+        const int per_group = 128 * l.tiles, groups = (n + per_group - 1) / per_group;
+        auto next = [&] {
+            if (++stage == l.stages) {
+                stage = 0;
+                phase ^= 1;
+            }
+        };
         if (warp == 0) {
             if (lane == 0)
-                for (int i = 0; i < groups * a.k_blocks; ++i) {
+                for (int i = 0; i < groups * l.steps; ++i) {
+                    const int first = i % l.steps * l.atoms, atoms = min(l.atoms, a.row_atoms - first);
                     if (!mbar_wait(&sh.empty[stage], phase ^ 1)) {
                         ok = false;
                         break;
                     }
-                    mbar_expect_tx(&sh.full[stage], uint32_t(a.N) * 128u);
-                    asm volatile(
-                        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
-                        "[%4];" ::"r"(stages + uint32_t(stage) * stage_bytes + x_at),
-                        "l"(&map_x), "r"(i % a.k_blocks * 64), "r"(0), "r"(smem_u32(&sh.full[stage]))
-                        : "memory");
-                    if (++stage == a.stages) {
-                        stage = 0;
-                        phase ^= 1;
-                    }
+                    mbar_expect_tx(&sh.full[stage], uint32_t(atoms) * X * a.N * kStepAtom);
+                    for (int x = 0; x < atoms * X; ++x)
+                        asm volatile(
+                            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
+                            "[%4];" ::"r"(smem + uint32_t(stage) * l.bytes + l.x_at + uint32_t(x) * a.N * kStepAtom),
+                            "l"(&map_x), "r"((first * X + x) * 64), "r"(0), "r"(smem_u32(&sh.full[stage]))
+                            : "memory");
+                    next();
                 }
-        } else if (warp >= 8) {
-            // eight lanes bring the 128 bytes of a row, a warp four rows at a time
-            const int chunk = lane & 7;
-            int issued = 0, done = stage;
-            auto arrive = [&] {
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.full[done]);
-                if (++done == a.stages) done = 0;
-            };
-            for (int g = 0; g < groups && ok; ++g) {
-                const char* from[kStepTiles][8];
-#pragma unroll
-                for (int t = 0; t < kStepTiles; ++t)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int at = (g * kStepTiles + t) * 128 + (warp & 3) * 32 + 4 * i + (lane >> 3);
-                        from[t][i] = at < n ? static_cast<const char*>(a.weight) + int64_t(sh.list[at]) * a.row_bytes + chunk * 16 : nullptr;
-                    }
-                for (int k = 0; k < a.k_blocks; ++k) {
-                    if (!mbar_wait(&sh.empty[stage], phase ^ 1)) {
-                        ok = false;
-                        break;
-                    }
-                    const bool have = k * 64 + chunk * 8 < a.H;
-                    const uint32_t at = stages + uint32_t(stage) * stage_bytes + uint32_t((warp & 3) * 32 + (lane >> 3)) * 128u;
-#pragma unroll
-                    for (int t = 0; t < kStepTiles; ++t)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (from[t][i])
-                                copy16(at + t * kStepTileBytes + i * 512 + uint32_t((chunk ^ ((4 * i + (lane >> 3)) & 7)) << 4),
-                                       have ? from[t][i] + k * 128 : from[t][i] - chunk * 16, have);
-                    asm volatile("cp.async.commit_group;" ::: "memory");
-                    if (++stage == a.stages) {
-                        stage = 0;
-                        phase ^= 1;
-                    }
-                    if (++issued > kStepLag) {
-                        asm volatile("cp.async.wait_group %0;" ::"n"(kStepLag) : "memory");
-                        arrive();
-                    }
-                }
-            }
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            for (int i = 0; i < min(issued, kStepLag); ++i) arrive();
         } else if (warp == 1) {
             if (lane == 0) {
                 const uint32_t idesc = kMmaBf16Desc<128, 0, false, false> | uint32_t(a.N / 8) << 17;
                 for (int g = 0; g < groups && ok; ++g) {
-                    const int it = group_at + g;
+                    const int it = groups_done + g, tiles = min(l.tiles, (n - g * per_group + 127) / 128);
                     if (!mbar_wait(&sh.sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
                         ok = false;
                         break;
                     }
                     tmem_fence_after();
-                    const uint32_t d = tmem + uint32_t(it & 1) * kStepTiles * a.N;
-                    for (int k = 0; k < a.k_blocks; ++k) {
+                    const uint32_t d = tmem + uint32_t(it & 1) * l.tiles * a.N;
+                    for (int s = 0; s < l.steps && ok; ++s) {
                         if (!mbar_wait(&sh.full[stage], phase)) {
                             ok = false;
                             break;
                         }
+                        // (weights were written as ordinary shared memory: the products read it another way)
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         tmem_fence_after();
-                        const uint32_t at = stages + uint32_t(stage) * stage_bytes;
-                        const uint64_t dx = mma_desc<false>(at + x_at);
+                        const int atoms = min(l.atoms, a.row_atoms - s * l.atoms);
+                        const uint32_t w_at = smem + uint32_t(stage) * l.bytes, x_at = w_at + l.x_at;
+                        for (int p = 0; p < atoms; ++p)
+                            for (int t = 0; t < tiles; ++t) {
+                                const bool add = s > 0 || p > 0;
+                                if (MX) {
+                                    for (int h = 0; h < 2; ++h, ++unit) {
+                                        const int q = unit & 3;
+                                        if (ok && !mbar_wait(&sh.w_full[q], (unit >> 2) & 1)) ok = false;
+                                        tmem_fence_after();
+                                        const uint64_t dx = mma_desc<false>(x_at + uint32_t(p * 4 + 2 * h) * a.N * kStepAtom);
+                                        const uint64_t dx1 = mma_desc<false>(x_at + uint32_t(p * 4 + 2 * h + 1) * a.N * kStepAtom);
 #pragma unroll
-                        for (int t = 0; t < kStepTiles; ++t) {
-                            if ((g * kStepTiles + t) * 128 >= n) break;
-                            const uint64_t dw = mma_desc<false>(at + t * kStepTileBytes);
+                                        for (int j = 0; j < 8; ++j)
+                                            mma_f16_from_tmem(d + t * a.N, tmem + 256 + 64 * q + 8 * j,
+                                                              (j < 4 ? dx : dx1) + (j & 3) * kDescStep16<false>, idesc,
+                                                              add || h > 0 || j > 0);
+                                        mma_commit<1>(&sh.w_empty[q]);
+                                    }
+                                } else {
+                                    const uint64_t dw = mma_desc<false>(w_at + uint32_t(p) * l.rows * kStepAtom + t * kStepTile);
+                                    const uint64_t dx = mma_desc<false>(x_at + uint32_t(p) * a.N * kStepAtom);
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                mma_f16<1>(d + t * a.N, dw + j * kDescStep16<false>, dx + j * kDescStep16<false>, idesc, k > 0 || j > 0);
-                        }
+                                    for (int j = 0; j < 4; ++j)
+                                        mma_f16<1>(d + t * a.N, dw + j * kDescStep16<false>, dx + j * kDescStep16<false>, idesc,
+                                                   add || j > 0);
+                                }
+                            }
                         mma_commit<1>(&sh.empty[stage]);
-                        if (++stage == a.stages) {
-                            stage = 0;
-                            phase ^= 1;
-                        }
+                        next();
                     }
                     mma_commit<1>(&sh.sums_full[it & 1]);
                 }
             }
+        } else if (MX && warp >= 12) {
+            // a thread a token: set 0 takes the first half of an atom's 256 weights, set 1 the second
+            const int half = (warp - 12) >> 2, row = (warp & 3) * 32 + lane;
+            for (int g = 0; g < groups && ok; ++g) {
+                const int tiles = min(l.tiles, (n - g * per_group + 127) / 128);
+                const uint8_t* scales[2];
+                uint32_t scale[2], scale_next[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const int at = g * per_group + t * 128 + row;
+                    scales[t] = t < tiles && at < n ? a.scales + int64_t(sh.list[at]) * a.scale_stride + 4 * half : nullptr;
+                    scale_next[t] = scales[t] && 4 * half < a.bytes / 16 ? ld_after_wait(reinterpret_cast<const uint32_t*>(scales[t])) : 0;
+                }
+                for (int s = 0; s < l.steps && ok; ++s) {
+                    if (!mbar_wait(&sh.full[stage], phase)) {
+                        ok = false;
+                        break;
+                    }
+                    const int atoms = min(l.atoms, a.row_atoms - s * l.atoms);
+                    for (int p = 0; p < atoms; ++p) {
+                        const int atom = s * l.atoms + p, left = a.bytes / 16 - 8 * atom - 4 * half;  // blocks from here on
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            scale[t] = scale_next[t];
+                            if (scales[t] && left > 8)
+                                scale_next[t] = ld_after_wait(reinterpret_cast<const uint32_t*>(scales[t] + 8 * (atom + 1)));
+                        }
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            if (t >= tiles) break;
+                            const uint32_t q = (unit + half) & 3;
+                            if (!mbar_wait(&sh.w_empty[q], (((unit + half) >> 2) & 1) ^ 1)) ok = false;
+                            tmem_fence_after();
+                            const int r = t * 128 + row;
+                            const uint32_t at = smem + uint32_t(stage) * l.bytes + (uint32_t(p) * l.rows + min(r, l.rows - 1)) * kStepAtom;
+#pragma unroll
+                            for (int b = 0; b < 4; b += 2) {
+                                uint32_t v[32];
+#pragma unroll
+                                for (int k = 0; k < 2; ++k) {
+                                    uint32_t w[4];
+                                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                                                 : "r"(at + (uint32_t((4 * half + b + k) ^ (r & 7)) << 4)));
+                                    // (behind the row there is no scale, and the weights are zeros)
+                                    const uint32_t sc = mx_scale_pair(b + k < left ? (scale[t] >> (8 * (b + k))) & 255u : 127u);
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        uint32_t o[4];
+                                        mx_word(w[i], sc, o);
+#pragma unroll
+                                        for (int e = 0; e < 4; ++e) v[16 * k + 4 * i + e] = o[e];
+                                    }
+                                }
+                                tmem_st32(tmem + 256 + 64 * q + 16 * b + (uint32_t((warp & 3) * 32) << 16), v);
+                            }
+                            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                            tmem_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&sh.w_full[q]);
+                            unit += 2;
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.empty[stage]);
+                    next();
+                }
+            }
+        } else if (warp >= 8) {
+            // eight lanes bring the 128 bytes of a row's atom, the four warps 16 rows at a time
+            const int chunk = lane & 7, row = (warp & 3) * 4 + (lane >> 3);
+            for (int g = 0; g < groups && ok; ++g) {
+                const char* from[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int at = g * per_group + i * 16 + row;
+                    from[i] = at < n && i * 16 + row < l.rows
+                                  ? static_cast<const char*>(a.weight) + int64_t(sh.list[at]) * a.row_bytes + chunk * 16
+                                  : nullptr;
+                }
+                for (int s = 0; s < l.steps; ++s) {
+                    if (!mbar_wait(&sh.empty[stage], phase ^ 1)) {
+                        ok = false;
+                        break;
+                    }
+                    const int atoms = min(l.atoms, a.row_atoms - s * l.atoms);
+                    uint32_t to = smem + uint32_t(stage) * l.bytes + uint32_t(row) * kStepAtom + uint32_t((chunk ^ (row & 7)) << 4);
+                    for (int p = 0; p < atoms; ++p, to += uint32_t(l.rows) * kStepAtom) {
+                        const int off = (s * l.atoms + p) * int(kStepAtom);
+                        const bool have = off + chunk * 16 < a.bytes;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (from[i]) copy16(to + i * 16 * kStepAtom, have ? from[i] + off : from[i] - chunk * 16, have);
+                    }
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.full[stage])) : "memory");
+                    next();
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
         } else if (warp >= 4) {
             const int quad = warp & 3;
             for (int g = 0; g < groups; ++g) {
-                const int it = group_at + g;
-                int token[kStepTiles];
-                uint32_t bits[kStepTiles][kStepRows / 32];
+                const int it = groups_done + g;
+                uint32_t bits[2][kStepRows / 32];
+                int token[2];
 #pragma unroll
-                for (int t = 0; t < kStepTiles; ++t) {
-                    const int at = (g * kStepTiles + t) * 128 + quad * 32 + lane;
-                    token[t] = at < n ? sh.list[at] : 0;
-                    step_bits(a, sh, token[t], at < n, bits[t]);
+                for (int t = 0; t < 2; ++t) {
+                    const int at = g * per_group + t * 128 + quad * 32 + lane;
+                    const bool have = t < l.tiles && at < n;
+                    token[t] = have ? sh.list[at] : 0;
+                    step_bits(a, sh, token[t], have, bits[t]);
                 }
                 if (!mbar_wait(&sh.sums_full[it & 1], (it >> 1) & 1)) {
                     ok = false;
@@ -406,35 +574,36 @@ __global__ void __launch_bounds__(kStepThreads, 1)
                 }
                 tmem_fence_after();
 #pragma unroll
-                for (int t = 0; t < kStepTiles; ++t)
-                    if ((g * kStepTiles + t) * 128 < n)
-                        step_scores(a, tmem + (uint32_t(it & 1) * kStepTiles + t) * a.N + (uint32_t(quad * 32) << 16), token[t], bits[t],
-                                    state, lane);
+                for (int t = 0; t < 2; ++t) {
+                    const int at = g * per_group + t * 128 + quad * 32;
+                    if (t < l.tiles && at < n)
+                        step_scores(a, sh.turn[quad], sh.list + at, tmem + uint32_t((it & 1) * l.tiles + t) * a.N + (uint32_t(quad * 32) << 16),
+                                    token[t], bits[t], state, lane);
+                }
                 tmem_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.sums_empty[it & 1]);
             }
         }
         __syncwarp();
-        group_at += groups;
+        groups_done += groups;
         __syncthreads();
     }
     if (!ok && lane == 0) atomicExch(a.status + 3, 1);
     // the four warps' states to one, out to the others' and, in the last block to come here, to the results
-    Partial* mine = reinterpret_cast<Partial*>(sh.entry);
     if (warp >= 4 && warp < 8) {
 #pragma unroll
-        for (int c = 0; c < kStepRows / 32; ++c) mine[(warp & 3) * kStepRows + 32 * c + lane] = state[c];
+        for (int c = 0; c < kStepRows / 32; ++c) sh.state[warp & 3][32 * c + lane] = state[c];
     }
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
     if (warp == 2) tmem_free<1>(tmem, columns);
     if (int(threadIdx.x) < a.B) {
-        Partial p = mine[threadIdx.x];
+        Partial p = sh.state[0][threadIdx.x];
 #pragma unroll
         for (int q = 1; q < 4; ++q) {
-            const Partial o = mine[q * kStepRows + threadIdx.x];
+            const Partial o = sh.state[q][threadIdx.x];
             partial_merge(p.m, p.s, p.pos, o.m, o.s, o.pos);
         }
         __stcg(reinterpret_cast<int4*>(&a.part[blockIdx.x * a.B + threadIdx.x]),
@@ -446,7 +615,7 @@ __global__ void __launch_bounds__(kStepThreads, 1)
     __syncthreads();
     if (!sh.is_last) return;
     __threadfence();
-    for (int row = warp; row < a.B; row += kStepThreads / 32) step_finish_row(a, row, gridDim.x, lane);
+    for (int row = warp; row < a.B; row += kThreads / 32) step_finish_row(a, row, gridDim.x, lane);
 }
 
 }  // namespace cfgzip
