@@ -120,14 +120,14 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
     return s;
 }
 
-// Tiled copies of a bf16 matrix of `rows` rows of `cols`, boxes of 64 columns by `box` rows in the 128-byte swizzle.
-int tensor_map(cfgzip_ctx* ctx, CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t stride, int box) {
+// Tiled copies of a matrix of `rows` rows of `cols` bf16 numbers (or bytes), boxes of 128 bytes by `box` rows in the 128-byte swizzle.
+int tensor_map(cfgzip_ctx* ctx, CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t stride, int box, bool bytes = false) {
     const cuuint64_t dims[2] = {cuuint64_t(cols), cuuint64_t(rows)};
-    const cuuint64_t strides[1] = {cuuint64_t(stride) * 2};
-    const cuuint32_t boxes[2] = {64, cuuint32_t(box)};
+    const cuuint64_t strides[1] = {cuuint64_t(stride) * (bytes ? 1 : 2)};
+    const cuuint32_t boxes[2] = {bytes ? 128u : 64u, cuuint32_t(box)};
     const cuuint32_t steps[2] = {1, 1};
     if (!ctx->encode_tiled ||
-        ctx->encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, boxes, steps,
+        ctx->encode_tiled(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, boxes, steps,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return CFGZIP_E_CUDA;
@@ -160,7 +160,7 @@ int dequantize(cfgzip_ctx* ctx, const cfgzip_head* h, int32_t t0, int32_t n, uin
 int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const uint16_t* hidden, int64_t hidden_stride,
              uint16_t* swapped, cudaStream_t st) {
     const bool mx = head->dtype == CFGZIP_MXFP4;
-    CUtensorMap map_x;
+    CUtensorMap map_x, map_w;
     int rc;
     a.N = up(a.B, 32);
     a.weight = head->weight;
@@ -174,7 +174,9 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
         a.hidden_stride = hidden_stride;
         a.swapped = swapped;
     }
-    if ((rc = tensor_map(ctx, &map_x, mx ? swapped : hidden, a.B, head->H, mx ? head->H : hidden_stride, a.N)) != CFGZIP_OK) return rc;
+    if ((rc = tensor_map(ctx, &map_x, mx ? swapped : hidden, a.B, head->H, mx ? head->H : hidden_stride, a.N)) != CFGZIP_OK ||
+        (rc = tensor_map(ctx, &map_w, head->weight, head->V, mx ? a.bytes : head->H, head->row_stride, kStepBox, mx)) != CFGZIP_OK)
+        return rc;
     a.n_counts = ceil_div(a.VW, kUnionWords);
     if ((rc = launch(ctx, k_head_union, dim3(unsigned(a.n_counts)), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
     if (a.logits) {
@@ -189,7 +191,7 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
     const size_t smem = size_t(a.smem) + 1024 + kStepTile;  // (products read 128 rows, also where fewer are there)
     auto kern = mx ? k_head_step<true> : k_head_step<false>;
     if ((rc = ensure_smem(ctx, kern, smem)) != CFGZIP_OK) return rc;
-    return launch(ctx, kern, dim3(blocks), dim3((mx ? kStepWarpsMx : kStepWarps) * 32), smem, st, a, map_x);
+    return launch(ctx, kern, dim3(blocks), dim3((mx ? kStepWarpsMx : kStepWarps) * 32), smem, st, a, map_x, map_w);
 }
 
 }  // namespace

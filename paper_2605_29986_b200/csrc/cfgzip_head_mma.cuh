@@ -223,7 +223,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     __shared__ __align__(8) uint64_t full[kMmaStages], empty[kMmaStages], sums_full[2], sums_empty[2];
     __shared__ uint32_t s_tmem;
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const int tiles = a.m_tiles * a.n_tiles * a.splits, pairs = gridDim.x / 2, pair = blockIdx.x / 2;
     if (threadIdx.x == 0) {
@@ -277,7 +277,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             constexpr uint32_t idesc = kMmaBf16Desc<256, 256, A_MN, B_MN>;
             Ring r;
             int it = 0;
@@ -297,13 +297,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                     tmem_fence_after();
                     const uint32_t at = stages + uint32_t(r.stage) * 2 * kMmaHalf;
                     const uint64_t da = mma_desc<A_MN>(at), db = mma_desc<B_MN>(at + kMmaHalf);
+                    if (elect_one()) {
 #pragma unroll
-                    for (int j = 0; j < kMmaK / 16; ++j)
-                        mma_f16<2>(d, da + j * kDescStep16<A_MN>, db + j * kDescStep16<B_MN>, idesc, k > t.k0 || j > 0);
-                    mma_commit<2>(&empty[r.stage]);
+                        for (int j = 0; j < kMmaK / 16; ++j)
+                            mma_f16<2>(d, da + j * kDescStep16<A_MN>, db + j * kDescStep16<B_MN>, idesc, k > t.k0 || j > 0);
+                        mma_commit<2>(&empty[r.stage]);
+                    }
+                    __syncwarp();
                     r.next<kMmaStages>();
                 }
-                mma_commit<2>(&sums_full[it & 1]);
+                if (elect_one()) mma_commit<2>(&sums_full[it & 1]);
+                __syncwarp();
             }
         }
     } else if (warp >= 4) {

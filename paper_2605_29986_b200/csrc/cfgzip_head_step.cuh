@@ -13,9 +13,9 @@ constexpr int kUnionWords = 32;    // mask words (1024 tokens) counted together
 constexpr int kStepRows = 128;     // rows of the batch a launch takes at most
 constexpr int kStepRowsMx = 64;    // ... from a 4-bit head: the hidden states are brought past four times as many weights a byte
 constexpr int kStepShare = 2048;   // tokens a block lists at a time
-constexpr int kStepWarps = 12;     // copies of hidden states, products, tensor memory, idle, four that read the scores, four that
-                                   // fetch weights
-constexpr int kStepWarpsMx = 20;   // ... and two sets of four that turn 4-bit weights into bf16
+constexpr int kStepWarps = 16;     // tiled copies, products, tensor memory, idle, four that read the scores, eight that fetch weights
+constexpr int kStepWarpsMx = 24;   // ... and two sets of four that turn 4-bit weights into bf16
+constexpr int kStepBox = 32;       // rows of weights a tiled copy brings
 constexpr int kStepStages = 12;    // most stages
 constexpr uint32_t kStepAtom = 128;             // bytes of a weight row in an atom, the width of the swizzle
 constexpr uint32_t kStepTile = 128 * kStepAtom; // an atom of 128 tokens
@@ -113,6 +113,12 @@ __global__ void __launch_bounds__(256) k_head_fill(const HeadStepArgs a) {
 __device__ __forceinline__ void copy16(uint32_t dst_smem, const void* src, bool have) {
     asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst_smem), "l"(src), "r"(have ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void tma_load(uint32_t dst_smem, const void* tensor_map, int x, int y, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst_smem),
+        "l"(tensor_map), "r"(x), "r"(y), "r"(smem_u32(bar))
+        : "memory");
+}
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
@@ -122,6 +128,7 @@ struct StepShared {
     uint32_t tmem;
     uint32_t valid[kStepRows / 32];  // rows that have a partition
     int32_t total, entries, is_last;
+    int32_t first;                   // token number 0 of the share, where all tokens are taken
     int32_t scan[kStepWarpsMx];
     int32_t list[kStepShare];        // the block's tokens, ascending
     union alignas(16) {
@@ -130,6 +137,10 @@ struct StepShared {
         Partial state[4][kStepRows];
     };
 };
+
+// A union of at least three quarters of the vocabulary is taken for all of it: whole boxes of rows by tiled copies go at 93 % of
+// the memory's rate, rows one by one at 80 % (32 rows of 128256 x 4096).
+__device__ __forceinline__ bool step_takes_all(const HeadStepArgs& a, int total) { return int64_t(total) * 4 >= int64_t(a.V) * 3; }
 
 // The block's share of the union: tokens number lo .. lo + n of it, to sh.list. All threads; ends with a barrier.
 template <int THREADS>
@@ -142,9 +153,12 @@ __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh,
     mine = __reduce_add_sync(0xFFFFFFFFu, mine);
     if (lane == 0 && mine) atomicAdd(&sh.total, mine);
     __syncthreads();
-    const int total = sh.total;
+    const bool all = step_takes_all(a, sh.total);
+    const int total = all ? a.V : sh.total;
     const int lo = int(int64_t(total) * share / shares), hi = int(int64_t(total) * (share + 1) / shares);
-    if (lo < hi) {  // (the same for every thread)
+    if (all) {
+        for (int i = tid; i < hi - lo; i += THREADS) sh.list[i] = lo + i;
+    } else if (lo < hi) {  // (the same for every thread)
         int front = 0;
         for (int base = 0; base < a.n_counts; base += THREADS) {
             const int i = base + tid, n = i < a.n_counts ? __ldcg(a.counts + i) : 0;
@@ -214,10 +228,11 @@ __device__ __forceinline__ void step_finish_row(const HeadStepArgs& a, int row, 
 }
 
 // What the rows allow of one token, a bit a row.
-__device__ __forceinline__ void step_bits(const HeadStepArgs& a, const StepShared& sh, int token, bool have, uint32_t (&bits)[kStepRows / 32]) {
+template <int W>
+__device__ __forceinline__ void step_bits(const HeadStepArgs& a, const StepShared& sh, int token, bool have, uint32_t (&bits)[W]) {
     const uint32_t* p = a.mask + (token >> 5);
 #pragma unroll
-    for (int c = 0; c < kStepRows / 32; ++c) {
+    for (int c = 0; c < W; ++c) {
         uint32_t w = 0;
         const int n = min(32, a.B - 32 * c);
         if (have)
@@ -229,10 +244,11 @@ __device__ __forceinline__ void step_bits(const HeadStepArgs& a, const StepShare
 
 // The scores of 128 tokens under the rows of the batch: a lane has a token, a column is a row; by way of shared memory a lane
 // has a row (32 c + lane) and the warp's 32 tokens, and keeps that row's state.
+template <int W>
 __device__ __forceinline__ void step_scores(const HeadStepArgs& a, float* turn, const int32_t* list, uint32_t tmem, int token,
-                                            const uint32_t (&bits)[kStepRows / 32], Partial (&state)[kStepRows / 32], int lane) {
+                                            const uint32_t (&bits)[W], Partial (&state)[W], int lane) {
 #pragma unroll
-    for (int c = 0; c < kStepRows / 32; ++c) {
+    for (int c = 0; c < W; ++c) {
         if (32 * c >= a.B) break;
         uint32_t v[32];
         tmem_ld32(tmem + 32 * c, v);
@@ -312,7 +328,7 @@ __device__ __forceinline__ void mma_f16_from_tmem(uint32_t d, uint32_t a, uint64
 }
 
 // How a block's stages are laid out: `tiles` tiles of 128 tokens side by side where it has more than 128, otherwise as many rows
-// as it has tokens (rounded up to 8) and so many more atoms of them. A product takes 128 rows all the same: what it reads behind
+// as it has tokens (rounded up to 32) and so many more atoms of them. A product takes 128 rows all the same: what it reads behind
 // the rows that are there gives sums that nobody reads.
 struct StepLayout {
     int tiles, rows, atoms, steps, stages;
@@ -323,7 +339,7 @@ __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int mos
     constexpr int X = MX ? 4 : 1;  // atoms of hidden states to an atom of weights
     StepLayout l;
     l.tiles = most > 128 ? 2 : 1;
-    l.rows = most > 128 ? 256 : (max(most, 1) + 7) & ~7;
+    l.rows = most > 128 ? 256 : (max(most, 1) + 31) & ~31;
     l.atoms = 1;
     while (l.atoms < 8 && l.atoms < a.row_atoms && 2 * l.atoms * (l.rows + X * a.N) * kStepAtom <= (24u << 10)) l.atoms *= 2;
     l.steps = (a.row_atoms + l.atoms - 1) / l.atoms;
@@ -335,16 +351,16 @@ __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int mos
 
 template <bool MX>
 __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
-    k_head_step(const __grid_constant__ HeadStepArgs a, const __grid_constant__ CUtensorMap map_x) {
-    constexpr int kThreads = (MX ? kStepWarpsMx : kStepWarps) * 32, X = MX ? 4 : 1;
+    k_head_step(const __grid_constant__ HeadStepArgs a, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w) {
+    constexpr int kThreads = (MX ? kStepWarpsMx : kStepWarps) * 32, X = MX ? 4 : 1, W = (MX ? kStepRowsMx : kStepRows) / 32;
     extern __shared__ char smem_raw[];
     __shared__ __align__(16) StepShared sh;
     const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t columns = MX ? 512 : 4 * a.N <= 128 ? 128 : 4 * a.N <= 256 ? 256 : 512;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStepStages; ++i) {
-            mbar_init(&sh.full[i], 1 + 128);        // hidden states, and every thread that fetches weights
+            mbar_init(&sh.full[i], 1 + 256);          // tiled copies, and every thread that fetches weights
             mbar_init(&sh.empty[i], MX ? 1 + 8 : 1);  // the products, and the warps that take weights apart
         }
         for (int i = 0; i < 2; ++i) {
@@ -357,6 +373,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         }
         mbar_init_fence();
         prefetch_tensor_map(&map_x);
+        prefetch_tensor_map(&map_w);
     }
     if (warp == 2) tmem_alloc<1>(&sh.tmem, columns);
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -372,13 +389,14 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     bool ok = true;
     int stage = 0, groups_done = 0;
     uint32_t phase = 0, unit = 0;
-    Partial state[kStepRows / 32];
+    Partial state[W];
 #pragma unroll
-    for (int c = 0; c < kStepRows / 32; ++c) state[c] = partial_empty();
+    for (int c = 0; c < W; ++c) state[c] = partial_empty();
     for (int round = 0; round < a.rounds; ++round) {
         const int shares = a.rounds * gridDim.x;
         const int n = step_share<kThreads>(a, sh, round * gridDim.x + blockIdx.x, shares);
-        const StepLayout l = step_layout<MX>(a, (sh.total + shares - 1) / shares);  // (the same in every round)
+        const bool all = step_takes_all(a, sh.total);
+        const StepLayout l = step_layout<MX>(a, ((all ? a.V : sh.total) + shares - 1) / shares);  // (the same in every round)
         const int per_group = 128 * l.tiles, groups = (n + per_group - 1) / per_group;
         auto next = [&] {
             if (++stage == l.stages) {
@@ -387,78 +405,94 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             }
         };
         if (warp == 0) {
-            if (lane == 0)
-                for (int i = 0; i < groups * l.steps; ++i) {
-                    const int first = i % l.steps * l.atoms, atoms = min(l.atoms, a.row_atoms - first);
+            for (int g = 0; g < groups && ok; ++g) {
+                // boxes of the group's rows, where the tiled copies bring the weights too
+                const int boxes = all ? (min(n - g * per_group, per_group) + kStepBox - 1) / kStepBox : 0;
+                const int token = all ? sh.list[0] + g * per_group : 0;
+                for (int s = 0; s < l.steps; ++s) {
+                    const int first = s * l.atoms, atoms = min(l.atoms, a.row_atoms - first);
                     if (!mbar_wait(&sh.empty[stage], phase ^ 1)) {
                         ok = false;
                         break;
                     }
-                    mbar_expect_tx(&sh.full[stage], uint32_t(atoms) * X * a.N * kStepAtom);
-                    for (int x = 0; x < atoms * X; ++x)
-                        asm volatile(
-                            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
-                            "[%4];" ::"r"(smem + uint32_t(stage) * l.bytes + l.x_at + uint32_t(x) * a.N * kStepAtom),
-                            "l"(&map_x), "r"((first * X + x) * 64), "r"(0), "r"(smem_u32(&sh.full[stage]))
-                            : "memory");
+                    const uint32_t at = smem + uint32_t(stage) * l.bytes;
+                    if (elect_one()) {
+                        mbar_expect_tx(&sh.full[stage], uint32_t(atoms) * (X * a.N + boxes * kStepBox) * kStepAtom);
+                        for (int p = 0; p < atoms; ++p)
+                            for (int i = 0; i < boxes; ++i)
+                                tma_load(at + uint32_t(p * l.rows + i * kStepBox) * kStepAtom, &map_w, (first + p) * (MX ? 128 : 64),
+                                         token + i * kStepBox, &sh.full[stage]);
+                        for (int x = 0; x < atoms * X; ++x)
+                            tma_load(at + l.x_at + uint32_t(x) * a.N * kStepAtom, &map_x, (first * X + x) * 64, 0, &sh.full[stage]);
+                    }
+                    __syncwarp();
                     next();
                 }
+            }
         } else if (warp == 1) {
-            if (lane == 0) {
-                const uint32_t idesc = kMmaBf16Desc<128, 0, false, false> | uint32_t(a.N / 8) << 17;
-                for (int g = 0; g < groups && ok; ++g) {
-                    const int it = groups_done + g, tiles = min(l.tiles, (n - g * per_group + 127) / 128);
-                    if (!mbar_wait(&sh.sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
+            const uint32_t idesc = kMmaBf16Desc<128, 0, false, false> | uint32_t(a.N / 8) << 17, x_step = uint32_t(a.N) * kStepAtom >> 4;
+            const uint32_t w_step = uint32_t(l.rows) * kStepAtom >> 4;
+            for (int g = 0; g < groups && ok; ++g) {
+                const int it = groups_done + g, tiles = min(l.tiles, (n - g * per_group + 127) / 128);
+                if (!mbar_wait(&sh.sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
+                    ok = false;
+                    break;
+                }
+                tmem_fence_after();
+                const uint32_t d0 = tmem + uint32_t(it & 1) * l.tiles * a.N;
+                for (int s = 0; s < l.steps && ok; ++s) {
+                    if (!mbar_wait(&sh.full[stage], phase)) {
                         ok = false;
                         break;
                     }
+                    // (weights were written as ordinary shared memory: the products read it another way)
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     tmem_fence_after();
-                    const uint32_t d = tmem + uint32_t(it & 1) * l.tiles * a.N;
-                    for (int s = 0; s < l.steps && ok; ++s) {
-                        if (!mbar_wait(&sh.full[stage], phase)) {
-                            ok = false;
-                            break;
-                        }
-                        // (weights were written as ordinary shared memory: the products read it another way)
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        tmem_fence_after();
-                        const int atoms = min(l.atoms, a.row_atoms - s * l.atoms);
-                        const uint32_t w_at = smem + uint32_t(stage) * l.bytes, x_at = w_at + l.x_at;
-                        for (int p = 0; p < atoms; ++p)
-                            for (int t = 0; t < tiles; ++t) {
-                                const bool add = s > 0 || p > 0;
-                                if (MX) {
-                                    for (int h = 0; h < 2; ++h, ++unit) {
-                                        const int q = unit & 3;
-                                        if (ok && !mbar_wait(&sh.w_full[q], (unit >> 2) & 1)) ok = false;
-                                        tmem_fence_after();
-                                        const uint64_t dx = mma_desc<false>(x_at + uint32_t(p * 4 + 2 * h) * a.N * kStepAtom);
-                                        const uint64_t dx1 = mma_desc<false>(x_at + uint32_t(p * 4 + 2 * h + 1) * a.N * kStepAtom);
+                    const int atoms = min(l.atoms, a.row_atoms - s * l.atoms);
+                    uint64_t dw0 = mma_desc<false>(smem + uint32_t(stage) * l.bytes);
+                    uint64_t dx = mma_desc<false>(smem + uint32_t(stage) * l.bytes + l.x_at);
+                    for (int p = 0; p < atoms; ++p, dx += X * x_step, dw0 += w_step) {
+                        const bool add = s > 0 || p > 0;
+                        for (int t = 0; t < tiles; ++t) {
+                            const uint32_t d = d0 + t * a.N;
+                            if (MX) {
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+                                    const uint32_t q = (unit + h) & 3;
+                                    if (ok && !mbar_wait(&sh.w_full[q], ((unit + h) >> 2) & 1)) ok = false;
+                                    tmem_fence_after();
+                                    const uint64_t dx0 = dx + 2 * h * x_step, dx1 = dx0 + x_step;
+                                    if (elect_one()) {
 #pragma unroll
                                         for (int j = 0; j < 8; ++j)
-                                            mma_f16_from_tmem(d + t * a.N, tmem + 256 + 64 * q + 8 * j,
-                                                              (j < 4 ? dx : dx1) + (j & 3) * kDescStep16<false>, idesc,
-                                                              add || h > 0 || j > 0);
+                                            mma_f16_from_tmem(d, tmem + 256 + 64 * q + 8 * j, (j < 4 ? dx0 : dx1) + (j & 3) * kDescStep16<false>,
+                                                              idesc, add || h > 0 || j > 0);
                                         mma_commit<1>(&sh.w_empty[q]);
                                     }
-                                } else {
-                                    const uint64_t dw = mma_desc<false>(w_at + uint32_t(p) * l.rows * kStepAtom + t * kStepTile);
-                                    const uint64_t dx = mma_desc<false>(x_at + uint32_t(p) * a.N * kStepAtom);
+                                    __syncwarp();
+                                }
+                                unit += 2;
+                            } else {
+                                const uint64_t dw = dw0 + t * (kStepTile >> 4);
+                                if (elect_one()) {
 #pragma unroll
                                     for (int j = 0; j < 4; ++j)
-                                        mma_f16<1>(d + t * a.N, dw + j * kDescStep16<false>, dx + j * kDescStep16<false>, idesc,
-                                                   add || j > 0);
+                                        mma_f16<1>(d, dw + j * kDescStep16<false>, dx + j * kDescStep16<false>, idesc, add || j > 0);
                                 }
+                                __syncwarp();
                             }
-                        mma_commit<1>(&sh.empty[stage]);
-                        next();
+                        }
                     }
-                    mma_commit<1>(&sh.sums_full[it & 1]);
+                    if (elect_one()) mma_commit<1>(&sh.empty[stage]);
+                    __syncwarp();
+                    next();
                 }
+                if (elect_one()) mma_commit<1>(&sh.sums_full[it & 1]);
+                __syncwarp();
             }
-        } else if (MX && warp >= 12) {
+        } else if (MX && warp >= 16) {
             // a thread a token: set 0 takes the first half of an atom's 256 weights, set 1 the second
-            const int half = (warp - 12) >> 2, row = (warp & 3) * 32 + lane;
+            const int half = (warp - 16) >> 2, row = (warp & 3) * 32 + lane;
             for (int g = 0; g < groups && ok; ++g) {
                 const int tiles = min(l.tiles, (n - g * per_group + 127) / 128);
                 const uint8_t* scales[2];
@@ -525,30 +559,31 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 }
             }
         } else if (warp >= 8) {
-            // eight lanes bring the 128 bytes of a row's atom, the four warps 16 rows at a time
-            const int chunk = lane & 7, row = (warp & 3) * 4 + (lane >> 3);
+            // eight lanes bring the 128 bytes of a row's atom, the eight warps 32 rows at a time
+            const int chunk = lane & 7, row = (warp - 8) * 4 + (lane >> 3);
             for (int g = 0; g < groups && ok; ++g) {
-                const char* from[16];
+                const int rows = all ? 0 : min(n - g * per_group, per_group);
+                const char* from[8];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int at = g * per_group + i * 16 + row;
-                    from[i] = at < n && i * 16 + row < l.rows
-                                  ? static_cast<const char*>(a.weight) + int64_t(sh.list[at]) * a.row_bytes + chunk * 16
-                                  : nullptr;
-                }
+                for (int i = 0; i < 8; ++i)
+                    if (i * 32 < rows)  // (rows behind the last one are filled up with it)
+                        from[i] = static_cast<const char*>(a.weight) +
+                                  int64_t(sh.list[min(g * per_group + i * 32 + row, n - 1)]) * a.row_bytes + chunk * 16;
                 for (int s = 0; s < l.steps; ++s) {
                     if (!mbar_wait(&sh.empty[stage], phase ^ 1)) {
                         ok = false;
                         break;
                     }
-                    const int atoms = min(l.atoms, a.row_atoms - s * l.atoms);
+                    const int first = s * l.atoms, atoms = min(l.atoms, a.row_atoms - first);
                     uint32_t to = smem + uint32_t(stage) * l.bytes + uint32_t(row) * kStepAtom + uint32_t((chunk ^ (row & 7)) << 4);
                     for (int p = 0; p < atoms; ++p, to += uint32_t(l.rows) * kStepAtom) {
-                        const int off = (s * l.atoms + p) * int(kStepAtom);
+                        const int off = (first + p) * int(kStepAtom);
                         const bool have = off + chunk * 16 < a.bytes;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (from[i]) copy16(to + i * 16 * kStepAtom, have ? from[i] + off : from[i] - chunk * 16, have);
+                        for (int i = 0; i < 8; ++i) {
+                            if (i * 32 >= rows) break;
+                            copy16(to + i * 32 * kStepAtom, have ? from[i] + off : from[i] - chunk * 16, have);
+                        }
                     }
                     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.full[stage])) : "memory");
                     next();
@@ -559,7 +594,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             const int quad = warp & 3;
             for (int g = 0; g < groups; ++g) {
                 const int it = groups_done + g;
-                uint32_t bits[2][kStepRows / 32];
+                uint32_t bits[2][W];
                 int token[2];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
@@ -593,7 +628,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     // the four warps' states to one, out to the others' and, in the last block to come here, to the results
     if (warp >= 4 && warp < 8) {
 #pragma unroll
-        for (int c = 0; c < kStepRows / 32; ++c) sh.state[warp & 3][32 * c + lane] = state[c];
+        for (int c = 0; c < W; ++c) sh.state[warp & 3][32 * c + lane] = state[c];
     }
     tmem_fence_before();
     __syncthreads();

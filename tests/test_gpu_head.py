@@ -91,18 +91,28 @@ STEPS = [
     (40000, 4128, 8, 300, 0.05, "mxfp4", 8),
     (20011, 320, 129, 300, 0.2, "mxfp4", 8),
     (9001, 64, 300, 130, 0.3, "mxfp4", 0),
+    # few tokens to a block, or hardly any, of long rows
+    (60000, 2048, 3, 300, 0.002, "bf16", 0),
+    (60000, 4104, 40, 300, 0.0005, "bf16", 8),
+    (60000, 2080, 3, 300, 0.002, "mxfp4", 0),
+    (60000, 4096, 40, 300, 0.0005, "mxfp4", 8),
+    # more than a block lists at a time
+    (400003, 8, 2, 5, 0.9, "bf16", 0),
+    (400003, 32, 2, 300, 0.5, "mxfp4", 0),
 ]
 
 
+@pytest.mark.parametrize("everything", [False, True])
 @pytest.mark.parametrize("V,H,B,K,density,head,pad", STEPS)
-def test_step(V, H, B, K, density, head, pad):
+def test_step(V, H, B, K, density, head, pad, everything):
     case = Case(V, H, B, head, seed=V + H + B, pad=pad)
     p = synth.zipf_partition(V, K, 1.1, seed=3) if K > 1 else synth.Partition(V=1, K=1, c=np.zeros(1, np.int32), r=np.zeros(1, np.int32),
                                                                             sizes=np.ones(1, np.int64))
     cm = class_masks(K, B, density, (5, V, B))
     if B > 2:
         cm[B // 2] = 0           # nothing allowed
-        cm[B - 1] = 0xFFFFFFFF   # everything, and bits of classes that are not there
+        if everything:
+            cm[B - 1] = 0xFFFFFFFF   # and bits of classes that are not there
     with Ctx([p]) as ctx:
         c, trep = torch.from_numpy(p.c).long().cuda(), torch.from_numpy(p.r[p.c]).cuda()
         mask = unpack(dev(cm), K)[:, c]
