@@ -61,7 +61,8 @@ constexpr int kPairs = 74;                           // pairs of SMs that plans 
 
 struct HeadSpace {
     // step
-    uint16_t* swapped;
+    uint16_t* half;
+    float* back;
     uint32_t *mask, *any, *ticket;
     int32_t* counts;
     Partial* states;
@@ -104,7 +105,10 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
         s.counts = c.take<int32_t>(ceil_div(h->V, 32 * kUnionWords));
         s.ticket = c.take<uint32_t>(1);
         s.states = c.take<Partial>(std::min<int64_t>(n, kStepRows) * kStepBlocks);
-        if (h->dtype == CFGZIP_MXFP4) s.swapped = c.take<uint16_t>(std::min<int64_t>(n, kStepRowsMx) * h->H);
+        if (h->dtype == CFGZIP_MXFP4) {
+            s.half = c.take<uint16_t>(std::min<int64_t>(n, kStepRowsMx) * h->H);
+            s.back = c.take<float>(kStepRowsMx);
+        }
     } else if (op == CFGZIP_HEAD_LOSS) {
         s.part = c.take<float2>(n * ceil_div(h->V, kMmaTile));
         s.of_target = c.take<float>(n);
@@ -158,7 +162,7 @@ int dequantize(cfgzip_ctx* ctx, const cfgzip_head* h, int32_t t0, int32_t n, uin
 
 // One decode step of up to kStepRows (kStepRowsMx) rows whose vocab masks are there.
 int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const uint16_t* hidden, int64_t hidden_stride,
-             uint16_t* swapped, cudaStream_t st) {
+             const HeadSpace& w, cudaStream_t st) {
     const bool mx = head->dtype == CFGZIP_MXFP4;
     CUtensorMap map_x, map_w;
     int rc;
@@ -172,13 +176,14 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
     if (mx) {
         a.hidden = hidden;
         a.hidden_stride = hidden_stride;
-        a.swapped = swapped;
+        a.half = w.half;
+        a.back = w.back;
     }
-    if ((rc = tensor_map(ctx, &map_x, mx ? swapped : hidden, a.B, head->H, mx ? head->H : hidden_stride, a.N)) != CFGZIP_OK ||
+    if ((rc = tensor_map(ctx, &map_x, mx ? w.half : hidden, a.B, head->H, mx ? head->H : hidden_stride, a.N)) != CFGZIP_OK ||
         (rc = tensor_map(ctx, &map_w, head->weight, head->V, mx ? a.bytes : head->H, head->row_stride, kStepBox, mx)) != CFGZIP_OK)
         return rc;
     a.n_counts = ceil_div(a.VW, kUnionWords);
-    if ((rc = launch(ctx, k_head_union, dim3(unsigned(a.n_counts)), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
+    if ((rc = launch(ctx, k_head_union, dim3(unsigned(a.n_counts + (mx ? a.B : 0))), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
     if (a.logits) {
         const dim3 grid(unsigned(std::max(1, std::min(ceil_div(a.V, 8192), 64))), unsigned(a.B));
         if ((rc = launch(ctx, a.logits_dtype == CFGZIP_BF16 ? k_head_fill<kBF16> : k_head_fill<kF32>, grid, dim3(256), 0, st, a)) !=
@@ -288,7 +293,7 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
         s.logp = logp_argmax ? logp_argmax + b : nullptr;
         s.lse = lse ? lse + b : nullptr;
         s.status = ctx->d_status;
-        rc = run_step(ctx, s, head, static_cast<const uint16_t*>(hidden) + b * hidden_stride, hidden_stride, w.swapped, st);
+        rc = run_step(ctx, s, head, static_cast<const uint16_t*>(hidden) + b * hidden_stride, hidden_stride, w, st);
         if (rc != CFGZIP_OK) return rc;
     }
     return CFGZIP_OK;

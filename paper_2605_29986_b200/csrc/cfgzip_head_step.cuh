@@ -36,9 +36,10 @@ struct HeadStepArgs {
     int32_t bytes;         // of a row of weights that count
     int32_t smem;          // shared memory for stages
     int32_t rounds;
-    const uint16_t* hidden;  // 4-bit heads: copied to `swapped` in the order in which their weights are taken apart
+    const uint16_t* hidden;  // 4-bit heads: rows brought to at most 2^15 and copied as f16 to `half`
     int64_t hidden_stride;
-    uint16_t* swapped;     // [B, H]
+    uint16_t* half;        // [B, H]
+    float* back;           // [B] what brings a row's products back
     uint32_t* any;         // [VW] union of the rows' masks
     int32_t* counts;       // tokens of it in every kUnionWords words
     int32_t n_counts;
@@ -59,20 +60,47 @@ __device__ __forceinline__ int step_row_part(const HeadStepArgs& a, int row) {
     return p >= 0 && p < a.n_parts && a.parts[p].live && a.parts[p].V == a.V ? p : -1;
 }
 
-// Union of the rows' masks, 32 words by a block: a warp ORs every eighth row.
+// A row of hidden states as f16, times the power of two that brings its largest to [2^14, 2^15): all of a bf16 number's bits are
+// kept down to 2^-29 of the largest, and what is lost below that is 2^-40 of it at most, nothing to a sum in 32 bits.
+__device__ __forceinline__ void half_row(const HeadStepArgs& a, int row) {
+    __shared__ uint32_t most[8];
+    const int vectors = a.H / 8, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint4* x = reinterpret_cast<const uint4*>(a.hidden + row * a.hidden_stride);
+    uint32_t top = 0;
+    for (int i = threadIdx.x; i < vectors; i += 256) {
+        const uint4 v = ld_after_wait(x + i);
+        top = __vmaxu2(__vmaxu2(top, __vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu)), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+    }
+    top = __reduce_max_sync(0xFFFFFFFFu, max(top >> 16, top & 0xFFFFu));
+    if (lane == 0) most[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 8; ++w) top = max(top, most[w]);
+    const int e = min(max(int(top >> 7), 15), 254);  // exponent of the largest, + 127
+    const float up = __uint_as_float(uint32_t(268 - e) << 23);  // 2^(14 - (e - 127))
+    if (threadIdx.x == 0) a.back[row] = __uint_as_float(uint32_t(max(e - 14, 1)) << 23);
+    for (int i = threadIdx.x; i < vectors; i += 256) {
+        const uint4 v = ld_after_wait(x + i);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            asm("cvt.rn.f16x2.f32 %0, %1, %2;"
+                : "=r"(o[j])
+                : "f"(__uint_as_float(w[j] & 0xFFFF0000u) * up), "f"(__uint_as_float(w[j] << 16) * up));
+        reinterpret_cast<uint4*>(a.half + int64_t(row) * a.H)[i] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+// Union of the rows' masks, 32 words by a block: a warp ORs every eighth row. Blocks behind those take a row of hidden states.
 __global__ void __launch_bounds__(256) k_head_union(const HeadStepArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, word = blockIdx.x * kUnionWords + lane;
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
-    if (a.swapped) {  // weights 0 to 7 of a word come out as 0 4 1 5 2 6 3 7
-        const int vectors = a.H / 8;
-        for (int i = blockIdx.x * 256 + threadIdx.x; i < a.B * vectors; i += gridDim.x * 256) {
-            const int row = i / vectors, col = i - row * vectors;
-            const uint4 v = ld_after_wait(reinterpret_cast<const uint4*>(a.hidden + row * a.hidden_stride) + col);
-            reinterpret_cast<uint4*>(a.swapped)[i] = make_uint4(prmt(v.x, v.z, 0x5410), prmt(v.x, v.z, 0x7632),
-                                                                prmt(v.y, v.w, 0x5410), prmt(v.y, v.w, 0x7632));
-        }
+    if (int(blockIdx.x) >= a.n_counts) {
+        half_row(a, int(blockIdx.x) - a.n_counts);
+        return;
     }
     uint32_t any = 0;
     if (word < a.VW)
@@ -124,11 +152,11 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
 }
 
 struct StepShared {
-    uint64_t full[kStepStages], empty[kStepStages], sums_full[2], sums_empty[2], w_full[4], w_empty[4];
+    uint64_t full[kStepStages], empty[kStepStages], sums_full[2], sums_empty[2], w_full[2], w_empty[2];
     uint32_t tmem;
     uint32_t valid[kStepRows / 32];  // rows that have a partition
-    int32_t total, entries, is_last;
-    int32_t first;                   // token number 0 of the share, where all tokens are taken
+    int32_t entries, is_last;
+    float back[kStepRowsMx];
     int32_t scan[kStepWarpsMx];
     int32_t list[kStepShare];        // the block's tokens, ascending
     union alignas(16) {
@@ -138,48 +166,47 @@ struct StepShared {
     };
 };
 
-// A union of at least three quarters of the vocabulary is taken for all of it: whole boxes of rows by tiled copies go at 93 % of
-// the memory's rate, rows one by one at 80 % (32 rows of 128256 x 4096).
-__device__ __forceinline__ bool step_takes_all(const HeadStepArgs& a, int total) { return int64_t(total) * 4 >= int64_t(a.V) * 3; }
-
-// The block's share of the union: tokens number lo .. lo + n of it, to sh.list. All threads; ends with a barrier.
+// The block's share of the union: its n tokens to sh.list; the longest share of any block to *most. A union of at least three
+// quarters of the vocabulary is taken for all of it (*all): boxes of rows by tiled copies come at the memory's rate, rows one by
+// one at 80 % of it. All threads; ends with a barrier.
 template <int THREADS>
-__device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh, int share, int shares) {
+__device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh, int share, int shares, bool* all, int* most) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) sh.total = sh.entries = 0;
-    __syncthreads();
+    if (tid == 0) sh.entries = 0;
+    const int strip = (a.n_counts + THREADS - 1) / THREADS, c0 = min(tid * strip, a.n_counts), c1 = min(c0 + strip, a.n_counts);
     int mine = 0;
-    for (int i = tid; i < a.n_counts; i += THREADS) mine += __ldcg(a.counts + i);
-    mine = __reduce_add_sync(0xFFFFFFFFu, mine);
-    if (lane == 0 && mine) atomicAdd(&sh.total, mine);
+    for (int i = c0; i < c1; ++i) mine += __ldcg(a.counts + i);
+    int before = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xFFFFFFFFu, before, d);
+        if (lane >= d) before += o;
+    }
+    if (lane == 31) sh.scan[warp] = before;
     __syncthreads();
-    const bool all = step_takes_all(a, sh.total);
-    const int total = all ? a.V : sh.total;
-    const int lo = int(int64_t(total) * share / shares), hi = int(int64_t(total) * (share + 1) / shares);
-    if (all) {
+    before -= mine;
+    uint32_t total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        const int o = sh.scan[w];
+        if (w < warp) before += o;
+        total += o;
+    }
+    *all = int64_t(total) * 4 >= int64_t(a.V) * 3;
+    if (*all) total = a.V;
+    // equal parts, the first `more` of them a token longer
+    const uint32_t each = total / uint32_t(shares), more = total - each * uint32_t(shares);
+    *most = int(each + (more > 0));
+    const int lo = int(each * uint32_t(share) + min(uint32_t(share), more)), hi = lo + int(each + (uint32_t(share) < more));
+    if (*all) {
         for (int i = tid; i < hi - lo; i += THREADS) sh.list[i] = lo + i;
     } else if (lo < hi) {  // (the same for every thread)
-        int front = 0;
-        for (int base = 0; base < a.n_counts; base += THREADS) {
-            const int i = base + tid, n = i < a.n_counts ? __ldcg(a.counts + i) : 0;
-            int sum = n;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int o = __shfl_up_sync(0xFFFFFFFFu, sum, d);
-                if (lane >= d) sum += o;
-            }
-            if (lane == 31) sh.scan[warp] = sum;
-            __syncthreads();
-            int before = front + sum - n;
-#pragma unroll
-            for (int w = 0; w < THREADS / 32; ++w) {
-                const int o = sh.scan[w];
-                if (w < warp) before += o;
-                front += o;
-            }
+        for (int i = c0; i < c1; ++i) {
+            const int n = strip == 1 ? mine : __ldcg(a.counts + i);
             if (n > 0 && before < hi && before + n > lo) sh.entry[atomicAdd(&sh.entries, 1)] = make_int2(i, before);
-            __syncthreads();
+            before += n;
         }
+        __syncthreads();
         for (int e = warp; e < sh.entries; e += THREADS / 32) {
             const int2 en = sh.entry[e];
             const int word = en.x * kUnionWords + lane;
@@ -244,15 +271,20 @@ __device__ __forceinline__ void step_bits(const HeadStepArgs& a, const StepShare
 
 // The scores of 128 tokens under the rows of the batch: a lane has a token, a column is a row; by way of shared memory a lane
 // has a row (32 c + lane) and the warp's 32 tokens, and keeps that row's state.
-template <int W>
-__device__ __forceinline__ void step_scores(const HeadStepArgs& a, float* turn, const int32_t* list, uint32_t tmem, int token,
-                                            const uint32_t (&bits)[W], Partial (&state)[W], int lane) {
+template <bool MX, int W>
+__device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& sh, int quad, float back, const int32_t* list, uint32_t tmem,
+                                            int token, const uint32_t (&bits)[W], Partial (&state)[W], int lane) {
+    float* turn = sh.turn[quad];
 #pragma unroll
     for (int c = 0; c < W; ++c) {
         if (32 * c >= a.B) break;
         uint32_t v[32];
         tmem_ld32(tmem + 32 * c, v);
         tmem_wait_ld();
+        if (MX) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * sh.back[32 * c + j] * back);
+        }
         if (a.logits) {
             const int n = min(32, a.B - 32 * c);
             if (a.logits_dtype == kBF16) {
@@ -290,24 +322,44 @@ __device__ __forceinline__ void step_scores(const HeadStepArgs& a, float* turn, 
     }
 }
 
-// Four 4-bit blocks of 32 weights (16 bytes each) of a token to tensor memory as bf16: sign, exponent and fraction of a weight go
-// to the top bits of a bf16 number, 2^126 below their value, and two exact products bring them up. Weights i and i + 4 of a word
-// come out side by side.
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+// 4-bit weights in tensor memory are f16, relative to the largest scale of their row: e2m1 numbers times 2^0 down to 2^-23 are
+// exact in f16, and of a block with a scale below that 2^-25 of the largest is lost at most. One conversion and one product for
+// two weights; going to bf16 by shifts, masks and a product takes 19 instructions for eight, not 8, and held the kernel up.
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     uint32_t d;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
-__device__ __forceinline__ void mx_word(uint32_t w, uint32_t scale, uint32_t (&out)[4]) {
-    const uint32_t up = 0x7E807E80u;  // 2^126
-    const uint32_t t[4] = {((w << 12) & 0x80008000u) | ((w << 6) & 0x01C001C0u), ((w << 8) & 0x80008000u) | ((w << 2) & 0x01C001C0u),
-                           ((w << 4) & 0x80008000u) | ((w >> 2) & 0x01C001C0u), (w & 0x80008000u) | ((w >> 6) & 0x01C001C0u)};
+__device__ __forceinline__ void mx_word(uint32_t w, uint32_t scale, uint32_t* out) {
+    uint32_t t[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(t[0]), "=r"(t[1]), "=r"(t[2]), "=r"(t[3])
+        : "r"(w));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = mul_bf16x2(mul_bf16x2(t[i], up), scale);
+    for (int i = 0; i < 4; ++i) out[i] = mul_f16x2(t[i], scale);
 }
-__device__ __forceinline__ uint32_t mx_scale_pair(uint32_t byte) {  // 2^(byte - 127) twice, as bf16
-    const uint32_t b = byte == 255u ? 0x7FC0u : byte ? byte << 7 : 0x0040u;
+// 2^(byte - largest) twice, as f16
+__device__ __forceinline__ uint32_t mx_scale_pair(uint32_t byte, uint32_t largest) {
+    const int d = int(byte) - int(largest);
+    const uint32_t b = d >= -14 ? uint32_t(15 + d) << 10 : d >= -24 ? 1u << (24 + d) : 0u;
     return b | b << 16;
+}
+// Largest scale byte of a row of n blocks (rows start on 16 bytes).
+__device__ __forceinline__ uint32_t mx_largest(const uint8_t* scales, int n) {
+    uint32_t top = 0;
+#pragma unroll 4
+    for (int i = 0; i < n; i += 16) {
+        const uint4 v = ld_after_wait(reinterpret_cast<const uint4*>(scales + i));
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int left = n - i - 4 * k;
+            top = __vmaxu4(top, left >= 4 ? w[k] : left <= 0 ? 0u : w[k] & ((1u << (8 * left)) - 1u));
+        }
+    }
+    top = __vmaxu4(top, top >> 16);
+    return max(top & 255u, (top >> 8) & 255u);
 }
 __device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&v)[32]) {
     asm volatile(
@@ -341,8 +393,12 @@ __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int mos
     l.tiles = most > 128 ? 2 : 1;
     l.rows = most > 128 ? 256 : (max(most, 1) + 31) & ~31;
     l.atoms = 1;
-    while (l.atoms < 8 && l.atoms < a.row_atoms && 2 * l.atoms * (l.rows + X * a.N) * kStepAtom <= (24u << 10)) l.atoms *= 2;
-    l.steps = (a.row_atoms + l.atoms - 1) / l.atoms;
+    int shift = 0;
+    while (shift < 3 && l.atoms < a.row_atoms && 2 * l.atoms * (l.rows + X * a.N) * kStepAtom <= (36u << 10)) {
+        l.atoms *= 2;
+        ++shift;
+    }
+    l.steps = (a.row_atoms + l.atoms - 1) >> shift;
     l.x_at = uint32_t(l.atoms) * l.rows * kStepAtom;
     l.bytes = l.x_at + uint32_t(l.atoms) * X * a.N * kStepAtom;
     l.stages = min(kStepStages, int(uint32_t(a.smem) / l.bytes));
@@ -366,9 +422,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.sums_full[i], 1);
             mbar_init(&sh.sums_empty[i], 4);
-        }
-        for (int i = 0; i < 4; ++i) {
-            mbar_init(&sh.w_full[i], 4);
+            mbar_init(&sh.w_full[i], 8);
             mbar_init(&sh.w_empty[i], 1);
         }
         mbar_init_fence();
@@ -382,6 +436,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         const uint32_t w = __ballot_sync(0xFFFFFFFFu, v);
         if (lane == 0) sh.valid[warp] = w;
     }
+    if (MX && int(threadIdx.x) < a.B) sh.back[threadIdx.x] = ld_after_wait(a.back + threadIdx.x);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
@@ -394,9 +449,10 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     for (int c = 0; c < W; ++c) state[c] = partial_empty();
     for (int round = 0; round < a.rounds; ++round) {
         const int shares = a.rounds * gridDim.x;
-        const int n = step_share<kThreads>(a, sh, round * gridDim.x + blockIdx.x, shares);
-        const bool all = step_takes_all(a, sh.total);
-        const StepLayout l = step_layout<MX>(a, ((all ? a.V : sh.total) + shares - 1) / shares);  // (the same in every round)
+        bool all;
+        int most;
+        const int n = step_share<kThreads>(a, sh, round * gridDim.x + blockIdx.x, shares, &all, &most);
+        const StepLayout l = step_layout<MX>(a, most);  // (the same in every round)
         const int per_group = 128 * l.tiles, groups = (n + per_group - 1) / per_group;
         auto next = [&] {
             if (++stage == l.stages) {
@@ -430,7 +486,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 }
             }
         } else if (warp == 1) {
-            const uint32_t idesc = kMmaBf16Desc<128, 0, false, false> | uint32_t(a.N / 8) << 17, x_step = uint32_t(a.N) * kStepAtom >> 4;
+            const uint32_t idesc = (MX ? kMmaF16Desc<128, 0, false, false> : kMmaBf16Desc<128, 0, false, false>) | uint32_t(a.N / 8) << 17, x_step = uint32_t(a.N) * kStepAtom >> 4;
             const uint32_t w_step = uint32_t(l.rows) * kStepAtom >> 4;
             for (int g = 0; g < groups && ok; ++g) {
                 const int it = groups_done + g, tiles = min(l.tiles, (n - g * per_group + 127) / 128);
@@ -449,41 +505,34 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     tmem_fence_after();
                     const int atoms = min(l.atoms, a.row_atoms - s * l.atoms);
-                    uint64_t dw0 = mma_desc<false>(smem + uint32_t(stage) * l.bytes);
-                    uint64_t dx = mma_desc<false>(smem + uint32_t(stage) * l.bytes + l.x_at);
-                    for (int p = 0; p < atoms; ++p, dx += X * x_step, dw0 += w_step) {
-                        const bool add = s > 0 || p > 0;
-                        for (int t = 0; t < tiles; ++t) {
-                            const uint32_t d = d0 + t * a.N;
-                            if (MX) {
-#pragma unroll
-                                for (int h = 0; h < 2; ++h) {
-                                    const uint32_t q = (unit + h) & 3;
-                                    if (ok && !mbar_wait(&sh.w_full[q], ((unit + h) >> 2) & 1)) ok = false;
-                                    tmem_fence_after();
-                                    const uint64_t dx0 = dx + 2 * h * x_step, dx1 = dx0 + x_step;
-                                    if (elect_one()) {
-#pragma unroll
-                                        for (int j = 0; j < 8; ++j)
-                                            mma_f16_from_tmem(d, tmem + 256 + 64 * q + 8 * j, (j < 4 ? dx0 : dx1) + (j & 3) * kDescStep16<false>,
-                                                              idesc, add || h > 0 || j > 0);
-                                        mma_commit<1>(&sh.w_empty[q]);
-                                    }
-                                    __syncwarp();
-                                }
-                                unit += 2;
-                            } else {
-                                const uint64_t dw = dw0 + t * (kStepTile >> 4);
+                    const uint64_t dw = mma_desc<false>(smem + uint32_t(stage) * l.bytes);
+                    const uint64_t dx = mma_desc<false>(smem + uint32_t(stage) * l.bytes + l.x_at);
+                    if (MX) {
+                        for (int p = 0; p < atoms; ++p)
+                            for (int t = 0; t < tiles; ++t, ++unit) {
+                                const uint32_t q = unit & 1;
+                                if (ok && !mbar_wait(&sh.w_full[q], (unit >> 1) & 1)) ok = false;
+                                tmem_fence_after();
                                 if (elect_one()) {
 #pragma unroll
-                                    for (int j = 0; j < 4; ++j)
-                                        mma_f16<1>(d, dw + j * kDescStep16<false>, dx + j * kDescStep16<false>, idesc, add || j > 0);
+                                    for (int j = 0; j < 16; ++j)
+                                        mma_f16_from_tmem(d0 + t * a.N, tmem + 256 + 128 * q + 8 * j,
+                                                          dx + (4 * p + j / 4) * x_step + (j & 3) * kDescStep16<false>, idesc,
+                                                          s > 0 || p > 0 || j > 0);
+                                    mma_commit<1>(&sh.w_empty[q]);
                                 }
                                 __syncwarp();
                             }
-                        }
+                        if (elect_one()) mma_commit<1>(&sh.empty[stage]);
+                    } else if (elect_one()) {
+                        for (int p = 0; p < atoms; ++p)
+                            for (int t = 0; t < tiles; ++t)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    mma_f16<1>(d0 + t * a.N, dw + p * w_step + t * (kStepTile >> 4) + j * kDescStep16<false>,
+                                               dx + p * x_step + j * kDescStep16<false>, idesc, s > 0 || p > 0 || j > 0);
+                        mma_commit<1>(&sh.empty[stage]);
                     }
-                    if (elect_one()) mma_commit<1>(&sh.empty[stage]);
                     __syncwarp();
                     next();
                 }
@@ -496,11 +545,13 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             for (int g = 0; g < groups && ok; ++g) {
                 const int tiles = min(l.tiles, (n - g * per_group + 127) / 128);
                 const uint8_t* scales[2];
-                uint32_t scale[2], scale_next[2];
+                uint32_t scale[2], scale_next[2], largest[2];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const int at = g * per_group + t * 128 + row;
-                    scales[t] = t < tiles && at < n ? a.scales + int64_t(sh.list[at]) * a.scale_stride + 4 * half : nullptr;
+                    scales[t] = t < tiles && at < n ? a.scales + int64_t(sh.list[at]) * a.scale_stride : nullptr;
+                    largest[t] = scales[t] ? mx_largest(scales[t], a.bytes / 16) : 0;
+                    if (scales[t]) scales[t] += 4 * half;
                     scale_next[t] = scales[t] && 4 * half < a.bytes / 16 ? ld_after_wait(reinterpret_cast<const uint32_t*>(scales[t])) : 0;
                 }
                 for (int s = 0; s < l.steps && ok; ++s) {
@@ -520,8 +571,8 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
 #pragma unroll
                         for (int t = 0; t < 2; ++t) {
                             if (t >= tiles) break;
-                            const uint32_t q = (unit + half) & 3;
-                            if (!mbar_wait(&sh.w_empty[q], (((unit + half) >> 2) & 1) ^ 1)) ok = false;
+                            const uint32_t q = unit & 1;
+                            if (!mbar_wait(&sh.w_empty[q], ((unit >> 1) & 1) ^ 1)) ok = false;
                             tmem_fence_after();
                             const int r = t * 128 + row;
                             const uint32_t at = smem + uint32_t(stage) * l.bytes + (uint32_t(p) * l.rows + min(r, l.rows - 1)) * kStepAtom;
@@ -535,22 +586,17 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                                                  : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
                                                  : "r"(at + (uint32_t((4 * half + b + k) ^ (r & 7)) << 4)));
                                     // (behind the row there is no scale, and the weights are zeros)
-                                    const uint32_t sc = mx_scale_pair(b + k < left ? (scale[t] >> (8 * (b + k))) & 255u : 127u);
+                                    const uint32_t sc = mx_scale_pair(b + k < left ? (scale[t] >> (8 * (b + k))) & 255u : 0u, largest[t]);
 #pragma unroll
-                                    for (int i = 0; i < 4; ++i) {
-                                        uint32_t o[4];
-                                        mx_word(w[i], sc, o);
-#pragma unroll
-                                        for (int e = 0; e < 4; ++e) v[16 * k + 4 * i + e] = o[e];
-                                    }
+                                    for (int i = 0; i < 4; ++i) mx_word(w[i], sc, v + 16 * k + 4 * i);
                                 }
-                                tmem_st32(tmem + 256 + 64 * q + 16 * b + (uint32_t((warp & 3) * 32) << 16), v);
+                                tmem_st32(tmem + 256 + 128 * q + 64 * half + 16 * b + (uint32_t((warp & 3) * 32) << 16), v);
                             }
                             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                             tmem_fence_before();
                             __syncwarp();
                             if (lane == 0) mbar_arrive(&sh.w_full[q]);
-                            unit += 2;
+                            ++unit;
                         }
                     }
                     __syncwarp();
@@ -596,12 +642,14 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 const int it = groups_done + g;
                 uint32_t bits[2][W];
                 int token[2];
+                float back[2];  // what brings a token's products back
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const int at = g * per_group + t * 128 + quad * 32 + lane;
                     const bool have = t < l.tiles && at < n;
                     token[t] = have ? sh.list[at] : 0;
                     step_bits(a, sh, token[t], have, bits[t]);
+                    back[t] = MX && have ? mx_scale(mx_largest(a.scales + int64_t(token[t]) * a.scale_stride, a.bytes / 16)) : 1.f;
                 }
                 if (!mbar_wait(&sh.sums_full[it & 1], (it >> 1) & 1)) {
                     ok = false;
@@ -612,7 +660,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 for (int t = 0; t < 2; ++t) {
                     const int at = g * per_group + t * 128 + quad * 32;
                     if (t < l.tiles && at < n)
-                        step_scores(a, sh.turn[quad], sh.list + at, tmem + uint32_t((it & 1) * l.tiles + t) * a.N + (uint32_t(quad * 32) << 16),
+                        step_scores<MX>(a, sh, quad, back[t], sh.list + at, tmem + uint32_t((it & 1) * l.tiles + t) * a.N + (uint32_t(quad * 32) << 16),
                                     token[t], bits[t], state, lane);
                 }
                 tmem_fence_before();

@@ -22,6 +22,9 @@ constexpr uint32_t kDescStep16 = MN ? 2048 >> 4 : 32 >> 4;
 template <int M, int N, bool A_MN, bool B_MN>
 constexpr uint32_t kMmaBf16Desc = 1u << 4 | 1u << 7 | 1u << 10 | uint32_t(A_MN) << 15 | uint32_t(B_MN) << 16 | uint32_t(N / 8) << 17 |
                               uint32_t(M / 16) << 24;
+// f16 x f16 -> f32
+template <int M, int N, bool A_MN, bool B_MN>
+constexpr uint32_t kMmaF16Desc = kMmaBf16Desc<M, N, A_MN, B_MN> & ~(1u << 7 | 1u << 10);
 
 // ---- tensor memory ------------------------------------------------------------------------------------------------------------
 template <int CTAS>
