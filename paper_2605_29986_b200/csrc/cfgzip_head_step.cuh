@@ -118,10 +118,23 @@ __global__ void __launch_bounds__(256) k_head_union(const HeadStepArgs a) {
     if (lane == 0) a.counts[blockIdx.x] = n;
 }
 
-// -inf for every score; the allowed ones are written over it.
+// A union of at least three quarters of the vocabulary is taken for all of it: boxes of rows by tiled copies come at the memory's
+// rate, rows one by one at 80 % of it.
+__device__ __forceinline__ bool step_takes_all(const HeadStepArgs& a, uint32_t total) { return int64_t(total) * 4 >= int64_t(a.V) * 3; }
+
+// -inf for every score; those of allowed tokens are written over it. (Where all tokens are taken, the step writes every score.)
 template <int DT>
 __global__ void __launch_bounds__(256) k_head_fill(const HeadStepArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ uint32_t total;
+    if (threadIdx.x == 0) total = 0;
+    __syncthreads();
+    uint32_t mine = 0;
+    for (int i = threadIdx.x; i < a.n_counts; i += 256) mine += uint32_t(__ldcg(a.counts + i));
+    mine = __reduce_add_sync(0xFFFFFFFFu, mine);
+    if ((threadIdx.x & 31) == 0) atomicAdd(&total, mine);
+    __syncthreads();
+    if (step_takes_all(a, total)) return;
     constexpr int ES = DT == kBF16 ? 2 : 4, PER = 16 / ES;
     const int row = blockIdx.y;
     if (step_row_part(a, row) < 0) return;
@@ -166,9 +179,8 @@ struct StepShared {
     };
 };
 
-// The block's share of the union: its n tokens to sh.list; the longest share of any block to *most. A union of at least three
-// quarters of the vocabulary is taken for all of it (*all): boxes of rows by tiled copies come at the memory's rate, rows one by
-// one at 80 % of it. All threads; ends with a barrier.
+// The block's share of the union: its n tokens to sh.list; the longest share of any block to *most, whether all tokens are taken
+// to *all. All threads; ends with a barrier.
 template <int THREADS>
 __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh, int share, int shares, bool* all, int* most) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -192,7 +204,7 @@ __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh,
         if (w < warp) before += o;
         total += o;
     }
-    *all = int64_t(total) * 4 >= int64_t(a.V) * 3;
+    *all = step_takes_all(a, total);
     if (*all) total = a.V;
     // equal parts, the first `more` of them a token longer
     const uint32_t each = total / uint32_t(shares), more = total - each * uint32_t(shares);
@@ -269,55 +281,60 @@ __device__ __forceinline__ void step_bits(const HeadStepArgs& a, const StepShare
     }
 }
 
-// The scores of 128 tokens under the rows of the batch: a lane has a token, a column is a row; by way of shared memory a lane
-// has a row (32 c + lane) and the warp's 32 tokens, and keeps that row's state.
+// The scores of a warp's 32 tokens under the rows of the batch: a lane has a token, a column is a row; by way of shared memory a
+// lane has a row (32 c + lane) and all of the tokens, and keeps that row's state. The loops stay short: a block comes here four
+// times, and straight code cost more in instruction fetches than it saved.
 template <bool MX, int W>
-__device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& sh, int quad, float back, const int32_t* list, uint32_t tmem,
-                                            int token, const uint32_t (&bits)[W], Partial (&state)[W], int lane) {
+__device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& sh, int quad, float back, const int32_t* list, int tokens,
+                                            bool all, uint32_t tmem, const uint32_t (&bits)[W], Partial (&state)[W], int lane) {
     float* turn = sh.turn[quad];
 #pragma unroll
     for (int c = 0; c < W; ++c) {
         if (32 * c >= a.B) break;
-        uint32_t v[32];
-        tmem_ld32(tmem + 32 * c, v);
-        tmem_wait_ld();
-        if (MX) {
+        const int rows = min(32, a.B - 32 * c);
+        {
+            uint32_t v[32];
+            __syncwarp();
+            tmem_ld32(tmem + 32 * c, v);
+            tmem_wait_ld();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * sh.back[32 * c + j] * back);
+            for (int j = 0; j < 32; ++j)
+                turn[j * 33 + lane] = (bits[c] >> j) & 1u ? (MX ? __uint_as_float(v[j]) * sh.back[32 * c + j] * back : __uint_as_float(v[j]))
+                                                          : -INFINITY;
         }
-        if (a.logits) {
-            const int n = min(32, a.B - 32 * c);
-            if (a.logits_dtype == kBF16) {
-                uint16_t* p = static_cast<uint16_t*>(a.logits) + 32 * c * a.logits_stride + token;
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (j < n && ((bits[c] >> j) & 1u)) p[j * a.logits_stride] = uint16_t(bf16_pair(__uint_as_float(v[j]), 0.f));
-            } else {
-                float* p = static_cast<float*>(a.logits) + 32 * c * a.logits_stride + token;
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (j < n && ((bits[c] >> j) & 1u)) p[j * a.logits_stride] = __uint_as_float(v[j]);
-            }
-        }
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < 32; ++j) turn[j * 33 + lane] = (bits[c] >> j) & 1u ? __uint_as_float(v[j]) : -INFINITY;
         const uint32_t has = warp_transpose32(bits[c], lane);
         __syncwarp();
+        if (a.logits) {
+            const uint32_t write = all ? (lane < tokens ? sh.valid[c] : 0u) : bits[c];
+            const int64_t at = 32 * c * a.logits_stride + (lane < tokens ? list[lane] : 0);
+            if (a.logits_dtype == kBF16) {
+                uint16_t* p = static_cast<uint16_t*>(a.logits) + at;
+#pragma unroll 4
+                for (int j = 0; j < rows; ++j, p += a.logits_stride)
+                    if ((write >> j) & 1u) *p = uint16_t(bf16_pair(turn[j * 33 + lane], 0.f));
+            } else {
+                float* p = static_cast<float*>(a.logits) + at;
+#pragma unroll 4
+                for (int j = 0; j < rows; ++j, p += a.logits_stride)
+                    if ((write >> j) & 1u) *p = turn[j * 33 + lane];
+            }
+        }
+        const float* mine = turn + lane * 33;
         float m = -INFINITY;
         int at = __ffs(has) - 1;
-#pragma unroll
+#pragma unroll 8
         for (int j = 0; j < 32; ++j) {
-            const float z = turn[lane * 33 + j];
-            v[j] = __float_as_uint(z);
+            const float z = mine[j];
             at = z > m ? j : at;
             m = fmaxf(m, z);
         }
         const float ref = fmaxf(m, kRefFloor);
-        float s[2] = {};
+        float s[4] = {};
+#pragma unroll 2
+        for (int j = 0; j < 32; j += 4)
 #pragma unroll
-        for (int j = 0; j < 32; ++j) s[j & 1] += ex2f((__uint_as_float(v[j]) - ref) * kLog2e);
-        if (has) partial_merge(state[c].m, state[c].s, state[c].pos, m, s[0] + s[1], list[at]);
+            for (int k = 0; k < 4; ++k) s[k] += ex2f((mine[j + k] - ref) * kLog2e);
+        if (has) partial_merge(state[c].m, state[c].s, state[c].pos, m, (s[0] + s[1]) + (s[2] + s[3]), list[at]);
         __syncwarp();
     }
 }
@@ -394,7 +411,7 @@ __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int mos
     l.rows = most > 128 ? 256 : (max(most, 1) + 31) & ~31;
     l.atoms = 1;
     int shift = 0;
-    while (shift < 3 && l.atoms < a.row_atoms && 2 * l.atoms * (l.rows + X * a.N) * kStepAtom <= (36u << 10)) {
+    while (shift < 3 && l.atoms < a.row_atoms && 2 * l.atoms * (l.rows + X * a.N) * kStepAtom <= (48u << 10)) {
         l.atoms *= 2;
         ++shift;
     }
@@ -416,13 +433,12 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     const uint32_t columns = MX ? 512 : 4 * a.N <= 128 ? 128 : 4 * a.N <= 256 ? 256 : 512;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStepStages; ++i) {
-            mbar_init(&sh.full[i], 1 + 256);          // tiled copies, and every thread that fetches weights
-            mbar_init(&sh.empty[i], MX ? 1 + 8 : 1);  // the products, and the warps that take weights apart
+            mbar_init(&sh.empty[i], MX ? 1 + 16 : 1);  // the products, and the pieces in which weights are taken apart
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.sums_full[i], 1);
             mbar_init(&sh.sums_empty[i], 4);
-            mbar_init(&sh.w_full[i], 8);
+            mbar_init(&sh.w_full[i], 16);
             mbar_init(&sh.w_empty[i], 1);
         }
         mbar_init_fence();
@@ -452,7 +468,14 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         bool all;
         int most;
         const int n = step_share<kThreads>(a, sh, round * gridDim.x + blockIdx.x, shares, &all, &most);
-        const StepLayout l = step_layout<MX>(a, most);  // (the same in every round)
+        const StepLayout l = step_layout<MX>(a, most);  // (the same in every round, as is `all`)
+        if (round == 0) {
+            if (threadIdx.x == 0) {
+                for (int i = 0; i < kStepStages; ++i) mbar_init(&sh.full[i], all ? 1 : 1 + 256);  // ... and every thread that fetches weights
+                mbar_init_fence();
+            }
+            __syncthreads();
+        }
         const int per_group = 128 * l.tiles, groups = (n + per_group - 1) / per_group;
         auto next = [&] {
             if (++stage == l.stages) {
@@ -502,7 +525,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                         break;
                     }
                     // (weights were written as ordinary shared memory: the products read it another way)
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    if (!all) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     tmem_fence_after();
                     const int atoms = min(l.atoms, a.row_atoms - s * l.atoms);
                     const uint64_t dw = mma_desc<false>(smem + uint32_t(stage) * l.bytes);
@@ -539,20 +562,20 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 if (elect_one()) mma_commit<1>(&sh.sums_full[it & 1]);
                 __syncwarp();
             }
-        } else if (MX && warp >= 16) {
-            // a thread a token: set 0 takes the first half of an atom's 256 weights, set 1 the second
-            const int half = (warp - 16) >> 2, row = (warp & 3) * 32 + lane;
+        } else if (MX && warp >= (all ? 8 : 16)) {
+            // a thread a token; an atom's 256 weights in four pieces, one to a set of four warps, or two where weights are also fetched
+            const int set = ((warp - 8) >> 2) ^ 2, sets = all ? 4 : 2, row = (warp & 3) * 32 + lane;
             for (int g = 0; g < groups && ok; ++g) {
-                const int tiles = min(l.tiles, (n - g * per_group + 127) / 128);
+                const int tiles = min(l.tiles, (n - g * per_group + 127) / 128), blocks = a.bytes / 16;
                 const uint8_t* scales[2];
-                uint32_t scale[2], scale_next[2], largest[2];
+                uint2 scale[2], scale_next[2];
+                uint32_t largest[2];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const int at = g * per_group + t * 128 + row;
                     scales[t] = t < tiles && at < n ? a.scales + int64_t(sh.list[at]) * a.scale_stride : nullptr;
-                    largest[t] = scales[t] ? mx_largest(scales[t], a.bytes / 16) : 0;
-                    if (scales[t]) scales[t] += 4 * half;
-                    scale_next[t] = scales[t] && 4 * half < a.bytes / 16 ? ld_after_wait(reinterpret_cast<const uint32_t*>(scales[t])) : 0;
+                    largest[t] = scales[t] ? mx_largest(scales[t], blocks) : 0;
+                    scale_next[t] = scales[t] ? *reinterpret_cast<const uint2*>(scales[t]) : make_uint2(0, 0);
                 }
                 for (int s = 0; s < l.steps && ok; ++s) {
                     if (!mbar_wait(&sh.full[stage], phase)) {
@@ -561,54 +584,58 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     }
                     const int atoms = min(l.atoms, a.row_atoms - s * l.atoms);
                     for (int p = 0; p < atoms; ++p) {
-                        const int atom = s * l.atoms + p, left = a.bytes / 16 - 8 * atom - 4 * half;  // blocks from here on
+                        const int atom = s * l.atoms + p;
 #pragma unroll
                         for (int t = 0; t < 2; ++t) {
                             scale[t] = scale_next[t];
-                            if (scales[t] && left > 8)
-                                scale_next[t] = ld_after_wait(reinterpret_cast<const uint32_t*>(scales[t] + 8 * (atom + 1)));
+                            if (scales[t] && 8 * atom + 8 < blocks)
+                                scale_next[t] = *reinterpret_cast<const uint2*>(scales[t] + 8 * (atom + 1));
                         }
 #pragma unroll
                         for (int t = 0; t < 2; ++t) {
                             if (t >= tiles) break;
                             const uint32_t q = unit & 1;
-                            if (!mbar_wait(&sh.w_empty[q], ((unit >> 1) & 1) ^ 1)) ok = false;
-                            tmem_fence_after();
                             const int r = t * 128 + row;
                             const uint32_t at = smem + uint32_t(stage) * l.bytes + (uint32_t(p) * l.rows + min(r, l.rows - 1)) * kStepAtom;
+                            if (!mbar_wait(&sh.w_empty[q], ((unit >> 1) & 1) ^ 1)) ok = false;
+                            tmem_fence_after();
+#pragma unroll 1
+                            for (int c = set; c < 4; c += sets) {
+                                uint32_t w[8], v[32];
 #pragma unroll
-                            for (int b = 0; b < 4; b += 2) {
-                                uint32_t v[32];
+                                for (int k = 0; k < 2; ++k)
+                                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                                 : "=r"(w[4 * k]), "=r"(w[4 * k + 1]), "=r"(w[4 * k + 2]), "=r"(w[4 * k + 3])
+                                                 : "r"(at + (uint32_t((2 * c + k) ^ (r & 7)) << 4)));
+                                const uint32_t two = (c & 2 ? scale[t].y : scale[t].x) >> (c & 1 ? 16 : 0);
 #pragma unroll
                                 for (int k = 0; k < 2; ++k) {
-                                    uint32_t w[4];
-                                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                                                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                                                 : "r"(at + (uint32_t((4 * half + b + k) ^ (r & 7)) << 4)));
                                     // (behind the row there is no scale, and the weights are zeros)
-                                    const uint32_t sc = mx_scale_pair(b + k < left ? (scale[t] >> (8 * (b + k))) & 255u : 0u, largest[t]);
+                                    const uint32_t sc = mx_scale_pair(8 * atom + 2 * c + k < blocks ? (two >> (8 * k)) & 255u : 0u, largest[t]);
 #pragma unroll
-                                    for (int i = 0; i < 4; ++i) mx_word(w[i], sc, v + 16 * k + 4 * i);
+                                    for (int i = 0; i < 4; ++i) mx_word(w[4 * k + i], sc, v + 16 * k + 4 * i);
                                 }
-                                tmem_st32(tmem + 256 + 128 * q + 64 * half + 16 * b + (uint32_t((warp & 3) * 32) << 16), v);
+                                __syncwarp();
+                                tmem_st32(tmem + 256 + 128 * q + 32 * c + (uint32_t((warp & 3) * 32) << 16), v);
+                                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                                tmem_fence_before();
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(&sh.w_full[q]);
                             }
-                            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                            tmem_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&sh.w_full[q]);
                             ++unit;
                         }
                     }
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.empty[stage]);
+                    if (lane == 0)
+                        for (int c = set; c < 4; c += sets) mbar_arrive(&sh.empty[stage]);
                     next();
                 }
             }
         } else if (warp >= 8) {
             // eight lanes bring the 128 bytes of a row's atom, the eight warps 32 rows at a time
             const int chunk = lane & 7, row = (warp - 8) * 4 + (lane >> 3);
-            for (int g = 0; g < groups && ok; ++g) {
-                const int rows = all ? 0 : min(n - g * per_group, per_group);
+            for (int g = all ? groups : 0; g < groups && ok; ++g) {  // (tiled copies bring them where all are taken)
+                const int rows = min(n - g * per_group, per_group);
                 const char* from[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -641,15 +668,14 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             for (int g = 0; g < groups; ++g) {
                 const int it = groups_done + g;
                 uint32_t bits[2][W];
-                int token[2];
                 float back[2];  // what brings a token's products back
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const int at = g * per_group + t * 128 + quad * 32 + lane;
                     const bool have = t < l.tiles && at < n;
-                    token[t] = have ? sh.list[at] : 0;
-                    step_bits(a, sh, token[t], have, bits[t]);
-                    back[t] = MX && have ? mx_scale(mx_largest(a.scales + int64_t(token[t]) * a.scale_stride, a.bytes / 16)) : 1.f;
+                    const int token = have ? sh.list[at] : 0;
+                    step_bits(a, sh, token, have, bits[t]);
+                    back[t] = MX && have ? mx_scale(mx_largest(a.scales + int64_t(token) * a.scale_stride, a.bytes / 16)) : 1.f;
                 }
                 if (!mbar_wait(&sh.sums_full[it & 1], (it >> 1) & 1)) {
                     ok = false;
@@ -660,8 +686,8 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 for (int t = 0; t < 2; ++t) {
                     const int at = g * per_group + t * 128 + quad * 32;
                     if (t < l.tiles && at < n)
-                        step_scores<MX>(a, sh, quad, back[t], sh.list + at, tmem + uint32_t((it & 1) * l.tiles + t) * a.N + (uint32_t(quad * 32) << 16),
-                                    token[t], bits[t], state, lane);
+                        step_scores<MX>(a, sh, quad, back[t], sh.list + at, n - at, all,
+                                        tmem + uint32_t((it & 1) * l.tiles + t) * a.N + (uint32_t(quad * 32) << 16), bits[t], state, lane);
                 }
                 tmem_fence_before();
                 __syncwarp();
