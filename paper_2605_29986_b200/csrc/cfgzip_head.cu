@@ -63,7 +63,7 @@ struct HeadSpace {
     // step
     uint16_t* half;
     float* back;
-    uint32_t *mask, *any, *ticket;
+    uint32_t *mask, *any, *bits, *ticket;
     int32_t* counts;
     Partial* states;
     // loss
@@ -102,11 +102,12 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
     if (op == CFGZIP_HEAD_STEP) {
         s.mask = c.take<uint32_t>(n * ceil_div(h->V, 32));
         s.any = c.take<uint32_t>(ceil_div(h->V, 32));
+        s.bits = c.take<uint32_t>(std::min<int64_t>(up(n, 32), kStepRows) * ceil_div(h->V, 32));
         s.counts = c.take<int32_t>(ceil_div(h->V, 32 * kUnionWords));
         s.ticket = c.take<uint32_t>(1);
         s.states = c.take<Partial>(std::min<int64_t>(n, kStepRows) * kStepBlocks);
         if (h->dtype == CFGZIP_MXFP4) {
-            s.half = c.take<uint16_t>(std::min<int64_t>(n, kStepRowsMx) * h->H);
+            s.half = c.take<uint16_t>(std::min<int64_t>(n, kStepRowsMx) * up(h->H, 2 * int(kStepAtom)));
             s.back = c.take<float>(kStepRowsMx);
         }
     } else if (op == CFGZIP_HEAD_LOSS) {
@@ -132,6 +133,20 @@ int tensor_map(cfgzip_ctx* ctx, CUtensorMap* map, const void* p, int64_t rows, i
     const cuuint32_t steps[2] = {1, 1};
     if (!ctx->encode_tiled ||
         ctx->encode_tiled(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, boxes, steps,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return CFGZIP_E_CUDA;
+    return CFGZIP_OK;
+}
+
+// Hidden states [rows, stride] (stride a multiple of 256) for tiled copies that bring 256 k of all rows, 64 after 64.
+int tensor_map_by_64(cfgzip_ctx* ctx, CUtensorMap* map, const uint16_t* p, int64_t rows, int64_t stride, int box) {
+    const cuuint64_t dims[3] = {64, cuuint64_t(rows), cuuint64_t(stride) / 64};
+    const cuuint64_t strides[2] = {cuuint64_t(stride) * 2, 128};
+    const cuuint32_t boxes[3] = {64, cuuint32_t(box), 4};
+    const cuuint32_t steps[3] = {1, 1, 1};
+    if (!ctx->encode_tiled ||
+        ctx->encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint16_t*>(p), dims, strides, boxes, steps,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return CFGZIP_E_CUDA;
@@ -164,7 +179,7 @@ int dequantize(cfgzip_ctx* ctx, const cfgzip_head* h, int32_t t0, int32_t n, uin
 int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const uint16_t* hidden, int64_t hidden_stride,
              const HeadSpace& w, cudaStream_t st) {
     const bool mx = head->dtype == CFGZIP_MXFP4;
-    CUtensorMap map_x, map_w;
+    CUtensorMap map_x, map_w, map_box;
     int rc;
     a.N = up(a.B, 32);
     a.weight = head->weight;
@@ -177,10 +192,14 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
         a.hidden = hidden;
         a.hidden_stride = hidden_stride;
         a.half = w.half;
+        a.half_stride = up(head->H, 2 * int(kStepAtom));
         a.back = w.back;
     }
-    if ((rc = tensor_map(ctx, &map_x, mx ? w.half : hidden, a.B, head->H, mx ? head->H : hidden_stride, a.N)) != CFGZIP_OK ||
-        (rc = tensor_map(ctx, &map_w, head->weight, head->V, mx ? a.bytes : head->H, head->row_stride, kStepBox, mx)) != CFGZIP_OK)
+    rc = mx ? tensor_map_by_64(ctx, &map_x, w.half, a.B, a.half_stride, a.N)
+            : tensor_map(ctx, &map_x, hidden, a.B, head->H, hidden_stride, a.N);
+    const int cols = mx ? a.bytes : head->H;
+    if (rc != CFGZIP_OK || (rc = tensor_map(ctx, &map_w, head->weight, head->V, cols, head->row_stride, 128, mx)) != CFGZIP_OK ||
+        (rc = tensor_map(ctx, &map_box, head->weight, head->V, cols, head->row_stride, kStepBox, mx)) != CFGZIP_OK)
         return rc;
     a.n_counts = ceil_div(a.VW, kUnionWords);
     if ((rc = launch(ctx, k_head_union, dim3(unsigned(a.n_counts + (mx ? a.B : 0))), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
@@ -192,11 +211,11 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
     }
     const unsigned blocks = unsigned(std::min(ctx->sm_count, kStepBlocks));
     a.rounds = ceil_div(ceil_div(a.V, blocks), kStepShare);
-    a.smem = 184 << 10;
+    a.smem = 182 << 10;
     const size_t smem = size_t(a.smem) + 1024 + kStepTile;  // (products read 128 rows, also where fewer are there)
     auto kern = mx ? k_head_step<true> : k_head_step<false>;
     if ((rc = ensure_smem(ctx, kern, smem)) != CFGZIP_OK) return rc;
-    return launch(ctx, kern, dim3(blocks), dim3((mx ? kStepWarpsMx : kStepWarps) * 32), smem, st, a, map_x, map_w);
+    return launch(ctx, kern, dim3(blocks), dim3((mx ? kStepWarpsMx : kStepWarps) * 32), smem, st, a, map_x, map_w, map_box);
 }
 
 }  // namespace
@@ -282,6 +301,7 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
         s.VW = ps.VW;
         s.H = head->H;
         s.any = w.any;
+        s.bits = w.bits;
         s.counts = w.counts;
         s.ticket = w.ticket;
         s.part = w.states;

@@ -254,7 +254,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                 const MmaTile t = mma_tile(a, i);
                 const int m = t.m * kMmaTile + int(rank) * 128, n = t.n * kMmaTile + int(rank) * 128;
                 for (int k = t.k0; k < t.k1; ++k) {
-                    if (!mbar_wait_cluster(&empty[r.stage], r.phase ^ 1)) {
+                    if (!ring_wait<true>(&empty[r.stage], r.phase ^ 1)) {
                         ok = false;
                         break;
                     }
@@ -284,13 +284,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             for (int i = pair; i < tiles && ok; i += pairs, ++it) {
                 const MmaTile t = mma_tile(a, i);
                 const uint32_t d = tmem + (it & 1) * 256;
-                if (!mbar_wait_cluster(&sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
+                if (!ring_wait<true>(&sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
                     ok = false;
                     break;
                 }
                 tmem_fence_after();
                 for (int k = t.k0; k < t.k1; ++k) {
-                    if (!mbar_wait_cluster(&full[r.stage], r.phase)) {
+                    if (!ring_wait<true>(&full[r.stage], r.phase)) {
                         ok = false;
                         break;
                     }
@@ -321,7 +321,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             const bool valid = row < a.rows;
             uint32_t bits[8];
             if (KIND == kMmaLoss || KIND == kMmaGrad) tile_mask(a, valid ? row : a.rows - 1, t.n * kMmaTile, bits);
-            if (!mbar_wait_cluster(&sums_full[set], (it >> 1) & 1)) {
+            if (!ring_wait<true>(&sums_full[set], (it >> 1) & 1)) {
                 ok = false;
                 break;
             }

@@ -15,7 +15,7 @@ constexpr int kStepRowsMx = 64;    // ... from a 4-bit head: the hidden states a
 constexpr int kStepShare = 2048;   // tokens a block lists at a time
 constexpr int kStepWarps = 16;     // tiled copies, products, tensor memory, idle, four that read the scores, eight that fetch weights
 constexpr int kStepWarpsMx = 24;   // ... and two sets of four that turn 4-bit weights into bf16
-constexpr int kStepBox = 32;       // rows of weights a tiled copy brings
+constexpr int kStepBox = 32;       // rows of weights a small tiled copy brings (a large one: 128)
 constexpr int kStepStages = 12;    // most stages
 constexpr uint32_t kStepAtom = 128;             // bytes of a weight row in an atom, the width of the swizzle
 constexpr uint32_t kStepTile = 128 * kStepAtom; // an atom of 128 tokens
@@ -38,9 +38,11 @@ struct HeadStepArgs {
     int32_t rounds;
     const uint16_t* hidden;  // 4-bit heads: rows brought to at most 2^15 and copied as f16 to `half`
     int64_t hidden_stride;
-    uint16_t* half;        // [B, H]
+    uint16_t* half;        // [B, half_stride], zeros behind H
+    int32_t half_stride;   // H rounded up to an atom's weights
     float* back;           // [B] what brings a row's products back
     uint32_t* any;         // [VW] union of the rows' masks
+    uint32_t* bits;        // [(B + 31) / 32, 32 VW] what 32 rows allow of a token, a bit a row
     int32_t* counts;       // tokens of it in every kUnionWords words
     int32_t n_counts;
     uint32_t* ticket;
@@ -79,8 +81,8 @@ __device__ __forceinline__ void half_row(const HeadStepArgs& a, int row) {
     const int e = min(max(int(top >> 7), 15), 254);  // exponent of the largest, + 127
     const float up = __uint_as_float(uint32_t(268 - e) << 23);  // 2^(14 - (e - 127))
     if (threadIdx.x == 0) a.back[row] = __uint_as_float(uint32_t(max(e - 14, 1)) << 23);
-    for (int i = threadIdx.x; i < vectors; i += 256) {
-        const uint4 v = ld_after_wait(x + i);
+    for (int i = threadIdx.x; i < a.half_stride / 8; i += 256) {
+        const uint4 v = i < vectors ? ld_after_wait(x + i) : make_uint4(0, 0, 0, 0);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
         uint32_t o[4];
 #pragma unroll
@@ -88,11 +90,12 @@ __device__ __forceinline__ void half_row(const HeadStepArgs& a, int row) {
             asm("cvt.rn.f16x2.f32 %0, %1, %2;"
                 : "=r"(o[j])
                 : "f"(__uint_as_float(w[j] & 0xFFFF0000u) * up), "f"(__uint_as_float(w[j] << 16) * up));
-        reinterpret_cast<uint4*>(a.half + int64_t(row) * a.H)[i] = make_uint4(o[0], o[1], o[2], o[3]);
+        reinterpret_cast<uint4*>(a.half + int64_t(row) * a.half_stride)[i] = make_uint4(o[0], o[1], o[2], o[3]);
     }
 }
 
-// Union of the rows' masks, 32 words by a block: a warp ORs every eighth row. Blocks behind those take a row of hidden states.
+// Union of the rows' masks, 32 words by a block, and the masks turned from 32 tokens of a row to 32 rows of a token: a warp takes
+// four words, a lane a row. Blocks behind those take a row of hidden states.
 __global__ void __launch_bounds__(256) k_head_union(const HeadStepArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -102,17 +105,30 @@ __global__ void __launch_bounds__(256) k_head_union(const HeadStepArgs a) {
         half_row(a, int(blockIdx.x) - a.n_counts);
         return;
     }
-    uint32_t any = 0;
-    if (word < a.VW)
-#pragma unroll 4
-        for (int row = warp; row < a.B; row += 8)
-            if (step_row_part(a, row) >= 0) any |= ld_after_wait(a.mask + row * a.mask_stride + word);
-    __shared__ uint32_t sh[8][32];
-    sh[warp][lane] = any;
+    __shared__ uint32_t sh[32];
+    if (threadIdx.x < 32) sh[threadIdx.x] = 0;
+    __syncthreads();
+    for (int c = 0; 32 * c < a.B; ++c) {
+        const int row = 32 * c + lane;
+        const bool has = row < a.B && step_row_part(a, row) >= 0;
+        const uint32_t* p = a.mask + int64_t(row) * a.mask_stride;
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int at = blockIdx.x * kUnionWords + 4 * warp + k;
+            w[k] = has && at < a.VW ? ld_after_wait(p + at) : 0u;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int at = blockIdx.x * kUnionWords + 4 * warp + k;
+            const uint32_t b = warp_transpose32(w[k], lane), any = __ballot_sync(0xFFFFFFFFu, b != 0);
+            if (at < a.VW) a.bits[(int64_t(c) * a.VW + at) * 32 + lane] = b;
+            if (lane == 0 && any) sh[4 * warp + k] |= any;
+        }
+    }
     __syncthreads();
     if (warp) return;
-#pragma unroll
-    for (int w = 1; w < 8; ++w) any |= sh[w][lane];
+    const uint32_t any = sh[lane];
     if (word < a.VW) a.any[word] = any;
     const int n = __reduce_add_sync(0xFFFFFFFFu, __popc(any));
     if (lane == 0) a.counts[blockIdx.x] = n;
@@ -160,6 +176,12 @@ __device__ __forceinline__ void tma_load(uint32_t dst_smem, const void* tensor_m
         "l"(tensor_map), "r"(x), "r"(y), "r"(smem_u32(bar))
         : "memory");
 }
+__device__ __forceinline__ void tma_load3(uint32_t dst_smem, const void* tensor_map, int x, int y, int z, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst_smem),
+        "l"(tensor_map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+        : "memory");
+}
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
@@ -169,7 +191,8 @@ struct StepShared {
     uint32_t tmem;
     uint32_t valid[kStepRows / 32];  // rows that have a partition
     int32_t entries, is_last;
-    float back[kStepRowsMx];
+    float back[kStepRowsMx];         // 4-bit heads: what brings a row's products back
+    float back_token[2][128];        // ... and a token's
     int32_t scan[kStepWarpsMx];
     int32_t list[kStepShare];        // the block's tokens, ascending
     union alignas(16) {
@@ -266,21 +289,6 @@ __device__ __forceinline__ void step_finish_row(const HeadStepArgs& a, int row, 
     if (!any) atomicAdd(a.status, 1);
 }
 
-// What the rows allow of one token, a bit a row.
-template <int W>
-__device__ __forceinline__ void step_bits(const HeadStepArgs& a, const StepShared& sh, int token, bool have, uint32_t (&bits)[W]) {
-    const uint32_t* p = a.mask + (token >> 5);
-#pragma unroll
-    for (int c = 0; c < W; ++c) {
-        uint32_t w = 0;
-        const int n = min(32, a.B - 32 * c);
-        if (have)
-#pragma unroll 8
-            for (int j = 0; j < n; ++j) w |= ((ld_after_wait(p + (32 * c + j) * a.mask_stride) >> (token & 31)) & 1u) << j;
-        bits[c] = w & sh.valid[c];
-    }
-}
-
 // The scores of a warp's 32 tokens under the rows of the batch: a lane has a token, a column is a row; by way of shared memory a
 // lane has a row (32 c + lane) and all of the tokens, and keeps that row's state. The loops stay short: a block comes here four
 // times, and straight code cost more in instruction fetches than it saved.
@@ -358,8 +366,9 @@ __device__ __forceinline__ void mx_word(uint32_t w, uint32_t scale, uint32_t* ou
 }
 // 2^(byte - largest) twice, as f16
 __device__ __forceinline__ uint32_t mx_scale_pair(uint32_t byte, uint32_t largest) {
-    const int d = int(byte) - int(largest);
-    const uint32_t b = d >= -14 ? uint32_t(15 + d) << 10 : d >= -24 ? 1u << (24 + d) : 0u;
+    const int e = int(byte) - int(largest) + 15;  // exponent field of a normal number
+    if (!__any_sync(0xFFFFFFFFu, e < 1)) return uint32_t(e) * 0x04000400u;
+    const uint32_t b = e >= 1 ? uint32_t(e) << 10 : e >= -9 ? 1u << (9 + e) : 0u;
     return b | b << 16;
 }
 // Largest scale byte of a row of n blocks (rows start on 16 bytes).
@@ -396,9 +405,12 @@ __device__ __forceinline__ void mma_f16_from_tmem(uint32_t d, uint32_t a, uint64
         : "memory");
 }
 
-// How a block's stages are laid out: `tiles` tiles of 128 tokens side by side where it has more than 128, otherwise as many rows
-// as it has tokens (rounded up to 32) and so many more atoms of them. A product takes 128 rows all the same: what it reads behind
-// the rows that are there gives sums that nobody reads.
+// How a block's stages are laid out: for blocks of more than 128 tokens two tiles of 128 side by side, which share the hidden
+// states (one from a 4-bit head, whose tiles come one by one through tensor memory); otherwise as many rows as there are tokens
+// (rounded up to 32) and so many more atoms of them. A product takes 128 rows all the same: what it reads behind the rows that are
+// there gives sums that nobody reads.
+template <bool MX>
+constexpr int kStepTiles = MX ? 1 : 2;
 struct StepLayout {
     int tiles, rows, atoms, steps, stages;
     uint32_t x_at, bytes;
@@ -407,8 +419,8 @@ template <bool MX>
 __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int most) {
     constexpr int X = MX ? 4 : 1;  // atoms of hidden states to an atom of weights
     StepLayout l;
-    l.tiles = most > 128 ? 2 : 1;
-    l.rows = most > 128 ? 256 : (max(most, 1) + 31) & ~31;
+    l.tiles = most > 128 ? kStepTiles<MX> : 1;
+    l.rows = most > 128 ? 128 * kStepTiles<MX> : (max(most, 1) + 31) & ~31;
     l.atoms = 1;
     int shift = 0;
     while (shift < 3 && l.atoms < a.row_atoms && 2 * l.atoms * (l.rows + X * a.N) * kStepAtom <= (48u << 10)) {
@@ -424,8 +436,10 @@ __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int mos
 
 template <bool MX>
 __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
-    k_head_step(const __grid_constant__ HeadStepArgs a, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w) {
+    k_head_step(const __grid_constant__ HeadStepArgs a, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                const __grid_constant__ CUtensorMap map_box) {
     constexpr int kThreads = (MX ? kStepWarpsMx : kStepWarps) * 32, X = MX ? 4 : 1, W = (MX ? kStepRowsMx : kStepRows) / 32;
+    constexpr int T = kStepTiles<MX>;
     extern __shared__ char smem_raw[];
     __shared__ __align__(16) StepShared sh;
     const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -436,7 +450,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             mbar_init(&sh.empty[i], MX ? 1 + 16 : 1);  // the products, and the pieces in which weights are taken apart
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&sh.sums_full[i], 1);
+            mbar_init(&sh.sums_full[i], MX ? 1 + 4 : 1);  // the products, and what brings them back
             mbar_init(&sh.sums_empty[i], 4);
             mbar_init(&sh.w_full[i], 16);
             mbar_init(&sh.w_empty[i], 1);
@@ -444,6 +458,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         mbar_init_fence();
         prefetch_tensor_map(&map_x);
         prefetch_tensor_map(&map_w);
+        prefetch_tensor_map(&map_box);
     }
     if (warp == 2) tmem_alloc<1>(&sh.tmem, columns);
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -485,24 +500,33 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         };
         if (warp == 0) {
             for (int g = 0; g < groups && ok; ++g) {
-                // boxes of the group's rows, where the tiled copies bring the weights too
-                const int boxes = all ? (min(n - g * per_group, per_group) + kStepBox - 1) / kStepBox : 0;
-                const int token = all ? sh.list[0] + g * per_group : 0;
+                // Where the tiled copies bring the weights too: whole tiles by one copy each (a copy takes some 130 cycles to go out,
+                // whatever it brings up to 4 KB), the rest in small boxes.
+                const int rows = all ? min(n - g * per_group, per_group) : 0, token = all ? sh.list[0] + g * per_group : 0;
+                int large = rows / 128, small = (rows - 128 * large + kStepBox - 1) / kStepBox;
+                if (small == 128 / kStepBox) {
+                    ++large;
+                    small = 0;
+                }
                 for (int s = 0; s < l.steps; ++s) {
                     const int first = s * l.atoms, atoms = min(l.atoms, a.row_atoms - first);
-                    if (!mbar_wait(&sh.empty[stage], phase ^ 1)) {
+                    if (!ring_wait(&sh.empty[stage], phase ^ 1)) {
                         ok = false;
                         break;
                     }
                     const uint32_t at = smem + uint32_t(stage) * l.bytes;
                     if (elect_one()) {
-                        mbar_expect_tx(&sh.full[stage], uint32_t(atoms) * (X * a.N + boxes * kStepBox) * kStepAtom);
-                        for (int p = 0; p < atoms; ++p)
-                            for (int i = 0; i < boxes; ++i)
-                                tma_load(at + uint32_t(p * l.rows + i * kStepBox) * kStepAtom, &map_w, (first + p) * (MX ? 128 : 64),
-                                         token + i * kStepBox, &sh.full[stage]);
-                        for (int x = 0; x < atoms * X; ++x)
-                            tma_load(at + l.x_at + uint32_t(x) * a.N * kStepAtom, &map_x, (first * X + x) * 64, 0, &sh.full[stage]);
+                        mbar_expect_tx(&sh.full[stage], uint32_t(atoms) * (X * a.N + large * 128 + small * kStepBox) * kStepAtom);
+                        for (int p = 0; p < atoms; ++p) {
+                            const int x = (first + p) * (MX ? 128 : 64);
+                            uint32_t to = at + uint32_t(p * l.rows) * kStepAtom;
+                            for (int i = 0; i < large; ++i, to += kStepTile) tma_load(to, &map_w, x, token + 128 * i, &sh.full[stage]);
+                            for (int i = 0; i < small; ++i, to += kStepBox * kStepAtom)
+                                tma_load(to, &map_box, x, token + 128 * large + i * kStepBox, &sh.full[stage]);
+                            to = at + l.x_at + uint32_t(p * X * a.N) * kStepAtom;
+                            if (MX) tma_load3(to, &map_x, 0, 0, (first + p) * X, &sh.full[stage]);
+                            else tma_load(to, &map_x, x, 0, &sh.full[stage]);
+                        }
                     }
                     __syncwarp();
                     next();
@@ -513,14 +537,14 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             const uint32_t w_step = uint32_t(l.rows) * kStepAtom >> 4;
             for (int g = 0; g < groups && ok; ++g) {
                 const int it = groups_done + g, tiles = min(l.tiles, (n - g * per_group + 127) / 128);
-                if (!mbar_wait(&sh.sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
+                if (!ring_wait(&sh.sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
                     ok = false;
                     break;
                 }
                 tmem_fence_after();
                 const uint32_t d0 = tmem + uint32_t(it & 1) * l.tiles * a.N;
                 for (int s = 0; s < l.steps && ok; ++s) {
-                    if (!mbar_wait(&sh.full[stage], phase)) {
+                    if (!ring_wait(&sh.full[stage], phase)) {
                         ok = false;
                         break;
                     }
@@ -531,21 +555,20 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     const uint64_t dw = mma_desc<false>(smem + uint32_t(stage) * l.bytes);
                     const uint64_t dx = mma_desc<false>(smem + uint32_t(stage) * l.bytes + l.x_at);
                     if (MX) {
-                        for (int p = 0; p < atoms; ++p)
-                            for (int t = 0; t < tiles; ++t, ++unit) {
-                                const uint32_t q = unit & 1;
-                                if (ok && !mbar_wait(&sh.w_full[q], (unit >> 1) & 1)) ok = false;
-                                tmem_fence_after();
-                                if (elect_one()) {
+                        for (int p = 0; p < atoms; ++p, ++unit) {
+                            const uint32_t q = unit & 1;
+                            if (ok && !ring_wait(&sh.w_full[q], (unit >> 1) & 1)) ok = false;
+                            tmem_fence_after();
+                            if (elect_one()) {
 #pragma unroll
-                                    for (int j = 0; j < 16; ++j)
-                                        mma_f16_from_tmem(d0 + t * a.N, tmem + 256 + 128 * q + 8 * j,
-                                                          dx + (4 * p + j / 4) * x_step + (j & 3) * kDescStep16<false>, idesc,
-                                                          s > 0 || p > 0 || j > 0);
-                                    mma_commit<1>(&sh.w_empty[q]);
-                                }
-                                __syncwarp();
+                                for (int j = 0; j < 16; ++j)
+                                    mma_f16_from_tmem(d0, tmem + 256 + 128 * q + 8 * j,
+                                                      dx + (4 * p + j / 4) * x_step + (j & 3) * kDescStep16<false>, idesc,
+                                                      s > 0 || p > 0 || j > 0);
+                                mma_commit<1>(&sh.w_empty[q]);
                             }
+                            __syncwarp();
+                        }
                         if (elect_one()) mma_commit<1>(&sh.empty[stage]);
                     } else if (elect_one()) {
                         for (int p = 0; p < atoms; ++p)
@@ -565,64 +588,56 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         } else if (MX && warp >= (all ? 8 : 16)) {
             // a thread a token; an atom's 256 weights in four pieces, one to a set of four warps, or two where weights are also fetched
             const int set = ((warp - 8) >> 2) ^ 2, sets = all ? 4 : 2, row = (warp & 3) * 32 + lane;
+            const int blocks = a.bytes / 16;
             for (int g = 0; g < groups && ok; ++g) {
-                const int tiles = min(l.tiles, (n - g * per_group + 127) / 128), blocks = a.bytes / 16;
-                const uint8_t* scales[2];
-                uint2 scale[2], scale_next[2];
-                uint32_t largest[2];
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const int at = g * per_group + t * 128 + row;
-                    scales[t] = t < tiles && at < n ? a.scales + int64_t(sh.list[at]) * a.scale_stride : nullptr;
-                    largest[t] = scales[t] ? mx_largest(scales[t], blocks) : 0;
-                    scale_next[t] = scales[t] ? *reinterpret_cast<const uint2*>(scales[t]) : make_uint2(0, 0);
+                const int token = g * 128 + row < n ? sh.list[g * 128 + row] : sh.list[0];
+                const uint8_t* scales = a.scales + int64_t(token) * a.scale_stride;
+                const uint32_t largest = mx_largest(scales, blocks);
+                uint2 scale, scale_next = *reinterpret_cast<const uint2*>(scales);
+                if (set == 0) {
+                    const int it = groups_done + g;
+                    if (!ring_wait(&sh.sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) ok = false;
+                    sh.back_token[it & 1][row] = mx_scale(largest);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.sums_full[it & 1]);
                 }
                 for (int s = 0; s < l.steps && ok; ++s) {
-                    if (!mbar_wait(&sh.full[stage], phase)) {
+                    if (!ring_wait(&sh.full[stage], phase)) {
                         ok = false;
                         break;
                     }
-                    const int atoms = min(l.atoms, a.row_atoms - s * l.atoms);
-                    for (int p = 0; p < atoms; ++p) {
-                        const int atom = s * l.atoms + p;
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) {
-                            scale[t] = scale_next[t];
-                            if (scales[t] && 8 * atom + 8 < blocks)
-                                scale_next[t] = *reinterpret_cast<const uint2*>(scales[t] + 8 * (atom + 1));
-                        }
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) {
-                            if (t >= tiles) break;
-                            const uint32_t q = unit & 1;
-                            const int r = t * 128 + row;
-                            const uint32_t at = smem + uint32_t(stage) * l.bytes + (uint32_t(p) * l.rows + min(r, l.rows - 1)) * kStepAtom;
-                            if (!mbar_wait(&sh.w_empty[q], ((unit >> 1) & 1) ^ 1)) ok = false;
-                            tmem_fence_after();
+                    const int first = s * l.atoms, atoms = min(l.atoms, a.row_atoms - first);
+                    uint32_t at = smem + uint32_t(stage) * l.bytes + uint32_t(min(row, l.rows - 1)) * kStepAtom;
+                    for (int p = 0; p < atoms; ++p, ++unit, at += uint32_t(l.rows) * kStepAtom) {
+                        scale = scale_next;
+                        const int next_block = 8 * (first + p) + 8;
+                        if (next_block < blocks) scale_next = *reinterpret_cast<const uint2*>(scales + next_block);
+                        const uint32_t q = unit & 1;
+                        if (!ring_wait(&sh.w_empty[q], ((unit >> 1) & 1) ^ 1)) ok = false;
+                        tmem_fence_after();
 #pragma unroll 1
-                            for (int c = set; c < 4; c += sets) {
-                                uint32_t w[8], v[32];
+                        for (int c = set; c < 4; c += sets) {
+                            uint32_t w[8], v[32];
 #pragma unroll
-                                for (int k = 0; k < 2; ++k)
-                                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                                                 : "=r"(w[4 * k]), "=r"(w[4 * k + 1]), "=r"(w[4 * k + 2]), "=r"(w[4 * k + 3])
-                                                 : "r"(at + (uint32_t((2 * c + k) ^ (r & 7)) << 4)));
-                                const uint32_t two = (c & 2 ? scale[t].y : scale[t].x) >> (c & 1 ? 16 : 0);
+                            for (int k = 0; k < 2; ++k)
+                                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                             : "=r"(w[4 * k]), "=r"(w[4 * k + 1]), "=r"(w[4 * k + 2]), "=r"(w[4 * k + 3])
+                                             : "r"(at + (uint32_t((2 * c + k) ^ (row & 7)) << 4)));
+                            const uint32_t two = (c & 2 ? scale.y : scale.x) >> (c & 1 ? 16 : 0);
 #pragma unroll
-                                for (int k = 0; k < 2; ++k) {
-                                    // (behind the row there is no scale, and the weights are zeros)
-                                    const uint32_t sc = mx_scale_pair(8 * atom + 2 * c + k < blocks ? (two >> (8 * k)) & 255u : 0u, largest[t]);
+                            for (int k = 0; k < 2; ++k) {
+                                // (behind the row there is no scale, and the weights are zeros)
+                                const uint32_t byte = next_block - 8 + 2 * c + k < blocks ? (two >> (8 * k)) & 255u : largest;
+                                const uint32_t sc = mx_scale_pair(byte, largest);
 #pragma unroll
-                                    for (int i = 0; i < 4; ++i) mx_word(w[4 * k + i], sc, v + 16 * k + 4 * i);
-                                }
-                                __syncwarp();
-                                tmem_st32(tmem + 256 + 128 * q + 32 * c + (uint32_t((warp & 3) * 32) << 16), v);
-                                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                                tmem_fence_before();
-                                __syncwarp();
-                                if (lane == 0) mbar_arrive(&sh.w_full[q]);
+                                for (int i = 0; i < 4; ++i) mx_word(w[4 * k + i], sc, v + 16 * k + 4 * i);
                             }
-                            ++unit;
+                            __syncwarp();
+                            tmem_st32(tmem + 256 + 128 * q + 32 * c + (uint32_t((warp & 3) * 32) << 16), v);
+                            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                            tmem_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&sh.w_full[q]);
                         }
                     }
                     __syncwarp();
@@ -636,14 +651,14 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             const int chunk = lane & 7, row = (warp - 8) * 4 + (lane >> 3);
             for (int g = all ? groups : 0; g < groups && ok; ++g) {  // (tiled copies bring them where all are taken)
                 const int rows = min(n - g * per_group, per_group);
-                const char* from[8];
+                const char* from[4 * T];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < 4 * T; ++i)
                     if (i * 32 < rows)  // (rows behind the last one are filled up with it)
                         from[i] = static_cast<const char*>(a.weight) +
                                   int64_t(sh.list[min(g * per_group + i * 32 + row, n - 1)]) * a.row_bytes + chunk * 16;
                 for (int s = 0; s < l.steps; ++s) {
-                    if (!mbar_wait(&sh.empty[stage], phase ^ 1)) {
+                    if (!ring_wait(&sh.empty[stage], phase ^ 1)) {
                         ok = false;
                         break;
                     }
@@ -653,7 +668,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                         const int off = (first + p) * int(kStepAtom);
                         const bool have = off + chunk * 16 < a.bytes;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
+                        for (int i = 0; i < 4 * T; ++i) {
                             if (i * 32 >= rows) break;
                             copy16(to + i * 32 * kStepAtom, have ? from[i] + off : from[i] - chunk * 16, have);
                         }
@@ -667,26 +682,25 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             const int quad = warp & 3;
             for (int g = 0; g < groups; ++g) {
                 const int it = groups_done + g;
-                uint32_t bits[2][W];
-                float back[2];  // what brings a token's products back
+                uint32_t bits[T][W];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
+                for (int t = 0; t < T; ++t) {
                     const int at = g * per_group + t * 128 + quad * 32 + lane;
                     const bool have = t < l.tiles && at < n;
                     const int token = have ? sh.list[at] : 0;
-                    step_bits(a, sh, token, have, bits[t]);
-                    back[t] = MX && have ? mx_scale(mx_largest(a.scales + int64_t(token) * a.scale_stride, a.bytes / 16)) : 1.f;
+#pragma unroll
+                    for (int c = 0; c < W; ++c) bits[t][c] = have && 32 * c < a.B ? ld_after_wait(a.bits + int64_t(c) * a.VW * 32 + token) : 0u;
                 }
-                if (!mbar_wait(&sh.sums_full[it & 1], (it >> 1) & 1)) {
+                if (!ring_wait(&sh.sums_full[it & 1], (it >> 1) & 1)) {
                     ok = false;
                     break;
                 }
                 tmem_fence_after();
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
+                for (int t = 0; t < T; ++t) {
                     const int at = g * per_group + t * 128 + quad * 32;
                     if (t < l.tiles && at < n)
-                        step_scores<MX>(a, sh, quad, back[t], sh.list + at, n - at, all,
+                        step_scores<MX>(a, sh, quad, MX ? sh.back_token[it & 1][quad * 32 + lane] : 1.f, sh.list + at, n - at, all,
                                         tmem + uint32_t((it & 1) * l.tiles + t) * a.N + (uint32_t(quad * 32) << 16), bits[t], state, lane);
                 }
                 tmem_fence_before();
