@@ -211,7 +211,7 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
     }
     const unsigned blocks = unsigned(std::min(ctx->sm_count, kStepBlocks));
     a.rounds = ceil_div(ceil_div(a.V, blocks), kStepShare);
-    a.smem = 182 << 10;
+    a.smem = 181 << 10;
     const size_t smem = size_t(a.smem) + 1024 + kStepTile;  // (products read 128 rows, also where fewer are there)
     auto kern = mx ? k_head_step<true> : k_head_step<false>;
     if ((rc = ensure_smem(ctx, kern, smem)) != CFGZIP_OK) return rc;

@@ -192,7 +192,7 @@ struct StepShared {
     uint32_t valid[kStepRows / 32];  // rows that have a partition
     int32_t entries, is_last;
     float back[kStepRowsMx];         // 4-bit heads: what brings a row's products back
-    float back_token[2][128];        // ... and a token's
+    uint8_t largest[kStepShare];     // ... and the largest scale byte of the tokens' rows
     int32_t scan[kStepWarpsMx];
     int32_t list[kStepShare];        // the block's tokens, ascending
     union alignas(16) {
@@ -364,10 +364,10 @@ __device__ __forceinline__ void mx_word(uint32_t w, uint32_t scale, uint32_t* ou
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = mul_f16x2(t[i], scale);
 }
-// 2^(byte - largest) twice, as f16
-__device__ __forceinline__ uint32_t mx_scale_pair(uint32_t byte, uint32_t largest) {
+// 2^(byte - largest) twice, as f16; `normal`: none is below 2^-14
+__device__ __forceinline__ uint32_t mx_scale_pair(uint32_t byte, uint32_t largest, bool normal) {
     const int e = int(byte) - int(largest) + 15;  // exponent field of a normal number
-    if (!__any_sync(0xFFFFFFFFu, e < 1)) return uint32_t(e) * 0x04000400u;
+    if (normal) return uint32_t(e) * 0x04000400u;
     const uint32_t b = e >= 1 ? uint32_t(e) << 10 : e >= -9 ? 1u << (9 + e) : 0u;
     return b | b << 16;
 }
@@ -447,12 +447,12 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     const uint32_t columns = MX ? 512 : 4 * a.N <= 128 ? 128 : 4 * a.N <= 256 ? 256 : 512;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStepStages; ++i) {
-            mbar_init(&sh.empty[i], MX ? 1 + 16 : 1);  // the products, and the pieces in which weights are taken apart
+            mbar_init(&sh.empty[i], MX ? 1 + 8 : 1);  // the products, and the warps that take weights apart
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&sh.sums_full[i], MX ? 1 + 4 : 1);  // the products, and what brings them back
+            mbar_init(&sh.sums_full[i], 1);
             mbar_init(&sh.sums_empty[i], 4);
-            mbar_init(&sh.w_full[i], 16);
+            mbar_init(&sh.w_full[i], 8);
             mbar_init(&sh.w_empty[i], 1);
         }
         mbar_init_fence();
@@ -492,6 +492,11 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             __syncthreads();
         }
         const int per_group = 128 * l.tiles, groups = (n + per_group - 1) / per_group;
+        if (MX && warp >= 4) {  // (the copies have begun meanwhile)
+            for (int i = threadIdx.x - 128; i < n; i += kThreads - 128)
+                sh.largest[i] = uint8_t(mx_largest(a.scales + int64_t(sh.list[i]) * a.scale_stride, a.bytes / 16));
+            asm volatile("bar.sync 1, %0;" ::"n"(kThreads - 128) : "memory");
+        }
         auto next = [&] {
             if (++stage == l.stages) {
                 stage = 0;
@@ -585,22 +590,16 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 if (elect_one()) mma_commit<1>(&sh.sums_full[it & 1]);
                 __syncwarp();
             }
-        } else if (MX && warp >= (all ? 8 : 16)) {
-            // a thread a token; an atom's 256 weights in four pieces, one to a set of four warps, or two where weights are also fetched
-            const int set = ((warp - 8) >> 2) ^ 2, sets = all ? 4 : 2, row = (warp & 3) * 32 + lane;
-            const int blocks = a.bytes / 16;
+        } else if (MX && warp >= 16) {
+            // a thread a token: one set of four warps takes the first half of an atom's 256 weights, the other the second
+            const int half = (warp - 16) >> 2, row = (warp & 3) * 32 + lane, blocks = a.bytes / 16;
+            const uint32_t to = tmem + 256 + 64 * half + (uint32_t((warp & 3) * 32) << 16);
+            auto scales_of = [&](int g) { return a.scales + int64_t(sh.list[min(g * 128 + row, n - 1)]) * a.scale_stride; };
+            const uint8_t* scales = groups > 0 ? scales_of(0) : nullptr;
+            uint4 scale = make_uint4(0, 0, 0, 0), scale_next = groups > 0 ? *reinterpret_cast<const uint4*>(scales) : scale;
             for (int g = 0; g < groups && ok; ++g) {
-                const int token = g * 128 + row < n ? sh.list[g * 128 + row] : sh.list[0];
-                const uint8_t* scales = a.scales + int64_t(token) * a.scale_stride;
-                const uint32_t largest = mx_largest(scales, blocks);
-                uint2 scale, scale_next = *reinterpret_cast<const uint2*>(scales);
-                if (set == 0) {
-                    const int it = groups_done + g;
-                    if (!ring_wait(&sh.sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) ok = false;
-                    sh.back_token[it & 1][row] = mx_scale(largest);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.sums_full[it & 1]);
-                }
+                const uint32_t largest = sh.largest[min(g * 128 + row, n - 1)], least = (largest > 14 ? largest - 14 : 0u) * 0x01010101u;
+                const uint8_t* scales_after = scales_of(g + 1);
                 for (int s = 0; s < l.steps && ok; ++s) {
                     if (!ring_wait(&sh.full[stage], phase)) {
                         ok = false;
@@ -608,43 +607,48 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     }
                     const int first = s * l.atoms, atoms = min(l.atoms, a.row_atoms - first);
                     uint32_t at = smem + uint32_t(stage) * l.bytes + uint32_t(min(row, l.rows - 1)) * kStepAtom;
-                    for (int p = 0; p < atoms; ++p, ++unit, at += uint32_t(l.rows) * kStepAtom) {
-                        scale = scale_next;
-                        const int next_block = 8 * (first + p) + 8;
-                        if (next_block < blocks) scale_next = *reinterpret_cast<const uint2*>(scales + next_block);
+                    for (int atom = first; atom < first + atoms; ++atom, ++unit, at += uint32_t(l.rows) * kStepAtom) {
+                        if (!(atom & 1)) {  // 16 scales serve two atoms; the next 16 come meanwhile
+                            scale = scale_next;
+                            scale_next = *reinterpret_cast<const uint4*>(8 * atom + 16 < blocks ? scales + 8 * atom + 16 : scales_after);
+                        }
                         const uint32_t q = unit & 1;
                         if (!ring_wait(&sh.w_empty[q], ((unit >> 1) & 1) ^ 1)) ok = false;
                         tmem_fence_after();
-#pragma unroll 1
-                        for (int c = set; c < 4; c += sets) {
-                            uint32_t w[8], v[32];
+                        uint32_t w[16];
 #pragma unroll
-                            for (int k = 0; k < 2; ++k)
-                                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                                             : "=r"(w[4 * k]), "=r"(w[4 * k + 1]), "=r"(w[4 * k + 2]), "=r"(w[4 * k + 3])
-                                             : "r"(at + (uint32_t((2 * c + k) ^ (row & 7)) << 4)));
-                            const uint32_t two = (c & 2 ? scale.y : scale.x) >> (c & 1 ? 16 : 0);
+                        for (int k = 0; k < 4; ++k)
+                            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(w[4 * k]), "=r"(w[4 * k + 1]), "=r"(w[4 * k + 2]), "=r"(w[4 * k + 3])
+                                         : "r"(at + (uint32_t((4 * half + k) ^ (row & 7)) << 4)));
+                        uint32_t four = atom & 1 ? (half ? scale.w : scale.z) : (half ? scale.y : scale.x);
+                        const int left = blocks - 8 * atom - 4 * half;  // (behind the row there is no scale, and the weights are zeros)
+                        if (left < 4) {
+                            const uint32_t there = left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+                            four = (four & there) | (largest * 0x01010101u & ~there);
+                        }
+                        const bool normal = !__any_sync(0xFFFFFFFFu, __vcmpltu4(four, least) != 0);
+#pragma unroll
+                        for (int b = 0; b < 4; b += 2) {
+                            uint32_t v[32];
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
-                                // (behind the row there is no scale, and the weights are zeros)
-                                const uint32_t byte = next_block - 8 + 2 * c + k < blocks ? (two >> (8 * k)) & 255u : largest;
-                                const uint32_t sc = mx_scale_pair(byte, largest);
+                                const uint32_t sc = mx_scale_pair((four >> (8 * (b + k))) & 255u, largest, normal);
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) mx_word(w[4 * k + i], sc, v + 16 * k + 4 * i);
+                                for (int i = 0; i < 4; ++i) mx_word(w[4 * (b + k) + i], sc, v + 16 * k + 4 * i);
                             }
-                            __syncwarp();
-                            tmem_st32(tmem + 256 + 128 * q + 32 * c + (uint32_t((warp & 3) * 32) << 16), v);
-                            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                            tmem_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&sh.w_full[q]);
+                            tmem_st32(to + 128 * q + 16 * b, v);
                         }
+                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sh.w_full[q]);
                     }
                     __syncwarp();
-                    if (lane == 0)
-                        for (int c = set; c < 4; c += sets) mbar_arrive(&sh.empty[stage]);
+                    if (lane == 0) mbar_arrive(&sh.empty[stage]);
                     next();
                 }
+                scales = scales_after;
             }
         } else if (warp >= 8) {
             // eight lanes bring the 128 bytes of a row's atom, the eight warps 32 rows at a time
@@ -700,7 +704,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 for (int t = 0; t < T; ++t) {
                     const int at = g * per_group + t * 128 + quad * 32;
                     if (t < l.tiles && at < n)
-                        step_scores<MX>(a, sh, quad, MX ? sh.back_token[it & 1][quad * 32 + lane] : 1.f, sh.list + at, n - at, all,
+                        step_scores<MX>(a, sh, quad, MX ? mx_scale(sh.largest[min(at + lane, n - 1)]) : 1.f, sh.list + at, n - at, all,
                                         tmem + uint32_t((it & 1) * l.tiles + t) * a.N + (uint32_t(quad * 32) << 16), bits[t], state, lane);
                 }
                 tmem_fence_before();
