@@ -387,15 +387,11 @@ __device__ __forceinline__ uint32_t mx_largest(const uint8_t* scales, int n) {
     top = __vmaxu4(top, top >> 16);
     return max(top & 255u, (top >> 8) & 255u);
 }
-__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&v)[32]) {
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&v)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
         "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
-        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]),
-        "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]),
-        "r"(v[31])
+        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
         : "memory");
 }
 __device__ __forceinline__ void mma_f16_from_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
@@ -615,12 +611,13 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                         const uint32_t q = unit & 1;
                         if (!ring_wait(&sh.w_empty[q], ((unit >> 1) & 1) ^ 1)) ok = false;
                         tmem_fence_after();
-                        uint32_t w[16];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
+                        auto fetch = [&](int k, uint32_t (&w)[4]) {
                             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(w[4 * k]), "=r"(w[4 * k + 1]), "=r"(w[4 * k + 2]), "=r"(w[4 * k + 3])
+                                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
                                          : "r"(at + (uint32_t((4 * half + k) ^ (row & 7)) << 4)));
+                        };
+                        uint32_t w[4];
+                        fetch(0, w);
                         uint32_t four = atom & 1 ? (half ? scale.w : scale.z) : (half ? scale.y : scale.x);
                         const int left = blocks - 8 * atom - 4 * half;  // (behind the row there is no scale, and the weights are zeros)
                         if (left < 4) {
@@ -628,16 +625,19 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                             four = (four & there) | (largest * 0x01010101u & ~there);
                         }
                         const bool normal = !__any_sync(0xFFFFFFFFu, __vcmpltu4(four, least) != 0);
+#pragma unroll 1
+                        for (int b = 0; b < 4; ++b) {
+                            uint32_t v[16], after[4];
+                            fetch((b + 1) & 3, after);
+                            const uint32_t sc = mx_scale_pair(four & 255u, largest, normal);
+                            four >>= 8;
 #pragma unroll
-                        for (int b = 0; b < 4; b += 2) {
-                            uint32_t v[32];
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                const uint32_t sc = mx_scale_pair((four >> (8 * (b + k))) & 255u, largest, normal);
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) mx_word(w[4 * (b + k) + i], sc, v + 16 * k + 4 * i);
+                            for (int i = 0; i < 4; ++i) {
+                                mx_word(w[i], sc, v + 4 * i);
+                                w[i] = after[i];
                             }
-                            tmem_st32(to + 128 * q + 16 * b, v);
+                            __syncwarp();
+                            tmem_st16(to + 128 * q + 16 * b, v);
                         }
                         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                         tmem_fence_before();
