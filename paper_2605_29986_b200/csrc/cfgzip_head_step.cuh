@@ -187,7 +187,7 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
 }
 
 struct StepShared {
-    uint64_t full[kStepStages], empty[kStepStages], sums_full[2], sums_empty[2], w_full[2], w_empty[2];
+    uint64_t full[kStepStages], empty[kStepStages], sums_full[2], sums_empty[2], w_full[3], w_empty[3];
     uint32_t tmem;
     uint32_t valid[kStepRows / 32];  // rows that have a partition
     int32_t entries, is_last;
@@ -419,7 +419,7 @@ __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int mos
     l.rows = most > 128 ? 128 * kStepTiles<MX> : (max(most, 1) + 31) & ~31;
     l.atoms = 1;
     int shift = 0;
-    while (shift < 3 && l.atoms < a.row_atoms && 2 * l.atoms * (l.rows + X * a.N) * kStepAtom <= (48u << 10)) {
+    while (!MX && shift < 3 && l.atoms < a.row_atoms && 2 * l.atoms * (l.rows + X * a.N) * kStepAtom <= (48u << 10)) {
         l.atoms *= 2;
         ++shift;
     }
@@ -443,12 +443,14 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     const uint32_t columns = MX ? 512 : 4 * a.N <= 128 ? 128 : 4 * a.N <= 256 ? 256 : 512;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStepStages; ++i) {
-            mbar_init(&sh.empty[i], MX ? 1 + 8 : 1);  // the products, and the warps that take weights apart
+            mbar_init(&sh.empty[i], MX ? 1 + 4 : 1);  // the products, and the warps that take weights apart
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.sums_full[i], 1);
             mbar_init(&sh.sums_empty[i], 4);
-            mbar_init(&sh.w_full[i], 8);
+        }
+        for (int i = 0; i < 3; ++i) {
+            mbar_init(&sh.w_full[i], 4);
             mbar_init(&sh.w_empty[i], 1);
         }
         mbar_init_fence();
@@ -470,7 +472,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     const uint32_t tmem = sh.tmem;
     bool ok = true;
     int stage = 0, groups_done = 0;
-    uint32_t phase = 0, unit = 0;
+    uint32_t phase = 0, set_phases = 0;
     Partial state[W];
 #pragma unroll
     for (int c = 0; c < W; ++c) state[c] = partial_empty();
@@ -488,6 +490,8 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             __syncthreads();
         }
         const int per_group = 128 * l.tiles, groups = (n + per_group - 1) / per_group;
+        const int sets = all ? 3 : 2;  // of four warps that take weights apart: with nothing to fetch, there are four more
+        int set = 0;
         if (MX && warp >= 4) {  // (the copies have begun meanwhile)
             for (int i = threadIdx.x - 128; i < n; i += kThreads - 128)
                 sh.largest[i] = uint8_t(mx_largest(a.scales + int64_t(sh.list[i]) * a.scale_stride, a.bytes / 16));
@@ -556,20 +560,18 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     const uint64_t dw = mma_desc<false>(smem + uint32_t(stage) * l.bytes);
                     const uint64_t dx = mma_desc<false>(smem + uint32_t(stage) * l.bytes + l.x_at);
                     if (MX) {
-                        for (int p = 0; p < atoms; ++p, ++unit) {
-                            const uint32_t q = unit & 1;
-                            if (ok && !ring_wait(&sh.w_full[q], (unit >> 1) & 1)) ok = false;
-                            tmem_fence_after();
-                            if (elect_one()) {
+                        if (ok && !ring_wait(&sh.w_full[set], (set_phases >> set) & 1)) ok = false;
+                        tmem_fence_after();
+                        if (elect_one()) {
 #pragma unroll
-                                for (int j = 0; j < 16; ++j)
-                                    mma_f16_from_tmem(d0, tmem + 256 + 128 * q + 8 * j,
-                                                      dx + (4 * p + j / 4) * x_step + (j & 3) * kDescStep16<false>, idesc,
-                                                      s > 0 || p > 0 || j > 0);
-                                mma_commit<1>(&sh.w_empty[q]);
-                            }
-                            __syncwarp();
+                            for (int j = 0; j < 16; ++j)
+                                mma_f16_from_tmem(d0, tmem + 128 * (set + 1) + 8 * j, dx + j / 4 * x_step + (j & 3) * kDescStep16<false>, idesc,
+                                                  s > 0 || j > 0);
+                            mma_commit<1>(&sh.w_empty[set]);
                         }
+                        __syncwarp();
+                        set_phases ^= 1u << set;
+                        if (++set == sets) set = 0;
                         if (elect_one()) mma_commit<1>(&sh.empty[stage]);
                     } else if (elect_one()) {
                         for (int p = 0; p < atoms; ++p)
@@ -586,70 +588,85 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 if (elect_one()) mma_commit<1>(&sh.sums_full[it & 1]);
                 __syncwarp();
             }
-        } else if (MX && warp >= 16) {
-            // a thread a token: one set of four warps takes the first half of an atom's 256 weights, the other the second
-            const int half = (warp - 16) >> 2, row = (warp & 3) * 32 + lane, blocks = a.bytes / 16;
-            const uint32_t to = tmem + 256 + 64 * half + (uint32_t((warp & 3) * 32) << 16);
-            auto scales_of = [&](int g) { return a.scales + int64_t(sh.list[min(g * 128 + row, n - 1)]) * a.scale_stride; };
-            const uint8_t* scales = groups > 0 ? scales_of(0) : nullptr;
-            uint4 scale = make_uint4(0, 0, 0, 0), scale_next = groups > 0 ? *reinterpret_cast<const uint4*>(scales) : scale;
-            for (int g = 0; g < groups && ok; ++g) {
-                const uint32_t largest = sh.largest[min(g * 128 + row, n - 1)], least = (largest > 14 ? largest - 14 : 0u) * 0x01010101u;
-                const uint8_t* scales_after = scales_of(g + 1);
-                for (int s = 0; s < l.steps && ok; ++s) {
-                    if (!ring_wait(&sh.full[stage], phase)) {
-                        ok = false;
-                        break;
-                    }
-                    const int first = s * l.atoms, atoms = min(l.atoms, a.row_atoms - first);
-                    uint32_t at = smem + uint32_t(stage) * l.bytes + uint32_t(min(row, l.rows - 1)) * kStepAtom;
-                    for (int atom = first; atom < first + atoms; ++atom, ++unit, at += uint32_t(l.rows) * kStepAtom) {
-                        if (!(atom & 1)) {  // 16 scales serve two atoms; the next 16 come meanwhile
-                            scale = scale_next;
-                            scale_next = *reinterpret_cast<const uint4*>(8 * atom + 16 < blocks ? scales + 8 * atom + 16 : scales_after);
-                        }
-                        const uint32_t q = unit & 1;
-                        if (!ring_wait(&sh.w_empty[q], ((unit >> 1) & 1) ^ 1)) ok = false;
-                        tmem_fence_after();
-                        auto fetch = [&](int k, uint32_t (&w)[4]) {
-                            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                                         : "r"(at + (uint32_t((4 * half + k) ^ (row & 7)) << 4)));
-                        };
-                        uint32_t w[4];
-                        fetch(0, w);
-                        uint32_t four = atom & 1 ? (half ? scale.w : scale.z) : (half ? scale.y : scale.x);
-                        const int left = blocks - 8 * atom - 4 * half;  // (behind the row there is no scale, and the weights are zeros)
-                        if (left < 4) {
-                            const uint32_t there = left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-                            four = (four & there) | (largest * 0x01010101u & ~there);
-                        }
-                        const bool normal = !__any_sync(0xFFFFFFFFu, __vcmpltu4(four, least) != 0);
+        } else if (MX && (warp >= 16 || (all && warp >= 8 && warp < 12))) {
+            // a thread a token, a set of warps every second or third atom
+            set = warp >= 16 ? (warp - 16) >> 2 : 2;
+            const int row = (warp & 3) * 32 + lane, blocks = a.bytes / 16;
+            const uint32_t to = tmem + 128 * (set + 1) + (uint32_t((warp & 3) * 32) << 16);
+            auto number = [&](int g) { return min(g * 128 + row, n - 1); };
+            auto scales_at = [&](int g, int s) {  // of an atom: eight
+                return *reinterpret_cast<const uint2*>(a.scales + int64_t(sh.list[number(g)]) * a.scale_stride + 8 * s);
+            };
+            int g = 0, s = set, at_stage = stage + set;
+            uint32_t at_phase = phase, largest = 0;
+            auto settle = [&] {
+                while (s >= l.steps) {
+                    s -= l.steps;
+                    ++g;
+                }
+                while (at_stage >= l.stages) {
+                    at_stage -= l.stages;
+                    at_phase ^= 1;
+                }
+            };
+            settle();
+            uint2 scale = g < groups ? scales_at(g, s) : make_uint2(0, 0);
+            while (g < groups && ok) {
+                const int atom = s, here = at_stage;
+                const uint32_t here_phase = at_phase;
+                largest = sh.largest[number(g)];
+                const uint32_t least = (largest > 14 ? largest - 14 : 0u) * 0x01010101u;
+                uint2 eight = scale;
+                s += sets;
+                at_stage += sets;
+                settle();
+                if (g < groups) scale = scales_at(g, s);  // (comes while this atom is taken apart)
+                const int left = blocks - 8 * atom;  // (behind the row there is no scale, and the weights are zeros)
+                if (left < 8) {
+                    const uint64_t there = (uint64_t(1) << (8 * left)) - 1, fill = uint64_t(largest) * 0x0101010101010101ull;
+                    const uint64_t e = ((uint64_t(eight.y) << 32 | eight.x) & there) | (fill & ~there);
+                    eight = make_uint2(uint32_t(e), uint32_t(e >> 32));
+                }
+                const bool normal = !__any_sync(0xFFFFFFFFu, (__vcmpltu4(eight.x, least) | __vcmpltu4(eight.y, least)) != 0);
+                if (!ring_wait(&sh.full[here], here_phase) || !ring_wait(&sh.w_empty[set], (set_phases & 1) ^ 1)) {
+                    ok = false;
+                    break;
+                }
+                tmem_fence_after();
+                const uint32_t at = smem + uint32_t(here) * l.bytes + uint32_t(min(row, l.rows - 1)) * kStepAtom;
+                auto fetch = [&](int k, uint32_t (&w)[4]) {
+                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                                 : "r"(at + (uint32_t(k ^ (row & 7)) << 4)));
+                };
+                uint32_t w[4];
+                fetch(0, w);
 #pragma unroll 1
-                        for (int b = 0; b < 4; ++b) {
-                            uint32_t v[16], after[4];
-                            fetch((b + 1) & 3, after);
-                            const uint32_t sc = mx_scale_pair(four & 255u, largest, normal);
-                            four >>= 8;
+                for (int b = 0; b < 8; ++b) {
+                    uint32_t v[16], after[4];
+                    fetch((b + 1) & 7, after);
+                    const uint32_t sc = mx_scale_pair(eight.x & 255u, largest, normal);
+                    eight.x = __funnelshift_r(eight.x, eight.y, 8);
+                    eight.y >>= 8;
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                mx_word(w[i], sc, v + 4 * i);
-                                w[i] = after[i];
-                            }
-                            __syncwarp();
-                            tmem_st16(to + 128 * q + 16 * b, v);
-                        }
-                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                        tmem_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&sh.w_full[q]);
+                    for (int i = 0; i < 4; ++i) {
+                        mx_word(w[i], sc, v + 4 * i);
+                        w[i] = after[i];
                     }
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.empty[stage]);
-                    next();
+                    tmem_st16(to + 16 * b, v);
                 }
-                scales = scales_after;
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&sh.w_full[set]);
+                    mbar_arrive(&sh.empty[here]);
+                }
+                set_phases ^= 1;
             }
+            // (every role goes through all of the round's stages)
+            for (int i = 0; i < groups * l.steps; ++i) next();
         } else if (warp >= 8) {
             // eight lanes bring the 128 bytes of a row's atom, the eight warps 32 rows at a time
             const int chunk = lane & 7, row = (warp - 8) * 4 + (lane >> 3);
