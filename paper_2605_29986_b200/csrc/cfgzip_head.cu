@@ -175,9 +175,19 @@ int dequantize(cfgzip_ctx* ctx, const cfgzip_head* h, int32_t t0, int32_t n, uin
                   static_cast<const uint8_t*>(h->scales) + t0 * h->scale_stride, h->scale_stride, h->H / 8, total, values, stride);
 }
 
-// One decode step of up to kStepRows (kStepRowsMx) rows whose vocab masks are there.
+// Masks of rows that share a partition whose class masks fit a table in shared memory; part null: the vocab masks are there.
+struct StepMasks {
+    const PartDev* part = nullptr;
+    const uint32_t* class_mask = nullptr;
+    int64_t class_stride = 0;
+    uint32_t* vocab_mask = nullptr;
+    int64_t vocab_stride = 0;
+};
+constexpr int kTableWords = 1280;  // longest class mask for it: 160 KB
+
+// One decode step of up to kStepRows (kStepRowsMx) rows.
 int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const uint16_t* hidden, int64_t hidden_stride,
-             const HeadSpace& w, cudaStream_t st) {
+             const HeadSpace& w, const StepMasks& m, cudaStream_t st) {
     const bool mx = head->dtype == CFGZIP_MXFP4;
     CUtensorMap map_x, map_w, map_box;
     int rc;
@@ -202,7 +212,16 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
         (rc = tensor_map(ctx, &map_box, head->weight, head->V, cols, head->row_stride, kStepBox, mx)) != CFGZIP_OK)
         return rc;
     a.n_counts = ceil_div(a.VW, kUnionWords);
-    if ((rc = launch(ctx, k_head_union, dim3(unsigned(a.n_counts + (mx ? a.B : 0))), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
+    const dim3 pieces(unsigned(a.n_counts + (mx ? a.B : 0)));
+    if (m.part) {
+        const size_t table = size_t(m.part->KW) * 128;
+        if ((rc = ensure_smem(ctx, k_head_masks, table)) != CFGZIP_OK ||
+            (rc = launch(ctx, k_head_masks, pieces, dim3(256), table, st, a, *m.part, m.class_mask, m.class_stride, m.vocab_mask,
+                         m.vocab_stride)) != CFGZIP_OK)
+            return rc;
+    } else if ((rc = launch(ctx, k_head_union, pieces, dim3(256), 0, st, a)) != CFGZIP_OK) {
+        return rc;
+    }
     if (a.logits) {
         const dim3 grid(unsigned(std::max(1, std::min(ceil_div(a.V, 8192), 64))), unsigned(a.B));
         if ((rc = launch(ctx, a.logits_dtype == CFGZIP_BF16 ? k_head_fill<kBF16> : k_head_fill<kF32>, grid, dim3(256), 0, st, a)) !=
@@ -284,12 +303,17 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint32_t* mask = vocab_mask ? vocab_mask : w.mask;
     const int64_t mask_stride = vocab_mask ? vocab_stride_words : ps.VW;
-    if ((rc = cfgzip_expand_mask(ctx, part0, row_part, class_mask, class_stride_words, mask, mask_stride, B, CFGZIP_DENSE, stream)) !=
+    const PartDev& one = ctx->parts[size_t(part0)].dev;
+    const bool table = !rows && one.c16 && one.KW <= kTableWords;
+    if (!table && (rc = cfgzip_expand_mask(ctx, part0, row_part, class_mask, class_stride_words, mask, mask_stride, B, CFGZIP_DENSE, stream)) !=
         CFGZIP_OK)
         return rc;
     const int32_t most = head->dtype == CFGZIP_MXFP4 ? kStepRowsMx : kStepRows;
     for (int32_t b = 0; b < B; b += most) {
         HeadStepArgs s{};
+        StepMasks m;
+        if (table) m = StepMasks{&one, class_mask + b * class_stride_words, class_stride_words,
+                                 vocab_mask ? vocab_mask + b * vocab_stride_words : nullptr, vocab_stride_words};
         s.parts = ctx->d_parts;
         s.part0 = part0;
         s.n_parts = int32_t(ctx->parts.size());
@@ -313,7 +337,7 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
         s.logp = logp_argmax ? logp_argmax + b : nullptr;
         s.lse = lse ? lse + b : nullptr;
         s.status = ctx->d_status;
-        rc = run_step(ctx, s, head, static_cast<const uint16_t*>(hidden) + b * hidden_stride, hidden_stride, w, st);
+        rc = run_step(ctx, s, head, static_cast<const uint16_t*>(hidden) + b * hidden_stride, hidden_stride, w, m, st);
         if (rc != CFGZIP_OK) return rc;
     }
     return CFGZIP_OK;

@@ -94,12 +94,79 @@ __device__ __forceinline__ void half_row(const HeadStepArgs& a, int row) {
     }
 }
 
+// What 32 words of tokens (kUnionWords) are worth to a batch, from each token's allowing rows: bits to a.bits, count, union; and with
+// `masks` the rows' vocab masks. A warp takes four words, a lane a token: allow(word, k) gives the bits, of word number 4 warp + k.
+template <typename F>
+__device__ __forceinline__ void union_chunk(const HeadStepArgs& a, int c, uint32_t* sh, uint32_t* masks, int64_t mask_stride, F&& allow) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int at = blockIdx.x * kUnionWords + 4 * warp + k;
+        const uint32_t b = allow(at, k), any = __ballot_sync(0xFFFFFFFFu, b != 0);
+        if (at < a.VW) a.bits[(int64_t(c) * a.VW + at) * 32 + lane] = b;
+        if (lane == 0 && any) sh[4 * warp + k] |= any;
+        if (masks) {
+            const uint32_t w = warp_transpose32(b, lane);
+            const int row = 32 * c + lane;
+            if (at < a.VW && row < a.B) masks[row * mask_stride + at] = w;
+        }
+    }
+}
+__device__ __forceinline__ void union_finish(const HeadStepArgs& a, const uint32_t* sh) {
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    const int word = blockIdx.x * kUnionWords + int(threadIdx.x);
+    const uint32_t any = sh[threadIdx.x];
+    if (word < a.VW) a.any[word] = any;
+    const int n = __reduce_add_sync(0xFFFFFFFFu, __popc(any));
+    if (threadIdx.x == 0) a.counts[blockIdx.x] = n;
+}
+
+// Rows of one partition: class masks turned to a table of 32 rows a class, a token's rows by one lookup. Vocab masks, union and turned
+// masks in one launch (expanding and turning by two took 3 to 5 us longer).
+__global__ void __launch_bounds__(256) k_head_masks(const HeadStepArgs a, const __grid_constant__ PartDev p, const uint32_t* class_mask,
+                                                    int64_t class_stride, uint32_t* masks, int64_t mask_stride) {
+    extern __shared__ uint32_t table[];
+    __shared__ uint32_t sh[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t cls[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int at = blockIdx.x * kUnionWords + 4 * warp + k;
+        cls[k] = int(blockIdx.x) < a.n_counts && at < a.VW ? __ldg(p.c16 + int64_t(at) * 32 + lane) : uint32_t(p.K);  // (K: no class)
+    }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
+    if (int(blockIdx.x) >= a.n_counts) {
+        half_row(a, int(blockIdx.x) - a.n_counts);
+        return;
+    }
+    if (threadIdx.x < 32) sh[threadIdx.x] = 0;
+    for (int c = 0; 32 * c < a.B; ++c) {
+        const int row = 32 * c + lane;
+        const uint32_t* m = class_mask + row * class_stride;
+        __syncthreads();
+        for (int k0 = warp; k0 < p.KW; k0 += 32) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = row < a.B && k0 + 8 * k < p.KW ? ld_after_wait(m + k0 + 8 * k) : 0u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k0 + 8 * k < p.KW) table[32 * (k0 + 8 * k) + lane] = warp_transpose32(w[k], lane);
+        }
+        __syncthreads();
+        union_chunk(a, c, sh, masks, mask_stride, [&](int, int k) { return cls[k] < uint32_t(p.K) ? table[cls[k]] : 0u; });
+    }
+    union_finish(a, sh);
+}
+
 // Union of the rows' masks, 32 words by a block, and the masks turned from 32 tokens of a row to 32 rows of a token: a warp takes
 // four words, a lane a row. Blocks behind those take a row of hidden states.
 __global__ void __launch_bounds__(256) k_head_union(const HeadStepArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, word = blockIdx.x * kUnionWords + lane;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
     if (int(blockIdx.x) >= a.n_counts) {
         half_row(a, int(blockIdx.x) - a.n_counts);
@@ -118,20 +185,9 @@ __global__ void __launch_bounds__(256) k_head_union(const HeadStepArgs a) {
             const int at = blockIdx.x * kUnionWords + 4 * warp + k;
             w[k] = has && at < a.VW ? ld_after_wait(p + at) : 0u;
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int at = blockIdx.x * kUnionWords + 4 * warp + k;
-            const uint32_t b = warp_transpose32(w[k], lane), any = __ballot_sync(0xFFFFFFFFu, b != 0);
-            if (at < a.VW) a.bits[(int64_t(c) * a.VW + at) * 32 + lane] = b;
-            if (lane == 0 && any) sh[4 * warp + k] |= any;
-        }
+        union_chunk(a, c, sh, nullptr, 0, [&](int, int k) { return warp_transpose32(w[k], lane); });
     }
-    __syncthreads();
-    if (warp) return;
-    const uint32_t any = sh[lane];
-    if (word < a.VW) a.any[word] = any;
-    const int n = __reduce_add_sync(0xFFFFFFFFu, __popc(any));
-    if (lane == 0) a.counts[blockIdx.x] = n;
+    union_finish(a, sh);
 }
 
 // A union of at least three quarters of the vocabulary is taken for all of it: boxes of rows by tiled copies come at the memory's
@@ -186,13 +242,26 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
+// Until a counter in shared memory has come to `least` (a count, not a phase: who waits may have let some go by). About half a
+// second at most; false: it has not.
+__device__ __forceinline__ bool wait_count(const uint32_t* count, uint32_t least) {
+    for (int it = 0; it < (1 << 22); ++it) {
+        uint32_t v;
+        asm volatile("ld.acquire.cta.shared::cta.u32 %0, [%1];" : "=r"(v) : "r"(smem_u32(count)) : "memory");
+        if (v >= least) return true;
+        if (it > 16) __nanosleep(100);
+    }
+    return false;
+}
+
 struct StepShared {
     uint64_t full[kStepStages], empty[kStepStages], sums_full[2], sums_empty[2], w_full[3], w_empty[3];
     uint32_t tmem;
     uint32_t valid[kStepRows / 32];  // rows that have a partition
     int32_t entries, is_last;
     float back[kStepRowsMx];         // 4-bit heads: what brings a row's products back
-    uint8_t largest[kStepShare];     // ... and the largest scale byte of the tokens' rows
+    uint32_t largest[2][128];        // ... and the largest scale byte of the rows of a tile's tokens
+    uint32_t largest_tiles[4];       // how many tiles' are there, by the quarters of a tile
     int32_t scan[kStepWarpsMx];
     int32_t list[kStepShare];        // the block's tokens, ascending
     union alignas(16) {
@@ -453,6 +522,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             mbar_init(&sh.w_full[i], 4);
             mbar_init(&sh.w_empty[i], 1);
         }
+        for (int i = 0; i < 4; ++i) sh.largest_tiles[i] = 0;
         mbar_init_fence();
         prefetch_tensor_map(&map_x);
         prefetch_tensor_map(&map_w);
@@ -492,11 +562,6 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         const int per_group = 128 * l.tiles, groups = (n + per_group - 1) / per_group;
         const int sets = all ? 3 : 2;  // of four warps that take weights apart: with nothing to fetch, there are four more
         int set = 0;
-        if (MX && warp >= 4) {  // (the copies have begun meanwhile)
-            for (int i = threadIdx.x - 128; i < n; i += kThreads - 128)
-                sh.largest[i] = uint8_t(mx_largest(a.scales + int64_t(sh.list[i]) * a.scale_stride, a.bytes / 16));
-            asm volatile("bar.sync 1, %0;" ::"n"(kThreads - 128) : "memory");
-        }
         auto next = [&] {
             if (++stage == l.stages) {
                 stage = 0;
@@ -597,7 +662,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             auto scales_at = [&](int g, int s) {  // of an atom: eight
                 return *reinterpret_cast<const uint2*>(a.scales + int64_t(sh.list[number(g)]) * a.scale_stride + 8 * s);
             };
-            int g = 0, s = set, at_stage = stage + set;
+            int g = 0, s = set, at_stage = stage + set, group = -1;
             uint32_t at_phase = phase, largest = 0;
             auto settle = [&] {
                 while (s >= l.steps) {
@@ -614,7 +679,15 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             while (g < groups && ok) {
                 const int atom = s, here = at_stage;
                 const uint32_t here_phase = at_phase;
-                largest = sh.largest[number(g)];
+                if (g != group) {
+                    group = g;
+                    const int it = groups_done + g;
+                    if (!wait_count(&sh.largest_tiles[warp & 3], uint32_t(it) + 1)) {
+                        ok = false;
+                        break;
+                    }
+                    largest = sh.largest[it & 1][row];
+                }
                 const uint32_t least = (largest > 14 ? largest - 14 : 0u) * 0x01010101u;
                 uint2 eight = scale;
                 s += sets;
@@ -628,7 +701,9 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     eight = make_uint2(uint32_t(e), uint32_t(e >> 32));
                 }
                 const bool normal = !__any_sync(0xFFFFFFFFu, (__vcmpltu4(eight.x, least) | __vcmpltu4(eight.y, least)) != 0);
-                if (!ring_wait(&sh.full[here], here_phase) || !ring_wait(&sh.w_empty[set], (set_phases & 1) ^ 1)) {
+                // The products of this set's atom before are through, so all atoms up to that one are: the stage's barrier cannot be a
+                // phase behind (there are at least as many stages as sets), and its parity says what it seems to.
+                if (!ring_wait(&sh.w_empty[set], (set_phases & 1) ^ 1) || !ring_wait(&sh.full[here], here_phase)) {
                     ok = false;
                     break;
                 }
@@ -701,8 +776,23 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             asm volatile("cp.async.wait_all;" ::: "memory");
         } else if (warp >= 4) {
             const int quad = warp & 3;
+            // 4-bit heads: the largest scales of a tile's rows are looked for a tile ahead
+            uint32_t largest = 0, largest_next = 0;
+            auto find_largest = [&](int g) {
+                if (g >= groups) return;
+                const int at = g * 128 + quad * 32 + lane, slot = (groups_done + g) & 1;
+                largest_next = mx_largest(a.scales + int64_t(sh.list[min(at, n - 1)]) * a.scale_stride, a.bytes / 16);
+                sh.largest[slot][quad * 32 + lane] = largest_next;
+                __syncwarp();
+                if (lane == 0)
+                    asm volatile("st.release.cta.shared::cta.u32 [%0], %1;" ::"r"(smem_u32(&sh.largest_tiles[quad])), "r"(groups_done + g + 1)
+                                 : "memory");
+            };
+            if (MX) find_largest(0);
             for (int g = 0; g < groups; ++g) {
                 const int it = groups_done + g;
+                largest = largest_next;
+                if (MX) find_largest(g + 1);
                 uint32_t bits[T][W];
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
@@ -721,7 +811,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 for (int t = 0; t < T; ++t) {
                     const int at = g * per_group + t * 128 + quad * 32;
                     if (t < l.tiles && at < n)
-                        step_scores<MX>(a, sh, quad, MX ? mx_scale(sh.largest[min(at + lane, n - 1)]) : 1.f, sh.list + at, n - at, all,
+                        step_scores<MX>(a, sh, quad, MX ? mx_scale(largest) : 1.f, sh.list + at, n - at, all,
                                         tmem + uint32_t((it & 1) * l.tiles + t) * a.N + (uint32_t(quad * 32) << 16), bits[t], state, lane);
                 }
                 tmem_fence_before();
