@@ -168,11 +168,13 @@ int run_mma(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUtenso
     return launch(ctx, kern, dim3(2 * pairs), dim3(kMmaThreads), kMmaSmem, st, a, map_a, map_b);
 }
 
-int dequantize(cfgzip_ctx* ctx, const cfgzip_head* h, int32_t t0, int32_t n, uint16_t* values, int64_t stride, cudaStream_t st) {
-    const int64_t total = int64_t(n) * (h->H / 8);
-    return launch(ctx, k_mx_dequantize, dim3(unsigned(ceil_div(total, 256 * kMxUnroll))), dim3(256), 0, st,
-                  static_cast<const uint8_t*>(h->weight) + t0 * h->row_stride, h->row_stride,
-                  static_cast<const uint8_t*>(h->scales) + t0 * h->scale_stride, h->scale_stride, h->H / 8, total, values, stride);
+// Threads of a launch that takes a head by vectors of 8 weights (mx_at).
+void mx_shape(const cfgzip_head* h, dim3* grid, dim3* block) {
+    const int vectors = h->H / 8, y = ceil_div(vectors, 512);
+    block->x = unsigned(up(ceil_div(vectors, y), 32));
+    block->y = std::max(1u, 256u / block->x);
+    grid->x = unsigned(ceil_div(h->V, int64_t(block->y) * kMxRows));
+    grid->y = unsigned(y);
 }
 
 // Masks of rows that share a partition whose class masks fit a table in shared memory; part null: the vocab masks are there.
@@ -259,10 +261,10 @@ int cfgzip_head_quantize(cfgzip_ctx* ctx, const void* weight, int dtype, int64_t
     if (!on16(weight, row_stride_elems * (dtype == CFGZIP_BF16 ? 2 : 4))) return CFGZIP_E_ALIGN;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;
-    const int64_t total = int64_t(head->V) * (head->H / 8);
-    return launch(ctx, dtype == CFGZIP_BF16 ? k_mx_quantize<kBF16> : k_mx_quantize<kF32>,
-                  dim3(unsigned(ceil_div(total, 256 * kMxUnroll))), dim3(256), 0, static_cast<cudaStream_t>(stream), weight,
-                  row_stride_elems, head->H / 8, total, static_cast<uint8_t*>(head->weight), head->row_stride,
+    dim3 grid, block;
+    mx_shape(head, &grid, &block);
+    return launch(ctx, dtype == CFGZIP_BF16 ? k_mx_quantize<kBF16> : k_mx_quantize<kF32>, grid, block, 0,
+                  static_cast<cudaStream_t>(stream), weight, row_stride_elems, head->H / 8, int(head->V), static_cast<uint8_t*>(head->weight), head->row_stride,
                   static_cast<uint8_t*>(head->scales), head->scale_stride);
 }
 
@@ -274,7 +276,11 @@ int cfgzip_head_dequantize(cfgzip_ctx* ctx, const cfgzip_head* head, void* value
     if ((rc = check_rows(head, values, row_stride_elems)) != CFGZIP_OK) return rc;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;
-    return dequantize(ctx, head, 0, head->V, static_cast<uint16_t*>(values), row_stride_elems, static_cast<cudaStream_t>(stream));
+    dim3 grid, block;
+    mx_shape(head, &grid, &block);
+    return launch(ctx, k_mx_dequantize, grid, block, 0, static_cast<cudaStream_t>(stream), static_cast<const uint8_t*>(head->weight),
+                  head->row_stride, static_cast<const uint8_t*>(head->scales), head->scale_stride, head->H / 8, int(head->V),
+                  static_cast<uint16_t*>(values), row_stride_elems);
 }
 
 int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_part, const uint32_t* class_mask,
@@ -386,7 +392,7 @@ int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidde
     f.loss = loss;
     f.lse = lse;
     f.status = ctx->d_status;
-    return launch(ctx, k_head_loss_finish, dim3(unsigned(ceil_div(N, 32))), dim3(256), 0, st, f);
+    return launch(ctx, k_head_loss_finish, dim3(unsigned(ceil_div(N, 8))), dim3(256), 0, st, f);
 }
 
 int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N,

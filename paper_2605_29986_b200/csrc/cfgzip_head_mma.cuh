@@ -345,7 +345,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     if (warp == 2) tmem_free<2>(tmem, 512);
 }
 
-// Partial states of a row's tiles to its results: 32 rows by a block, a warp takes every eighth tile.
+// Partial states of a row's tiles to its results: eight rows by a block, a thread takes every 32nd tile of one.
 struct FinishArgs {
     const float2* part;
     const float* of_target;
@@ -358,27 +358,36 @@ struct FinishArgs {
 };
 __global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 8 + (lane & 7);
     float m = -INFINITY, s = 0.f;
     if (row < a.rows)
 #pragma unroll 4
-        for (int t = warp; t < a.tiles; t += 8) {
+        for (int t = warp * 4 + (lane >> 3); t < a.tiles; t += 32) {
             const float2 p = __ldcg(a.part + int64_t(t) * a.rows + row);
             const float next = fmaxf(m, p.x), ref = fmaxf(next, kRefFloor);
             s = s * ex2f((fmaxf(m, kRefFloor) - ref) * kLog2e) + p.y * ex2f((fmaxf(p.x, kRefFloor) - ref) * kLog2e);
             m = next;
         }
-    __shared__ float2 sh[8][32];
-    sh[warp][lane] = make_float2(m, s);
+    __shared__ float2 sh[32][8];
+    sh[warp * 4 + (lane >> 3)][lane & 7] = make_float2(m, s);
     __syncthreads();
-    if (warp || row >= a.rows) return;
+    if (warp) return;
+    // four threads a row, eight states each
     float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[w][lane].x);
+    for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[8 * (lane >> 3) + w][lane & 7].x);
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
     const float ref = fmaxf(top, kRefFloor);
     s = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) s += sh[w][lane].y * ex2f((fmaxf(sh[w][lane].x, kRefFloor) - ref) * kLog2e);
+    for (int w = 0; w < 8; ++w) {
+        const float2 p = sh[8 * (lane >> 3) + w][lane & 7];
+        s += p.y * ex2f((fmaxf(p.x, kRefFloor) - ref) * kLog2e);
+    }
+    s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);
+    s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
+    if (lane >= 8 || row >= a.rows) return;
     const float log_sum = logf(s);
     if (a.lse) a.lse[row] = s > 0.f ? top + log_sum : -INFINITY;
     const int t = ld_after_wait(a.targets + row);
@@ -407,8 +416,8 @@ __global__ void __launch_bounds__(256) k_head_round(const float* from, int64_t s
             f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
             f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
         }
-        const MxAt at = mx_at(i, vectors);
-        *reinterpret_cast<uint4*>(to + at.row * to_stride + 8 * at.col) =
+        const int64_t row = i / vectors;
+        *reinterpret_cast<uint4*>(to + row * to_stride + 8 * (i - row * vectors)) =
             make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
     }
 }

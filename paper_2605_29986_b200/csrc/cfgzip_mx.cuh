@@ -7,7 +7,7 @@
 namespace cfgzip {
 
 constexpr int kMxBlock = 32;      // weights per scale
-constexpr int kMxUnroll = 4;      // vectors of 8 weights a thread has in flight
+constexpr int kMxRows = 4;  // rows a thread has in flight, a vector of 8 weights of each
 
 // Eight f32 to eight e2m1 codes, ties to even, above 6 to 6; the first in the lowest four bits.
 __device__ __forceinline__ uint32_t e2m1_codes(const float (&f)[8]) {
@@ -26,41 +26,47 @@ __device__ __forceinline__ uint32_t e2m1_codes(const float (&f)[8]) {
 // 2^(scale - 127) as f32; the scale byte 0 is below the normal numbers.
 __device__ __forceinline__ float mx_scale(uint32_t byte) { return __uint_as_float(byte ? (byte == 255u ? 0x7FC00000u : byte << 23) : 0x00400000u); }
 
-// Where a vector of 8 weights lies: `vectors` of them to a row, in the order of the memory.
+// A thread takes a vector of 8 weights of four neighbouring rows (row0 and on; vectors to a row along x, so that nothing has to be
+// divided), four lanes a block of weights, whose largest goes around by shuffles.
 struct MxAt {
-    int64_t row;
-    int col;  // vector of the row
+    int64_t row0;
+    int col;  // vector of the rows
+    bool have;
 };
-__device__ __forceinline__ MxAt mx_at(int64_t i, int vectors) {
-    if (i >> 32) return MxAt{i / vectors, int(i % vectors)};
-    const uint32_t r = uint32_t(i) / uint32_t(vectors);
-    return MxAt{int64_t(r), int(uint32_t(i) - r * uint32_t(vectors))};
+__device__ __forceinline__ MxAt mx_at(int vectors) {
+    const int col = blockIdx.y * blockDim.x + threadIdx.x;
+    return MxAt{(int64_t(blockIdx.x) * blockDim.y + threadIdx.y) * kMxRows, min(col, vectors - 1), col < vectors};
 }
 
-// A thread takes a vector of 8 weights, four neighbours a block; the largest goes around by shuffles. A block of threads takes
-// kMxUnroll * blockDim consecutive vectors, H is a multiple of 32, so a block of weights never leaves its four lanes.
-template <int DT>
-__global__ void __launch_bounds__(256) k_mx_quantize(const void* weight, int64_t row_stride, int vectors, int64_t total,
-                                                     uint8_t* packed, int64_t packed_stride, uint8_t* scales, int64_t scale_stride) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int64_t first = int64_t(blockIdx.x) * (256 * kMxUnroll) + threadIdx.x;
-    uint4 raw[kMxUnroll][DT == kF32 ? 2 : 1];
-    MxAt at[kMxUnroll];
+// bf16 weights of a vector as f32
+__device__ __forceinline__ void mx_unpack(const uint4 (&raw)[1], float (&f)[8]) {
+    const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
 #pragma unroll
-    for (int u = 0; u < kMxUnroll; ++u) {
-        const int64_t i = first + u * 256;
-        at[u] = mx_at(i < total ? i : total - 1, vectors);
-        const char* p = static_cast<const char*>(weight) + (at[u].row * row_stride + 8 * int64_t(at[u].col)) * (DT == kF32 ? 4 : 2);
+    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+}
+__device__ __forceinline__ void mx_unpack(const uint4 (&raw)[2], float (&f)[8]) {
+    const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(w[j]);
+}
+
+template <int DT>
+__global__ void __launch_bounds__(512) k_mx_quantize(const void* weight, int64_t row_stride, int vectors, int rows, uint8_t* packed,
+                                                     int64_t packed_stride, uint8_t* scales, int64_t scale_stride) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const MxAt at = mx_at(vectors);
+    uint4 raw[kMxRows][DT == kF32 ? 2 : 1];
+#pragma unroll
+    for (int u = 0; u < kMxRows; ++u) {
+        const int64_t row = min(at.row0 + u, int64_t(rows) - 1);
+        const char* p = static_cast<const char*>(weight) + (row * row_stride + 8 * int64_t(at.col)) * (DT == kF32 ? 4 : 2);
         raw[u][0] = ld_stream16(p);
         if (DT == kF32) raw[u][DT == kF32 ? 1 : 0] = ld_stream16(p + 16);
     }
 #pragma unroll
-    for (int u = 0; u < kMxUnroll; ++u) {
+    for (int u = 0; u < kMxRows; ++u) {
         float f[8];
-        const uint32_t* w = &raw[u][0].x;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            f[j] = DT == kF32 ? __uint_as_float(w[j]) : __uint_as_float(j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+        mx_unpack(raw[u], f);
         uint32_t most = 0;  // largest magnitude, as bits: in the order of the values, and NaN above infinity
 #pragma unroll
         for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(f[j]) & 0x7FFFFFFFu);
@@ -72,50 +78,47 @@ __global__ void __launch_bounds__(256) k_mx_quantize(const void* weight, int64_t
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] *= up;
         const uint32_t codes = byte == 255u ? 0u : e2m1_codes(f);
-        if (first + u * 256 < total) {
-            *reinterpret_cast<uint32_t*>(packed + at[u].row * packed_stride + 4 * int64_t(at[u].col)) = codes;
-            if ((at[u].col & 3) == 0) scales[at[u].row * scale_stride + (at[u].col >> 2)] = uint8_t(byte);
+        const int64_t row = at.row0 + u;
+        if (at.have && row < rows) {
+            *reinterpret_cast<uint32_t*>(packed + row * packed_stride + 4 * int64_t(at.col)) = codes;
+            if ((at.col & 3) == 0) scales[row * scale_stride + (at.col >> 2)] = uint8_t(byte);
         }
     }
 }
 
-// Eight e2m1 codes of a word to bf16 pairs: each times 2^(byte - 127). The product is exact in 32 bits and in bf16.
+// Eight e2m1 codes of a word as bf16, each times 2^(byte - 127): f16 numbers first, whose bits, with the exponent moved down three
+// places, are bf16 numbers 2^112 below the values; the two products that bring them up are exact.
 __device__ __forceinline__ uint4 mx_values(uint32_t codes, uint32_t byte) {
-    const float s = mx_scale(byte);
-    uint32_t out[4];
+    const uint32_t scale = (byte == 255u ? 0x7FC0u : byte ? byte << 7 : 0x0040u) * 0x00010001u;
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(codes));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        float v[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const uint32_t code = codes >> (8 * j + 4 * k);
-            // exponent and fraction at the top of the fraction field of a number below the normal ones: 2^126 times too small
-            const float m = __uint_as_float((code & 7u) << 22) * 0x1p126f;
-            v[k] = (code & 8u ? -m : m) * s;
-        }
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(out[j]) : "f"(v[1]), "f"(v[0]));
+        const uint32_t low = (h[j] & 0x80008000u) | ((h[j] & 0x7FFF7FFFu) >> 3);
+        asm("{\n\t.reg .b32 t;\n\tmul.rn.bf16x2 t, %1, %2;\n\tmul.rn.bf16x2 %0, t, %3;\n\t}"
+            : "=r"(h[j])
+            : "r"(low), "r"(0x77807780u), "r"(scale));  // 2^112
     }
-    return make_uint4(out[0], out[1], out[2], out[3]);
+    return make_uint4(h[0], h[1], h[2], h[3]);
 }
 
-__global__ void __launch_bounds__(256) k_mx_dequantize(const uint8_t* packed, int64_t packed_stride, const uint8_t* scales,
-                                                       int64_t scale_stride, int vectors, int64_t total, uint16_t* values,
-                                                       int64_t row_stride) {
+__global__ void __launch_bounds__(512) k_mx_dequantize(const uint8_t* packed, int64_t packed_stride, const uint8_t* scales,
+                                                       int64_t scale_stride, int vectors, int rows, uint16_t* values, int64_t row_stride) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int64_t first = int64_t(blockIdx.x) * (256 * kMxUnroll) + threadIdx.x;
-    uint32_t codes[kMxUnroll], byte[kMxUnroll];
-    MxAt at[kMxUnroll];
+    const MxAt at = mx_at(vectors);
+    uint32_t codes[kMxRows], byte[kMxRows];
 #pragma unroll
-    for (int u = 0; u < kMxUnroll; ++u) {
-        const int64_t i = first + u * 256;
-        at[u] = mx_at(i < total ? i : total - 1, vectors);
-        codes[u] = ld_after_wait(reinterpret_cast<const uint32_t*>(packed + at[u].row * packed_stride + 4 * int64_t(at[u].col)));
-        byte[u] = ld_after_wait(scales + at[u].row * scale_stride + (at[u].col >> 2));
+    for (int u = 0; u < kMxRows; ++u) {
+        const int64_t row = min(at.row0 + u, int64_t(rows) - 1);
+        codes[u] = ld_after_wait(reinterpret_cast<const uint32_t*>(packed + row * packed_stride + 4 * int64_t(at.col)));
+        byte[u] = ld_after_wait(scales + row * scale_stride + (at.col >> 2));
     }
 #pragma unroll
-    for (int u = 0; u < kMxUnroll; ++u)
-        if (first + u * 256 < total)
-            st_stream16(values + at[u].row * row_stride + 8 * int64_t(at[u].col), mx_values(codes[u], byte[u]));
+    for (int u = 0; u < kMxRows; ++u)
+        if (at.have && at.row0 + u < rows) st_stream16(values + (at.row0 + u) * row_stride + 8 * int64_t(at.col), mx_values(codes[u], byte[u]));
 }
 
 }  // namespace cfgzip
