@@ -111,7 +111,7 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
             s.back = c.take<float>(kStepRowsMx);
         }
     } else if (op == CFGZIP_HEAD_LOSS) {
-        s.part = c.take<float2>(n * ceil_div(h->V, kMmaTile));
+        s.part = c.take<float2>(n * ceil_div(h->V, kMmaTile) * 2);
         s.of_target = c.take<float>(n);
     } else {
         const int64_t most = kPieceBytes / 2 / std::max<int64_t>(n, 1) / kMmaTile * kMmaTile;
@@ -383,7 +383,7 @@ int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidde
     FinishArgs f{};
     f.part = w.part;
     f.of_target = w.of_target;
-    f.tiles = a.n_tiles;
+    f.tiles = 2 * a.n_tiles;
     f.rows = N;
     f.V = head->V;
     f.mask = vocab_mask;

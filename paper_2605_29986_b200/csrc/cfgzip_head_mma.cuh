@@ -19,6 +19,9 @@ constexpr int kMmaThreads = 384;   // a warp for the copies, one for the product
 constexpr int kMmaStages = 6;
 constexpr int kMmaTile = 256;      // rows and columns of a pair's tile
 constexpr int kMmaK = 64;          // k of a stage
+// Stages whose sums are left in tensor memory, where every addition is cut off towards zero (-1e-9 of a sum per element of k); the
+// loss, whose scores go out in 32 bits, adds the portions up in registers, rounded. The gradient's are rounded to bf16 in any case.
+constexpr int kMmaPortion = 8;
 constexpr uint32_t kMmaHalf = 128 * kMmaK * 2;           // bytes of one operand of a stage in one block
 constexpr size_t kMmaSmem = size_t(kMmaStages) * 2 * kMmaHalf + 1024;
 
@@ -36,7 +39,7 @@ struct MmaArgs {
     int32_t t0, V;             // the piece starts at token t0
     const int32_t* targets;
     const float *lse, *d_loss;
-    float2* part;              // loss: [n_tiles, rows] largest score and sum
+    float2* part;              // loss: [2 n_tiles, rows] largest score and sum of half a tile
     float* of_target;          // loss: [rows]
     // results
     void* out;
@@ -65,12 +68,13 @@ __device__ __forceinline__ MmaTile mma_tile(const MmaArgs& a, int i) {
     return t;
 }
 
-// What a row allows of the 256 tokens from column n0 of the piece on, 32 to a word.
-__device__ __forceinline__ void tile_mask(const MmaArgs& a, int row, int n0, uint32_t (&bits)[8]) {
+// What a row allows of the 32 W tokens from column n0 of the piece on, 32 to a word.
+template <int W>
+__device__ __forceinline__ void tile_mask(const MmaArgs& a, int row, int n0, uint32_t (&bits)[W]) {
     const int t = a.t0 + n0, left = min(a.cols - n0, kMmaTile);
     const uint32_t* p = a.mask + (a.mask ? int64_t(row) * a.mask_stride + (t >> 5) : 0);
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
+    for (int c = 0; c < W; ++c) {
         const int n = left - 32 * c;
         uint32_t w = 0;
         if (n > 0) w = (a.mask ? ld_after_wait(p + c) : 0xFFFFFFFFu) & (n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u);
@@ -78,44 +82,27 @@ __device__ __forceinline__ void tile_mask(const MmaArgs& a, int row, int n0, uin
     }
 }
 
-// Largest allowed score and the sum of exponentials, of one row and 256 tokens.
-__device__ __forceinline__ void loss_epilogue(const MmaArgs& a, const MmaTile& t, int row, uint32_t tmem, bool valid,
-                                              const uint32_t (&bits)[8]) {
-    float m = -INFINITY, s = 0.f;
-    const int n0 = t.n * kMmaTile;
+// Largest allowed score and the sum of exponentials, of one row and half a tile's tokens.
+__device__ __forceinline__ void loss_epilogue(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, float (&z)[128],
+                                              const uint32_t (&bits)[4]) {
+    const int n0 = t.n * kMmaTile + 128 * half;
     const int asked = valid ? ld_after_wait(a.targets + row) : -1, target = asked < 0 ? -1 : asked - (a.t0 + n0);
-#pragma unroll 1
-    for (int c = 0; c < 8; ++c) {
-        uint32_t v[32];
-        __syncwarp();
-        tmem_ld32(tmem + 32 * c, v);
-        tmem_wait_ld();
-        if (__any_sync(0xFFFFFFFFu, (target >> 5) == c)) {
+    if (__any_sync(0xFFFFFFFFu, uint32_t(target) < 128u)) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (target == 32 * c + j) a.of_target[row] = __uint_as_float(v[j]);
-        }
-        uint32_t w = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w = k == c ? bits[k] : w;
-        float top = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            v[j] = (w >> j) & 1u ? v[j] : 0xFF800000u;
-            top = fmaxf(top, __uint_as_float(v[j]));
-        }
-        const float next = fmaxf(m, top), ref = fmaxf(next, kRefFloor);
-        s *= ex2f((fmaxf(m, kRefFloor) - ref) * kLog2e);
-        m = next;
-        float s1 = 0.f;
-#pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-            s += ex2f((__uint_as_float(v[j]) - ref) * kLog2e);
-            s1 += ex2f((__uint_as_float(v[j + 1]) - ref) * kLog2e);
-        }
-        s += s1;
+        for (int j = 0; j < 128; ++j)
+            if (target == j) a.of_target[row] = z[j];
     }
-    if (valid) a.part[int64_t(t.n) * a.rows + row] = make_float2(m, s);
+    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int j = 0; j < 128; ++j) {
+        z[j] = (bits[j / 32] >> (j & 31)) & 1u ? z[j] : -INFINITY;
+        m[j & 3] = fmaxf(m[j & 3], z[j]);
+    }
+    const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), ref = fmaxf(top, kRefFloor);
+    float s[4] = {};
+#pragma unroll
+    for (int j = 0; j < 128; ++j) s[j & 3] += ex2f((z[j] - ref) * kLog2e);
+    if (valid) a.part[int64_t(2 * t.n + half) * a.rows + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
 }
 
 // g = d (exp(z - lse) - [target]) of the allowed tokens, as bf16.
@@ -222,6 +209,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kMmaStages], empty[kMmaStages], sums_full[2], sums_empty[2];
     __shared__ uint32_t s_tmem;
+    constexpr bool kPortion = KIND == kMmaLoss;
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -233,7 +221,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sums_full[i], 1);
-            mbar_init(&sums_empty[i], 8);  // four warps of either block
+            mbar_init(&sums_empty[i], kPortion ? 16 : 8);  // four warps of either block (all eight)
         }
         mbar_init_fence();
         prefetch_tensor_map(&map_a);
@@ -281,34 +269,70 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             constexpr uint32_t idesc = kMmaBf16Desc<256, 256, A_MN, B_MN>;
             Ring r;
             int it = 0;
-            for (int i = pair; i < tiles && ok; i += pairs, ++it) {
+            for (int i = pair; i < tiles && ok; i += pairs) {
                 const MmaTile t = mma_tile(a, i);
-                const uint32_t d = tmem + (it & 1) * 256;
-                if (!ring_wait<true>(&sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
-                    ok = false;
-                    break;
-                }
-                tmem_fence_after();
-                for (int k = t.k0; k < t.k1; ++k) {
-                    if (!ring_wait<true>(&full[r.stage], r.phase)) {
+                for (int k = t.k0; k < t.k1 && ok; ++it) {
+                    const uint32_t d = tmem + (it & 1) * 256;
+                    const int first = k, last = kPortion ? min(k + kMmaPortion, t.k1) : t.k1;
+                    if (!ring_wait<true>(&sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
                         ok = false;
                         break;
                     }
                     tmem_fence_after();
-                    const uint32_t at = stages + uint32_t(r.stage) * 2 * kMmaHalf;
-                    const uint64_t da = mma_desc<A_MN>(at), db = mma_desc<B_MN>(at + kMmaHalf);
-                    if (elect_one()) {
+                    for (; k < last; ++k) {
+                        if (!ring_wait<true>(&full[r.stage], r.phase)) {
+                            ok = false;
+                            break;
+                        }
+                        tmem_fence_after();
+                        const uint32_t at = stages + uint32_t(r.stage) * 2 * kMmaHalf;
+                        const uint64_t da = mma_desc<A_MN>(at), db = mma_desc<B_MN>(at + kMmaHalf);
+                        if (elect_one()) {
 #pragma unroll
-                        for (int j = 0; j < kMmaK / 16; ++j)
-                            mma_f16<2>(d, da + j * kDescStep16<A_MN>, db + j * kDescStep16<B_MN>, idesc, k > t.k0 || j > 0);
-                        mma_commit<2>(&empty[r.stage]);
+                            for (int j = 0; j < kMmaK / 16; ++j)
+                                mma_f16<2>(d, da + j * kDescStep16<A_MN>, db + j * kDescStep16<B_MN>, idesc, k > first || j > 0);
+                            mma_commit<2>(&empty[r.stage]);
+                        }
+                        __syncwarp();
+                        r.next<kMmaStages>();
                     }
+                    if (elect_one()) mma_commit<2>(&sums_full[it & 1]);
                     __syncwarp();
-                    r.next<kMmaStages>();
                 }
-                if (elect_one()) mma_commit<2>(&sums_full[it & 1]);
-                __syncwarp();
             }
+        }
+    } else if (warp >= 4 && kPortion) {
+        // Both sets read every portion, a half of the columns each, and keep the sums in registers.
+        const int half = (warp - 4) >> 2, quad = warp & 3;
+        const uint32_t empty_bar[2] = {peer_shared(&sums_empty[0], 0), peer_shared(&sums_empty[1], 0)};
+        int it = 0;
+        for (int i = pair; i < tiles && ok; i += pairs) {
+            const MmaTile t = mma_tile(a, i);
+            const int row = t.m * kMmaTile + int(rank) * 128 + quad * 32 + lane;
+            const bool valid = row < a.rows;
+            uint32_t bits[4];
+            tile_mask(a, valid ? row : a.rows - 1, t.n * kMmaTile + 128 * half, bits);
+            float sums[128] = {};
+            for (int k = t.k0; k < t.k1; k += kMmaPortion, ++it) {
+                if (!ring_wait<true>(&sums_full[it & 1], (it >> 1) & 1)) {
+                    ok = false;
+                    break;
+                }
+                tmem_fence_after();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t v[32];
+                    __syncwarp();
+                    tmem_ld32(tmem + (it & 1) * 256 + 128 * half + 32 * c + (uint32_t(quad * 32) << 16), v);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sums[32 * c + j] += __uint_as_float(v[j]);
+                }
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_at_peer(empty_bar[it & 1]);
+            }
+            if (ok) loss_epilogue(a, t, half, row, valid, sums, bits);
         }
     } else if (warp >= 4) {
         const int set = (warp - 4) >> 2, quad = warp & 3;
@@ -320,14 +344,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             const int row = t.m * kMmaTile + int(rank) * 128 + quad * 32 + lane;
             const bool valid = row < a.rows;
             uint32_t bits[8];
-            if (KIND == kMmaLoss || KIND == kMmaGrad) tile_mask(a, valid ? row : a.rows - 1, t.n * kMmaTile, bits);
+            if (KIND == kMmaGrad) tile_mask(a, valid ? row : a.rows - 1, t.n * kMmaTile, bits);
             if (!ring_wait<true>(&sums_full[set], (it >> 1) & 1)) {
                 ok = false;
                 break;
             }
             tmem_fence_after();
             const uint32_t d = tmem + set * 256 + (uint32_t(quad * 32) << 16);
-            if (KIND == kMmaLoss) loss_epilogue(a, t, row, d, valid, bits);
             if (KIND == kMmaGrad) grad_epilogue(a, t, row, d, valid, bits);
             if (KIND == kMmaSum) out_epilogue<false>(a, t, row, d, valid);
             if (KIND == kMmaBf16) out_epilogue<true>(a, t, row, d, valid);

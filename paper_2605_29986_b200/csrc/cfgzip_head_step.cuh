@@ -363,7 +363,7 @@ __device__ __forceinline__ void step_finish_row(const HeadStepArgs& a, int row, 
 // times, and straight code cost more in instruction fetches than it saved.
 template <bool MX, int W>
 __device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& sh, int quad, float back, const int32_t* list, int tokens,
-                                            bool all, uint32_t tmem, const uint32_t (&bits)[W], Partial (&state)[W], int lane) {
+                                            bool all, uint32_t tmem, int cuts, uint32_t cut_step, const uint32_t (&bits)[W], Partial (&state)[W], int lane) {
     float* turn = sh.turn[quad];
 #pragma unroll
     for (int c = 0; c < W; ++c) {
@@ -374,6 +374,17 @@ __device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& s
             __syncwarp();
             tmem_ld32(tmem + 32 * c, v);
             tmem_wait_ld();
+#pragma unroll 1
+            for (int i = 1; !MX && i < cuts; ++i) {
+#pragma unroll
+                for (int h = 0; h < 32; h += 16) {
+                    uint32_t u[16];
+                    tmem_ld16(tmem + i * cut_step + 32 * c + h, u);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[h + j] = __float_as_uint(__uint_as_float(v[h + j]) + __uint_as_float(u[j]));
+                }
+            }
 #pragma unroll
             for (int j = 0; j < 32; ++j)
                 turn[j * 33 + lane] = (bits[c] >> j) & 1u ? (MX ? __uint_as_float(v[j]) * sh.back[32 * c + j] * back : __uint_as_float(v[j]))
@@ -470,22 +481,30 @@ __device__ __forceinline__ void mma_f16_from_tmem(uint32_t d, uint32_t a, uint64
         : "memory");
 }
 
-// How a block's stages are laid out: for blocks of more than 128 tokens two tiles of 128 side by side, which share the hidden
-// states (one from a 4-bit head, whose tiles come one by one through tensor memory); otherwise as many rows as there are tokens
+// How a block's stages are laid out: for blocks of more than 128 tokens and up to 32 rows two tiles of 128 side by side, which share
+// the hidden states; otherwise one (of a 4-bit head they come one by one through tensor memory), of as many rows as there are tokens
 // (rounded up to 32) and so many more atoms of them. A product takes 128 rows all the same: what it reads behind the rows that are
 // there gives sums that nobody reads.
 template <bool MX>
-constexpr int kStepTiles = MX ? 1 : 2;
+constexpr int kStepTiles = MX ? 1 : 2;  // most
+//
+// The products' sums in tensor memory are cut off towards zero at every addition (measured: -1e-9 of the score per element of the
+// row, 4e-6 for 4096, ten times what sums that are rounded come to), so that a row's k is cut in `cuts` pieces with sums of their own,
+// as many as there is room for, which are added up, and rounded, when they are read. (Of a 4-bit head there are none: its weights on
+// their way take the room.)
 struct StepLayout {
-    int tiles, rows, atoms, steps, stages;
+    int tiles, rows, atoms, steps, stages, cuts, cut_atoms;
     uint32_t x_at, bytes;
 };
 template <bool MX>
 __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int most) {
     constexpr int X = MX ? 4 : 1;  // atoms of hidden states to an atom of weights
     StepLayout l;
-    l.tiles = most > 128 ? kStepTiles<MX> : 1;
-    l.rows = most > 128 ? 128 * kStepTiles<MX> : (max(most, 1) + 31) & ~31;
+    l.tiles = most > 128 && a.N == 32 ? kStepTiles<MX> : 1;
+    l.rows = most > 128 ? 128 * l.tiles : (max(most, 1) + 31) & ~31;
+    const int room = MX ? 1 : 512 / (2 * l.tiles * a.N);
+    l.cut_atoms = room >= 8 ? (a.row_atoms + 7) >> 3 : room >= 4 ? (a.row_atoms + 3) >> 2 : room >= 2 ? (a.row_atoms + 1) >> 1 : a.row_atoms;
+    l.cuts = (a.row_atoms + l.cut_atoms - 1) / l.cut_atoms;
     l.atoms = 1;
     int shift = 0;
     while (!MX && shift < 3 && l.atoms < a.row_atoms && 2 * l.atoms * (l.rows + X * a.N) * kStepAtom <= (48u << 10)) {
@@ -509,7 +528,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     __shared__ __align__(16) StepShared sh;
     const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
-    const uint32_t columns = MX ? 512 : 4 * a.N <= 128 ? 128 : 4 * a.N <= 256 ? 256 : 512;
+    const uint32_t columns = 512;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStepStages; ++i) {
             mbar_init(&sh.empty[i], MX ? 1 + 4 : 1);  // the products, and the warps that take weights apart
@@ -612,7 +631,8 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     break;
                 }
                 tmem_fence_after();
-                const uint32_t d0 = tmem + uint32_t(it & 1) * l.tiles * a.N;
+                uint32_t d0 = tmem + uint32_t(it & 1) * l.cuts * l.tiles * a.N;
+                int in_cut = 0;  // atoms of the cut that are through
                 for (int s = 0; s < l.steps && ok; ++s) {
                     if (!ring_wait(&sh.full[stage], phase)) {
                         ok = false;
@@ -631,7 +651,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
 #pragma unroll
                             for (int j = 0; j < 16; ++j)
                                 mma_f16_from_tmem(d0, tmem + 128 * (set + 1) + 8 * j, dx + j / 4 * x_step + (j & 3) * kDescStep16<false>, idesc,
-                                                  s > 0 || j > 0);
+                                                  in_cut > 0 || j > 0);
                             mma_commit<1>(&sh.w_empty[set]);
                         }
                         __syncwarp();
@@ -639,15 +659,23 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                         if (++set == sets) set = 0;
                         if (elect_one()) mma_commit<1>(&sh.empty[stage]);
                     } else if (elect_one()) {
-                        for (int p = 0; p < atoms; ++p)
+                        uint32_t d = d0;
+                        int in = in_cut;
+                        for (int p = 0; p < atoms; ++p) {
                             for (int t = 0; t < tiles; ++t)
 #pragma unroll
                                 for (int j = 0; j < 4; ++j)
-                                    mma_f16<1>(d0 + t * a.N, dw + p * w_step + t * (kStepTile >> 4) + j * kDescStep16<false>,
-                                               dx + p * x_step + j * kDescStep16<false>, idesc, s > 0 || p > 0 || j > 0);
+                                    mma_f16<1>(d + t * a.N, dw + p * w_step + t * (kStepTile >> 4) + j * kDescStep16<false>,
+                                               dx + p * x_step + j * kDescStep16<false>, idesc, in > 0 || j > 0);
+                            if (++in == l.cut_atoms) {
+                                in = 0;
+                                d += l.tiles * a.N;
+                            }
+                        }
                         mma_commit<1>(&sh.empty[stage]);
                     }
                     __syncwarp();
+                    for (in_cut += atoms; in_cut >= l.cut_atoms; in_cut -= l.cut_atoms) d0 += l.tiles * a.N;
                     next();
                 }
                 if (elect_one()) mma_commit<1>(&sh.sums_full[it & 1]);
@@ -812,7 +840,8 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     const int at = g * per_group + t * 128 + quad * 32;
                     if (t < l.tiles && at < n)
                         step_scores<MX>(a, sh, quad, MX ? mx_scale(largest) : 1.f, sh.list + at, n - at, all,
-                                        tmem + uint32_t((it & 1) * l.tiles + t) * a.N + (uint32_t(quad * 32) << 16), bits[t], state, lane);
+                                        tmem + uint32_t((it & 1) * l.cuts * l.tiles + t) * a.N + (uint32_t(quad * 32) << 16), l.cuts,
+                                        uint32_t(l.tiles) * a.N, bits[t], state, lane);
                 }
                 tmem_fence_before();
                 __syncwarp();
