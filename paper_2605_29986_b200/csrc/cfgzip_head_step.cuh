@@ -369,26 +369,25 @@ __device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& s
     for (int c = 0; c < W; ++c) {
         if (32 * c >= a.B) break;
         const int rows = min(32, a.B - 32 * c);
-        {
-            uint32_t v[32];
+#pragma unroll
+        for (int h = 0; h < 32; h += 16) {
+            uint32_t v[16];
             __syncwarp();
-            tmem_ld32(tmem + 32 * c, v);
+            tmem_ld16(tmem + 32 * c + h, v);
             tmem_wait_ld();
 #pragma unroll 1
-            for (int i = 1; !MX && i < cuts; ++i) {
+            for (int i = 1; i < cuts; ++i) {
+                uint32_t u[16];
+                tmem_ld16(tmem + i * cut_step + 32 * c + h, u);
+                tmem_wait_ld();
 #pragma unroll
-                for (int h = 0; h < 32; h += 16) {
-                    uint32_t u[16];
-                    tmem_ld16(tmem + i * cut_step + 32 * c + h, u);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[h + j] = __float_as_uint(__uint_as_float(v[h + j]) + __uint_as_float(u[j]));
-                }
+                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(u[j]));
             }
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-                turn[j * 33 + lane] = (bits[c] >> j) & 1u ? (MX ? __uint_as_float(v[j]) * sh.back[32 * c + j] * back : __uint_as_float(v[j]))
-                                                          : -INFINITY;
+            for (int j = 0; j < 16; ++j)
+                turn[(h + j) * 33 + lane] = (bits[c] >> (h + j)) & 1u
+                                                ? (MX ? __uint_as_float(v[j]) * sh.back[32 * c + h + j] * back : __uint_as_float(v[j]))
+                                                : -INFINITY;
         }
         const uint32_t has = warp_transpose32(bits[c], lane);
         __syncwarp();
@@ -490,8 +489,7 @@ constexpr int kStepTiles = MX ? 1 : 2;  // most
 //
 // The products' sums in tensor memory are cut off towards zero at every addition (measured: -1e-9 of the score per element of the
 // row, 4e-6 for 4096, ten times what sums that are rounded come to), so that a row's k is cut in `cuts` pieces with sums of their own,
-// as many as there is room for, which are added up, and rounded, when they are read. (Of a 4-bit head there are none: its weights on
-// their way take the room.)
+// as many as there is room for, which are added up, and rounded, when they are read.
 struct StepLayout {
     int tiles, rows, atoms, steps, stages, cuts, cut_atoms;
     uint32_t x_at, bytes;
@@ -502,7 +500,7 @@ __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int mos
     StepLayout l;
     l.tiles = most > 128 && a.N == 32 ? kStepTiles<MX> : 1;
     l.rows = most > 128 ? 128 * l.tiles : (max(most, 1) + 31) & ~31;
-    const int room = MX ? 1 : 512 / (2 * l.tiles * a.N);
+    const int room = (MX ? 128 : 512) / (2 * l.tiles * a.N);
     l.cut_atoms = room >= 8 ? (a.row_atoms + 7) >> 3 : room >= 4 ? (a.row_atoms + 3) >> 2 : room >= 2 ? (a.row_atoms + 1) >> 1 : a.row_atoms;
     l.cuts = (a.row_atoms + l.cut_atoms - 1) / l.cut_atoms;
     l.atoms = 1;
