@@ -105,7 +105,8 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
         s.bits = c.take<uint32_t>(std::min<int64_t>(up(n, 32), kStepRows) * ceil_div(h->V, 32));
         s.counts = c.take<int32_t>(ceil_div(h->V, 32 * kUnionWords));
         s.ticket = c.take<uint32_t>(1);
-        s.states = c.take<Partial>(std::min<int64_t>(n, kStepRows) * kStepBlocks);
+        const bool tall = n > kStepRows && h->dtype == CFGZIP_BF16;
+        s.states = c.take<Partial>(std::max(std::min<int64_t>(n, kStepRows) * kStepBlocks, tall ? n * 2 * ceil_div(h->V, kMmaTile) : 0));
         if (h->dtype == CFGZIP_MXFP4) {
             s.half = c.take<uint16_t>(std::min<int64_t>(n, kStepRowsMx) * up(h->H, 2 * int(kStepAtom)));
             s.back = c.take<float>(kStepRowsMx);
@@ -310,11 +311,43 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
     uint32_t* mask = vocab_mask ? vocab_mask : w.mask;
     const int64_t mask_stride = vocab_mask ? vocab_stride_words : ps.VW;
     const PartDev& one = ctx->parts[size_t(part0)].dev;
-    const bool table = !rows && one.c16 && one.KW <= kTableWords;
+    // More rows than one pass over the weights takes are a product of two tall matrices, and together they allow most of the
+    // vocabulary. (256 rows of 128256 x 4096: 2 passes 476 us. Its scores leave in the wrong order to be stored.)
+    const bool tall = B > kStepRows && head->dtype == CFGZIP_BF16 && !logits;
+    const bool table = !tall && !rows && one.c16 && one.KW <= kTableWords;
     if (!table && (rc = cfgzip_expand_mask(ctx, part0, row_part, class_mask, class_stride_words, mask, mask_stride, B, CFGZIP_DENSE, stream)) !=
         CFGZIP_OK)
         return rc;
     const int32_t most = head->dtype == CFGZIP_MXFP4 ? kStepRowsMx : kStepRows;
+    if (tall) {
+        CUtensorMap map_x, map_w;
+        if ((rc = tensor_map(ctx, &map_x, hidden, B, head->H, hidden_stride, 128)) != CFGZIP_OK ||
+            (rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, 128)) != CFGZIP_OK)
+            return rc;
+        MmaArgs a{};
+        a.rows = B;
+        a.cols = a.V = head->V;
+        a.k_blocks = ceil_div(head->H, kMmaK);
+        a.m_fast = 1;
+        a.mask = mask;
+        a.mask_stride = mask_stride;
+        a.states = w.states;
+        if ((rc = run_mma<false, false, kMmaStep>(ctx, a, map_x, map_w, st)) != CFGZIP_OK) return rc;
+        HeadStepArgs s{};
+        s.parts = ctx->d_parts;
+        s.part0 = part0;
+        s.n_parts = int32_t(ctx->parts.size());
+        s.row_part = rows;
+        s.B = B;
+        s.V = head->V;
+        s.part = w.states;
+        s.argmax = argmax;
+        s.rep = rep;
+        s.logp = logp_argmax;
+        s.lse = lse;
+        s.status = ctx->d_status;
+        return launch(ctx, k_head_step_finish, dim3(unsigned(ceil_div(B, 8))), dim3(256), 0, st, s, 2 * a.n_tiles);
+    }
     for (int32_t b = 0; b < B; b += most) {
         HeadStepArgs s{};
         StepMasks m;

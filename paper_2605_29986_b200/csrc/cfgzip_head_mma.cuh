@@ -25,7 +25,7 @@ constexpr int kMmaPortion = 8;
 constexpr uint32_t kMmaHalf = 128 * kMmaK * 2;           // bytes of one operand of a stage in one block
 constexpr size_t kMmaSmem = size_t(kMmaStages) * 2 * kMmaHalf + 1024;
 
-enum : int { kMmaLoss = 0, kMmaGrad = 1, kMmaSum = 2, kMmaBf16 = 3 };
+enum : int { kMmaLoss = 0, kMmaGrad = 1, kMmaSum = 2, kMmaBf16 = 3, kMmaStep = 4 };
 
 struct MmaArgs {
     int32_t rows, cols;        // of the result (tokens x piece of the vocabulary, ...)
@@ -41,6 +41,7 @@ struct MmaArgs {
     const float *lse, *d_loss;
     float2* part;              // loss: [2 n_tiles, rows] largest score and sum of half a tile
     float* of_target;          // loss: [rows]
+    Partial* states;           // step: [2 n_tiles, rows] the same with the token
     // results
     void* out;
     int64_t ld;                // elements
@@ -103,6 +104,30 @@ __device__ __forceinline__ void loss_epilogue(const MmaArgs& a, const MmaTile& t
 #pragma unroll
     for (int j = 0; j < 128; ++j) s[j & 3] += ex2f((z[j] - ref) * kLog2e);
     if (valid) a.part[int64_t(2 * t.n + half) * a.rows + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+}
+
+// Largest allowed score, its lowest token and the sum of exponentials, of one row and half a tile's tokens.
+__device__ __forceinline__ void step_epilogue(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, float (&z)[128],
+                                              const uint32_t (&bits)[4]) {
+    float m = -INFINITY;
+    int at = kNoPos;
+#pragma unroll
+    for (int c = 3; c >= 0; --c)
+        if (bits[c]) at = 32 * c + __ffs(bits[c]) - 1;  // (scores that are all -inf)
+#pragma unroll
+    for (int j = 0; j < 128; ++j) {
+        z[j] = (bits[j / 32] >> (j & 31)) & 1u ? z[j] : -INFINITY;
+        at = z[j] > m ? j : at;
+        m = fmaxf(m, z[j]);
+    }
+    const float ref = fmaxf(m, kRefFloor);
+    float s[4] = {};
+#pragma unroll
+    for (int j = 0; j < 128; ++j) s[j & 3] += ex2f((z[j] - ref) * kLog2e);
+    if (valid)
+        *reinterpret_cast<int4*>(&a.states[int64_t(2 * t.n + half) * a.rows + row]) =
+            make_int4(__float_as_int(m), __float_as_int((s[0] + s[1]) + (s[2] + s[3])),
+                      at == kNoPos ? kNoPos : a.t0 + t.n * kMmaTile + 128 * half + at, 0);
 }
 
 // g = d (exp(z - lse) - [target]) of the allowed tokens, as bf16.
@@ -209,7 +234,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kMmaStages], empty[kMmaStages], sums_full[2], sums_empty[2];
     __shared__ uint32_t s_tmem;
-    constexpr bool kPortion = KIND == kMmaLoss;
+    constexpr bool kPortion = KIND == kMmaLoss || KIND == kMmaStep;
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -332,7 +357,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                 __syncwarp();
                 if (lane == 0) arrive_at_peer(empty_bar[it & 1]);
             }
-            if (ok) loss_epilogue(a, t, half, row, valid, sums, bits);
+            if (ok && KIND == kMmaLoss) loss_epilogue(a, t, half, row, valid, sums, bits);
+            if (ok && KIND == kMmaStep) step_epilogue(a, t, half, row, valid, sums, bits);
         }
     } else if (warp >= 4) {
         const int set = (warp - 4) >> 2, quad = warp & 3;

@@ -329,18 +329,18 @@ __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh,
     return hi - lo;
 }
 
-// The state of one row from every block's, and the row's results; a warp.
+// The state of one row from every block's ([blocks, B] in a.part), and the row's results; a warp.
 __device__ __forceinline__ void step_finish_row(const HeadStepArgs& a, int row, int blocks, int lane) {
     const int part = step_row_part(a, row);
     if (part < 0) return;
     float top = -INFINITY;
-    for (int i = lane; i < blocks; i += 32) top = fmaxf(top, __ldcg(&a.part[i * a.B + row].m));
+    for (int i = lane; i < blocks; i += 32) top = fmaxf(top, __ldcg(&a.part[int64_t(i) * a.B + row].m));
     top = redux_max(top);
     const float ref = fmaxf(top, kRefFloor);
     float s = 0.f;
     int pos = kNoPos;
     for (int i = lane; i < blocks; i += 32) {
-        const int4 v = __ldcg(reinterpret_cast<const int4*>(&a.part[i * a.B + row]));
+        const int4 v = __ldcg(reinterpret_cast<const int4*>(&a.part[int64_t(i) * a.B + row]));
         const float m = __int_as_float(v.x);
         s += __int_as_float(v.y) * ex2f((fmaxf(m, kRefFloor) - ref) * kLog2e);
         if (m == top) pos = min(pos, v.z);
@@ -877,6 +877,13 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     if (!sh.is_last) return;
     __threadfence();
     for (int row = warp; row < a.B; row += kThreads / 32) step_finish_row(a, row, gridDim.x, lane);
+}
+
+// Results of rows whose states are those of `states` pieces of the vocabulary, a warp a row.
+__global__ void __launch_bounds__(256) k_head_step_finish(const HeadStepArgs a, int states) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int row = blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (row < a.B) step_finish_row(a, row, states, threadIdx.x & 31);
 }
 
 }  // namespace cfgzip
