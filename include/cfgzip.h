@@ -299,7 +299,10 @@ int cfgzip_head_dequantize(cfgzip_ctx* ctx, const cfgzip_head* head, void* value
 
 /*
  * cfgzip_masked_logsoftmax_argmax from hidden states: the scores of the tokens that some row of the batch allows are computed
- * (weights of other tokens are not read) and reduced without being stored.
+ * and reduced without being stored. Weights of other tokens are not read, unless nearly all are allowed (15/16 of them, 3/4 for a
+ * 4-bit head) or the batch has more than 128 rows; they have no part in the results in any case, whatever they are. Scores are
+ * within about 1e-6 of their largest partial sums (4-bit heads: weights of a block whose scale is more than 2^23 times below the
+ * largest of its row are cut off at 2^-25 of that).
  *   part0, row_part, class_mask : as there; the partitions' V is that of the head (CFGZIP_E_RANGE otherwise)
  *   hidden     : dev bf16 [B, hidden_stride]
  *   vocab_mask : nullable, as there
@@ -333,7 +336,8 @@ int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidde
  * Its gradient. With g[n, t] = d_loss[n] * (exp(z[n, t] - lse[n]) - [t = targets[n]]) over the allowed tokens, and 0 in rows
  * whose loss is not a finite function of z (a negative target, one that is not allowed, nothing allowed):
  *   d_hidden[n, :] = sum_t g[n, t] * weight[t, :],    d_weight[t, :] = sum_n g[n, t] * hidden[n, :]
- * The scores are computed again; g is rounded to bf16 (relative 2^-9) for the two products, which accumulate in 32 bits.
+ * The scores are computed again; g is rounded to bf16 (by 2^-8 of itself at most) for the two products, which accumulate in 32
+ * bits; a gradient in 32 bits has that in it too.
  *   hidden .. targets : as given to cfgzip_head_loss, and lse as it returned it (required)
  *   d_loss     : dev float [N]
  *   d_hidden   : nullable dev bf16 [N, d_hidden_stride] (written)

@@ -255,11 +255,11 @@ int cfgzip_head_workspace(const cfgzip_head* head, int op, int32_t rows, int64_t
 
 int cfgzip_head_quantize(cfgzip_ctx* ctx, const void* weight, int dtype, int64_t row_stride_elems, const cfgzip_head* head,
                          void* stream) {
-    if (!ctx || !weight || (dtype != CFGZIP_F32 && dtype != CFGZIP_BF16)) return CFGZIP_E_ARG;
-    int rc = check_head(head);
+    const int rc = check_head(head);
     if (rc != CFGZIP_OK) return rc;
-    if (head->dtype != CFGZIP_MXFP4 || row_stride_elems < head->H) return CFGZIP_E_ARG;
+    if (head->dtype != CFGZIP_MXFP4 || !weight || (dtype != CFGZIP_F32 && dtype != CFGZIP_BF16) || row_stride_elems < head->H) return CFGZIP_E_ARG;
     if (!on16(weight, row_stride_elems * (dtype == CFGZIP_BF16 ? 2 : 4))) return CFGZIP_E_ALIGN;
+    if (!ctx) return CFGZIP_E_ARG;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;
     dim3 grid, block;
@@ -270,11 +270,11 @@ int cfgzip_head_quantize(cfgzip_ctx* ctx, const void* weight, int dtype, int64_t
 }
 
 int cfgzip_head_dequantize(cfgzip_ctx* ctx, const cfgzip_head* head, void* values, int64_t row_stride_elems, void* stream) {
-    if (!ctx) return CFGZIP_E_ARG;
     int rc = check_head(head);
     if (rc != CFGZIP_OK) return rc;
     if (head->dtype != CFGZIP_MXFP4) return CFGZIP_E_ARG;
     if ((rc = check_rows(head, values, row_stride_elems)) != CFGZIP_OK) return rc;
+    if (!ctx) return CFGZIP_E_ARG;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;
     dim3 grid, block;
@@ -289,9 +289,19 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
                      uint32_t* vocab_mask, int64_t vocab_stride_words, void* logits, int logits_dtype, int64_t logits_stride,
                      int32_t* argmax, int32_t* rep, float* logp_argmax, float* lse, void* workspace, int64_t workspace_bytes,
                      void* stream) {
-    if (!ctx || B < 0) return CFGZIP_E_ARG;
     int rc = check_head(head);
     if (rc != CFGZIP_OK) return rc;
+    if (B < 0) return CFGZIP_E_ARG;
+    HeadSpace w{};
+    if (B > 0) {
+        if (!argmax || !class_mask || class_stride_words <= 0 || (vocab_mask && vocab_stride_words < ceil_div(head->V, 32))) return CFGZIP_E_ARG;
+        if (logits && ((logits_dtype != CFGZIP_F32 && logits_dtype != CFGZIP_BF16) || logits_stride < head->V)) return CFGZIP_E_ARG;
+        if ((rc = check_rows(head, hidden, hidden_stride)) != CFGZIP_OK) return rc;
+        if (!workspace) return CFGZIP_E_ARG;
+        w = head_space(head, CFGZIP_HEAD_STEP, B, workspace);
+        if (workspace_bytes < w.bytes) return CFGZIP_E_NOMEM;
+    }
+    if (!ctx) return CFGZIP_E_ARG;
     bool planned;
     const int32_t* rows = row_part;
     if ((rc = resolve_row_part(ctx, part0, &rows, B, &planned)) != CFGZIP_OK) return rc;
@@ -299,12 +309,7 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
     if ((rc = resolve_parts(ctx, part0, rows != nullptr, &ps)) != CFGZIP_OK) return rc;
     if (ps.V != head->V) return CFGZIP_E_RANGE;
     if (B == 0) return CFGZIP_OK;
-    if (!argmax || !class_mask || class_stride_words < ps.maxKW || (vocab_mask && vocab_stride_words < ps.VW)) return CFGZIP_E_ARG;
-    if (logits && ((logits_dtype != CFGZIP_F32 && logits_dtype != CFGZIP_BF16) || logits_stride < head->V)) return CFGZIP_E_ARG;
-    if ((rc = check_rows(head, hidden, hidden_stride)) != CFGZIP_OK) return rc;
-    if (!workspace) return CFGZIP_E_ARG;
-    const HeadSpace w = head_space(head, CFGZIP_HEAD_STEP, B, workspace);
-    if (workspace_bytes < w.bytes) return CFGZIP_E_NOMEM;
+    if (class_stride_words < ps.maxKW) return CFGZIP_E_ARG;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -385,16 +390,16 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
 int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N,
                      const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* targets, float* loss, float* lse,
                      void* workspace, int64_t workspace_bytes, void* stream) {
-    if (!ctx || N < 0) return CFGZIP_E_ARG;
     int rc = check_head(head);
     if (rc != CFGZIP_OK) return rc;
-    if (head->dtype != CFGZIP_BF16) return CFGZIP_E_ARG;
-    if (N == 0) return CFGZIP_OK;
+    if (head->dtype != CFGZIP_BF16 || N < 0) return CFGZIP_E_ARG;
+    if (N == 0) return ctx ? CFGZIP_OK : CFGZIP_E_ARG;
     if (!targets || !loss || (vocab_mask && vocab_stride_words < ceil_div(head->V, 32))) return CFGZIP_E_ARG;
     if ((rc = check_rows(head, hidden, hidden_stride)) != CFGZIP_OK) return rc;
     if (!workspace) return CFGZIP_E_ARG;
     const HeadSpace w = head_space(head, CFGZIP_HEAD_LOSS, N, workspace);
     if (workspace_bytes < w.bytes) return CFGZIP_E_NOMEM;
+    if (!ctx) return CFGZIP_E_ARG;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -432,10 +437,9 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
                               const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* targets, const float* lse,
                               const float* d_loss, void* d_hidden, int64_t d_hidden_stride, void* d_weight, int d_weight_dtype,
                               int64_t d_weight_stride, int accumulate, void* workspace, int64_t workspace_bytes, void* stream) {
-    if (!ctx || N < 0) return CFGZIP_E_ARG;
     int rc = check_head(head);
     if (rc != CFGZIP_OK) return rc;
-    if (head->dtype != CFGZIP_BF16 || (!d_hidden && !d_weight)) return CFGZIP_E_ARG;
+    if (head->dtype != CFGZIP_BF16 || N < 0 || (!d_hidden && !d_weight)) return CFGZIP_E_ARG;
     if (d_weight) {
         if ((d_weight_dtype != CFGZIP_F32 && d_weight_dtype != CFGZIP_BF16) || d_weight_stride < head->H) return CFGZIP_E_ARG;
         if (!on16(d_weight, d_weight_stride * (d_weight_dtype == CFGZIP_BF16 ? 2 : 4))) return CFGZIP_E_ALIGN;
@@ -448,6 +452,7 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
     }
     const HeadSpace w = head_space(head, CFGZIP_HEAD_LOSS_BACKWARD, N, workspace);
     if (N > 0 && workspace_bytes < w.bytes) return CFGZIP_E_NOMEM;
+    if (!ctx) return CFGZIP_E_ARG;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -123,8 +123,9 @@ def test_step(V, H, B, K, density, head, pad, everything):
             assert cz.cfgzip_poll_status(ctx.h) == (int((~mask.any(dim=1)).sum()), 0, 0)
 
 
-def test_step_on_rows_of_several_partitions_and_rows_of_none():
-    V, H, B = 3001, 128, 70
+@pytest.mark.parametrize("B", [70, 150])  # (one pass over the weights, and a product of two tall matrices where logits are not asked for)
+def test_step_on_rows_of_several_partitions_and_rows_of_none(B):
+    V, H = 3001, 128
     parts = [synth.zipf_partition(V, K, 1.1, seed=K) for K in (40, 300, 77)]
     for head in ("bf16", "mxfp4"):
         case = Case(V, H, B, head, seed=11)
@@ -140,7 +141,7 @@ def test_step_on_rows_of_several_partitions_and_rows_of_none():
                 reps[b] = torch.from_numpy(p.r[p.c]).cuda()
             ids = np.array(ctx.ids, dtype=np.int32)[which]
             bad = np.zeros(B, dtype=bool)
-            bad[[0, 33, 69]] = True
+            bad[[0, 33, B - 1]] = True
             ids[bad] = [-1, 1000, 3]
             cz.cfgzip_poll_status(ctx.h)
             for logits in (None, torch.float32):
@@ -188,6 +189,73 @@ def test_step_reads_nothing_of_tokens_that_no_row_allows():
         with Ctx([p]) as ctx:
             out = run_step(ctx, case, dev(cm), B, logits=torch.float32)
             check_step(case, out, mask, torch.from_numpy(p.r[p.c]).cuda())
+
+
+def test_step_refuses_a_head_of_another_vocabulary_and_short_masks():
+    V, K = 300, 40
+    case, other = Case(V, 64, 2, seed=1), Case(V + 1, 64, 2, seed=1)
+    with Ctx([synth.zipf_partition(V, K, 1.1, seed=1)]) as ctx:
+        cm = dev(class_masks(K, 2, 0.5, (1, 1)))
+        am = torch.full((2,), -7, dtype=torch.int32, device="cuda")
+        ws = torch.zeros(1 << 22, dtype=torch.uint8, device="cuda")
+
+        def status(case, part=None, stride=2):
+            with pytest.raises(cz.CfgzipError) as e:
+                cz.cfgzip_head_step(ctx.h, ctx.ids[0] if part is None else part, None, cm, stride, case.head, case.hidden, 64, 2, None, 0,
+                                    None, 0, 0, am, None, None, None, ws, ws.numel())
+            return e.value.status
+
+        assert status(other) == cz.E_RANGE and status(case, part=5) == cz.E_RANGE and status(case, stride=1) == cz.E_ARG
+        torch.cuda.synchronize()
+        assert am.tolist() == [-7, -7]
+
+
+def test_two_steps_at_once_with_a_workspace_each():
+    V, H, B, K = 30000, 512, 20, 300
+    p = synth.zipf_partition(V, K, 1.1, seed=3)
+    c, trep = torch.from_numpy(p.c).long().cuda(), torch.from_numpy(p.r[p.c]).cuda()
+    cases = [Case(V, H, B, head, seed=k) for k, head in enumerate(("bf16", "mxfp4"))]
+    streams = [torch.cuda.Stream() for _ in cases]
+    masks = [dev(class_masks(K, B, d, (2, 1))) for d in (0.05, 0.6)]
+    ctxs = [Ctx([p]) for _ in cases]  # (a context is one stream's)
+    try:
+        torch.cuda.synchronize()
+        outs = []
+        for case, ctx, st, cm in zip(cases, ctxs, streams, masks):
+            out = dict(vocab_mask=None, logits=None, argmax=torch.zeros(B, dtype=torch.int32, device="cuda"),
+                       rep=torch.zeros(B, dtype=torch.int32, device="cuda"), logp=torch.zeros(B, device="cuda"), lse=torch.zeros(B, device="cuda"))
+            outs.append((out, case.workspace(cz.HEAD_STEP)))
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for (out, ws), case, ctx, st, cm in zip(outs, cases, ctxs, streams, masks):
+                cz.cfgzip_head_step(ctx.h, ctx.ids[0], None, cm, cm.shape[1], case.head, case.hidden, H, B, None, 0, None, 0, 0, out["argmax"],
+                                    out["rep"], out["logp"], out["lse"], ws, ws.numel(), st)
+        torch.cuda.synchronize()
+        for (out, _), case, cm in zip(outs, cases, masks):
+            check_step(case, out, unpack(cm, K)[:, c], trep)
+    finally:
+        for ctx in ctxs:
+            ctx.close()
+
+
+def test_four_bit_rows_whose_scales_are_far_apart():
+    """Blocks up to 2^23 below the largest scale of their row count in full, and far ones do not spoil the near ones."""
+    V, H, B, K = 400, 256, 5, 9
+    case = Case(V, H, B, "mxfp4", seed=7)
+    case.scales[:] = torch.randint(100, 123, (V, H // 32), generator=case.gen, device="cuda").to(torch.uint8)
+    case.scales[5], case.scales[6, 1:], case.scales[7] = 0, 0, 200   # hardly anything, one block alone, large weights
+    case.hidden[:, 32:] *= 0.25
+    case.x64, case.w64 = case.hidden.double(), mx_values(case.packed, case.scales, H).cuda()
+    case.refresh()
+    # a 4-bit head's weights may be off by 2^-25 of the largest scale of their row
+    top = torch.ldexp(torch.ones(V, dtype=torch.float64, device="cuda"), case.scales.int().amax(dim=1) - 127)
+    case.z_tol = case.z_tol + case.x64.abs().sum(dim=1, keepdim=True) * top * 2.0 ** -25
+    p = synth.zipf_partition(V, K, 1.1, seed=8)
+    with Ctx([p]) as ctx:
+        cm = class_masks(K, B, 0.6, (3, 1))
+        out = run_step(ctx, case, dev(cm), B, logits=torch.float32)
+        mask = unpack(dev(cm), K)[:, torch.from_numpy(p.c).long().cuda()]
+        check_step(case, out, mask, torch.from_numpy(p.r[p.c]).cuda())
 
 
 def test_step_replayed_from_a_graph_on_another_stream():
@@ -443,6 +511,57 @@ def test_gradient(V, H, N, density, pad):
         alone = torch.full((V, H), 77.0, dtype=torch.float32, device="cuda")
         run_backward(ctx, case, packed, targets, lse, d_loss, None, alone)
         assert close(alone, g.T @ case.x64, g.T, g_tol.T, case.x64, N)
+
+
+def test_gradient_in_several_pieces_of_the_vocabulary():
+    V, H, N = 27001, 64, 5003  # scores of two pieces, the second one short; more cuts of the sum than it has stages are not made
+    case, mask, packed, targets = loss_inputs(V, H, N, 0.5, 0, seed=3)
+    assert 2 * N * V > 256 << 20
+    d_loss = torch.rand(N, generator=case.gen, device="cuda") / N
+    g, g_tol = gradient(case, mask, targets, d_loss)
+    with Ctx([]) as ctx:
+        _, lse = run_loss(ctx, case, packed, targets)
+        d_hidden = torch.zeros((N, H), dtype=torch.bfloat16, device="cuda")
+        d_weight = torch.zeros((V, H), dtype=torch.float32, device="cuda")
+        run_backward(ctx, case, packed, targets, lse, d_loss, d_hidden, d_weight)
+        assert close(d_hidden, g @ case.w64, g, g_tol, case.w64, V)
+        assert close(d_weight, g.T @ case.x64, g.T, g_tol.T, case.x64, N)
+        again = torch.zeros_like(d_weight), torch.zeros_like(d_hidden)
+        run_backward(ctx, case, packed, targets, lse, d_loss, again[1], again[0])
+        assert torch.equal(again[0], d_weight) and torch.equal(again[1], d_hidden)
+
+
+def test_gradient_replayed_from_a_graph():
+    V, H, N = 5003, 128, 300
+    case, mask, packed, targets = loss_inputs(V, H, N, 0.3, 0, seed=4)
+    with Ctx([]) as ctx:
+        ws = case.workspace(cz.HEAD_LOSS_BACKWARD), case.workspace(cz.HEAD_LOSS)
+        loss, lse, d_loss = torch.zeros(N, device="cuda"), torch.zeros(N, device="cuda"), torch.full((N,), 1.0 / N, device="cuda")
+        d_hidden, d_weight = torch.zeros((N, H), dtype=torch.bfloat16, device="cuda"), torch.zeros((V, H), device="cuda")
+
+        def both(st):
+            cz.cfgzip_head_loss(ctx.h, case.head, case.hidden, H, N, packed, packed.shape[1], targets, loss, lse, ws[1], ws[1].numel(), st)
+            cz.cfgzip_head_loss_backward(ctx.h, case.head, case.hidden, H, N, packed, packed.shape[1], targets, lse, d_loss, d_hidden, H,
+                                         d_weight, cz.F32, H, 1, ws[0], ws[0].numel(), st)
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        both(side)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            both(side)
+        d_weight.zero_()
+        x = torch.empty((N, H), device="cuda").normal_(0.0, 2.0, generator=case.gen).to(torch.bfloat16)
+        case.hidden.copy_(x)
+        case.x64 = x.double()
+        case.refresh()
+        graph.replay()
+        graph.replay()  # (adds up)
+        torch.cuda.synchronize()
+        g, g_tol = gradient(case, mask, targets, d_loss)
+        assert close(d_hidden, g @ case.w64, g, g_tol, case.w64, V)
+        assert close(d_weight, 2 * (g.T @ case.x64), 2 * g.T, 2 * g_tol.T, case.x64, N)
 
 
 def test_gradient_is_that_of_the_loss():
