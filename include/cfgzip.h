@@ -265,7 +265,8 @@ int cfgzip_map_tokens(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_
  *   CFGZIP_MXFP4 : two weights to a byte, the one with the lower index in the lower half, row_stride in bytes; each is e2m1
  *                  (sign bit, then 0, 0.5, 1, 1.5, 2, 3, 4, 6) times 2^(scale - 127) with one scale byte per 32 weights of a
  *                  row in `scales`, scale_stride bytes from row to row. H a multiple of 32. A scale of 255 is not taken (NaN).
- * Rows of weights, scales, hidden states and gradients start on 16 bytes (CFGZIP_E_ALIGN otherwise); H at most 65536.
+ * Rows of weights, scales, hidden states and gradients start on 16 bytes (CFGZIP_E_ALIGN otherwise); H at most 65536, V at
+ * most 2^30 (CFGZIP_E_RANGE).
  * Hidden states are bf16. They may be any values whose products stay finite; +inf and NaN scores are outside the contract.
  */
 typedef struct cfgzip_head {

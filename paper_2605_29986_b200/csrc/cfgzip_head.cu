@@ -14,14 +14,15 @@ using namespace cfgzip;
 
 namespace {
 
-constexpr int kHeadMost = 65536;  // longest row of a head
+constexpr int kHeadMost = 65536;      // longest row of a head
+constexpr int kHeadTokens = 1 << 30;  // most rows
 
 bool on16(const void* p, int64_t stride_bytes) { return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(stride_bytes)) & 15u) == 0; }
 
 int check_head_shape(const cfgzip_head* h) {
     if (!h || h->V <= 0 || h->H <= 0 || (h->dtype != CFGZIP_BF16 && h->dtype != CFGZIP_MXFP4) || h->reserved) return CFGZIP_E_ARG;
     if (h->H % (h->dtype == CFGZIP_BF16 ? 8 : kMxBlock)) return CFGZIP_E_ARG;
-    return h->H > kHeadMost ? CFGZIP_E_RANGE : CFGZIP_OK;
+    return h->H > kHeadMost || h->V > kHeadTokens ? CFGZIP_E_RANGE : CFGZIP_OK;
 }
 
 int check_head(const cfgzip_head* h) {

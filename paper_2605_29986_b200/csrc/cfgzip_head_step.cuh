@@ -1,6 +1,14 @@
 // The decode step from hidden states. The scores of a batch are a product with one side short (the rows of the batch), so the
 // weights are what takes the time, and only those of tokens that some row allows are read: the union of the rows' masks is
-// compacted to a list of tokens, every block takes an equal share of it and gathers those rows of the head by tiled copies.
+// compacted to a list of tokens, of which every block takes an equal share. The tokens' rows are the long side of tcgen05 products
+// (128 tokens x up to 128 rows), k in stages of shared memory; the scores of a tile go from tensor memory into the rows' running
+// maximum, sum and choice. The last block to finish puts the blocks' together.
+//
+// 32 rows of 128256 x 4096 (bf16, 97 % allowed by some row): 1.05 GB in 181 us with the masks, 5.8 TB/s; inside the loop the copies run
+// at the memory's rate, and 25 us go to the masks, the list, the first loads and the last scores. From 4 bits: 279 MB in 92 us; tiled
+// copies of 128-byte pieces of 128 rows bring 5.2 TB/s at most (measured alone), the rest is the same 25 us and the threads that turn
+// weights into f16, which take 1000 cycles for 128 tokens x 256 weights where the copies take 850. One row of 32000 x 2048: 23 us, of
+// which the loads need 6; what is left is latency (masks 4, list 3, first loads 2, scores and results 4, launches).
 #pragma once
 
 #include <cuda.h>
@@ -14,7 +22,7 @@ constexpr int kStepRows = 128;     // rows of the batch a launch takes at most
 constexpr int kStepRowsMx = 64;    // ... from a 4-bit head: the hidden states are brought past four times as many weights a byte
 constexpr int kStepShare = 2048;   // tokens a block lists at a time
 constexpr int kStepWarps = 16;     // tiled copies, products, tensor memory, idle, four that read the scores, eight that fetch weights
-constexpr int kStepWarpsMx = 24;   // ... and two sets of four that turn 4-bit weights into bf16
+constexpr int kStepWarpsMx = 24;   // ... and two sets of four that turn 4-bit weights into f16
 constexpr int kStepBox = 32;       // rows of weights a small tiled copy brings (a large one: 128)
 constexpr int kStepStages = 12;    // most stages
 constexpr uint32_t kStepAtom = 128;             // bytes of a weight row in an atom, the width of the swizzle
@@ -366,7 +374,8 @@ __device__ __forceinline__ void step_finish_row(const HeadStepArgs& a, int row, 
 // times, and straight code cost more in instruction fetches than it saved.
 template <bool MX, int W>
 __device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& sh, int quad, float back, const int32_t* list, int tokens,
-                                            bool all, uint32_t tmem, int cuts, uint32_t cut_step, const uint32_t (&bits)[W], Partial (&state)[W], int lane) {
+                                            bool all, uint32_t tmem, int cuts, uint32_t cut_step, const uint32_t (&bits)[W],
+                                            Partial (&state)[W], int lane) {
     float* turn = sh.turn[quad];
 #pragma unroll
     for (int c = 0; c < W; ++c) {
@@ -431,7 +440,7 @@ __device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& s
 
 // 4-bit weights in tensor memory are f16, relative to the largest scale of their row: e2m1 numbers times 2^0 down to 2^-23 are
 // exact in f16, and of a block with a scale below that 2^-25 of the largest is lost at most. One conversion and one product for
-// two weights; going to bf16 by shifts, masks and a product takes 19 instructions for eight, not 8, and held the kernel up.
+// two weights; going to bf16 by shifts, masks and products takes 23 instructions for eight (32 rows of 128256 x 4096: 163 us, 130).
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
@@ -456,7 +465,7 @@ __device__ __forceinline__ uint32_t mx_scale_pair(uint32_t byte, uint32_t larges
 // Largest scale byte of a row of n blocks (rows start on 16 bytes).
 __device__ __forceinline__ uint32_t mx_largest(const uint8_t* scales, int n) {
     uint32_t top = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < n; i += 16) {
         const uint4 v = ld_after_wait(reinterpret_cast<const uint4*>(scales + i));
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -483,12 +492,13 @@ __device__ __forceinline__ void mma_f16_from_tmem(uint32_t d, uint32_t a, uint64
         : "memory");
 }
 
+template <bool MX>
+constexpr int kStepTiles = MX ? 1 : 2;  // tiles that share a stage at most
+
 // How a block's stages are laid out: for blocks of more than 128 tokens and up to 32 rows two tiles of 128 side by side, which share
 // the hidden states; otherwise one (of a 4-bit head they come one by one through tensor memory), of as many rows as there are tokens
 // (rounded up to 32) and so many more atoms of them. A product takes 128 rows all the same: what it reads behind the rows that are
 // there gives sums that nobody reads.
-template <bool MX>
-constexpr int kStepTiles = MX ? 1 : 2;  // most
 //
 // The products' sums in tensor memory are cut off towards zero at every addition (measured: -1e-9 of the score per element of the
 // row, 4e-6 for 4096, ten times what sums that are rounded come to), so that a row's k is cut in `cuts` pieces with sums of their own,
@@ -529,11 +539,8 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     __shared__ __align__(16) StepShared sh;
     const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
-    const uint32_t columns = 512;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStepStages; ++i) {
-            mbar_init(&sh.empty[i], MX ? 1 + 4 : 1);  // the products, and the warps that take weights apart
-        }
+        for (int i = 0; i < kStepStages; ++i) mbar_init(&sh.empty[i], MX ? 1 + 4 : 1);  // the products, and the warps that take weights apart
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.sums_full[i], 1);
             mbar_init(&sh.sums_empty[i], 4);
@@ -548,7 +555,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         prefetch_tensor_map(&map_w);
         prefetch_tensor_map(&map_box);
     }
-    if (warp == 2) tmem_alloc<1>(&sh.tmem, columns);
+    if (warp == 2) tmem_alloc<1>(&sh.tmem, 512);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (threadIdx.x < kStepRows) {
         const bool v = int(threadIdx.x) < a.B && step_row_part(a, threadIdx.x) >= 0;
@@ -623,8 +630,8 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 }
             }
         } else if (warp == 1) {
-            const uint32_t idesc = (MX ? kMmaF16Desc<128, 0, false, false> : kMmaBf16Desc<128, 0, false, false>) | uint32_t(a.N / 8) << 17, x_step = uint32_t(a.N) * kStepAtom >> 4;
-            const uint32_t w_step = uint32_t(l.rows) * kStepAtom >> 4;
+            const uint32_t idesc = (MX ? kMmaF16Desc<128, 0, false, false> : kMmaBf16Desc<128, 0, false, false>) | uint32_t(a.N / 8) << 17;
+            const uint32_t x_step = uint32_t(a.N) * kStepAtom >> 4, w_step = uint32_t(l.rows) * kStepAtom >> 4;
             for (int g = 0; g < groups && ok; ++g) {
                 const int it = groups_done + g, tiles = min(l.tiles, (n - g * per_group + 127) / 128);
                 if (!ring_wait(&sh.sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
@@ -862,7 +869,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    if (warp == 2) tmem_free<1>(tmem, columns);
+    if (warp == 2) tmem_free<1>(tmem, 512);
     if (int(threadIdx.x) < a.B) {
         Partial p = sh.state[0][threadIdx.x];
 #pragma unroll

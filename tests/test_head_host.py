@@ -25,6 +25,7 @@ BAD_HEADS = [
     (dict(H=0), cz.E_ARG),
     (dict(H=63), cz.E_ARG),                       # 8 to a vector
     (dict(H=65544, row_stride=65544), cz.E_RANGE),
+    (dict(V=(1 << 30) + 1), cz.E_RANGE),
     (dict(dtype=cz.F32), cz.E_ARG),
     (dict(dtype=7), cz.E_ARG),
     (dict(reserved=1), cz.E_ARG),
