@@ -220,10 +220,10 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
     if (m.part) {
         const size_t table = size_t(m.part->KW) * 128;
         if ((rc = ensure_smem(ctx, k_head_masks, table)) != CFGZIP_OK ||
-            (rc = launch(ctx, k_head_masks, pieces, dim3(256), table, st, a, *m.part, m.class_mask, m.class_stride, m.vocab_mask,
+            (rc = launch(ctx, k_head_masks, pieces, dim3(kUnionThreads), table, st, a, *m.part, m.class_mask, m.class_stride, m.vocab_mask,
                          m.vocab_stride)) != CFGZIP_OK)
             return rc;
-    } else if ((rc = launch(ctx, k_head_union, pieces, dim3(256), 0, st, a)) != CFGZIP_OK) {
+    } else if ((rc = launch(ctx, k_head_union, pieces, dim3(kUnionThreads), 0, st, a)) != CFGZIP_OK) {
         return rc;
     }
     if (a.logits) {

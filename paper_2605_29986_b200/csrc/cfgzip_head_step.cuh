@@ -17,7 +17,9 @@
 
 namespace cfgzip {
 
-constexpr int kUnionWords = 32;    // mask words (1024 tokens) counted together
+constexpr int kUnionWords = 32;    // mask words (1024 tokens) counted together, by a block
+constexpr int kUnionThreads = 512;
+constexpr int kUnionEach = kUnionWords / (kUnionThreads / 32);  // words a warp takes
 constexpr int kStepRows = 128;     // rows of the batch a launch takes at most
 constexpr int kStepRowsMx = 64;    // ... from a 4-bit head: the hidden states are brought past four times as many weights a byte
 constexpr int kStepShare = 2048;   // tokens a block lists at a time
@@ -73,11 +75,11 @@ __device__ __forceinline__ int step_row_part(const HeadStepArgs& a, int row) {
 // A row of hidden states as f16, times the power of two that brings its largest to [2^14, 2^15): all of a bf16 number's bits are
 // kept down to 2^-29 of the largest, and what is lost below that is 2^-40 of it at most, nothing to a sum in 32 bits.
 __device__ __forceinline__ void half_row(const HeadStepArgs& a, int row) {
-    __shared__ uint32_t most[8];
+    __shared__ uint32_t most[kUnionThreads / 32];
     const int vectors = a.H / 8, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint4* x = reinterpret_cast<const uint4*>(a.hidden + row * a.hidden_stride);
     uint32_t top = 0;
-    for (int i = threadIdx.x; i < vectors; i += 256) {
+    for (int i = threadIdx.x; i < vectors; i += kUnionThreads) {
         const uint4 v = ld_after_wait(x + i);
         top = __vmaxu2(__vmaxu2(top, __vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu)), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
     }
@@ -85,11 +87,11 @@ __device__ __forceinline__ void half_row(const HeadStepArgs& a, int row) {
     if (lane == 0) most[warp] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 8; ++w) top = max(top, most[w]);
+    for (int w = 0; w < kUnionThreads / 32; ++w) top = max(top, most[w]);
     const int e = min(max(int(top >> 7), 15), 254);  // exponent of the largest, + 127
     const float up = __uint_as_float(uint32_t(268 - e) << 23);  // 2^(14 - (e - 127))
     if (threadIdx.x == 0) a.back[row] = __uint_as_float(uint32_t(max(e - 14, 1)) << 23);
-    for (int i = threadIdx.x; i < a.half_stride / 8; i += 256) {
+    for (int i = threadIdx.x; i < a.half_stride / 8; i += kUnionThreads) {
         const uint4 v = i < vectors ? ld_after_wait(x + i) : make_uint4(0, 0, 0, 0);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
         uint32_t o[4];
@@ -103,16 +105,16 @@ __device__ __forceinline__ void half_row(const HeadStepArgs& a, int row) {
 }
 
 // What 32 words of tokens (kUnionWords) are worth to a batch, from each token's allowing rows: bits to a.bits, count, union; and with
-// `masks` the rows' vocab masks. A warp takes four words, a lane a token: allow(word, k) gives the bits, of word number 4 warp + k.
+// `masks` the rows' vocab masks. A warp takes kUnionEach words, a lane a token: allow(word, k) gives the bits.
 template <typename F>
 __device__ __forceinline__ void union_chunk(const HeadStepArgs& a, int c, uint32_t* sh, uint32_t* masks, int64_t mask_stride, F&& allow) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int at = blockIdx.x * kUnionWords + 4 * warp + k;
+    for (int k = 0; k < kUnionEach; ++k) {
+        const int at = blockIdx.x * kUnionWords + kUnionEach * warp + k;
         const uint32_t b = allow(at, k), any = __ballot_sync(0xFFFFFFFFu, b != 0);
         if (at < a.VW) a.bits[(int64_t(c) * a.VW + at) * 32 + lane] = b;
-        if (lane == 0 && any) sh[4 * warp + k] |= any;
+        if (lane == 0 && any) sh[kUnionEach * warp + k] |= any;
         if (masks) {
             const uint32_t w = warp_transpose32(b, lane);
             const int row = 32 * c + lane;
@@ -132,15 +134,15 @@ __device__ __forceinline__ void union_finish(const HeadStepArgs& a, const uint32
 
 // Rows of one partition: class masks turned to a table of 32 rows a class, a token's rows by one lookup. Vocab masks, union and turned
 // masks in one launch (expanding and turning by two took 3 to 5 us longer).
-__global__ void __launch_bounds__(256) k_head_masks(const HeadStepArgs a, const __grid_constant__ PartDev p, const uint32_t* class_mask,
+__global__ void __launch_bounds__(kUnionThreads) k_head_masks(const HeadStepArgs a, const __grid_constant__ PartDev p, const uint32_t* class_mask,
                                                     int64_t class_stride, uint32_t* masks, int64_t mask_stride) {
     extern __shared__ uint32_t table[];
     __shared__ uint32_t sh[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    uint32_t cls[4];
+    uint32_t cls[kUnionEach];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int at = blockIdx.x * kUnionWords + 4 * warp + k;
+    for (int k = 0; k < kUnionEach; ++k) {
+        const int at = blockIdx.x * kUnionWords + kUnionEach * warp + k;
         cls[k] = int(blockIdx.x) < a.n_counts && at < a.VW ? __ldg(p.c16 + int64_t(at) * 32 + lane) : uint32_t(p.K);  // (K: no class)
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -155,13 +157,14 @@ __global__ void __launch_bounds__(256) k_head_masks(const HeadStepArgs a, const 
         const int row = 32 * c + lane;
         const uint32_t* m = class_mask + row * class_stride;
         __syncthreads();
-        for (int k0 = warp; k0 < p.KW; k0 += 32) {
+        constexpr int kWarps = kUnionThreads / 32;
+        for (int k0 = warp; k0 < p.KW; k0 += 4 * kWarps) {
             uint32_t w[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = row < a.B && k0 + 8 * k < p.KW ? ld_after_wait(m + k0 + 8 * k) : 0u;
+            for (int k = 0; k < 4; ++k) w[k] = row < a.B && k0 + kWarps * k < p.KW ? ld_after_wait(m + k0 + kWarps * k) : 0u;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (k0 + 8 * k < p.KW) table[32 * (k0 + 8 * k) + lane] = warp_transpose32(w[k], lane);
+                if (k0 + kWarps * k < p.KW) table[32 * (k0 + kWarps * k) + lane] = warp_transpose32(w[k], lane);
         }
         __syncthreads();
         union_chunk(a, c, sh, masks, mask_stride, [&](int, int k) { return cls[k] < uint32_t(p.K) ? table[cls[k]] : 0u; });
@@ -170,8 +173,8 @@ __global__ void __launch_bounds__(256) k_head_masks(const HeadStepArgs a, const 
 }
 
 // Union of the rows' masks, 32 words by a block, and the masks turned from 32 tokens of a row to 32 rows of a token: a warp takes
-// four words, a lane a row. Blocks behind those take a row of hidden states.
-__global__ void __launch_bounds__(256) k_head_union(const HeadStepArgs a) {
+// kUnionEach words, a lane a row. Blocks behind those take a row of hidden states.
+__global__ void __launch_bounds__(kUnionThreads) k_head_union(const HeadStepArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -187,10 +190,10 @@ __global__ void __launch_bounds__(256) k_head_union(const HeadStepArgs a) {
         const int row = 32 * c + lane;
         const bool has = row < a.B && step_row_part(a, row) >= 0;
         const uint32_t* p = a.mask + int64_t(row) * a.mask_stride;
-        uint32_t w[4];
+        uint32_t w[kUnionEach];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int at = blockIdx.x * kUnionWords + 4 * warp + k;
+        for (int k = 0; k < kUnionEach; ++k) {
+            const int at = blockIdx.x * kUnionWords + kUnionEach * warp + k;
             w[k] = has && at < a.VW ? ld_after_wait(p + at) : 0u;
         }
         union_chunk(a, c, sh, nullptr, 0, [&](int, int k) { return warp_transpose32(w[k], lane); });
