@@ -195,7 +195,7 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
     const bool mx = head->dtype == CFGZIP_MXFP4;
     CUtensorMap map_x, map_w, map_box;
     int rc;
-    a.N = up(a.B, 32);
+    a.N = a.B <= 16 ? 16 : up(a.B, 32);
     a.weight = head->weight;
     a.row_bytes = head->row_stride * (mx ? 1 : 2);
     a.bytes = mx ? head->H / 2 : head->H * 2;

@@ -41,7 +41,7 @@ struct HeadStepArgs {
     int64_t row_bytes;
     const uint8_t* scales;
     int64_t scale_stride;
-    int32_t N;             // columns of a tile: B rounded up to 32
+    int32_t N;             // columns of a tile: B rounded up to 32, or 16
     int32_t row_atoms;     // atoms of a row of weights
     int32_t bytes;         // of a row of weights that count
     int32_t smem;          // shared memory for stages
@@ -204,8 +204,8 @@ __global__ void __launch_bounds__(kUnionThreads) k_head_union(const HeadStepArgs
 // A union of most of the vocabulary is taken for all of it, in boxes of rows by tiled copies. bf16 weights come one by one at the same
 // rate (one row of 128256 x 4096, 95 % allowed: 177 us, all of them 179); 4-bit ones take threads for it that otherwise turn weights
 // into f16 (32 rows of the same, 84 %: 107 us, all 96; 66 %: 87 and 95).
-__device__ __forceinline__ bool step_takes_all(const HeadStepArgs& a, uint32_t total) {
-    return int64_t(total) * 16 >= int64_t(a.V) * (a.half ? 12 : 15);
+__device__ __forceinline__ bool step_takes_all(const HeadStepArgs& a, uint32_t total, bool mx) {
+    return int64_t(total) * 16 >= int64_t(a.V) * (mx ? 12 : 15);
 }
 
 // -inf for every score; those of allowed tokens are written over it. (Where all tokens are taken, the step writes every score.)
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(256) k_head_fill(const HeadStepArgs a) {
     mine = __reduce_add_sync(0xFFFFFFFFu, mine);
     if ((threadIdx.x & 31) == 0) atomicAdd(&total, mine);
     __syncthreads();
-    if (step_takes_all(a, total)) return;
+    if (step_takes_all(a, total, a.half)) return;
     constexpr int ES = DT == kBF16 ? 2 : 4, PER = 16 / ES;
     const int row = blockIdx.y;
     if (step_row_part(a, row) < 0) return;
@@ -287,7 +287,7 @@ struct StepShared {
 
 // The block's share of the union: its n tokens to sh.list; the longest share of any block to *most, whether all tokens are taken
 // to *all. All threads; ends with a barrier.
-template <int THREADS>
+template <bool MX, int THREADS>
 __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh, int share, int shares, bool* all, int* most) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) sh.entries = 0;
@@ -310,7 +310,7 @@ __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh,
         if (w < warp) before += o;
         total += o;
     }
-    *all = step_takes_all(a, total);
+    *all = step_takes_all(a, total, MX);
     if (*all) total = a.V;
     // equal parts, the first `more` of them a token longer
     const uint32_t each = total / uint32_t(shares), more = total - each * uint32_t(shares);
@@ -386,6 +386,7 @@ __device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& s
         const int rows = min(32, a.B - 32 * c);
 #pragma unroll
         for (int h = 0; h < 32; h += 16) {
+            if (32 * c + h >= a.B) break;  // (of rows that are not there nothing is read below)
             uint32_t v[16];
             __syncwarp();
             tmem_ld16(tmem + 32 * c + h, v);
@@ -468,7 +469,7 @@ __device__ __forceinline__ uint32_t mx_scale_pair(uint32_t byte, uint32_t larges
 // Largest scale byte of a row of n blocks (rows start on 16 bytes).
 __device__ __forceinline__ uint32_t mx_largest(const uint8_t* scales, int n) {
     uint32_t top = 0;
-#pragma unroll 8
+#pragma unroll 4
     for (int i = 0; i < n; i += 16) {
         const uint4 v = ld_after_wait(reinterpret_cast<const uint4*>(scales + i));
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -514,10 +515,10 @@ template <bool MX>
 __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int most) {
     constexpr int X = MX ? 4 : 1;  // atoms of hidden states to an atom of weights
     StepLayout l;
-    l.tiles = most > 128 && a.N == 32 ? kStepTiles<MX> : 1;
+    l.tiles = most > 128 && a.N <= 32 ? kStepTiles<MX> : 1;
     l.rows = most > 128 ? 128 * l.tiles : (max(most, 1) + 31) & ~31;
     const int room = (MX ? 128 : 512) / (2 * l.tiles * a.N);
-    l.cut_atoms = room >= 8 ? (a.row_atoms + 7) >> 3 : room >= 4 ? (a.row_atoms + 3) >> 2 : room >= 2 ? (a.row_atoms + 1) >> 1 : a.row_atoms;
+    l.cut_atoms = room >= 16 ? (a.row_atoms + 15) >> 4 : room >= 8 ? (a.row_atoms + 7) >> 3 : room >= 4 ? (a.row_atoms + 3) >> 2 : room >= 2 ? (a.row_atoms + 1) >> 1 : a.row_atoms;
     l.cuts = (a.row_atoms + l.cut_atoms - 1) / l.cut_atoms;
     l.atoms = 1;
     int shift = 0;
@@ -580,7 +581,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         const int shares = a.rounds * gridDim.x;
         bool all;
         int most;
-        const int n = step_share<kThreads>(a, sh, round * gridDim.x + blockIdx.x, shares, &all, &most);
+        const int n = step_share<MX, kThreads>(a, sh, round * gridDim.x + blockIdx.x, shares, &all, &most);
         const StepLayout l = step_layout<MX>(a, most);  // (the same in every round, as is `all`)
         if (round == 0) {
             if (threadIdx.x == 0) {
