@@ -84,12 +84,27 @@ int up(int64_t n, int to) { return int((n + to - 1) / to * to); }
 int cuts(int64_t tiles, int k_blocks, int64_t result_elems) {
     int best = 1;
     double least = 0;
-    for (int s = 1; s <= 16 && s <= std::max(1, k_blocks / 16); ++s) {
+    for (int s = 1; s <= kPairs && s <= std::max(1, k_blocks / 16); ++s) {
         const double waves = double((tiles * s + kPairs - 1) / kPairs);
         const double us = waves * ((k_blocks + s - 1) / s) * 0.4 + s * double(result_elems) * 8e-6 / 6.5;
         if (s == 1 || us < least) {
             least = us;
             best = s;
+        }
+    }
+    return best;
+}
+
+// Columns of the tiles of scores: 256, or fewer where the last round of pairs would have few tiles (77 rows of 32000: 125 tiles of 256
+// take 74 pairs two rounds, and 143 of 224 as well). What a tile costs besides its columns is taken for 32 of them.
+int tile_width(int64_t rows, int64_t cols) {
+    int best = kMmaTile;
+    int64_t least = 0;
+    for (int w = kMmaTile; w >= 160; w -= 32) {
+        const int64_t tiles = ((rows + kMmaTile - 1) / kMmaTile) * ((cols + w - 1) / w), cost = (tiles + kPairs - 1) / kPairs * (w + 32);
+        if (w == kMmaTile || cost < least) {
+            least = cost;
+            best = w;
         }
     }
     return best;
@@ -107,13 +122,13 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
         s.counts = c.take<int32_t>(ceil_div(h->V, 32 * kUnionWords));
         s.ticket = c.take<uint32_t>(1);
         const bool tall = n > kStepRows && h->dtype == CFGZIP_BF16;
-        s.states = c.take<Partial>(std::max(std::min<int64_t>(n, kStepRows) * kStepBlocks, tall ? n * 2 * ceil_div(h->V, kMmaTile) : 0));
+        s.states = c.take<Partial>(std::max(std::min<int64_t>(n, kStepRows) * kStepBlocks, tall ? n * 2 * ceil_div(h->V, tile_width(n, h->V)) : 0));
         if (h->dtype == CFGZIP_MXFP4) {
             s.half = c.take<uint16_t>(std::min<int64_t>(n, kStepRowsMx) * up(h->H, 2 * int(kStepAtom)));
             s.back = c.take<float>(kStepRowsMx);
         }
     } else if (op == CFGZIP_HEAD_LOSS) {
-        s.part = c.take<float2>(n * ceil_div(h->V, kMmaTile) * 2);
+        s.part = c.take<float2>(n * ceil_div(h->V, tile_width(n, h->V)) * 2);
         s.of_target = c.take<float>(n);
     } else {
         const int64_t most = kPieceBytes / 2 / std::max<int64_t>(n, 1) / kMmaTile * kMmaTile;
@@ -155,19 +170,38 @@ int tensor_map_by_64(cfgzip_ctx* ctx, CUtensorMap* map, const uint16_t* p, int64
     return CFGZIP_OK;
 }
 
+// Results of a product that go out by tiled copies of 128 bytes of 32 rows.
+int tensor_map_out(cfgzip_ctx* ctx, CUtensorMap* map, const MmaArgs& a, bool bf16) {
+    const cuuint64_t es = bf16 ? 2 : 4;
+    const cuuint64_t dims[3] = {cuuint64_t(a.cols), cuuint64_t(a.rows), cuuint64_t(a.splits)};
+    const cuuint64_t strides[2] = {cuuint64_t(a.ld) * es, cuuint64_t(a.splits > 1 ? a.split_elems : a.ld) * es};
+    const cuuint32_t boxes[3] = {cuuint32_t(128 / es), 32, 1};
+    const cuuint32_t steps[3] = {1, 1, 1};
+    if (!ctx->encode_tiled ||
+        ctx->encode_tiled(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, a.out, dims, strides, boxes, steps,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return CFGZIP_E_CUDA;
+    return CFGZIP_OK;
+}
+
 template <bool A_MN, bool B_MN, int KIND>
 int run_mma(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUtensorMap& map_b, cudaStream_t st) {
+    constexpr bool kOut = KIND == kMmaSum || KIND == kMmaBf16;
+    if (kOut) a.width = kMmaTile;
     a.m_tiles = ceil_div(a.rows, kMmaTile);
-    a.n_tiles = ceil_div(a.cols, kMmaTile);
+    a.n_tiles = ceil_div(a.cols, a.width);
     a.splits = std::max(1, a.splits);
     a.status = ctx->d_status;
     auto kern = k_head_mma<A_MN, B_MN, KIND>;
-    const int rc = ensure_smem(ctx, kern, kMmaSmem);
-    if (rc != CFGZIP_OK) return rc;
+    const size_t smem = kMmaSmem + (kOut ? 8 * kMmaOut : 0);
+    CUtensorMap map_out = map_a;
+    int rc = kOut ? tensor_map_out(ctx, &map_out, a, KIND == kMmaBf16) : CFGZIP_OK;
+    if (rc != CFGZIP_OK || (rc = ensure_smem(ctx, kern, smem)) != CFGZIP_OK) return rc;
     const int64_t tiles = int64_t(a.m_tiles) * a.n_tiles * a.splits;
     if (tiles >= (int64_t(1) << 30)) return CFGZIP_E_RANGE;
     const unsigned pairs = unsigned(std::min<int64_t>(tiles, ctx->sm_count / 2));
-    return launch(ctx, kern, dim3(2 * pairs), dim3(kMmaThreads), kMmaSmem, st, a, map_a, map_b);
+    return launch(ctx, kern, dim3(2 * pairs), dim3(kMmaThreads), smem, st, a, map_a, map_b, map_out);
 }
 
 // Threads of a launch that takes a head by vectors of 8 weights (mx_at).
@@ -328,9 +362,10 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
     if (tall) {
         CUtensorMap map_x, map_w;
         if ((rc = tensor_map(ctx, &map_x, hidden, B, head->H, hidden_stride, 128)) != CFGZIP_OK ||
-            (rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, 128)) != CFGZIP_OK)
+            (rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, tile_width(B, head->V) / 2)) != CFGZIP_OK)
             return rc;
         MmaArgs a{};
+        a.width = tile_width(B, head->V);
         a.rows = B;
         a.cols = a.V = head->V;
         a.k_blocks = ceil_div(head->H, kMmaK);
@@ -406,9 +441,10 @@ int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidde
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     CUtensorMap map_x, map_w;
     if ((rc = tensor_map(ctx, &map_x, hidden, N, head->H, hidden_stride, 128)) != CFGZIP_OK ||
-        (rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, 128)) != CFGZIP_OK)
+        (rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, tile_width(N, head->V) / 2)) != CFGZIP_OK)
         return rc;
     MmaArgs a{};
+    a.width = tile_width(N, head->V);
     a.rows = N;
     a.cols = a.V = head->V;
     a.k_blocks = ceil_div(head->H, kMmaK);
@@ -475,12 +511,14 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
         const int32_t n = std::min(w.piece, head->V - t0);
         const uint16_t* weights = static_cast<const uint16_t*>(head->weight) + t0 * head->row_stride;
         // (columns of the piece behind the vocabulary are outside the maps: they come as zeros)
-        if ((rc = tensor_map(ctx, &w_k, weights, n, H, head->row_stride, 128)) != CFGZIP_OK ||
+        const int width = tile_width(N, n);
+        if ((rc = tensor_map(ctx, &w_k, weights, n, H, head->row_stride, width / 2)) != CFGZIP_OK ||
             (rc = tensor_map(ctx, &w_mn, weights, n, H, head->row_stride, 64)) != CFGZIP_OK ||
             (rc = tensor_map(ctx, &g_k, w.g, N, n, w.piece, 128)) != CFGZIP_OK ||
             (rc = tensor_map(ctx, &g_mn, w.g, N, n, w.piece, 64)) != CFGZIP_OK)
             return rc;
         MmaArgs a{};
+        a.width = width;
         a.rows = N;
         a.cols = n;
         a.k_blocks = ceil_div(H, kMmaK);

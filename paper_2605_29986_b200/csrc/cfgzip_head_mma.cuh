@@ -28,11 +28,13 @@ constexpr int kMmaK = 64;          // k of a stage
 constexpr int kMmaPortion = 8;
 constexpr uint32_t kMmaHalf = 128 * kMmaK * 2;           // bytes of one operand of a stage in one block
 constexpr size_t kMmaSmem = size_t(kMmaStages) * 2 * kMmaHalf + 1024;
+constexpr uint32_t kMmaOut = 32 * 128;                   // bytes a warp has on their way out: 32 rows of 128
 
 enum : int { kMmaLoss = 0, kMmaGrad = 1, kMmaSum = 2, kMmaBf16 = 3, kMmaStep = 4 };
 
 struct MmaArgs {
     int32_t rows, cols;        // of the result (tokens x piece of the vocabulary, ...)
+    int32_t width;             // columns of a tile
     int32_t m_tiles, n_tiles;
     int32_t k_blocks, splits;  // the k range is cut in `splits`, each with a result of its own
     int32_t m_fast;            // neighbouring tiles go along m
@@ -73,10 +75,10 @@ __device__ __forceinline__ MmaTile mma_tile(const MmaArgs& a, int i) {
     return t;
 }
 
-// What a row allows of the 32 W tokens from column n0 of the piece on, 32 to a word.
+// What a row allows of the tile's tokens from column n0 of the piece on, up to 32 W, 32 to a word.
 template <int W>
-__device__ __forceinline__ void tile_mask(const MmaArgs& a, int row, int n0, uint32_t (&bits)[W]) {
-    const int t = a.t0 + n0, left = min(a.cols - n0, kMmaTile);
+__device__ __forceinline__ void tile_mask(const MmaArgs& a, const MmaTile& tile, int row, int n0, uint32_t (&bits)[W]) {
+    const int t = a.t0 + n0, left = min(a.cols, (tile.n + 1) * a.width) - n0;
     const uint32_t* p = a.mask + (a.mask ? int64_t(row) * a.mask_stride + (t >> 5) : 0);
 #pragma unroll
     for (int c = 0; c < W; ++c) {
@@ -87,12 +89,13 @@ __device__ __forceinline__ void tile_mask(const MmaArgs& a, int row, int n0, uin
     }
 }
 
-// Largest allowed score and the sum of exponentials, of one row and half a tile's tokens.
+// Largest allowed score and the sum of exponentials, of one row and half a tile's tokens (the first 128 of them, the rest).
 __device__ __forceinline__ void loss_epilogue(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, float (&z)[128],
                                               const uint32_t (&bits)[4]) {
-    const int n0 = t.n * kMmaTile + 128 * half;
-    const int asked = valid ? ld_after_wait(a.targets + row) : -1, target = asked < 0 ? -1 : asked - (a.t0 + n0);
-    if (__any_sync(0xFFFFFFFFu, uint32_t(target) < 128u)) {
+    const int n0 = t.n * a.width + 128 * half, mine = min(128, a.width - 128 * half);
+    const int asked = valid ? ld_after_wait(a.targets + row) : -1, there = asked < 0 ? -1 : asked - (a.t0 + n0);
+    const int target = there < mine ? there : -1;
+    if (__any_sync(0xFFFFFFFFu, target >= 0)) {
 #pragma unroll
         for (int j = 0; j < 128; ++j)
             if (target == j) a.of_target[row] = z[j];
@@ -131,13 +134,13 @@ __device__ __forceinline__ void step_epilogue(const MmaArgs& a, const MmaTile& t
     if (valid)
         *reinterpret_cast<int4*>(&a.states[int64_t(2 * t.n + half) * a.rows + row]) =
             make_int4(__float_as_int(m), __float_as_int((s[0] + s[1]) + (s[2] + s[3])),
-                      at == kNoPos ? kNoPos : a.t0 + t.n * kMmaTile + 128 * half + at, 0);
+                      at == kNoPos ? kNoPos : a.t0 + t.n * a.width + 128 * half + at, 0);
 }
 
 // g = d (exp(z - lse) - [target]) of the allowed tokens, as bf16.
 __device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t, int row, uint32_t tmem, bool valid,
                                               const uint32_t (&bits)[8]) {
-    const int n0 = t.n * kMmaTile;
+    const int n0 = t.n * a.width;
     int target = -1;
     float d = 0.f, lse = 0.f;
     bool has = false;
@@ -150,7 +153,8 @@ __device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t
         target = has ? target - (a.t0 + n0) : -1;
     }
 #pragma unroll 1
-    for (int c = 0; c < 8; ++c) {
+    for (int c = 0; 32 * c < a.width; ++c) {
+        if (n0 + 32 * c >= a.ld) break;
         uint32_t v[32];
         __syncwarp();
         tmem_ld32(tmem + 32 * c, v);
@@ -182,59 +186,85 @@ __device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t
     }
 }
 
+__device__ __forceinline__ void tma_store3(const void* tensor_map, int x, int y, int z, uint32_t src_smem) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];\n\tcp.async.bulk.commit_group;" ::"l"(tensor_map),
+                 "r"(x), "r"(y), "r"(z), "r"(src_smem)
+                 : "memory");
+}
+
 // Sums as they are (f32), or rounded to bf16; added to what is there where asked for. Rows start on 16 bytes, columns come in
-// multiples of 8.
+// multiples of 8. A warp's 32 rows go out 128 bytes at a time by a tiled copy from shared memory, which leaves out what is behind the
+// last row or column: sums of few stages wait for nothing but their stores, and stored by lanes, a row each, they took twice as
+// long (gradient of 50021 x 1024 for 100 tokens: 50 us).
 template <bool BF16>
-__device__ __forceinline__ void out_epilogue(const MmaArgs& a, const MmaTile& t, int row, uint32_t tmem, bool valid) {
-    const int n0 = t.n * kMmaTile;
-    const int64_t at = t.split * a.split_elems + int64_t(row) * a.ld + n0;
+__device__ __forceinline__ void out_epilogue(const MmaArgs& a, const CUtensorMap& map, const MmaTile& t, int first, int lane, uint32_t tmem,
+                                             uint32_t buffer) {
+    constexpr int kCols = BF16 ? 64 : 32;
+    if (first >= a.rows) return;
+    const int row = first + lane;
+    const bool add = a.add && row < a.rows;
 #pragma unroll 1
-    for (int c = 0; c < 8; ++c) {
-        if (n0 + 32 * c >= a.cols) break;
-        uint32_t v[32];
-        __syncwarp();
-        tmem_ld32(tmem + 32 * c, v);
-        tmem_wait_ld();
-        if (!valid) continue;
+    for (int c = 0; c < kMmaTile / kCols; ++c) {
+        const int n = t.n * kMmaTile + kCols * c;
+        if (n >= a.cols) break;
+        const int64_t at = t.split * a.split_elems + int64_t(row) * a.ld + n;
+        uint32_t o[32];
+        if (BF16) {
 #pragma unroll
-        for (int j = 0; j < 32; j += 8) {
-            if (n0 + 32 * c + j >= a.cols) break;
-            if (BF16) {
-                uint4* p = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at + 32 * c + j);
-                if (a.add) {
-                    const uint4 b = *p;
+            for (int h = 0; h < 2; ++h) {
+                uint32_t v[32];
+                __syncwarp();
+                tmem_ld32(tmem + kCols * c + 32 * h, v);
+                tmem_wait_ld();
+                if (add) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        if (n + 32 * h + j >= a.cols) break;
+                        const uint4 b = ld_after_wait(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.out) + at + 32 * h + j));
+                        const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            v[j + k] = __float_as_uint(__uint_as_float(v[j + k]) + __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16));
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[16 * h + j] = bf16_pair(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+            }
+        } else {
+            __syncwarp();
+            tmem_ld32(tmem + kCols * c, o);
+            tmem_wait_ld();
+            if (add) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    if (n + j >= a.cols) break;
+                    const uint4 b = ld_after_wait(reinterpret_cast<const uint4*>(static_cast<const float*>(a.out) + at + j));
                     const uint32_t w[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        v[j + k] = __float_as_uint(__uint_as_float(v[j + k]) +
-                                                   __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16));
-                }
-                *p = make_uint4(bf16_pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])),
-                                bf16_pair(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])),
-                                bf16_pair(__uint_as_float(v[j + 4]), __uint_as_float(v[j + 5])),
-                                bf16_pair(__uint_as_float(v[j + 6]), __uint_as_float(v[j + 7])));
-            } else {
-                float4* p = reinterpret_cast<float4*>(static_cast<float*>(a.out) + at + 32 * c + j);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    float4 o = make_float4(__uint_as_float(v[j + 4 * k]), __uint_as_float(v[j + 4 * k + 1]),
-                                           __uint_as_float(v[j + 4 * k + 2]), __uint_as_float(v[j + 4 * k + 3]));
-                    if (a.add) {
-                        const float4 b = p[k];
-                        o = make_float4(o.x + b.x, o.y + b.y, o.z + b.z, o.w + b.w);
-                    }
-                    p[k] = o;
+                    for (int k = 0; k < 4; ++k) o[j + k] = __float_as_uint(__uint_as_float(o[j + k]) + __uint_as_float(w[k]));
                 }
             }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (the copy before has read the buffer)
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffer + uint32_t(lane) * 128 + (uint32_t(j ^ (lane & 7)) << 4)),
+                         "r"(o[4 * j]), "r"(o[4 * j + 1]), "r"(o[4 * j + 2]), "r"(o[4 * j + 3])
+                         : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) tma_store3(&map, n, first, t.split, buffer);
     }
 }
 
-// D[rows, cols] = A B^T in tiles of 256 x 256 by pairs of blocks (each holds 128 rows of A and of B, and the sums of its 128
-// rows), persistent. Operands K-major (k contiguous) or MN-major, from tensor maps with boxes of 64 x 128 or 64 x 64.
+// D[rows, cols] = A B^T in tiles of 256 x width by pairs of blocks (each holds 128 rows of A and half of B's, and the sums of its 128
+// rows), persistent. Operands K-major (k contiguous) or MN-major, from tensor maps with boxes of 64 x 128 (x width / 2) or 64 x 64;
+// an MN-major B and results that go out by tiled copies have a width of 256.
 template <bool A_MN, bool B_MN, int KIND>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
-    k_head_mma(const __grid_constant__ MmaArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
+    k_head_mma(const __grid_constant__ MmaArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ CUtensorMap map_out) {
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kMmaStages], empty[kMmaStages], sums_full[2], sums_empty[2];
     __shared__ uint32_t s_tmem;
@@ -269,13 +299,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             Ring r;
             for (int i = pair; i < tiles && ok; i += pairs) {
                 const MmaTile t = mma_tile(a, i);
-                const int m = t.m * kMmaTile + int(rank) * 128, n = t.n * kMmaTile + int(rank) * 128;
+                const int m = t.m * kMmaTile + int(rank) * 128, n = t.n * a.width + int(rank) * (a.width / 2);
                 for (int k = t.k0; k < t.k1; ++k) {
                     if (!ring_wait<true>(&empty[r.stage], r.phase ^ 1)) {
                         ok = false;
                         break;
                     }
-                    if (rank == 0) mbar_expect_tx(&full[r.stage], 4 * kMmaHalf);
+                    if (rank == 0) mbar_expect_tx(&full[r.stage], 2 * kMmaHalf + uint32_t(a.width) * kMmaK * 2);
                     const uint32_t bar = peer_shared(&full[r.stage], 0), at = stages + uint32_t(r.stage) * 2 * kMmaHalf;
                     if (A_MN) {
                         tma_load_pair(at, &map_a, m, k * kMmaK, bar);
@@ -295,7 +325,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
         }
     } else if (warp == 1) {
         if (rank == 0) {
-            constexpr uint32_t idesc = kMmaBf16Desc<256, 256, A_MN, B_MN>;
+            const uint32_t idesc = kMmaBf16Desc<256, 0, A_MN, B_MN> | uint32_t(a.width / 8) << 17;
             Ring r;
             int it = 0;
             for (int i = pair; i < tiles && ok; i += pairs) {
@@ -340,7 +370,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             const int row = t.m * kMmaTile + int(rank) * 128 + quad * 32 + lane;
             const bool valid = row < a.rows;
             uint32_t bits[4];
-            tile_mask(a, valid ? row : a.rows - 1, t.n * kMmaTile + 128 * half, bits);
+            tile_mask(a, t, valid ? row : a.rows - 1, t.n * a.width + 128 * half, bits);
             float sums[128] = {};
             for (int k = t.k0; k < t.k1; k += kMmaPortion, ++it) {
                 if (!ring_wait<true>(&sums_full[it & 1], (it >> 1) & 1)) {
@@ -374,7 +404,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             const int row = t.m * kMmaTile + int(rank) * 128 + quad * 32 + lane;
             const bool valid = row < a.rows;
             uint32_t bits[8];
-            if (KIND == kMmaGrad) tile_mask(a, valid ? row : a.rows - 1, t.n * kMmaTile, bits);
+            if (KIND == kMmaGrad) tile_mask(a, t, valid ? row : a.rows - 1, t.n * a.width, bits);
             if (!ring_wait<true>(&sums_full[set], (it >> 1) & 1)) {
                 ok = false;
                 break;
@@ -382,12 +412,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             tmem_fence_after();
             const uint32_t d = tmem + set * 256 + (uint32_t(quad * 32) << 16);
             if (KIND == kMmaGrad) grad_epilogue(a, t, row, d, valid, bits);
-            if (KIND == kMmaSum) out_epilogue<false>(a, t, row, d, valid);
-            if (KIND == kMmaBf16) out_epilogue<true>(a, t, row, d, valid);
+            if (KIND == kMmaSum || KIND == kMmaBf16)
+                out_epilogue<KIND == kMmaBf16>(a, map_out, t, row - lane, lane, d, stages + kMmaStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
             tmem_fence_before();
             __syncwarp();
             if (lane == 0) arrive_at_peer(empty_bar);
         }
+        if (KIND != kMmaGrad && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     if (!ok && lane == 0) atomicExch(a.status + 3, 1);
     __syncwarp();
@@ -463,6 +494,7 @@ __global__ void __launch_bounds__(256) k_head_round(const float* from, int64_t s
     const int64_t total = int64_t(rows) * vectors;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
         float f[8] = {};
+#pragma unroll 4
         for (int s = 0; s < splits; ++s) {
             const float4* p = reinterpret_cast<const float4*>(from + s * split_elems + 8 * i);
             const float4 x = __ldcg(p), y = __ldcg(p + 1);
