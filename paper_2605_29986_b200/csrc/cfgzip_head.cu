@@ -560,7 +560,7 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
     }
     if (!d_hidden) return CFGZIP_OK;
     const int splits = std::min(w.splits, ceil_div(std::min(w.piece, head->V), kMmaK));
-    const int64_t blocks = std::min<int64_t>(ceil_div(int64_t(N) * (H / 8), 256), int64_t(ctx->sm_count) * 8);
+    const int64_t blocks = std::min<int64_t>(ceil_div(int64_t(N) * (H / 4), 256), int64_t(ctx->sm_count) * 8);
     return launch(ctx, k_head_round, dim3(unsigned(blocks)), dim3(256), 0, st, (const float*)w.sums, int64_t(N) * H, splits,
                   static_cast<uint16_t*>(d_hidden), d_hidden_stride, int(N), H);
 }

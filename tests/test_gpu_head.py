@@ -82,6 +82,9 @@ STEPS = [
     (40000, 520, 64, 300, 0.01, "bf16", 0),
     (20011, 320, 129, 300, 0.2, "bf16", 8),
     (9001, 64, 300, 130, 0.3, "bf16", 0),
+    (14001, 64, 200, 130, 0.3, "bf16", 0),
+    (16001, 72, 150, 130, 0.3, "bf16", 8),
+    (18901, 64, 256, 130, 0.3, "bf16", 0),
     (1, 16, 5, 1, 0.9, "bf16", 0),
     (100, 32, 1, 3, 0.5, "mxfp4", 0),
     (129, 64, 3, 9, 0.5, "mxfp4", 8),
@@ -385,6 +388,10 @@ LOSSES = [
     (12000, 320, 300, None, 0),
     (33001, 64, 513, 0.5, 0),
     (700, 1032, 260, 0.02, 8),
+    # vocabularies that take tiles of 192, 224 and 256 columns (the others: 160)
+    (14001, 64, 130, 0.3, 0),
+    (16001, 64, 256, None, 8),
+    (18901, 136, 40, 0.5, 8),
 ]
 
 
