@@ -4,11 +4,12 @@
 // (128 tokens x up to 128 rows), k in stages of shared memory; the scores of a tile go from tensor memory into the rows' running
 // maximum, sum and choice. The last block to finish puts the blocks' together.
 //
-// 32 rows of 128256 x 4096 (bf16, 97 % allowed by some row): 1.05 GB in 181 us with the masks, 5.8 TB/s; inside the loop the copies run
-// at the memory's rate, and 25 us go to the masks, the list, the first loads and the last scores. From 4 bits: 279 MB in 92 us; tiled
-// copies of 128-byte pieces of 128 rows bring 5.2 TB/s at most (measured alone), the rest is the same 25 us and the threads that turn
-// weights into f16, which take 1000 cycles for 128 tokens x 256 weights where the copies take 850. One row of 32000 x 2048: 23 us, of
-// which the loads need 6; what is left is latency (masks 4, list 3, first loads 2, scores and results 4, launches).
+// 32 rows of 128256 x 4096 (bf16, 97 % allowed by some row): 1.05 GB in 178 to 182 us with the masks, 5.8 TB/s; inside the loop the
+// copies run at the memory's rate, and 25 us go to the masks, the list, the first loads and the last scores. From 4 bits: 279 MB in 86
+// to 93 us, one row of 151936 x 2560 in 62. Boxes of 128-byte pieces of 128 rows come at 5.1 to 5.7 TB/s (measured alone), 850 cycles
+// for 128 tokens x 256 weights, turning those into f16 takes 550 (the loop alone); from 17 rows on the hidden states, which every block
+// brings past again for each tile, are as many bytes as the weights (16 rows: 77 us, 32: 86, 64: 118). One row of 32000 x 2048: 20 us,
+// of which the loads need 6; what is left is latency (masks 4, list 3, first loads 2, scores and results 4, launches).
 #pragma once
 
 #include <cuda.h>
