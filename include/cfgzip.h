@@ -265,8 +265,8 @@ int cfgzip_map_tokens(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_
  *   CFGZIP_MXFP4 : two weights to a byte, the one with the lower index in the lower half, row_stride in bytes; each is e2m1
  *                  (sign bit, then 0, 0.5, 1, 1.5, 2, 3, 4, 6) times 2^(scale - 127) with one scale byte per 32 weights of a
  *                  row in `scales`, scale_stride bytes from row to row. H a multiple of 32. A scale of 255 is not taken (NaN).
- * Rows of weights, scales, hidden states and gradients start on 16 bytes (CFGZIP_E_ALIGN otherwise); H at most 65536, V at
- * most 2^30 (CFGZIP_E_RANGE).
+ * Rows of weights, scales, hidden states and gradients start on 16 bytes (CFGZIP_E_ALIGN otherwise); H at most 65536, V and
+ * the rows of a batch at most 2^30 (CFGZIP_E_RANGE).
  * Hidden states are bf16. They may be any values whose products stay finite; +inf and NaN scores are outside the contract.
  */
 typedef struct cfgzip_head {
@@ -338,7 +338,8 @@ int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidde
  * whose loss is not a finite function of z (a negative target, one that is not allowed, nothing allowed):
  *   d_hidden[n, :] = sum_t g[n, t] * weight[t, :],    d_weight[t, :] = sum_n g[n, t] * hidden[n, :]
  * The scores are computed again; g is rounded to bf16 (by 2^-8 of itself at most) for the two products, which accumulate in 32
- * bits; a gradient in 32 bits has that in it too.
+ * bits; a gradient in 32 bits has that in it too. Where g is 0 it is multiplied all the same: weights of masked tokens and hidden
+ * states of rows without a loss have to be finite here (what they are otherwise makes no difference).
  *   hidden .. targets : as given to cfgzip_head_loss, and lse as it returned it (required)
  *   d_loss     : dev float [N]
  *   d_hidden   : nullable dev bf16 [N, d_hidden_stride] (written)

@@ -15,7 +15,7 @@ using namespace cfgzip;
 namespace {
 
 constexpr int kHeadMost = 65536;      // longest row of a head
-constexpr int kHeadTokens = 1 << 30;  // most rows
+constexpr int kHeadTokens = 1 << 30;  // most rows of a head, and of a batch
 
 bool on16(const void* p, int64_t stride_bytes) { return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(stride_bytes)) & 15u) == 0; }
 
@@ -80,11 +80,13 @@ struct HeadSpace {
 int up(int64_t n, int to) { return int((n + to - 1) / to * to); }
 
 // Cuts of a sum over k_blocks stages whose result has `tiles` tiles: more cuts fill the last wave of pairs better, and each is
-// one more f32 result written and read. A stage takes a pair about 0.4 us, a result's bytes 1 / 6.5 us per MB.
+// one more f32 result written and read. A stage takes a pair about 0.4 us, a result's bytes 1 / 6.5 us per MB. At most kCutTiles
+// tiles in all where there are cuts.
+constexpr int kCutTiles = 8 * kPairs;
 int cuts(int64_t tiles, int k_blocks, int64_t result_elems) {
     int best = 1;
     double least = 0;
-    for (int s = 1; s <= kPairs && s <= std::max(1, k_blocks / 16); ++s) {
+    for (int s = 1; s <= kPairs && s <= std::max(1, k_blocks / 16) && (s == 1 || s * tiles <= kCutTiles); ++s) {
         const double waves = double((tiles * s + kPairs - 1) / kPairs);
         const double us = waves * ((k_blocks + s - 1) / s) * 0.4 + s * double(result_elems) * 8e-6 / 6.5;
         if (s == 1 || us < least) {
@@ -96,12 +98,16 @@ int cuts(int64_t tiles, int k_blocks, int64_t result_elems) {
 }
 
 // Columns of the tiles of scores: 256, or fewer where the last round of pairs would have few tiles (77 rows of 32000: 125 tiles of 256
-// take 74 pairs two rounds, and 143 of 224 as well). What a tile costs besides its columns is taken for 32 of them.
+// take 74 pairs two rounds, and 143 of 224 as well). What a tile costs besides its columns is taken for 32 of them. From 16 rounds on
+// there is nothing to gain.
+constexpr int kNarrowest = 160, kNarrowTiles = 16 * kPairs;
 int tile_width(int64_t rows, int64_t cols) {
+    const int64_t high = (rows + kMmaTile - 1) / kMmaTile;
+    if (high * ((cols + kMmaTile - 1) / kMmaTile) > kNarrowTiles) return kMmaTile;
     int best = kMmaTile;
     int64_t least = 0;
-    for (int w = kMmaTile; w >= 160; w -= 32) {
-        const int64_t tiles = ((rows + kMmaTile - 1) / kMmaTile) * ((cols + w - 1) / w), cost = (tiles + kPairs - 1) / kPairs * (w + 32);
+    for (int w = kMmaTile; w >= kNarrowest; w -= 32) {
+        const int64_t tiles = high * ((cols + w - 1) / w), cost = (tiles + kPairs - 1) / kPairs * (w + 32);
         if (w == kMmaTile || cost < least) {
             least = cost;
             best = w;
@@ -110,6 +116,13 @@ int tile_width(int64_t rows, int64_t cols) {
     return best;
 }
 
+// The most states, one for each half tile of a row's scores, that any batch of up to `rows` rows comes to.
+int64_t most_states(int64_t rows, int64_t cols) {
+    const int64_t wide = (cols + kMmaTile - 1) / kMmaTile, narrow = (cols + kNarrowest - 1) / kNarrowest;
+    return 2 * std::max(rows * wide, std::min<int64_t>(rows, kMmaTile * (kNarrowTiles / wide)) * narrow);
+}
+
+// What is taken for `rows` rows is enough for fewer, whose tiles, pieces and cuts are others.
 HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace) {
     const uintptr_t skip = (256 - reinterpret_cast<uintptr_t>(workspace) % 256) % 256;
     Carve c(workspace ? static_cast<char*>(workspace) + skip : nullptr);
@@ -122,21 +135,21 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
         s.counts = c.take<int32_t>(ceil_div(h->V, 32 * kUnionWords));
         s.ticket = c.take<uint32_t>(1);
         const bool tall = n > kStepRows && h->dtype == CFGZIP_BF16;
-        s.states = c.take<Partial>(std::max(std::min<int64_t>(n, kStepRows) * kStepBlocks, tall ? n * 2 * ceil_div(h->V, tile_width(n, h->V)) : 0));
+        s.states = c.take<Partial>(std::max(std::min<int64_t>(n, kStepRows) * kStepBlocks, tall ? most_states(n, h->V) : 0));
         if (h->dtype == CFGZIP_MXFP4) {
             s.half = c.take<uint16_t>(std::min<int64_t>(n, kStepRowsMx) * up(h->H, 2 * int(kStepAtom)));
             s.back = c.take<float>(kStepRowsMx);
         }
     } else if (op == CFGZIP_HEAD_LOSS) {
-        s.part = c.take<float2>(n * ceil_div(h->V, tile_width(n, h->V)) * 2);
+        s.part = c.take<float2>(most_states(n, h->V));
         s.of_target = c.take<float>(n);
     } else {
-        const int64_t most = kPieceBytes / 2 / std::max<int64_t>(n, 1) / kMmaTile * kMmaTile;
-        s.piece = int32_t(std::min<int64_t>(up(h->V, kMmaTile), std::max<int64_t>(most, kMmaTile)));
-        const int64_t tiles = int64_t(ceil_div(n, kMmaTile)) * ceil_div(h->H, kMmaTile);
-        s.splits = cuts(tiles, s.piece / kMmaK, n * h->H);
-        s.g = c.take<uint16_t>(n * s.piece);
-        s.sums = c.take<float>(n * h->H * s.splits);
+        const int64_t all = up(h->V, kMmaTile), room = kPieceBytes / 2, across = ceil_div(h->H, kMmaTile);
+        s.piece = int32_t(std::min(all, std::max<int64_t>(room / std::max<int64_t>(n, 1) / kMmaTile * kMmaTile, kMmaTile)));
+        s.splits = cuts(ceil_div(n, kMmaTile) * across, s.piece / kMmaK, n * h->H);
+        const int64_t most_cuts = std::max<int64_t>(1, std::min({int64_t(kPairs), kCutTiles / across, all / kMmaK / 16}));
+        s.g = c.take<uint16_t>(std::max(std::min(n * all, room), n * kMmaTile));
+        s.sums = c.take<float>(std::max(n * h->H, std::min<int64_t>(n * h->H * most_cuts, int64_t(kCutTiles) * kMmaTile * kMmaTile)));
     }
     s.bytes = c.used + 256;
     return s;
@@ -284,6 +297,7 @@ int cfgzip_head_workspace(const cfgzip_head* head, int op, int32_t rows, int64_t
     const int rc = check_head_shape(head);
     if (rc != CFGZIP_OK) return rc;
     if (op != CFGZIP_HEAD_STEP && head->dtype != CFGZIP_BF16) return CFGZIP_E_ARG;
+    if (rows > kHeadTokens) return CFGZIP_E_RANGE;
     *bytes = head_space(head, op, rows, nullptr).bytes;
     return CFGZIP_OK;
 }
@@ -327,6 +341,7 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
     int rc = check_head(head);
     if (rc != CFGZIP_OK) return rc;
     if (B < 0) return CFGZIP_E_ARG;
+    if (B > kHeadTokens) return CFGZIP_E_RANGE;
     HeadSpace w{};
     if (B > 0) {
         if (!argmax || !class_mask || class_stride_words <= 0 || (vocab_mask && vocab_stride_words < ceil_div(head->V, 32))) return CFGZIP_E_ARG;
@@ -429,6 +444,7 @@ int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidde
     int rc = check_head(head);
     if (rc != CFGZIP_OK) return rc;
     if (head->dtype != CFGZIP_BF16 || N < 0) return CFGZIP_E_ARG;
+    if (N > kHeadTokens) return CFGZIP_E_RANGE;
     if (N == 0) return ctx ? CFGZIP_OK : CFGZIP_E_ARG;
     if (!targets || !loss || (vocab_mask && vocab_stride_words < ceil_div(head->V, 32))) return CFGZIP_E_ARG;
     if ((rc = check_rows(head, hidden, hidden_stride)) != CFGZIP_OK) return rc;
@@ -477,6 +493,7 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
     int rc = check_head(head);
     if (rc != CFGZIP_OK) return rc;
     if (head->dtype != CFGZIP_BF16 || N < 0 || (!d_hidden && !d_weight)) return CFGZIP_E_ARG;
+    if (N > kHeadTokens) return CFGZIP_E_RANGE;
     if (d_weight) {
         if ((d_weight_dtype != CFGZIP_F32 && d_weight_dtype != CFGZIP_BF16) || d_weight_stride < head->H) return CFGZIP_E_ARG;
         if (!on16(d_weight, d_weight_stride * (d_weight_dtype == CFGZIP_BF16 ? 2 : 4))) return CFGZIP_E_ALIGN;

@@ -87,6 +87,7 @@ def test_arguments_of_the_step():
                    dict(hidden_stride=56), dict(vocab_mask=GOOD, vocab_stride_words=3), dict(logits=GOOD, logits_stride=99),
                    dict(logits=GOOD, logits_stride=100, logits_dtype=2)):
         assert step(h, **change) == cz.E_ARG, change
+    assert step(h, B=(1 << 30) + 1) == cz.E_RANGE
     for change in (dict(hidden=GOOD + 2), dict(hidden_stride=68)):
         assert step(h, **change) == cz.E_ALIGN, change
     for h in (head(), head(dtype=cz.MXFP4)):
@@ -102,6 +103,7 @@ def test_arguments_of_the_loss_and_its_gradient():
                    dict(vocab_mask=GOOD, vocab_stride_words=3)):
         assert loss(h, **change) == cz.E_ARG and backward(h, **change) == cz.E_ARG, change
     assert loss(h, loss=None) == cz.E_ARG
+    assert loss(h, N=(1 << 30) + 1) == cz.E_RANGE and backward(h, N=(1 << 30) + 1) == cz.E_RANGE
     for change in (dict(lse=None), dict(d_loss=None), dict(d_hidden=None, d_weight=None), dict(d_hidden_stride=56), dict(d_weight_stride=56),
                    dict(d_weight_dtype=2)):
         assert backward(h, **change) == cz.E_ARG, change
@@ -139,6 +141,14 @@ def test_workspaces():
     assert status(cz.cfgzip_head_workspace, head(H=63), cz.HEAD_STEP, 1) == cz.E_ARG
     assert status(cz.cfgzip_head_workspace, head(dtype=cz.MXFP4), cz.HEAD_LOSS, 1) == cz.E_ARG
     assert cz.load_library().cfgzip_head_workspace(ctypes.byref(h), 0, 1, None) == cz.E_ARG
+    # enough for `rows` rows is enough for fewer, however those are cut
+    for V, H in ((1, 8), (300, 64), (18901, 256), (50021, 1024), (128256, 4096), (1 << 20, 65536)):
+        for dtype in (cz.BF16, cz.MXFP4)[:1 if H % 32 else 2]:
+            h = head(V=V, H=H, dtype=dtype)
+            for op in (cz.HEAD_STEP, cz.HEAD_LOSS, cz.HEAD_LOSS_BACKWARD)[:1 if dtype == cz.MXFP4 else 3]:
+                sizes = [cz.cfgzip_head_workspace(h, op, n) for n in list(range(1, 6000)) + list(range(6000, 1 << 20, 50021))]
+                assert all(a <= b for a, b in zip(sizes, sizes[1:])), (V, H, dtype, op)
+    assert status(cz.cfgzip_head_workspace, head(), cz.HEAD_STEP, (1 << 30) + 1) == cz.E_RANGE
     # the loss keeps no logits, and the gradient no more than a piece of them, however many tokens there are
     assert cz.cfgzip_head_workspace(head(V=128256, H=4096), cz.HEAD_LOSS, 8192) < 128256 * 8192 // 8
     big = cz.cfgzip_head_workspace(head(V=128256, H=4096), cz.HEAD_LOSS_BACKWARD, 65536)
