@@ -348,18 +348,15 @@ __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh,
 __device__ __forceinline__ void step_finish_row(const HeadStepArgs& a, int row, int blocks, int lane) {
     const int part = step_row_part(a, row);
     if (part < 0) return;
-    float top = -INFINITY;
-    for (int i = lane; i < blocks; i += 32) top = fmaxf(top, __ldcg(&a.part[int64_t(i) * a.B + row].m));
-    top = redux_max(top);
-    const float ref = fmaxf(top, kRefFloor);
-    float s = 0.f;
-    int pos = kNoPos;
+    Partial p = partial_empty();
+#pragma unroll 4
     for (int i = lane; i < blocks; i += 32) {
         const int4 v = __ldcg(reinterpret_cast<const int4*>(&a.part[int64_t(i) * a.B + row]));
-        const float m = __int_as_float(v.x);
-        s += __int_as_float(v.y) * ex2f((fmaxf(m, kRefFloor) - ref) * kLog2e);
-        if (m == top) pos = min(pos, v.z);
+        partial_merge(p.m, p.s, p.pos, __int_as_float(v.x), __int_as_float(v.y), v.z);
     }
+    const float top = redux_max(p.m), ref = fmaxf(top, kRefFloor);
+    float s = p.s * ex2f((fmaxf(p.m, kRefFloor) - ref) * kLog2e);
+    int pos = p.m == top ? p.pos : kNoPos;
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
     pos = __reduce_min_sync(0xFFFFFFFFu, pos);
