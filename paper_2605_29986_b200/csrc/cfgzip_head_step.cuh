@@ -349,10 +349,14 @@ __device__ __forceinline__ void step_finish_row(const HeadStepArgs& a, int row, 
     const int part = step_row_part(a, row);
     if (part < 0) return;
     Partial p = partial_empty();
-#pragma unroll 4
-    for (int i = lane; i < blocks; i += 32) {
-        const int4 v = __ldcg(reinterpret_cast<const int4*>(&a.part[int64_t(i) * a.B + row]));
-        partial_merge(p.m, p.s, p.pos, __int_as_float(v.x), __int_as_float(v.y), v.z);
+    for (int i = lane; i < blocks; i += 160) {  // (five at a time: what 148 blocks have, in one go)
+        int4 v[5];
+#pragma unroll
+        for (int k = 0; k < 5; ++k)
+            v[k] = i + 32 * k < blocks ? __ldcg(reinterpret_cast<const int4*>(&a.part[int64_t(i + 32 * k) * a.B + row]))
+                                       : make_int4(__float_as_int(-INFINITY), 0, kNoPos, 0);
+#pragma unroll
+        for (int k = 0; k < 5; ++k) partial_merge(p.m, p.s, p.pos, __int_as_float(v[k].x), __int_as_float(v[k].y), v[k].z);
     }
     const float top = redux_max(p.m), ref = fmaxf(top, kRefFloor);
     float s = p.s * ex2f((fmaxf(p.m, kRefFloor) - ref) * kLog2e);
