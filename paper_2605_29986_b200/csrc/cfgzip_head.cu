@@ -483,7 +483,7 @@ int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidde
     f.loss = loss;
     f.lse = lse;
     f.status = ctx->d_status;
-    return launch(ctx, k_head_loss_finish, dim3(unsigned(ceil_div(N, 8))), dim3(256), 0, st, f);
+    return launch(ctx, k_head_loss_finish, dim3(unsigned(ceil_div(N, kFinishRows))), dim3(256), 0, st, f);
 }
 
 int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N,

@@ -429,7 +429,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     if (warp == 2) tmem_free<2>(tmem, 512);
 }
 
-// Partial states of a row's tiles to its results: eight rows by a block, a thread takes every 32nd tile of one.
+// Partial states of a row's tiles to its results: four rows by a block, a thread takes every 64th tile of one, five at a time.
+constexpr int kFinishRows = 4;
 struct FinishArgs {
     const float2* part;
     const float* of_target;
@@ -442,36 +443,45 @@ struct FinishArgs {
 };
 __global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 8 + (lane & 7);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * kFinishRows + (lane & 3);
     float m = -INFINITY, s = 0.f;
     if (row < a.rows)
-#pragma unroll 4
-        for (int t = warp * 4 + (lane >> 3); t < a.tiles; t += 32) {
-            const float2 p = __ldcg(a.part + int64_t(t) * a.rows + row);
-            const float next = fmaxf(m, p.x), ref = fmaxf(next, kRefFloor);
-            s = s * ex2f((fmaxf(m, kRefFloor) - ref) * kLog2e) + p.y * ex2f((fmaxf(p.x, kRefFloor) - ref) * kLog2e);
+        for (int t = warp * 8 + (lane >> 2); t < a.tiles; t += 320) {
+            float2 p[5];
+#pragma unroll
+            for (int k = 0; k < 5; ++k)
+                p[k] = t + 64 * k < a.tiles ? __ldcg(a.part + int64_t(t + 64 * k) * a.rows + row) : make_float2(-INFINITY, 0.f);
+            float next = m;
+#pragma unroll
+            for (int k = 0; k < 5; ++k) next = fmaxf(next, p[k].x);
+            const float ref = fmaxf(next, kRefFloor);
+            s *= ex2f((fmaxf(m, kRefFloor) - ref) * kLog2e);
+#pragma unroll
+            for (int k = 0; k < 5; ++k) s += p[k].y * ex2f((fmaxf(p[k].x, kRefFloor) - ref) * kLog2e);
             m = next;
         }
-    __shared__ float2 sh[32][8];
-    sh[warp * 4 + (lane >> 3)][lane & 7] = make_float2(m, s);
+    __shared__ float2 sh[64][kFinishRows];
+    sh[warp * 8 + (lane >> 2)][lane & 3] = make_float2(m, s);
     __syncthreads();
     if (warp) return;
-    // four threads a row, eight states each
+    // eight threads a row, eight states each
     float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[8 * (lane >> 3) + w][lane & 7].x);
+    for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[8 * (lane >> 2) + w][lane & 3].x);
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
     const float ref = fmaxf(top, kRefFloor);
     s = 0.f;
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
-        const float2 p = sh[8 * (lane >> 3) + w][lane & 7];
+        const float2 p = sh[8 * (lane >> 2) + w][lane & 3];
         s += p.y * ex2f((fmaxf(p.x, kRefFloor) - ref) * kLog2e);
     }
+    s += __shfl_xor_sync(0xFFFFFFFFu, s, 4);
     s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);
     s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
-    if (lane >= 8 || row >= a.rows) return;
+    if (lane >= kFinishRows || row >= a.rows) return;
     const float log_sum = logf(s);
     if (a.lse) a.lse[row] = s > 0.f ? top + log_sum : -INFINITY;
     const int t = ld_after_wait(a.targets + row);
