@@ -445,6 +445,10 @@ __global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * kFinishRows + (lane & 3);
     float m = -INFINITY, s = 0.f;
+    // (what the end needs is asked for before the states: the target's score is there or is not looked at)
+    const bool ends = warp == 0 && lane < kFinishRows && row < a.rows;
+    const int target = ends ? ld_after_wait(a.targets + row) : -1;
+    const float of_target = ends ? ld_after_wait(a.of_target + row) : 0.f;
     if (row < a.rows)
         for (int t = warp * 8 + (lane >> 2); t < a.tiles; t += 320) {
             float2 p[5];
@@ -460,6 +464,8 @@ __global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
             for (int k = 0; k < 5; ++k) s += p[k].y * ex2f((fmaxf(p[k].x, kRefFloor) - ref) * kLog2e);
             m = next;
         }
+    bool has = target >= 0 && target < a.V;
+    if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (target >> 5)) >> (target & 31)) & 1u;
     __shared__ float2 sh[64][kFinishRows];
     sh[warp * 8 + (lane >> 2)][lane & 3] = make_float2(m, s);
     __syncthreads();
@@ -481,18 +487,12 @@ __global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
     s += __shfl_xor_sync(0xFFFFFFFFu, s, 4);
     s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);
     s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
-    if (lane >= kFinishRows || row >= a.rows) return;
+    if (!ends) return;
     const float log_sum = logf(s);
     if (a.lse) a.lse[row] = s > 0.f ? top + log_sum : -INFINITY;
-    const int t = ld_after_wait(a.targets + row);
+    if (target >= a.V) atomicAdd(a.status + 1, 1);
     float loss = 0.f;
-    if (t >= a.V) atomicAdd(a.status + 1, 1);
-    if (t >= 0) {
-        bool has = t < a.V;
-        if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (t >> 5)) >> (t & 31)) & 1u;
-        const float z = has ? ld_after_wait(a.of_target + row) : -INFINITY;
-        loss = z > -INFINITY ? (top - z) + log_sum : INFINITY;
-    }
+    if (target >= 0) loss = has && of_target > -INFINITY ? (top - of_target) + log_sum : INFINITY;
     a.loss[row] = loss;
 }
 
