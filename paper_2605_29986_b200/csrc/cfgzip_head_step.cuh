@@ -348,6 +348,7 @@ __device__ __forceinline__ int step_share(const HeadStepArgs& a, StepShared& sh,
 __device__ __forceinline__ void step_finish_row(const HeadStepArgs& a, int row, int blocks, int lane) {
     const int part = step_row_part(a, row);
     if (part < 0) return;
+    const int32_t* reps = a.parts[part].trep;  // (asked for before the states)
     Partial p = partial_empty();
     for (int i = lane; i < blocks; i += 160) {  // (five at a time: what 148 blocks have, in one go)
         int4 v[5];
@@ -368,7 +369,7 @@ __device__ __forceinline__ void step_finish_row(const HeadStepArgs& a, int row, 
     const bool any = pos != kNoPos;
     const float log_sum = logf(s);
     a.argmax[row] = any ? pos : -1;
-    if (a.rep) a.rep[row] = any ? a.parts[part].trep[pos] : -1;
+    if (a.rep) a.rep[row] = any ? reps[pos] : -1;
     if (a.logp) a.logp[row] = s > 0.f ? -log_sum : -INFINITY;
     if (a.lse) a.lse[row] = s > 0.f ? top + log_sum : -INFINITY;
     if (!any) atomicAdd(a.status, 1);
