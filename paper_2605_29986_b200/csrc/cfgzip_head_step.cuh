@@ -4,12 +4,12 @@
 // (128 tokens x up to 128 rows), k in stages of shared memory; the scores of a tile go from tensor memory into the rows' running
 // maximum, sum and choice. The last block to finish puts the blocks' together.
 //
-// 32 rows of 128256 x 4096 (bf16, 97 % allowed by some row): 1.05 GB in 178 to 182 us with the masks, 5.8 TB/s; inside the loop the
-// copies run at the memory's rate, and 25 us go to the masks, the list, the first loads and the last scores. From 4 bits: 279 MB in 86
-// to 93 us, one row of 151936 x 2560 in 62. Boxes of 128-byte pieces of 128 rows come at 5.1 to 5.7 TB/s (measured alone), 850 cycles
-// for 128 tokens x 256 weights, turning those into f16 takes 550 (the loop alone); from 17 rows on the hidden states, which every block
-// brings past again for each tile, are as many bytes as the weights (16 rows: 77 us, 32: 86, 64: 118). One row of 32000 x 2048: 20 us,
-// of which the loads need 6; what is left is latency (masks 4, list 3, first loads 2, scores and results 4, launches).
+// 32 rows of 128256 x 4096 (bf16, 97 % allowed by some row): 1.05 GB in 173 to 179 us with the masks, 5.9 TB/s; inside the loop the
+// copies run at the memory's rate, and some 20 us go to the masks, the list, the first loads and the last scores. From 4 bits: 279 MB
+// in 81 to 92 us, one row of 151936 x 2560 in 63. Boxes of 128-byte pieces of 128 rows come at 5.1 to 5.7 TB/s (measured alone), 850
+// cycles for 128 tokens x 256 weights, turning those into f16 takes 550 (the loop alone); from 17 rows on the hidden states, which
+// every block brings past again for each tile, are as many bytes as the weights (16 rows: 75 us, 32: 82, 64: 111). One row of 32000 x
+// 2048: 20 us, of which the loads need 6; what is left is latency (masks 4, list 3, first loads 2, scores and results 3, launches).
 #pragma once
 
 #include <cuda.h>
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kUnionThreads) k_head_union(const HeadStepArgs
 
 // A union of most of the vocabulary is taken for all of it, in boxes of rows by tiled copies. bf16 weights come one by one at the same
 // rate (one row of 128256 x 4096, 95 % allowed: 177 us, all of them 179); 4-bit ones take threads for it that otherwise turn weights
-// into f16 (32 rows of the same, 84 %: 107 us, all 96; 66 %: 87 and 95).
+// into f16 (32 rows of the same, 70 %: 79 us, all 83; 58 %: 69 and 83; at 84 % one by one took 10 us longer than all).
 __device__ __forceinline__ bool step_takes_all(const HeadStepArgs& a, uint32_t total, bool mx) {
     return int64_t(total) * 16 >= int64_t(a.V) * (mx ? 12 : 15);
 }
