@@ -337,8 +337,10 @@ int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidde
  * Its gradient. With g[n, t] = d_loss[n] * (exp(z[n, t] - lse[n]) - [t = targets[n]]) over the allowed tokens, and 0 in rows
  * whose loss is not a finite function of z (a negative target, one that is not allowed, nothing allowed):
  *   d_hidden[n, :] = sum_t g[n, t] * weight[t, :],    d_weight[t, :] = sum_n g[n, t] * hidden[n, :]
- * The scores are computed again; g is rounded to bf16 (by 2^-8 of itself at most) for the two products, which accumulate in 32
- * bits; a gradient in 32 bits has that in it too. Where g is 0 it is multiplied all the same: weights of masked tokens and hidden
+ * The scores are computed again, the same to the last bit as in the loss: the only token of a row has g = 0. exp(z - lse) is as
+ * exact as the scores; the difference on the target, of which little is left where the model is sure of it, has in it what lse was
+ * rounded by (some 2^-24 |lse| of d_loss) and is rounded by nothing else. g is then rounded to bf16 (by 2^-8 of itself at most)
+ * for the two products, which accumulate in 32 bits; a gradient in 32 bits has that in it too. Where g is 0 it is multiplied all the same: weights of masked tokens and hidden
  * states of rows without a loss have to be finite here (what they are otherwise makes no difference).
  *   hidden .. targets : as given to cfgzip_head_loss, and lse as it returned it (required)
  *   d_loss     : dev float [N]

@@ -23,8 +23,9 @@ constexpr int kMmaThreads = 384;   // a warp for the copies, one for the product
 constexpr int kMmaStages = 6;
 constexpr int kMmaTile = 256;      // rows and columns of a pair's tile
 constexpr int kMmaK = 64;          // k of a stage
-// Stages whose sums are left in tensor memory, where every addition is cut off towards zero (-1e-9 of a sum per element of k); the
-// loss, whose scores go out in 32 bits, adds the portions up in registers, rounded. The gradient's are rounded to bf16 in any case.
+// Stages whose sums are left in tensor memory, where every addition is cut off towards zero (-1e-9 of a sum per element of k); scores
+// add the portions up in registers, rounded. Those of the gradient too: what counts of them are differences to an lse that was made of
+// the loss's (a gradient of 4096 tokens takes 4 % longer for it: 9.7 -> 10.1 ms).
 constexpr int kMmaPortion = 8;
 constexpr uint32_t kMmaHalf = 128 * kMmaK * 2;           // bytes of one operand of a stage in one block
 constexpr size_t kMmaSmem = size_t(kMmaStages) * 2 * kMmaHalf + 1024;
@@ -137,10 +138,12 @@ __device__ __forceinline__ void step_epilogue(const MmaArgs& a, const MmaTile& t
                       at == kNoPos ? kNoPos : a.t0 + t.n * a.width + 128 * half + at, 0);
 }
 
-// g = d (exp(z - lse) - [target]) of the allowed tokens, as bf16.
-__device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t, int row, uint32_t tmem, bool valid,
-                                              const uint32_t (&bits)[8]) {
-    const int n0 = t.n * a.width;
+// g = d (exp(z - lse) - [target]) of the allowed tokens, as bf16, of one row and half a tile's tokens. A target that the model is sure of
+// has all of its g in the small difference exp(z - lse) - 1: the scores are made as the loss makes them, portion by portion, so that z
+// here is the z in lse to the last bit, and the difference is not taken of a rounded exponential. The only token of a row gets 0.
+__device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, const float (&z)[128],
+                                              const uint32_t (&bits)[4]) {
+    const int n0 = t.n * a.width + 128 * half, mine = min(128, a.width - 128 * half);
     int target = -1;
     float d = 0.f, lse = 0.f;
     bool has = false;
@@ -151,38 +154,29 @@ __device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t
         if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (target >> 5)) >> (target & 31)) & 1u;
         if (has) d = ld_after_wait(a.d_loss + row);
         target = has ? target - (a.t0 + n0) : -1;
+        if (target >= mine) target = -1;
     }
-#pragma unroll 1
-    for (int c = 0; 32 * c < a.width; ++c) {
-        if (n0 + 32 * c >= a.ld) break;
-        uint32_t v[32];
-        __syncwarp();
-        tmem_ld32(tmem + 32 * c, v);
-        tmem_wait_ld();
-        uint32_t w = 0;
+    float of_target = 0.f;
+    if (__any_sync(0xFFFFFFFFu, target >= 0)) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w = k == c ? bits[k] : w;
-        if (!has) w = 0;
+        for (int j = 0; j < 128; ++j) of_target = target == j ? z[j] : of_target;
+        of_target = d * expm1f(of_target - lse);
+    }
+    uint16_t* p = static_cast<uint16_t*>(a.out) + int64_t(row) * a.ld + n0;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const float p = ex2f((__uint_as_float(v[j]) - lse) * kLog2e);
-            v[j] = __float_as_uint((w >> j) & 1u ? d * p : 0.f);
+    for (int c = 0; c < 8; ++c) {
+        if (16 * c >= mine || n0 + 16 * c >= a.ld) break;
+        const uint32_t w = has ? bits[c / 2] >> (16 * (c & 1)) : 0u;
+        float g[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            g[j] = (w >> j) & 1u ? d * ex2f((z[16 * c + j] - lse) * kLog2e) : 0.f;
+            g[j] = target == 16 * c + j ? of_target : g[j];
         }
-        if (__any_sync(0xFFFFFFFFu, (target >> 5) == c)) {
+        uint32_t o[8];
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (has && target == 32 * c + j) v[j] = __float_as_uint(__uint_as_float(v[j]) - d);
-        }
-        if (valid) {
-            uint16_t* p = static_cast<uint16_t*>(a.out) + int64_t(row) * a.ld + n0 + 32 * c;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t o[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = bf16_pair(__uint_as_float(v[16 * h + 2 * j]), __uint_as_float(v[16 * h + 2 * j + 1]));
-                st_global32(p + 16 * h, o);
-            }
-        }
+        for (int j = 0; j < 8; ++j) o[j] = bf16_pair(g[2 * j], g[2 * j + 1]);
+        if (valid) st_global32(p + 16 * c, o);
     }
 }
 
@@ -268,7 +262,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kMmaStages], empty[kMmaStages], sums_full[2], sums_empty[2];
     __shared__ uint32_t s_tmem;
-    constexpr bool kPortion = KIND == kMmaLoss || KIND == kMmaStep;
+    constexpr bool kPortion = KIND == kMmaLoss || KIND == kMmaStep || KIND == kMmaGrad;
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -393,6 +387,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             }
             if (ok && KIND == kMmaLoss) loss_epilogue(a, t, half, row, valid, sums, bits);
             if (ok && KIND == kMmaStep) step_epilogue(a, t, half, row, valid, sums, bits);
+            if (ok && KIND == kMmaGrad) grad_epilogue(a, t, half, row, valid, sums, bits);
         }
     } else if (warp >= 4) {
         const int set = (warp - 4) >> 2, quad = warp & 3;
@@ -402,23 +397,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             if ((it & 1) != set) continue;
             const MmaTile t = mma_tile(a, i);
             const int row = t.m * kMmaTile + int(rank) * 128 + quad * 32 + lane;
-            const bool valid = row < a.rows;
-            uint32_t bits[8];
-            if (KIND == kMmaGrad) tile_mask(a, t, valid ? row : a.rows - 1, t.n * a.width, bits);
             if (!ring_wait<true>(&sums_full[set], (it >> 1) & 1)) {
                 ok = false;
                 break;
             }
             tmem_fence_after();
             const uint32_t d = tmem + set * 256 + (uint32_t(quad * 32) << 16);
-            if (KIND == kMmaGrad) grad_epilogue(a, t, row, d, valid, bits);
             if (KIND == kMmaSum || KIND == kMmaBf16)
                 out_epilogue<KIND == kMmaBf16>(a, map_out, t, row - lane, lane, d, stages + kMmaStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
             tmem_fence_before();
             __syncwarp();
             if (lane == 0) arrive_at_peer(empty_bar);
         }
-        if (KIND != kMmaGrad && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     if (!ok && lane == 0) atomicExch(a.status + 3, 1);
     __syncwarp();
