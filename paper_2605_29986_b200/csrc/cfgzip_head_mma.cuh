@@ -27,6 +27,9 @@ constexpr int kMmaK = 64;          // k of a stage
 // add the portions up in registers, rounded. Those of the gradient too: what counts of them are differences to an lse that was made of
 // the loss's (a gradient of 4096 tokens takes 4 % longer for it: 9.7 -> 10.1 ms).
 constexpr int kMmaPortion = 8;
+// ... and the sums over tokens of the gradient, which may be over a whole text or vocabulary (in one go 65536 tokens lose 3e-4 of a sum of
+// positive terms, 200003 lose 1.3e-3; in portions of 2048 under 8e-6. 1000 tokens of 50021 x 1024: 318 -> 329 us).
+constexpr int kMmaOutPortion = 32;
 constexpr uint32_t kMmaHalf = 128 * kMmaK * 2;           // bytes of one operand of a stage in one block
 constexpr size_t kMmaSmem = size_t(kMmaStages) * 2 * kMmaHalf + 1024;
 constexpr uint32_t kMmaOut = 32 * 128;                   // bytes a warp has on their way out: 32 rows of 128
@@ -191,54 +194,32 @@ __device__ __forceinline__ void tma_store3(const void* tensor_map, int x, int y,
 // last row or column: sums of few stages wait for nothing but their stores, and stored by lanes, a row each, they took twice as
 // long (gradient of 50021 x 1024 for 100 tokens: 50 us).
 template <bool BF16>
-__device__ __forceinline__ void out_epilogue(const MmaArgs& a, const CUtensorMap& map, const MmaTile& t, int first, int lane, uint32_t tmem,
-                                             uint32_t buffer) {
+__device__ __forceinline__ void out_epilogue(const MmaArgs& a, const CUtensorMap& map, const MmaTile& t, int half, int first, int lane,
+                                             float (&sums)[128], uint32_t buffer) {
     constexpr int kCols = BF16 ? 64 : 32;
     if (first >= a.rows) return;
     const int row = first + lane;
     const bool add = a.add && row < a.rows;
-#pragma unroll 1
-    for (int c = 0; c < kMmaTile / kCols; ++c) {
-        const int n = t.n * kMmaTile + kCols * c;
+#pragma unroll
+    for (int c = 0; c < 128 / kCols; ++c) {
+        const int n = t.n * kMmaTile + 128 * half + kCols * c;
         if (n >= a.cols) break;
-        const int64_t at = t.split * a.split_elems + int64_t(row) * a.ld + n;
+        float* f = sums + kCols * c;
         uint32_t o[32];
-        if (BF16) {
+        if (add) {
+            const char* from = static_cast<const char*>(a.out) + (t.split * a.split_elems + int64_t(row) * a.ld + n) * (BF16 ? 2 : 4);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t v[32];
-                __syncwarp();
-                tmem_ld32(tmem + kCols * c + 32 * h, v);
-                tmem_wait_ld();
-                if (add) {
+            for (int j = 0; j < 8; ++j) {
+                if (n + j * kCols / 8 >= a.cols) break;
+                const uint4 b = ld_after_wait(reinterpret_cast<const uint4*>(from + 16 * j));
+                const uint32_t w[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
-                        if (n + 32 * h + j >= a.cols) break;
-                        const uint4 b = ld_after_wait(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.out) + at + 32 * h + j));
-                        const uint32_t w[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            v[j + k] = __float_as_uint(__uint_as_float(v[j + k]) + __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16));
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[16 * h + j] = bf16_pair(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
-            }
-        } else {
-            __syncwarp();
-            tmem_ld32(tmem + kCols * c, o);
-            tmem_wait_ld();
-            if (add) {
-#pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                    if (n + j >= a.cols) break;
-                    const uint4 b = ld_after_wait(reinterpret_cast<const uint4*>(static_cast<const float*>(a.out) + at + j));
-                    const uint32_t w[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) o[j + k] = __float_as_uint(__uint_as_float(o[j + k]) + __uint_as_float(w[k]));
-                }
+                for (int k = 0; k < kCols / 8; ++k)
+                    f[j * kCols / 8 + k] += __uint_as_float(BF16 ? (k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16) : w[k & 3]);
             }
         }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) o[j] = BF16 ? bf16_pair(f[2 * j % kCols], f[(2 * j + 1) % kCols]) : __float_as_uint(f[j % kCols]);
         if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (the copy before has read the buffer)
         __syncwarp();
 #pragma unroll
@@ -262,7 +243,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kMmaStages], empty[kMmaStages], sums_full[2], sums_empty[2];
     __shared__ uint32_t s_tmem;
-    constexpr bool kPortion = KIND == kMmaLoss || KIND == kMmaStep || KIND == kMmaGrad;
+    constexpr bool kOut = KIND == kMmaSum || KIND == kMmaBf16;
+    constexpr int kPortion = kOut ? kMmaOutPortion : kMmaPortion;
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -274,7 +256,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sums_full[i], 1);
-            mbar_init(&sums_empty[i], kPortion ? 16 : 8);  // four warps of either block (all eight)
+            mbar_init(&sums_empty[i], 16);  // eight warps of either block
         }
         mbar_init_fence();
         prefetch_tensor_map(&map_a);
@@ -326,7 +308,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                 const MmaTile t = mma_tile(a, i);
                 for (int k = t.k0; k < t.k1 && ok; ++it) {
                     const uint32_t d = tmem + (it & 1) * 256;
-                    const int first = k, last = kPortion ? min(k + kMmaPortion, t.k1) : t.k1;
+                    const int first = k, last = min(k + kPortion, t.k1);
                     if (!ring_wait<true>(&sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
                         ok = false;
                         break;
@@ -354,7 +336,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                 }
             }
         }
-    } else if (warp >= 4 && kPortion) {
+    } else if (warp >= 4) {
         // Both sets read every portion, a half of the columns each, and keep the sums in registers.
         const int half = (warp - 4) >> 2, quad = warp & 3;
         const uint32_t empty_bar[2] = {peer_shared(&sums_empty[0], 0), peer_shared(&sums_empty[1], 0)};
@@ -364,9 +346,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             const int row = t.m * kMmaTile + int(rank) * 128 + quad * 32 + lane;
             const bool valid = row < a.rows;
             uint32_t bits[4];
-            tile_mask(a, t, valid ? row : a.rows - 1, t.n * a.width + 128 * half, bits);
+            if (!kOut) tile_mask(a, t, valid ? row : a.rows - 1, t.n * a.width + 128 * half, bits);
             float sums[128] = {};
-            for (int k = t.k0; k < t.k1; k += kMmaPortion, ++it) {
+            for (int k = t.k0; k < t.k1; k += kPortion, ++it) {
                 if (!ring_wait<true>(&sums_full[it & 1], (it >> 1) & 1)) {
                     ok = false;
                     break;
@@ -388,28 +370,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             if (ok && KIND == kMmaLoss) loss_epilogue(a, t, half, row, valid, sums, bits);
             if (ok && KIND == kMmaStep) step_epilogue(a, t, half, row, valid, sums, bits);
             if (ok && KIND == kMmaGrad) grad_epilogue(a, t, half, row, valid, sums, bits);
+            if (ok && kOut)
+                out_epilogue<KIND == kMmaBf16>(a, map_out, t, half, row - lane, lane, sums,
+                                               stages + kMmaStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
         }
-    } else if (warp >= 4) {
-        const int set = (warp - 4) >> 2, quad = warp & 3;
-        const uint32_t empty_bar = peer_shared(&sums_empty[set], 0);
-        int it = 0;
-        for (int i = pair; i < tiles; i += pairs, ++it) {
-            if ((it & 1) != set) continue;
-            const MmaTile t = mma_tile(a, i);
-            const int row = t.m * kMmaTile + int(rank) * 128 + quad * 32 + lane;
-            if (!ring_wait<true>(&sums_full[set], (it >> 1) & 1)) {
-                ok = false;
-                break;
-            }
-            tmem_fence_after();
-            const uint32_t d = tmem + set * 256 + (uint32_t(quad * 32) << 16);
-            if (KIND == kMmaSum || KIND == kMmaBf16)
-                out_epilogue<KIND == kMmaBf16>(a, map_out, t, row - lane, lane, d, stages + kMmaStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
-            tmem_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_at_peer(empty_bar);
-        }
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (kOut && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     if (!ok && lane == 0) atomicExch(a.status + 3, 1);
     __syncwarp();

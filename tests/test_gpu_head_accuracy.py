@@ -69,3 +69,33 @@ def test_gradient_of_sure_targets(V, H, N):
     tol[rows, t] = want[rows, t].abs() * 2.0 ** -8 + d[:, 0] * (want_lse[:, 0].abs() * 2.0 ** -24 + 64 * 2.0 ** -24 + others * 2.0 ** -13)
     off = (got - want).abs()
     assert (off <= tol)[~alone].all(), (off / tol.clamp(min=1e-30))[~alone].max().item()
+
+
+# ---- sums over many tokens ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("N", [2048, 16000, 65536, 200003])
+def test_weight_gradient_summed_over_many_tokens(N):
+    V, H = 64, 72
+    g = torch.Generator(device="cuda")
+    g.manual_seed(N)
+    weight = torch.zeros((V, H), dtype=torch.bfloat16, device="cuda")  # all scores 0: p = 1 / V, a power of two
+    x = torch.rand((N, H), generator=g, device="cuda").to(torch.bfloat16)
+    d_loss = (torch.rand(N, generator=g, device="cuda") + 0.5).to(torch.bfloat16).float()
+    targets = torch.zeros(N, dtype=torch.int32, device="cuda")
+    lse = torch.full((N,), float(np.log(V)), device="cuda")
+    d_weight = torch.full((V, H), 3.0, device="cuda")
+    head = cz.cfgzip_head(weight, cz.BF16, V, H)
+    with Ctx([]) as ctx:
+        ws = workspace(head, cz.HEAD_LOSS_BACKWARD, N)
+        for accumulate in (0, 1):
+            cz.cfgzip_head_loss_backward(ctx.h, head, x, H, N, None, 0, targets, lse, d_loss, None, 0, d_weight, cz.F32, H, accumulate,
+                                         ws, ws.numel(), torch.cuda.current_stream())
+            torch.cuda.synchronize()
+            # g = d / V, rounded to bf16, is d / V: an exponential 2^-21 off is far from the next bf16 number
+            want = (1 + accumulate) * (d_loss.double() @ x.double()) / V
+            # 128 additions to tensor memory of 16 products each at a time, each cut off by less than 2^-23 of a sum that grows evenly, so
+            # half of that of the last on average; then a rounding for every such portion, and two at the end
+            tol = 64 * 2.0 ** -23 + (N / 2048 + 2) * 2.0 ** -24
+            off = ((d_weight.double() - want) / want)[1:]
+            assert off.abs().max() <= tol, off.abs().max().item()
+            # the row of the targets: g = d (1 / V - 1), 63 / 64 of d, which bf16 holds to 2^-8
+            assert ((d_weight[0].double() / want + V - 1).abs() <= (V - 1) * (2.0 ** -8 + tol)).all()
