@@ -375,13 +375,66 @@ __device__ __forceinline__ void step_finish_row(const HeadStepArgs& a, int row, 
     if (!any) atomicAdd(a.status, 1);
 }
 
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+
+// Where the sums of a warp's 32 tokens are: `cuts` pieces in tensor memory, cut_step columns apart, and, where they are a later portion
+// of a row, what the portions before came to: in tensor memory too, or (4-bit heads, whose weights need the room) in shared memory,
+// a lane a word, a column every 512 bytes.
+struct StepSums {
+    uint32_t at, cut_step, kept;
+    float* kept_shared;
+    int cuts;
+    bool later;
+};
+// Sixteen columns of them from `column` on.
+template <bool MX>
+__device__ __forceinline__ void step_sums(const StepSums& p, int column, uint32_t (&v)[16]) {
+    __syncwarp();
+    tmem_ld16(p.at + column, v);
+    tmem_wait_ld();
+#pragma unroll 1
+    for (int i = MX ? 1 : 1 - int(p.later); i < p.cuts; ++i) {
+        uint32_t u[16];
+        tmem_ld16(i == 0 ? p.kept + column : p.at + i * p.cut_step + column, u);
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(u[j]));
+    }
+    if (MX)  // (not a branch around the loads: with one the kernel takes 80 registers and spills, 86 -> 98 us for 32 rows)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + (p.later ? p.kept_shared[(column + j) * 128] : 0.f));
+}
+// A portion that is not a row's last, put with those before it.
+template <bool MX>
+__device__ __forceinline__ void step_keep(const StepSums& p, int columns) {
+#pragma unroll 1
+    for (int h = 0; h < columns; h += 16) {
+        uint32_t v[16];
+        step_sums<MX>(p, h, v);
+        if (MX) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) p.kept_shared[(h + j) * 128] = __uint_as_float(v[j]);
+        } else {
+            __syncwarp();
+            tmem_st16(p.kept + h, v);
+        }
+    }
+    if (!MX) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
 // The scores of a warp's 32 tokens under the rows of the batch: a lane has a token, a column is a row; by way of shared memory a
 // lane has a row (32 c + lane) and all of the tokens, and keeps that row's state. The loops stay short: a block comes here four
 // times, and straight code cost more in instruction fetches than it saved.
 template <bool MX, int W>
 __device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& sh, int quad, float back, const int32_t* list, int tokens,
-                                            bool all, uint32_t tmem, int cuts, uint32_t cut_step, const uint32_t (&bits)[W],
-                                            Partial (&state)[W], int lane) {
+                                            bool all, const StepSums& sums, const uint32_t (&bits)[W], Partial (&state)[W],
+                                            int lane) {
     float* turn = sh.turn[quad];
 #pragma unroll
     for (int c = 0; c < W; ++c) {
@@ -391,17 +444,7 @@ __device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& s
         for (int h = 0; h < 32; h += 16) {
             if (32 * c + h >= a.B) break;  // (of rows that are not there nothing is read below)
             uint32_t v[16];
-            __syncwarp();
-            tmem_ld16(tmem + 32 * c + h, v);
-            tmem_wait_ld();
-#pragma unroll 1
-            for (int i = 1; i < cuts; ++i) {
-                uint32_t u[16];
-                tmem_ld16(tmem + i * cut_step + 32 * c + h, u);
-                tmem_wait_ld();
-#pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(u[j]));
-            }
+            step_sums<MX>(sums, 32 * c + h, v);
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 turn[(h + j) * 33 + lane] = (bits[c] >> (h + j)) & 1u
@@ -485,13 +528,6 @@ __device__ __forceinline__ uint32_t mx_largest(const uint8_t* scales, int n) {
     top = __vmaxu4(top, top >> 16);
     return max(top & 255u, (top >> 8) & 255u);
 }
-__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&v)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
-        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
-        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
-        : "memory");
-}
 __device__ __forceinline__ void mma_f16_from_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -509,20 +545,24 @@ constexpr int kStepTiles = MX ? 1 : 2;  // tiles that share a stage at most
 //
 // The products' sums in tensor memory are cut off towards zero at every addition (measured: -1e-9 of the score per element of the
 // row, 4e-6 for 4096, ten times what sums that are rounded come to), so that a row's k is cut in `cuts` pieces with sums of their own,
-// as many as there is room for, which are added up, and rounded, when they are read.
+// as many as there is room for, which are added up, and rounded, when they are read. Pieces of more than kStepCut elements are not
+// taken: a longer row comes in portions of that many pieces, one portion's sums being read while the next one's are made.
+constexpr int kStepCut = 1024;
 struct StepLayout {
     int tiles, rows, atoms, steps, stages, cuts, cut_atoms;
-    uint32_t x_at, bytes;
+    int portions, portion_steps, last_cuts;
+    uint32_t x_at, bytes, kept;
 };
 template <bool MX>
 __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int most) {
     constexpr int X = MX ? 4 : 1;  // atoms of hidden states to an atom of weights
+    constexpr int kColumns = MX ? 128 : 512, kCut = kStepCut / (MX ? 256 : 64);
     StepLayout l;
     l.tiles = most > 128 && a.N <= 32 ? kStepTiles<MX> : 1;
     l.rows = most > 128 ? 128 * l.tiles : (max(most, 1) + 31) & ~31;
-    const int room = (MX ? 128 : 512) / (2 * l.tiles * a.N);
+    const int wide = l.tiles * a.N;
+    int room = kColumns / (2 * wide);
     l.cut_atoms = room >= 16 ? (a.row_atoms + 15) >> 4 : room >= 8 ? (a.row_atoms + 7) >> 3 : room >= 4 ? (a.row_atoms + 3) >> 2 : room >= 2 ? (a.row_atoms + 1) >> 1 : a.row_atoms;
-    l.cuts = (a.row_atoms + l.cut_atoms - 1) / l.cut_atoms;
     l.atoms = 1;
     int shift = 0;
     while (!MX && shift < 3 && l.atoms < a.row_atoms && 2 * l.atoms * (l.rows + X * a.N) * kStepAtom <= (48u << 10)) {
@@ -532,7 +572,24 @@ __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int mos
     l.steps = (a.row_atoms + l.atoms - 1) >> shift;
     l.x_at = uint32_t(l.atoms) * l.rows * kStepAtom;
     l.bytes = l.x_at + uint32_t(l.atoms) * X * a.N * kStepAtom;
-    l.stages = min(kStepStages, int(uint32_t(a.smem) / l.bytes));
+    uint32_t smem = uint32_t(a.smem);
+    if (l.cut_atoms <= kCut) {
+        l.cuts = l.last_cuts = (a.row_atoms + l.cut_atoms - 1) / l.cut_atoms;
+        l.portions = 1;
+        l.portion_steps = l.steps;
+        l.kept = 0;
+    } else {
+        // (portions end with a stage: kCut is a multiple of a stage's atoms)
+        if (MX) smem -= uint32_t(wide) * 512;
+        else room = (kColumns - wide) / (2 * wide);
+        l.cut_atoms = kCut;
+        l.cuts = room;
+        l.portions = (a.row_atoms + room * kCut - 1) / (room * kCut);
+        l.portion_steps = (room * kCut) >> shift;
+        l.last_cuts = (a.row_atoms - (l.portions - 1) * room * kCut + kCut - 1) / kCut;
+        l.kept = MX ? smem : uint32_t(2 * room * wide);
+    }
+    l.stages = min(kStepStages, int(smem / l.bytes));
     return l;
 }
 
@@ -640,15 +697,26 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             const uint32_t idesc = (MX ? kMmaF16Desc<128, 0, false, false> : kMmaBf16Desc<128, 0, false, false>) | uint32_t(a.N / 8) << 17;
             const uint32_t x_step = uint32_t(a.N) * kStepAtom >> 4, w_step = uint32_t(l.rows) * kStepAtom >> 4;
             for (int g = 0; g < groups && ok; ++g) {
-                const int it = groups_done + g, tiles = min(l.tiles, (n - g * per_group + 127) / 128);
-                if (!ring_wait(&sh.sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
-                    ok = false;
-                    break;
-                }
-                tmem_fence_after();
-                uint32_t d0 = tmem + uint32_t(it & 1) * l.cuts * l.tiles * a.N;
+                const int tiles = min(l.tiles, (n - g * per_group + 127) / 128);
+                int it = (groups_done + g) * l.portions - 1, left = 0;  // portion, stages left of it
+                uint32_t d0 = 0;
                 int in_cut = 0;  // atoms of the cut that are through
                 for (int s = 0; s < l.steps && ok; ++s) {
+                    if (left-- == 0) {
+                        if (s > 0) {
+                            if (elect_one()) mma_commit<1>(&sh.sums_full[it & 1]);
+                            __syncwarp();
+                        }
+                        ++it;
+                        left = l.portion_steps - 1;
+                        if (!ring_wait(&sh.sums_empty[it & 1], ((it >> 1) & 1) ^ 1)) {
+                            ok = false;
+                            break;
+                        }
+                        tmem_fence_after();
+                        d0 = tmem + uint32_t(it & 1) * l.cuts * l.tiles * a.N;
+                        in_cut = 0;
+                    }
                     if (!ring_wait(&sh.full[stage], phase)) {
                         ok = false;
                         break;
@@ -833,7 +901,6 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             };
             if (MX) find_largest(0);
             for (int g = 0; g < groups; ++g) {
-                const int it = groups_done + g;
                 largest = largest_next;
                 if (MX) find_largest(g + 1);
                 uint32_t bits[T][W];
@@ -845,22 +912,39 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
 #pragma unroll
                     for (int c = 0; c < W; ++c) bits[t][c] = have && 32 * c < a.B ? ld_after_wait(a.bits + int64_t(c) * a.VW * 32 + token) : 0u;
                 }
-                if (!ring_wait(&sh.sums_full[it & 1], (it >> 1) & 1)) {
-                    ok = false;
-                    break;
+                int it = (groups_done + g) * l.portions;
+                auto sums_of = [&](int t, bool last) {
+                    const uint32_t lanes = uint32_t(quad * 32) << 16;
+                    return StepSums{tmem + uint32_t((it & 1) * l.cuts * l.tiles + t) * a.N + lanes, uint32_t(l.tiles) * a.N,
+                                    tmem + l.kept + uint32_t(t) * a.N + lanes,
+                                    reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + l.kept) + quad * 32 + lane,
+                                    last ? l.last_cuts : l.cuts, it > (groups_done + g) * l.portions};
+                };
+                auto wait_sums = [&] {
+                    ok = ring_wait(&sh.sums_full[it & 1], (it >> 1) & 1);
+                    tmem_fence_after();
+                    return ok;
+                };
+                auto release = [&] {
+                    tmem_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.sums_empty[it & 1]);
+                };
+#pragma unroll 1
+                for (int p = 1; p < l.portions && wait_sums(); ++p, ++it) {
+#pragma unroll
+                    for (int t = 0; t < T; ++t)
+                        if (t < l.tiles && g * per_group + t * 128 + quad * 32 < n) step_keep<MX>(sums_of(t, false), a.B);
+                    release();
                 }
-                tmem_fence_after();
+                if (!ok || !wait_sums()) break;
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
                     const int at = g * per_group + t * 128 + quad * 32;
                     if (t < l.tiles && at < n)
-                        step_scores<MX>(a, sh, quad, MX ? mx_scale(largest) : 1.f, sh.list + at, n - at, all,
-                                        tmem + uint32_t((it & 1) * l.cuts * l.tiles + t) * a.N + (uint32_t(quad * 32) << 16), l.cuts,
-                                        uint32_t(l.tiles) * a.N, bits[t], state, lane);
+                        step_scores<MX>(a, sh, quad, MX ? mx_scale(largest) : 1.f, sh.list + at, n - at, all, sums_of(t, true), bits[t], state, lane);
                 }
-                tmem_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.sums_empty[it & 1]);
+                release();
             }
         }
         __syncwarp();

@@ -4,9 +4,10 @@ import numpy as np
 import pytest
 import torch
 
+import synth
 from paper_2605_29986_b200 import binding as cz
 from _gpu_util import Ctx
-from _head_util import pack
+from _head_util import mx_values, pack
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -99,3 +100,44 @@ def test_weight_gradient_summed_over_many_tokens(N):
             assert off.abs().max() <= tol, off.abs().max().item()
             # the row of the targets: g = d (1 / V - 1), 63 / 64 of d, which bf16 holds to 2^-8
             assert ((d_weight[0].double() / want + V - 1).abs() <= (V - 1) * (2.0 ** -8 + tol)).all()
+
+
+# ---- scores of the decode step, of long rows and large batches ------------------------------------------------------------
+def one_class(V):
+    return synth.Partition(V=V, K=1, c=np.zeros(V, np.int32), r=np.zeros(1, np.int32), sizes=np.array([V]))
+
+
+def positive_head(kind, V, H, gen):
+    """Weights above 0, so that nothing cancels and what is cut off of a sum is cut off of the score."""
+    if kind == "bf16":
+        weight = torch.rand((V, H), generator=gen, device="cuda").to(torch.bfloat16)
+        return cz.cfgzip_head(weight, cz.BF16, V, H), weight.double()
+    packed = (torch.randint(0, 256, (V, H // 2), generator=gen, device="cuda", dtype=torch.int32) & 0x77).to(torch.uint8)
+    scales = torch.randint(120, 125, (V, (H // 32 + 15) // 16 * 16), generator=gen, device="cuda", dtype=torch.int32).to(torch.uint8)
+    head = cz.cfgzip_head(packed, cz.MXFP4, V, H, H // 2, scales, scales.shape[1])
+    return head, mx_values(packed, scales, H).cuda()
+
+
+@pytest.mark.parametrize("kind,H,B", [(kind, H, B) for kind in ("bf16", "mxfp4") for H in (1024, 4096, 4128, 8192, 16384, 65536)
+                                      for B in (1, 16, 32, 48, 64, 128) if kind == "bf16" or B <= 64])
+def test_scores_of_long_rows(kind, H, B):
+    V = 20000 if H in (4096, 4128) else 300  # (blocks with 128 tokens and more, and with a few)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(H + B)
+    head, weight = positive_head(kind, V, H, gen)
+    hidden = torch.rand((B, H), generator=gen, device="cuda").to(torch.bfloat16)
+    logits = torch.full((B, V), 99.0, device="cuda")
+    argmax = torch.full((B,), -7, dtype=torch.int32, device="cuda")
+    with Ctx([one_class(V)]) as ctx:
+        ws = workspace(head, cz.HEAD_STEP, B)
+        class_mask = torch.ones((B, 1), dtype=torch.int32, device="cuda")
+        cz.cfgzip_head_step(ctx.h, ctx.ids[0], None, class_mask, 1, head, hidden, H, B, None, 0, logits, cz.F32, V, argmax, None, None,
+                            None, ws, ws.numel(), torch.cuda.current_stream())
+        torch.cuda.synchronize()
+    z = hidden.double() @ weight.T
+    off = (logits.double() - z) / z
+    # A piece of 1024 elements is 64 additions to tensor memory of 16 products each, cut off by less than 2^-23 of a sum that grows
+    # evenly, so half of that of the last on average. Then a rounding for every piece, and two for 4-bit heads' powers.
+    tol = 32 * 2.0 ** -23 + (H / 1024 + 3) * 2.0 ** -24
+    assert off.abs().max() <= tol, (off.abs().max().item(), off.mean().item())
+    assert off.mean().abs() <= 16 * 2.0 ** -23, off.mean().item()  # what is cut off is half a unit on average, roundings are even
