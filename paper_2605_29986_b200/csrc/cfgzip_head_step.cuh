@@ -488,9 +488,9 @@ __device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& s
     }
 }
 
-// 4-bit weights in tensor memory are f16, relative to the largest scale of their row: e2m1 numbers times 2^0 down to 2^-23 are
-// exact in f16, and of a block with a scale below that 2^-25 of the largest is lost at most. One conversion and one product for
-// two weights; going to bf16 by shifts, masks and products takes 23 instructions for eight (32 rows of 128256 x 4096: 163 us, 130).
+// 4-bit weights in tensor memory are f16, relative to the largest scale of their row, which becomes 2^13: e2m1 numbers times 2^13 (6 of
+// them are below f16's largest number) down to 2^-23 are exact in f16, and of a weight whose scale is below that 6 * 2^-38 of the largest
+// scale is lost at most. One conversion and one product for two weights; going to bf16 by shifts, masks and products takes 23 instructions for eight (32 rows of 128256 x 4096: 163 us, 130).
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
@@ -505,9 +505,10 @@ __device__ __forceinline__ void mx_word(uint32_t w, uint32_t scale, uint32_t* ou
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = mul_f16x2(t[i], scale);
 }
-// 2^(byte - largest) twice, as f16; `normal`: none is below 2^-14
+// 2^(byte - largest + kMxTop) twice, as f16; `normal`: none is below 2^-14
+constexpr int kMxTop = 13;
 __device__ __forceinline__ uint32_t mx_scale_pair(uint32_t byte, uint32_t largest, bool normal) {
-    const int e = int(byte) - int(largest) + 15;  // exponent field of a normal number
+    const int e = int(byte) - int(largest) + kMxTop + 15;  // exponent field of a normal number
     if (normal) return uint32_t(e) * 0x04000400u;
     const uint32_t b = e >= 1 ? uint32_t(e) << 10 : e >= -9 ? 1u << (9 + e) : 0u;
     return b | b << 16;
@@ -799,7 +800,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     }
                     largest = sh.largest[it & 1][row];
                 }
-                const uint32_t least = (largest > 14 ? largest - 14 : 0u) * 0x01010101u;
+                const uint32_t least = (largest > 14 + kMxTop ? largest - (14 + kMxTop) : 0u) * 0x01010101u;
                 uint2 eight = scale;
                 s += sets;
                 at_stage += sets;
@@ -942,7 +943,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 for (int t = 0; t < T; ++t) {
                     const int at = g * per_group + t * 128 + quad * 32;
                     if (t < l.tiles && at < n)
-                        step_scores<MX>(a, sh, quad, MX ? mx_scale(largest) : 1.f, sh.list + at, n - at, all, sums_of(t, true), bits[t], state, lane);
+                        step_scores<MX>(a, sh, quad, MX ? mx_scale(largest) * (1.f / (1 << kMxTop)) : 1.f, sh.list + at, n - at, all, sums_of(t, true), bits[t], state, lane);
                 }
                 release();
             }

@@ -141,3 +141,46 @@ def test_scores_of_long_rows(kind, H, B):
     tol = 32 * 2.0 ** -23 + (H / 1024 + 3) * 2.0 ** -24
     assert off.abs().max() <= tol, (off.abs().max().item(), off.mean().item())
     assert off.mean().abs() <= 16 * 2.0 ** -23, off.mean().item()  # what is cut off is half a unit on average, roundings are even
+
+
+# ---- 4-bit weights and hidden states of very different sizes --------------------------------------------------------------
+def four_bit_step(codes, scales, hidden):
+    """Scores from a 4-bit head of these codes and scale bytes, and the same in 64 bits."""
+    V, H = codes.shape
+    packed = (codes[:, ::2] | (codes[:, 1::2] << 4)).to(torch.uint8)
+    packed = torch.nn.functional.pad(packed, (0, -(H // 2) % 16)).contiguous()
+    scales = torch.nn.functional.pad(scales.to(torch.uint8), (0, -(H // 32) % 16)).contiguous()
+    head = cz.cfgzip_head(packed, cz.MXFP4, V, H, packed.shape[1], scales, scales.shape[1])
+    B = hidden.shape[0]
+    logits = torch.full((B, V), 99.0, device="cuda")
+    argmax = torch.full((B,), -7, dtype=torch.int32, device="cuda")
+    with Ctx([one_class(V)]) as ctx:
+        ws = workspace(head, cz.HEAD_STEP, B)
+        class_mask = torch.ones((B, 1), dtype=torch.int32, device="cuda")
+        cz.cfgzip_head_step(ctx.h, ctx.ids[0], None, class_mask, 1, head, hidden, H, B, None, 0, logits, cz.F32, V, argmax, None, None,
+                            None, ws, ws.numel(), torch.cuda.current_stream())
+        torch.cuda.synchronize()
+    weight = mx_values(packed, scales, H).cuda()
+    return logits.double(), weight
+
+
+@pytest.mark.parametrize("zeros", [False, True])  # the block with the largest scale holds weights, or only zeros
+@pytest.mark.parametrize("H,V", [(128, 120), (1056, 400)])
+def test_four_bit_blocks_far_below_the_largest_of_their_row(H, V, zeros):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(H)
+    codes = torch.randint(0, 16, (V, H), generator=gen, device="cuda", dtype=torch.int32)
+    below = torch.arange(V, device="cuda", dtype=torch.int32) % 40
+    scales = torch.full((V, H // 32), 150, dtype=torch.int32, device="cuda")
+    scales[:, 1:] -= below.unsqueeze(1)
+    if zeros:
+        codes[:, :32] = 0
+    hidden = torch.empty((3, H), device="cuda").normal_(0.0, 2.0, generator=gen)
+    hidden[:2, :32] = 0.0  # what is left of these rows is the small blocks' alone
+    hidden = hidden.to(torch.bfloat16)
+    got, weight = four_bit_step(codes, scales, hidden)
+    x = hidden.double().abs()
+    tol = H * 2.0 ** -24 * (x @ weight.abs().T)
+    # scales more than 2^36 below the largest: a weight is off by up to 6 times 2^-38 of that
+    tol += (below > 36) * 6 * 2.0 ** -38 * 2.0 ** (150 - 127) * x[:, 32:].sum(dim=1, keepdim=True)
+    assert ((got - hidden.double() @ weight.T).abs() <= tol).all()
