@@ -446,10 +446,14 @@ __device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& s
             uint32_t v[16];
             step_sums<MX>(sums, 32 * c + h, v);
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                turn[(h + j) * 33 + lane] = (bits[c] >> (h + j)) & 1u
-                                                ? (MX ? __uint_as_float(v[j]) * sh.back[32 * c + h + j] * back : __uint_as_float(v[j]))
-                                                : -INFINITY;
+            for (int j = 0; j < 16; ++j) {
+                float z = __uint_as_float(v[j]);
+                if (MX) {  // the smaller power first: large hidden states and small weights, or the other way round, meet in the middle
+                    const float x = sh.back[32 * c + h + j];
+                    z = z * (back < x ? back : x) * (back < x ? x : back);  // (a scale byte of 255 stays NaN)
+                }
+                turn[(h + j) * 33 + lane] = (bits[c] >> (h + j)) & 1u ? z : -INFINITY;
+            }
         }
         const uint32_t has = warp_transpose32(bits[c], lane);
         __syncwarp();

@@ -184,3 +184,17 @@ def test_four_bit_blocks_far_below_the_largest_of_their_row(H, V, zeros):
     # scales more than 2^36 below the largest: a weight is off by up to 6 times 2^-38 of that
     tol += (below > 36) * 6 * 2.0 ** -38 * 2.0 ** (150 - 127) * x[:, 32:].sum(dim=1, keepdim=True)
     assert ((got - hidden.double() @ weight.T).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("hidden_power,scale", [(124, 5), (110, 1), (-100, 230), (-120, 247), (0, 127), (60, 60)])
+def test_four_bit_scores_of_powers_far_apart(hidden_power, scale):
+    V, H = 140, 1024
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(scale)
+    codes = torch.randint(1, 8, (V, H), generator=gen, device="cuda", dtype=torch.int32)  # (all above 0: nothing cancels)
+    scales = torch.full((V, H // 32), scale, dtype=torch.int32, device="cuda")
+    hidden = ((1.0 + torch.rand((20, H), generator=gen, device="cuda")).double() * 2.0 ** hidden_power).to(torch.bfloat16)
+    got, weight = four_bit_step(codes, scales, hidden)
+    want = hidden.double() @ weight.T
+    assert (want < 2.0 ** 127).all() and (want > 2.0 ** -120).all()  # finite, and above the numbers that lose bits
+    assert ((got - want).abs() <= H * 2.0 ** -24 * want).all()
