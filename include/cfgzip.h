@@ -546,7 +546,8 @@ int cfgzip_launch_count(cfgzip_ctx* ctx, int64_t* out);
  *   "test_expire_waits"  test hook, default 0: 1 makes every warp of the streaming kernel report its first wait
  *                  for an asynchronous copy as run out AFTER the wait has completed, so that the error path
  *                  (flag, bounded drain of the copies in flight, cfgzip_poll_status -> CFGZIP_E_CUDA) can be
- *                  exercised with nothing left in flight; the results of such a call are undefined
+ *                  exercised with nothing left in flight; the results of such a call are undefined. The
+ *                  products of the cfgzip_head calls report theirs when their first stages are asked for
  *   "spread"       1 = launches of at most one block per SM (the streaming kernel of a small batch, the per-row
  *                  kernels of 32 to 148 rows) ask for more than half of an SM's shared memory, so that two of
  *                  their blocks never share an SM (default), 0 = only what the block needs

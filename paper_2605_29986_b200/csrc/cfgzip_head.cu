@@ -206,6 +206,7 @@ int run_mma(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUtenso
     a.n_tiles = ceil_div(a.cols, a.width);
     a.splits = std::max(1, a.splits);
     a.status = ctx->d_status;
+    a.expire = ctx->expire_test;
     auto kern = k_head_mma<A_MN, B_MN, KIND>;
     const size_t smem = kMmaSmem + (kOut ? 8 * kMmaOut : 0);
     CUtensorMap map_out = map_a;
@@ -282,6 +283,7 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
     const unsigned blocks = unsigned(std::min(ctx->sm_count, kStepBlocks));
     a.rounds = ceil_div(ceil_div(a.V, blocks), kStepShare);
     a.smem = 181 << 10;
+    a.expire = ctx->expire_test;
     const size_t smem = size_t(a.smem) + 1024 + kStepTile;  // (products read 128 rows, also where fewer are there)
     auto kern = mx ? k_head_step<true> : k_head_step<false>;
     if ((rc = ensure_smem(ctx, kern, smem)) != CFGZIP_OK) return rc;

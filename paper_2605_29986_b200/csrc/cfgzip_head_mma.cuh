@@ -43,6 +43,7 @@ struct MmaArgs {
     int32_t k_blocks, splits;  // the k range is cut in `splits`, each with a result of its own
     int32_t m_fast;            // neighbouring tiles go along m
     int32_t* status;
+    int32_t expire;            // test hook: the block reports a wait as run out when the first stages are asked for (see cfgzip_set_tuning)
     // scores
     const uint32_t* mask;
     int64_t mask_stride;
@@ -242,7 +243,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                const __grid_constant__ CUtensorMap map_out) {
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kMmaStages], empty[kMmaStages], sums_full[2], sums_empty[2];
-    __shared__ uint32_t s_tmem;
+    __shared__ __align__(8) uint64_t drained;
+    __shared__ uint32_t s_tmem, s_end[2];  // (of either block: the stages it has asked for, and in the highest bit whether a wait ran out)
     constexpr bool kOut = KIND == kMmaSum || KIND == kMmaBf16;
     constexpr int kPortion = kOut ? kMmaOutPortion : kMmaPortion;
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -258,6 +260,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             mbar_init(&sums_full[i], 1);
             mbar_init(&sums_empty[i], 16);  // eight warps of either block
         }
+        mbar_init(&drained, 1);
         mbar_init_fence();
         prefetch_tensor_map(&map_a);
         prefetch_tensor_map(&map_b);
@@ -269,14 +272,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     tmem_fence_after();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t tmem = s_tmem;
-    bool ok = true;
+    bool ok = warp == 0 || !a.expire;  // (the hook: nothing is done with the first stages asked for)
+    uint32_t asked = 0;
     if (warp == 0) {
         if (lane == 0) {
             Ring r;
             for (int i = pair; i < tiles && ok; i += pairs) {
                 const MmaTile t = mma_tile(a, i);
                 const int m = t.m * kMmaTile + int(rank) * 128, n = t.n * a.width + int(rank) * (a.width / 2);
-                for (int k = t.k0; k < t.k1; ++k) {
+                const int k1 = a.expire ? min(t.k1, t.k0 + kMmaStages) : t.k1;
+                for (int k = t.k0; k < k1; ++k) {
                     if (!ring_wait<true>(&empty[r.stage], r.phase ^ 1)) {
                         ok = false;
                         break;
@@ -295,8 +300,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                     } else {
                         tma_load_pair(at + kMmaHalf, &map_b, k * kMmaK, n, bar);
                     }
+                    ++asked;
                     r.next<kMmaStages>();
                 }
+                if (a.expire) ok = false;
             }
         }
     } else if (warp == 1) {
@@ -376,12 +383,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
         }
         if (kOut && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
-    if (!ok && lane == 0) atomicExch(a.status + 3, 1);
     __syncwarp();
     tmem_fence_before();
-    __syncthreads();
+    const uint32_t failed = __syncthreads_or(!ok) ? 0x80000000u : 0u;
+    if (threadIdx.x == 0) {
+        s_end[rank] = asked | failed;
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_shared(&s_end[rank], rank ^ 1)), "r"(asked | failed) : "memory");
+    }
+    __syncwarp();
     cluster_barrier();
     tmem_fence_after();
+    if ((s_end[0] | s_end[1]) >> 31) {
+        // A wait ran out: the copies that either block has asked for (the first one's barriers count both's) and the products get the same
+        // bounded time once more, then the blocks leave without results.
+        if (rank == 0 && threadIdx.x == 0) {
+            atomicExch(a.status + 3, 1);
+            const uint32_t most = max(s_end[0] & 0x7FFFFFFFu, s_end[1] & 0x7FFFFFFFu);
+            for (uint32_t i = most - min(most, uint32_t(kMmaStages)); i < most; ++i)
+                mbar_wait_cluster(&full[i % kMmaStages], (i / kMmaStages) & 1);
+        }
+        __syncwarp();
+        if (rank == 0 && warp == 1) {
+            if (elect_one()) mma_commit<2>(&drained);
+            __syncwarp();
+            mbar_wait_cluster(&drained, 0);
+        }
+        __syncwarp();
+        __syncthreads();
+        cluster_barrier();
+    }
     if (warp == 2) tmem_free<2>(tmem, 512);
 }
 

@@ -47,6 +47,7 @@ struct HeadStepArgs {
     int32_t bytes;         // of a row of weights that count
     int32_t smem;          // shared memory for stages
     int32_t rounds;
+    int32_t expire;        // test hook: the block reports a wait as run out when the first stages are asked for (see cfgzip_set_tuning)
     const uint16_t* hidden;  // 4-bit heads: rows brought to at most 2^15 and copied as f16 to `half`
     int64_t hidden_stride;
     uint16_t* half;        // [B, half_stride], zeros behind H
@@ -270,10 +271,10 @@ __device__ __forceinline__ bool wait_count(const uint32_t* count, uint32_t least
 }
 
 struct StepShared {
-    uint64_t full[kStepStages], empty[kStepStages], sums_full[2], sums_empty[2], w_full[3], w_empty[3];
+    uint64_t full[kStepStages], empty[kStepStages], sums_full[2], sums_empty[2], w_full[3], w_empty[3], drained;
     uint32_t tmem;
     uint32_t valid[kStepRows / 32];  // rows that have a partition
-    int32_t entries, is_last;
+    int32_t entries, is_last, stages;
     float back[kStepRowsMx];         // 4-bit heads: what brings a row's products back
     uint32_t largest[2][128];        // ... and the largest scale byte of the rows of a tile's tokens
     uint32_t largest_tiles[4];       // how many tiles' are there, by the quarters of a tile
@@ -366,7 +367,7 @@ __device__ __forceinline__ void step_finish_row(const HeadStepArgs& a, int row, 
     for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
     pos = __reduce_min_sync(0xFFFFFFFFu, pos);
     if (lane) return;
-    const bool any = pos != kNoPos;
+    const bool any = uint32_t(pos) < uint32_t(a.V);  // (also where a wait ran out and there are no states)
     const float log_sum = logf(s);
     a.argmax[row] = any ? pos : -1;
     if (a.rep) a.rep[row] = any ? reps[pos] : -1;
@@ -618,6 +619,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
             mbar_init(&sh.w_full[i], 4);
             mbar_init(&sh.w_empty[i], 1);
         }
+        mbar_init(&sh.drained, 1);
         for (int i = 0; i < 4; ++i) sh.largest_tiles[i] = 0;
         mbar_init_fence();
         prefetch_tensor_map(&map_x);
@@ -637,6 +639,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
     tmem_fence_after();
     const uint32_t tmem = sh.tmem;
     bool ok = true;
+    int failed = 0;
     int stage = 0, groups_done = 0;
     uint32_t phase = 0, set_phases = 0;
     Partial state[W];
@@ -650,6 +653,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         const StepLayout l = step_layout<MX>(a, most);  // (the same in every round, as is `all`)
         if (round == 0) {
             if (threadIdx.x == 0) {
+                sh.stages = l.stages;
                 for (int i = 0; i < kStepStages; ++i) mbar_init(&sh.full[i], all ? 1 : 1 + 256);  // ... and every thread that fetches weights
                 mbar_init_fence();
             }
@@ -658,6 +662,9 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         const int per_group = 128 * l.tiles, groups = (n + per_group - 1) / per_group;
         const int sets = all ? 3 : 2;  // of four warps that take weights apart: with nothing to fetch, there are four more
         int set = 0;
+        // the hook: nothing is done with the first stages asked for
+        const int asked_steps = a.expire ? min(l.steps, l.stages) : l.steps;
+        if (a.expire) ok = warp == 0 || (warp >= 8 && warp < 16 && !all);
         auto next = [&] {
             if (++stage == l.stages) {
                 stage = 0;
@@ -674,7 +681,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     ++large;
                     small = 0;
                 }
-                for (int s = 0; s < l.steps; ++s) {
+                for (int s = 0; s < asked_steps; ++s) {
                     const int first = s * l.atoms, atoms = min(l.atoms, a.row_atoms - first);
                     if (!ring_wait(&sh.empty[stage], phase ^ 1)) {
                         ok = false;
@@ -697,6 +704,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     __syncwarp();
                     next();
                 }
+                if (a.expire) ok = false;
             }
         } else if (warp == 1) {
             const uint32_t idesc = (MX ? kMmaF16Desc<128, 0, false, false> : kMmaBf16Desc<128, 0, false, false>) | uint32_t(a.N / 8) << 17;
@@ -869,7 +877,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     if (i * 32 < rows)  // (rows behind the last one are filled up with it)
                         from[i] = static_cast<const char*>(a.weight) +
                                   int64_t(sh.list[min(g * per_group + i * 32 + row, n - 1)]) * a.row_bytes + chunk * 16;
-                for (int s = 0; s < l.steps; ++s) {
+                for (int s = 0; s < asked_steps; ++s) {
                     if (!ring_wait(&sh.empty[stage], phase ^ 1)) {
                         ok = false;
                         break;
@@ -888,6 +896,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.full[stage])) : "memory");
                     next();
                 }
+                if (a.expire) ok = false;
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
         } else if (warp >= 4) {
@@ -905,7 +914,7 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                                  : "memory");
             };
             if (MX) find_largest(0);
-            for (int g = 0; g < groups; ++g) {
+            for (int g = 0; g < groups && ok; ++g) {
                 largest = largest_next;
                 if (MX) find_largest(g + 1);
                 uint32_t bits[T][W];
@@ -954,9 +963,24 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
         }
         __syncwarp();
         groups_done += groups;
-        __syncthreads();
+        failed = __syncthreads_or(!ok);
+        if (failed) break;
     }
-    if (!ok && lane == 0) atomicExch(a.status + 3, 1);
+    if (failed) {
+        // A wait ran out: the copies in flight and the products get the same bounded time once more (other copies to shared memory have
+        // been waited for), then the block leaves with what it has. (In the loop this took the 4-bit kernel 80 registers and spills.)
+        if (threadIdx.x == 0) {
+            atomicExch(a.status + 3, 1);
+            for (int i = 0; i < sh.stages; ++i) mbar_wait(&sh.full[i], i < stage ? phase : phase ^ 1);  // (one never asked for counts as through)
+        }
+        __syncwarp();
+        if (warp == 1) {
+            if (elect_one()) mma_commit<1>(&sh.drained);
+            __syncwarp();
+            mbar_wait(&sh.drained, 0);
+        }
+        __syncwarp();
+    }
     // the four warps' states to one, out to the others' and, in the last block to come here, to the results
     if (warp >= 4 && warp < 8) {
 #pragma unroll
