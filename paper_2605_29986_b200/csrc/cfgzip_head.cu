@@ -198,16 +198,18 @@ int tensor_map_out(cfgzip_ctx* ctx, CUtensorMap* map, const MmaArgs& a, bool bf1
     return CFGZIP_OK;
 }
 
-template <bool A_MN, bool B_MN, int KIND>
+template <bool A_MN, bool B_MN, int KIND, bool LONG = true>
 int run_mma(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUtensorMap& map_b, cudaStream_t st) {
     constexpr bool kOut = KIND == kMmaSum || KIND == kMmaBf16;
+    a.splits = std::max(1, a.splits);
+    if constexpr (kOut && LONG)
+        if (ceil_div(a.k_blocks, a.splits) <= kMmaOutPortion) return run_mma<A_MN, B_MN, KIND, false>(ctx, a, map_a, map_b, st);
     if (kOut) a.width = kMmaTile;
     a.m_tiles = ceil_div(a.rows, kMmaTile);
     a.n_tiles = ceil_div(a.cols, a.width);
-    a.splits = std::max(1, a.splits);
     a.status = ctx->d_status;
     a.expire = ctx->expire_test;
-    auto kern = k_head_mma<A_MN, B_MN, KIND>;
+    auto kern = k_head_mma<A_MN, B_MN, KIND, LONG>;
     const size_t smem = kMmaSmem + (kOut ? 8 * kMmaOut : 0);
     CUtensorMap map_out = map_a;
     int rc = kOut ? tensor_map_out(ctx, &map_out, a, KIND == kMmaBf16) : CFGZIP_OK;

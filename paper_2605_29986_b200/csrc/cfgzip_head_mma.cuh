@@ -25,10 +25,10 @@ constexpr int kMmaTile = 256;      // rows and columns of a pair's tile
 constexpr int kMmaK = 64;          // k of a stage
 // Stages whose sums are left in tensor memory, where every addition is cut off towards zero (-1e-9 of a sum per element of k); scores
 // add the portions up in registers, rounded. Those of the gradient too: what counts of them are differences to an lse that was made of
-// the loss's (a gradient of 4096 tokens takes 4 % longer for it: 9.7 -> 10.1 ms).
+// the loss's (for which a gradient of 4096 tokens of 128256 x 4096 takes 4 % longer, 9.4 -> 9.8 ms in a row).
 constexpr int kMmaPortion = 8;
 // ... and the sums over tokens of the gradient, which may be over a whole text or vocabulary (in one go 65536 tokens lose 3e-4 of a sum of
-// positive terms, 200003 lose 1.3e-3; in portions of 2048 under 8e-6. 1000 tokens of 50021 x 1024: 318 -> 329 us).
+// positive terms, 200003 lose 1.3e-3; in portions of 2048 under 8e-6. 4000 tokens of 8000 x 2048: 108 us for d_weight, in one go 104).
 constexpr int kMmaOutPortion = 32;
 constexpr uint32_t kMmaHalf = 128 * kMmaK * 2;           // bytes of one operand of a stage in one block
 constexpr size_t kMmaSmem = size_t(kMmaStages) * 2 * kMmaHalf + 1024;
@@ -195,49 +195,46 @@ __device__ __forceinline__ void tma_store3(const void* tensor_map, int x, int y,
 // last row or column: sums of few stages wait for nothing but their stores, and stored by lanes, a row each, they took twice as
 // long (gradient of 50021 x 1024 for 100 tokens: 50 us).
 template <bool BF16>
-__device__ __forceinline__ void out_epilogue(const MmaArgs& a, const CUtensorMap& map, const MmaTile& t, int half, int first, int lane,
-                                             float (&sums)[128], uint32_t buffer) {
-    constexpr int kCols = BF16 ? 64 : 32;
-    if (first >= a.rows) return;
-    const int row = first + lane;
-    const bool add = a.add && row < a.rows;
+constexpr int kOutCols = BF16 ? 64 : 32;  // columns in 128 bytes
+template <bool BF16>
+__device__ __forceinline__ void out_columns(const MmaArgs& a, const CUtensorMap& map, const MmaTile& t, int n, int first, int lane, bool add,
+                                            float* f, uint32_t buffer) {
+    constexpr int kCols = kOutCols<BF16>;
+    if (add) {
+        const char* from = static_cast<const char*>(a.out) + (t.split * a.split_elems + int64_t(first + lane) * a.ld + n) * (BF16 ? 2 : 4);
 #pragma unroll
-    for (int c = 0; c < 128 / kCols; ++c) {
-        const int n = t.n * kMmaTile + 128 * half + kCols * c;
-        if (n >= a.cols) break;
-        float* f = sums + kCols * c;
-        uint32_t o[32];
-        if (add) {
-            const char* from = static_cast<const char*>(a.out) + (t.split * a.split_elems + int64_t(row) * a.ld + n) * (BF16 ? 2 : 4);
+        for (int j = 0; j < 8; ++j) {
+            if (n + j * kCols / 8 >= a.cols) break;
+            const uint4 b = ld_after_wait(reinterpret_cast<const uint4*>(from + 16 * j));
+            const uint32_t w[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (n + j * kCols / 8 >= a.cols) break;
-                const uint4 b = ld_after_wait(reinterpret_cast<const uint4*>(from + 16 * j));
-                const uint32_t w[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                for (int k = 0; k < kCols / 8; ++k)
-                    f[j * kCols / 8 + k] += __uint_as_float(BF16 ? (k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16) : w[k & 3]);
-            }
+            for (int k = 0; k < kCols / 8; ++k)
+                f[j * kCols / 8 + k] += __uint_as_float(BF16 ? (k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16) : w[k & 3]);
         }
-#pragma unroll
-        for (int j = 0; j < 32; ++j) o[j] = BF16 ? bf16_pair(f[2 * j % kCols], f[(2 * j + 1) % kCols]) : __float_as_uint(f[j % kCols]);
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (the copy before has read the buffer)
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffer + uint32_t(lane) * 128 + (uint32_t(j ^ (lane & 7)) << 4)),
-                         "r"(o[4 * j]), "r"(o[4 * j + 1]), "r"(o[4 * j + 2]), "r"(o[4 * j + 3])
-                         : "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) tma_store3(&map, n, first, t.split, buffer);
     }
+    uint32_t o[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) o[j] = BF16 ? bf16_pair(f[2 * j % kCols], f[(2 * j + 1) % kCols]) : __float_as_uint(f[j % kCols]);
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (the copy before has read the buffer)
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffer + uint32_t(lane) * 128 + (uint32_t(j ^ (lane & 7)) << 4)),
+                     "r"(o[4 * j]), "r"(o[4 * j + 1]), "r"(o[4 * j + 2]), "r"(o[4 * j + 3])
+                     : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) tma_store3(&map, n, first, t.split, buffer);
 }
 
 // D[rows, cols] = A B^T in tiles of 256 x width by pairs of blocks (each holds 128 rows of A and half of B's, and the sums of its 128
 // rows), persistent. Operands K-major (k contiguous) or MN-major, from tensor maps with boxes of 64 x 128 (x width / 2) or 64 x 64;
 // an MN-major B and results that go out by tiled copies have a width of 256.
-template <bool A_MN, bool B_MN, int KIND>
+//
+// Sums are read portion by portion by both sets of warps, a half of the columns each, and added up in registers. Where no tile's sum
+// has more than one portion (LONG false), and what takes the time is the results' way out, the sets take tiles in turn instead, straight
+// from tensor memory (100 tokens of 50021 x 1024: 31 us for d_weight against 38).
+template <bool A_MN, bool B_MN, int KIND, bool LONG>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     k_head_mma(const __grid_constant__ MmaArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ CUtensorMap map_out) {
@@ -247,6 +244,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     __shared__ uint32_t s_tmem, s_end[2];  // (of either block: the stages it has asked for, and in the highest bit whether a wait ran out)
     constexpr bool kOut = KIND == kMmaSum || KIND == kMmaBf16;
     constexpr int kPortion = kOut ? kMmaOutPortion : kMmaPortion;
+    constexpr bool kTurns = !LONG;
+    static_assert(kOut || LONG, "scores are summed in portions");
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -258,7 +257,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sums_full[i], 1);
-            mbar_init(&sums_empty[i], 16);  // eight warps of either block
+            mbar_init(&sums_empty[i], kTurns ? 8 : 16);  // four warps of either block (all eight)
         }
         mbar_init(&drained, 1);
         mbar_init_fence();
@@ -343,8 +342,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                 }
             }
         }
-    } else if (warp >= 4) {
-        // Both sets read every portion, a half of the columns each, and keep the sums in registers.
+    } else if (warp >= 4 && !kTurns) {
         const int half = (warp - 4) >> 2, quad = warp & 3;
         const uint32_t empty_bar[2] = {peer_shared(&sums_empty[0], 0), peer_shared(&sums_empty[1], 0)};
         int it = 0;
@@ -377,11 +375,53 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             if (ok && KIND == kMmaLoss) loss_epilogue(a, t, half, row, valid, sums, bits);
             if (ok && KIND == kMmaStep) step_epilogue(a, t, half, row, valid, sums, bits);
             if (ok && KIND == kMmaGrad) grad_epilogue(a, t, half, row, valid, sums, bits);
-            if (ok && kOut)
-                out_epilogue<KIND == kMmaBf16>(a, map_out, t, half, row - lane, lane, sums,
-                                               stages + kMmaStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
+            if (ok && kOut && row - lane < a.rows) {
+                const bool add = a.add && valid;
+                constexpr int kCols = kOutCols<KIND == kMmaBf16>;
+#pragma unroll
+                for (int c = 0; c < 128 / kCols; ++c) {
+                    const int n = t.n * kMmaTile + 128 * half + kCols * c;
+                    if (n >= a.cols) break;
+                    out_columns<KIND == kMmaBf16>(a, map_out, t, n, row - lane, lane, add, sums + kCols * c,
+                                                  stages + kMmaStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
+                }
+            }
         }
         if (kOut && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    } else if (warp >= 4) {
+        const int set = (warp - 4) >> 2, quad = warp & 3;
+        const uint32_t empty_bar = peer_shared(&sums_empty[set], 0);
+        int it = 0;
+        for (int i = pair; i < tiles && ok; i += pairs, ++it) {
+            if ((it & 1) != set) continue;
+            const MmaTile t = mma_tile(a, i);
+            const int first = t.m * kMmaTile + int(rank) * 128 + quad * 32;
+            if (!ring_wait<true>(&sums_full[set], (it >> 1) & 1)) {
+                ok = false;
+                break;
+            }
+            tmem_fence_after();
+            const bool add = a.add && first + lane < a.rows;
+            constexpr int kCols = kOutCols<KIND == kMmaBf16>;
+#pragma unroll 1
+            for (int n = t.n * kMmaTile, c = 0; c < kMmaTile && n < a.cols && first < a.rows; c += kCols, n += kCols) {
+                float f[kCols];
+#pragma unroll
+                for (int h = 0; h < kCols; h += 32) {
+                    uint32_t v[32];
+                    __syncwarp();
+                    tmem_ld32(tmem + set * 256 + c + h + (uint32_t(quad * 32) << 16), v);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) f[h + j] = __uint_as_float(v[j]);
+                }
+                out_columns<KIND == kMmaBf16>(a, map_out, t, n, first, lane, add, f, stages + kMmaStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
+            }
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at_peer(empty_bar);
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     tmem_fence_before();

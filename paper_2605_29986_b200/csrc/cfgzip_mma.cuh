@@ -110,8 +110,10 @@ __device__ __forceinline__ void tma_load_pair(uint32_t dst_smem, const void* ten
         "l"(tensor_map), "r"(x), "r"(y), "r"(bar)
         : "memory");
 }
+// An arrival that lets go of sums whose loads from tensor memory are complete (waited for): nothing else has to be seen by who waits, and
+// a release would first wait for the warp's stores to global memory (gradient of the scores, 1000 tokens of 50021 x 1024: 96 against 86 us).
 __device__ __forceinline__ void arrive_at_peer(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void prefetch_tensor_map(const void* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
