@@ -118,10 +118,16 @@ def positive_head(kind, V, H, gen):
     return head, mx_values(packed, scales, H).cuda()
 
 
-@pytest.mark.parametrize("kind,H,B", [(kind, H, B) for kind in ("bf16", "mxfp4") for H in (1024, 4096, 4128, 8192, 16384, 65536)
-                                      for B in (1, 16, 32, 48, 64, 128) if kind == "bf16" or B <= 64])
-def test_scores_of_long_rows(kind, H, B):
-    V = 20000 if H in (4096, 4128) else 300  # (blocks with 128 tokens and more, and with a few)
+LONG = [(kind, H, B, 20000 if H in (4096, 4128) else 300)  # (blocks with 128 tokens and more, and with a few)
+        for kind in ("bf16", "mxfp4") for H in (1024, 4096, 4128, 8192, 16384, 65536) for B in (1, 16, 32, 48, 64, 128)
+        if kind == "bf16" or B <= 64]
+# 300 tokens to a block and more, and more than a block lists at a time
+LONG += [("bf16", 8192, 16, 50000), ("bf16", 8192, 32, 50000), ("bf16", 8192, 70, 50000), ("bf16", 4096, 96, 50000),
+         ("mxfp4", 8192, 40, 50000), ("mxfp4", 8192, 12, 50000), ("mxfp4", 1312, 33, 310000), ("bf16", 2056, 100, 310000)]
+
+
+@pytest.mark.parametrize("kind,H,B,V", LONG)
+def test_scores_of_long_rows(kind, H, B, V):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(H + B)
     head, weight = positive_head(kind, V, H, gen)
@@ -198,3 +204,38 @@ def test_four_bit_scores_of_powers_far_apart(hidden_power, scale):
     want = hidden.double() @ weight.T
     assert (want < 2.0 ** 127).all() and (want > 2.0 ** -120).all()  # finite, and above the numbers that lose bits
     assert ((got - want).abs() <= H * 2.0 ** -24 * want).all()
+
+
+@pytest.mark.parametrize("H", [1024, 4096, 16384, 65536])
+@pytest.mark.parametrize("N", [40, 150])
+def test_normalisers_of_long_rows(H, N):
+    """The loss, and the step of more than 128 rows: sums in pieces of 512."""
+    V = 300
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(H + N)
+    head, weight = positive_head("bf16", V, H, gen)
+    hidden = (torch.rand((N, H), generator=gen, device="cuda") * 2.0 ** -6).to(torch.bfloat16)
+    targets = torch.randint(0, V, (N,), generator=gen, device="cuda", dtype=torch.int32)
+    loss, lse, step_lse = (torch.full((N,), 99.0, device="cuda") for _ in range(3))
+    argmax = torch.full((N,), -7, dtype=torch.int32, device="cuda")
+    st = torch.cuda.current_stream()
+    with Ctx([one_class(V)]) as ctx:
+        ws = workspace(head, cz.HEAD_LOSS, N)
+        cz.cfgzip_head_loss(ctx.h, head, hidden, H, N, None, 0, targets, loss, lse, ws, ws.numel(), st)
+        ws = workspace(head, cz.HEAD_STEP, N)
+        class_mask = torch.ones((N, 1), dtype=torch.int32, device="cuda")
+        cz.cfgzip_head_step(ctx.h, ctx.ids[0], None, class_mask, 1, head, hidden, H, N, None, 0, None, cz.F32, V, argmax, None, None,
+                            step_lse, ws, ws.numel(), st)
+        torch.cuda.synchronize()
+    z = hidden.double() @ weight.T
+    want, top = torch.logsumexp(z, dim=1), z.amax(dim=1)
+    of_target = z[torch.arange(N, device="cuda"), targets.long()]
+    # A piece of 512 is 32 additions to tensor memory, cut off by less than 2^-23 of a sum that grows evenly, half of that of the last on
+    # average; then a rounding for every piece. (Steps of up to 128 rows: twice as long.) To lse a sum of V exponentials of relative
+    # accuracy 2^-20 and two roundings are added, to the loss the target's score as well.
+    pieces = 1 if N > 128 else 2
+    score = 16 * 2.0 ** -23 + H / 512 * 2.0 ** -24
+    rest = 2.0 ** -20 + 2.0 ** -23 * top
+    assert ((lse.double() - want).abs() <= score * top + rest).all()
+    assert ((step_lse.double() - want).abs() <= pieces * score * top + rest).all()
+    assert ((loss.double() - (want - of_target)).abs() <= score * (top + of_target) + rest).all()
