@@ -494,8 +494,6 @@ DensePlan plan_multi(cfgzip_ctx* ctx, const PartSet& ps, int32_t B, int masks_pe
     return d;
 }
 
-// A call may pass CFGZIP_ROWS_AS_PLANNED for its row -> partition vector: it then means the vector given to the
-// last cfgzip_plan_rows, whose grouping is still in the plan buffers.
 int check_step_args(cfgzip_ctx* ctx, const uint32_t* class_mask, int64_t cm_stride, int32_t B, int mode) {
     if (!ctx || B < 0) return CFGZIP_E_ARG;
     if (mode != CFGZIP_AUTO && mode != CFGZIP_DENSE && mode != CFGZIP_SPARSE) return CFGZIP_E_ARG;

@@ -370,8 +370,10 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
     uint32_t* mask = vocab_mask ? vocab_mask : w.mask;
     const int64_t mask_stride = vocab_mask ? vocab_stride_words : ps.VW;
     const PartDev& one = ctx->parts[size_t(part0)].dev;
-    // More rows than one pass over the weights takes are a product of two tall matrices, and together they allow most of the
-    // vocabulary. (256 rows of 128256 x 4096: 252 us, a pass of 128 rows alone 221. Its scores leave in the wrong order to be stored.)
+    // More rows than one pass over the weights takes are a product of two tall matrices, over all of the head: what the rows allow
+    // together is known on the device alone. (128256 x 4096: 256 rows that allow most of it 236 to 241 us, a pass of 128 rows alone 221, so
+    // two of them 442; 256 rows that allow 3 to 21 % of it together would take 177 to 213 in two passes, 129 rows that allow 3 % 112 and
+    // not 225. The scores of this product leave in the wrong order to be stored.)
     const bool tall = B > kStepRows && head->dtype == CFGZIP_BF16 && !logits;
     const bool table = !tall && !rows && one.c16 && one.KW <= kTableWords;
     if (!table && (rc = cfgzip_expand_mask(ctx, part0, row_part, class_mask, class_stride_words, mask, mask_stride, B, CFGZIP_DENSE, stream)) !=

@@ -1,8 +1,8 @@
 // Products of tall matrices for the head: scores of the loss and its gradient, and the two products of the gradient; also the scores of
 // decode steps of many rows. Bound by the tensor cores from some 200 rows on: pairs of blocks (cta_group::2) on tiles of 256 x 256, so
-// that each SM reads half of either operand from shared memory, six stages of 64 k, sums of two tiles in tensor memory so that one is
-// read while the next is made. A gradient of 4096 tokens, 128256 x 4096, runs at 1320 to 1570 TFLOP/s as power allows (cuBLAS: 1380 long,
-// 1620 short), the loss of 8192 at 1250 to 1290.
+// that each SM reads half of either operand from shared memory, six stages of 64 k, sums of two portions in tensor memory so that one
+// is read while the next is made. A gradient of 4096 tokens, 128256 x 4096, takes 9.3 to 10.1 ms, 1270 to 1390 TFLOP/s as power allows
+// (cuBLAS: 1380 long, 1620 short), the loss of 8192 6.65 to 6.73 ms, 1280 to 1290.
 #pragma once
 
 #include <cuda.h>

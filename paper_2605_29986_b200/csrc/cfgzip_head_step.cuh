@@ -6,10 +6,10 @@
 //
 // 32 rows of 128256 x 4096 (bf16, 97 % allowed by some row): 1.05 GB in 173 to 179 us with the masks, 5.9 TB/s; inside the loop the
 // copies run at the memory's rate, and some 20 us go to the masks, the list, the first loads and the last scores. From 4 bits: 279 MB
-// in 81 to 92 us, one row of 151936 x 2560 in 63. Boxes of 128-byte pieces of 128 rows come at 5.1 to 5.7 TB/s (measured alone), 850
+// in 85 to 92 us, one row of 151936 x 2560 in 65. Boxes of 128-byte pieces of 128 rows come at 5.1 to 5.7 TB/s (measured alone), 850
 // cycles for 128 tokens x 256 weights, turning those into f16 takes 550 (the loop alone); from 17 rows on the hidden states, which
-// every block brings past again for each tile, are as many bytes as the weights (16 rows: 75 us, 32: 82, 64: 111). One row of 32000 x
-// 2048: 20 us, of which the loads need 6; what is left is latency (masks 4, list 3, first loads 2, scores and results 3, launches).
+// every block brings past again for each tile, are as many bytes as the weights (16 rows: 76 us, 32: 85, 64: 122, of which the sums in portions are 11). One row of 32000 x
+// 2048: 20 us, of which the loads need 6; what is left is latency (masks 4, list 3, first loads 2, scores and results 3, two launches).
 #pragma once
 
 #include <cuda.h>

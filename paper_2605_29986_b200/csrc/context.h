@@ -203,6 +203,8 @@ inline int resolve_parts(cfgzip_ctx* ctx, cfgzip_part_id part0, bool mixed, Part
     return CFGZIP_OK;
 }
 
+// A call may pass CFGZIP_ROWS_AS_PLANNED for its row -> partition vector: it then means the vector given to the
+// last cfgzip_plan_rows, whose grouping is still in the plan buffers.
 inline int resolve_row_part(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t** row_part, int32_t B, bool* planned) {
     *planned = false;
     if (*row_part != CFGZIP_ROWS_AS_PLANNED) return CFGZIP_OK;
