@@ -233,7 +233,7 @@ __device__ __forceinline__ void out_columns(const MmaArgs& a, const CUtensorMap&
 //
 // Sums are read portion by portion by both sets of warps, a half of the columns each, and added up in registers. Where no tile's sum
 // has more than one portion (LONG false), and what takes the time is the results' way out, the sets take tiles in turn instead, straight
-// from tensor memory (100 tokens of 50021 x 1024: 31 us for d_weight against 38).
+// from tensor memory (100 tokens of 50021 x 1024: 26 us for d_weight against 38).
 template <bool A_MN, bool B_MN, int KIND, bool LONG>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     k_head_mma(const __grid_constant__ MmaArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -443,8 +443,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                 mbar_wait_cluster(&full[i % kMmaStages], (i / kMmaStages) & 1);
         }
         __syncwarp();
-        if (rank == 0 && warp == 1) {
-            if (elect_one()) mma_commit<2>(&drained);
+        if (warp == 1) {
+            if (rank == 0 && elect_one()) mma_commit<2>(&drained);  // (arrives in both blocks)
             __syncwarp();
             mbar_wait_cluster(&drained, 0);
         }

@@ -8,8 +8,9 @@
 // copies run at the memory's rate, and some 20 us go to the masks, the list, the first loads and the last scores. From 4 bits: 279 MB
 // in 85 to 92 us, one row of 151936 x 2560 in 65. Boxes of 128-byte pieces of 128 rows come at 5.1 to 5.7 TB/s (measured alone), 850
 // cycles for 128 tokens x 256 weights, turning those into f16 takes 550 (the loop alone); from 17 rows on the hidden states, which
-// every block brings past again for each tile, are as many bytes as the weights (16 rows: 76 us, 32: 85, 64: 122, of which the sums in portions are 11). One row of 32000 x
-// 2048: 20 us, of which the loads need 6; what is left is latency (masks 4, list 3, first loads 2, scores and results 3, two launches).
+// every block brings past again for each tile, are as many bytes as the weights (16 rows: 76 us, 32: 85, 64: 122, of which the sums in
+// portions are 11). One row of 32000 x 2048: 20 us, of which the loads need 6; what is left is latency (masks 4, list 3, first loads 2,
+// scores and results 3, two launches).
 #pragma once
 
 #include <cuda.h>
@@ -495,7 +496,8 @@ __device__ __forceinline__ void step_scores(const HeadStepArgs& a, StepShared& s
 
 // 4-bit weights in tensor memory are f16, relative to the largest scale of their row, which becomes 2^13: e2m1 numbers times 2^13 (6 of
 // them are below f16's largest number) down to 2^-23 are exact in f16, and of a weight whose scale is below that 6 * 2^-38 of the largest
-// scale is lost at most. One conversion and one product for two weights; going to bf16 by shifts, masks and products takes 23 instructions for eight (32 rows of 128256 x 4096: 163 us, 130).
+// scale is lost at most. One conversion and one product for two weights; going to bf16 by shifts, masks and products takes 23
+// instructions for eight (32 rows of 128256 x 4096: 163 us, 130).
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
@@ -956,7 +958,8 @@ __global__ void __launch_bounds__((MX ? kStepWarpsMx : kStepWarps) * 32, 1)
                 for (int t = 0; t < T; ++t) {
                     const int at = g * per_group + t * 128 + quad * 32;
                     if (t < l.tiles && at < n)
-                        step_scores<MX>(a, sh, quad, MX ? mx_scale(largest) * (1.f / (1 << kMxTop)) : 1.f, sh.list + at, n - at, all, sums_of(t, true), bits[t], state, lane);
+                        step_scores<MX>(a, sh, quad, MX ? mx_scale(largest) * (1.f / (1 << kMxTop)) : 1.f, sh.list + at, n - at, all,
+                                        sums_of(t, true), bits[t], state, lane);
                 }
                 release();
             }
