@@ -302,7 +302,7 @@ int cfgzip_head_dequantize(cfgzip_ctx* ctx, const cfgzip_head* head, void* value
  * cfgzip_masked_logsoftmax_argmax from hidden states: the scores of the tokens that some row of the batch allows are computed
  * and reduced without being stored. Weights of other tokens are not read, unless nearly all are allowed (15/16 of them, 3/4 for a
  * 4-bit head) or the batch has more than 128 rows; they have no part in the results in any case, whatever they are. Scores are
- * within about 1e-6 of their largest partial sums, of rows of any length in batches of any size. Weights of a 4-bit head whose scale is
+ * within about 2e-6 of their largest partial sums, of rows of any length in batches of any size. Weights of a 4-bit head whose scale is
  * more than 2^36 times below the largest scale of their row (which counts whatever is in its block) may be off by 6 * 2^-38 of that.
  *   part0, row_part, class_mask : as there; the partitions' V is that of the head (CFGZIP_E_RANGE otherwise)
  *   hidden     : dev bf16 [B, hidden_stride]
