@@ -6,10 +6,9 @@
 //
 // 32 rows of 128256 x 4096 (bf16, 97 % allowed by some row): 1.05 GB in 173 to 179 us with the masks, 5.9 TB/s; inside the loop the
 // copies run at the memory's rate, and some 20 us go to the masks, the list, the first loads and the last scores. From 4 bits: 279 MB
-// in 85 to 92 us, one row of 151936 x 2560 in 65. Boxes of 128-byte pieces of 128 rows come at 5.1 to 5.7 TB/s (measured alone), 850
+// in 84 to 92 us, one row of 151936 x 2560 in 65. Boxes of 128-byte pieces of 128 rows come at 5.1 to 5.7 TB/s (measured alone), 850
 // cycles for 128 tokens x 256 weights, turning those into f16 takes 550 (the loop alone); from 17 rows on the hidden states, which
-// every block brings past again for each tile, are as many bytes as the weights (16 rows: 76 us, 32: 85, 64: 122, of which the sums in
-// portions are 11). One row of 32000 x 2048: 20 us, of which the loads need 6; what is left is latency (masks 4, list 3, first loads 2,
+// every block brings past again for each tile, are as many bytes as the weights (16 rows: 76 us, 32: 84, 64: 113). One row of 32000 x 2048: 20 us, of which the loads need 6; what is left is latency (masks 4, list 3, first loads 2,
 // scores and results 3, two launches).
 #pragma once
 
@@ -553,10 +552,12 @@ constexpr int kStepTiles = MX ? 1 : 2;  // tiles that share a stage at most
 //
 // The products' sums in tensor memory are cut off towards zero at every addition (measured: -1e-9 of the score per element of the
 // row, 4e-6 for 4096, ten times what sums that are rounded come to), so that a row's k is cut in `cuts` pieces with sums of their own,
-// as many as there is room for, which are added up, and rounded, when they are read. Pieces of more than kStepCut elements are not
-// taken: a longer row comes in portions of that many pieces, one portion's sums being read while the next one's are made (scores of positive
-// products from 4096 to 65536 elements: off by 1.7e-6, 2.2e-6 at most; from 4 bits by 1.5e-7, 7e-7 at most).
-constexpr int kStepCut = 1024;
+// as many as there is room for, which are added up, and rounded, when they are read. Pieces of more than 1024 elements are not
+// taken: a longer row comes in portions of that many pieces, one portion's sums being read while the next one's are made (scores of
+// positive products from 4096 to 65536 elements: off by 1.7e-6, 2.2e-6 at most). From 4 bits, whose products have ten bits and lose
+// less, 2048 (off by 5e-7, 9e-7 at most; pieces of 1024 leave 1.5e-7, but 64 rows of 128256 x 4096 then take 122 us instead of 113).
+template <bool MX>
+constexpr int kStepCut = MX ? 2048 / 256 : 1024 / 64;  // atoms
 struct StepLayout {
     int tiles, rows, atoms, steps, stages, cuts, cut_atoms;
     int portions, portion_steps, last_cuts;
@@ -565,7 +566,7 @@ struct StepLayout {
 template <bool MX>
 __device__ __forceinline__ StepLayout step_layout(const HeadStepArgs& a, int most) {
     constexpr int X = MX ? 4 : 1;  // atoms of hidden states to an atom of weights
-    constexpr int kColumns = MX ? 128 : 512, kCut = kStepCut / (MX ? 256 : 64);
+    constexpr int kColumns = MX ? 128 : 512, kCut = kStepCut<MX>;
     StepLayout l;
     l.tiles = most > 128 && a.N <= 32 ? kStepTiles<MX> : 1;
     l.rows = most > 128 ? 128 * l.tiles : (max(most, 1) + 31) & ~31;
