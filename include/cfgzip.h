@@ -355,6 +355,49 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
                               int64_t d_weight_stride, int accumulate, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
+ * ---- Scoring: log probabilities of tokens that are given (an answer, a sampled token, a draft), the entropy of the distribution that
+ * they come from, and the most probable alternatives; and the gradient that training a policy on them needs. Section 2.2 defines the
+ * distribution: the scores of the tokens that the grammar allows, the others at -inf.
+ *
+ * With zt = z * inv_temperature over the tokens that row n allows:
+ *   lse[n] = log sum exp(zt),   logp[n] = zt[tokens[n]] - lse[n],   entropy[n] = -sum p log p with p = exp(zt - lse[n])
+ *   logits     : dev [N, row_stride_elems] of `dtype` (CFGZIP_F32 or CFGZIP_BF16), row_stride_elems >= V, rows may start at any element;
+ *                read only, and not scaled by 1/T. V at most 2^21, N at most 2^30 (CFGZIP_E_RANGE)
+ *   vocab_mask : NULL (everything is allowed: logits that a step has masked in place too) or dev uint32 [N, vocab_stride_words], as
+ *                cfgzip_expand_mask writes them. Logits that are not allowed may be anything, NaN among it; vectors of eight tokens of
+ *                which none is allowed are not read
+ *   tokens     : dev int32 [N], NULL where logp is. logp of a negative one is 0, of one that is not allowed or whose logit is -inf it is
+ *                -inf; of one at V or above too, and it counts as a bad token
+ *   inv_temperature : above 0, at most 1e6
+ *   n_top      : 0 to 32; the n_top tokens with the largest logits of those allowed, largest first, equal ones (-0.0 == +0.0) by token
+ *                id, lowest first. Where fewer have a probability the rest is token -1 with log probability -inf
+ *   logp, entropy, lse : dev float [N], each nullable. A row with nothing allowed: lse -inf, entropy 0, logp -inf (0 where no token is given)
+ *   top_tokens, top_logp : dev int32 and float [N, n_top] (not looked at where n_top is 0)
+ * Allowed logits below -1e29 count as -inf; +inf and NaN among them are outside the contract. Statistics are held in 32 bits. The results
+ * are the same from call to call.
+ */
+int cfgzip_token_logprobs(cfgzip_ctx* ctx, const void* logits, int dtype, int64_t row_stride_elems, int32_t N, int32_t V,
+                          const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* tokens, float inv_temperature,
+                          int32_t n_top, float* logp, float* entropy, float* lse, int32_t* top_tokens, float* top_logp, void* stream);
+
+/*
+ * Its gradient with respect to the logits, for gradients d_logp and d_entropy of the two results:
+ *   d_logits[n, t] = inv_temperature * (d_logp[n] * ([t = tokens[n]] - p) - d_entropy[n] * p * (log p + entropy[n]))
+ * over the allowed tokens, and 0 for the others. d_logp has no part in rows whose logp is 0 or -inf as said above (no token given, one
+ * that is not allowed); a row with nothing allowed is all 0. At the given token 1 - p is taken without its difference to 1, so that a
+ * token the model is sure of keeps its gradient.
+ *   logits .. inv_temperature : as given to cfgzip_token_logprobs
+ *   lse, entropy : dev float [N], as it returned them (entropy NULL where d_entropy is)
+ *   d_logp, d_entropy : dev float [N], one of them nullable
+ *   d_logits   : dev [N, d_stride_elems] of `dtype`, d_stride_elems >= V; elements at V and above of a row are not touched. May be
+ *                `logits` itself with the same stride; must not overlap it otherwise
+ */
+int cfgzip_token_logprobs_backward(cfgzip_ctx* ctx, const void* logits, int dtype, int64_t row_stride_elems, int32_t N, int32_t V,
+                                   const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* tokens, float inv_temperature,
+                                   const float* lse, const float* entropy, const float* d_logp, const float* d_entropy, void* d_logits,
+                                   int64_t d_stride_elems, void* stream);
+
+/*
  * Host-only choice between CFGZIP_DENSE and CFGZIP_SPARSE for a batch whose class masks are still in host memory,
  * which is where the grammar engine leaves them (Section 3.1, "Inference": the engine produces the mask over the
  * classes; Section 4 runs it on the CPU). Adds up the sizes of the classes every row allows and returns

@@ -54,6 +54,9 @@ _SIGNATURES = {
     "cfgzip_head_loss": (_int, [_vp, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp]),
     "cfgzip_head_loss_backward": (_int, [_vp, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _int, _i64, _int,
                                          _vp, _i64, _vp]),
+    "cfgzip_token_logprobs": (_int, [_vp, _vp, _int, _i64, _i32, _i32, _vp, _i64, _vp, ctypes.c_float, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "cfgzip_token_logprobs_backward": (_int, [_vp, _vp, _int, _i64, _i32, _i32, _vp, _i64, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, _vp,
+                                              _i64, _vp]),
     "cfgzip_choose_mode": (_int, [_vp, _i32, _vp, _vp, _i64, _i32, _int]),
     "cfgzip_decode_step_host": (_int, [_vp, _i32, _vp, _vp, _i64, _vp, _int, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _int,
                                        _vp]),
@@ -198,6 +201,10 @@ _STEP_CALLS = {
     "cfgzip_head_loss_backward": ("pppiipippppipiiipis", 18, "ctx head hidden hidden_stride N vocab_mask vocab_stride_words targets "
                                   "lse d_loss d_hidden d_hidden_stride d_weight d_weight_dtype d_weight_stride accumulate workspace "
                                   "workspace_bytes stream"),
+    "cfgzip_token_logprobs": ("ppiiiipipfippppps", 11, "ctx logits dtype row_stride_elems N V vocab_mask vocab_stride_words tokens "
+                              "inv_temperature n_top logp entropy lse top_tokens top_logp stream"),
+    "cfgzip_token_logprobs_backward": ("ppiiiipipfpppppis", 16, "ctx logits dtype row_stride_elems N V vocab_mask vocab_stride_words "
+                                       "tokens inv_temperature lse entropy d_logp d_entropy d_logits d_stride_elems stream"),
 }
 
 

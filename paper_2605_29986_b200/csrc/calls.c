@@ -132,7 +132,7 @@ static PyObject* done(const Call* c, int status) {
 }
 
 enum { EXPAND_MASK, MASK_LOGITS, FUSED, SAMPLE, SAMPLE_FILTERED, MULTI_MASK, PLAN_ROWS, MAP_TOKENS, STEP_HOST,
-       HEAD_QUANTIZE, HEAD_DEQUANTIZE, HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD, N_CALLS };
+       HEAD_QUANTIZE, HEAD_DEQUANTIZE, HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD, LOGPROBS, LOGPROBS_BACKWARD, N_CALLS };
 
 #define STEP_ARGS                                                                                                     \
     "ctx", "part0", "row_part", "class_mask", "class_stride_words", "logits", "dtype", "row_stride_elems", "B", "vocab_mask", \
@@ -171,6 +171,12 @@ static Call calls[N_CALLS] = {
      {"ctx", "head", "hidden", "hidden_stride", "N", "vocab_mask", "vocab_stride_words", "targets", "lse", "d_loss", "d_hidden",
       "d_hidden_stride", "d_weight", "d_weight_dtype", "d_weight_stride", "accumulate", "workspace", "workspace_bytes", "stream"},
      NULL},
+    {"cfgzip_token_logprobs", "ppiiiipipfippppps", 11,
+     {"ctx", "logits", "dtype", "row_stride_elems", "N", "V", "vocab_mask", "vocab_stride_words", "tokens", "inv_temperature", "n_top",
+      "logp", "entropy", "lse", "top_tokens", "top_logp", "stream"}, NULL},
+    {"cfgzip_token_logprobs_backward", "ppiiiipipfpppppis", 16,
+     {"ctx", "logits", "dtype", "row_stride_elems", "N", "V", "vocab_mask", "vocab_stride_words", "tokens", "inv_temperature", "lse",
+      "entropy", "d_logp", "d_entropy", "d_logits", "d_stride_elems", "stream"}, NULL},
 };
 
 #define I(k) ((int32_t)v[k].i)
@@ -254,6 +260,16 @@ static PyObject* py_cfgzip_head_loss_backward(PyObject* self, PyObject* const* a
          P(12), I(13), L(14), I(15), P(16), L(17), P(18));
 }
 
+static PyObject* py_cfgzip_token_logprobs(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    CALL(LOGPROBS, cfgzip_token_logprobs, CTX, P(1), I(2), L(3), I(4), I(5), P(6), L(7), P(8), F(9), I(10), P(11), P(12), P(13), P(14),
+         P(15), P(16));
+}
+
+static PyObject* py_cfgzip_token_logprobs_backward(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    CALL(LOGPROBS_BACKWARD, cfgzip_token_logprobs_backward, CTX, P(1), I(2), L(3), I(4), I(5), P(6), L(7), P(8), F(9), P(10), P(11),
+         P(12), P(13), P(14), L(15), P(16));
+}
+
 /* bind(addresses by name, raise): where the functions are, and what to call with (status, call) when one fails */
 static PyObject* py_bind(PyObject* self, PyObject* args) {
     PyObject *addresses, *raise;
@@ -290,6 +306,8 @@ static PyMethodDef methods[] = {
     METHOD(cfgzip_head_step),
     METHOD(cfgzip_head_loss),
     METHOD(cfgzip_head_loss_backward),
+    METHOD(cfgzip_token_logprobs),
+    METHOD(cfgzip_token_logprobs_backward),
     {"bind", py_bind, METH_VARARGS, NULL},
     {NULL, NULL, 0, NULL},
 };

@@ -153,7 +153,7 @@ int launch(cfgzip_ctx* ctx, void (*kernel)(KArgs...), dim3 grid, dim3 block, siz
 // microsecond of host time. large_clusters: the kernel also comes in clusters of more than eight blocks.
 template <typename K>
 int ensure_smem(cfgzip_ctx* ctx, K kernel, size_t bytes, bool large_clusters = false) {
-    if (bytes <= 48 * 1024) return CFGZIP_OK;
+    if (bytes <= 48 * 1024 && !large_clusters) return CFGZIP_OK;
     const void* fn = reinterpret_cast<const void*>(kernel);
     for (const auto& k : ctx->smem_allowed)
         if (k.first == fn) return bytes <= k.second ? CFGZIP_OK : CFGZIP_E_CUDA;
