@@ -282,7 +282,13 @@ typedef struct cfgzip_head {
 /* Device memory that a call of the given kind wants in `workspace` for up to `rows` rows. The caller owns it; it holds nothing
  * from one call to the next, and calls that can overlap on the GPU (graphs replayed side by side too) need one each. Calls with
  * less give CFGZIP_E_NOMEM. Host only, touches no GPU. */
-enum { CFGZIP_HEAD_STEP = 0, CFGZIP_HEAD_LOSS = 1, CFGZIP_HEAD_LOSS_BACKWARD = 2 };
+enum {
+    CFGZIP_HEAD_STEP = 0,
+    CFGZIP_HEAD_LOSS = 1,
+    CFGZIP_HEAD_LOSS_BACKWARD = 2,
+    CFGZIP_HEAD_LOGPROBS = 4, /* (3 is none) */
+    CFGZIP_HEAD_LOGPROBS_BACKWARD = 5
+};
 int cfgzip_head_workspace(const cfgzip_head* head, int op, int32_t rows, int64_t* bytes);
 
 /*
@@ -396,6 +402,35 @@ int cfgzip_token_logprobs_backward(cfgzip_ctx* ctx, const void* logits, int dtyp
                                    const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* tokens, float inv_temperature,
                                    const float* lse, const float* entropy, const float* d_logp, const float* d_entropy, void* d_logits,
                                    int64_t d_stride_elems, void* stream);
+
+/*
+ * The same from hidden states: cfgzip_token_logprobs without the logits (in pieces of the vocabulary, as cfgzip_head_loss does), without a
+ * temperature and without alternatives.
+ *   head, hidden, vocab_mask, workspace : as in cfgzip_head_loss (the workspace of CFGZIP_HEAD_LOGPROBS)
+ *   tokens             : dev int32 [N], logp : dev float [N]; logp as there: 0 for a negative token, -inf for one that is not allowed, for
+ *                        one at V or above too, which counts as a bad token
+ *   entropy, lse       : nullable dev float [N], as there
+ * Scores are as exact as those of cfgzip_head_loss. Allowed scores below -1e29 count as -inf.
+ */
+int cfgzip_head_logprobs(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N,
+                         const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* tokens, float* logp, float* entropy,
+                         float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Its gradient. With g[n, t] = d_logp[n] * ([t = tokens[n]] - p) - d_entropy[n] * p * (log p + entropy[n]) over the allowed tokens (d_logp
+ * has no part in rows whose logp is not a finite function of z, a row with nothing allowed has none):
+ *   d_hidden[n, :] = sum_t g[n, t] * weight[t, :],    d_weight[t, :] = sum_n g[n, t] * hidden[n, :]
+ * The scores are computed again, the same to the last bit, and g is rounded to bf16, as in cfgzip_head_loss_backward; what is said there of
+ * accuracy, and of weights and hidden states that have to be finite where g is 0, holds here.
+ *   lse, entropy       : as cfgzip_head_logprobs returned them (entropy NULL where d_entropy is)
+ *   d_logp, d_entropy  : dev float [N], one of them nullable (tokens too where d_logp is)
+ *   the others         : as in cfgzip_head_loss_backward (the workspace of CFGZIP_HEAD_LOGPROBS_BACKWARD)
+ */
+int cfgzip_head_logprobs_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N,
+                                  const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* tokens, const float* lse,
+                                  const float* entropy, const float* d_logp, const float* d_entropy, void* d_hidden,
+                                  int64_t d_hidden_stride, void* d_weight, int d_weight_dtype, int64_t d_weight_stride, int accumulate,
+                                  void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
  * Host-only choice between CFGZIP_DENSE and CFGZIP_SPARSE for a batch whose class masks are still in host memory,

@@ -20,7 +20,7 @@ except ImportError:  # it could not be built here: the same functions through ct
 
 F32, BF16, MXFP4 = 0, 1, 2  # (MXFP4: heads only)
 AUTO, DENSE, SPARSE = 0, 1, 2
-HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD = 0, 1, 2
+HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD, HEAD_LOGPROBS, HEAD_LOGPROBS_BACKWARD = 0, 1, 2, 4, 5
 OK, E_ARG, E_RANGE, E_PARTITION, E_ALIGN, E_CUDA, E_NOMEM = 0, -1, -2, -3, -4, -5, -6
 
 _vp, _i32, _i64, _int = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_int
@@ -57,6 +57,9 @@ _SIGNATURES = {
     "cfgzip_token_logprobs": (_int, [_vp, _vp, _int, _i64, _i32, _i32, _vp, _i64, _vp, ctypes.c_float, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
     "cfgzip_token_logprobs_backward": (_int, [_vp, _vp, _int, _i64, _i32, _i32, _vp, _i64, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, _vp,
                                               _i64, _vp]),
+    "cfgzip_head_logprobs": (_int, [_vp, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "cfgzip_head_logprobs_backward": (_int, [_vp, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _int, _i64,
+                                             _int, _vp, _i64, _vp]),
     "cfgzip_choose_mode": (_int, [_vp, _i32, _vp, _vp, _i64, _i32, _int]),
     "cfgzip_decode_step_host": (_int, [_vp, _i32, _vp, _vp, _i64, _vp, _int, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _int,
                                        _vp]),
@@ -205,6 +208,11 @@ _STEP_CALLS = {
                               "inv_temperature n_top logp entropy lse top_tokens top_logp stream"),
     "cfgzip_token_logprobs_backward": ("ppiiiipipfpppppis", 16, "ctx logits dtype row_stride_elems N V vocab_mask vocab_stride_words "
                                        "tokens inv_temperature lse entropy d_logp d_entropy d_logits d_stride_elems stream"),
+    "cfgzip_head_logprobs": ("pppiipipppppis", 13, "ctx head hidden hidden_stride N vocab_mask vocab_stride_words tokens logp entropy "
+                             "lse workspace workspace_bytes stream"),
+    "cfgzip_head_logprobs_backward": ("pppiipippppppipiiipis", 20, "ctx head hidden hidden_stride N vocab_mask vocab_stride_words tokens "
+                                      "lse entropy d_logp d_entropy d_hidden d_hidden_stride d_weight d_weight_dtype d_weight_stride "
+                                      "accumulate workspace workspace_bytes stream"),
 }
 
 
@@ -257,7 +265,7 @@ class cfgzip_head(ctypes.Structure):
 
 
 def cfgzip_head_workspace(head: cfgzip_head, op: int, rows: int) -> int:
-    """Bytes of device memory a call of kind `op` (HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD) wants for up to `rows` rows."""
+    """Bytes of device memory a call of kind `op` (HEAD_STEP, HEAD_LOSS, ...) wants for up to `rows` rows."""
     out = _i64(0)
     _check(load_library().cfgzip_head_workspace(_ptr(head), op, rows, ctypes.byref(out)), "cfgzip_head_workspace")
     return out.value

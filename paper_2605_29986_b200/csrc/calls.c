@@ -132,7 +132,8 @@ static PyObject* done(const Call* c, int status) {
 }
 
 enum { EXPAND_MASK, MASK_LOGITS, FUSED, SAMPLE, SAMPLE_FILTERED, MULTI_MASK, PLAN_ROWS, MAP_TOKENS, STEP_HOST,
-       HEAD_QUANTIZE, HEAD_DEQUANTIZE, HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD, LOGPROBS, LOGPROBS_BACKWARD, N_CALLS };
+       HEAD_QUANTIZE, HEAD_DEQUANTIZE, HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD, LOGPROBS, LOGPROBS_BACKWARD, HEAD_LOGPROBS,
+       HEAD_LOGPROBS_BACKWARD, N_CALLS };
 
 #define STEP_ARGS                                                                                                     \
     "ctx", "part0", "row_part", "class_mask", "class_stride_words", "logits", "dtype", "row_stride_elems", "B", "vocab_mask", \
@@ -177,6 +178,13 @@ static Call calls[N_CALLS] = {
     {"cfgzip_token_logprobs_backward", "ppiiiipipfpppppis", 16,
      {"ctx", "logits", "dtype", "row_stride_elems", "N", "V", "vocab_mask", "vocab_stride_words", "tokens", "inv_temperature", "lse",
       "entropy", "d_logp", "d_entropy", "d_logits", "d_stride_elems", "stream"}, NULL},
+    {"cfgzip_head_logprobs", "pppiipipppppis", 13,
+     {"ctx", "head", "hidden", "hidden_stride", "N", "vocab_mask", "vocab_stride_words", "tokens", "logp", "entropy", "lse", "workspace",
+      "workspace_bytes", "stream"}, NULL},
+    {"cfgzip_head_logprobs_backward", "pppiipippppppipiiipis", 20,
+     {"ctx", "head", "hidden", "hidden_stride", "N", "vocab_mask", "vocab_stride_words", "tokens", "lse", "entropy", "d_logp", "d_entropy",
+      "d_hidden", "d_hidden_stride", "d_weight", "d_weight_dtype", "d_weight_stride", "accumulate", "workspace", "workspace_bytes",
+      "stream"}, NULL},
 };
 
 #define I(k) ((int32_t)v[k].i)
@@ -270,6 +278,15 @@ static PyObject* py_cfgzip_token_logprobs_backward(PyObject* self, PyObject* con
          P(12), P(13), P(14), L(15), P(16));
 }
 
+static PyObject* py_cfgzip_head_logprobs(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    CALL(HEAD_LOGPROBS, cfgzip_head_logprobs, CTX, HEAD(1), P(2), L(3), I(4), P(5), L(6), P(7), P(8), P(9), P(10), P(11), L(12), P(13));
+}
+
+static PyObject* py_cfgzip_head_logprobs_backward(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    CALL(HEAD_LOGPROBS_BACKWARD, cfgzip_head_logprobs_backward, CTX, HEAD(1), P(2), L(3), I(4), P(5), L(6), P(7), P(8), P(9), P(10),
+         P(11), P(12), L(13), P(14), I(15), L(16), I(17), P(18), L(19), P(20));
+}
+
 /* bind(addresses by name, raise): where the functions are, and what to call with (status, call) when one fails */
 static PyObject* py_bind(PyObject* self, PyObject* args) {
     PyObject *addresses, *raise;
@@ -308,6 +325,8 @@ static PyMethodDef methods[] = {
     METHOD(cfgzip_head_loss_backward),
     METHOD(cfgzip_token_logprobs),
     METHOD(cfgzip_token_logprobs_backward),
+    METHOD(cfgzip_head_logprobs),
+    METHOD(cfgzip_head_logprobs_backward),
     {"bind", py_bind, METH_VARARGS, NULL},
     {NULL, NULL, 0, NULL},
 };

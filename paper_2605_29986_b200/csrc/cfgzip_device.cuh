@@ -19,6 +19,10 @@ constexpr float kRefFloor = -1.7e38f; // lowest reference used for exp(z - ref)
 // logit, and one such run of fill values (-1e10, -1e30) in a lane made the sum of its whole row NaN.
 constexpr float kRefLow = -2147483648.f;
 
+// Where the sum of exponentials comes with one of exp(d) d: logits below kFew count as -inf, and masked ones take the value kNone, so far
+// below any reference that its exponential is 0, but finite (0 times infinity would be in the second sum).
+constexpr float kNone = -1e30f, kFew = -1e29f;
+
 enum : int { kF32 = 0, kBF16 = 1 };
 
 // One loaded partition, as the kernels see it (all pointers are device memory).

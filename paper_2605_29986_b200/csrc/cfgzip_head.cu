@@ -9,6 +9,7 @@
 #include "cfgzip_head_mma.cuh"
 #include "cfgzip_head_step.cuh"
 #include "context.h"
+#include "products.h"
 
 using namespace cfgzip;
 
@@ -16,8 +17,6 @@ namespace {
 
 constexpr int kHeadMost = 65536;      // longest row of a head
 constexpr int kHeadTokens = 1 << 30;  // most rows of a head, and of a batch
-
-bool on16(const void* p, int64_t stride_bytes) { return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(stride_bytes)) & 15u) == 0; }
 
 int check_head_shape(const cfgzip_head* h) {
     if (!h || h->V <= 0 || h->H <= 0 || (h->dtype != CFGZIP_BF16 && h->dtype != CFGZIP_MXFP4) || h->reserved) return CFGZIP_E_ARG;
@@ -43,22 +42,8 @@ int check_rows(const cfgzip_head* h, const void* p, int64_t stride) {
     return on16(p, stride * 2) ? CFGZIP_OK : CFGZIP_E_ALIGN;
 }
 
-// A workspace taken apart; with no memory behind it, only counted.
-struct Carve {
-    char* at;
-    int64_t used = 0;
-    explicit Carve(void* p) : at(static_cast<char*>(p)) {}
-    template <typename T>
-    T* take(int64_t n) {
-        T* r = at ? reinterpret_cast<T*>(at + used) : nullptr;
-        used += (n * int64_t(sizeof(T)) + 255) / 256 * 256;
-        return r;
-    }
-};
-
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // most of the gradient of the scores that is held at a time
 constexpr int kStepBlocks = 148;                     // blocks of a decode step at most
-constexpr int kPairs = 74;                           // pairs of SMs that plans are made for (a plan is right for any number)
 
 struct HeadSpace {
     // step
@@ -67,8 +52,9 @@ struct HeadSpace {
     uint32_t *mask, *any, *bits, *ticket;
     int32_t* counts;
     Partial* states;
-    // loss
+    // loss, log probabilities
     float2* part;
+    float4* part_entropy;
     float* of_target;
     // gradient
     int32_t piece, splits;  // tokens of a piece, cuts of the sum over them
@@ -76,51 +62,6 @@ struct HeadSpace {
     float* sums;
     int64_t bytes;
 };
-
-int up(int64_t n, int to) { return int((n + to - 1) / to * to); }
-
-// Cuts of a sum over k_blocks stages whose result has `tiles` tiles: more cuts fill the last wave of pairs better, and each is
-// one more f32 result written and read. A stage takes a pair about 0.4 us, a result's bytes 1 / 6.5 us per MB. At most kCutTiles
-// tiles in all where there are cuts.
-constexpr int kCutTiles = 8 * kPairs;
-int cuts(int64_t tiles, int k_blocks, int64_t result_elems) {
-    int best = 1;
-    double least = 0;
-    for (int s = 1; s <= kPairs && s <= std::max(1, k_blocks / 16) && (s == 1 || s * tiles <= kCutTiles); ++s) {
-        const double waves = double((tiles * s + kPairs - 1) / kPairs);
-        const double us = waves * ((k_blocks + s - 1) / s) * 0.4 + s * double(result_elems) * 8e-6 / 6.5;
-        if (s == 1 || us < least) {
-            least = us;
-            best = s;
-        }
-    }
-    return best;
-}
-
-// Columns of the tiles of scores: 256, or fewer where the last round of pairs would have few tiles (77 rows of 32000: 125 tiles of 256
-// take 74 pairs two rounds, and 143 of 224 as well). What a tile costs besides its columns is taken for 32 of them. From 16 rounds on
-// there is nothing to gain.
-constexpr int kNarrowest = 160, kNarrowTiles = 16 * kPairs;
-int tile_width(int64_t rows, int64_t cols) {
-    const int64_t high = (rows + kMmaTile - 1) / kMmaTile;
-    if (high * ((cols + kMmaTile - 1) / kMmaTile) > kNarrowTiles) return kMmaTile;
-    int best = kMmaTile;
-    int64_t least = 0;
-    for (int w = kMmaTile; w >= kNarrowest; w -= 32) {
-        const int64_t tiles = high * ((cols + w - 1) / w), cost = (tiles + kPairs - 1) / kPairs * (w + 32);
-        if (w == kMmaTile || cost < least) {
-            least = cost;
-            best = w;
-        }
-    }
-    return best;
-}
-
-// The most states, one for each half tile of a row's scores, that any batch of up to `rows` rows comes to.
-int64_t most_states(int64_t rows, int64_t cols) {
-    const int64_t wide = (cols + kMmaTile - 1) / kMmaTile, narrow = (cols + kNarrowest - 1) / kNarrowest;
-    return 2 * std::max(rows * wide, std::min<int64_t>(rows, kMmaTile * (kNarrowTiles / wide)) * narrow);
-}
 
 // What is taken for `rows` rows is enough for fewer, whose tiles, pieces and cuts are others.
 HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace) {
@@ -143,6 +84,9 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
     } else if (op == CFGZIP_HEAD_LOSS) {
         s.part = c.take<float2>(most_states(n, h->V));
         s.of_target = c.take<float>(n);
+    } else if (op == CFGZIP_HEAD_LOGPROBS) {
+        s.part_entropy = c.take<float4>(most_states(n, h->V));
+        s.of_target = c.take<float>(n);
     } else {
         const int64_t all = up(h->V, kMmaTile), room = kPieceBytes / 2, across = ceil_div(h->H, kMmaTile);
         s.piece = int32_t(std::min(all, std::max<int64_t>(room / std::max<int64_t>(n, 1) / kMmaTile * kMmaTile, kMmaTile)));
@@ -153,20 +97,6 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
     }
     s.bytes = c.used + 256;
     return s;
-}
-
-// Tiled copies of a matrix of `rows` rows of `cols` bf16 numbers (or bytes), boxes of 128 bytes by `box` rows in the 128-byte swizzle.
-int tensor_map(cfgzip_ctx* ctx, CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t stride, int box, bool bytes = false) {
-    const cuuint64_t dims[2] = {cuuint64_t(cols), cuuint64_t(rows)};
-    const cuuint64_t strides[1] = {cuuint64_t(stride) * (bytes ? 1 : 2)};
-    const cuuint32_t boxes[2] = {bytes ? 128u : 64u, cuuint32_t(box)};
-    const cuuint32_t steps[2] = {1, 1};
-    if (!ctx->encode_tiled ||
-        ctx->encode_tiled(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, boxes, steps,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return CFGZIP_E_CUDA;
-    return CFGZIP_OK;
 }
 
 // Hidden states [rows, stride] (stride a multiple of 256) for tiled copies that bring 256 k of all rows, 64 after 64.
@@ -181,43 +111,6 @@ int tensor_map_by_64(cfgzip_ctx* ctx, CUtensorMap* map, const uint16_t* p, int64
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return CFGZIP_E_CUDA;
     return CFGZIP_OK;
-}
-
-// Results of a product that go out by tiled copies of 128 bytes of 32 rows.
-int tensor_map_out(cfgzip_ctx* ctx, CUtensorMap* map, const MmaArgs& a, bool bf16) {
-    const cuuint64_t es = bf16 ? 2 : 4;
-    const cuuint64_t dims[3] = {cuuint64_t(a.cols), cuuint64_t(a.rows), cuuint64_t(a.splits)};
-    const cuuint64_t strides[2] = {cuuint64_t(a.ld) * es, cuuint64_t(a.splits > 1 ? a.split_elems : a.ld) * es};
-    const cuuint32_t boxes[3] = {cuuint32_t(128 / es), 32, 1};
-    const cuuint32_t steps[3] = {1, 1, 1};
-    if (!ctx->encode_tiled ||
-        ctx->encode_tiled(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, a.out, dims, strides, boxes, steps,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return CFGZIP_E_CUDA;
-    return CFGZIP_OK;
-}
-
-template <bool A_MN, bool B_MN, int KIND, bool LONG = true>
-int run_mma(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUtensorMap& map_b, cudaStream_t st) {
-    constexpr bool kOut = KIND == kMmaSum || KIND == kMmaBf16;
-    a.splits = std::max(1, a.splits);
-    if constexpr (kOut && LONG)
-        if (ceil_div(a.k_blocks, a.splits) <= kMmaOutPortion) return run_mma<A_MN, B_MN, KIND, false>(ctx, a, map_a, map_b, st);
-    if (kOut) a.width = kMmaTile;
-    a.m_tiles = ceil_div(a.rows, kMmaTile);
-    a.n_tiles = ceil_div(a.cols, a.width);
-    a.status = ctx->d_status;
-    a.expire = ctx->expire_test;
-    auto kern = k_head_mma<A_MN, B_MN, KIND, LONG>;
-    const size_t smem = kMmaSmem + (kOut ? 8 * kMmaOut : 0);
-    CUtensorMap map_out = map_a;
-    int rc = kOut ? tensor_map_out(ctx, &map_out, a, KIND == kMmaBf16) : CFGZIP_OK;
-    if (rc != CFGZIP_OK || (rc = ensure_smem(ctx, kern, smem)) != CFGZIP_OK) return rc;
-    const int64_t tiles = int64_t(a.m_tiles) * a.n_tiles * a.splits;
-    if (tiles >= (int64_t(1) << 30)) return CFGZIP_E_RANGE;
-    const unsigned pairs = unsigned(std::min<int64_t>(tiles, ctx->sm_count / 2));
-    return launch(ctx, kern, dim3(2 * pairs), dim3(kMmaThreads), smem, st, a, map_a, map_b, map_out);
 }
 
 // Threads of a launch that takes a head by vectors of 8 weights (mx_at).
@@ -292,12 +185,121 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
     return launch(ctx, kern, dim3(blocks), dim3((mx ? kStepWarpsMx : kStepWarps) * 32), smem, st, a, map_x, map_w, map_box);
 }
 
+// What a gradient is of: of the loss, or of log probabilities and entropies.
+struct GradientOf {
+    const int32_t* targets;
+    const float *lse, *entropy;
+    const float *d_loss, *d_entropy;  // (d_loss: of the log probabilities where `scores` is true)
+    bool scores;
+};
+
+int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N, const uint32_t* vocab_mask,
+                  int64_t vocab_stride_words, const GradientOf& of, void* d_hidden, int64_t d_hidden_stride, void* d_weight,
+                  int d_weight_dtype, int64_t d_weight_stride, int accumulate, void* workspace, int64_t workspace_bytes, void* stream) {
+    int rc = check_head(head);
+    if (rc != CFGZIP_OK) return rc;
+    if (head->dtype != CFGZIP_BF16 || N < 0 || (!d_hidden && !d_weight)) return CFGZIP_E_ARG;
+    if (N > kHeadTokens) return CFGZIP_E_RANGE;
+    if (d_weight) {
+        if ((d_weight_dtype != CFGZIP_F32 && d_weight_dtype != CFGZIP_BF16) || d_weight_stride < head->H) return CFGZIP_E_ARG;
+        if (!on16(d_weight, d_weight_stride * (d_weight_dtype == CFGZIP_BF16 ? 2 : 4))) return CFGZIP_E_ALIGN;
+    }
+    if (d_hidden && (rc = check_rows(head, d_hidden, d_hidden_stride)) != CFGZIP_OK) return rc;
+    if (N > 0) {
+        if (of.scores ? !of.d_loss && !of.d_entropy : !of.d_loss) return CFGZIP_E_ARG;
+        if (!of.lse || (of.d_loss && !of.targets) || (of.d_entropy && !of.entropy) || (vocab_mask && vocab_stride_words < ceil_div(head->V, 32))) return CFGZIP_E_ARG;
+        if ((rc = check_rows(head, hidden, hidden_stride)) != CFGZIP_OK) return rc;
+        if (!workspace) return CFGZIP_E_ARG;
+    }
+    const HeadSpace w = head_space(head, CFGZIP_HEAD_LOSS_BACKWARD, N, workspace);
+    if (N > 0 && workspace_bytes < w.bytes) return CFGZIP_E_NOMEM;
+    if (!ctx) return CFGZIP_E_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return CFGZIP_E_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int H = head->H;
+    if (N == 0) {  // an empty sum
+        if (!d_weight || accumulate) return CFGZIP_OK;
+        const size_t es = d_weight_dtype == CFGZIP_BF16 ? 2 : 4;
+        if (cudaMemset2DAsync(d_weight, size_t(d_weight_stride) * es, 0, size_t(H) * es, size_t(head->V), st) != cudaSuccess) {
+            cudaGetLastError();
+            return CFGZIP_E_CUDA;
+        }
+        return CFGZIP_OK;
+    }
+    CUtensorMap x_k, x_mn, w_k, w_mn, g_k, g_mn;
+    if ((rc = tensor_map(ctx, &x_k, hidden, N, H, hidden_stride, 128)) != CFGZIP_OK ||
+        (rc = tensor_map(ctx, &x_mn, hidden, N, H, hidden_stride, 64)) != CFGZIP_OK)
+        return rc;
+    for (int32_t t0 = 0; t0 < head->V; t0 += w.piece) {
+        const int32_t n = std::min(w.piece, head->V - t0);
+        const uint16_t* weights = static_cast<const uint16_t*>(head->weight) + t0 * head->row_stride;
+        // (columns of the piece behind the vocabulary are outside the maps: they come as zeros)
+        const int width = tile_width(N, n);
+        if ((rc = tensor_map(ctx, &w_k, weights, n, H, head->row_stride, width / 2)) != CFGZIP_OK ||
+            (rc = tensor_map(ctx, &w_mn, weights, n, H, head->row_stride, 64)) != CFGZIP_OK ||
+            (rc = tensor_map(ctx, &g_k, w.g, N, n, w.piece, 128)) != CFGZIP_OK ||
+            (rc = tensor_map(ctx, &g_mn, w.g, N, n, w.piece, 64)) != CFGZIP_OK)
+            return rc;
+        MmaArgs a{};
+        a.width = width;
+        a.rows = N;
+        a.cols = n;
+        a.k_blocks = ceil_div(H, kMmaK);
+        a.m_fast = 1;
+        a.t0 = t0;
+        a.V = head->V;
+        a.mask = vocab_mask;
+        a.mask_stride = vocab_stride_words;
+        a.targets = of.targets;
+        a.lse = of.lse;
+        a.d_loss = of.d_loss;
+        a.entropy = of.entropy;
+        a.d_entropy = of.d_entropy;
+        a.out = w.g;
+        a.ld = w.piece;
+        rc = of.scores ? run_mma<false, false, kMmaGradEntropy>(ctx, a, x_k, w_k, st) : run_mma<false, false, kMmaGrad>(ctx, a, x_k, w_k, st);
+        if (rc != CFGZIP_OK) return rc;
+        if (d_hidden) {
+            MmaArgs b{};
+            b.rows = N;
+            b.cols = H;
+            b.k_blocks = ceil_div(n, kMmaK);
+            b.splits = std::min(w.splits, b.k_blocks);
+            b.out = w.sums;
+            b.ld = H;
+            b.split_elems = int64_t(N) * H;
+            b.add = t0 > 0;
+            if ((rc = run_mma<false, true, kMmaSum>(ctx, b, g_k, w_mn, st)) != CFGZIP_OK) return rc;
+        }
+        if (d_weight) {
+            MmaArgs b{};
+            b.rows = n;
+            b.cols = H;
+            b.k_blocks = ceil_div(N, kMmaK);
+            b.ld = d_weight_stride;
+            b.add = accumulate;
+            const bool half = d_weight_dtype == CFGZIP_BF16;
+            b.out = static_cast<char*>(d_weight) + int64_t(t0) * d_weight_stride * (half ? 2 : 4);
+            rc = half ? run_mma<true, true, kMmaBf16>(ctx, b, g_mn, x_mn, st) : run_mma<true, true, kMmaSum>(ctx, b, g_mn, x_mn, st);
+            if (rc != CFGZIP_OK) return rc;
+        }
+    }
+    if (!d_hidden) return CFGZIP_OK;
+    const int splits = std::min(w.splits, ceil_div(std::min(w.piece, head->V), kMmaK));
+    const int64_t blocks = std::min<int64_t>(ceil_div(int64_t(N) * (H / 4), 256), int64_t(ctx->sm_count) * 8);
+    return launch(ctx, k_head_round, dim3(unsigned(blocks)), dim3(256), 0, st, (const float*)w.sums, int64_t(N) * H, splits,
+                  static_cast<uint16_t*>(d_hidden), d_hidden_stride, int(N), H);
+}
+
 }  // namespace
 
 extern "C" {
 
 int cfgzip_head_workspace(const cfgzip_head* head, int op, int32_t rows, int64_t* bytes) {
-    if (!bytes || rows < 0 || op < CFGZIP_HEAD_STEP || op > CFGZIP_HEAD_LOSS_BACKWARD) return CFGZIP_E_ARG;
+    const bool known = (op >= CFGZIP_HEAD_STEP && op <= CFGZIP_HEAD_LOSS_BACKWARD) || op == CFGZIP_HEAD_LOGPROBS ||
+                       op == CFGZIP_HEAD_LOGPROBS_BACKWARD;
+    if (!bytes || rows < 0 || !known) return CFGZIP_E_ARG;
     const int rc = check_head_shape(head);
     if (rc != CFGZIP_OK) return rc;
     if (op != CFGZIP_HEAD_STEP && head->dtype != CFGZIP_BF16) return CFGZIP_E_ARG;
@@ -496,96 +498,68 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
                               const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* targets, const float* lse,
                               const float* d_loss, void* d_hidden, int64_t d_hidden_stride, void* d_weight, int d_weight_dtype,
                               int64_t d_weight_stride, int accumulate, void* workspace, int64_t workspace_bytes, void* stream) {
+    const GradientOf of{targets, lse, nullptr, d_loss, nullptr, false};
+    return head_gradient(ctx, head, hidden, hidden_stride, N, vocab_mask, vocab_stride_words, of, d_hidden, d_hidden_stride, d_weight,
+                         d_weight_dtype, d_weight_stride, accumulate, workspace, workspace_bytes, stream);
+}
+
+int cfgzip_head_logprobs(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N,
+                         const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* tokens, float* logp, float* entropy,
+                         float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
     int rc = check_head(head);
     if (rc != CFGZIP_OK) return rc;
-    if (head->dtype != CFGZIP_BF16 || N < 0 || (!d_hidden && !d_weight)) return CFGZIP_E_ARG;
+    if (head->dtype != CFGZIP_BF16 || N < 0) return CFGZIP_E_ARG;
     if (N > kHeadTokens) return CFGZIP_E_RANGE;
-    if (d_weight) {
-        if ((d_weight_dtype != CFGZIP_F32 && d_weight_dtype != CFGZIP_BF16) || d_weight_stride < head->H) return CFGZIP_E_ARG;
-        if (!on16(d_weight, d_weight_stride * (d_weight_dtype == CFGZIP_BF16 ? 2 : 4))) return CFGZIP_E_ALIGN;
-    }
-    if (d_hidden && (rc = check_rows(head, d_hidden, d_hidden_stride)) != CFGZIP_OK) return rc;
-    if (N > 0) {
-        if (!targets || !lse || !d_loss || (vocab_mask && vocab_stride_words < ceil_div(head->V, 32))) return CFGZIP_E_ARG;
-        if ((rc = check_rows(head, hidden, hidden_stride)) != CFGZIP_OK) return rc;
-        if (!workspace) return CFGZIP_E_ARG;
-    }
-    const HeadSpace w = head_space(head, CFGZIP_HEAD_LOSS_BACKWARD, N, workspace);
-    if (N > 0 && workspace_bytes < w.bytes) return CFGZIP_E_NOMEM;
+    if (N == 0) return ctx ? CFGZIP_OK : CFGZIP_E_ARG;
+    if (!tokens || !logp || (vocab_mask && vocab_stride_words < ceil_div(head->V, 32))) return CFGZIP_E_ARG;
+    if ((rc = check_rows(head, hidden, hidden_stride)) != CFGZIP_OK) return rc;
+    if (!workspace) return CFGZIP_E_ARG;
+    const HeadSpace w = head_space(head, CFGZIP_HEAD_LOGPROBS, N, workspace);
+    if (workspace_bytes < w.bytes) return CFGZIP_E_NOMEM;
     if (!ctx) return CFGZIP_E_ARG;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int H = head->H;
-    if (N == 0) {  // an empty sum
-        if (!d_weight || accumulate) return CFGZIP_OK;
-        const size_t es = d_weight_dtype == CFGZIP_BF16 ? 2 : 4;
-        if (cudaMemset2DAsync(d_weight, size_t(d_weight_stride) * es, 0, size_t(H) * es, size_t(head->V), st) != cudaSuccess) {
-            cudaGetLastError();
-            return CFGZIP_E_CUDA;
-        }
-        return CFGZIP_OK;
-    }
-    CUtensorMap x_k, x_mn, w_k, w_mn, g_k, g_mn;
-    if ((rc = tensor_map(ctx, &x_k, hidden, N, H, hidden_stride, 128)) != CFGZIP_OK ||
-        (rc = tensor_map(ctx, &x_mn, hidden, N, H, hidden_stride, 64)) != CFGZIP_OK)
+    CUtensorMap map_x, map_w;
+    MmaArgs a{};
+    a.width = tile_width(N, head->V);
+    if ((rc = tensor_map(ctx, &map_x, hidden, N, head->H, hidden_stride, 128)) != CFGZIP_OK ||
+        (rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, a.width / 2)) != CFGZIP_OK)
         return rc;
-    for (int32_t t0 = 0; t0 < head->V; t0 += w.piece) {
-        const int32_t n = std::min(w.piece, head->V - t0);
-        const uint16_t* weights = static_cast<const uint16_t*>(head->weight) + t0 * head->row_stride;
-        // (columns of the piece behind the vocabulary are outside the maps: they come as zeros)
-        const int width = tile_width(N, n);
-        if ((rc = tensor_map(ctx, &w_k, weights, n, H, head->row_stride, width / 2)) != CFGZIP_OK ||
-            (rc = tensor_map(ctx, &w_mn, weights, n, H, head->row_stride, 64)) != CFGZIP_OK ||
-            (rc = tensor_map(ctx, &g_k, w.g, N, n, w.piece, 128)) != CFGZIP_OK ||
-            (rc = tensor_map(ctx, &g_mn, w.g, N, n, w.piece, 64)) != CFGZIP_OK)
-            return rc;
-        MmaArgs a{};
-        a.width = width;
-        a.rows = N;
-        a.cols = n;
-        a.k_blocks = ceil_div(H, kMmaK);
-        a.m_fast = 1;
-        a.t0 = t0;
-        a.V = head->V;
-        a.mask = vocab_mask;
-        a.mask_stride = vocab_stride_words;
-        a.targets = targets;
-        a.lse = lse;
-        a.d_loss = d_loss;
-        a.out = w.g;
-        a.ld = w.piece;
-        if ((rc = run_mma<false, false, kMmaGrad>(ctx, a, x_k, w_k, st)) != CFGZIP_OK) return rc;
-        if (d_hidden) {
-            MmaArgs b{};
-            b.rows = N;
-            b.cols = H;
-            b.k_blocks = ceil_div(n, kMmaK);
-            b.splits = std::min(w.splits, b.k_blocks);
-            b.out = w.sums;
-            b.ld = H;
-            b.split_elems = int64_t(N) * H;
-            b.add = t0 > 0;
-            if ((rc = run_mma<false, true, kMmaSum>(ctx, b, g_k, w_mn, st)) != CFGZIP_OK) return rc;
-        }
-        if (d_weight) {
-            MmaArgs b{};
-            b.rows = n;
-            b.cols = H;
-            b.k_blocks = ceil_div(N, kMmaK);
-            b.ld = d_weight_stride;
-            b.add = accumulate;
-            const bool half = d_weight_dtype == CFGZIP_BF16;
-            b.out = static_cast<char*>(d_weight) + int64_t(t0) * d_weight_stride * (half ? 2 : 4);
-            rc = half ? run_mma<true, true, kMmaBf16>(ctx, b, g_mn, x_mn, st) : run_mma<true, true, kMmaSum>(ctx, b, g_mn, x_mn, st);
-            if (rc != CFGZIP_OK) return rc;
-        }
-    }
-    if (!d_hidden) return CFGZIP_OK;
-    const int splits = std::min(w.splits, ceil_div(std::min(w.piece, head->V), kMmaK));
-    const int64_t blocks = std::min<int64_t>(ceil_div(int64_t(N) * (H / 4), 256), int64_t(ctx->sm_count) * 8);
-    return launch(ctx, k_head_round, dim3(unsigned(blocks)), dim3(256), 0, st, (const float*)w.sums, int64_t(N) * H, splits,
-                  static_cast<uint16_t*>(d_hidden), d_hidden_stride, int(N), H);
+    a.rows = N;
+    a.cols = a.V = head->V;
+    a.k_blocks = ceil_div(head->H, kMmaK);
+    a.m_fast = 1;
+    a.mask = vocab_mask;
+    a.mask_stride = vocab_stride_words;
+    a.targets = tokens;
+    a.sums = w.part_entropy;
+    a.of_target = w.of_target;
+    if ((rc = run_mma<false, false, kMmaLogprobs>(ctx, a, map_x, map_w, st)) != CFGZIP_OK) return rc;
+    LogprobsFinishArgs f{};
+    f.sums = w.part_entropy;
+    f.of_target = w.of_target;
+    f.tiles = 2 * a.n_tiles;
+    f.rows = N;
+    f.V = head->V;
+    f.mask = vocab_mask;
+    f.mask_stride = vocab_stride_words;
+    f.tokens = tokens;
+    f.logp = logp;
+    f.entropy = entropy;
+    f.lse = lse;
+    f.status = ctx->d_status;
+    return launch(ctx, k_head_logprobs_finish, dim3(unsigned(ceil_div(N, kFinishRows))), dim3(256), 0, st, f);
+}
+
+int cfgzip_head_logprobs_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, int64_t hidden_stride, int32_t N,
+                                  const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* tokens, const float* lse,
+                                  const float* entropy, const float* d_logp, const float* d_entropy, void* d_hidden, int64_t d_hidden_stride,
+                                  void* d_weight, int d_weight_dtype, int64_t d_weight_stride, int accumulate, void* workspace,
+                                  int64_t workspace_bytes, void* stream) {
+    const GradientOf of{tokens, lse, entropy, d_logp, d_entropy, true};
+    return head_gradient(ctx, head, hidden, hidden_stride, N, vocab_mask, vocab_stride_words, of, d_hidden, d_hidden_stride, d_weight,
+                         d_weight_dtype, d_weight_stride, accumulate, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -34,7 +34,7 @@ constexpr uint32_t kMmaHalf = 128 * kMmaK * 2;           // bytes of one operand
 constexpr size_t kMmaSmem = size_t(kMmaStages) * 2 * kMmaHalf + 1024;
 constexpr uint32_t kMmaOut = 32 * 128;                   // bytes a warp has on their way out: 32 rows of 128
 
-enum : int { kMmaLoss = 0, kMmaGrad = 1, kMmaSum = 2, kMmaBf16 = 3, kMmaStep = 4 };
+enum : int { kMmaLoss = 0, kMmaGrad = 1, kMmaSum = 2, kMmaBf16 = 3, kMmaStep = 4, kMmaLogprobs = 5, kMmaGradEntropy = 6 };
 
 struct MmaArgs {
     int32_t rows, cols;        // of the result (tokens x piece of the vocabulary, ...)
@@ -50,8 +50,10 @@ struct MmaArgs {
     int32_t t0, V;             // the piece starts at token t0
     const int32_t* targets;
     const float *lse, *d_loss;
+    const float *entropy, *d_entropy;  // gradient of log probabilities (whose gradient is in d_loss, null where it is 0) and entropies
     float2* part;              // loss: [2 n_tiles, rows] largest score and sum of half a tile
-    float* of_target;          // loss: [rows]
+    float4* sums;              // log probabilities: [2 n_tiles, rows] the same with the sum of exp(d) d
+    float* of_target;          // loss, log probabilities: [rows]
     Partial* states;           // step: [2 n_tiles, rows] the same with the token
     // results
     void* out;
@@ -94,9 +96,8 @@ __device__ __forceinline__ void tile_mask(const MmaArgs& a, const MmaTile& tile,
     }
 }
 
-// Largest allowed score and the sum of exponentials, of one row and half a tile's tokens (the first 128 of them, the rest).
-__device__ __forceinline__ void loss_epilogue(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, float (&z)[128],
-                                              const uint32_t (&bits)[4]) {
+// The score of the row's target, where this half tile has it.
+__device__ __forceinline__ void store_of_target(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, const float (&z)[128]) {
     const int n0 = t.n * a.width + 128 * half, mine = min(128, a.width - 128 * half);
     const int asked = valid ? ld_after_wait(a.targets + row) : -1, there = asked < 0 ? -1 : asked - (a.t0 + n0);
     const int target = there < mine ? there : -1;
@@ -105,6 +106,12 @@ __device__ __forceinline__ void loss_epilogue(const MmaArgs& a, const MmaTile& t
         for (int j = 0; j < 128; ++j)
             if (target == j) a.of_target[row] = z[j];
     }
+}
+
+// Largest allowed score and the sum of exponentials, of one row and half a tile's tokens (the first 128 of them, the rest).
+__device__ __forceinline__ void loss_epilogue(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, float (&z)[128],
+                                              const uint32_t (&bits)[4]) {
+    store_of_target(a, t, half, row, valid, z);
     float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
     for (int j = 0; j < 128; ++j) {
@@ -116,6 +123,30 @@ __device__ __forceinline__ void loss_epilogue(const MmaArgs& a, const MmaTile& t
 #pragma unroll
     for (int j = 0; j < 128; ++j) s[j & 3] += ex2f((z[j] - ref) * kLog2e);
     if (valid) a.part[int64_t(2 * t.n + half) * a.rows + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+}
+
+// The same with the sum of exp(d) d, d = z - largest, which the entropy is made of.
+__device__ __forceinline__ void logprobs_epilogue(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, float (&z)[128],
+                                                  const uint32_t (&bits)[4]) {
+    store_of_target(a, t, half, row, valid, z);
+    float m[4] = {kNone, kNone, kNone, kNone};
+#pragma unroll
+    for (int j = 0; j < 128; ++j) {
+        z[j] = (bits[j / 32] >> (j & 31)) & 1u ? z[j] : kNone;
+        m[j & 3] = fmaxf(m[j & 3], z[j]);
+    }
+    const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), ref = fmaxf(top, kFew);
+    float s[4] = {}, d[4] = {};
+#pragma unroll
+    for (int j = 0; j < 128; ++j) {
+        const float x = fmaxf(z[j] - ref, 2.f * kNone), e = ex2f(x * kLog2e);
+        s[j & 3] += e;
+        d[j & 3] = fmaf(e, x, d[j & 3]);
+    }
+    if (valid) {
+        const float s4 = (s[0] + s[1]) + (s[2] + s[3]), d4 = (d[0] + d[1]) + (d[2] + d[3]);
+        *reinterpret_cast<float4*>(&a.sums[int64_t(2 * t.n + half) * a.rows + row]) = make_float4(ref, s4, d4, 0.f);
+    }
 }
 
 // Largest allowed score, its lowest token and the sum of exponentials, of one row and half a tile's tokens.
@@ -145,36 +176,57 @@ __device__ __forceinline__ void step_epilogue(const MmaArgs& a, const MmaTile& t
 // g = d (exp(z - lse) - [target]) of the allowed tokens, as bf16, of one row and half a tile's tokens. A target that the model is sure of
 // has all of its g in the small difference exp(z - lse) - 1: the scores are made as the loss makes them, portion by portion, so that z
 // here is the z in lse to the last bit, and the difference is not taken of a rounded exponential. The only token of a row gets 0.
+// With entropies (d is minus the gradient of the log probability then): g = p (d + b (x + entropy)) with x = z - lse and b minus the gradient
+// of the entropy, on the target d (p - 1) + p b (x + entropy). The entropy has its gradient in rows without a target too.
+template <bool ENTROPY>
 __device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, const float (&z)[128],
                                               const uint32_t (&bits)[4]) {
     const int n0 = t.n * a.width + 128 * half, mine = min(128, a.width - 128 * half);
     int target = -1;
-    float d = 0.f, lse = 0.f;
-    bool has = false;
+    float d = 0.f, lse = 0.f, b = 0.f, entropy = 0.f;
+    bool has = false, any = false;
     if (valid) {
-        target = ld_after_wait(a.targets + row);
+        if (!ENTROPY || a.d_loss) target = ld_after_wait(a.targets + row);
         lse = ld_after_wait(a.lse + row);
         has = target >= 0 && target < a.V && lse > -INFINITY;
         if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (target >> 5)) >> (target & 31)) & 1u;
         if (has) d = ld_after_wait(a.d_loss + row);
         target = has ? target - (a.t0 + n0) : -1;
         if (target >= mine) target = -1;
+        any = has;
+        if (ENTROPY) {
+            d = -d;
+            any = lse > -INFINITY;
+            lse = any ? lse : 0.f;
+            if (a.d_entropy && any) {
+                b = -ld_after_wait(a.d_entropy + row);
+                entropy = ld_after_wait(a.entropy + row);
+            }
+        }
     }
+    const float at_zero = fmaf(b, entropy, d);
     float of_target = 0.f;
     if (__any_sync(0xFFFFFFFFu, target >= 0)) {
 #pragma unroll
         for (int j = 0; j < 128; ++j) of_target = target == j ? z[j] : of_target;
-        of_target = d * expm1f(of_target - lse);
+        const float x = of_target - lse;
+        of_target = d * expm1f(x);
+        if (ENTROPY) of_target = fmaf(ex2f(x * kLog2e) * b, x + entropy, of_target);
     }
     uint16_t* p = static_cast<uint16_t*>(a.out) + int64_t(row) * a.ld + n0;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
         if (16 * c >= mine || n0 + 16 * c >= a.ld) break;
-        const uint32_t w = has ? bits[c / 2] >> (16 * (c & 1)) : 0u;
+        const uint32_t w = any ? bits[c / 2] >> (16 * (c & 1)) : 0u;
         float g[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            g[j] = (w >> j) & 1u ? d * ex2f((z[16 * c + j] - lse) * kLog2e) : 0.f;
+            if (ENTROPY) {
+                const float x = fmaxf(z[16 * c + j] - lse, -200.f);
+                g[j] = (w >> j) & 1u ? ex2f(x * kLog2e) * fmaf(b, x, at_zero) : 0.f;
+            } else {
+                g[j] = (w >> j) & 1u ? d * ex2f((z[16 * c + j] - lse) * kLog2e) : 0.f;
+            }
             g[j] = target == 16 * c + j ? of_target : g[j];
         }
         uint32_t o[8];
@@ -374,7 +426,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             }
             if (ok && KIND == kMmaLoss) loss_epilogue(a, t, half, row, valid, sums, bits);
             if (ok && KIND == kMmaStep) step_epilogue(a, t, half, row, valid, sums, bits);
-            if (ok && KIND == kMmaGrad) grad_epilogue(a, t, half, row, valid, sums, bits);
+            if (ok && KIND == kMmaLogprobs) logprobs_epilogue(a, t, half, row, valid, sums, bits);
+            if (ok && KIND == kMmaGrad) grad_epilogue<false>(a, t, half, row, valid, sums, bits);
+            if (ok && KIND == kMmaGradEntropy) grad_epilogue<true>(a, t, half, row, valid, sums, bits);
             if (ok && kOut && row - lane < a.rows) {
                 const bool add = a.add && valid;
                 constexpr int kCols = kOutCols<KIND == kMmaBf16>;
@@ -467,7 +521,7 @@ struct FinishArgs {
     float *loss, *lse;
     int32_t* status;
 };
-__global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
+static __global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * kFinishRows + (lane & 3);
     float m = -INFINITY, s = 0.f;
@@ -522,9 +576,82 @@ __global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
     a.loss[row] = loss;
 }
 
+// The same for log probabilities and entropies. A state's reference is its largest score, kFew where it has none.
+struct LogprobsFinishArgs {
+    const float4* sums;
+    const float* of_target;
+    int32_t tiles, rows, V;
+    const uint32_t* mask;
+    int64_t mask_stride;
+    const int32_t* tokens;
+    float *logp, *entropy, *lse;
+    int32_t* status;
+};
+static __global__ void __launch_bounds__(256) k_head_logprobs_finish(const LogprobsFinishArgs a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * kFinishRows + (lane & 3);
+    const bool ends = warp == 0 && lane < kFinishRows && row < a.rows;
+    const int token = ends ? ld_after_wait(a.tokens + row) : -1;
+    const float of_token = ends ? ld_after_wait(a.of_target + row) : 0.f;
+    float m = kFew, s = 0.f, d = 0.f;
+    if (row < a.rows)
+        for (int t = warp * 8 + (lane >> 2); t < a.tiles; t += 320) {
+            float4 p[5];
+#pragma unroll
+            for (int k = 0; k < 5; ++k)
+                p[k] = t + 64 * k < a.tiles ? __ldcg(a.sums + int64_t(t + 64 * k) * a.rows + row) : make_float4(kFew, 0.f, 0.f, 0.f);
+            float next = m;
+#pragma unroll
+            for (int k = 0; k < 5; ++k) next = fmaxf(next, p[k].x);
+            const float by = m - next, e = ex2f(by * kLog2e);
+            d = fmaf(by, s, d) * e;
+            s *= e;
+#pragma unroll
+            for (int k = 0; k < 5; ++k) {
+                const float of = p[k].x - next, f = ex2f(of * kLog2e);
+                d = fmaf(fmaf(of, p[k].y, p[k].z), f, d);
+                s = fmaf(p[k].y, f, s);
+            }
+            m = next;
+        }
+    bool has = token >= 0 && token < a.V;
+    if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (token >> 5)) >> (token & 31)) & 1u;
+    __shared__ float4 sh[64][kFinishRows];
+    sh[warp * 8 + (lane >> 2)][lane & 3] = make_float4(m, s, d, 0.f);
+    __syncthreads();
+    if (warp) return;
+    // eight threads a row, eight states each
+    float top = kFew;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[8 * (lane >> 2) + w][lane & 3].x);
+#pragma unroll
+    for (int k = 4; k <= 16; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, k));
+    s = d = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+        const float4 p = sh[8 * (lane >> 2) + w][lane & 3];
+        const float of = p.x - top, f = ex2f(of * kLog2e);
+        d = fmaf(fmaf(of, p.y, p.z), f, d);
+        s = fmaf(p.y, f, s);
+    }
+#pragma unroll
+    for (int k = 4; k <= 16; k <<= 1) {
+        s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
+        d += __shfl_xor_sync(0xFFFFFFFFu, d, k);
+    }
+    if (!ends) return;
+    const float log_sum = logf(s);
+    if (a.lse) a.lse[row] = s > 0.f ? top + log_sum : -INFINITY;
+    if (a.entropy) a.entropy[row] = s > 0.f ? fmaxf(log_sum - d / s, 0.f) : 0.f;
+    if (token >= a.V) atomicAdd(a.status + 1, 1);
+    float logp = 0.f;
+    if (token >= 0) logp = has && of_token > kFew ? (of_token - top) - log_sum : -INFINITY;
+    a.logp[row] = logp;
+}
+
 // The sums of `splits` cuts, added up and rounded; four to a thread, n a multiple of 8. (Few rows have many cuts: what takes time is
 // how many loads a thread waits for, one after the other. 500 x 256 from 37 cuts: 18 us with eight to a thread, four at a time.)
-__global__ void __launch_bounds__(256) k_head_round(const float* from, int64_t split_elems, int splits, uint16_t* to, int64_t to_stride,
+static __global__ void __launch_bounds__(256) k_head_round(const float* from, int64_t split_elems, int splits, uint16_t* to, int64_t to_stride,
                                                     int rows, int n) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int vectors = n / 4;

@@ -10,9 +10,6 @@
 
 namespace cfgzip {
 
-// Logits below kFew count as -inf. Masked ones take the value kNone, so far below any reference that its exponential is 0, but finite: a
-// sum of exp(d) d would have 0 times infinity in it.
-constexpr float kNone = -1e30f, kFew = -1e29f;
 constexpr int kLogprobsThreads = 256;
 constexpr int kLogprobsChunk = 256;      // tokens whose largest logit is kept together: eight to a lane
 constexpr int kLogprobsTopMost = 32;     // alternatives at most
