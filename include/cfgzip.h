@@ -433,6 +433,63 @@ int cfgzip_head_logprobs_backward(cfgzip_ctx* ctx, const cfgzip_head* head, cons
                                   void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
+ * ---- The layer in front of a head: a matrix product with bias, activation and residual, which drafts hidden states for a token further
+ * ahead (the head's calls then choose, score or train that token under the grammar), and its gradient.
+ *
+ *   y[r, :] = residual[r, :] + act(x[r, :] W^T + bias)
+ *
+ * The weights are bf16 [out, in], rows row_stride apart; the bias is nullable, CFGZIP_F32 or CFGZIP_BF16 [out]. in and out are multiples
+ * of 8, at most 65536 (CFGZIP_E_RANGE, as for more than 2^24 rows of a batch). Weights, bias and the rows of x, residual, y, slope and the
+ * gradients start on 16 bytes (CFGZIP_E_ALIGN otherwise). The struct only describes memory that is the caller's.
+ * Activations: none, max(h, 0), h Phi(h) with the normal distribution's Phi, the same by way of tanh (0.5 h (1 + tanh(sqrt(2 / pi) (h +
+ * 0.044715 h^3)))), h / (1 + exp(-h)). Products are summed and activations computed in 32 bits, and y is rounded once.
+ */
+enum { CFGZIP_ACT_NONE = 0, CFGZIP_ACT_RELU = 1, CFGZIP_ACT_GELU = 2, CFGZIP_ACT_GELU_TANH = 3, CFGZIP_ACT_SILU = 4 };
+typedef struct cfgzip_layer {
+    const void* weight; /* dev bf16 [out, row_stride] */
+    const void* bias;   /* nullable dev [out] */
+    int64_t row_stride; /* elements */
+    int32_t in, out;
+    int32_t activation;
+    int32_t bias_dtype; /* CFGZIP_F32 or CFGZIP_BF16 */
+} cfgzip_layer;
+
+/* Device memory that a call wants in `workspace` for up to `rows` rows, as cfgzip_head_workspace says it for a head. It may be 0, and
+ * `workspace` NULL then. Host only, touches no GPU. */
+enum { CFGZIP_LAYER_FORWARD = 0, CFGZIP_LAYER_BACKWARD = 1 };
+int cfgzip_layer_workspace(const cfgzip_layer* layer, int op, int32_t rows, int64_t* bytes);
+
+/*
+ *   x        : dev bf16 [rows, x_stride]
+ *   residual : nullable dev bf16 [rows, residual_stride]; may be x (where in = out)
+ *   y        : dev bf16 [rows, y_stride] (written); may be the residual with the same stride unless that is x; overlaps nothing else
+ *   slope    : nullable dev bf16 [rows, slope_stride] (written): the activation's derivative, which is what the gradient needs of the
+ *              forward pass (rounded to bf16, 2^-9 of itself: the gradient's own factor is rounded no finer)
+ */
+int cfgzip_layer_forward(cfgzip_ctx* ctx, const cfgzip_layer* layer, const void* x, int64_t x_stride, int32_t rows, const void* residual,
+                         int64_t residual_stride, void* y, int64_t y_stride, void* slope, int64_t slope_stride, void* workspace,
+                         int64_t workspace_bytes, void* stream);
+
+/*
+ * With g = d_y * slope, rounded to bf16 as a factor of the two products (d_bias is of what was not rounded):
+ *   d_x = g W + add,    d_weight = g^T x,    d_bias = the sum of g over the rows
+ *   layer    : as given to the forward pass (its bias is not looked at)
+ *   x        : as given there (NULL where d_weight is)
+ *   slope    : as cfgzip_layer_forward wrote it (not looked at without an activation)
+ *   d_y      : dev bf16 [rows, d_y_stride]; it is the residual's gradient too
+ *   add      : nullable dev bf16 [rows, add_stride] of `in` columns, added in 32 bits: d_y where the residual was x. It may be d_x with the
+ *              same stride
+ *   d_x      : nullable dev bf16 [rows, d_x_stride] (written); overlaps no input but add
+ *   d_weight : nullable dev [out, d_weight_stride] of d_weight_dtype (CFGZIP_BF16 or CFGZIP_F32); d_bias : nullable dev float [out].
+ *              Both are written, or added to where accumulate is not 0
+ * The results do not depend on timing (no atomic additions).
+ */
+int cfgzip_layer_backward(cfgzip_ctx* ctx, const cfgzip_layer* layer, const void* x, int64_t x_stride, int32_t rows, const void* slope,
+                          int64_t slope_stride, const void* d_y, int64_t d_y_stride, const void* add, int64_t add_stride, void* d_x,
+                          int64_t d_x_stride, void* d_weight, int d_weight_dtype, int64_t d_weight_stride, float* d_bias, int accumulate,
+                          void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
  * Host-only choice between CFGZIP_DENSE and CFGZIP_SPARSE for a batch whose class masks are still in host memory,
  * which is where the grammar engine leaves them (Section 3.1, "Inference": the engine produces the mask over the
  * classes; Section 4 runs it on the CPU). Adds up the sizes of the classes every row allows and returns

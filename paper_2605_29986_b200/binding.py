@@ -20,6 +20,8 @@ except ImportError:  # it could not be built here: the same functions through ct
 
 F32, BF16, MXFP4 = 0, 1, 2  # (MXFP4: heads only)
 AUTO, DENSE, SPARSE = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
+LAYER_FORWARD, LAYER_BACKWARD = 0, 1
 HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD, HEAD_LOGPROBS, HEAD_LOGPROBS_BACKWARD = 0, 1, 2, 4, 5
 OK, E_ARG, E_RANGE, E_PARTITION, E_ALIGN, E_CUDA, E_NOMEM = 0, -1, -2, -3, -4, -5, -6
 
@@ -60,6 +62,10 @@ _SIGNATURES = {
     "cfgzip_head_logprobs": (_int, [_vp, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
     "cfgzip_head_logprobs_backward": (_int, [_vp, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _int, _i64,
                                              _int, _vp, _i64, _vp]),
+    "cfgzip_layer_workspace": (_int, [_vp, _int, _i32, ctypes.POINTER(_i64)]),
+    "cfgzip_layer_forward": (_int, [_vp, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "cfgzip_layer_backward": (_int, [_vp, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _int, _i64, _vp, _int,
+                                     _vp, _i64, _vp]),
     "cfgzip_choose_mode": (_int, [_vp, _i32, _vp, _vp, _i64, _i32, _int]),
     "cfgzip_decode_step_host": (_int, [_vp, _i32, _vp, _vp, _i64, _vp, _int, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _int,
                                        _vp]),
@@ -213,6 +219,10 @@ _STEP_CALLS = {
     "cfgzip_head_logprobs_backward": ("pppiipippppppipiiipis", 20, "ctx head hidden hidden_stride N vocab_mask vocab_stride_words tokens "
                                       "lse entropy d_logp d_entropy d_hidden d_hidden_stride d_weight d_weight_dtype d_weight_stride "
                                       "accumulate workspace workspace_bytes stream"),
+    "cfgzip_layer_forward": ("pppiipipipipis", 13, "ctx layer x x_stride rows residual residual_stride y y_stride slope slope_stride "
+                             "workspace workspace_bytes stream"),
+    "cfgzip_layer_backward": ("pppiipipipipipiipipis", 20, "ctx layer x x_stride rows slope slope_stride d_y d_y_stride add add_stride "
+                              "d_x d_x_stride d_weight d_weight_dtype d_weight_stride d_bias accumulate workspace workspace_bytes stream"),
 }
 
 
@@ -268,6 +278,29 @@ def cfgzip_head_workspace(head: cfgzip_head, op: int, rows: int) -> int:
     """Bytes of device memory a call of kind `op` (HEAD_STEP, HEAD_LOSS, ...) wants for up to `rows` rows."""
     out = _i64(0)
     _check(load_library().cfgzip_head_workspace(_ptr(head), op, rows, ctypes.byref(out)), "cfgzip_head_workspace")
+    return out.value
+
+
+class cfgzip_layer(ctypes.Structure):
+    """Description of a layer: bf16 weights [out, in] on the device, an activation, a bias.
+
+    The buffers stay the caller's; this keeps a reference to those it was made from."""
+    _fields_ = [("weight", _vp), ("bias", _vp), ("row_stride", _i64), ("in_", _i32), ("out", _i32), ("activation", _i32),
+                ("bias_dtype", _i32)]
+
+    def __init__(self, weight, in_: int, out: int, activation: int = ACT_NONE, bias=None, bias_dtype: int = F32,
+                 row_stride: Optional[int] = None):
+        super().__init__(_ptr(weight), _ptr(bias), in_ if row_stride is None else row_stride, in_, out, activation, bias_dtype)
+        self.buffers = (weight, bias)
+
+    def data_ptr(self) -> int:
+        return ctypes.addressof(self)
+
+
+def cfgzip_layer_workspace(layer: cfgzip_layer, op: int, rows: int) -> int:
+    """Bytes of device memory a call of kind `op` (LAYER_FORWARD, LAYER_BACKWARD) wants for up to `rows` rows."""
+    out = _i64(0)
+    _check(load_library().cfgzip_layer_workspace(_ptr(layer), op, rows, ctypes.byref(out)), "cfgzip_layer_workspace")
     return out.value
 
 

@@ -133,7 +133,7 @@ static PyObject* done(const Call* c, int status) {
 
 enum { EXPAND_MASK, MASK_LOGITS, FUSED, SAMPLE, SAMPLE_FILTERED, MULTI_MASK, PLAN_ROWS, MAP_TOKENS, STEP_HOST,
        HEAD_QUANTIZE, HEAD_DEQUANTIZE, HEAD_STEP, HEAD_LOSS, HEAD_LOSS_BACKWARD, LOGPROBS, LOGPROBS_BACKWARD, HEAD_LOGPROBS,
-       HEAD_LOGPROBS_BACKWARD, N_CALLS };
+       HEAD_LOGPROBS_BACKWARD, LAYER_FORWARD, LAYER_BACKWARD, N_CALLS };
 
 #define STEP_ARGS                                                                                                     \
     "ctx", "part0", "row_part", "class_mask", "class_stride_words", "logits", "dtype", "row_stride_elems", "B", "vocab_mask", \
@@ -185,6 +185,12 @@ static Call calls[N_CALLS] = {
      {"ctx", "head", "hidden", "hidden_stride", "N", "vocab_mask", "vocab_stride_words", "tokens", "lse", "entropy", "d_logp", "d_entropy",
       "d_hidden", "d_hidden_stride", "d_weight", "d_weight_dtype", "d_weight_stride", "accumulate", "workspace", "workspace_bytes",
       "stream"}, NULL},
+    {"cfgzip_layer_forward", "pppiipipipipis", 13,
+     {"ctx", "layer", "x", "x_stride", "rows", "residual", "residual_stride", "y", "y_stride", "slope", "slope_stride", "workspace",
+      "workspace_bytes", "stream"}, NULL},
+    {"cfgzip_layer_backward", "pppiipipipipipiipipis", 20,
+     {"ctx", "layer", "x", "x_stride", "rows", "slope", "slope_stride", "d_y", "d_y_stride", "add", "add_stride", "d_x", "d_x_stride",
+      "d_weight", "d_weight_dtype", "d_weight_stride", "d_bias", "accumulate", "workspace", "workspace_bytes", "stream"}, NULL},
 };
 
 #define I(k) ((int32_t)v[k].i)
@@ -287,6 +293,17 @@ static PyObject* py_cfgzip_head_logprobs_backward(PyObject* self, PyObject* cons
          P(11), P(12), L(13), P(14), I(15), L(16), I(17), P(18), L(19), P(20));
 }
 
+#define LAYER(k) ((const cfgzip_layer*)v[k].p)
+
+static PyObject* py_cfgzip_layer_forward(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    CALL(LAYER_FORWARD, cfgzip_layer_forward, CTX, LAYER(1), P(2), L(3), I(4), P(5), L(6), P(7), L(8), P(9), L(10), P(11), L(12), P(13));
+}
+
+static PyObject* py_cfgzip_layer_backward(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+    CALL(LAYER_BACKWARD, cfgzip_layer_backward, CTX, LAYER(1), P(2), L(3), I(4), P(5), L(6), P(7), L(8), P(9), L(10), P(11), L(12), P(13),
+         I(14), L(15), P(16), I(17), P(18), L(19), P(20));
+}
+
 /* bind(addresses by name, raise): where the functions are, and what to call with (status, call) when one fails */
 static PyObject* py_bind(PyObject* self, PyObject* args) {
     PyObject *addresses, *raise;
@@ -327,6 +344,8 @@ static PyMethodDef methods[] = {
     METHOD(cfgzip_token_logprobs_backward),
     METHOD(cfgzip_head_logprobs),
     METHOD(cfgzip_head_logprobs_backward),
+    METHOD(cfgzip_layer_forward),
+    METHOD(cfgzip_layer_backward),
     {"bind", py_bind, METH_VARARGS, NULL},
     {NULL, NULL, 0, NULL},
 };

@@ -1,0 +1,59 @@
+// Activations with their derivatives, and the biases in front of them.
+#pragma once
+
+#include "cfgzip_device.cuh"
+
+namespace cfgzip {
+
+enum : int { kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4 };
+
+// The activation and its derivative. Logistic functions are 1 / (1 + exp), which is 0 or 1 where the exponential leaves the numbers; the
+// polynomials are taken of arguments within 64, behind which nothing changes any more.
+template <int ACT>
+__device__ __forceinline__ float activation(float h, float* slope) {
+    if (ACT == kActRelu) {
+        *slope = h > 0.f ? 1.f : 0.f;
+        return fmaxf(h, 0.f);
+    }
+    if (ACT == kActGelu) {
+        const float phi = normcdff(h), c = fminf(fmaxf(h, -64.f), 64.f);
+        *slope = fmaf(c, 0.3989422804f * ex2f(c * c * (-0.5f * kLog2e)), phi);
+        return h * phi;
+    }
+    if (ACT == kActGeluTanh) {  // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u)), u = k (h + 0.044715 h^3), k = sqrt(2 / pi)
+        const float c = fminf(fmaxf(h, -64.f), 64.f), two_k = 1.5957691216f;
+        const float q = __fdividef(1.f, 1.f + ex2f(-kLog2e * two_k * c * fmaf(0.044715f, c * c, 1.f)));
+        *slope = fmaf(c * q * (1.f - q), two_k * fmaf(3.f * 0.044715f, c * c, 1.f), q);
+        return h * q;
+    }
+    if (ACT == kActSilu) {
+        const float q = 1.f / (1.f + ex2f(-kLog2e * h));
+        *slope = q * fmaf(h, 1.f - q, 1.f);
+        return h * q;
+    }
+    *slope = 1.f;
+    return h;
+}
+
+__device__ __forceinline__ void bf16_values(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f[2 * j] = __uint_as_float(w[j] << 16);
+        f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+    }
+}
+// Eight biases from feature n on (n and their number a multiple of 8).
+__device__ __forceinline__ void bias_values(const void* bias, bool bf16, int n, float (&f)[8]) {
+    if (bf16) {
+        bf16_values(ld_after_wait(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(bias) + n)), f);
+    } else {
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(bias) + n);
+        const uint4 a = ld_after_wait(p), b = ld_after_wait(p + 1);
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(w[j]);
+    }
+}
+
+}  // namespace cfgzip

@@ -293,6 +293,12 @@ __device__ __forceinline__ float redux_max(float v, uint32_t members = 0xFFFFFFF
     return m;
 }
 
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {  // nearest, ties to even
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
 // Packed pairs of floats (sm_100 has two-wide fp32 multiply-add and add).
 __device__ __forceinline__ unsigned long long pack2(float lo, float hi) {
     unsigned long long p;
@@ -305,6 +311,11 @@ __device__ __forceinline__ void unpack2(unsigned long long p, float& lo, float& 
 __device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
     unsigned long long d;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
 __device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {

@@ -6,8 +6,10 @@
 #include <cstdint>
 
 #include "cfgzip.h"
+#include "cfgzip_head_finish.cuh"
 #include "cfgzip_head_mma.cuh"
 #include "cfgzip_head_step.cuh"
+#include "cfgzip_mx.cuh"
 #include "context.h"
 #include "products.h"
 

@@ -1,0 +1,167 @@
+// Last steps of the head's tall products: partial states to results, cuts of a sum to bf16.
+#pragma once
+
+#include "cfgzip_device.cuh"
+
+namespace cfgzip {
+
+// Partial states of a row's tiles to its results: four rows by a block, a thread takes every 64th tile of one, five at a time.
+constexpr int kFinishRows = 4;
+struct FinishArgs {
+    const float2* part;
+    const float* of_target;
+    int32_t tiles, rows, V;
+    const uint32_t* mask;
+    int64_t mask_stride;
+    const int32_t* targets;
+    float *loss, *lse;
+    int32_t* status;
+};
+__global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * kFinishRows + (lane & 3);
+    float m = -INFINITY, s = 0.f;
+    // (what the end needs is asked for before the states: the target's score is there or is not looked at)
+    const bool ends = warp == 0 && lane < kFinishRows && row < a.rows;
+    const int target = ends ? ld_after_wait(a.targets + row) : -1;
+    const float of_target = ends ? ld_after_wait(a.of_target + row) : 0.f;
+    if (row < a.rows)
+        for (int t = warp * 8 + (lane >> 2); t < a.tiles; t += 320) {
+            float2 p[5];
+#pragma unroll
+            for (int k = 0; k < 5; ++k)
+                p[k] = t + 64 * k < a.tiles ? __ldcg(a.part + int64_t(t + 64 * k) * a.rows + row) : make_float2(-INFINITY, 0.f);
+            float next = m;
+#pragma unroll
+            for (int k = 0; k < 5; ++k) next = fmaxf(next, p[k].x);
+            const float ref = fmaxf(next, kRefFloor);
+            s *= ex2f((fmaxf(m, kRefFloor) - ref) * kLog2e);
+#pragma unroll
+            for (int k = 0; k < 5; ++k) s += p[k].y * ex2f((fmaxf(p[k].x, kRefFloor) - ref) * kLog2e);
+            m = next;
+        }
+    bool has = target >= 0 && target < a.V;
+    if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (target >> 5)) >> (target & 31)) & 1u;
+    __shared__ float2 sh[64][kFinishRows];
+    sh[warp * 8 + (lane >> 2)][lane & 3] = make_float2(m, s);
+    __syncthreads();
+    if (warp) return;
+    // eight threads a row, eight states each
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[8 * (lane >> 2) + w][lane & 3].x);
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+    const float ref = fmaxf(top, kRefFloor);
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+        const float2 p = sh[8 * (lane >> 2) + w][lane & 3];
+        s += p.y * ex2f((fmaxf(p.x, kRefFloor) - ref) * kLog2e);
+    }
+    s += __shfl_xor_sync(0xFFFFFFFFu, s, 4);
+    s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);
+    s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
+    if (!ends) return;
+    const float log_sum = logf(s);
+    if (a.lse) a.lse[row] = s > 0.f ? top + log_sum : -INFINITY;
+    if (target >= a.V) atomicAdd(a.status + 1, 1);
+    float loss = 0.f;
+    if (target >= 0) loss = has && of_target > -INFINITY ? (top - of_target) + log_sum : INFINITY;
+    a.loss[row] = loss;
+}
+
+// The same for log probabilities and entropies. A state's reference is its largest score, kFew where it has none.
+struct LogprobsFinishArgs {
+    const float4* sums;
+    const float* of_target;
+    int32_t tiles, rows, V;
+    const uint32_t* mask;
+    int64_t mask_stride;
+    const int32_t* tokens;
+    float *logp, *entropy, *lse;
+    int32_t* status;
+};
+__global__ void __launch_bounds__(256) k_head_logprobs_finish(const LogprobsFinishArgs a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * kFinishRows + (lane & 3);
+    const bool ends = warp == 0 && lane < kFinishRows && row < a.rows;
+    const int token = ends ? ld_after_wait(a.tokens + row) : -1;
+    const float of_token = ends ? ld_after_wait(a.of_target + row) : 0.f;
+    float m = kFew, s = 0.f, d = 0.f;
+    if (row < a.rows)
+        for (int t = warp * 8 + (lane >> 2); t < a.tiles; t += 320) {
+            float4 p[5];
+#pragma unroll
+            for (int k = 0; k < 5; ++k)
+                p[k] = t + 64 * k < a.tiles ? __ldcg(a.sums + int64_t(t + 64 * k) * a.rows + row) : make_float4(kFew, 0.f, 0.f, 0.f);
+            float next = m;
+#pragma unroll
+            for (int k = 0; k < 5; ++k) next = fmaxf(next, p[k].x);
+            const float by = m - next, e = ex2f(by * kLog2e);
+            d = fmaf(by, s, d) * e;
+            s *= e;
+#pragma unroll
+            for (int k = 0; k < 5; ++k) {
+                const float of = p[k].x - next, f = ex2f(of * kLog2e);
+                d = fmaf(fmaf(of, p[k].y, p[k].z), f, d);
+                s = fmaf(p[k].y, f, s);
+            }
+            m = next;
+        }
+    bool has = token >= 0 && token < a.V;
+    if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (token >> 5)) >> (token & 31)) & 1u;
+    __shared__ float4 sh[64][kFinishRows];
+    sh[warp * 8 + (lane >> 2)][lane & 3] = make_float4(m, s, d, 0.f);
+    __syncthreads();
+    if (warp) return;
+    // eight threads a row, eight states each
+    float top = kFew;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[8 * (lane >> 2) + w][lane & 3].x);
+#pragma unroll
+    for (int k = 4; k <= 16; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, k));
+    s = d = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+        const float4 p = sh[8 * (lane >> 2) + w][lane & 3];
+        const float of = p.x - top, f = ex2f(of * kLog2e);
+        d = fmaf(fmaf(of, p.y, p.z), f, d);
+        s = fmaf(p.y, f, s);
+    }
+#pragma unroll
+    for (int k = 4; k <= 16; k <<= 1) {
+        s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
+        d += __shfl_xor_sync(0xFFFFFFFFu, d, k);
+    }
+    if (!ends) return;
+    const float log_sum = logf(s);
+    if (a.lse) a.lse[row] = s > 0.f ? top + log_sum : -INFINITY;
+    if (a.entropy) a.entropy[row] = s > 0.f ? fmaxf(log_sum - d / s, 0.f) : 0.f;
+    if (token >= a.V) atomicAdd(a.status + 1, 1);
+    float logp = 0.f;
+    if (token >= 0) logp = has && of_token > kFew ? (of_token - top) - log_sum : -INFINITY;
+    a.logp[row] = logp;
+}
+
+// The sums of `splits` cuts, added up and rounded; four to a thread, n a multiple of 8. (Few rows have many cuts: what takes time is
+// how many loads a thread waits for, one after the other. 500 x 256 from 37 cuts: 18 us with eight to a thread, four at a time.)
+__global__ void __launch_bounds__(256) k_head_round(const float* from, int64_t split_elems, int splits, uint16_t* to, int64_t to_stride,
+                                                    int rows, int n) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int vectors = n / 4;
+    const int64_t total = int64_t(rows) * vectors;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
+        float f[4] = {};
+#pragma unroll 8
+        for (int s = 0; s < splits; ++s) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(from + s * split_elems + 4 * i));
+            f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
+        }
+        const int64_t row = i / vectors;
+        *reinterpret_cast<uint2*>(to + row * to_stride + 4 * (i - row * vectors)) = make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]));
+    }
+}
+
+}  // namespace cfgzip

@@ -7,18 +7,12 @@
 
 #include <cuda.h>
 
+#include "cfgzip_activation.cuh"
 #include "cfgzip_mma.cuh"
-#include "cfgzip_mx.cuh"
 
 namespace cfgzip {
 
 __device__ __forceinline__ float bf16_f32(uint16_t v) { return __uint_as_float(uint32_t(v) << 16); }
-__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {  // nearest, ties to even
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
 constexpr int kMmaThreads = 384;   // a warp for the copies, one for the products, two idle, two sets of four that read the sums
 constexpr int kMmaStages = 6;
 constexpr int kMmaTile = 256;      // rows and columns of a pair's tile
@@ -30,11 +24,13 @@ constexpr int kMmaPortion = 8;
 // ... and the sums over tokens of the gradient, which may be over a whole text or vocabulary (in one go 65536 tokens lose 3e-4 of a sum of
 // positive terms, 200003 lose 1.3e-3; in portions of 2048 under 8e-6. 4000 tokens of 8000 x 2048: 108 us for d_weight, in one go 104).
 constexpr int kMmaOutPortion = 32;
+constexpr int kLayerStagesTall = 5;                      // of the layer's products, whose results need twice the room on their way out
 constexpr uint32_t kMmaHalf = 128 * kMmaK * 2;           // bytes of one operand of a stage in one block
 constexpr size_t kMmaSmem = size_t(kMmaStages) * 2 * kMmaHalf + 1024;
 constexpr uint32_t kMmaOut = 32 * 128;                   // bytes a warp has on their way out: 32 rows of 128
 
-enum : int { kMmaLoss = 0, kMmaGrad = 1, kMmaSum = 2, kMmaBf16 = 3, kMmaStep = 4, kMmaLogprobs = 5, kMmaGradEntropy = 6 };
+enum : int { kMmaLoss = 0, kMmaGrad = 1, kMmaSum = 2, kMmaBf16 = 3, kMmaStep = 4, kMmaLogprobs = 5, kMmaGradEntropy = 6,
+             kMmaLayer = 8 };  // (kMmaLayer and the activation)
 
 struct MmaArgs {
     int32_t rows, cols;        // of the result (tokens x piece of the vocabulary, ...)
@@ -60,6 +56,9 @@ struct MmaArgs {
     int64_t ld;                // elements
     int64_t split_elems;
     int32_t add;
+    // layer
+    const void* bias;
+    int32_t bias_bf16, has_residual, has_slope;
 };
 
 __device__ __forceinline__ void st_global32(void* p, const uint32_t (&v)[8]) {
@@ -279,6 +278,67 @@ __device__ __forceinline__ void out_columns(const MmaArgs& a, const CUtensorMap&
     if (lane == 0) tma_store3(&map, n, first, t.split, buffer);
 }
 
+// A layer's results, 64 columns of a warp's 32 rows at a time, straight from tensor memory. The residual comes by a tiled copy into the
+// buffer that y leaves from (a lane's own 16 bytes), the activation's derivative has a buffer of its own. The bias, the same for all
+// lanes, comes from the L1.
+template <int ACT>
+__device__ __forceinline__ bool layer_columns(const MmaArgs& a, const CUtensorMap& map_y, const CUtensorMap& map_residual,
+                                              const CUtensorMap& map_slope, int n, int first, int lane, uint32_t tmem, uint32_t buffer,
+                                              uint64_t* bar, uint32_t* phase) {
+    bool ok = true;
+    if (lane == 0) {
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (the copies before have read the buffers)
+        if (a.has_residual) {
+            mbar_expect_tx(bar, kMmaOut);
+            asm volatile(
+                "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(buffer),
+                "l"(&map_residual), "r"(n), "r"(first), "r"(smem_u32(bar))
+                : "memory");
+        }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t v[32];
+        tmem_ld32(tmem + 32 * h, v);
+        tmem_wait_ld();
+        if (h == 0 && a.has_residual) {
+            ok = ring_wait(bar, *phase) || (mbar_wait(bar, *phase) && false);
+            *phase ^= 1;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float f[8], s[8], bias[8] = {};
+            if (a.bias && n + 32 * h + 8 * j < a.cols) bias_values(a.bias, a.bias_bf16, n + 32 * h + 8 * j, bias);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = activation<ACT>(__uint_as_float(v[8 * j + k]) + bias[k], &s[k]);
+            const uint32_t at = buffer + uint32_t(lane) * 128 + (uint32_t((4 * h + j) ^ (lane & 7)) << 4);
+            if (a.has_residual) {
+                uint4 r;
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(at) : "memory");
+                float of[8];
+                bf16_values(r, of);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) f[k] += of[k];
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(bf16_pair(f[0], f[1])), "r"(bf16_pair(f[2], f[3])),
+                         "r"(bf16_pair(f[4], f[5])), "r"(bf16_pair(f[6], f[7]))
+                         : "memory");
+            if (ACT != kActNone && a.has_slope)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + kMmaOut), "r"(bf16_pair(s[0], s[1])),
+                             "r"(bf16_pair(s[2], s[3])), "r"(bf16_pair(s[4], s[5])), "r"(bf16_pair(s[6], s[7]))
+                             : "memory");
+        }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        tma_store3(&map_y, n, first, 0, buffer);
+        if (ACT != kActNone && a.has_slope) tma_store3(&map_slope, n, first, 0, buffer + kMmaOut);
+    }
+    return ok;
+}
+
 // D[rows, cols] = A B^T in tiles of 256 x width by pairs of blocks (each holds 128 rows of A and half of B's, and the sums of its 128
 // rows), persistent. Operands K-major (k contiguous) or MN-major, from tensor maps with boxes of 64 x 128 (x width / 2) or 64 x 64;
 // an MN-major B and results that go out by tiled copies have a width of 256.
@@ -286,24 +346,29 @@ __device__ __forceinline__ void out_columns(const MmaArgs& a, const CUtensorMap&
 // Sums are read portion by portion by both sets of warps, a half of the columns each, and added up in registers. Where no tile's sum
 // has more than one portion (LONG false), and what takes the time is the results' way out, the sets take tiles in turn instead, straight
 // from tensor memory (100 tokens of 50021 x 1024: 26 us for d_weight against 38).
+//
+// A layer's sums stay in tensor memory to their end: their results are bf16, and what is cut off (1e-9 of a sum per element of k) is far
+// below that.
 template <bool A_MN, bool B_MN, int KIND, bool LONG>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
-    k_head_mma(const __grid_constant__ MmaArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-               const __grid_constant__ CUtensorMap map_out) {
+__device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_out,
+                                             const CUtensorMap& map_residual, const CUtensorMap& map_slope) {
+    constexpr bool kLayer = KIND >= kMmaLayer;
+    constexpr int kStages = kLayer ? kLayerStagesTall : kMmaStages;
     extern __shared__ char smem_raw[];
-    __shared__ __align__(8) uint64_t full[kMmaStages], empty[kMmaStages], sums_full[2], sums_empty[2];
+    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2];
+    __shared__ __align__(8) uint64_t residual_full[kLayer ? 8 : 1];
     __shared__ __align__(8) uint64_t drained;
     __shared__ uint32_t s_tmem, s_end[2];  // (of either block: the stages it has asked for, and in the highest bit whether a wait ran out)
     constexpr bool kOut = KIND == kMmaSum || KIND == kMmaBf16;
-    constexpr int kPortion = kOut ? kMmaOutPortion : kMmaPortion;
+    constexpr int kPortion = kLayer ? 1 << 30 : kOut ? kMmaOutPortion : kMmaPortion;
     constexpr bool kTurns = !LONG;
-    static_assert(kOut || LONG, "scores are summed in portions");
+    static_assert(kOut || kLayer || LONG, "scores are summed in portions");
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const int tiles = a.m_tiles * a.n_tiles * a.splits, pairs = gridDim.x / 2, pair = blockIdx.x / 2;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kMmaStages; ++i) {
+        for (int i = 0; i < kStages; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
         }
@@ -312,6 +377,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             mbar_init(&sums_empty[i], kTurns ? 8 : 16);  // four warps of either block (all eight)
         }
         mbar_init(&drained, 1);
+        if (kLayer)
+            for (int i = 0; i < 8; ++i) mbar_init(&residual_full[i], 1);
         mbar_init_fence();
         prefetch_tensor_map(&map_a);
         prefetch_tensor_map(&map_b);
@@ -331,7 +398,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
             for (int i = pair; i < tiles && ok; i += pairs) {
                 const MmaTile t = mma_tile(a, i);
                 const int m = t.m * kMmaTile + int(rank) * 128, n = t.n * a.width + int(rank) * (a.width / 2);
-                const int k1 = a.expire ? min(t.k1, t.k0 + kMmaStages) : t.k1;
+                const int k1 = a.expire ? min(t.k1, t.k0 + kStages) : t.k1;
                 for (int k = t.k0; k < k1; ++k) {
                     if (!ring_wait<true>(&empty[r.stage], r.phase ^ 1)) {
                         ok = false;
@@ -352,7 +419,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                         tma_load_pair(at + kMmaHalf, &map_b, k * kMmaK, n, bar);
                     }
                     ++asked;
-                    r.next<kMmaStages>();
+                    r.next<kStages>();
                 }
                 if (a.expire) ok = false;
             }
@@ -387,7 +454,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                             mma_commit<2>(&empty[r.stage]);
                         }
                         __syncwarp();
-                        r.next<kMmaStages>();
+                        r.next<kStages>();
                     }
                     if (elect_one()) mma_commit<2>(&sums_full[it & 1]);
                     __syncwarp();
@@ -437,7 +504,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                     const int n = t.n * kMmaTile + 128 * half + kCols * c;
                     if (n >= a.cols) break;
                     out_columns<KIND == kMmaBf16>(a, map_out, t, n, row - lane, lane, add, sums + kCols * c,
-                                                  stages + kMmaStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
+                                                  stages + kStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
                 }
             }
         }
@@ -445,6 +512,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     } else if (warp >= 4) {
         const int set = (warp - 4) >> 2, quad = warp & 3;
         const uint32_t empty_bar = peer_shared(&sums_empty[set], 0);
+        uint32_t residual_phase = 0;
         int it = 0;
         for (int i = pair; i < tiles && ok; i += pairs, ++it) {
             if ((it & 1) != set) continue;
@@ -455,21 +523,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
                 break;
             }
             tmem_fence_after();
-            const bool add = a.add && first + lane < a.rows;
-            constexpr int kCols = kOutCols<KIND == kMmaBf16>;
+            if constexpr (kLayer) {
 #pragma unroll 1
-            for (int n = t.n * kMmaTile, c = 0; c < kMmaTile && n < a.cols && first < a.rows; c += kCols, n += kCols) {
-                float f[kCols];
+                for (int n = t.n * a.width, c = 0; c < a.width && n < a.cols && first < a.rows; c += 64, n += 64)
+                    ok = layer_columns<KIND - kMmaLayer>(a, map_out, map_residual, map_slope, n, first, lane,
+                                                         tmem + set * 256 + c + (uint32_t(quad * 32) << 16),
+                                                         stages + kStages * 2 * kMmaHalf + uint32_t(warp - 4) * (2 * kMmaOut),
+                                                         &residual_full[kLayer ? warp - 4 : 0], &residual_phase) && ok;
+            } else {
+                const bool add = a.add && first + lane < a.rows;
+                constexpr int kCols = kOutCols<KIND == kMmaBf16>;
+#pragma unroll 1
+                for (int n = t.n * kMmaTile, c = 0; c < kMmaTile && n < a.cols && first < a.rows; c += kCols, n += kCols) {
+                    float f[kCols];
 #pragma unroll
-                for (int h = 0; h < kCols; h += 32) {
-                    uint32_t v[32];
-                    __syncwarp();
-                    tmem_ld32(tmem + set * 256 + c + h + (uint32_t(quad * 32) << 16), v);
-                    tmem_wait_ld();
+                    for (int h = 0; h < kCols; h += 32) {
+                        uint32_t v[32];
+                        __syncwarp();
+                        tmem_ld32(tmem + set * 256 + c + h + (uint32_t(quad * 32) << 16), v);
+                        tmem_wait_ld();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) f[h + j] = __uint_as_float(v[j]);
+                        for (int j = 0; j < 32; ++j) f[h + j] = __uint_as_float(v[j]);
+                    }
+                    out_columns<KIND == kMmaBf16>(a, map_out, t, n, first, lane, add, f, stages + kStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
                 }
-                out_columns<KIND == kMmaBf16>(a, map_out, t, n, first, lane, add, f, stages + kMmaStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
             }
             tmem_fence_before();
             __syncwarp();
@@ -493,8 +570,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
         if (rank == 0 && threadIdx.x == 0) {
             atomicExch(a.status + 3, 1);
             const uint32_t most = max(s_end[0] & 0x7FFFFFFFu, s_end[1] & 0x7FFFFFFFu);
-            for (uint32_t i = most - min(most, uint32_t(kMmaStages)); i < most; ++i)
-                mbar_wait_cluster(&full[i % kMmaStages], (i / kMmaStages) & 1);
+            for (uint32_t i = most - min(most, uint32_t(kStages)); i < most; ++i)
+                mbar_wait_cluster(&full[i % kStages], (i / kStages) & 1);
         }
         __syncwarp();
         if (warp == 1) {
@@ -509,163 +586,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     if (warp == 2) tmem_free<2>(tmem, 512);
 }
 
-// Partial states of a row's tiles to its results: four rows by a block, a thread takes every 64th tile of one, five at a time.
-constexpr int kFinishRows = 4;
-struct FinishArgs {
-    const float2* part;
-    const float* of_target;
-    int32_t tiles, rows, V;
-    const uint32_t* mask;
-    int64_t mask_stride;
-    const int32_t* targets;
-    float *loss, *lse;
-    int32_t* status;
-};
-static __global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * kFinishRows + (lane & 3);
-    float m = -INFINITY, s = 0.f;
-    // (what the end needs is asked for before the states: the target's score is there or is not looked at)
-    const bool ends = warp == 0 && lane < kFinishRows && row < a.rows;
-    const int target = ends ? ld_after_wait(a.targets + row) : -1;
-    const float of_target = ends ? ld_after_wait(a.of_target + row) : 0.f;
-    if (row < a.rows)
-        for (int t = warp * 8 + (lane >> 2); t < a.tiles; t += 320) {
-            float2 p[5];
-#pragma unroll
-            for (int k = 0; k < 5; ++k)
-                p[k] = t + 64 * k < a.tiles ? __ldcg(a.part + int64_t(t + 64 * k) * a.rows + row) : make_float2(-INFINITY, 0.f);
-            float next = m;
-#pragma unroll
-            for (int k = 0; k < 5; ++k) next = fmaxf(next, p[k].x);
-            const float ref = fmaxf(next, kRefFloor);
-            s *= ex2f((fmaxf(m, kRefFloor) - ref) * kLog2e);
-#pragma unroll
-            for (int k = 0; k < 5; ++k) s += p[k].y * ex2f((fmaxf(p[k].x, kRefFloor) - ref) * kLog2e);
-            m = next;
-        }
-    bool has = target >= 0 && target < a.V;
-    if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (target >> 5)) >> (target & 31)) & 1u;
-    __shared__ float2 sh[64][kFinishRows];
-    sh[warp * 8 + (lane >> 2)][lane & 3] = make_float2(m, s);
-    __syncthreads();
-    if (warp) return;
-    // eight threads a row, eight states each
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[8 * (lane >> 2) + w][lane & 3].x);
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-    const float ref = fmaxf(top, kRefFloor);
-    s = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-        const float2 p = sh[8 * (lane >> 2) + w][lane & 3];
-        s += p.y * ex2f((fmaxf(p.x, kRefFloor) - ref) * kLog2e);
-    }
-    s += __shfl_xor_sync(0xFFFFFFFFu, s, 4);
-    s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);
-    s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
-    if (!ends) return;
-    const float log_sum = logf(s);
-    if (a.lse) a.lse[row] = s > 0.f ? top + log_sum : -INFINITY;
-    if (target >= a.V) atomicAdd(a.status + 1, 1);
-    float loss = 0.f;
-    if (target >= 0) loss = has && of_target > -INFINITY ? (top - of_target) + log_sum : INFINITY;
-    a.loss[row] = loss;
+template <bool A_MN, bool B_MN, int KIND, bool LONG>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
+    k_head_mma(const __grid_constant__ MmaArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ CUtensorMap map_out) {
+    mma_products<A_MN, B_MN, KIND, LONG>(a, map_a, map_b, map_out, map_out, map_out);
 }
 
-// The same for log probabilities and entropies. A state's reference is its largest score, kFew where it has none.
-struct LogprobsFinishArgs {
-    const float4* sums;
-    const float* of_target;
-    int32_t tiles, rows, V;
-    const uint32_t* mask;
-    int64_t mask_stride;
-    const int32_t* tokens;
-    float *logp, *entropy, *lse;
-    int32_t* status;
-};
-static __global__ void __launch_bounds__(256) k_head_logprobs_finish(const LogprobsFinishArgs a) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * kFinishRows + (lane & 3);
-    const bool ends = warp == 0 && lane < kFinishRows && row < a.rows;
-    const int token = ends ? ld_after_wait(a.tokens + row) : -1;
-    const float of_token = ends ? ld_after_wait(a.of_target + row) : 0.f;
-    float m = kFew, s = 0.f, d = 0.f;
-    if (row < a.rows)
-        for (int t = warp * 8 + (lane >> 2); t < a.tiles; t += 320) {
-            float4 p[5];
-#pragma unroll
-            for (int k = 0; k < 5; ++k)
-                p[k] = t + 64 * k < a.tiles ? __ldcg(a.sums + int64_t(t + 64 * k) * a.rows + row) : make_float4(kFew, 0.f, 0.f, 0.f);
-            float next = m;
-#pragma unroll
-            for (int k = 0; k < 5; ++k) next = fmaxf(next, p[k].x);
-            const float by = m - next, e = ex2f(by * kLog2e);
-            d = fmaf(by, s, d) * e;
-            s *= e;
-#pragma unroll
-            for (int k = 0; k < 5; ++k) {
-                const float of = p[k].x - next, f = ex2f(of * kLog2e);
-                d = fmaf(fmaf(of, p[k].y, p[k].z), f, d);
-                s = fmaf(p[k].y, f, s);
-            }
-            m = next;
-        }
-    bool has = token >= 0 && token < a.V;
-    if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (token >> 5)) >> (token & 31)) & 1u;
-    __shared__ float4 sh[64][kFinishRows];
-    sh[warp * 8 + (lane >> 2)][lane & 3] = make_float4(m, s, d, 0.f);
-    __syncthreads();
-    if (warp) return;
-    // eight threads a row, eight states each
-    float top = kFew;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[8 * (lane >> 2) + w][lane & 3].x);
-#pragma unroll
-    for (int k = 4; k <= 16; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, k));
-    s = d = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-        const float4 p = sh[8 * (lane >> 2) + w][lane & 3];
-        const float of = p.x - top, f = ex2f(of * kLog2e);
-        d = fmaf(fmaf(of, p.y, p.z), f, d);
-        s = fmaf(p.y, f, s);
-    }
-#pragma unroll
-    for (int k = 4; k <= 16; k <<= 1) {
-        s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
-        d += __shfl_xor_sync(0xFFFFFFFFu, d, k);
-    }
-    if (!ends) return;
-    const float log_sum = logf(s);
-    if (a.lse) a.lse[row] = s > 0.f ? top + log_sum : -INFINITY;
-    if (a.entropy) a.entropy[row] = s > 0.f ? fmaxf(log_sum - d / s, 0.f) : 0.f;
-    if (token >= a.V) atomicAdd(a.status + 1, 1);
-    float logp = 0.f;
-    if (token >= 0) logp = has && of_token > kFew ? (of_token - top) - log_sum : -INFINITY;
-    a.logp[row] = logp;
-}
-
-// The sums of `splits` cuts, added up and rounded; four to a thread, n a multiple of 8. (Few rows have many cuts: what takes time is
-// how many loads a thread waits for, one after the other. 500 x 256 from 37 cuts: 18 us with eight to a thread, four at a time.)
-static __global__ void __launch_bounds__(256) k_head_round(const float* from, int64_t split_elems, int splits, uint16_t* to, int64_t to_stride,
-                                                    int rows, int n) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int vectors = n / 4;
-    const int64_t total = int64_t(rows) * vectors;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
-        float f[4] = {};
-#pragma unroll 8
-        for (int s = 0; s < splits; ++s) {
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(from + s * split_elems + 4 * i));
-            f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
-        }
-        const int64_t row = i / vectors;
-        *reinterpret_cast<uint2*>(to + row * to_stride + 4 * (i - row * vectors)) = make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]));
-    }
+template <bool B_MN, int ACT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
+    k_layer_mma(const __grid_constant__ MmaArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_residual,
+                const __grid_constant__ CUtensorMap map_slope) {
+    mma_products<false, B_MN, kMmaLayer + ACT, false>(a, map_a, map_b, map_y, map_residual, map_slope);
 }
 
 }  // namespace cfgzip

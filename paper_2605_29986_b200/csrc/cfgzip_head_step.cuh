@@ -15,6 +15,7 @@
 #include <cuda.h>
 
 #include "cfgzip_head_mma.cuh"
+#include "cfgzip_mx.cuh"
 
 namespace cfgzip {
 

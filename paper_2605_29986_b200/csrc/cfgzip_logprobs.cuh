@@ -52,21 +52,10 @@ __device__ __forceinline__ uint32_t octet_bits(const uint8_t* mask, int head, in
     return (b >> head) & 0xFFu;
 }
 
-__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
-    unsigned long long d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
-}
-
-__device__ __forceinline__ uint32_t bf16_two(float lo, float hi) {  // nearest, ties to even
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
 }
 
 // Eight logits in registers as they were loaded.
@@ -523,7 +512,7 @@ __global__ void __launch_bounds__(256) k_token_logprobs_backward(const LogprobsB
                 d = token == g.token ? g.at_token(x, it) : g.at(x, it);
             }
             if (DT == kBF16)
-                reinterpret_cast<uint16_t*>(to)[token] = uint16_t(bf16_two(d, d));
+                reinterpret_cast<uint16_t*>(to)[token] = uint16_t(bf16_pair(d, d));
             else
                 reinterpret_cast<float*>(to)[token] = d;
         }
@@ -572,7 +561,7 @@ __global__ void __launch_bounds__(256) k_token_logprobs_backward(const LogprobsB
             }
             if constexpr (DT == kBF16) {
                 st_stream16(to + int64_t(first) * kSize,
-                            make_uint4(bf16_two(d[0], d[1]), bf16_two(d[2], d[3]), bf16_two(d[4], d[5]), bf16_two(d[6], d[7])));
+                            make_uint4(bf16_pair(d[0], d[1]), bf16_pair(d[2], d[3]), bf16_pair(d[4], d[5]), bf16_pair(d[6], d[7])));
             } else {
                 const uint4 lo = make_uint4(__float_as_uint(d[0]), __float_as_uint(d[1]), __float_as_uint(d[2]), __float_as_uint(d[3]));
                 const uint4 hi = make_uint4(__float_as_uint(d[4]), __float_as_uint(d[5]), __float_as_uint(d[6]), __float_as_uint(d[7]));
