@@ -374,7 +374,7 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
  *                which none is allowed are not read
  *   tokens     : dev int32 [N], NULL where logp is. logp of a negative one is 0, of one that is not allowed or whose logit is -inf it is
  *                -inf; of one at V or above too, and it counts as a bad token
- *   inv_temperature : above 0, at most 1e6
+ *   inv_temperature : 1e-6 to 1e6
  *   n_top      : 0 to 32; the n_top tokens with the largest logits of those allowed, largest first, equal ones (-0.0 == +0.0) by token
  *                id, lowest first. Where fewer have a probability the rest is token -1 with log probability -inf
  *   logp, entropy, lse : dev float [N], each nullable. A row with nothing allowed: lse -inf, entropy 0, logp -inf (0 where no token is given)
@@ -395,8 +395,8 @@ int cfgzip_token_logprobs(cfgzip_ctx* ctx, const void* logits, int dtype, int64_
  *   logits .. inv_temperature : as given to cfgzip_token_logprobs
  *   lse, entropy : dev float [N], as it returned them (entropy NULL where d_entropy is)
  *   d_logp, d_entropy : dev float [N], one of them nullable
- *   d_logits   : dev [N, d_stride_elems] of `dtype`, d_stride_elems >= V; elements at V and above of a row are not touched. May be
- *                `logits` itself with the same stride; must not overlap it otherwise
+ *   d_logits   : dev [N, d_stride_elems] of `dtype`, d_stride_elems >= V; elements at V and above of a row are not touched. Must not
+ *                overlap the logits: all of a row's gradient looks at the given token's (CFGZIP_E_ARG where they are the same)
  */
 int cfgzip_token_logprobs_backward(cfgzip_ctx* ctx, const void* logits, int dtype, int64_t row_stride_elems, int32_t N, int32_t V,
                                    const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* tokens, float inv_temperature,

@@ -10,11 +10,13 @@
 
 namespace cfgzip {
 
-constexpr int kLogprobsThreads = 256;
 constexpr int kLogprobsChunk = 256;      // tokens whose largest logit is kept together: eight to a lane
 constexpr int kLogprobsTopMost = 32;     // alternatives at most
 constexpr int kLogprobsList = 256;       // candidates that are put in order by counting
-constexpr float kLogprobsSlack = 8.f;    // powers of two that a value may be above the reference of its sum
+constexpr int kLogprobsPicks = 128;      // chunks that are read once more, at most
+constexpr int kLogprobsAll = 64;         // ... where all that have an allowed token are
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLogprobsSlack = 8.f;    // powers of two that a logit may be above the reference of its sum
 
 struct LogprobsArgs {
     const void* logits;
@@ -45,12 +47,28 @@ __device__ __forceinline__ RowShape row_shape(const void* row, int V) {
     return s;
 }
 
-// The allow bits of the octet that starts at token head + 8 o.
+// The allow bits of the octet that starts at token head + 8 o, alone.
 __device__ __forceinline__ uint32_t octet_bits(const uint8_t* mask, int head, int o) {
     uint32_t b = ld_after_wait(mask + o);
     if (head) b |= ld_after_wait(mask + o + 1) << 8;
     return (b >> head) & 0xFFu;
 }
+
+// The allow bits of a warp's next chunks (`n` of them, at most 4, `step` apart), eight words of 32 to each: lane l has word l % 8 of chunk
+// c + step (l / 8). They are asked for a round ahead of the logits, which wait for them, and put in place when they are used.
+struct ChunkBits {
+    uint32_t word, after;
+    __device__ __forceinline__ void ask(const uint32_t* mask, int head, int V, int c, int c1, int step, int n, int lane) {
+        const int chunk = c + step * (lane >> 3), at = 8 * chunk + (lane & 7), words = (V + 31) / 32;
+        const bool have = chunk < c1 && lane < 8 * n;
+        word = have && at < words ? ld_after_wait(mask + at) : 0u;
+        after = have && head && (lane & 7) == 7 && at + 1 < words ? ld_after_wait(mask + at + 1) : 0u;
+    }
+    __device__ __forceinline__ uint32_t from(int head, int lane) const {  // bits from `head` on: the next word's first ones come in
+        const uint32_t next = __shfl_down_sync(0xFFFFFFFFu, word, 1);
+        return __funnelshift_r(word, (lane & 7) == 7 ? after : next, head);
+    }
+};
 
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
     uint32_t d;
@@ -69,8 +87,12 @@ struct Logits8<kBF16> {
     __device__ __forceinline__ void load(const void* row, int first) {
         v = ld_stream16(static_cast<const uint16_t*>(row) + first);
     }
-    // The values, masked ones and what is below kNone as that, and the largest of them.
-    __device__ __forceinline__ float values(uint32_t bits, bool masked, float (&f)[8]) {
+    __device__ __forceinline__ void load_anywhere(const void* row, int first) {
+        const uint16_t* p = static_cast<const uint16_t*>(row) + first;
+        v = make_uint4(p[0] | uint32_t(p[1]) << 16, p[2] | uint32_t(p[3]) << 16, p[4] | uint32_t(p[5]) << 16, p[6] | uint32_t(p[7]) << 16);
+    }
+    // Masked ones, and what is below kNone, become that. Returns the largest.
+    __device__ __forceinline__ float settle(uint32_t bits, bool masked) {
         if (masked) {
             const uint32_t xl = nibble_to_byte_msbs(bits & 0xFu), xh = nibble_to_byte_msbs(bits >> 4);
             const uint32_t m0 = prmt(xl, 0u, 0x9988), m1 = prmt(xl, 0u, 0xBBAA), m2 = prmt(xh, 0u, 0x9988), m3 = prmt(xh, 0u, 0xBBAA);
@@ -79,13 +101,17 @@ struct Logits8<kBF16> {
             v.z = (v.z & m2) | (kNone2 & ~m2);
             v.w = (v.w & m3) | (kNone2 & ~m3);
         }
-        const uint32_t a = max_bf16x2(v.x, kNone2), b = max_bf16x2(v.y, kNone2), c = max_bf16x2(v.z, kNone2), d = max_bf16x2(v.w, kNone2);
-        const uint32_t m = max_bf16x2(max_bf16x2(a, b), max_bf16x2(c, d));
-        f[0] = __uint_as_float(a << 16); f[1] = __uint_as_float(a & 0xFFFF0000u);
-        f[2] = __uint_as_float(b << 16); f[3] = __uint_as_float(b & 0xFFFF0000u);
-        f[4] = __uint_as_float(c << 16); f[5] = __uint_as_float(c & 0xFFFF0000u);
-        f[6] = __uint_as_float(d << 16); f[7] = __uint_as_float(d & 0xFFFF0000u);
+        v = make_uint4(max_bf16x2(v.x, kNone2), max_bf16x2(v.y, kNone2), max_bf16x2(v.z, kNone2), max_bf16x2(v.w, kNone2));
+        const uint32_t m = max_bf16x2(max_bf16x2(v.x, v.y), max_bf16x2(v.z, v.w));
         return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+    }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f[2 * j] = __uint_as_float(w[j] << 16);
+            f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+        }
     }
 };
 template <>
@@ -100,42 +126,57 @@ struct Logits8<kF32> {
         a = ld_stream16(p);
         b = ld_stream16(p + 4);
     }
-    __device__ __forceinline__ float values(uint32_t bits, bool masked, float (&f)[8]) {
-        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    __device__ __forceinline__ void load_anywhere(const void* row, int first) {
+        const uint32_t* p = static_cast<const uint32_t*>(row) + first;
+        a = make_uint4(p[0], p[1], p[2], p[3]);
+        b = make_uint4(p[4], p[5], p[6], p[7]);
+    }
+    __device__ __forceinline__ float settle(uint32_t bits, bool masked) {
+        uint32_t* const w[8] = {&a.x, &a.y, &a.z, &a.w, &b.x, &b.y, &b.z, &b.w};
+        float f[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            f[j] = fmaxf(__uint_as_float(w[j]), kNone);
+            f[j] = fmaxf(__uint_as_float(*w[j]), kNone);
             if (masked) f[j] = (bits >> j) & 1u ? f[j] : kNone;
+            *w[j] = __float_as_uint(f[j]);
         }
         return fmaxf(fmax3(fmax3(f[0], f[1], f[2]), f[3], f[4]), fmax3(f[5], f[6], f[7]));
     }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(w[j]);
+    }
 };
 
-// Sums of exp((z - ref) / T) and of that times z - ref, the reference a value of the thread's that was its largest up to kLogprobsSlack
-// powers of two ago. The differences are taken before anything is multiplied: a row's logits may be far from zero.
+// Sums of 2^t and 2^t t, t = z log2(e) / T + n, over a thread's logits. The reference -n is a whole number, so that t is rounded once however
+// far from zero a row is, all threads' t are of the same numbers, and a sum goes over to another reference exactly. It follows the largest
+// logit so far: up to kLogprobsSlack below it.
 struct EntropySums {
-    float ref = kFew;
+    float n;                          // (of kFew at first: what counts moves it)
     unsigned long long s = 0, d = 0;  // pairs of partial sums
-    __device__ __forceinline__ void add(const float (&f)[8], float top, float scale) {
-        if ((top - ref) * scale > kLogprobsSlack) move(top, scale);
-        const unsigned long long minus = pack2(-ref, -ref), by = pack2(scale, scale);
+    __device__ __forceinline__ explicit EntropySums(float scale) : n(-rintf(kFew * scale)) {}
+    __device__ __forceinline__ void follow(float top, float scale) {
+        if (fmaf(top, scale, n) > kLogprobsSlack) move(-rintf(top * scale));
+    }
+    __device__ __forceinline__ void add(const float (&f)[8], float scale) {
+        const unsigned long long by = pack2(scale, scale), plus = pack2(n, n);
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
-            const unsigned long long x = add2(pack2(f[j], f[j + 1]), minus);
+            const unsigned long long t = fma2(pack2(f[j], f[j + 1]), by, plus);
             float t0, t1;
-            unpack2(mul2(x, by), t0, t1);
+            unpack2(t, t0, t1);
             const unsigned long long e = pack2(ex2f(t0), ex2f(t1));
             s = add2(s, e);
-            d = fma2(e, x, d);
+            d = fma2(e, t, d);
         }
     }
-    // to another reference: z - to = (z - ref) + (ref - to)
-    __device__ __forceinline__ void move(float to, float scale) {
-        const float by = ref - to, e = ex2f(by * scale);
+    __device__ __forceinline__ void move(float to) {
+        const float by = to - n, e = ex2f(by);
         const unsigned long long e2 = pack2(e, e);
         d = mul2(fma2(pack2(by, by), s, d), e2);
         s = mul2(s, e2);
-        ref = to;
+        n = to;
     }
     __device__ __forceinline__ float2 total() const {
         float s0, s1, d0, d1;
@@ -156,25 +197,53 @@ __device__ __forceinline__ float candidate_value(unsigned long long key) {
 }
 
 // A chunk's tokens, up to eight to a lane: chunk 0 the tokens before the row's first vector, then 256 at a time, at last those behind the
-// last vector. Returns the first token; the values are kNone where there is none, or none that counts.
+// last vector. The values are kNone where there is none, or none that counts; `first` is the first value's token. Returns the largest.
 template <int DT, bool MASKED>
-__device__ __forceinline__ int chunk_values(const LogprobsArgs& a, const void* row, const uint8_t* mask, const RowShape& r, int chunk,
-                                            int chunks, int lane, float (&f)[8]) {
+__device__ __forceinline__ float chunk_values(const LogprobsArgs& a, const void* row, const uint8_t* mask, const RowShape& r, int chunk,
+                                              int chunks, int lane, float (&f)[8], int* first) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = kNone;
     if (chunk > 0 && chunk <= chunks) {
-        const int o = (chunk - 1) * 32 + lane, first = r.head + 8 * o;
-        if (o >= r.octets) return first;
+        const int o = (chunk - 1) * 32 + lane;
+        *first = r.head + 8 * o;
+        if (o >= r.octets) return kNone;
         const uint32_t bits = MASKED ? octet_bits(mask, r.head, o) : 0xFFu;
         Logits8<DT> v;
-        v.load(row, first);
-        v.values(bits, MASKED, f);
-        return first;
+        v.load(row, *first);
+        const float top = v.settle(bits, MASKED);
+        v.get(f);
+        return top;
     }
     const int token = chunk ? r.head + 8 * r.octets + lane : lane;
+    *first = token;
     if (lane < (chunk ? r.tail : r.head) && (!MASKED || ((ld_after_wait(mask + (token >> 3)) >> (token & 7)) & 1u)))
         f[0] = fmaxf(load_elem<DT>(row, token), kNone);
-    return token;
+    return f[0];
+}
+
+// A bar that at least n of the values reach, and hardly more than 1.5 n as long as they come in no order: the n-th largest (n at most 32) of
+// the largest values of 64 runs of neighbours, two to a lane of one warp. kNone where fewer than n runs have a value that counts.
+__device__ __forceinline__ float bar_of_runs(const float* values, int all, int n, int lane) {
+    const int run = ((all + 63) / 64) | 1;  // (odd, for the banks)
+    float best[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int lo = min((32 * k + lane) * run, all), hi = min(lo + run, all);
+        best[k] = kNone;
+        for (int i = lo; i < hi; ++i) best[k] = fmaxf(best[k], values[i]);
+    }
+    float bar = kNone;
+    for (int k = 0; k < n; ++k) {
+        const float mine = fmaxf(best[0], best[1]);
+        bar = redux_max(mine);
+        if (!(bar > kFew)) return kNone;
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, mine == bar);
+        if (lane == __ffs(who) - 1) {
+            best[1] = best[0] == bar ? best[1] : kNone;
+            best[0] = best[0] == bar ? kNone : best[0];
+        }
+    }
+    return bar;
 }
 
 // The first n of `all` largest values by value, then by place, and the last one's value: by one warp, each lane with a run of neighbours
@@ -216,18 +285,20 @@ __device__ __forceinline__ Picked pick_largest(float* values, int all, int n, in
 // A cluster of blocks (of 1 to 16) a row; a warp takes 256 tokens at a time, four loads of a lane in flight. The blocks' sums meet in the
 // first block.
 //
-// Alternatives: the largest logit of every 256 tokens comes for one warp reduction. In the order (largest logit, then lower place) the
-// first n of these chunks hold the first n tokens (n chunks ahead of a token's own hold n tokens ahead of it). One warp picks them, the
-// block reads them once more (from the L2, n * 256 tokens), keeps what is not below the n-th chunk's largest, hardly more than n tokens,
-// and every one of those counts how many are ahead of it.
-template <int DT, bool MASKED>
-__global__ void __launch_bounds__(kLogprobsThreads, 4) k_token_logprobs(const LogprobsArgs a, int blocks) {
+// Alternatives: the largest logit of every chunk of 256 tokens comes for one warp reduction. A bar that at least n chunks' largest reach is
+// one that at least n tokens reach, and all tokens that reach it are in chunks that do. One warp finds a bar that hardly more than n do
+// (bar_of_runs), the block reads those chunks once more from the L2 and lists the tokens, and each of them counts how many are ahead of it.
+// Equal logits may put too many chunks above a bar. In the order (largest logit, then place) the first n chunks hold the first n tokens (n
+// chunks ahead of a token's own hold n tokens ahead of it), and can be picked one after the other: 0.5 us each.
+template <int DT, bool MASKED, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const LogprobsArgs a, int blocks) {
+    constexpr int kThreads = WARPS * 32;
     extern __shared__ float s_chunk[];  // the first block's: largest logit of every chunk
-    __shared__ float s_ref[8], s_sum[8], s_dif[8];
+    __shared__ float s_ref[WARPS], s_sum[WARPS], s_dif[WARPS];
     __shared__ float4 s_block[kClusterMost];
     __shared__ unsigned long long s_list[kLogprobsList];
-    __shared__ int s_pick[kLogprobsTopMost], s_picked, s_listed;
-    __shared__ float s_bar, s_eight[32 * kLogprobsTopMost];
+    __shared__ int s_pick[kLogprobsPicks], s_picked, s_listed;
+    __shared__ float s_bar, s_most, s_log_sum, s_eight[32 * kLogprobsAll];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t row = blockIdx.x / blocks;
     const int rank = int(blockIdx.x - row * blocks);
@@ -238,7 +309,7 @@ __global__ void __launch_bounds__(kLogprobsThreads, 4) k_token_logprobs(const Lo
     const int chunks = (r.octets + 31) / 32;
     const int c1 = int(int64_t(chunks) * (rank + 1) / blocks);
     const uint32_t chunk_at = peer_shared(s_chunk, 0);
-    if (threadIdx.x == 0) s_listed = 0;
+    if (threadIdx.x == 0) s_listed = s_picked = 0;
     cluster_barrier();  // (the first block is there to be written to)
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
@@ -250,51 +321,82 @@ __global__ void __launch_bounds__(kLogprobsThreads, 4) k_token_logprobs(const Lo
         if (token >= 0 && token < a.V && (!MASKED || ((ld_after_wait(mask + (token >> 3)) >> (token & 7)) & 1u))) of_token = load_elem<DT>(z, token);
     }
 
-    EntropySums sums;
+    EntropySums sums(scale);
     float most = kNone;
     // tokens beside the vectors
     if (warp == 0 && (rank == 0 || rank == blocks - 1)) {
 #pragma unroll 1
         for (int edge = rank == 0 ? 0 : 1; edge < (rank == blocks - 1 ? 2 : 1); ++edge) {
             float f[8];
-            chunk_values<DT, MASKED>(a, z, mask, r, edge ? chunks + 1 : 0, chunks, lane, f);
-            most = fmaxf(most, f[0]);
-            sums.add(f, f[0], scale);
-            const float top = redux_max(f[0]);
+            int first;
+            const float mine = chunk_values<DT, MASKED>(a, z, mask, r, edge ? chunks + 1 : 0, chunks, lane, f, &first);
+            const float top = redux_max(mine);
+            most = fmaxf(most, top);
+            if (top > kNone) {
+                sums.follow(mine, scale);
+                sums.add(f, scale);
+            }
             if (a.n_top && lane == 0) st_peer_u32(chunk_at + 4u * uint32_t(edge ? chunks + 1 : 0), __float_as_uint(top));
         }
     }
-    constexpr int kAhead = 4;
+    constexpr int kAhead = DT == kF32 && MASKED ? 3 : 4;  // chunks of a warp at a time (registers)
+    int c = int(int64_t(chunks) * rank / blocks) + warp;
+    const int whole = min(c1, r.octets / 32);  // (only a row's last chunk may not be)
+    const uint32_t* words = MASKED ? a.mask + row * a.mask_stride : nullptr;
+    ChunkBits chunk_bits;
+    if (MASKED) chunk_bits.ask(words, r.head, a.V, c, c1, WARPS, kAhead, lane);
 #pragma unroll 1
-    for (int c = int(int64_t(chunks) * rank / blocks) + warp; c < c1; c += 8 * kAhead) {
-        uint32_t bits[kAhead];
+    for (; c + WARPS * (kAhead - 1) < whole; c += WARPS * kAhead) {
         Logits8<DT> v[kAhead];
+        uint32_t bits[kAhead];
+        float top[kAhead];
+        const uint32_t of_chunks = MASKED ? chunk_bits.from(r.head, lane) : 0u;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const int o = (c + 8 * k) * 32 + lane;
-            bits[k] = c + 8 * k < c1 && o < r.octets ? (MASKED ? octet_bits(mask, r.head, o) : 0xFFu) : 0u;
+            bits[k] = MASKED ? __shfl_sync(0xFFFFFFFFu, of_chunks, 8 * k + (lane >> 2)) >> (8 * (lane & 3)) & 0xFFu : 0xFFu;
+            if (!MASKED || bits[k]) v[k].load(z, r.head + 8 * ((c + WARPS * k) * 32 + lane));  // (what is not read is masked)
         }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {  // (vectors of which nothing is allowed are not read)
-            v[k].none();
-            if (bits[k]) v[k].load(z, r.head + 8 * ((c + 8 * k) * 32 + lane));
-        }
+        if (MASKED) chunk_bits.ask(words, r.head, a.V, c + WARPS * kAhead, c1, WARPS, kAhead, lane);
+        float mine = kNone;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            if (c + 8 * k >= c1) break;
+            top[k] = v[k].settle(bits[k], MASKED);
+            mine = fmaxf(mine, top[k]);
+        }
+        most = fmaxf(most, mine);
+        sums.follow(mine, scale);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
             float f[8];
-            const float top = v[k].values(bits[k], MASKED, f);
-            most = fmaxf(most, top);
-            sums.add(f, top, scale);
-            if (a.n_top) {
-                const float of_chunk = redux_max(top);
-                if (lane == 0) st_peer_u32(chunk_at + 4u * uint32_t(c + 8 * k + 1), __float_as_uint(of_chunk));
+            v[k].get(f);
+            sums.add(f, scale);
+        }
+        if (a.n_top) {
+            float of_chunk = redux_max(top[0]);
+#pragma unroll
+            for (int k = 1; k < kAhead; ++k) {
+                const float x = redux_max(top[k]);
+                of_chunk = lane == k ? x : of_chunk;
             }
+            if (lane < kAhead) st_peer_u32(chunk_at + 4u * uint32_t(c + WARPS * lane + 1), __float_as_uint(of_chunk));
+        }
+    }
+#pragma unroll 1
+    for (; c < c1; c += WARPS) {
+        float f[8];
+        int first;
+        const float mine = chunk_values<DT, MASKED>(a, z, mask, r, c + 1, chunks, lane, f, &first);
+        most = fmaxf(most, mine);
+        sums.follow(mine, scale);
+        sums.add(f, scale);
+        if (a.n_top) {
+            const float of_chunk = redux_max(mine);
+            if (lane == 0) st_peer_u32(chunk_at + 4u * uint32_t(c + 1), __float_as_uint(of_chunk));
         }
     }
     // the block's sums
     most = fmaxf(redux_max(most), kFew);
-    sums.move(most, scale);
+    sums.move(-rintf(most * scale));
     float2 t = sums.total();
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) {
@@ -310,11 +412,12 @@ __global__ void __launch_bounds__(kLogprobsThreads, 4) k_token_logprobs(const Lo
     if (threadIdx.x == 0) {
         float m = s_ref[0];
 #pragma unroll
-        for (int w = 1; w < 8; ++w) m = fmaxf(m, s_ref[w]);
+        for (int w = 1; w < WARPS; ++w) m = fmaxf(m, s_ref[w]);
+        const float to = rintf(m * scale);
         float s = 0.f, d = 0.f;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) {
-            const float by = s_ref[w] - m, e = ex2f(by * scale);
+        for (int w = 0; w < WARPS; ++w) {
+            const float by = rintf(s_ref[w] * scale) - to, e = ex2f(by);
             s = fmaf(s_sum[w], e, s);
             d = fmaf(fmaf(by, s_sum[w], s_dif[w]), e, d);
         }
@@ -327,19 +430,24 @@ __global__ void __launch_bounds__(kLogprobsThreads, 4) k_token_logprobs(const Lo
     cluster_barrier();
     if (rank != 0) return;
 
-    float m = kFew;
-    for (int b = 0; b < blocks; ++b) m = fmaxf(m, s_block[b].x);
-    float s = 0.f, d = 0.f;
-    for (int b = 0; b < blocks; ++b) {
-        const float4 p = s_block[b];
-        const float by = p.x - m, e = ex2f(by * scale);
-        s = fmaf(p.y, e, s);
-        d = fmaf(fmaf(by, p.y, p.z), e, d);
-    }
-    const float log_sum = logf(s);  // (-inf where nothing is allowed)
     if (threadIdx.x == 0) {
+        float m = kFew;
+        for (int b = 0; b < blocks; ++b) m = fmaxf(m, s_block[b].x);
+        const float to = rintf(m * scale);
+        float s = 0.f, d = 0.f;
+        for (int b = 0; b < blocks; ++b) {
+            const float4 p = s_block[b];
+            const float by = rintf(p.x * scale) - to, e = ex2f(by);
+            s = fmaf(p.y, e, s);
+            d = fmaf(fmaf(by, p.y, p.z), e, d);
+        }
+        // relative to the largest logit itself, whose exponential is divided out as it was added: a row's only token has log probability 0
+        const float of_most = fmaf(m, scale, -to);
+        const float log_sum = logf(s / ex2f(of_most));  // (-inf where nothing is allowed)
+        s_most = m;
+        s_log_sum = log_sum;
         if (a.lse) a.lse[row] = s > 0.f ? fmaf(m, a.inv_temperature, log_sum) : -INFINITY;
-        if (a.entropy) a.entropy[row] = s > 0.f ? fmaxf(log_sum - a.inv_temperature * (d / s), 0.f) : 0.f;
+        if (a.entropy) a.entropy[row] = s > 0.f ? fmaxf(log_sum - kLn2 * (d / s - of_most), 0.f) : 0.f;
         if (a.tokens) {
             float logp = 0.f;
             if (token >= 0) logp = of_token > kFew ? fmaf(of_token - m, a.inv_temperature, -log_sum) : -INFINITY;
@@ -348,49 +456,76 @@ __global__ void __launch_bounds__(kLogprobsThreads, 4) k_token_logprobs(const Lo
         }
     }
     if (!a.n_top) return;
+    __syncwarp();
 
+    // the chunks that hold them, by one warp
     if (warp == 0) {
-        const Picked p = pick_largest(s_chunk, chunks + 2, a.n_top, s_pick, lane);
-        if (lane == 0) {
-            s_picked = p.n;
-            s_bar = p.n < a.n_top ? kNone : p.bar;
+        const float bar = bar_of_runs(s_chunk, chunks + 2, a.n_top, lane);
+        if (lane == 0) s_bar = bar;
+    }
+    __syncthreads();
+    const float first_bar = s_bar;
+    for (int i = int(threadIdx.x); i < chunks + 2; i += kThreads) {
+        const float x = s_chunk[i];
+        if (x > kFew && x >= first_bar) {
+            const int at = atomicAdd(&s_picked, 1);
+            if (at < kLogprobsPicks) s_pick[at] = i;
         }
     }
     __syncthreads();
-    const int picked = s_picked;
-    if (picked < a.n_top) {
-        // Fewer chunks with an allowed token than tokens wanted: the same once more with eight tokens at a time. Where there are fewer of
-        // those too, everything they hold fits the list.
-        for (int i = warp; i < picked; i += 8) {
+    int picked = s_picked;
+    if (picked > (first_bar > kFew ? kLogprobsPicks : kLogprobsAll)) {  // (many equal ones, or all in a few runs)
+        __syncthreads();
+        if (warp == 0) {
+            const Picked p = pick_largest(s_chunk, chunks + 2, a.n_top, s_pick, lane);
+            if (lane == 0) {
+                s_picked = p.n;
+                s_bar = p.bar;
+            }
+        }
+        __syncthreads();
+        picked = s_picked;
+    }
+    if (!(s_bar > kFew)) {
+        // All chunks that have an allowed token, few of them: the same once more with eight tokens at a time. Where fewer of those than
+        // tokens wanted have one, everything they hold fits the list.
+        for (int i = warp; i < picked; i += WARPS) {
             float f[8];
-            chunk_values<DT, MASKED>(a, z, mask, r, s_pick[i], chunks, lane, f);
-            s_eight[32 * i + lane] = fmax3(fmax3(f[0], f[1], f[2]), fmax3(f[3], f[4], f[5]), fmaxf(f[6], f[7]));
+            int first;
+            s_eight[32 * i + lane] = chunk_values<DT, MASKED>(a, z, mask, r, s_pick[i], chunks, lane, f, &first);
         }
         __syncthreads();
         if (warp == 0) {
-            const Picked p = pick_largest(s_eight, 32 * picked, a.n_top, nullptr, lane);
-            if (lane == 0 && p.n == a.n_top) s_bar = p.bar;
+            float bar = bar_of_runs(s_eight, 32 * picked, a.n_top, lane);
+            if (!(bar > kFew)) {
+                const Picked p = pick_largest(s_eight, 32 * picked, a.n_top, nullptr, lane);
+                if (p.n == a.n_top) bar = p.bar;
+            }
+            if (lane == 0) s_bar = bar;
         }
         __syncthreads();
     }
     const float bar = s_bar;
-    for (int i = warp; i < picked; i += 8) {
+    for (int i = warp; i < picked; i += WARPS) {
         float f[8];
-        const int first = chunk_values<DT, MASKED>(a, z, mask, r, s_pick[i], chunks, lane, f);
+        int first;
+        if (chunk_values<DT, MASKED>(a, z, mask, r, s_pick[i], chunks, lane, f, &first) >= bar) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (f[j] >= bar && f[j] > kFew) {
-                const int at = atomicAdd(&s_listed, 1);
-                if (at < kLogprobsList) s_list[at] = candidate_key(f[j], first + j);
-            }
+            for (int j = 0; j < 8; ++j)
+                if (f[j] >= bar && f[j] > kFew) {
+                    const int at = atomicAdd(&s_listed, 1);
+                    if (at < kLogprobsList) s_list[at] = candidate_key(f[j], first + j);
+                }
+        }
     }
     __syncthreads();
     const int listed = s_listed;
+    const float m = s_most, log_sum = s_log_sum;
     int32_t* tokens = a.top_tokens + row * a.n_top;
     float* logps = a.top_logp + row * a.n_top;
     if (listed <= kLogprobsList) {
-        if (int(threadIdx.x) < listed) {
-            const unsigned long long key = s_list[threadIdx.x];
+        for (int k = int(threadIdx.x); k < listed; k += kThreads) {
+            const unsigned long long key = s_list[k];
             int ahead = 0;
             for (int i = 0; i < listed; ++i) ahead += s_list[i] > key;
             if (ahead < a.n_top) {
@@ -398,7 +533,7 @@ __global__ void __launch_bounds__(kLogprobsThreads, 4) k_token_logprobs(const Lo
                 logps[ahead] = fmaf(candidate_value(key) - m, a.inv_temperature, -log_sum);
             }
         }
-        for (int i = listed + int(threadIdx.x); i < a.n_top; i += kLogprobsThreads) {
+        for (int i = listed + int(threadIdx.x); i < a.n_top; i += kThreads) {
             tokens[i] = -1;
             logps[i] = -INFINITY;
         }
@@ -408,9 +543,10 @@ __global__ void __launch_bounds__(kLogprobsThreads, 4) k_token_logprobs(const Lo
     unsigned long long last = ~0ull;
     for (int n = 0; n < a.n_top; ++n) {
         unsigned long long best = 0;
-        for (int i = warp; i < picked; i += 8) {
+        for (int i = warp; i < picked; i += WARPS) {
             float f[8];
-            const int first = chunk_values<DT, MASKED>(a, z, mask, r, s_pick[i], chunks, lane, f);
+            int first;
+            chunk_values<DT, MASKED>(a, z, mask, r, s_pick[i], chunks, lane, f, &first);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (f[j] >= bar && f[j] > kFew) {
@@ -424,7 +560,7 @@ __global__ void __launch_bounds__(kLogprobsThreads, 4) k_token_logprobs(const Lo
         if (lane == 0) s_list[warp] = best;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < 8; ++w) best = max(best, s_list[w]);
+        for (int w = 0; w < WARPS; ++w) best = max(best, s_list[w]);
         last = best;
         if (threadIdx.x == 0) {
             tokens[n] = int(~uint32_t(best));
@@ -452,62 +588,127 @@ struct LogprobsBackwardArgs {
 struct RowGradient {
     float lse, a, b, d, entropy;
     int token;
-    bool any;
     __device__ __forceinline__ float at(float z, float inv_temperature) const {
         const float x = fmaxf(fmaf(z, inv_temperature, -lse), -200.f);
         return ex2f(x * kLog2e) * fmaf(b, x, a);
+    }
+    __device__ __forceinline__ void at_pair(float z0, float z1, float inv_temperature, float* d0, float* d1) const {
+        float x0, x1;
+        unpack2(fma2(pack2(z0, z1), pack2(inv_temperature, inv_temperature), pack2(-lse, -lse)), x0, x1);
+        const unsigned long long x = pack2(fmaxf(x0, -200.f), fmaxf(x1, -200.f));
+        unpack2(mul2(x, pack2(kLog2e, kLog2e)), x0, x1);
+        unpack2(mul2(pack2(ex2f(x0), ex2f(x1)), fma2(pack2(b, b), x, pack2(a, a))), *d0, *d1);
     }
     __device__ __forceinline__ float at_token(float z, float inv_temperature) const {
         const float x = fmaf(z, inv_temperature, -lse);
         return fmaf(ex2f(x * kLog2e) * b, x + entropy, -d * expm1f(x));
     }
 };
+// ... what is asked for at once, and what depends on it.
+struct RowInputs {
+    float lse, d_logp, d_entropy, entropy;
+    int token;
+};
+__device__ __forceinline__ RowInputs row_inputs(const LogprobsBackwardArgs& a, int64_t row) {
+    RowInputs i;
+    i.lse = ld_after_wait(a.lse + row);
+    i.token = a.d_logp ? ld_after_wait(a.tokens + row) : -1;
+    i.d_logp = a.d_logp ? ld_after_wait(a.d_logp + row) : 0.f;
+    i.d_entropy = a.d_entropy ? ld_after_wait(a.d_entropy + row) : 0.f;
+    i.entropy = a.d_entropy ? ld_after_wait(a.entropy + row) : 0.f;
+    return i;
+}
 template <int DT, bool MASKED>
-__device__ __forceinline__ RowGradient row_gradient(const LogprobsBackwardArgs& a, int64_t row, const void* z, const uint8_t* mask) {
+__device__ __forceinline__ RowGradient row_gradient(const LogprobsBackwardArgs& a, const RowInputs& i, const void* z, const uint8_t* mask) {
     RowGradient g{};
     g.token = -1;
-    const float lse = ld_after_wait(a.lse + row);
-    if (!(lse > -INFINITY)) return g;
-    g.lse = lse;
-    if (a.d_logp) {
-        const int token = ld_after_wait(a.tokens + row);
-        const float d = ld_after_wait(a.d_logp + row);
-        if (token >= 0 && token < a.V && (!MASKED || ((ld_after_wait(mask + (token >> 3)) >> (token & 7)) & 1u)) && load_elem<DT>(z, token) > kFew) {
-            g.token = token;
-            g.d = d * a.inv_temperature;
+    if (!(i.lse > -INFINITY)) return g;
+    g.lse = i.lse;
+    if (i.token >= 0 && i.token < a.V) {
+        const float of_token = load_elem<DT>(z, i.token);
+        const uint32_t bits = MASKED ? ld_after_wait(mask + (i.token >> 3)) >> (i.token & 7) : 1u;
+        if ((bits & 1u) && of_token > kFew) {
+            g.token = i.token;
+            g.d = i.d_logp * a.inv_temperature;
         }
     }
-    if (a.d_entropy) {
-        g.entropy = ld_after_wait(a.entropy + row);
-        g.b = -ld_after_wait(a.d_entropy + row) * a.inv_temperature;
-    }
+    g.entropy = i.entropy;
+    g.b = -i.d_entropy * a.inv_temperature;
     g.a = fmaf(g.b, g.entropy, -g.d);
-    g.any = g.d != 0.f || g.b != 0.f;
     return g;
 }
 
-// An element, an octet at a time from the gradient's own boundaries on. Logits whose rows start at another place relative to 16 bytes are
-// read element by element. Rows without a gradient are written without being read.
-template <int DT, bool MASKED>
-__global__ void __launch_bounds__(256) k_token_logprobs_backward(const LogprobsBackwardArgs a) {
-    constexpr int kSize = DT == kBF16 ? 2 : 4;
+// Octets of a thread of the gradient, and tokens of a block, at most: 32 KB of logits in flight.
+template <int DT>
+constexpr int kLogprobsOctets = DT == kBF16 ? 8 : 4;
+template <int DT>
+constexpr int kLogprobsPiece = kLogprobsOctets<DT> * 2048;
+
+// An octet at a time from the gradient's own boundaries on. Logits whose rows start at another place relative to 16 bytes (TOGETHER false) are
+// read element by element. Rows without a gradient are written without being read. A block does its tokens in one go: masks and the row's numbers are asked
+// for, then the logits, then what the row's constants need of the given token, so that three latencies follow one another, and four or more
+// blocks of an SM share them.
+template <int DT, bool MASKED, bool TOGETHER>
+__global__ void __launch_bounds__(256, 4) k_token_logprobs_backward(const LogprobsBackwardArgs a) {
+    constexpr int kSize = DT == kBF16 ? 2 : 4, kAhead = kLogprobsOctets<DT>;
     const int64_t row = blockIdx.x / a.pieces;
     const int piece = int(blockIdx.x - row * a.pieces);
     const char* z = static_cast<const char*>(a.logits) + row * a.stride * kSize;
     char* to = static_cast<char*>(a.d_logits) + row * a.d_stride * kSize;
     const uint8_t* mask = MASKED ? reinterpret_cast<const uint8_t*>(a.mask + row * a.mask_stride) : nullptr;
     const RowShape r = row_shape<DT>(to, a.V);
-    const bool together = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(to)) & 15u) == 0;
-    const int o1 = int(int64_t(r.octets) * (piece + 1) / a.pieces);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const RowGradient g = row_gradient<DT, MASKED>(a, row, z, mask);
+    const bool wide = (reinterpret_cast<uintptr_t>(to + r.head * kSize) & 31u) == 0;
+    const int o = int(int64_t(r.octets) * piece / a.pieces) + int(threadIdx.x), o1 = int(int64_t(r.octets) * (piece + 1) / a.pieces);
     const float it = a.inv_temperature;
-
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    uint32_t bits[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) bits[k] = o + 256 * k < o1 ? (MASKED ? octet_bits(mask, r.head, o + 256 * k) : 0xFFu) : 0u;
+    const RowInputs inputs = row_inputs(a, row);
+    const bool any = inputs.lse > -INFINITY && ((inputs.token >= 0 && inputs.d_logp != 0.f) || inputs.d_entropy != 0.f);
+    Logits8<DT> v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+        if (!MASKED) v[k].none();  // (with a mask, what is not read is masked)
+        if (!any) bits[k] = 0u;
+        const int first = r.head + 8 * (o + 256 * k);
+        if (TOGETHER && bits[k]) v[k].load(z, first);
+        if (!TOGETHER && bits[k]) v[k].load_anywhere(z, first);
+    }
+    const RowGradient g = row_gradient<DT, MASKED>(a, inputs, z, mask);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+        if (o + 256 * k >= o1) break;
+        const int first = r.head + 8 * (o + 256 * k);
+        float f[8], d[8];
+        v[k].settle(bits[k], MASKED);
+        v[k].get(f);
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) g.at_pair(f[j], f[j + 1], it, &d[j], &d[j + 1]);
+        if (uint32_t(g.token - first) < 8u) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (g.token == first + j) d[j] = g.at_token(f[j], it);
+        }
+        if constexpr (DT == kBF16) {
+            st_stream16(to + int64_t(first) * kSize,
+                        make_uint4(bf16_pair(d[0], d[1]), bf16_pair(d[2], d[3]), bf16_pair(d[4], d[5]), bf16_pair(d[6], d[7])));
+        } else {
+            const uint4 lo = make_uint4(__float_as_uint(d[0]), __float_as_uint(d[1]), __float_as_uint(d[2]), __float_as_uint(d[3]));
+            const uint4 hi = make_uint4(__float_as_uint(d[4]), __float_as_uint(d[5]), __float_as_uint(d[6]), __float_as_uint(d[7]));
+            if (wide) {
+                st_stream32(to + int64_t(first) * kSize, lo, hi);
+            } else {
+                st_stream16(to + int64_t(first) * kSize, lo);
+                st_stream16(to + int64_t(first) * kSize + 16, hi);
+            }
+        }
+    }
     if (piece == 0 && threadIdx.x < 16) {  // tokens beside the vectors
         const int i = int(threadIdx.x), token = i < 8 ? i : r.head + 8 * r.octets + i - 8;
         if (i < 8 ? i < r.head : i - 8 < r.tail) {
             float d = 0.f;
-            if (g.any && (!MASKED || ((ld_after_wait(mask + (token >> 3)) >> (token & 7)) & 1u))) {
+            if (any && (!MASKED || ((ld_after_wait(mask + (token >> 3)) >> (token & 7)) & 1u))) {
                 const float x = load_elem<DT>(z, token);
                 d = token == g.token ? g.at_token(x, it) : g.at(x, it);
             }
@@ -515,63 +716,6 @@ __global__ void __launch_bounds__(256) k_token_logprobs_backward(const LogprobsB
                 reinterpret_cast<uint16_t*>(to)[token] = uint16_t(bf16_pair(d, d));
             else
                 reinterpret_cast<float*>(to)[token] = d;
-        }
-    }
-    constexpr int kAhead = 4;
-    const bool wide = (reinterpret_cast<uintptr_t>(to + r.head * kSize) & 31u) == 0;
-#pragma unroll 1
-    for (int o = int(int64_t(r.octets) * piece / a.pieces) + int(threadIdx.x); o < o1; o += 256 * kAhead) {
-        uint32_t bits[kAhead];
-        Logits8<DT> v[kAhead];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) bits[k] = g.any && o + 256 * k < o1 ? (MASKED ? octet_bits(mask, r.head, o + 256 * k) : 0xFFu) : 0u;
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            v[k].none();
-            const int first = r.head + 8 * (o + 256 * k);
-            if (bits[k]) {
-                if (together) {
-                    v[k].load(z, first);
-                } else {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        w[j] = DT == kBF16 ? reinterpret_cast<const uint16_t*>(z)[first + j] : reinterpret_cast<const uint32_t*>(z)[first + j];
-                    if constexpr (DT == kBF16) {
-                        v[k].v = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
-                    } else {
-                        v[k].a = make_uint4(w[0], w[1], w[2], w[3]);
-                        v[k].b = make_uint4(w[4], w[5], w[6], w[7]);
-                    }
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            if (o + 256 * k >= o1) break;
-            const int first = r.head + 8 * (o + 256 * k);
-            float f[8], d[8];
-            v[k].values(bits[k], MASKED, f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = g.at(f[j], it);
-            if (uint32_t(g.token - first) < 8u) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (g.token == first + j) d[j] = g.at_token(f[j], it);
-            }
-            if constexpr (DT == kBF16) {
-                st_stream16(to + int64_t(first) * kSize,
-                            make_uint4(bf16_pair(d[0], d[1]), bf16_pair(d[2], d[3]), bf16_pair(d[4], d[5]), bf16_pair(d[6], d[7])));
-            } else {
-                const uint4 lo = make_uint4(__float_as_uint(d[0]), __float_as_uint(d[1]), __float_as_uint(d[2]), __float_as_uint(d[3]));
-                const uint4 hi = make_uint4(__float_as_uint(d[4]), __float_as_uint(d[5]), __float_as_uint(d[6]), __float_as_uint(d[7]));
-                if (wide) {
-                    st_stream32(to + int64_t(first) * kSize, lo, hi);
-                } else {
-                    st_stream16(to + int64_t(first) * kSize, lo);
-                    st_stream16(to + int64_t(first) * kSize + 16, hi);
-                }
-            }
         }
     }
 }

@@ -183,6 +183,17 @@ def test_rows_far_from_zero(offset):
         rows.check(rows.run(ctx, 10), 10)
 
 
+@pytest.mark.parametrize("t", [1e-6, 1e-3, 1e3, 1e6])
+def test_temperatures_far_from_one(t):
+    with Ctx([]) as ctx:
+        for dtype in (torch.bfloat16, torch.float32):
+            for density in (None, 0.3):
+                rows = Rows(4, 9001, dtype, density=density, t=t)
+                out = rows.run(ctx, 10)
+                rows.check(out, 10)
+                check_gradient(rows, backward(ctx, rows, out), out["lse"], out["entropy"], *rows.d)
+
+
 def test_rows_that_rise_and_fall():
     # the reference of a sum has to move, upwards from the start of the row or once at its end
     V = 60000
@@ -212,7 +223,7 @@ def test_only_what_is_asked_for_is_written():
 
 def test_offsets_behind_two_billion_elements():
     V, stride = 1000, (1 << 30) + 8
-    buffer = torch.empty(2 * stride + V, dtype=torch.bfloat16, device="cuda")
+    buffer = torch.empty(2 * stride + 3 * V, dtype=torch.bfloat16, device="cuda")
     rows = Rows(3, V)
     logits = rows.logits
     rows.logits = buffer.as_strided((3, V), (stride, 1))
@@ -221,11 +232,10 @@ def test_offsets_behind_two_billion_elements():
     with Ctx([]) as ctx:
         out = rows.run(ctx, 5)
         rows.check(out, 5)
-        d = torch.empty_like(logits)
+        d = buffer.as_strided((3, V), (stride, 1), 2 * V)
         cz.cfgzip_token_logprobs_backward(ctx.h, rows.logits, cz.BF16, stride, 3, V, None, 0, rows.tokens, 1.0, out["lse"], out["entropy"],
-                                          out["lse"], out["lse"], rows.logits, stride, torch.cuda.current_stream())
-        rows.logits, rows.stride = logits, V
-        check_gradient(rows, buffer.as_strided((3, V), (stride, 1)), out["lse"], out["entropy"], out["lse"], out["lse"])
+                                          out["lse"], out["lse"], d, stride, torch.cuda.current_stream())
+        check_gradient(rows, d, out["lse"], out["entropy"], out["lse"], out["lse"])
 
 
 # ---- the gradient -----------------------------------------------------------------------------------------------------------
@@ -256,13 +266,14 @@ def check_gradient(rows, got, lse, entropy, d_logp, d_entropy):
     has = (t >= 0) & (t < rows.V) & some
     has &= z.gather(1, t.clamp(0, rows.V - 1).unsqueeze(1)).squeeze(1) > -INF
     d = torch.where(has.unsqueeze(1), d, 0.0)
+    at = torch.arange(rows.N, device="cuda")[has]
+    rest = -torch.expm1(x[at, t[has]])  # 1 - p of the given tokens
     x = torch.where(p > 0, x, 0.0)
     want = -p * d - e * p * (x + H)
-    at = torch.arange(rows.N, device="cuda")[has]
-    want[at, t[has]] = -(d.squeeze(1)[has]) * torch.expm1(x[at, t[has]]) - (e * p * (x + H))[at, t[has]]
-    # p: its exponent is off by 2^-22 of itself, the exponential by a few units; the terms are added in 32 bits
-    tol = p * (d.abs() + e.abs() * (x.abs() + H)) * (2.0 ** -20 + x.abs() * 2.0 ** -21)
-    tol[at, t[has]] += d.squeeze(1)[has].abs() * (torch.expm1(x[at, t[has]]).abs() + p[at, t[has]] * x[at, t[has]].abs()) * 2.0 ** -21
+    want[at, t[has]] = d.squeeze(1)[has] * rest - (e * p * (x + H))[at, t[has]]
+    # p: its exponent is off by 2^-22 of itself, the exponential by a few units, and below 2^-126 it is 0; the terms are added in 32 bits
+    tol = (d.abs() + e.abs() * (x.abs() + H)) * (p * (2.0 ** -20 + x.abs() * 2.0 ** -21) + 2.0 ** -126)
+    tol[at, t[has]] += d.squeeze(1)[has].abs() * (rest.abs() + p[at, t[has]] * x[at, t[has]].abs()) * 2.0 ** -21
     tol = tol * it + (want * it).abs() * HALF[rows.dtype] + 1e-36
     assert got.isfinite().all()
     assert ((got.double() - want * it).abs() <= tol).all()
@@ -291,16 +302,23 @@ def test_gradient(N, V, pad, shift, dtype):
             check_gradient(rows, got, out["lse"], out["entropy"], None, d_entropy)
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-def test_gradient_in_the_place_of_the_logits(dtype):
+def test_gradient_of_tokens_that_have_no_probability():
+    # masked in place or not allowed by the mask: no part in the gradient, whichever of a row's blocks looks
+    N, V = 6, 60000
     with Ctx([]) as ctx:
-        rows = Rows(50, 10007, dtype, density=0.5)
-        out = rows.run(ctx)
-        want = backward(ctx, rows, out)
-        cz.cfgzip_token_logprobs_backward(ctx.h, rows.logits, CODE[dtype], rows.stride, rows.N, rows.V, rows.mask, rows.words, rows.tokens,
-                                          1.0, out["lse"], out["entropy"], rows.d[0], rows.d[1], rows.logits, rows.stride,
-                                          torch.cuda.current_stream())
-        assert torch.equal(rows.logits, want)
+        for dtype in (torch.bfloat16, torch.float32):
+            rows = Rows(N, V, dtype, density=0.5)
+            rows.allowed[torch.arange(N), rows.tokens.long()] = torch.arange(N, device="cuda") % 2 == 0
+            rows.allow(rows.allowed)
+            out = rows.run(ctx)
+            a = backward(ctx, rows, out)
+            check_gradient(rows, a, out["lse"], out["entropy"], *rows.d)
+            rows.logits.masked_fill_(~rows.allowed, -INF)
+            rows.mask = None
+            b = backward(ctx, rows, out, *rows.d)
+            assert torch.equal(a, b)
+            alone = backward(ctx, rows, out, d_logp=rows.d[0])
+            assert (alone[1::2] == 0).all() and (alone[::2] != 0).any(dim=1).all()
 
 
 def test_gradient_of_sure_tokens():

@@ -14,7 +14,7 @@ def forward(**change):
 
 def backward(**change):
     a = dict(ctx=None, logits=GOOD, dtype=cz.BF16, row_stride_elems=100, N=3, V=100, vocab_mask=None, vocab_stride_words=0, tokens=GOOD,
-             inv_temperature=1.0, lse=GOOD, entropy=GOOD, d_logp=GOOD, d_entropy=GOOD, d_logits=GOOD, d_stride_elems=100)
+             inv_temperature=1.0, lse=GOOD, entropy=GOOD, d_logp=GOOD, d_entropy=GOOD, d_logits=2 * GOOD, d_stride_elems=100)
     a.update(change)
     return status(cz.cfgzip_token_logprobs_backward, **a)
 
@@ -30,6 +30,7 @@ BOTH = [
     (dict(vocab_mask=GOOD, vocab_stride_words=3), cz.E_ARG),
     (dict(inv_temperature=0.0), cz.E_ARG),
     (dict(inv_temperature=-1.0), cz.E_ARG),
+    (dict(inv_temperature=1e-7), cz.E_ARG),
     (dict(inv_temperature=float("nan")), cz.E_ARG),
     (dict(inv_temperature=float("inf")), cz.E_ARG),
     (dict(inv_temperature=2e6), cz.E_ARG),
@@ -54,7 +55,7 @@ def test_arguments_of_the_log_probabilities():
 
 def test_arguments_of_their_gradient():
     for change in (dict(lse=None), dict(entropy=None), dict(d_logp=None, d_entropy=None), dict(tokens=None), dict(d_logits=None),
-                   dict(d_stride_elems=99)):
+                   dict(d_logits=GOOD), dict(d_stride_elems=99)):
         assert backward(**change) == cz.E_ARG, change
     assert backward(d_logits=GOOD + 1) == cz.E_ALIGN
     assert backward(d_logits=GOOD + 2, dtype=cz.F32) == cz.E_ALIGN
