@@ -84,6 +84,7 @@ struct LogprobsFinishArgs {
     int32_t* status;
 };
 __global__ void __launch_bounds__(256) k_head_logprobs_finish(const LogprobsFinishArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * kFinishRows + (lane & 3);
     const bool ends = warp == 0 && lane < kFinishRows && row < a.rows;

@@ -58,7 +58,9 @@ struct MmaArgs {
     int32_t add;
     // layer
     const void* bias;
-    int32_t bias_bf16, has_residual, has_slope;
+    const uint16_t* residual;
+    int64_t residual_stride;
+    int32_t bias_bf16, has_slope;
 };
 
 __device__ __forceinline__ void st_global32(void* p, const uint32_t (&v)[8]) {
@@ -278,55 +280,59 @@ __device__ __forceinline__ void out_columns(const MmaArgs& a, const CUtensorMap&
     if (lane == 0) tma_store3(&map, n, first, t.split, buffer);
 }
 
-// A layer's results, 64 columns of a warp's 32 rows at a time, straight from tensor memory. The residual comes by a tiled copy into the
-// buffer that y leaves from (a lane's own 16 bytes), the activation's derivative has a buffer of its own. The bias, the same for all
-// lanes, comes from the L1.
-template <int ACT>
-__device__ __forceinline__ bool layer_columns(const MmaArgs& a, const CUtensorMap& map_y, const CUtensorMap& map_residual,
-                                              const CUtensorMap& map_slope, int n, int first, int lane, uint32_t tmem, uint32_t buffer,
-                                              uint64_t* bar, uint32_t* phase) {
-    bool ok = true;
-    if (lane == 0) {
-        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (the copies before have read the buffers)
-        if (a.has_residual) {
-            mbar_expect_tx(bar, kMmaOut);
-            asm volatile(
-                "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(buffer),
-                "l"(&map_residual), "r"(n), "r"(first), "r"(smem_u32(bar))
-                : "memory");
-        }
+// A lane's part of the residual in 64 columns from n on: its row's 128 bytes. Asked for 64 columns ahead.
+struct LayerResidual {
+    uint4 v[8];
+    __device__ __forceinline__ void ask(const MmaArgs& a, int row, int n, int j) {
+        v[j] = make_uint4(0, 0, 0, 0);
+        if (a.residual && row < a.rows && n + 8 * j < a.cols)
+            v[j] = ld_after_wait(reinterpret_cast<const uint4*>(a.residual + int64_t(row) * a.residual_stride + n + 8 * j));
     }
-    __syncwarp();
+};
+
+// A layer's results, 64 columns of a warp's 32 rows at a time, straight from tensor memory. y and the activation's derivative leave by tiled
+// copies from a buffer each. The bias, the same for all lanes, comes from the L1.
+template <int ACT>
+__device__ __forceinline__ void layer_columns(const MmaArgs& a, const CUtensorMap& map_y, const CUtensorMap& map_slope, int n, int first,
+                                              int lane, uint32_t tmem, uint32_t buffer, LayerResidual& residual, int next) {
+    // (32 columns at a time: all loads, then all arithmetic, so that its chains run side by side, then all stores)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        uint32_t v[32];
+        uint32_t v[32], y[16], s[16];
+        float bias[4][8] = {};
         tmem_ld32(tmem + 32 * h, v);
+        if (a.bias) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (n + 32 * h + 8 * j < a.cols) bias_values(a.bias, a.bias_bf16, n + 32 * h + 8 * j, bias[j]);
+        }
         tmem_wait_ld();
-        if (h == 0 && a.has_residual) {
-            ok = ring_wait(bar, *phase) || (mbar_wait(bar, *phase) && false);
-            *phase ^= 1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float f[8], by[8], of[8];
+            bf16_values(residual.v[4 * h + j], of);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = activation<ACT>(__uint_as_float(v[8 * j + k]) + bias[j][k], &by[k]) + of[k];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                y[4 * j + k] = bf16_pair(f[2 * k], f[2 * k + 1]);
+                s[4 * j + k] = bf16_pair(by[2 * k], by[2 * k + 1]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) residual.ask(a, first + lane, next, 4 * h + j);
+        if (h == 0) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (the copies before have read the buffers)
+            __syncwarp();
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float f[8], s[8], bias[8] = {};
-            if (a.bias && n + 32 * h + 8 * j < a.cols) bias_values(a.bias, a.bias_bf16, n + 32 * h + 8 * j, bias);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = activation<ACT>(__uint_as_float(v[8 * j + k]) + bias[k], &s[k]);
             const uint32_t at = buffer + uint32_t(lane) * 128 + (uint32_t((4 * h + j) ^ (lane & 7)) << 4);
-            if (a.has_residual) {
-                uint4 r;
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(at) : "memory");
-                float of[8];
-                bf16_values(r, of);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) f[k] += of[k];
-            }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(bf16_pair(f[0], f[1])), "r"(bf16_pair(f[2], f[3])),
-                         "r"(bf16_pair(f[4], f[5])), "r"(bf16_pair(f[6], f[7]))
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(y[4 * j]), "r"(y[4 * j + 1]), "r"(y[4 * j + 2]), "r"(y[4 * j + 3])
                          : "memory");
             if (ACT != kActNone && a.has_slope)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + kMmaOut), "r"(bf16_pair(s[0], s[1])),
-                             "r"(bf16_pair(s[2], s[3])), "r"(bf16_pair(s[4], s[5])), "r"(bf16_pair(s[6], s[7]))
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + kMmaOut), "r"(s[4 * j]), "r"(s[4 * j + 1]),
+                             "r"(s[4 * j + 2]), "r"(s[4 * j + 3])
                              : "memory");
         }
     }
@@ -336,7 +342,6 @@ __device__ __forceinline__ bool layer_columns(const MmaArgs& a, const CUtensorMa
         tma_store3(&map_y, n, first, 0, buffer);
         if (ACT != kActNone && a.has_slope) tma_store3(&map_slope, n, first, 0, buffer + kMmaOut);
     }
-    return ok;
 }
 
 // D[rows, cols] = A B^T in tiles of 256 x width by pairs of blocks (each holds 128 rows of A and half of B's, and the sums of its 128
@@ -351,12 +356,11 @@ __device__ __forceinline__ bool layer_columns(const MmaArgs& a, const CUtensorMa
 // below that.
 template <bool A_MN, bool B_MN, int KIND, bool LONG>
 __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_out,
-                                             const CUtensorMap& map_residual, const CUtensorMap& map_slope) {
+                                             const CUtensorMap& map_slope) {
     constexpr bool kLayer = KIND >= kMmaLayer;
     constexpr int kStages = kLayer ? kLayerStagesTall : kMmaStages;
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2];
-    __shared__ __align__(8) uint64_t residual_full[kLayer ? 8 : 1];
     __shared__ __align__(8) uint64_t drained;
     __shared__ uint32_t s_tmem, s_end[2];  // (of either block: the stages it has asked for, and in the highest bit whether a wait ran out)
     constexpr bool kOut = KIND == kMmaSum || KIND == kMmaBf16;
@@ -377,8 +381,6 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
             mbar_init(&sums_empty[i], kTurns ? 8 : 16);  // four warps of either block (all eight)
         }
         mbar_init(&drained, 1);
-        if (kLayer)
-            for (int i = 0; i < 8; ++i) mbar_init(&residual_full[i], 1);
         mbar_init_fence();
         prefetch_tensor_map(&map_a);
         prefetch_tensor_map(&map_b);
@@ -512,24 +514,30 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
     } else if (warp >= 4) {
         const int set = (warp - 4) >> 2, quad = warp & 3;
         const uint32_t empty_bar = peer_shared(&sums_empty[set], 0);
-        uint32_t residual_phase = 0;
         int it = 0;
         for (int i = pair; i < tiles && ok; i += pairs, ++it) {
-            if ((it & 1) != set) continue;
+            // (a layer's last tile of a pair is shared: nothing else is left to do meanwhile)
+            const bool shared = kLayer && i + pairs >= tiles;
+            if ((it & 1) != set && !shared) continue;
             const MmaTile t = mma_tile(a, i);
             const int first = t.m * kMmaTile + int(rank) * 128 + quad * 32;
-            if (!ring_wait<true>(&sums_full[set], (it >> 1) & 1)) {
+            const int c0 = shared ? set * 128 : 0, c1 = shared ? c0 + 128 : kMmaTile;
+            LayerResidual residual;
+            if constexpr (kLayer) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) residual.ask(a, first + lane, t.n * kMmaTile + c0, j);
+            }
+            if (!ring_wait<true>(&sums_full[kLayer ? it & 1 : set], (it >> 1) & 1)) {
                 ok = false;
                 break;
             }
             tmem_fence_after();
             if constexpr (kLayer) {
 #pragma unroll 1
-                for (int n = t.n * a.width, c = 0; c < a.width && n < a.cols && first < a.rows; c += 64, n += 64)
-                    ok = layer_columns<KIND - kMmaLayer>(a, map_out, map_residual, map_slope, n, first, lane,
-                                                         tmem + set * 256 + c + (uint32_t(quad * 32) << 16),
-                                                         stages + kStages * 2 * kMmaHalf + uint32_t(warp - 4) * (2 * kMmaOut),
-                                                         &residual_full[kLayer ? warp - 4 : 0], &residual_phase) && ok;
+                for (int c = c0, n = t.n * kMmaTile + c0; c < c1 && n < a.cols && first < a.rows; c += 64, n += 64)
+                    layer_columns<KIND - kMmaLayer>(a, map_out, map_slope, n, first, lane, tmem + (it & 1) * 256 + c + (uint32_t(quad * 32) << 16),
+                                                    stages + kStages * 2 * kMmaHalf + uint32_t(warp - 4) * (2 * kMmaOut), residual,
+                                                    c + 64 < c1 ? n + 64 : a.cols);
             } else {
                 const bool add = a.add && first + lane < a.rows;
                 constexpr int kCols = kOutCols<KIND == kMmaBf16>;
@@ -550,7 +558,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
             }
             tmem_fence_before();
             __syncwarp();
-            if (lane == 0) arrive_at_peer(empty_bar);
+            if (lane == 0 && !shared) arrive_at_peer(empty_bar);
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
@@ -590,15 +598,14 @@ template <bool A_MN, bool B_MN, int KIND, bool LONG>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     k_head_mma(const __grid_constant__ MmaArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ CUtensorMap map_out) {
-    mma_products<A_MN, B_MN, KIND, LONG>(a, map_a, map_b, map_out, map_out, map_out);
+    mma_products<A_MN, B_MN, KIND, LONG>(a, map_a, map_b, map_out, map_out);
 }
 
 template <bool B_MN, int ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMmaThreads, 1)
     k_layer_mma(const __grid_constant__ MmaArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_residual,
-                const __grid_constant__ CUtensorMap map_slope) {
-    mma_products<false, B_MN, kMmaLayer + ACT, false>(a, map_a, map_b, map_y, map_residual, map_slope);
+                const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_slope) {
+    mma_products<false, B_MN, kMmaLayer + ACT, false>(a, map_a, map_b, map_y, map_slope);
 }
 
 }  // namespace cfgzip

@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 #include "cfgzip.h"
@@ -38,9 +39,12 @@ int check_matrix(const void* p, int64_t stride, int n) {
 constexpr int kGradientRuns = 64;  // runs of rows that the bias's gradient is summed over, at most
 int gradient_run(int32_t rows) { return std::max(64, up(ceil_div(rows, kGradientRuns), 32)); }
 
-// Cuts of the sum over rows in the weights' gradient, whose result is small where a layer is.
+// Cuts of the sum over rows in the weights' gradient, where its result has too few tiles to fill the pairs. Each cut is a result in 32 bits
+// written and read again, and a launch: not where the last of several rounds could be fuller (8192 rows of 4096 x 4096, whose 256 tiles take 3.5
+// rounds: 225 us in two cuts, 205 in one).
 int weight_cuts(const cfgzip_layer* l, int32_t rows) {
-    return cuts(int64_t(ceil_div(l->out, kMmaTile)) * ceil_div(l->in, kMmaTile), ceil_div(rows, kMmaK), int64_t(l->in) * l->out);
+    const int64_t tiles = int64_t(ceil_div(l->out, kMmaTile)) * ceil_div(l->in, kMmaTile);
+    return tiles > kPairs ? 1 : cuts(tiles, ceil_div(rows, kMmaK), int64_t(l->in) * l->out);
 }
 
 struct LayerSpace {
@@ -57,7 +61,7 @@ LayerSpace layer_space(const cfgzip_layer* l, int op, int32_t rows, void* worksp
     s.g = c.take<uint16_t>(l->activation == CFGZIP_ACT_NONE ? 0 : int64_t(rows) * l->out);
     s.sums = c.take<float>(int64_t(std::min(kGradientRuns, ceil_div(rows, 64))) * l->out);
     const int64_t tiles = int64_t(ceil_div(l->out, kMmaTile)) * ceil_div(l->in, kMmaTile);
-    const int most = std::min<int64_t>({kPairs, kCutTiles / tiles, ceil_div(rows, kMmaK) / 16});
+    const int most = tiles > kPairs ? 1 : std::min<int64_t>({kPairs, kCutTiles / tiles, ceil_div(rows, kMmaK) / 16});
     if (most > 1) s.parts = c.take<float>(int64_t(most) * l->in * l->out);
     s.bytes = c.used + 256;
     return s;
@@ -82,18 +86,37 @@ struct LayerProduct {
     int64_t slope_stride;
 };
 
-// Tiles of 128 features by `n` rows, each over a cluster of `blocks` blocks.
+// Tiles of 128 features by `n` rows, each over a cluster of `blocks` blocks with `stages` stages each.
 struct FewPlan {
-    int n, tiles, groups, blocks;
+    int n, tiles, groups, blocks, stages;
+    uint32_t stage_bytes;
+    double us;
 };
+// The number of blocks that takes the least time: rounds of clusters (not all SMs can be had four or eight at a time) times a block's stages
+// and what it takes besides, some 3 us. A stage is bound by its operands' way from the L2, 110 bytes a ns and SM. Blocks of few stages fit an
+// SM twice. (500 rows, 2568 -> 1032: 36 tiles by clusters of 4 take two rounds, 19.2 us, by clusters of 2 one, 9.5 us.)
 FewPlan few_plan(const cfgzip_ctx* ctx, const LayerProduct& p) {
-    FewPlan f;
+    FewPlan f{};
     f.n = p.rows >= 128 ? 128 : up(p.rows, 16);
     f.tiles = ceil_div(p.features, 128);
     f.groups = ceil_div(p.rows, f.n);
-    const int k_blocks = ceil_div(p.k, kMmaK);
-    f.blocks = 1;
-    while (f.blocks < kLayerBlocks && int64_t(f.tiles) * f.groups * (f.blocks + 1) <= ctx->sm_count && f.blocks + 1 <= k_blocks / 2) ++f.blocks;
+    f.stage_bytes = kLayerWeights + uint32_t(f.n) * 128;
+    const int k_blocks = ceil_div(p.k, kMmaK), most = std::min(kLayerStages, int((200u << 10) / f.stage_bytes));
+    const double clusters = double(f.tiles) * f.groups;
+    const int least = ceil_div(int64_t(f.n) * kLayerRow * 4, f.stage_bytes);  // what the sums take on their way out
+    for (int s = 1; s <= kLayerBlocks && (s == 1 || 2 * s <= k_blocks); ++s) {
+        const int steps = ceil_div(k_blocks, s), stages = std::max(std::min(most, steps), least);
+        const int twice = 2 * (size_t(stages) * f.stage_bytes + 2560) <= size_t(ctx->smem_optin) ? 2 : 1;
+        const int limit = s == 1 ? ctx->sm_count : ctx->cluster_limit[s] - (s == 3 || s == 5 ? 3 : 0);
+        if (limit <= 0) continue;
+        const double rounds = std::ceil(clusters / (double(limit) * twice));
+        const double beside = std::max(1.0, std::min(double(twice), clusters * s / ctx->sm_count));
+        const double us = rounds * (steps * beside * f.stage_bytes / 110e3 + 3.0 + 0.3 * s);
+        if (f.blocks && us >= f.us) continue;
+        f.blocks = s;
+        f.stages = stages;
+        f.us = us;
+    }
     return f;
 }
 
@@ -108,8 +131,8 @@ int run_few(cfgzip_ctx* ctx, const LayerProduct& p, const FewPlan& f, cudaStream
     a.features = p.features;
     a.N = f.n;
     a.k_blocks = ceil_div(p.k, kMmaK);
-    a.stage_bytes = kLayerWeights + uint32_t(f.n) * 128;
-    a.stages = std::min(kLayerStages, int((200u << 10) / a.stage_bytes));
+    a.stage_bytes = f.stage_bytes;
+    a.stages = f.stages;
     a.act = p.act;
     a.bias = p.bias;
     a.bias_bf16 = p.bias_bf16;
@@ -132,7 +155,7 @@ int run_few(cfgzip_ctx* ctx, const LayerProduct& p, const FewPlan& f, cudaStream
 
 template <bool B_MN, int ACT>
 int run_tall_as(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_y,
-                const CUtensorMap& map_residual, const CUtensorMap& map_slope, cudaStream_t st) {
+                const CUtensorMap& map_slope, cudaStream_t st) {
     auto kern = k_layer_mma<B_MN, ACT>;
     const size_t smem = size_t(kLayerStagesTall) * 2 * kMmaHalf + 1024 + 8 * 2 * kMmaOut;
     const int rc = ensure_smem(ctx, kern, smem);
@@ -140,7 +163,7 @@ int run_tall_as(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUt
     const int64_t tiles = int64_t(a.m_tiles) * a.n_tiles;
     if (tiles >= (int64_t(1) << 30)) return CFGZIP_E_RANGE;
     const unsigned pairs = unsigned(std::min<int64_t>(tiles, ctx->sm_count / 2));
-    return launch(ctx, kern, dim3(2 * pairs), dim3(kMmaThreads), smem, st, a, map_a, map_b, map_y, map_residual, map_slope);
+    return launch(ctx, kern, dim3(2 * pairs), dim3(kMmaThreads), smem, st, a, map_a, map_b, map_y, map_slope);
 }
 
 int run_tall(cfgzip_ctx* ctx, const LayerProduct& p, cudaStream_t st) {
@@ -158,42 +181,39 @@ int run_tall(cfgzip_ctx* ctx, const LayerProduct& p, cudaStream_t st) {
     a.ld = p.y_stride;
     a.bias = p.bias;
     a.bias_bf16 = p.bias_bf16;
-    a.has_residual = p.residual != nullptr;
+    a.residual = static_cast<const uint16_t*>(p.residual);
+    a.residual_stride = p.residual_stride;
     a.has_slope = p.slope != nullptr;
-    CUtensorMap map_a, map_b, map_y, map_residual, map_slope;
+    CUtensorMap map_a, map_b, map_y, map_slope;
     int rc;
     if ((rc = tensor_map(ctx, &map_a, p.a, p.rows, p.k, p.a_stride, 128)) != CFGZIP_OK ||
         (rc = p.turned ? tensor_map(ctx, &map_b, p.weight, p.k, p.features, p.weight_stride, 64)
                        : tensor_map(ctx, &map_b, p.weight, p.features, p.k, p.weight_stride, 128)) != CFGZIP_OK ||
         (rc = tensor_map_out(ctx, &map_y, a, true)) != CFGZIP_OK)
         return rc;
-    map_residual = map_slope = map_y;
-    if (p.residual && (rc = tensor_map(ctx, &map_residual, p.residual, p.rows, p.features, p.residual_stride, 32)) != CFGZIP_OK) return rc;
+    map_slope = map_y;
     if (p.slope) {
         MmaArgs s = a;
         s.out = p.slope;
         s.ld = p.slope_stride;
         if ((rc = tensor_map_out(ctx, &map_slope, s, true)) != CFGZIP_OK) return rc;
     }
-    if (p.turned) return run_tall_as<true, kActNone>(ctx, a, map_a, map_b, map_y, map_residual, map_slope, st);
+    if (p.turned) return run_tall_as<true, kActNone>(ctx, a, map_a, map_b, map_y, map_slope, st);
     switch (p.act) {
-        case CFGZIP_ACT_RELU: return run_tall_as<false, kActRelu>(ctx, a, map_a, map_b, map_y, map_residual, map_slope, st);
-        case CFGZIP_ACT_GELU: return run_tall_as<false, kActGelu>(ctx, a, map_a, map_b, map_y, map_residual, map_slope, st);
-        case CFGZIP_ACT_GELU_TANH: return run_tall_as<false, kActGeluTanh>(ctx, a, map_a, map_b, map_y, map_residual, map_slope, st);
-        case CFGZIP_ACT_SILU: return run_tall_as<false, kActSilu>(ctx, a, map_a, map_b, map_y, map_residual, map_slope, st);
-        default: return run_tall_as<false, kActNone>(ctx, a, map_a, map_b, map_y, map_residual, map_slope, st);
+        case CFGZIP_ACT_RELU: return run_tall_as<false, kActRelu>(ctx, a, map_a, map_b, map_y, map_slope, st);
+        case CFGZIP_ACT_GELU: return run_tall_as<false, kActGelu>(ctx, a, map_a, map_b, map_y, map_slope, st);
+        case CFGZIP_ACT_GELU_TANH: return run_tall_as<false, kActGeluTanh>(ctx, a, map_a, map_b, map_y, map_slope, st);
+        case CFGZIP_ACT_SILU: return run_tall_as<false, kActSilu>(ctx, a, map_a, map_b, map_y, map_slope, st);
+        default: return run_tall_as<false, kActNone>(ctx, a, map_a, map_b, map_y, map_slope, st);
     }
 }
 
 int run_product(cfgzip_ctx* ctx, const LayerProduct& p, cudaStream_t st) {
     const FewPlan f = few_plan(ctx, p);
-    const int k_blocks = ceil_div(p.k, kMmaK);
-    // Rounds of blocks (pairs of them) times what a stage of 64 k takes in each: a tile of 128 x 128 about 0.3 us, bound by its operands'
-    // way from the L2, a pair's of 256 x 256 0.4 us.
-    const int few_rounds = ceil_div(int64_t(f.tiles) * f.groups * f.blocks, ctx->sm_count);
+    // A stage of 64 k of a pair's 256 x 256 takes 0.4 us, and some 6 us are not covered by other tiles.
     const int tall_rounds = ceil_div(int64_t(ceil_div(p.rows, kMmaTile)) * ceil_div(p.features, kMmaTile), ctx->sm_count / 2);
-    const double few = few_rounds * (ceil_div(k_blocks, f.blocks) * 0.3 + 2.0), tall = tall_rounds * (k_blocks * 0.4) + 4.0;
-    if (p.rows > 128 && tall < few) return run_tall(ctx, p, st);
+    const double tall = tall_rounds * (ceil_div(p.k, kMmaK) * 0.4) + 6.0;
+    if (p.rows > 128 && tall < f.us) return run_tall(ctx, p, st);
     return p.turned ? run_few<true>(ctx, p, f, st) : run_few<false>(ctx, p, f, st);
 }
 
@@ -302,7 +322,7 @@ int cfgzip_layer_backward(cfgzip_ctx* ctx, const cfgzip_layer* layer, const void
         a.sums = d_bias ? w.sums : nullptr;
         const int runs = ceil_div(rows, a.run);
         if ((rc = launch(ctx, k_layer_gradient, dim3(unsigned(ceil_div(O, 256)), unsigned(runs)), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
-        if (d_bias && (rc = launch(ctx, k_layer_bias, dim3(unsigned(ceil_div(O, 256))), dim3(256), 0, st, (const float*)w.sums, runs, O, d_bias,
+        if (d_bias && (rc = launch(ctx, k_layer_bias, dim3(unsigned(ceil_div(O, 32))), dim3(256), 0, st, (const float*)w.sums, runs, O, d_bias,
                                    accumulate)) != CFGZIP_OK)
             return rc;
         if (acts) {

@@ -31,6 +31,11 @@ constexpr int kLayerStages = 12;                    // at most
 constexpr int kLayerBlocks = 8;                     // blocks of a cluster at most
 constexpr uint32_t kLayerWeights = 128 * 64 * 2;    // bytes of weights in a stage
 
+// Where the sums of a row's 128 features lie in shared memory: the first four of every eight side by side, the others behind them, so that 16
+// lanes that take eight each read 256 bytes at a time, and 32 that write one each write to all banks.
+constexpr int kLayerRow = 144;
+__device__ __forceinline__ int layer_place(int feature) { return (feature >> 3) * 4 + (feature & 3) + (feature & 4 ? 80 : 0); }
+
 // Eight features of a row: the sum, by way of the epilogue, to where it goes.
 template <int ACT>
 __device__ __forceinline__ void layer_finish(const LayerArgs& a, int row, int n, float (&f)[8], const float (&bias)[8], const float (&residual)[8]) {
@@ -51,7 +56,7 @@ __device__ __forceinline__ void layer_finish(const LayerArgs& a, int row, int n,
 // Sums stay in tensor memory over all of a block's k: what its additions cut off (1e-9 of the sum per element) is far below the rounding
 // of the result to bf16.
 template <bool A_MN>
-__global__ void __launch_bounds__(kLayerThreads, 1)
+__global__ void __launch_bounds__(kLayerThreads, 2)
     k_layer_few(const __grid_constant__ LayerArgs a, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x) {
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kLayerStages], empty[kLayerStages], done, drained;
@@ -78,21 +83,22 @@ __global__ void __launch_bounds__(kLayerThreads, 1)
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t tmem = s_tmem;
     bool ok = warp == 0 || !a.expire;  // (the hook: nothing is done with the first stages asked for)
     int asked = 0;
 
-    // this thread's results: eight features each, dealt over the blocks 256 at a time. What the first ones need besides the sums is asked
-    // for now.
-    const int items = rows * 16;
-    const int first = rank * kLayerThreads + int(threadIdx.x);
-    float bias[8] = {}, residual[8] = {};
-    auto ask = [&](int i) {
-        const int n = n0 + 8 * (i & 15), row = row0 + (i >> 4);
-        if (i >= items || n >= a.features) return;
-        if (a.bias) bias_values(a.bias, a.bias_bf16, n, bias);
-        if (a.residual) bf16_values(ld_after_wait(reinterpret_cast<const uint4*>(a.residual + int64_t(row) * a.residual_stride + n)), residual);
+    // This thread's results: eight features each, always the same ones, of every 16 * blocks-th row. What the next ones need besides the sums
+    // is asked for ahead.
+    const int first = (int(threadIdx.x) >> 4) * blocks + rank, step = blocks * (kLayerThreads / 16);
+    const int n = n0 + 8 * (int(threadIdx.x) & 15);
+    const bool mine = n < a.features;
+    float bias[8] = {};
+    uint4 next = make_uint4(0, 0, 0, 0);
+    auto ask = [&](int row) {
+        if (a.residual && mine && row < rows)
+            next = ld_after_wait(reinterpret_cast<const uint4*>(a.residual + int64_t(row0 + row) * a.residual_stride + n));
     };
 
     if (warp == 0) {
@@ -147,6 +153,7 @@ __global__ void __launch_bounds__(kLayerThreads, 1)
         if (elect_one()) mma_commit<1>(&done);
         __syncwarp();
     }
+    if (a.bias && mine && first < rows) bias_values(a.bias, a.bias_bf16, n, bias);
     ask(first);
     if (ok && !ring_wait(&done, 0)) ok = false;
     const bool failed = __syncthreads_or(!ok);
@@ -165,7 +172,7 @@ __global__ void __launch_bounds__(kLayerThreads, 1)
         __syncthreads();
     }
     tmem_fence_after();
-    // sums to shared memory, [row][128 features], over the stages: all copies have landed and all products have read them
+    // sums to shared memory, a row of features for each of the tile's, over the stages: all copies have landed and all products have read them
     float* const part = reinterpret_cast<float*>(base);
     for (int c = warp >> 2; c * 16 < a.N; c += 2) {
         uint32_t v[16];
@@ -174,7 +181,7 @@ __global__ void __launch_bounds__(kLayerThreads, 1)
         tmem_wait_ld();
         if (16 * c < rows) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) part[(16 * c + j) * 128 + (warp & 3) * 32 + lane] = k0 < k1 ? __uint_as_float(v[j]) : 0.f;
+            for (int j = 0; j < 16; ++j) part[(16 * c + j) * kLayerRow + layer_place((warp & 3) * 32 + lane)] = k0 < k1 ? __uint_as_float(v[j]) : 0.f;
         }
     }
     tmem_fence_before();
@@ -182,18 +189,19 @@ __global__ void __launch_bounds__(kLayerThreads, 1)
     if (warp == 2) tmem_free<1>(tmem, columns);
     __syncwarp();
     cluster_barrier();
-    if (!failed) {
-        for (int i = first; i < items; i += blocks * kLayerThreads) {
-            if (i != first) ask(i);
-            const int n = n0 + 8 * (i & 15), row = row0 + (i >> 4);
-            if (n >= a.features) continue;
+    if (!failed && mine) {
+        for (int row = first; row < rows; row += step) {
+            float residual[8];
+            bf16_values(next, residual);
+            ask(row + step);
+            // (each block begins with its own sums and goes round: all at the same block's, they would get an eighth of its speed each)
             uint4 v[kLayerBlocks][2];
 #pragma unroll
             for (int b = 0; b < kLayerBlocks; ++b)
                 if (b < blocks) {
-                    const uint32_t from = peer_shared(part + (i >> 4) * 128 + 8 * (i & 15), uint32_t(b));
+                    const uint32_t from = peer_shared(part + row * kLayerRow + ((n - n0) >> 1), uint32_t(rank + b < blocks ? rank + b : rank + b - blocks));
                     v[b][0] = ld_peer_v4(from);
-                    v[b][1] = ld_peer_v4(from + 16);
+                    v[b][1] = ld_peer_v4(from + 80 * sizeof(float));
                 }
             float f[8] = {};
 #pragma unroll
@@ -203,11 +211,11 @@ __global__ void __launch_bounds__(kLayerThreads, 1)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) f[j] += __uint_as_float(w[j]);
                 }
-            if (a.act == kActSilu) layer_finish<kActSilu>(a, row, n, f, bias, residual);
-            else if (a.act == kActGelu) layer_finish<kActGelu>(a, row, n, f, bias, residual);
-            else if (a.act == kActGeluTanh) layer_finish<kActGeluTanh>(a, row, n, f, bias, residual);
-            else if (a.act == kActRelu) layer_finish<kActRelu>(a, row, n, f, bias, residual);
-            else layer_finish<kActNone>(a, row, n, f, bias, residual);
+            if (a.act == kActSilu) layer_finish<kActSilu>(a, row0 + row, n, f, bias, residual);
+            else if (a.act == kActGelu) layer_finish<kActGelu>(a, row0 + row, n, f, bias, residual);
+            else if (a.act == kActGeluTanh) layer_finish<kActGeluTanh>(a, row0 + row, n, f, bias, residual);
+            else if (a.act == kActRelu) layer_finish<kActRelu>(a, row0 + row, n, f, bias, residual);
+            else layer_finish<kActNone>(a, row0 + row, n, f, bias, residual);
         }
     }
     __syncwarp();
@@ -227,6 +235,7 @@ struct LayerGradientArgs {
     float* sums;                  // [runs, features], nullable
 };
 __global__ void __launch_bounds__(256) k_layer_gradient(const LayerGradientArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ float sh[8][256 + 8];
     const int col = int(blockIdx.x) * 256 + int(threadIdx.x & 31) * 8, warp = threadIdx.x >> 5;
@@ -276,14 +285,22 @@ __global__ void __launch_bounds__(256) k_layer_gradient(const LayerGradientArgs 
     a.sums[int64_t(blockIdx.y) * a.features + c] = total;
 }
 
-// The sums of `parts`, added up; to f32, added to what is there where asked for.
+// The sums of `parts`, added up; to f32, added to what is there where asked for. A block takes 32 columns, a warp every eighth part.
 __global__ void __launch_bounds__(256) k_layer_bias(const float* sums, int parts, int features, float* d_bias, int accumulate) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int c = int(blockIdx.x) * 256 + int(threadIdx.x);
-    if (c >= features) return;
+    __shared__ float sh[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = int(blockIdx.x) * 32 + lane;
     float total = 0.f;
+    if (c < features) {
 #pragma unroll 8
-    for (int p = 0; p < parts; ++p) total += __ldcg(sums + int64_t(p) * features + c);
+        for (int p = warp; p < parts; p += 8) total += __ldcg(sums + int64_t(p) * features + c);
+    }
+    sh[warp][lane] = total;
+    __syncthreads();
+    if (warp || c >= features) return;
+#pragma unroll
+    for (int w = 1; w < 8; ++w) total += sh[w][lane];
     d_bias[c] = accumulate ? d_bias[c] + total : total;
 }
 
@@ -297,6 +314,7 @@ struct LayerRoundArgs {
     int32_t bf16, accumulate;
 };
 __global__ void __launch_bounds__(256) k_layer_round(const LayerRoundArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int vectors = a.n / 4;
     const int64_t total = int64_t(a.rows) * vectors;

@@ -69,6 +69,8 @@ class Layer:
         of, by = activation(self.act, h)
         want = of if residual is None else of + residual.double()
         tol = 1.13 * h_tol + of.abs() * 2.0 ** -19 + 2.0 ** -24 + want.abs() * HALF * 1.001
+        if self.act == "gelu":
+            tol = tol + h.abs() * 0.5 * 1.5e-7  # the approximation of erf
         assert ((y.double() - want).abs() <= tol).all()
         if slope is None:
             return
