@@ -50,14 +50,6 @@ __device__ __forceinline__ float activation(float h, float* slope) {
     return h;
 }
 
-__device__ __forceinline__ void bf16_values(const uint4& v, float (&f)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        f[2 * j] = __uint_as_float(w[j] << 16);
-        f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-    }
-}
 // Eight biases from feature n on (n and their number a multiple of 8).
 __device__ __forceinline__ void bias_values(const void* bias, bool bf16, int n, float (&f)[8]) {
     if (bf16) {

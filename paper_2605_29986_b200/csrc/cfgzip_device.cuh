@@ -299,6 +299,15 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {  // nearest,
     return r;
 }
 
+__device__ __forceinline__ void bf16_values(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f[2 * j] = __uint_as_float(w[j] << 16);
+        f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+    }
+}
+
 // Packed pairs of floats (sm_100 has two-wide fp32 multiply-add and add).
 __device__ __forceinline__ unsigned long long pack2(float lo, float hi) {
     unsigned long long p;

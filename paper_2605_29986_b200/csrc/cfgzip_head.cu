@@ -62,6 +62,9 @@ struct HeadSpace {
     int32_t piece, splits;  // tokens of a piece, cuts of the sum over them
     uint16_t* g;
     float* sums;
+    // ... of log probabilities
+    float *rest, *kept;
+    int32_t *first_of, *next_of;
     int64_t bytes;
 };
 
@@ -95,6 +98,12 @@ HeadSpace head_space(const cfgzip_head* h, int op, int32_t rows, void* workspace
         s.splits = cuts(ceil_div(n, kMmaTile) * across, s.piece / kMmaK, n * h->H);
         const int64_t most_cuts = std::max<int64_t>(1, std::min({int64_t(kPairs), kCutTiles / across, all / kMmaK / 16}));
         s.g = c.take<uint16_t>(std::max(std::min(n * all, room), n * kMmaTile));
+        if (op == CFGZIP_HEAD_LOGPROBS_BACKWARD) {
+            s.rest = c.take<float>(n);
+            s.next_of = c.take<int32_t>(n);
+            s.first_of = c.take<int32_t>(h->V);
+            s.kept = c.take<float>(n * h->H);
+        }
         s.sums = c.take<float>(std::max(n * h->H, std::min<int64_t>(n * h->H * most_cuts, int64_t(kCutTiles) * kMmaTile * kMmaTile)));
     }
     s.bytes = c.used + 256;
@@ -213,7 +222,7 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
         if ((rc = check_rows(head, hidden, hidden_stride)) != CFGZIP_OK) return rc;
         if (!workspace) return CFGZIP_E_ARG;
     }
-    const HeadSpace w = head_space(head, CFGZIP_HEAD_LOSS_BACKWARD, N, workspace);
+    const HeadSpace w = head_space(head, of.scores ? CFGZIP_HEAD_LOGPROBS_BACKWARD : CFGZIP_HEAD_LOSS_BACKWARD, N, workspace);
     if (N > 0 && workspace_bytes < w.bytes) return CFGZIP_E_NOMEM;
     if (!ctx) return CFGZIP_E_ARG;
     DeviceGuard guard(ctx->device);
@@ -232,6 +241,10 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
     CUtensorMap x_k, x_mn, w_k, w_mn, g_k, g_mn;
     if ((rc = tensor_map(ctx, &x_k, hidden, N, H, hidden_stride, 128)) != CFGZIP_OK ||
         (rc = tensor_map(ctx, &x_mn, hidden, N, H, hidden_stride, 64)) != CFGZIP_OK)
+        return rc;
+    const int32_t* targets = of.d_loss ? of.targets : nullptr;
+    if (of.scores && targets && (rc = launch(ctx, k_head_targets, dim3(unsigned(ceil_div(int64_t(head->V) + N, 256))), dim3(256), 0, st, targets, int(N),
+                                  int(head->V), w.first_of, w.next_of, w.rest)) != CFGZIP_OK)
         return rc;
     for (int32_t t0 = 0; t0 < head->V; t0 += w.piece) {
         const int32_t n = std::min(w.piece, head->V - t0);
@@ -258,6 +271,7 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
         a.d_loss = of.d_loss;
         a.entropy = of.entropy;
         a.d_entropy = of.d_entropy;
+        a.rest = w.rest;
         a.out = w.g;
         a.ld = w.piece;
         rc = of.scores ? run_mma<false, false, kMmaGradEntropy>(ctx, a, x_k, w_k, st) : run_mma<false, false, kMmaGrad>(ctx, a, x_k, w_k, st);
@@ -283,13 +297,49 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
             b.add = accumulate;
             const bool half = d_weight_dtype == CFGZIP_BF16;
             b.out = static_cast<char*>(d_weight) + int64_t(t0) * d_weight_stride * (half ? 2 : 4);
-            rc = half ? run_mma<true, true, kMmaBf16>(ctx, b, g_mn, x_mn, st) : run_mma<true, true, kMmaSum>(ctx, b, g_mn, x_mn, st);
+            b.t0 = t0;
+            b.first_of = w.first_of;
+            b.kept = w.kept;
+            if (of.scores && targets)
+                rc = half ? run_mma<true, true, kMmaBf16Targets>(ctx, b, g_mn, x_mn, st) : run_mma<true, true, kMmaSumTargets>(ctx, b, g_mn, x_mn, st);
+            else
+                rc = half ? run_mma<true, true, kMmaBf16>(ctx, b, g_mn, x_mn, st) : run_mma<true, true, kMmaSum>(ctx, b, g_mn, x_mn, st);
             if (rc != CFGZIP_OK) return rc;
         }
     }
-    if (!d_hidden) return CFGZIP_OK;
     const int splits = std::min(w.splits, ceil_div(std::min(w.piece, head->V), kMmaK));
     const int64_t blocks = std::min<int64_t>(ceil_div(int64_t(N) * (H / 4), 256), int64_t(ctx->sm_count) * 8);
+    if (of.scores && targets) {
+        WeightTargetsArgs t{};
+        t.targets = targets;
+        t.first_of = w.first_of;
+        t.next_of = w.next_of;
+        t.rest = w.rest;
+        t.kept = w.kept;
+        t.hidden = static_cast<const uint16_t*>(hidden);
+        t.hidden_stride = hidden_stride;
+        t.to = d_weight;
+        t.to_stride = d_weight_stride;
+        t.V = head->V;
+        t.H = H;
+        t.bf16 = d_weight_dtype == CFGZIP_BF16;
+        RoundTargetsArgs r{};
+        r.from = w.sums;
+        r.split_elems = int64_t(N) * H;
+        r.splits = splits;
+        r.rows = N;
+        r.n = H;
+        r.V = head->V;
+        r.to = static_cast<uint16_t*>(d_hidden);
+        r.to_stride = d_hidden_stride;
+        r.targets = targets;
+        r.rest = w.rest;
+        r.weight = static_cast<const uint16_t*>(head->weight);
+        r.weight_stride = head->row_stride;
+        const int rows = d_weight ? N : 0;
+        return launch(ctx, k_head_targets_finish, dim3(unsigned(rows + (d_hidden ? blocks : 0))), dim3(256), 0, st, t, r, rows);
+    }
+    if (!d_hidden) return CFGZIP_OK;
     return launch(ctx, k_head_round, dim3(unsigned(blocks)), dim3(256), 0, st, (const float*)w.sums, int64_t(N) * H, splits,
                   static_cast<uint16_t*>(d_hidden), d_hidden_stride, int(N), H);
 }

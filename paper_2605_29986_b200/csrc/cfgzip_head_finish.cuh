@@ -165,4 +165,116 @@ __global__ void __launch_bounds__(256) k_head_round(const float* from, int64_t s
     }
 }
 
+// k_head_round, with what the rows' targets were rounded by.
+struct RoundTargetsArgs {
+    const float* from;
+    int64_t split_elems;
+    int32_t splits, rows, n, V;
+    uint16_t* to;
+    int64_t to_stride;
+    const int32_t* targets;
+    const float* rest;
+    const uint16_t* weight;
+    int64_t weight_stride;
+};
+__device__ __forceinline__ void round_targets(const RoundTargetsArgs& a, int block, int blocks) {
+    const int vectors = a.n / 4;
+    const int64_t total = int64_t(a.rows) * vectors;
+    for (int64_t i = int64_t(block) * 256 + threadIdx.x; i < total; i += int64_t(blocks) * 256) {
+        const int64_t row = i / vectors;
+        const int col = 4 * int(i - row * vectors);
+        const int target = ld_after_wait(a.targets + row);
+        const float rest = ld_after_wait(a.rest + row);
+        float f[4] = {};
+#pragma unroll 8
+        for (int s = 0; s < a.splits; ++s) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(a.from + s * a.split_elems + 4 * i));
+            f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
+        }
+        if (target >= 0 && target < a.V && rest != 0.f) {
+            const uint2 w = *reinterpret_cast<const uint2*>(a.weight + int64_t(target) * a.weight_stride + col);
+            f[0] = fmaf(rest, __uint_as_float(w.x << 16), f[0]);
+            f[1] = fmaf(rest, __uint_as_float(w.x & 0xFFFF0000u), f[1]);
+            f[2] = fmaf(rest, __uint_as_float(w.y << 16), f[2]);
+            f[3] = fmaf(rest, __uint_as_float(w.y & 0xFFFF0000u), f[3]);
+        }
+        *reinterpret_cast<uint2*>(a.to + row * a.to_stride + col) = make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]));
+    }
+}
+
+// The rows that have a token for a target as a chain in the order of the rows: each token's first one (-1: none), each row's next one. A
+// thread a token, and behind them a thread a row, compares all targets, 1024 at a time from shared memory. Nothing is left of the targets
+// yet (rest 0). (4096 rows of 128256 tokens: some 20 us of a gradient of 9 ms; no order of arrival plays a part.)
+__global__ void __launch_bounds__(256) k_head_targets(const int32_t* targets, int N, int V, int32_t* first_of, int32_t* next_of, float* rest) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ __align__(16) int32_t sh[1024];
+    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    const int row = int(i - V), token = i < V ? int(i) : row < N ? ld_after_wait(targets + row) : -1;
+    const bool asks = token >= 0 && token < V;
+    const int after = i < V ? -1 : row;
+    int found = -1;
+    for (int n0 = 0; n0 < N; n0 += 1024) {
+        __syncthreads();
+        for (int k = threadIdx.x; k < 1024; k += 256) sh[k] = n0 + k < N ? ld_after_wait(targets + n0 + k) : -1;
+        __syncthreads();
+        const int here = min(1024, (N - n0 + 3) & ~3);
+        for (int k = 0; k < here && asks && found < 0; k += 4) {
+            const int4 t = *reinterpret_cast<const int4*>(sh + k);
+            if (t.x != token && t.y != token && t.z != token && t.w != token) continue;
+            const int n = n0 + k - after;  // (rows up to `after` do not count)
+            found = t.x == token && n > 0 ? n0 + k : t.y == token && n + 1 > 0 ? n0 + k + 1 : t.z == token && n + 2 > 0 ? n0 + k + 2
+                  : t.w == token && n + 3 > 0 ? n0 + k + 3 : -1;
+        }
+    }
+    if (i < V) {
+        first_of[i] = found;
+    } else if (row < N) {
+        next_of[row] = found;
+        rest[row] = 0.f;
+    }
+}
+
+// The rows of the head's gradient that are targets, once more: their sums as they were kept, and what their rows' g was rounded by times the
+// hidden states. A block a row of the text; the first row of a chain does all of it.
+struct WeightTargetsArgs {
+    const int32_t *targets, *first_of, *next_of;
+    const float *rest, *kept;
+    const uint16_t* hidden;
+    int64_t hidden_stride;
+    void* to;
+    int64_t to_stride;
+    int32_t V, H, bf16;
+};
+__device__ __forceinline__ void weight_targets(const WeightTargetsArgs& a, int row) {
+    const int target = ld_after_wait(a.targets + row);
+    if (target < 0 || target >= a.V || ld_after_wait(a.first_of + target) != row) return;
+    for (int c = 4 * int(threadIdx.x); c < a.H; c += 1024) {
+        const float4 sum = __ldcg(reinterpret_cast<const float4*>(a.kept + int64_t(row) * a.H + c));
+        float f[4] = {sum.x, sum.y, sum.z, sum.w};
+        for (int m = row; m >= 0; m = ld_after_wait(a.next_of + m)) {
+            const float rest = ld_after_wait(a.rest + m);
+            const uint2 x = *reinterpret_cast<const uint2*>(a.hidden + int64_t(m) * a.hidden_stride + c);
+            f[0] = fmaf(rest, __uint_as_float(x.x << 16), f[0]);
+            f[1] = fmaf(rest, __uint_as_float(x.x & 0xFFFF0000u), f[1]);
+            f[2] = fmaf(rest, __uint_as_float(x.y << 16), f[2]);
+            f[3] = fmaf(rest, __uint_as_float(x.y & 0xFFFF0000u), f[3]);
+        }
+        if (a.bf16)
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.to) + target * a.to_stride + c) = make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]));
+        else
+            *reinterpret_cast<float4*>(static_cast<float*>(a.to) + target * a.to_stride + c) = make_float4(f[0], f[1], f[2], f[3]);
+    }
+}
+
+// Both, one behind the other: the first `rows` blocks take a row's target each.
+__global__ void __launch_bounds__(256) k_head_targets_finish(const WeightTargetsArgs w, const RoundTargetsArgs r, int rows) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (int(blockIdx.x) < rows)
+        weight_targets(w, int(blockIdx.x));
+    else
+        round_targets(r, int(blockIdx.x) - rows, int(gridDim.x) - rows);
+}
+
 }  // namespace cfgzip

@@ -29,8 +29,14 @@ constexpr uint32_t kMmaHalf = 128 * kMmaK * 2;           // bytes of one operand
 constexpr size_t kMmaSmem = size_t(kMmaStages) * 2 * kMmaHalf + 1024;
 constexpr uint32_t kMmaOut = 32 * 128;                   // bytes a warp has on their way out: 32 rows of 128
 
-enum : int { kMmaLoss = 0, kMmaGrad = 1, kMmaSum = 2, kMmaBf16 = 3, kMmaStep = 4, kMmaLogprobs = 5, kMmaGradEntropy = 6,
-             kMmaLayer = 8 };  // (kMmaLayer and the activation)
+// Kinds of products: scores (of the loss, its gradient, a step, log probabilities, their gradient), sums in 32 bits or bf16, the same where the
+// sums of some rows are kept, and (kMmaLayer and the activation) a layer.
+enum : int { kMmaLoss = 0, kMmaGrad = 1, kMmaSum = 2, kMmaBf16 = 3, kMmaStep = 4, kMmaLogprobs = 5, kMmaGradEntropy = 6, kMmaSumTargets = 7,
+             kMmaBf16Targets = 8, kMmaLayer = 16 };
+template <int KIND>
+constexpr bool kMmaToBf16 = KIND == kMmaBf16 || KIND == kMmaBf16Targets;
+template <int KIND>
+constexpr bool kMmaOfSums = kMmaToBf16<KIND> || KIND == kMmaSum || KIND == kMmaSumTargets;
 
 struct MmaArgs {
     int32_t rows, cols;        // of the result (tokens x piece of the vocabulary, ...)
@@ -56,6 +62,9 @@ struct MmaArgs {
     int64_t ld;                // elements
     int64_t split_elems;
     int32_t add;
+    float* rest;               // gradient of log probabilities: [rows] what the targets' g was rounded by
+    const int32_t* first_of;   // sums of targets: [V] the first row with this target, or -1
+    float* kept;               // ... [rows of the text, cols] the sums of its row of the result, in 32 bits
     // layer
     const void* bias;
     const uint16_t* residual;
@@ -178,7 +187,9 @@ __device__ __forceinline__ void step_epilogue(const MmaArgs& a, const MmaTile& t
 // has all of its g in the small difference exp(z - lse) - 1: the scores are made as the loss makes them, portion by portion, so that z
 // here is the z in lse to the last bit, and the difference is not taken of a rounded exponential. The only token of a row gets 0.
 // With entropies (d is minus the gradient of the log probability then): g = p (d + b (x + entropy)) with x = z - lse and b minus the gradient
-// of the entropy, on the target d (p - 1) + p b (x + entropy). The entropy has its gradient in rows without a target too.
+// of the entropy, on the target d (p - 1) + p b (x + entropy). The entropy has its gradient in rows without a target too. What the target's g,
+// as a rule by far the largest of its row, loses in bf16 is kept, and added to the sums of the two products before they are rounded: of few
+// rows, whose targets' roundings do not even out, a gradient would be off by up to 2^-9 more.
 template <bool ENTROPY>
 __device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, const float (&z)[128],
                                               const uint32_t (&bits)[4]) {
@@ -212,7 +223,10 @@ __device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t
         for (int j = 0; j < 128; ++j) of_target = target == j ? z[j] : of_target;
         const float x = of_target - lse;
         of_target = d * expm1f(x);
-        if (ENTROPY) of_target = fmaf(ex2f(x * kLog2e) * b, x + entropy, of_target);
+        if (ENTROPY) {
+            of_target = fmaf(ex2f(x * kLog2e) * b, x + entropy, of_target);
+            if (target >= 0) a.rest[row] = of_target - __uint_as_float(bf16_pair(0.f, of_target) & 0xFFFF0000u);
+        }
     }
     uint16_t* p = static_cast<uint16_t*>(a.out) + int64_t(row) * a.ld + n0;
 #pragma unroll
@@ -249,9 +263,9 @@ __device__ __forceinline__ void tma_store3(const void* tensor_map, int x, int y,
 // long (gradient of 50021 x 1024 for 100 tokens: 50 us).
 template <bool BF16>
 constexpr int kOutCols = BF16 ? 64 : 32;  // columns in 128 bytes
-template <bool BF16>
+template <bool BF16, bool TARGETS>
 __device__ __forceinline__ void out_columns(const MmaArgs& a, const CUtensorMap& map, const MmaTile& t, int n, int first, int lane, bool add,
-                                            float* f, uint32_t buffer) {
+                                            int chain, float* f, uint32_t buffer) {
     constexpr int kCols = kOutCols<BF16>;
     if (add) {
         const char* from = static_cast<const char*>(a.out) + (t.split * a.split_elems + int64_t(first + lane) * a.ld + n) * (BF16 ? 2 : 4);
@@ -264,6 +278,12 @@ __device__ __forceinline__ void out_columns(const MmaArgs& a, const CUtensorMap&
             for (int k = 0; k < kCols / 8; ++k)
                 f[j * kCols / 8 + k] += __uint_as_float(BF16 ? (k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16) : w[k & 3]);
         }
+    }
+    if (TARGETS && chain >= 0) {  // (a row of some row's target: its sums once more, as they are)
+        float* p = a.kept + int64_t(chain) * a.cols + n;
+#pragma unroll
+        for (int j = 0; j < kCols / 4; ++j)
+            if (n + 4 * j < a.cols) *reinterpret_cast<float4*>(p + 4 * j) = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
     }
     uint32_t o[32];
 #pragma unroll
@@ -363,7 +383,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
     __shared__ __align__(8) uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2];
     __shared__ __align__(8) uint64_t drained;
     __shared__ uint32_t s_tmem, s_end[2];  // (of either block: the stages it has asked for, and in the highest bit whether a wait ran out)
-    constexpr bool kOut = KIND == kMmaSum || KIND == kMmaBf16;
+    constexpr bool kOut = kMmaOfSums<KIND>, kTargets = KIND == kMmaSumTargets || KIND == kMmaBf16Targets;
     constexpr int kPortion = kLayer ? 1 << 30 : kOut ? kMmaOutPortion : kMmaPortion;
     constexpr bool kTurns = !LONG;
     static_assert(kOut || kLayer || LONG, "scores are summed in portions");
@@ -473,6 +493,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
             const bool valid = row < a.rows;
             uint32_t bits[4];
             if (!kOut) tile_mask(a, t, valid ? row : a.rows - 1, t.n * a.width + 128 * half, bits);
+            const int chain = kTargets && valid ? ld_after_wait(a.first_of + a.t0 + row) : -1;
             float sums[128] = {};
             for (int k = t.k0; k < t.k1; k += kPortion, ++it) {
                 if (!ring_wait<true>(&sums_full[it & 1], (it >> 1) & 1)) {
@@ -500,12 +521,12 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
             if (ok && KIND == kMmaGradEntropy) grad_epilogue<true>(a, t, half, row, valid, sums, bits);
             if (ok && kOut && row - lane < a.rows) {
                 const bool add = a.add && valid;
-                constexpr int kCols = kOutCols<KIND == kMmaBf16>;
+                constexpr int kCols = kOutCols<kMmaToBf16<KIND>>;
 #pragma unroll
                 for (int c = 0; c < 128 / kCols; ++c) {
                     const int n = t.n * kMmaTile + 128 * half + kCols * c;
                     if (n >= a.cols) break;
-                    out_columns<KIND == kMmaBf16>(a, map_out, t, n, row - lane, lane, add, sums + kCols * c,
+                    out_columns<kMmaToBf16<KIND>, kTargets>(a, map_out, t, n, row - lane, lane, add, chain, sums + kCols * c,
                                                   stages + kStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
                 }
             }
@@ -527,6 +548,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
 #pragma unroll
                 for (int j = 0; j < 8; ++j) residual.ask(a, first + lane, t.n * kMmaTile + c0, j);
             }
+            const int chain = kTargets && first + lane < a.rows ? ld_after_wait(a.first_of + a.t0 + first + lane) : -1;
             if (!ring_wait<true>(&sums_full[kLayer ? it & 1 : set], (it >> 1) & 1)) {
                 ok = false;
                 break;
@@ -540,7 +562,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
                                                     c + 64 < c1 ? n + 64 : a.cols);
             } else {
                 const bool add = a.add && first + lane < a.rows;
-                constexpr int kCols = kOutCols<KIND == kMmaBf16>;
+                constexpr int kCols = kOutCols<kMmaToBf16<KIND>>;
 #pragma unroll 1
                 for (int n = t.n * kMmaTile, c = 0; c < kMmaTile && n < a.cols && first < a.rows; c += kCols, n += kCols) {
                     float f[kCols];
@@ -553,7 +575,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
 #pragma unroll
                         for (int j = 0; j < 32; ++j) f[h + j] = __uint_as_float(v[j]);
                     }
-                    out_columns<KIND == kMmaBf16>(a, map_out, t, n, first, lane, add, f, stages + kStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
+                    out_columns<kMmaToBf16<KIND>, kTargets>(a, map_out, t, n, first, lane, add, chain, f, stages + kStages * 2 * kMmaHalf + uint32_t(warp - 4) * kMmaOut);
                 }
             }
             tmem_fence_before();

@@ -106,7 +106,7 @@ inline int tensor_map_out(cfgzip_ctx* ctx, CUtensorMap* map, const MmaArgs& a, b
 
 template <bool A_MN, bool B_MN, int KIND, bool LONG = true>
 int run_mma(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUtensorMap& map_b, cudaStream_t st) {
-    constexpr bool kOut = KIND == kMmaSum || KIND == kMmaBf16;
+    constexpr bool kOut = kMmaOfSums<KIND>;
     a.splits = std::max(1, a.splits);
     if constexpr (kOut && LONG)
         if (ceil_div(a.k_blocks, a.splits) <= kMmaOutPortion) return run_mma<A_MN, B_MN, KIND, false>(ctx, a, map_a, map_b, st);
@@ -118,7 +118,7 @@ int run_mma(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUtenso
     auto kern = k_head_mma<A_MN, B_MN, KIND, LONG>;
     const size_t smem = kMmaSmem + (kOut ? 8 * kMmaOut : 0);
     CUtensorMap map_out = map_a;
-    int rc = kOut ? tensor_map_out(ctx, &map_out, a, KIND == kMmaBf16) : CFGZIP_OK;
+    int rc = kOut ? tensor_map_out(ctx, &map_out, a, kMmaToBf16<KIND>) : CFGZIP_OK;
     if (rc != CFGZIP_OK || (rc = ensure_smem(ctx, kern, smem)) != CFGZIP_OK) return rc;
     const int64_t tiles = int64_t(a.m_tiles) * a.n_tiles * a.splits;
     if (tiles >= (int64_t(1) << 30)) return CFGZIP_E_RANGE;

@@ -6,7 +6,7 @@ import synth
 from paper_2605_29986_b200 import binding as cz
 from _gpu_util import Ctx, dev
 from _head_util import Case, class_masks, pack, unpack
-from test_gpu_head import LOSSES, close, loss_inputs, run_backward, run_loss, words
+from test_gpu_head import LOSSES, close, loss_inputs, run_loss, words
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -112,11 +112,35 @@ def test_gradient(V, H, N, density, pad):
             assert (d_hidden[:, H:] == 77.0).all() and (d_weight[:, H:] == 77.0).all()
             assert close(d_hidden[:, :H], g @ case.w64, g, g_tol, case.w64, V)
             assert close(d_weight[:, :H], g.T @ case.x64, g.T, g_tol.T, case.x64, N, before)
-        # without entropies it is the gradient of the loss, the other way round
-        a, b = torch.zeros((N, H), dtype=torch.bfloat16, device="cuda"), torch.zeros((N, H), dtype=torch.bfloat16, device="cuda")
-        run_gradient(ctx, case, packed, tokens, lse, None, d_logp, None, a, None)
-        run_backward(ctx, case, packed, tokens, lse, -d_logp, b, None)
-        assert torch.equal(a, b)
+        # either one alone is the same
+        g, g_tol = gradient(case, mask, tokens, d_logp, d_entropy)
+        alone = torch.full((N, H), 77.0, dtype=torch.bfloat16, device="cuda"), torch.zeros((V, H), device="cuda")
+        both = torch.zeros_like(alone[0]), torch.zeros_like(alone[1])
+        run_gradient(ctx, case, packed, tokens, lse, entropy, d_logp, d_entropy, alone[0], None)
+        run_gradient(ctx, case, packed, tokens, lse, entropy, d_logp, d_entropy, None, alone[1])
+        run_gradient(ctx, case, packed, tokens, lse, entropy, d_logp, d_entropy, *both)
+        assert torch.equal(alone[0], both[0]) and torch.equal(alone[1], both[1])
+
+
+@pytest.mark.parametrize("V,H,N", [(300, 64, 1), (5003, 256, 9), (2000, 1032, 300), (40, 64, 1000), (27001, 64, 5003)])
+def test_what_the_targets_were_rounded_by_is_not_lost(V, H, N):
+    """Weights and hidden states that tell the terms of a gradient apart: what a target's g loses in bf16 comes back in 32 bits (several rows
+    may have the same target)."""
+    case, mask, packed, tokens = loss_inputs(V, H, N, None, 0, seed=11)
+    d_logp = torch.rand(N, generator=case.gen, device="cuda") + 0.5
+    with Ctx([]) as ctx:
+        _, _, lse = run(ctx, case, packed, tokens)
+        d_weight = torch.zeros((V, H), device="cuda")
+        d_hidden = torch.zeros((N, H), dtype=torch.bfloat16, device="cuda")
+        run_gradient(ctx, case, packed, tokens, lse, None, d_logp, None, d_hidden, d_weight)
+        g, g_tol = gradient(case, mask, tokens, d_logp, None)
+        rows, t = torch.arange(N, device="cuda"), tokens.long().clamp(0, V - 1)
+        has = (tokens >= 0) & (tokens < V)
+        # (the tolerance of a target's g, without its rounding to bf16: twice a rounding in 32 bits)
+        at = rows[has], t[has]
+        g_tol[at] -= g[at].abs() * (2.0 ** -8 - 2.0 ** -23)
+        assert close(d_weight, g.T @ case.x64, g.T, g_tol.T, case.x64, N)
+        assert close(d_hidden, g @ case.w64, g, g_tol, case.w64, V)
 
 
 def test_gradient_in_several_pieces_of_the_vocabulary():
