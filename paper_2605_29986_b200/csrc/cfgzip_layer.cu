@@ -319,10 +319,16 @@ int cfgzip_layer_backward(cfgzip_ctx* ctx, const cfgzip_layer* layer, const void
         a.slope = acts ? static_cast<const uint16_t*>(slope) : nullptr;
         a.slope_stride = slope_stride;
         a.g = w.g;
-        a.sums = d_bias ? w.sums : nullptr;
-        const int runs = ceil_div(rows, a.run);
-        if ((rc = launch(ctx, k_layer_gradient, dim3(unsigned(ceil_div(O, 256)), unsigned(runs)), dim3(256), 0, st, a)) != CFGZIP_OK) return rc;
-        if (d_bias && (rc = launch(ctx, k_layer_bias, dim3(unsigned(ceil_div(O, 32))), dim3(256), 0, st, (const float*)w.sums, runs, O, d_bias,
+        a.runs = ceil_div(rows, a.run);
+        const bool one = a.runs <= kGradientCluster;
+        a.sums = d_bias && !one ? w.sums : nullptr;
+        a.d_bias = one ? d_bias : nullptr;
+        a.accumulate = accumulate;
+        ctx->cluster_now = a.d_bias ? a.runs : 1;
+        rc = launch(ctx, k_layer_gradient, dim3(unsigned(ceil_div(O, 256) * a.runs)), dim3(256), 0, st, a);
+        ctx->cluster_now = 1;
+        if (rc != CFGZIP_OK) return rc;
+        if (a.sums && (rc = launch(ctx, k_layer_bias, dim3(unsigned(ceil_div(O, 32))), dim3(256), 0, st, (const float*)w.sums, a.runs, O, d_bias,
                                    accumulate)) != CFGZIP_OK)
             return rc;
         if (acts) {

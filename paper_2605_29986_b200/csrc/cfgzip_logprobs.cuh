@@ -310,17 +310,19 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
     const int c1 = int(int64_t(chunks) * (rank + 1) / blocks);
     const uint32_t chunk_at = peer_shared(s_chunk, 0);
     if (threadIdx.x == 0) s_listed = s_picked = 0;
-    cluster_barrier();  // (the first block is there to be written to)
+    cluster_arrive();
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // the given token's logit, asked for ahead
     int token = -1;
     float of_token = -INFINITY;
-    if (rank == 0 && threadIdx.x == 0 && a.tokens) {
+    if (rank == 0 && threadIdx.x == 32 && a.tokens) {
         token = ld_after_wait(a.tokens + row);
         if (token >= 0 && token < a.V && (!MASKED || ((ld_after_wait(mask + (token >> 3)) >> (token & 7)) & 1u))) of_token = load_elem<DT>(z, token);
     }
 
+    __syncwarp();
+    cluster_wait();  // (the first block is there to be written to)
     EntropySums sums(scale);
     float most = kNone;
     // tokens beside the vectors
@@ -430,7 +432,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
     cluster_barrier();
     if (rank != 0) return;
 
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 32) {  // (the second warp, while the first looks for the alternatives)
         float m = kFew;
         for (int b = 0; b < blocks; ++b) m = fmaxf(m, s_block[b].x);
         const float to = rintf(m * scale);
