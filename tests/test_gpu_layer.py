@@ -85,7 +85,7 @@ SHAPES = [
     (1, 8, 8, 0), (1, 64, 40, 8), (2, 72, 128, 0), (15, 128, 136, 8), (16, 256, 256, 0), (17, 200, 264, 0), (31, 1000, 128, 8),
     (32, 2048, 512, 0), (33, 520, 1032, 0), (64, 4096, 128, 0), (100, 328, 2056, 8), (128, 512, 384, 0), (129, 512, 384, 8),
     (200, 1024, 256, 0), (257, 72, 1000, 0), (1, 4096, 4096, 0), (3, 8192, 200, 0), (500, 1032, 2568, 8), (1500, 264, 520, 0),
-    (3000, 1024, 1032, 8), (5000, 512, 768, 0), (9001, 136, 264, 0), (2049, 4104, 520, 0), (20000, 8, 8, 0),
+    (3000, 1024, 1032, 8), (5000, 512, 768, 0), (9001, 136, 264, 0), (2049, 4104, 520, 0), (20000, 8, 8, 0), (4000, 2056, 2312, 8), (1800, 5000, 1024, 0),
 ]
 
 
