@@ -49,7 +49,8 @@ enum {
     CFGZIP_E_PARTITION = -3, /* c / r do not describe a partition (see cfgzip_check_partition) */
     CFGZIP_E_ALIGN = -4,     /* rows that must be 16-byte aligned are not: logits of cfgzip_multi_mask_logsoftmax_argmax and
                                 cfgzip_rmw_floor (every other call takes logits rows that start anywhere), and the weights,
-                                scales, hidden states and their gradients of the cfgzip_head calls */
+                                scales, hidden states and their gradients of the cfgzip_head calls, the matrices of the
+                                cfgzip_layer calls, logits of cfgzip_token_logprobs that do not start on an element */
     CFGZIP_E_CUDA = -5,      /* a CUDA runtime call failed (no device, launch error) */
     CFGZIP_E_NOMEM = -6      /* device allocation failed, or B exceeds the reserved rows */
 };
@@ -421,7 +422,8 @@ int cfgzip_head_logprobs(cfgzip_ctx* ctx, const cfgzip_head* head, const void* h
  * has no part in rows whose logp is not a finite function of z, a row with nothing allowed has none):
  *   d_hidden[n, :] = sum_t g[n, t] * weight[t, :],    d_weight[t, :] = sum_n g[n, t] * hidden[n, :]
  * The scores are computed again, the same to the last bit, and g is rounded to bf16, as in cfgzip_head_loss_backward; what is said there of
- * accuracy, and of weights and hidden states that have to be finite where g is 0, holds here.
+ * accuracy, and of weights and hidden states that have to be finite where g is 0, holds here. Only what the given token's g is rounded by,
+ * as a rule by far the largest of its row, is added to the sums of both products in 32 bits.
  *   lse, entropy       : as cfgzip_head_logprobs returned them (entropy NULL where d_entropy is)
  *   d_logp, d_entropy  : dev float [N], one of them nullable (tokens too where d_logp is)
  *   the others         : as in cfgzip_head_loss_backward (the workspace of CFGZIP_HEAD_LOGPROBS_BACKWARD)
@@ -464,7 +466,7 @@ int cfgzip_layer_workspace(const cfgzip_layer* layer, int op, int32_t rows, int6
  *   residual : nullable dev bf16 [rows, residual_stride]; may be x (where in = out)
  *   y        : dev bf16 [rows, y_stride] (written); may be the residual with the same stride unless that is x; overlaps nothing else
  *   slope    : nullable dev bf16 [rows, slope_stride] (written): the activation's derivative, which is what the gradient needs of the
- *              forward pass (rounded to bf16, 2^-9 of itself: the gradient's own factor is rounded no finer)
+ *              forward pass (rounded to bf16, 2^-8 of itself: the gradient's own factor is rounded no finer)
  */
 int cfgzip_layer_forward(cfgzip_ctx* ctx, const cfgzip_layer* layer, const void* x, int64_t x_stride, int32_t rows, const void* residual,
                          int64_t residual_stride, void* y, int64_t y_stride, void* slope, int64_t slope_stride, void* workspace,
@@ -682,7 +684,7 @@ int cfgzip_launch_count(cfgzip_ctx* ctx, int64_t* out);
  *                  for an asynchronous copy as run out AFTER the wait has completed, so that the error path
  *                  (flag, bounded drain of the copies in flight, cfgzip_poll_status -> CFGZIP_E_CUDA) can be
  *                  exercised with nothing left in flight; the results of such a call are undefined. The
- *                  products of the cfgzip_head calls report theirs when their first stages are asked for
+ *                  products of the cfgzip_head and cfgzip_layer calls report theirs when their first stages are asked for
  *   "spread"       1 = launches of at most one block per SM (the streaming kernel of a small batch, the per-row
  *                  kernels of 32 to 148 rows) ask for more than half of an SM's shared memory, so that two of
  *                  their blocks never share an SM (default), 0 = only what the block needs

@@ -189,7 +189,7 @@ __device__ __forceinline__ void step_epilogue(const MmaArgs& a, const MmaTile& t
 // With entropies (d is minus the gradient of the log probability then): g = p (d + b (x + entropy)) with x = z - lse and b minus the gradient
 // of the entropy, on the target d (p - 1) + p b (x + entropy). The entropy has its gradient in rows without a target too. What the target's g,
 // as a rule by far the largest of its row, loses in bf16 is kept, and added to the sums of the two products before they are rounded: of few
-// rows, whose targets' roundings do not even out, a gradient would be off by up to 2^-9 more.
+// rows, whose targets' roundings do not even out, a gradient would be off by up to 2^-8 of itself more.
 template <bool ENTROPY>
 __device__ __forceinline__ void grad_epilogue(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, const float (&z)[128],
                                               const uint32_t (&bits)[4]) {
