@@ -243,8 +243,8 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
         (rc = tensor_map(ctx, &x_mn, hidden, N, H, hidden_stride, 64)) != CFGZIP_OK)
         return rc;
     const int32_t* targets = of.d_loss ? of.targets : nullptr;
-    if (of.scores && targets && (rc = launch(ctx, k_head_targets, dim3(unsigned(ceil_div(int64_t(head->V) + N, 256))), dim3(256), 0, st, targets, int(N),
-                                  int(head->V), w.first_of, w.next_of, w.rest)) != CFGZIP_OK)
+    if (of.scores && targets && (rc = launch(ctx, k_head_targets, dim3(unsigned(ceil_div(N, 8 * kTargetRows))), dim3(256), 0, st, targets, int(N),
+                                                    int(head->V), w.first_of, w.next_of, w.rest)) != CFGZIP_OK)
         return rc;
     for (int32_t t0 = 0; t0 < head->V; t0 += w.piece) {
         const int32_t n = std::min(w.piece, head->V - t0);
@@ -298,6 +298,8 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
             const bool half = d_weight_dtype == CFGZIP_BF16;
             b.out = static_cast<char*>(d_weight) + int64_t(t0) * d_weight_stride * (half ? 2 : 4);
             b.t0 = t0;
+            b.targets = targets;
+            b.text_rows = N;
             b.first_of = w.first_of;
             b.kept = w.kept;
             if (of.scores && targets)

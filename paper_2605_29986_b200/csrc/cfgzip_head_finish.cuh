@@ -202,36 +202,48 @@ __device__ __forceinline__ void round_targets(const RoundTargetsArgs& a, int blo
     }
 }
 
-// The rows that have a token for a target as a chain in the order of the rows: each token's first one (-1: none), each row's next one. A
-// thread a token, and behind them a thread a row, compares all targets, 1024 at a time from shared memory. Nothing is left of the targets
-// yet (rest 0). (4096 rows of 128256 tokens: some 20 us of a gradient of 9 ms; no order of arrival plays a part.)
+// The rows that have a token for a target as a chain in the order of the rows: the first row of each token that is a target, each row's next
+// one. A warp compares its four rows' targets with all others, 32 at a time; no order of arrival plays a part. Tokens that are no target keep
+// what the workspace held before: whoever asks for a token's first row looks whether that row has it (first_row), which spares writing, and
+// searching for, all of the vocabulary's. Nothing is left of the targets yet (rest 0).
+constexpr int kTargetRows = 4;
 __global__ void __launch_bounds__(256) k_head_targets(const int32_t* targets, int N, int V, int32_t* first_of, int32_t* next_of, float* rest) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    __shared__ __align__(16) int32_t sh[1024];
-    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    const int row = int(i - V), token = i < V ? int(i) : row < N ? ld_after_wait(targets + row) : -1;
-    const bool asks = token >= 0 && token < V;
-    const int after = i < V ? -1 : row;
-    int found = -1;
-    for (int n0 = 0; n0 < N; n0 += 1024) {
-        __syncthreads();
-        for (int k = threadIdx.x; k < 1024; k += 256) sh[k] = n0 + k < N ? ld_after_wait(targets + n0 + k) : -1;
-        __syncthreads();
-        const int here = min(1024, (N - n0 + 3) & ~3);
-        for (int k = 0; k < here && asks && found < 0; k += 4) {
-            const int4 t = *reinterpret_cast<const int4*>(sh + k);
-            if (t.x != token && t.y != token && t.z != token && t.w != token) continue;
-            const int n = n0 + k - after;  // (rows up to `after` do not count)
-            found = t.x == token && n > 0 ? n0 + k : t.y == token && n + 1 > 0 ? n0 + k + 1 : t.z == token && n + 2 > 0 ? n0 + k + 2
-                  : t.w == token && n + 3 > 0 ? n0 + k + 3 : -1;
+    const int lane = int(threadIdx.x) & 31, r0 = kTargetRows * (int(blockIdx.x) * 8 + int(threadIdx.x >> 5));
+    if (r0 >= N) return;
+    int mine[kTargetRows], next[kTargetRows];
+    bool before[kTargetRows];
+#pragma unroll
+    for (int j = 0; j < kTargetRows; ++j) {
+        mine[j] = r0 + j < N ? ld_after_wait(targets + r0 + j) : -1;
+        next[j] = INT_MAX;
+        before[j] = false;
+    }
+    for (int n0 = 0; n0 < N; n0 += 128) {
+        int other[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) other[q] = n0 + 32 * q + lane < N ? ld_after_wait(targets + n0 + 32 * q + lane) : -1;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int n = n0 + 32 * q + lane;
+#pragma unroll
+            for (int j = 0; j < kTargetRows; ++j) {
+                const bool same = other[q] == mine[j];
+                before[j] |= same && n < r0 + j;
+                if (same && n > r0 + j) next[j] = min(next[j], n);
+            }
         }
     }
-    if (i < V) {
-        first_of[i] = found;
-    } else if (row < N) {
-        next_of[row] = found;
-        rest[row] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kTargetRows; ++j) {
+        const int found = __reduce_min_sync(0xFFFFFFFFu, next[j]);
+        const bool first = !__any_sync(0xFFFFFFFFu, before[j]);
+        if (lane == 0 && r0 + j < N) {
+            next_of[r0 + j] = found < N ? found : -1;
+            rest[r0 + j] = 0.f;
+            if (first && mine[j] >= 0 && mine[j] < V) first_of[mine[j]] = r0 + j;
+        }
     }
 }
 

@@ -63,7 +63,8 @@ struct MmaArgs {
     int64_t split_elems;
     int32_t add;
     float* rest;               // gradient of log probabilities: [rows] what the targets' g was rounded by
-    const int32_t* first_of;   // sums of targets: [V] the first row with this target, or -1
+    const int32_t* first_of;   // sums of targets: [V] the first row with this target; anything where there is none
+    int32_t text_rows;         // ... of the text, with their targets
     float* kept;               // ... [rows of the text, cols] the sums of its row of the result, in 32 bits
     // layer
     const void* bias;
@@ -76,6 +77,12 @@ __device__ __forceinline__ void st_global32(void* p, const uint32_t (&v)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
                  "r"(v[5]), "r"(v[6]), "r"(v[7])
                  : "memory");
+}
+
+// The first row of the text with the token for its target, or -1.
+__device__ __forceinline__ int first_row(const MmaArgs& a, int token) {
+    const int row = ld_after_wait(a.first_of + token);
+    return unsigned(row) < unsigned(a.text_rows) && ld_after_wait(a.targets + row) == token ? row : -1;
 }
 
 struct MmaTile {
@@ -493,7 +500,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
             const bool valid = row < a.rows;
             uint32_t bits[4];
             if (!kOut) tile_mask(a, t, valid ? row : a.rows - 1, t.n * a.width + 128 * half, bits);
-            const int chain = kTargets && valid ? ld_after_wait(a.first_of + a.t0 + row) : -1;
+            const int chain = kTargets && valid ? first_row(a, a.t0 + row) : -1;
             float sums[128] = {};
             for (int k = t.k0; k < t.k1; k += kPortion, ++it) {
                 if (!ring_wait<true>(&sums_full[it & 1], (it >> 1) & 1)) {
@@ -548,7 +555,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
 #pragma unroll
                 for (int j = 0; j < 8; ++j) residual.ask(a, first + lane, t.n * kMmaTile + c0, j);
             }
-            const int chain = kTargets && first + lane < a.rows ? ld_after_wait(a.first_of + a.t0 + first + lane) : -1;
+            const int chain = kTargets && first + lane < a.rows ? first_row(a, a.t0 + first + lane) : -1;
             if (!ring_wait<true>(&sums_full[kLayer ? it & 1 : set], (it >> 1) & 1)) {
                 ok = false;
                 break;
