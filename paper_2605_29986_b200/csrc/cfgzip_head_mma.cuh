@@ -42,6 +42,7 @@ struct MmaArgs {
     int32_t rows, cols;        // of the result (tokens x piece of the vocabulary, ...)
     int32_t width;             // columns of a tile
     int32_t m_tiles, n_tiles;
+    int32_t box;               // rows of A, where its k is contiguous, that a block fetches at a time
     int32_t k_blocks, splits;  // the k range is cut in `splits`, each with a result of its own
     int32_t m_fast;            // neighbouring tiles go along m
     int32_t* status;
@@ -428,17 +429,19 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
                 const MmaTile t = mma_tile(a, i);
                 const int m = t.m * kMmaTile + int(rank) * 128, n = t.n * a.width + int(rank) * (a.width / 2);
                 const int k1 = a.expire ? min(t.k1, t.k0 + kStages) : t.k1;
+                const bool first_only = !A_MN && a.rows <= 128;
+                const uint32_t bytes = (A_MN ? 2 * kMmaHalf : uint32_t(a.box) * (first_only ? 1 : 2) * kMmaK * 2) + uint32_t(a.width) * kMmaK * 2;
                 for (int k = t.k0; k < k1; ++k) {
                     if (!ring_wait<true>(&empty[r.stage], r.phase ^ 1)) {
                         ok = false;
                         break;
                     }
-                    if (rank == 0) mbar_expect_tx(&full[r.stage], 2 * kMmaHalf + uint32_t(a.width) * kMmaK * 2);
+                    if (rank == 0) mbar_expect_tx(&full[r.stage], bytes);
                     const uint32_t bar = peer_shared(&full[r.stage], 0), at = stages + uint32_t(r.stage) * 2 * kMmaHalf;
                     if (A_MN) {
                         tma_load_pair(at, &map_a, m, k * kMmaK, bar);
                         tma_load_pair(at + kMmaHalf / 2, &map_a, m + 64, k * kMmaK, bar);
-                    } else {
+                    } else if (!first_only || rank == 0) {
                         tma_load_pair(at, &map_a, k * kMmaK, m, bar);
                     }
                     if (B_MN) {

@@ -172,6 +172,7 @@ int run_tall(cfgzip_ctx* ctx, const LayerProduct& p, cudaStream_t st) {
     a.cols = p.features;
     a.width = kMmaTile;
     a.m_tiles = ceil_div(p.rows, kMmaTile);
+    a.box = a_box(p.rows);
     a.n_tiles = ceil_div(p.features, kMmaTile);
     a.k_blocks = ceil_div(p.k, kMmaK);
     a.splits = 1;
@@ -186,7 +187,7 @@ int run_tall(cfgzip_ctx* ctx, const LayerProduct& p, cudaStream_t st) {
     a.has_slope = p.slope != nullptr;
     CUtensorMap map_a, map_b, map_y, map_slope;
     int rc;
-    if ((rc = tensor_map(ctx, &map_a, p.a, p.rows, p.k, p.a_stride, 128)) != CFGZIP_OK ||
+    if ((rc = tensor_map(ctx, &map_a, p.a, p.rows, p.k, p.a_stride, a_box(p.rows))) != CFGZIP_OK ||
         (rc = p.turned ? tensor_map(ctx, &map_b, p.weight, p.k, p.features, p.weight_stride, 64)
                        : tensor_map(ctx, &map_b, p.weight, p.features, p.k, p.weight_stride, 128)) != CFGZIP_OK ||
         (rc = tensor_map_out(ctx, &map_y, a, true)) != CFGZIP_OK)
