@@ -380,7 +380,7 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
  *                id, lowest first. Where fewer have a probability the rest is token -1 with log probability -inf
  *   logp, entropy, lse : dev float [N], each nullable. A row with nothing allowed: lse -inf, entropy 0, logp -inf (0 where no token is given)
  *   top_tokens, top_logp : dev int32 and float [N, n_top] (not looked at where n_top is 0)
- * Allowed logits below -1e29 count as -inf; +inf and NaN among them are outside the contract. Statistics are held in 32 bits. The results
+ * Allowed logits below -1e29 count as -inf; +inf and NaN among them, and zt that no float holds, are outside the contract. Statistics are held in 32 bits. The results
  * are the same from call to call.
  */
 int cfgzip_token_logprobs(cfgzip_ctx* ctx, const void* logits, int dtype, int64_t row_stride_elems, int32_t N, int32_t V,
@@ -465,6 +465,7 @@ int cfgzip_layer_workspace(const cfgzip_layer* layer, int op, int32_t rows, int6
  *   x        : dev bf16 [rows, x_stride]
  *   residual : nullable dev bf16 [rows, residual_stride]; may be x (where in = out)
  *   y        : dev bf16 [rows, y_stride] (written); may be the residual with the same stride unless that is x; overlaps nothing else
+ *              (CFGZIP_E_ARG where y starts where x does, or slope where another of these does)
  *   slope    : nullable dev bf16 [rows, slope_stride] (written): the activation's derivative, which is what the gradient needs of the
  *              forward pass (rounded to bf16, 2^-8 of itself: the gradient's own factor is rounded no finer)
  */
@@ -481,7 +482,8 @@ int cfgzip_layer_forward(cfgzip_ctx* ctx, const cfgzip_layer* layer, const void*
  *   d_y      : dev bf16 [rows, d_y_stride]; it is the residual's gradient too
  *   add      : nullable dev bf16 [rows, add_stride] of `in` columns, added in 32 bits: d_y where the residual was x. It may be d_x with the
  *              same stride
- *   d_x      : nullable dev bf16 [rows, d_x_stride] (written); overlaps no input but add
+ *   d_x      : nullable dev bf16 [rows, d_x_stride] (written); overlaps no input but add (CFGZIP_E_ARG where it starts where d_y, x or
+ *              slope does)
  *   d_weight : nullable dev [out, d_weight_stride] of d_weight_dtype (CFGZIP_BF16 or CFGZIP_F32); d_bias : nullable dev float [out].
  *              Both are written, or added to where accumulate is not 0
  * The results do not depend on timing (no atomic additions).

@@ -246,6 +246,8 @@ int cfgzip_layer_forward(cfgzip_ctx* ctx, const cfgzip_layer* layer, const void*
     const LayerSpace w = layer_space(layer, CFGZIP_LAYER_FORWARD, rows, workspace);
     if (w.bytes && !workspace) return CFGZIP_E_ARG;
     if (workspace_bytes < w.bytes) return CFGZIP_E_NOMEM;
+    // (rows of x are read while others are written; the residual is read where y is written, by the same thread)
+    if (y == x || (slope && (slope == x || slope == y || slope == residual))) return CFGZIP_E_ARG;
     if (!ctx) return CFGZIP_E_ARG;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;
@@ -294,6 +296,7 @@ int cfgzip_layer_backward(cfgzip_ctx* ctx, const cfgzip_layer* layer, const void
     }
     const LayerSpace w = layer_space(layer, CFGZIP_LAYER_BACKWARD, rows, workspace);
     if (rows > 0 && workspace_bytes < w.bytes) return CFGZIP_E_NOMEM;
+    if (rows > 0 && d_x && (d_x == d_y || d_x == x || (acts && d_x == slope))) return CFGZIP_E_ARG;
     if (!ctx) return CFGZIP_E_ARG;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return CFGZIP_E_CUDA;

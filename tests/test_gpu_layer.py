@@ -291,3 +291,22 @@ def test_drafting_and_training_a_layer_under_a_grammar():
         assert close(d_x, g @ l.w64, g.abs() @ l.w64.abs(), n, d_y)
         assert close(d_weight, g.T @ l.x64, g.abs().T @ l.x64.abs(), B)
         assert close(d_bias, (d_y.double() * slope.double()).sum(dim=0), (d_y.double() * slope.double()).abs().sum(dim=0), B)
+
+
+def test_results_in_the_place_of_what_others_still_read_are_refused():
+    with Ctx([]) as ctx:
+        l = Layer(5, 64, 64, "silu", "none")
+        y, slope, d_x = (torch.zeros_like(l.x) for _ in range(3))
+        st, ws = torch.cuda.current_stream(), l.workspace(cz.LAYER_BACKWARD)
+
+        def refused(call, *a):
+            with pytest.raises(cz.CfgzipError) as e:
+                call(ctx.h, l.layer, *a, ws, ws.numel(), st)
+            assert e.value.status == cz.E_ARG
+
+        for y_, slope_ in ((l.x, slope), (l.x, None), (y, l.x), (y, y), (y, d_x)):
+            refused(cz.cfgzip_layer_forward, l.x, 64, 5, d_x, 64, y_, 64, slope_, 64)
+        for d_x_ in (y, l.x, slope):
+            refused(cz.cfgzip_layer_backward, l.x, 64, 5, slope, 64, y, 64, y, 64, d_x_, 64, None, cz.F32, 0, None, 0)
+        torch.cuda.synchronize()
+        assert not y.any() and not slope.any() and not d_x.any()
