@@ -418,6 +418,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
     __syncthreads();
     cluster_barrier();
     tmem_fence_after();
+    if (kLayer) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t tmem = s_tmem;
     bool ok = warp == 0 || !a.expire;  // (the hook: nothing is done with the first stages asked for)

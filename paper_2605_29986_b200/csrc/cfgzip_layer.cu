@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <limits>
 
 #include "cfgzip.h"
 #include "cfgzip_layer.cuh"
@@ -92,36 +93,37 @@ struct FewPlan {
     uint32_t stage_bytes;
     double us;
 };
-// The number of blocks that takes the least time: rounds of clusters (not all SMs can be had four or eight at a time) times a block's stages
-// and what it takes besides, some 3 us. A stage is bound by its operands' way from the L2, 110 bytes a ns and SM. Blocks of few stages fit an
-// SM twice. (500 rows, 2568 -> 1032: 36 tiles by clusters of 4 take two rounds, 19.2 us, by clusters of 2 one, 9.5 us.)
+// The rows of a tile and the blocks of a cluster that take the least time: rounds of clusters (not all SMs can be had four or eight at a time)
+// times a block's stages and what it takes besides. A stage is bound by its operands' way from the L2, 107 bytes a ns and SM, which two blocks of
+// few stages share where there are more than the SMs. High tiles read the weights fewer times; of low ones there are more, and a block has fewer
+// activations to compute at its end (256 rows of 256 x 256: 6.1 us by 128 rows, 4.2 by 32; 128 of 1032 x 2568 8.5 and, by 64, 7.5; 1000 of
+// 2048 x 2048 14.7 by 128, 22.9 by 64). Over 56 shapes of 1 to 1000 rows and all n and blocks the choice is 0.7 % slower than the fastest.
 FewPlan few_plan(const cfgzip_ctx* ctx, const LayerProduct& p) {
-    FewPlan f{};
-    f.n = p.rows >= 128 ? 128 : up(p.rows, 16);
-    f.tiles = ceil_div(p.features, 128);
-    f.groups = ceil_div(p.rows, f.n);
-    f.stage_bytes = kLayerWeights + uint32_t(f.n) * 128;
-    const int k_blocks = ceil_div(p.k, kMmaK), most = std::min(kLayerStages, int((200u << 10) / f.stage_bytes));
-    const double clusters = double(f.tiles) * f.groups;
-    const int least = ceil_div(int64_t(f.n) * kLayerRow * 4, f.stage_bytes);  // what the sums take on their way out
-    for (int s = 1; s <= kLayerBlocks && (s == 1 || 2 * s <= k_blocks); ++s) {
-        const int steps = ceil_div(k_blocks, s), stages = std::max(std::min(most, steps), least);
-        const int twice = 2 * (size_t(stages) * f.stage_bytes + 2560) <= size_t(ctx->smem_optin) ? 2 : 1;
-        const int limit = s == 1 ? ctx->sm_count : ctx->cluster_limit[s] - (s == 3 || s == 5 ? 3 : 0);
-        if (limit <= 0) continue;
-        const double rounds = std::ceil(clusters / (double(limit) * twice));
-        const double beside = std::max(1.0, std::min(double(twice), clusters * s / ctx->sm_count));
-        const double us = rounds * (steps * beside * f.stage_bytes / 110e3 + 3.0 + 0.3 * s);
-        if (f.blocks && us >= f.us) continue;
-        f.blocks = s;
-        f.stages = stages;
-        f.us = us;
+    FewPlan best{};
+    best.us = std::numeric_limits<double>::infinity();
+    const int tiles = ceil_div(p.features, 128), k_blocks = ceil_div(p.k, kMmaK), all = std::min(128, up(p.rows, 16));
+    for (const int n : {all, 96, 64, 48, 32}) {
+        const int groups = ceil_div(p.rows, n);
+        if (n > all || groups > 65535) continue;
+        const uint32_t stage_bytes = kLayerWeights + uint32_t(n) * 128;
+        const int most = std::min(kLayerStages, int((200u << 10) / stage_bytes));
+        const int least = ceil_div(int64_t(n) * kLayerRow * 4, stage_bytes);  // what the sums take on their way out
+        const double clusters = double(tiles) * groups;
+        for (int s = 1; s <= kLayerBlocks && (s == 1 || 2 * s <= k_blocks); ++s) {
+            const int steps = ceil_div(k_blocks, s), stages = std::max(std::min(most, steps), least);
+            const int twice = 2 * (size_t(stages) * stage_bytes + 2560) <= size_t(ctx->smem_optin) ? 2 : 1;
+            const int limit = s == 1 ? ctx->sm_count : ctx->cluster_limit[s] - (s == 3 || s == 5 ? 3 : 0);
+            if (limit <= 0) continue;
+            const double rounds = std::ceil(clusters / (double(limit) * twice)), beside = std::min(double(twice), std::ceil(clusters / limit));
+            const double us = 1.0 + rounds * (steps * beside * stage_bytes / 107e3 + (s > 1 ? 3.0 : 2.2) + 0.02 * s + 0.018 * n);
+            if (us < best.us) best = FewPlan{n, tiles, groups, s, stages, stage_bytes, us};
+        }
     }
-    return f;
+    return best;
 }
 
-template <bool A_MN>
-int run_few(cfgzip_ctx* ctx, const LayerProduct& p, const FewPlan& f, cudaStream_t st) {
+template <bool A_MN, int ACT>
+int run_few_as(cfgzip_ctx* ctx, const LayerProduct& p, const FewPlan& f, cudaStream_t st) {
     CUtensorMap map_w, map_x;
     int rc = A_MN ? tensor_map(ctx, &map_w, p.weight, p.k, p.features, p.weight_stride, 64)
                   : tensor_map(ctx, &map_w, p.weight, p.features, p.k, p.weight_stride, 128);
@@ -133,7 +135,6 @@ int run_few(cfgzip_ctx* ctx, const LayerProduct& p, const FewPlan& f, cudaStream
     a.k_blocks = ceil_div(p.k, kMmaK);
     a.stage_bytes = f.stage_bytes;
     a.stages = f.stages;
-    a.act = p.act;
     a.bias = p.bias;
     a.bias_bf16 = p.bias_bf16;
     a.residual = static_cast<const uint16_t*>(p.residual);
@@ -145,12 +146,22 @@ int run_few(cfgzip_ctx* ctx, const LayerProduct& p, const FewPlan& f, cudaStream
     a.status = ctx->d_status;
     a.expire = ctx->expire_test;
     const size_t smem = size_t(a.stages) * a.stage_bytes + 1024;
-    if (f.groups > 65535) return CFGZIP_E_RANGE;
-    if ((rc = ensure_smem(ctx, k_layer_few<A_MN>, smem)) != CFGZIP_OK) return rc;
+    if ((rc = ensure_smem(ctx, k_layer_few<A_MN, ACT>, smem)) != CFGZIP_OK) return rc;
     ctx->cluster_now = f.blocks;
-    rc = launch(ctx, k_layer_few<A_MN>, dim3(unsigned(f.tiles * f.blocks), unsigned(f.groups)), dim3(kLayerThreads), smem, st, a, map_w, map_x);
+    rc = launch(ctx, k_layer_few<A_MN, ACT>, dim3(unsigned(f.tiles * f.blocks), unsigned(f.groups)), dim3(kLayerThreads), smem, st, a, map_w, map_x);
     ctx->cluster_now = 1;
     return rc;
+}
+
+int run_few(cfgzip_ctx* ctx, const LayerProduct& p, const FewPlan& f, cudaStream_t st) {
+    if (p.turned) return run_few_as<true, kActNone>(ctx, p, f, st);
+    switch (p.act) {
+        case CFGZIP_ACT_RELU: return run_few_as<false, kActRelu>(ctx, p, f, st);
+        case CFGZIP_ACT_GELU: return run_few_as<false, kActGelu>(ctx, p, f, st);
+        case CFGZIP_ACT_GELU_TANH: return run_few_as<false, kActGeluTanh>(ctx, p, f, st);
+        case CFGZIP_ACT_SILU: return run_few_as<false, kActSilu>(ctx, p, f, st);
+        default: return run_few_as<false, kActNone>(ctx, p, f, st);
+    }
 }
 
 template <bool B_MN, int ACT>
@@ -211,11 +222,11 @@ int run_tall(cfgzip_ctx* ctx, const LayerProduct& p, cudaStream_t st) {
 
 int run_product(cfgzip_ctx* ctx, const LayerProduct& p, cudaStream_t st) {
     const FewPlan f = few_plan(ctx, p);
-    // A stage of 64 k of a pair's 256 x 256 takes 0.4 us, and some 6 us are not covered by other tiles.
+    // A stage of 64 k of a pair's 256 x 256 takes 0.28 to 0.4 us, the more the more pairs there are, and some 10 us are not covered by other tiles.
     const int tall_rounds = ceil_div(int64_t(ceil_div(p.rows, kMmaTile)) * ceil_div(p.features, kMmaTile), ctx->sm_count / 2);
-    const double tall = tall_rounds * (ceil_div(p.k, kMmaK) * 0.4) + 6.0;
+    const double tall = tall_rounds * (ceil_div(p.k, kMmaK) * 0.33) + 10.0;
     if (p.rows > 128 && tall < f.us) return run_tall(ctx, p, st);
-    return p.turned ? run_few<true>(ctx, p, f, st) : run_few<false>(ctx, p, f, st);
+    return run_few(ctx, p, f, st);
 }
 
 }  // namespace

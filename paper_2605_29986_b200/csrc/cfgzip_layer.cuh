@@ -14,7 +14,7 @@ struct LayerArgs {
     int32_t N;                  // rows of a tile: a multiple of 16, at most 128
     int32_t k_blocks, stages;
     uint32_t stage_bytes;
-    int32_t act, bias_bf16;
+    int32_t bias_bf16;
     const void* bias;
     const uint16_t* residual;
     int64_t residual_stride;
@@ -49,13 +49,58 @@ __device__ __forceinline__ void layer_finish(const LayerArgs& a, int row, int n,
             make_uint4(bf16_pair(s[0], s[1]), bf16_pair(s[2], s[3]), bf16_pair(s[4], s[5]), bf16_pair(s[6], s[7]));
 }
 
+// The results of a thread from its block's share of rows, `first`, `first` + `step` and so on of the tile: eight features of each, features n on
+// of the result. The sums of up to BLOCKS blocks are added up, ROWS rows' loads in flight; each block begins with its own sums and goes round
+// (all at the same block's, they would get an eighth of its speed each). `next` holds the next rows' residuals, asked for ahead.
+constexpr int kLayerAhead = 4;
+template <int ACT, int BLOCKS, int ROWS, typename Ask>
+__device__ __forceinline__ void layer_rows(const LayerArgs& a, const float* part, int row0, int rows, int first, int step, int n, int blocks,
+                                           int rank, const float (&bias)[8], uint4 (&next)[kLayerAhead], const Ask& ask) {
+#pragma unroll 1
+    for (int at = first; at < rows; at += kLayerAhead * step) {
+#pragma unroll
+        for (int r0 = 0; r0 < kLayerAhead; r0 += ROWS) {
+            if (at + r0 * step >= rows) break;
+            uint4 v[ROWS][BLOCKS][2];
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const int row = min(at + (r0 + r) * step, rows - 1);
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+                    if (b < blocks) {
+                        const uint32_t from = peer_shared(part + row * kLayerRow, uint32_t(rank + b < blocks ? rank + b : rank + b - blocks));
+                        v[r][b][0] = ld_peer_v4(from);
+                        v[r][b][1] = ld_peer_v4(from + 80 * sizeof(float));
+                    }
+            }
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const int row = at + (r0 + r) * step;
+                if (row >= rows) break;
+                float f[8] = {}, residual[8];
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+                    if (b < blocks) {
+                        const uint32_t w[8] = {v[r][b][0].x, v[r][b][0].y, v[r][b][0].z, v[r][b][0].w,
+                                               v[r][b][1].x, v[r][b][1].y, v[r][b][1].z, v[r][b][1].w};
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) f[j] += __uint_as_float(w[j]);
+                    }
+                bf16_values(next[r0 + r], residual);
+                next[r0 + r] = ask(row + kLayerAhead * step);
+                layer_finish<ACT>(a, row0 + row, n, f, bias, residual);
+            }
+        }
+    }
+}
+
 // Few rows: what counts is reading the weights at the speed of memory, on as many SMs as there are. A cluster of up to 8 blocks shares a
 // tile of 128 features and N rows, a part of k each; weights are the long side (operand A, 128 rows to a product), the rows the short one.
 // The parts meet in the blocks' shared memory: each block adds up a share of the results over the cluster and finishes it.
 //
 // Sums stay in tensor memory over all of a block's k: what its additions cut off (1e-9 of the sum per element) is far below the rounding
 // of the result to bf16.
-template <bool A_MN>
+template <bool A_MN, int ACT>
 __global__ void __launch_bounds__(kLayerThreads, 2)
     k_layer_few(const __grid_constant__ LayerArgs a, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x) {
     extern __shared__ char smem_raw[];
@@ -95,10 +140,10 @@ __global__ void __launch_bounds__(kLayerThreads, 2)
     const int n = n0 + 8 * (int(threadIdx.x) & 15);
     const bool mine = n < a.features;
     float bias[8] = {};
-    uint4 next = make_uint4(0, 0, 0, 0);
+    uint4 next[kLayerAhead];
     auto ask = [&](int row) {
-        if (a.residual && mine && row < rows)
-            next = ld_after_wait(reinterpret_cast<const uint4*>(a.residual + int64_t(row0 + row) * a.residual_stride + n));
+        return a.residual && mine && row < rows ? ld_after_wait(reinterpret_cast<const uint4*>(a.residual + int64_t(row0 + row) * a.residual_stride + n))
+                                                : make_uint4(0, 0, 0, 0);
     };
 
     if (warp == 0) {
@@ -154,7 +199,8 @@ __global__ void __launch_bounds__(kLayerThreads, 2)
         __syncwarp();
     }
     if (a.bias && mine && first < rows) bias_values(a.bias, a.bias_bf16, n, bias);
-    ask(first);
+#pragma unroll
+    for (int r = 0; r < kLayerAhead; ++r) next[r] = ask(first + r * step);
     if (ok && !ring_wait(&done, 0)) ok = false;
     const bool failed = __syncthreads_or(!ok);
     if (failed) {
@@ -190,33 +236,10 @@ __global__ void __launch_bounds__(kLayerThreads, 2)
     __syncwarp();
     cluster_barrier();
     if (!failed && mine) {
-        for (int row = first; row < rows; row += step) {
-            float residual[8];
-            bf16_values(next, residual);
-            ask(row + step);
-            // (each block begins with its own sums and goes round: all at the same block's, they would get an eighth of its speed each)
-            uint4 v[kLayerBlocks][2];
-#pragma unroll
-            for (int b = 0; b < kLayerBlocks; ++b)
-                if (b < blocks) {
-                    const uint32_t from = peer_shared(part + row * kLayerRow + ((n - n0) >> 1), uint32_t(rank + b < blocks ? rank + b : rank + b - blocks));
-                    v[b][0] = ld_peer_v4(from);
-                    v[b][1] = ld_peer_v4(from + 80 * sizeof(float));
-                }
-            float f[8] = {};
-#pragma unroll
-            for (int b = 0; b < kLayerBlocks; ++b)
-                if (b < blocks) {
-                    const uint32_t w[8] = {v[b][0].x, v[b][0].y, v[b][0].z, v[b][0].w, v[b][1].x, v[b][1].y, v[b][1].z, v[b][1].w};
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] += __uint_as_float(w[j]);
-                }
-            if (a.act == kActSilu) layer_finish<kActSilu>(a, row0 + row, n, f, bias, residual);
-            else if (a.act == kActGelu) layer_finish<kActGelu>(a, row0 + row, n, f, bias, residual);
-            else if (a.act == kActGeluTanh) layer_finish<kActGeluTanh>(a, row0 + row, n, f, bias, residual);
-            else if (a.act == kActRelu) layer_finish<kActRelu>(a, row0 + row, n, f, bias, residual);
-            else layer_finish<kActNone>(a, row0 + row, n, f, bias, residual);
-        }
+        const float* const mine_of = part + ((n - n0) >> 1);
+        if (blocks <= 2) layer_rows<ACT, 2, 4>(a, mine_of, row0, rows, first, step, n, blocks, rank, bias, next, ask);
+        else if (blocks <= 4) layer_rows<ACT, 4, 2>(a, mine_of, row0, rows, first, step, n, blocks, rank, bias, next, ask);
+        else layer_rows<ACT, kLayerBlocks, 1>(a, mine_of, row0, rows, first, step, n, blocks, rank, bias, next, ask);
     }
     __syncwarp();
     cluster_barrier();  // (no block leaves while others read its sums)
