@@ -466,8 +466,8 @@ int cfgzip_layer_workspace(const cfgzip_layer* layer, int op, int32_t rows, int6
  *   residual : nullable dev bf16 [rows, residual_stride]; may be x (where in = out)
  *   y        : dev bf16 [rows, y_stride] (written); may be the residual with the same stride unless that is x; overlaps nothing else
  *              (CFGZIP_E_ARG where y starts where x does, or slope where another of these does)
- *   slope    : nullable dev bf16 [rows, slope_stride] (written): the activation's derivative, which is what the gradient needs of the
- *              forward pass (rounded to bf16, 2^-8 of itself: the gradient's own factor is rounded no finer)
+ *   slope    : nullable dev bf16 [rows, slope_stride] (written; not touched without an activation): the activation's derivative, which is
+ *              what the gradient needs of the forward pass (rounded to bf16, 2^-8 of itself: the gradient's own factor is rounded no finer)
  */
 int cfgzip_layer_forward(cfgzip_ctx* ctx, const cfgzip_layer* layer, const void* x, int64_t x_stride, int32_t rows, const void* residual,
                          int64_t residual_stride, void* y, int64_t y_stride, void* slope, int64_t slope_stride, void* workspace,

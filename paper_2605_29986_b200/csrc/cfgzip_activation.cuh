@@ -13,43 +13,75 @@ __device__ __forceinline__ float rcpf(float x) {
     return y;
 }
 
-// The activation and its derivative. Logistic functions are 1 / (1 + exp), which is 0 or 1 where the exponential leaves the numbers; the
-// polynomials are taken of arguments within 64, behind which nothing changes any more. Without branches, so that the elements of a row are
-// computed side by side: with an IEEE division the epilogue took as long as the product (8192 x 4096 x 4096: 212 against 180 us).
+// The activation of two numbers, and its derivative. Logistic functions are 1 / (1 + exp), which is 0 or 1 where the exponential leaves the
+// numbers; the polynomial of the derivative of the one by way of tanh is taken of arguments within 64, behind which nothing changes any more.
+// Without branches, so that the elements of a row are computed side by side, two to an instruction: with an IEEE division the epilogue took as
+// long as the product (8192 x 4096 x 4096: 212 against 180 us).
 // The normal distribution's Phi is made of the complementary error function as in Abramowitz and Stegun, 7.1.26 (within 1.5e-7), whose
 // exponential the derivative needs too.
+using pair2 = unsigned long long;
+__device__ __forceinline__ pair2 both(float x) { return pack2(x, x); }
+__device__ __forceinline__ pair2 ex2_pair(pair2 x) {
+    float a, b;
+    unpack2(x, a, b);
+    return pack2(ex2f(a), ex2f(b));
+}
+__device__ __forceinline__ pair2 rcp_pair(pair2 x) {
+    float a, b;
+    unpack2(x, a, b);
+    return pack2(rcpf(a), rcpf(b));
+}
+__device__ __forceinline__ void bf16_pairs(const uint4& v, pair2 (&p)[4]) {
+    float f[8];
+    bf16_values(v, f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j] = pack2(f[2 * j], f[2 * j + 1]);
+}
 template <int ACT>
-__device__ __forceinline__ float activation(float h, float* slope) {
+__device__ __forceinline__ pair2 activation(pair2 h, pair2* slope) {
+    float h0, h1;
+    unpack2(h, h0, h1);
     if (ACT == kActRelu) {
-        *slope = h > 0.f ? 1.f : 0.f;
-        return fmaxf(h, 0.f);
+        *slope = pack2(h0 > 0.f ? 1.f : 0.f, h1 > 0.f ? 1.f : 0.f);
+        return pack2(fmaxf(h0, 0.f), fmaxf(h1, 0.f));
     }
     if (ACT == kActGelu) {
-        const float c = fminf(fmaxf(h, -64.f), 64.f), x = fabsf(c) * 0.70710678f, e = ex2f(c * c * (-0.5f * kLog2e));
-        const float t = rcpf(fmaf(0.3275911f, x, 1.f));
-        float p = fmaf(1.061405429f, t, -1.453152027f);
-        p = fmaf(p, t, 1.421413741f);
-        p = fmaf(p, t, -0.284496736f);
-        p = fmaf(p, t, 0.254829592f) * t * 0.5f;
-        const float phi = h < 0.f ? p * e : fmaf(-p, e, 1.f);
-        *slope = fmaf(c * 0.3989422804f, e, phi);
-        return h * phi;
+        const pair2 e = ex2_pair(mul2(mul2(h, h), both(-0.5f * kLog2e)));
+        const pair2 t = rcp_pair(fma2(pack2(fabsf(h0), fabsf(h1)), both(0.3275911f * 0.70710678f), both(1.f)));
+        pair2 p = fma2(both(0.5f * 1.061405429f), t, both(0.5f * -1.453152027f));
+        p = fma2(p, t, both(0.5f * 1.421413741f));
+        p = fma2(p, t, both(0.5f * -0.284496736f));
+        p = mul2(mul2(fma2(p, t, both(0.5f * 0.254829592f)), t), e);
+        float p0, p1;
+        unpack2(p, p0, p1);
+        const pair2 phi = pack2(h0 < 0.f ? p0 : 1.f - p0, h1 < 0.f ? p1 : 1.f - p1);
+        *slope = fma2(mul2(h, both(0.3989422804f)), e, phi);
+        return mul2(h, phi);
     }
     if (ACT == kActGeluTanh) {  // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u)), u = k (h + 0.044715 h^3), k = sqrt(2 / pi)
-        const float c = fminf(fmaxf(h, -64.f), 64.f), two_k = 1.5957691216f;
-        const float q = rcpf(1.f + ex2f(-kLog2e * two_k * c * fmaf(0.044715f, c * c, 1.f)));
-        *slope = fmaf(c * q * (1.f - q), two_k * fmaf(3.f * 0.044715f, c * c, 1.f), q);
-        return h * q;
+        const pair2 c = pack2(fminf(fmaxf(h0, -64.f), 64.f), fminf(fmaxf(h1, -64.f), 64.f)), square = mul2(c, c);
+        constexpr float kTwoK = 1.5957691216f;
+        const pair2 u = mul2(c, fma2(both(-kLog2e * kTwoK * 0.044715f), square, both(-kLog2e * kTwoK)));
+        const pair2 q = rcp_pair(add2(ex2_pair(u), both(1.f)));
+        *slope = fma2(mul2(mul2(c, q), fma2(q, both(-1.f), both(1.f))), fma2(both(kTwoK * 3.f * 0.044715f), square, both(kTwoK)), q);
+        return mul2(h, q);
     }
     if (ACT == kActSilu) {
-        const float q = rcpf(1.f + ex2f(-kLog2e * h));
-        *slope = q * fmaf(h, 1.f - q, 1.f);
-        return h * q;
+        const pair2 q = rcp_pair(add2(ex2_pair(mul2(h, both(-kLog2e))), both(1.f)));
+        *slope = mul2(q, fma2(h, fma2(q, both(-1.f), both(1.f)), both(1.f)));
+        return mul2(h, q);
     }
-    *slope = 1.f;
+    *slope = both(1.f);
     return h;
 }
 
+// One as it is stored, its bits.
+__device__ __forceinline__ uint32_t bias_bits(const void* bias, bool bf16, int n) {
+    if (!bf16) return ld_after_wait(static_cast<const uint32_t*>(bias) + n);
+    uint32_t v;
+    asm volatile("ld.global.u16 %0, [%1];" : "=r"(v) : "l"(__cvta_generic_to_global(static_cast<const uint16_t*>(bias) + n)));
+    return v;
+}
 // Eight biases from feature n on (n and their number a multiple of 8).
 __device__ __forceinline__ void bias_values(const void* bias, bool bf16, int n, float (&f)[8]) {
     if (bf16) {

@@ -308,67 +308,97 @@ __device__ __forceinline__ void out_columns(const MmaArgs& a, const CUtensorMap&
     if (lane == 0) tma_store3(&map, n, first, t.split, buffer);
 }
 
-// A lane's part of the residual in 64 columns from n on: its row's 128 bytes. Asked for 64 columns ahead.
-struct LayerResidual {
-    uint4 v[8];
-    __device__ __forceinline__ void ask(const MmaArgs& a, int row, int n, int j) {
-        v[j] = make_uint4(0, 0, 0, 0);
-        if (a.residual && row < a.rows && n + 8 * j < a.cols)
-            v[j] = ld_after_wait(reinterpret_cast<const uint4*>(a.residual + int64_t(row) * a.residual_stride + n + 8 * j));
+// What a warp's next 64 columns need besides the sums, asked for ahead: two biases of a lane, and the residual, a row's 128 bytes by eight lanes
+// (by one lane, 16 bytes at a time, the loads of a warp touch 32 lines each).
+struct LayerAhead {
+    uint32_t bias[2];  // (bf16 ones as they are stored: put in place here, each load would be waited for)
+    uint4 residual[8];
+    __device__ __forceinline__ void ask_bias(const MmaArgs& a, int n, int end, int lane) {
+        if (!a.bias || n >= end) return;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) bias[h] = n + 32 * h + lane < a.cols ? bias_bits(a.bias, a.bias_bf16, n + 32 * h + lane) : 0u;
+    }
+    __device__ __forceinline__ void ask_residual(const MmaArgs& a, int first, int n, int end, int lane) {
+        if (!a.residual || n >= end) return;
+        const int col = n + 8 * (lane & 7);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int row = first + 4 * j + (lane >> 3);
+            residual[j] = make_uint4(0, 0, 0, 0);
+            if (row < a.rows && col < a.cols)
+                residual[j] = ld_after_wait(reinterpret_cast<const uint4*>(a.residual + int64_t(row) * a.residual_stride + col));
+        }
     }
 };
 
 // A layer's results, 64 columns of a warp's 32 rows at a time, straight from tensor memory. y and the activation's derivative leave by tiled
-// copies from a buffer each. The bias, the same for all lanes, comes from the L1.
-template <int ACT>
+// copies from a buffer each; without a derivative y takes the two in turn. The residual comes to its lanes by way of y's place. A bias, the same
+// for all lanes, is in 32 floats of shared memory (loaded by all lanes from the L1 it took 10 us of 40).
+template <int ACT, bool SLOPE>
 __device__ __forceinline__ void layer_columns(const MmaArgs& a, const CUtensorMap& map_y, const CUtensorMap& map_slope, int n, int first,
-                                              int lane, uint32_t tmem, uint32_t buffer, LayerResidual& residual, int next) {
+                                              int lane, uint32_t tmem, uint32_t buffer, float* table, LayerAhead& ahead, int end) {
+    const uint32_t row = buffer + uint32_t(lane) * 128, turn = uint32_t(lane & 7);
     // (32 columns at a time: all loads, then all arithmetic, so that its chains run side by side, then all stores)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         uint32_t v[32], y[16], s[16];
-        float bias[4][8] = {};
         tmem_ld32(tmem + 32 * h, v);
-        if (a.bias) {
+        if (h == 0) {
+            if (lane == 0) {  // (the copies before have read the buffer)
+                if (SLOPE)
+                    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                else
+                    asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            }
+            __syncwarp();
+            if (a.residual) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (n + 32 * h + 8 * j < a.cols) bias_values(a.bias, a.bias_bf16, n + 32 * h + 8 * j, bias[j]);
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t r = uint32_t(4 * j + (lane >> 3));
+                    st_shared16(buffer + r * 128 + ((turn ^ (r & 7u)) << 4), ahead.residual[j]);
+                }
+            }
+            ahead.ask_residual(a, first, n + 64, end, lane);
         }
+        if (a.bias) table[lane] = __uint_as_float(ahead.bias[h] << (a.bias_bf16 ? 16 : 0));
+        if (h == 1) ahead.ask_bias(a, n + 64, end, lane);
+        __syncwarp();
         tmem_wait_ld();
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float f[8], by[8], of[8];
-            bf16_values(residual.v[4 * h + j], of);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = activation<ACT>(__uint_as_float(v[8 * j + k]) + bias[j][k], &by[k]) + of[k];
+            const uint32_t at = row + ((uint32_t(4 * h + j) ^ turn) << 4);
+            pair2 of[4] = {}, bias[4] = {};
+            if (a.residual) bf16_pairs(ld_shared16(at), of);
+            if (a.bias) {
+                const ulonglong2 lo = *reinterpret_cast<const ulonglong2*>(table + 8 * j), hi = *reinterpret_cast<const ulonglong2*>(table + 8 * j + 4);
+                bias[0] = lo.x; bias[1] = lo.y; bias[2] = hi.x; bias[3] = hi.y;
+            }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                y[4 * j + k] = bf16_pair(f[2 * k], f[2 * k + 1]);
-                s[4 * j + k] = bf16_pair(by[2 * k], by[2 * k + 1]);
+                pair2 by;
+                const pair2 of_h = activation<ACT>(add2(pack2(__uint_as_float(v[8 * j + 2 * k]), __uint_as_float(v[8 * j + 2 * k + 1])), bias[k]), &by);
+                float f0, f1;
+                unpack2(add2(of_h, of[k]), f0, f1);
+                y[4 * j + k] = bf16_pair(f0, f1);
+                if (SLOPE) {
+                    unpack2(by, f0, f1);
+                    s[4 * j + k] = bf16_pair(f0, f1);
+                }
             }
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) residual.ask(a, first + lane, next, 4 * h + j);
-        if (h == 0) {
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (the copies before have read the buffers)
-            __syncwarp();
-        }
-#pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t at = buffer + uint32_t(lane) * 128 + (uint32_t((4 * h + j) ^ (lane & 7)) << 4);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(y[4 * j]), "r"(y[4 * j + 1]), "r"(y[4 * j + 2]), "r"(y[4 * j + 3])
-                         : "memory");
-            if (ACT != kActNone && a.has_slope)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + kMmaOut), "r"(s[4 * j]), "r"(s[4 * j + 1]),
-                             "r"(s[4 * j + 2]), "r"(s[4 * j + 3])
-                             : "memory");
+            const uint32_t at = row + ((uint32_t(4 * h + j) ^ turn) << 4);
+            st_shared16(at, make_uint4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]));
+            if (SLOPE) st_shared16(at + kMmaOut, make_uint4(s[4 * j], s[4 * j + 1], s[4 * j + 2], s[4 * j + 3]));
         }
+        if (h == 0) __syncwarp();  // (the biases have been read)
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) {
         tma_store3(&map_y, n, first, 0, buffer);
-        if (ACT != kActNone && a.has_slope) tma_store3(&map_slope, n, first, 0, buffer + kMmaOut);
+        if (SLOPE) tma_store3(&map_slope, n, first, 0, buffer + kMmaOut);
     }
 }
 
@@ -390,6 +420,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2];
     __shared__ __align__(8) uint64_t drained;
+    __shared__ __align__(16) float s_bias[kLayer ? 8 : 1][32];
     __shared__ uint32_t s_tmem, s_end[2];  // (of either block: the stages it has asked for, and in the highest bit whether a wait ran out)
     constexpr bool kOut = kMmaOfSums<KIND>, kTargets = KIND == kMmaSumTargets || KIND == kMmaBf16Targets;
     constexpr int kPortion = kLayer ? 1 << 30 : kOut ? kMmaOutPortion : kMmaPortion;
@@ -547,6 +578,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
         const int set = (warp - 4) >> 2, quad = warp & 3;
         const uint32_t empty_bar = peer_shared(&sums_empty[set], 0);
         int it = 0;
+        uint32_t turn = 0;
         for (int i = pair; i < tiles && ok; i += pairs, ++it) {
             // (a layer's last tile of a pair is shared: nothing else is left to do meanwhile)
             const bool shared = kLayer && i + pairs >= tiles;
@@ -554,10 +586,11 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
             const MmaTile t = mma_tile(a, i);
             const int first = t.m * kMmaTile + int(rank) * 128 + quad * 32;
             const int c0 = shared ? set * 128 : 0, c1 = shared ? c0 + 128 : kMmaTile;
-            LayerResidual residual;
+            LayerAhead ahead;
+            const int n0 = t.n * kMmaTile + c0, end = min(a.cols, t.n * kMmaTile + c1);
             if constexpr (kLayer) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) residual.ask(a, first + lane, t.n * kMmaTile + c0, j);
+                ahead.ask_bias(a, n0, end, lane);
+                ahead.ask_residual(a, first, n0, end, lane);
             }
             const int chain = kTargets && first + lane < a.rows ? first_row(a, a.t0 + first + lane) : -1;
             if (!ring_wait<true>(&sums_full[kLayer ? it & 1 : set], (it >> 1) & 1)) {
@@ -566,11 +599,18 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
             }
             tmem_fence_after();
             if constexpr (kLayer) {
+                constexpr int kAct = KIND - kMmaLayer;
+                const uint32_t of_warp = stages + kStages * 2 * kMmaHalf + uint32_t(warp - 4) * (2 * kMmaOut);
 #pragma unroll 1
-                for (int c = c0, n = t.n * kMmaTile + c0; c < c1 && n < a.cols && first < a.rows; c += 64, n += 64)
-                    layer_columns<KIND - kMmaLayer>(a, map_out, map_slope, n, first, lane, tmem + (it & 1) * 256 + c + (uint32_t(quad * 32) << 16),
-                                                    stages + kStages * 2 * kMmaHalf + uint32_t(warp - 4) * (2 * kMmaOut), residual,
-                                                    c + 64 < c1 ? n + 64 : a.cols);
+                for (int c = c0, n = n0; n < end && first < a.rows; c += 64, n += 64) {
+                    const uint32_t from = tmem + (it & 1) * 256 + c + (uint32_t(quad * 32) << 16);
+                    if (kAct != kActNone && a.has_slope) {
+                        layer_columns<kAct, true>(a, map_out, map_slope, n, first, lane, from, of_warp, s_bias[warp - 4], ahead, end);
+                    } else {
+                        layer_columns<kAct, false>(a, map_out, map_slope, n, first, lane, from, of_warp + turn, s_bias[warp - 4], ahead, end);
+                        turn ^= kMmaOut;
+                    }
+                }
             } else {
                 const bool add = a.add && first + lane < a.rows;
                 constexpr int kCols = kOutCols<kMmaToBf16<KIND>>;

@@ -277,7 +277,7 @@ int cfgzip_layer_forward(cfgzip_ctx* ctx, const cfgzip_layer* layer, const void*
     p.residual_stride = residual_stride;
     p.y = y;
     p.y_stride = y_stride;
-    p.slope = slope;
+    p.slope = layer->activation != CFGZIP_ACT_NONE ? slope : nullptr;
     p.slope_stride = slope_stride;
     return run_product(ctx, p, static_cast<cudaStream_t>(stream));
 }

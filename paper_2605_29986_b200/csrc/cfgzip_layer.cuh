@@ -41,7 +41,12 @@ template <int ACT>
 __device__ __forceinline__ void layer_finish(const LayerArgs& a, int row, int n, float (&f)[8], const float (&bias)[8], const float (&residual)[8]) {
     float s[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = activation<ACT>(f[j] + bias[j], &s[j]) + residual[j];
+    for (int j = 0; j < 8; j += 2) {
+        pair2 by;
+        const pair2 of_h = activation<ACT>(add2(pack2(f[j], f[j + 1]), pack2(bias[j], bias[j + 1])), &by);
+        unpack2(add2(of_h, pack2(residual[j], residual[j + 1])), f[j], f[j + 1]);
+        unpack2(by, s[j], s[j + 1]);
+    }
     *reinterpret_cast<uint4*>(a.y + int64_t(row) * a.y_stride + n) =
         make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
     if (a.slope)
