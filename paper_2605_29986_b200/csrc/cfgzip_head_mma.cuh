@@ -411,7 +411,8 @@ __device__ __forceinline__ void layer_columns(const MmaArgs& a, const CUtensorMa
 // from tensor memory (100 tokens of 50021 x 1024: 26 us for d_weight against 38).
 //
 // A layer's sums stay in tensor memory to their end: their results are bf16, and what is cut off (1e-9 of a sum per element of k) is far
-// below that.
+// below that. (8192 rows of 4096 -> 4096 with bias, residual and derivative: 180 to 193 us, 1.42 to 1.53 PFLOP/s; of 512 -> 4096 56, bound by
+// what is done with the sums.)
 template <bool A_MN, bool B_MN, int KIND, bool LONG>
 __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_out,
                                              const CUtensorMap& map_slope) {
