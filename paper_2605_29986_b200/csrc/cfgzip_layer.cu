@@ -87,22 +87,22 @@ struct LayerProduct {
     int64_t slope_stride;
 };
 
-// Tiles of 128 features by `n` rows, each over a cluster of `blocks` blocks with `stages` stages each.
+// Tiles of 128 features by `n` rows (at most 256), each over a cluster of `blocks` blocks with `stages` stages each.
 struct FewPlan {
     int n, tiles, groups, blocks, stages;
     uint32_t stage_bytes;
     double us;
 };
 // The rows of a tile and the blocks of a cluster that take the least time: rounds of clusters (not all SMs can be had four or eight at a time)
-// times a block's stages and what it takes besides. A stage is bound by its operands' way from the L2, 107 bytes a ns and SM, which two blocks of
-// few stages share where there are more than the SMs. High tiles read the weights fewer times; of low ones there are more, and a block has fewer
-// activations to compute at its end (256 rows of 256 x 256: 6.1 us by 128 rows, 4.2 by 32; 128 of 1032 x 2568 8.5 and, by 64, 7.5; 1000 of
-// 2048 x 2048 14.7 by 128, 22.9 by 64). Over 56 shapes of 1 to 1000 rows and all n and blocks the choice is 0.7 % slower than the fastest.
+// times a block's stages and what it takes besides. A stage is bound by its operands' way from the L2, 100 to 130 bytes a ns and SM, which two blocks
+// of few stages share where there are more than the SMs. High tiles read the weights fewer times; of low ones there are more, and a block has
+// fewer activations to compute at its end (256 rows of 256 x 256: 6.1 us by 128 rows, 4.2 by 32; 128 of 1032 x 2568 8.5 and, by 64, 7.5; 500 of
+// 4096 x 4096 37.7 by 64, 21.5 by 128, 18.9 by 256). Over 80 shapes of 1 to 2000 rows the choice of all is 0.5 % slower than the fastest.
 FewPlan few_plan(const cfgzip_ctx* ctx, const LayerProduct& p) {
     FewPlan best{};
     best.us = std::numeric_limits<double>::infinity();
-    const int tiles = ceil_div(p.features, 128), k_blocks = ceil_div(p.k, kMmaK), all = std::min(128, up(p.rows, 16));
-    for (const int n : {all, 96, 64, 48, 32}) {
+    const int tiles = ceil_div(p.features, 128), k_blocks = ceil_div(p.k, kMmaK), all = std::min(256, up(p.rows, 16));
+    for (const int n : {all, 192, 128, 96, 64, 48, 32}) {
         const int groups = ceil_div(p.rows, n);
         if (n > all || groups > 65535) continue;
         const uint32_t stage_bytes = kLayerWeights + uint32_t(n) * 128;
@@ -115,7 +115,7 @@ FewPlan few_plan(const cfgzip_ctx* ctx, const LayerProduct& p) {
             const int limit = s == 1 ? ctx->sm_count : ctx->cluster_limit[s] - (s == 3 || s == 5 ? 3 : 0);
             if (limit <= 0) continue;
             const double rounds = std::ceil(clusters / (double(limit) * twice)), beside = std::min(double(twice), std::ceil(clusters / limit));
-            const double us = 1.0 + rounds * (steps * beside * stage_bytes / 107e3 + (s > 1 ? 3.0 : 2.2) + 0.02 * s + 0.018 * n);
+            const double us = 1.0 + rounds * (steps * beside * (0.17 + 0.0008 * n) + (s > 1 ? 3.0 : 2.2) + 0.02 * s + 0.016 * n);
             if (us < best.us) best = FewPlan{n, tiles, groups, s, stages, stage_bytes, us};
         }
     }
@@ -222,9 +222,9 @@ int run_tall(cfgzip_ctx* ctx, const LayerProduct& p, cudaStream_t st) {
 
 int run_product(cfgzip_ctx* ctx, const LayerProduct& p, cudaStream_t st) {
     const FewPlan f = few_plan(ctx, p);
-    // A stage of 64 k of a pair's 256 x 256 takes 0.28 to 0.4 us, the more the more pairs there are, and some 10 us are not covered by other tiles.
+    // A stage of 64 k of a pair's 256 x 256 takes some 0.3 us, and 8.5 us are not covered by other tiles.
     const int tall_rounds = ceil_div(int64_t(ceil_div(p.rows, kMmaTile)) * ceil_div(p.features, kMmaTile), ctx->sm_count / 2);
-    const double tall = tall_rounds * (ceil_div(p.k, kMmaK) * 0.33) + 10.0;
+    const double tall = tall_rounds * (ceil_div(p.k, kMmaK) * 0.3) + 8.5;
     if (p.rows > 128 && tall < f.us) return run_tall(ctx, p, st);
     return run_few(ctx, p, f, st);
 }

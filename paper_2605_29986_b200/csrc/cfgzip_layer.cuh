@@ -11,7 +11,7 @@ namespace cfgzip {
 
 struct LayerArgs {
     int32_t rows, features;     // of the result
-    int32_t N;                  // rows of a tile: a multiple of 16, at most 128
+    int32_t N;                  // rows of a tile: a multiple of 16, at most 256
     int32_t k_blocks, stages;
     uint32_t stage_bytes;
     int32_t bias_bf16;
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kLayerThreads, 2)
     const int blocks = int(cluster_blocks()), rank = int(cluster_rank());
     const int n0 = int(blockIdx.x) / blocks * 128, row0 = int(blockIdx.y) * a.N, rows = min(a.N, a.rows - row0);
     const int k0 = int(int64_t(a.k_blocks) * rank / blocks), k1 = int(int64_t(a.k_blocks) * (rank + 1) / blocks);
-    const uint32_t columns = a.N <= 32 ? 32u : a.N <= 64 ? 64u : 128u;
+    const uint32_t columns = a.N <= 32 ? 32u : a.N <= 64 ? 64u : a.N <= 128 ? 128u : 256u;
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) {
             mbar_init(&full[i], 1);
