@@ -16,7 +16,7 @@ constexpr int kLogprobsList = 256;       // candidates that are put in order by 
 constexpr int kLogprobsPicks = 128;      // chunks that are read once more, at most
 constexpr int kLogprobsAll = 64;         // ... where all that have an allowed token are
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kLogprobsSlack = 8.f;    // powers of two that a logit may be above the reference of its sum
+constexpr float kLogprobsSlack = 4.f;    // powers of two that a logit may be above the reference of its sum (t is rounded the coarser the larger it is)
 
 struct LogprobsArgs {
     const void* logits;
@@ -159,17 +159,23 @@ struct EntropySums {
     __device__ __forceinline__ void follow(float top, float scale) {
         if (fmaf(top, scale, n) > kLogprobsSlack) move(-rintf(top * scale));
     }
+    // Those of eight logits are added up first (FIRST): of a row that has one probable token the sum is 1 and little, and each addition to the
+    // 1 may take half a step of it.
+    template <bool FIRST>
     __device__ __forceinline__ void add(const float (&f)[8], float scale) {
         const unsigned long long by = pack2(scale, scale), plus = pack2(n, n);
+        unsigned long long of_s = s, of_d = d;
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
             const unsigned long long t = fma2(pack2(f[j], f[j + 1]), by, plus);
             float t0, t1;
             unpack2(t, t0, t1);
             const unsigned long long e = pack2(ex2f(t0), ex2f(t1));
-            s = add2(s, e);
-            d = fma2(e, t, d);
+            of_s = j || !FIRST ? add2(of_s, e) : e;
+            of_d = j || !FIRST ? fma2(e, t, of_d) : mul2(e, t);
         }
+        s = FIRST ? add2(s, of_s) : of_s;
+        d = FIRST ? add2(d, of_d) : of_d;
     }
     __device__ __forceinline__ void move(float to) {
         const float by = to - n, e = ex2f(by);
@@ -178,11 +184,11 @@ struct EntropySums {
         s = mul2(s, e2);
         n = to;
     }
-    __device__ __forceinline__ float2 total() const {
+    __device__ __forceinline__ double2 total() const {
         float s0, s1, d0, d1;
         unpack2(s, s0, s1);
         unpack2(d, d0, d1);
-        return make_float2(s0 + s1, d0 + d1);
+        return make_double2(double(s0) + double(s1), double(d0) + double(d1));
     }
 };
 
@@ -291,14 +297,15 @@ __device__ __forceinline__ Picked pick_largest(float* values, int all, int n, in
 // Equal logits may put too many chunks above a bar. In the order (largest logit, then place) the first n chunks hold the first n tokens (n
 // chunks ahead of a token's own hold n tokens ahead of it), and can be picked one after the other: 0.5 us each.
 //
-// 4096 bf16 rows of 128256 take 171 us (6.1 TB/s), with 5 alternatives 184; 1000 of 100003 under masks 52, bound by instruction issue; 32 of
-// 128256 with 20 alternatives 9, and one of 32000 5, by latency.
+// 4096 bf16 rows of 128256 take 175 us (6.0 TB/s), with 5 alternatives 190; 1000 of 100003 under masks 53, bound by instruction issue; 32 of
+// 128256 with 20 alternatives 9 to 10, and one of 32000 5, by latency. What is done in 64 bits, and eight logits added up first, are 1.5 % of
+// the large ones.
 template <int DT, bool MASKED, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const LogprobsArgs a, int blocks) {
     constexpr int kThreads = WARPS * 32;
     extern __shared__ float s_chunk[];  // the first block's: largest logit of every chunk
-    __shared__ float s_ref[WARPS], s_sum[WARPS], s_dif[WARPS];
-    __shared__ float4 s_block[kClusterMost];
+    __shared__ float s_ref[WARPS], s_block_ref[kClusterMost];
+    __shared__ double2 s_sum[WARPS], s_block[kClusterMost];  // sums of 2^t and 2^t t
     __shared__ unsigned long long s_list[kLogprobsList];
     __shared__ int s_pick[kLogprobsPicks], s_picked, s_listed;
     __shared__ float s_bar, s_most, s_log_sum, s_eight[32 * kLogprobsAll];
@@ -326,6 +333,8 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
 
     __syncwarp();
     cluster_wait();  // (the first block is there to be written to)
+    // (f32 rows under masks have no registers for it: 1000 of 100003 91 us instead of 74)
+    constexpr bool kFirst = !(DT == kF32 && MASKED);
     EntropySums sums(scale);
     float most = kNone;
     // tokens beside the vectors
@@ -339,7 +348,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
             most = fmaxf(most, top);
             if (top > kNone) {
                 sums.follow(mine, scale);
-                sums.add(f, scale);
+                sums.add<kFirst>(f, scale);
             }
             if (a.n_top && lane == 0) st_peer_u32(chunk_at + 4u * uint32_t(edge ? chunks + 1 : 0), __float_as_uint(top));
         }
@@ -374,7 +383,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
         for (int k = 0; k < kAhead; ++k) {
             float f[8];
             v[k].get(f);
-            sums.add(f, scale);
+            sums.add<kFirst>(f, scale);
         }
         if (a.n_top) {
             float of_chunk = redux_max(top[0]);
@@ -393,7 +402,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
         const float mine = chunk_values<DT, MASKED>(a, z, mask, r, c + 1, chunks, lane, f, &first);
         most = fmaxf(most, mine);
         sums.follow(mine, scale);
-        sums.add(f, scale);
+        sums.add<kFirst>(f, scale);
         if (a.n_top) {
             const float of_chunk = redux_max(mine);
             if (lane == 0) st_peer_u32(chunk_at + 4u * uint32_t(c + 1), __float_as_uint(of_chunk));
@@ -402,7 +411,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
     // the block's sums
     most = fmaxf(redux_max(most), kFew);
     sums.move(-rintf(most * scale));
-    float2 t = sums.total();
+    double2 t = sums.total();  // (few additions from here on: in 64 bits)
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) {
         t.x += __shfl_xor_sync(0xFFFFFFFFu, t.x, d);
@@ -410,8 +419,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
     }
     if (lane == 0) {
         s_ref[warp] = most;
-        s_sum[warp] = t.x;
-        s_dif[warp] = t.y;
+        s_sum[warp] = t;
     }
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -419,17 +427,20 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
 #pragma unroll
         for (int w = 1; w < WARPS; ++w) m = fmaxf(m, s_ref[w]);
         const float to = rintf(m * scale);
-        float s = 0.f, d = 0.f;
+        double s = 0.0, d = 0.0;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
+            const double2 p = s_sum[w];
             const float by = rintf(s_ref[w] * scale) - to, e = ex2f(by);
-            s = fmaf(s_sum[w], e, s);
-            d = fmaf(fmaf(by, s_sum[w], s_dif[w]), e, d);
+            s = fma(p.x, double(e), s);
+            d = fma(fma(double(by), p.x, p.y), double(e), d);
         }
+        st_peer_u32(peer_shared(&s_block_ref[rank], 0), __float_as_uint(m));
         const uint32_t at = peer_shared(&s_block[rank], 0);
-        st_peer_u32(at, __float_as_uint(m));
-        st_peer_u32(at + 4, __float_as_uint(s));
-        st_peer_u32(at + 8, __float_as_uint(d));
+        st_peer_u32(at, uint32_t(__double2loint(s)));
+        st_peer_u32(at + 4, uint32_t(__double2hiint(s)));
+        st_peer_u32(at + 8, uint32_t(__double2loint(d)));
+        st_peer_u32(at + 12, uint32_t(__double2hiint(d)));
     }
     __syncwarp();
     cluster_barrier();
@@ -437,22 +448,24 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
 
     if (threadIdx.x == 32) {  // (the second warp, while the first looks for the alternatives)
         float m = kFew;
-        for (int b = 0; b < blocks; ++b) m = fmaxf(m, s_block[b].x);
+        for (int b = 0; b < blocks; ++b) m = fmaxf(m, s_block_ref[b]);
         const float to = rintf(m * scale);
-        float s = 0.f, d = 0.f;
+        double s = 0.0, d = 0.0;
         for (int b = 0; b < blocks; ++b) {
-            const float4 p = s_block[b];
-            const float by = rintf(p.x * scale) - to, e = ex2f(by);
-            s = fmaf(p.y, e, s);
-            d = fmaf(fmaf(by, p.y, p.z), e, d);
+            const double2 p = s_block[b];
+            const float by = rintf(s_block_ref[b] * scale) - to, e = ex2f(by);
+            s = fma(p.x, double(e), s);
+            d = fma(fma(double(by), p.x, p.y), double(e), d);
         }
-        // relative to the largest logit itself, whose exponential is divided out as it was added: a row's only token has log probability 0
-        const float of_most = fmaf(m, scale, -to);
-        const float log_sum = logf(s / ex2f(of_most));  // (-inf where nothing is allowed)
+        // relative to the largest logit itself, whose exponential is taken off and divided out as it was added: a row's only token has log
+        // probability 0, and one that is nearly certain keeps what the others have together
+        const float of_most = fmaf(m, scale, -to), e_most = ex2f(of_most);
+        const double rest = s - double(e_most);
+        const float log_sum = log1pf(float(rest) / e_most);  // (-inf where nothing is allowed)
         s_most = m;
         s_log_sum = log_sum;
-        if (a.lse) a.lse[row] = s > 0.f ? fmaf(m, a.inv_temperature, log_sum) : -INFINITY;
-        if (a.entropy) a.entropy[row] = s > 0.f ? fmaxf(log_sum - kLn2 * (d / s - of_most), 0.f) : 0.f;
+        if (a.lse) a.lse[row] = s > 0.0 ? fmaf(m, a.inv_temperature, log_sum) : -INFINITY;
+        if (a.entropy) a.entropy[row] = s > 0.0 ? fmaxf(log_sum - kLn2 * (float(fma(-double(of_most), rest, d - double(e_most * of_most))) / float(s)), 0.f) : 0.f;
         if (a.tokens) {
             float logp = 0.f;
             if (token >= 0) logp = of_token > kFew ? fmaf(of_token - m, a.inv_temperature, -log_sum) : -INFINITY;

@@ -393,3 +393,28 @@ def test_captured_calls_on_another_stream_and_two_at_once():
             torch.cuda.synchronize()
             for (out, d), (o, to) in zip(want, results):
                 assert all(torch.equal(out[k], o[k]) for k in out) and torch.equal(d, to)
+
+
+@pytest.mark.parametrize("V", [2000, 50000])
+def test_a_nearly_certain_token_keeps_what_the_others_have_together(V):
+    """The sum is 1 and little: its logarithm is good to the bits of the little, not of the 1, where both are added up by different threads."""
+    N, st = 3, torch.cuda.current_stream()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    z = torch.empty((N, V), device="cuda").normal_(generator=g)
+    z[:, :8] = -math.inf
+    z[:, 5] = torch.tensor([18.0, 21.5, 25.0], device="cuda")
+    tokens = torch.full((N,), 5, dtype=torch.int32, device="cuda")
+    logp, entropy, lse = (torch.zeros(N, device="cuda") for _ in range(3))
+    with Ctx([]) as ctx:
+        cz.cfgzip_token_logprobs(ctx.h, z, cz.F32, V, N, V, None, 0, tokens, 1.0, 0, logp, entropy, lse, None, None, st)
+        torch.cuda.synchronize()
+    want = torch.log_softmax(z.double(), dim=1)
+    # the others' terms: 2^t with t of 45 at most, rounded once (2^-19 ln 2), a scale good to 2^-24 (45 times 2^-24 ln 2), an exponential
+    # good to 2^-22, and additions of as many: together below 2^-18; of the entropy's terms t counts once more. 196 runs of 256 tokens are
+    # dealt to 16 times 8 warps: one thread adds a second eight tokens to its sum of the certain one, half a step of a number up to sqrt(2)
+    # (its sum of 2^t t, t up to 1/2, is smaller)
+    second = 2.0 ** -24 if V > 2048 else 0.0
+    assert ((logp - want[:, 5]).abs() <= 2.0 ** -17 * want[:, 5].abs() + second).all()
+    want_entropy = torch.special.entr(want.exp()).sum(dim=1)
+    assert ((entropy - want_entropy).abs() <= 2.0 ** -16 * want_entropy + 2 * second).all()
