@@ -108,8 +108,7 @@ inline int tensor_map_out(cfgzip_ctx* ctx, CUtensorMap* map, const MmaArgs& a, b
 }
 
 // Rows of A, where its k is contiguous, in a block's copies: what lies behind the last one is not asked for (rows outside a map cost the
-// copies more than they seem: log probabilities of one row of 32000 x 2048 46 -> 31 us, of 128256 x 4096 221 -> 191), and the sums of
-// whatever stands in shared memory there are not stored.
+// copies more than they seem: log probabilities of one row of 32000 x 2048 46 -> 31 us, of 128256 x 4096 221 -> 191).
 inline int a_box(int64_t rows) { return int(std::min<int64_t>(128, up(rows, 8))); }
 
 template <bool A_MN, bool B_MN, int KIND, bool LONG = true>
