@@ -89,6 +89,9 @@ int cfgzip_token_logprobs(cfgzip_ctx* ctx, const void* logits, int dtype, int64_
     a.mask_stride = vocab_stride_words;
     a.tokens = tokens;
     a.inv_temperature = inv_temperature;
+    a.powers.scale = inv_temperature * kLog2e;
+    a.powers.far = kFarPowers / a.powers.scale;
+    a.powers.slack = kLogprobsSlack / a.powers.scale;
     a.n_top = n_top;
     a.logp = logp;
     a.entropy = entropy;

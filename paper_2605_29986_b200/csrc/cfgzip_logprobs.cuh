@@ -18,6 +18,12 @@ constexpr int kLogprobsAll = 64;         // ... where all that have an allowed t
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLogprobsSlack = 4.f;    // powers of two that a logit may be above the reference of its sum (t is rounded the coarser the larger it is)
 
+// Logits in powers of two: `scale` powers to a unit (log2(e) / T); from `far` on the whole number next to a logit's powers would have to be
+// rounded itself; `slack` is kLogprobsSlack powers.
+struct Powers {
+    float scale, far, slack;
+};
+
 struct LogprobsArgs {
     const void* logits;
     int64_t stride;
@@ -26,6 +32,7 @@ struct LogprobsArgs {
     int64_t mask_stride;
     const int32_t* tokens;
     float inv_temperature;
+    Powers powers;
     int32_t n_top;
     float *logp, *entropy, *lse;
     int32_t* top_tokens;
@@ -105,6 +112,14 @@ struct Logits8<kBF16> {
         const uint32_t m = max_bf16x2(max_bf16x2(v.x, v.y), max_bf16x2(v.z, v.w));
         return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
     }
+    // Less `top`, not below kNone (a difference that bf16 does not hold is far beyond what weighs anything: see Reference).
+    __device__ __forceinline__ void relative_to(float top) {
+        float f[8];
+        get(f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = fmaxf(f[j] - top, kNone);
+        v = make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
+    }
     __device__ __forceinline__ void get(float (&f)[8]) const {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -142,6 +157,11 @@ struct Logits8<kF32> {
         }
         return fmaxf(fmax3(fmax3(f[0], f[1], f[2]), f[3], f[4]), fmax3(f[5], f[6], f[7]));
     }
+    __device__ __forceinline__ void relative_to(float top) {
+        uint32_t* const w[8] = {&a.x, &a.y, &a.z, &a.w, &b.x, &b.y, &b.z, &b.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) *w[j] = __float_as_uint(fmaxf(__uint_as_float(*w[j]) - top, kNone));
+    }
     __device__ __forceinline__ void get(float (&f)[8]) const {
         const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -149,20 +169,39 @@ struct Logits8<kF32> {
     }
 };
 
-// Sums of 2^t and 2^t t, t = z log2(e) / T + n, over a thread's logits. The reference -n is a whole number, so that t is rounded once however
-// far from zero a row is, all threads' t are of the same numbers, and a sum goes over to another reference exactly. It follows the largest
-// logit so far: up to kLogprobsSlack below it.
+// What t, the exponent of a logit in powers of two, is relative to: a logit `top`. Near zero that is the whole number of powers next to it, -n:
+// t = z scale + n is rounded once, all threads' t are of the same numbers, and a sum goes over to another reference exactly. Far from zero a
+// float holds no such n (that of -1e10 would be off by 440 powers): t = (z - top) scale, whose difference is exact wherever it does not come
+// to millions of powers. (`top` alone is kept: f32 rows under masks have no register for more, 1000 of 100003 71 and 86 us.)
+constexpr float kFarPowers = 4194304.f;
+struct Reference {
+    float top;
+    __device__ __forceinline__ bool far(const Powers& p) const { return fabsf(top) >= p.far; }
+    __device__ __forceinline__ float near_n(const Powers& p) const {
+        constexpr float kWhole = 12582912.f;  // (its step is 1: nearest whole number)
+        return kWhole - fmaf(top, p.scale, kWhole);
+    }
+    __device__ __forceinline__ float r(const Powers& p) const { return far(p) ? top : 0.f; }
+    __device__ __forceinline__ float n(const Powers& p) const { return far(p) ? 0.f : near_n(p); }
+    __device__ __forceinline__ float power(float z, const Powers& p) const { return fmaf(z - r(p), p.scale, n(p)); }
+    // What has to be added to t to have it relative to a reference that is no lower. (Bounded, so that an empty sum stays 0 and one that is too
+    // low to count becomes 0.)
+    __device__ __forceinline__ float to(const Reference& other, const Powers& p) const {
+        return fminf(fmaxf(fmaf(r(p) - other.r(p), p.scale, other.n(p) - n(p)), -4096.f), 1.f);
+    }
+};
+
+// Sums of 2^t and 2^t t over a thread's logits. The reference follows the largest logit so far: up to kLogprobsSlack below it.
 struct EntropySums {
-    float n;                          // (of kFew at first: what counts moves it)
+    Reference at{kFew};
     unsigned long long s = 0, d = 0;  // pairs of partial sums
-    __device__ __forceinline__ explicit EntropySums(float scale) : n(-rintf(kFew * scale)) {}
-    __device__ __forceinline__ void follow(float top, float scale) {
-        if (fmaf(top, scale, n) > kLogprobsSlack) move(-rintf(top * scale));
+    __device__ __forceinline__ void follow(float top, const Powers& p) {
+        if (top - at.top > p.slack) move(Reference{top}, p);
     }
     // Those of eight logits are added up first (FIRST): of a row that has one probable token the sum is 1 and little, and each addition to the
-    // 1 may take half a step of it.
+    // 1 may take half a step of it. Where the reference is far from zero the logits have been made relative to it.
     template <bool FIRST>
-    __device__ __forceinline__ void add(const float (&f)[8], float scale) {
+    __device__ __forceinline__ void add(const float (&f)[8], float scale, float n) {
         const unsigned long long by = pack2(scale, scale), plus = pack2(n, n);
         unsigned long long of_s = s, of_d = d;
 #pragma unroll
@@ -177,12 +216,22 @@ struct EntropySums {
         s = FIRST ? add2(s, of_s) : of_s;
         d = FIRST ? add2(d, of_d) : of_d;
     }
-    __device__ __forceinline__ void move(float to) {
-        const float by = to - n, e = ex2f(by);
+    // ... of eight that a thread has at a time, `top` the largest
+    template <bool FIRST>
+    __device__ __forceinline__ void take(float (&f)[8], float top, const Powers& p) {
+        follow(top, p);
+        if (at.far(p) && top > kFew) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = fmaxf(f[j] - at.top, kNone);
+        }
+        add<FIRST>(f, p.scale, at.n(p));
+    }
+    __device__ __forceinline__ void move(const Reference& to, const Powers& p) {
+        const float by = at.to(to, p), e = ex2f(by);
         const unsigned long long e2 = pack2(e, e);
         d = mul2(fma2(pack2(by, by), s, d), e2);
         s = mul2(s, e2);
-        n = to;
+        at = to;
     }
     __device__ __forceinline__ double2 total() const {
         float s0, s1, d0, d1;
@@ -312,7 +361,6 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t row = blockIdx.x / blocks;
     const int rank = int(blockIdx.x - row * blocks);
-    const float scale = a.inv_temperature * kLog2e;
     const char* z = static_cast<const char*>(a.logits) + row * a.stride * (DT == kBF16 ? 2 : 4);
     const uint8_t* mask = MASKED ? reinterpret_cast<const uint8_t*>(a.mask + row * a.mask_stride) : nullptr;
     const RowShape r = row_shape<DT>(z, a.V);
@@ -335,7 +383,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
     cluster_wait();  // (the first block is there to be written to)
     // (f32 rows under masks have no registers for it: 1000 of 100003 91 us instead of 74)
     constexpr bool kFirst = !(DT == kF32 && MASKED);
-    EntropySums sums(scale);
+    EntropySums sums;
     float most = kNone;
     // tokens beside the vectors
     if (warp == 0 && (rank == 0 || rank == blocks - 1)) {
@@ -347,8 +395,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
             const float top = redux_max(mine);
             most = fmaxf(most, top);
             if (top > kNone) {
-                sums.follow(mine, scale);
-                sums.add<kFirst>(f, scale);
+                sums.take<kFirst>(f, mine, a.powers);
             }
             if (a.n_top && lane == 0) st_peer_u32(chunk_at + 4u * uint32_t(edge ? chunks + 1 : 0), __float_as_uint(top));
         }
@@ -378,12 +425,20 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
             mine = fmaxf(mine, top[k]);
         }
         most = fmaxf(most, mine);
-        sums.follow(mine, scale);
+        sums.follow(mine, a.powers);
+        float n = sums.at.near_n(a.powers);
+        if (sums.at.far(a.powers)) {
+            n = 0.f;
+            if (mine > kFew) {  // (masked ones weigh nothing as they are)
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) v[k].relative_to(sums.at.top);
+            }
+        }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             float f[8];
             v[k].get(f);
-            sums.add<kFirst>(f, scale);
+            sums.add<kFirst>(f, a.powers.scale, n);
         }
         if (a.n_top) {
             float of_chunk = redux_max(top[0]);
@@ -401,8 +456,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
         int first;
         const float mine = chunk_values<DT, MASKED>(a, z, mask, r, c + 1, chunks, lane, f, &first);
         most = fmaxf(most, mine);
-        sums.follow(mine, scale);
-        sums.add<kFirst>(f, scale);
+        sums.take<kFirst>(f, mine, a.powers);
         if (a.n_top) {
             const float of_chunk = redux_max(mine);
             if (lane == 0) st_peer_u32(chunk_at + 4u * uint32_t(c + 1), __float_as_uint(of_chunk));
@@ -410,7 +464,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
     }
     // the block's sums
     most = fmaxf(redux_max(most), kFew);
-    sums.move(-rintf(most * scale));
+    sums.move(Reference{most}, a.powers);
     double2 t = sums.total();  // (few additions from here on: in 64 bits)
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) {
@@ -426,12 +480,12 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
         float m = s_ref[0];
 #pragma unroll
         for (int w = 1; w < WARPS; ++w) m = fmaxf(m, s_ref[w]);
-        const float to = rintf(m * scale);
+        const Reference to{m};
         double s = 0.0, d = 0.0;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
             const double2 p = s_sum[w];
-            const float by = rintf(s_ref[w] * scale) - to, e = ex2f(by);
+            const float by = Reference{s_ref[w]}.to(to, a.powers), e = ex2f(by);
             s = fma(p.x, double(e), s);
             d = fma(fma(double(by), p.x, p.y), double(e), d);
         }
@@ -449,17 +503,17 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
     if (threadIdx.x == 32) {  // (the second warp, while the first looks for the alternatives)
         float m = kFew;
         for (int b = 0; b < blocks; ++b) m = fmaxf(m, s_block_ref[b]);
-        const float to = rintf(m * scale);
+        const Reference to{m};
         double s = 0.0, d = 0.0;
         for (int b = 0; b < blocks; ++b) {
             const double2 p = s_block[b];
-            const float by = rintf(s_block_ref[b] * scale) - to, e = ex2f(by);
+            const float by = Reference{s_block_ref[b]}.to(to, a.powers), e = ex2f(by);
             s = fma(p.x, double(e), s);
             d = fma(fma(double(by), p.x, p.y), double(e), d);
         }
         // relative to the largest logit itself, whose exponential is taken off and divided out as it was added: a row's only token has log
         // probability 0, and one that is nearly certain keeps what the others have together
-        const float of_most = fmaf(m, scale, -to), e_most = ex2f(of_most);
+        const float of_most = to.power(m, a.powers), e_most = ex2f(of_most);
         const double rest = s - double(e_most);
         const float log_sum = log1pf(float(rest) / e_most);  // (-inf where nothing is allowed)
         s_most = m;
@@ -603,22 +657,24 @@ struct LogprobsBackwardArgs {
 
 // What of a row's gradient does not depend on the token: g = p (a + b x) with x = zt - lse, and at the given token
 // -d expm1(x) + p b (x + entropy), which keeps what is left of d (1 - p) where the model is sure.
+// x above 0 is what lse was rounded by, a half at the most below 2^24; further out lse says nothing of p, which is kept within e.
 struct RowGradient {
     float lse, a, b, d, entropy;
     int token;
+    static __device__ __forceinline__ float within(float x) { return fminf(fmaxf(x, -200.f), 1.f); }
     __device__ __forceinline__ float at(float z, float inv_temperature) const {
-        const float x = fmaxf(fmaf(z, inv_temperature, -lse), -200.f);
+        const float x = within(fmaf(z, inv_temperature, -lse));
         return ex2f(x * kLog2e) * fmaf(b, x, a);
     }
     __device__ __forceinline__ void at_pair(float z0, float z1, float inv_temperature, float* d0, float* d1) const {
         float x0, x1;
         unpack2(fma2(pack2(z0, z1), pack2(inv_temperature, inv_temperature), pack2(-lse, -lse)), x0, x1);
-        const unsigned long long x = pack2(fmaxf(x0, -200.f), fmaxf(x1, -200.f));
+        const unsigned long long x = pack2(within(x0), within(x1));
         unpack2(mul2(x, pack2(kLog2e, kLog2e)), x0, x1);
         unpack2(mul2(pack2(ex2f(x0), ex2f(x1)), fma2(pack2(b, b), x, pack2(a, a))), *d0, *d1);
     }
     __device__ __forceinline__ float at_token(float z, float inv_temperature) const {
-        const float x = fmaf(z, inv_temperature, -lse);
+        const float x = within(fmaf(z, inv_temperature, -lse));
         return fmaf(ex2f(x * kLog2e) * b, x + entropy, -d * expm1f(x));
     }
 };
