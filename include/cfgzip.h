@@ -351,7 +351,7 @@ int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidde
  * states of rows without a loss have to be finite here (what they are otherwise makes no difference).
  *   hidden .. targets : as given to cfgzip_head_loss, and lse as it returned it (required)
  *   d_loss     : dev float [N]
- *   d_hidden   : nullable dev bf16 [N, d_hidden_stride] (written)
+ *   d_hidden   : nullable dev bf16 [N, d_hidden_stride] (written at the end: it may be in the place of the hidden states)
  *   d_weight   : nullable dev [V, d_weight_stride] of d_weight_dtype (CFGZIP_BF16 or CFGZIP_F32); written, or added to where
  *                accumulate is not 0
  * The results do not depend on timing (no atomic additions).

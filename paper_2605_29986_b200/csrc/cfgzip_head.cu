@@ -196,6 +196,12 @@ int run_step(cfgzip_ctx* ctx, HeadStepArgs& a, const cfgzip_head* head, const ui
     return launch(ctx, kern, dim3(blocks), dim3((mx ? kStepWarpsMx : kStepWarps) * 32), smem, st, a, map_x, map_w, map_box);
 }
 
+// Do two matrices of `rows` rows of `n` bf16 numbers have memory in common, rows and what is between them taken together?
+bool overlap(const void* p, int64_t p_stride, const void* q, int64_t q_stride, int64_t rows, int n) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a < b + uintptr_t((rows - 1) * q_stride + n) * 2 && b < a + uintptr_t((rows - 1) * p_stride + n) * 2;
+}
+
 // What a gradient is of: of the loss, or of log probabilities and entropies.
 struct GradientOf {
     const int32_t* targets;
@@ -339,6 +345,11 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
         r.weight = static_cast<const uint16_t*>(head->weight);
         r.weight_stride = head->row_stride;
         const int rows = d_weight ? N : 0;
+        // (in one launch the hidden states would be read while a gradient in their place is written)
+        if (rows && d_hidden && overlap(hidden, hidden_stride, d_hidden, d_hidden_stride, N, H)) {
+            rc = launch(ctx, k_head_targets_finish, dim3(unsigned(rows)), dim3(256), 0, st, t, r, rows);
+            return rc != CFGZIP_OK ? rc : launch(ctx, k_head_targets_finish, dim3(unsigned(blocks)), dim3(256), 0, st, t, r, 0);
+        }
         return launch(ctx, k_head_targets_finish, dim3(unsigned(rows + (d_hidden ? blocks : 0))), dim3(256), 0, st, t, r, rows);
     }
     if (!d_hidden) return CFGZIP_OK;
