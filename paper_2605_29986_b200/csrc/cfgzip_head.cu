@@ -216,7 +216,7 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
     int rc = check_head(head);
     if (rc != CFGZIP_OK) return rc;
     if (head->dtype != CFGZIP_BF16 || N < 0 || (!d_hidden && !d_weight)) return CFGZIP_E_ARG;
-    if (N > kHeadTokens) return CFGZIP_E_RANGE;
+    if (N > kHeadTokens || (of.scores && int64_t(N) * ceil_div(head->H, kTargetCols) > kHeadTokens)) return CFGZIP_E_RANGE;  // (blocks)
     if (d_weight) {
         if ((d_weight_dtype != CFGZIP_F32 && d_weight_dtype != CFGZIP_BF16) || d_weight_stride < head->H) return CFGZIP_E_ARG;
         if (!on16(d_weight, d_weight_stride * (d_weight_dtype == CFGZIP_BF16 ? 2 : 4))) return CFGZIP_E_ALIGN;
@@ -328,6 +328,7 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
         t.hidden_stride = hidden_stride;
         t.to = d_weight;
         t.to_stride = d_weight_stride;
+        t.N = N;
         t.V = head->V;
         t.H = H;
         t.bf16 = d_weight_dtype == CFGZIP_BF16;
@@ -344,13 +345,14 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
         r.rest = w.rest;
         r.weight = static_cast<const uint16_t*>(head->weight);
         r.weight_stride = head->row_stride;
-        const int rows = d_weight ? N : 0;
+        const int rows = d_weight ? N : 0, slices = ceil_div(N, kTargetSlice), ahead = d_weight && N > kTargetSteps ? slices * ceil_div(H, kTargetCols) : 0;
         // (in one launch the hidden states would be read while a gradient in their place is written)
         if (rows && d_hidden && overlap(hidden, hidden_stride, d_hidden, d_hidden_stride, N, H)) {
-            rc = launch(ctx, k_head_targets_finish, dim3(unsigned(rows)), dim3(256), 0, st, t, r, rows);
-            return rc != CFGZIP_OK ? rc : launch(ctx, k_head_targets_finish, dim3(unsigned(blocks)), dim3(256), 0, st, t, r, 0);
+            rc = launch(ctx, k_head_targets_finish, dim3(unsigned(ahead + rows)), dim3(256), 0, st, t, r, ahead, slices, rows);
+            return rc != CFGZIP_OK ? rc : launch(ctx, k_head_targets_finish, dim3(unsigned(blocks)), dim3(256), 0, st, t, r, 0, 0, 0);
         }
-        return launch(ctx, k_head_targets_finish, dim3(unsigned(rows + (d_hidden ? blocks : 0))), dim3(256), 0, st, t, r, rows);
+        return launch(ctx, k_head_targets_finish, dim3(unsigned(ahead + rows + (d_hidden ? blocks : 0))), dim3(256), 0, st, t, r, ahead,
+                      slices, rows);
     }
     if (!d_hidden) return CFGZIP_OK;
     return launch(ctx, k_head_round, dim3(unsigned(blocks)), dim3(256), 0, st, (const float*)w.sums, int64_t(N) * H, splits,

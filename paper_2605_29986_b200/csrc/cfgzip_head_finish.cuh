@@ -248,7 +248,11 @@ __global__ void __launch_bounds__(256) k_head_targets(const int32_t* targets, in
 }
 
 // The rows of the head's gradient that are targets, once more: their sums as they were kept, and what their rows' g was rounded by times the
-// hidden states. A block a row of the text; the first row of a chain does all of it.
+// hidden states. A block a row of the text; the first row of a chain does all of it. Each step along a chain is a load that waits for the one
+// before. Answers under a grammar repeat some tokens again and again: chains of more than kTargetSteps rows are listed by looking through the
+// targets, and have a block for every kTargetCols columns, in which four groups of threads add up every fourth row, four loads in flight
+// (gradient of 1000 tokens of 32000 x 2048, all the same: 775 us along the chain).
+constexpr int kTargetCols = 512, kTargetSteps = 8, kTargetList = 1024, kTargetSlice = 4;
 struct WeightTargetsArgs {
     const int32_t *targets, *first_of, *next_of;
     const float *rest, *kept;
@@ -256,37 +260,121 @@ struct WeightTargetsArgs {
     int64_t hidden_stride;
     void* to;
     int64_t to_stride;
-    int32_t V, H, bf16;
+    int32_t N, V, H, bf16;
 };
+__device__ __forceinline__ void store_weight_targets(const WeightTargetsArgs& a, int target, int c, const float4& f) {
+    if (a.bf16)
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.to) + target * a.to_stride + c) = make_uint2(bf16_pair(f.x, f.y), bf16_pair(f.z, f.w));
+    else
+        *reinterpret_cast<float4*>(static_cast<float*>(a.to) + target * a.to_stride + c) = f;
+}
+__device__ __forceinline__ void weight_targets_of_many(const WeightTargetsArgs& a, int row, int target, int c0) {
+    __shared__ int s_row[kTargetList], s_count[32];
+    __shared__ float s_rest[kTargetList];
+    __shared__ __align__(16) float s_sum[4][kTargetCols];
+    const int warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31, group = int(threadIdx.x) >> 6, mine = 8 * (int(threadIdx.x) & 63);
+    const bool some = c0 + mine < a.H;
+    float f[8] = {};
+    for (int n0 = row; n0 < a.N; n0 += kTargetList) {  // 1024 targets at a time, those that are this one in the rows' order
+        uint32_t same[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int n = n0 + 256 * q + int(threadIdx.x);
+            same[q] = __ballot_sync(0xFFFFFFFFu, n < a.N && ld_after_wait(a.targets + n) == target);
+            if (lane == 0) s_count[8 * q + warp] = __popc(same[q]);
+        }
+        __syncthreads();
+        const int count = s_count[lane];
+        int ahead = count;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int x = __shfl_up_sync(0xFFFFFFFFu, ahead, d);
+            ahead += lane >= d ? x : 0;
+        }
+        const int all = __shfl_sync(0xFFFFFFFFu, ahead, 31);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int at = __shfl_sync(0xFFFFFFFFu, ahead - count, 8 * q + warp) + __popc(same[q] & ((1u << lane) - 1u));
+            if ((same[q] >> lane) & 1u) {
+                const int n = n0 + 256 * q + int(threadIdx.x);
+                s_row[at] = n;
+                s_rest[at] = ld_after_wait(a.rest + n);
+            }
+        }
+        __syncthreads();
+        if (some) {
+#pragma unroll 4
+            for (int i = group; i < all; i += 4) {
+                float x[8];
+                bf16_values(ld_after_wait(reinterpret_cast<const uint4*>(a.hidden + int64_t(s_row[i]) * a.hidden_stride + c0 + mine)), x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = fmaf(s_rest[i], x[j], f[j]);
+            }
+        }
+        __syncthreads();
+    }
+    if (some) {
+        *reinterpret_cast<float4*>(&s_sum[group][mine]) = make_float4(f[0], f[1], f[2], f[3]);
+        *reinterpret_cast<float4*>(&s_sum[group][mine + 4]) = make_float4(f[4], f[5], f[6], f[7]);
+    }
+    __syncthreads();
+    const int at = 4 * int(threadIdx.x);
+    if (at >= kTargetCols || c0 + at >= a.H) return;
+    float4 sum = __ldcg(reinterpret_cast<const float4*>(a.kept + int64_t(row) * a.H + c0 + at));
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const float4 x = *reinterpret_cast<const float4*>(&s_sum[g][at]);
+        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+    }
+    store_weight_targets(a, target, c0 + at, sum);
+}
+// The first row of a chain: -1 where this row is none, else the row behind it, or kTargetMany behind kTargetSteps rows.
+constexpr int kTargetNone = -2, kTargetMany = INT_MAX;
+__device__ __forceinline__ int chain_of(const WeightTargetsArgs& a, int row, int target) {
+    if (target < 0 || target >= a.V || ld_after_wait(a.first_of + target) != row) return kTargetNone;
+    const int next = ld_after_wait(a.next_of + row);
+    int m = next;
+    for (int n = 1; m >= 0 && n < kTargetSteps; ++n) m = ld_after_wait(a.next_of + m);
+    return m >= 0 ? kTargetMany : next;
+}
 __device__ __forceinline__ void weight_targets(const WeightTargetsArgs& a, int row) {
-    const int target = ld_after_wait(a.targets + row);
-    if (target < 0 || target >= a.V || ld_after_wait(a.first_of + target) != row) return;
+    const int target = ld_after_wait(a.targets + row), next = chain_of(a, row, target);
+    if (next == kTargetNone || next == kTargetMany) return;
     for (int c = 4 * int(threadIdx.x); c < a.H; c += 1024) {
-        const float4 sum = __ldcg(reinterpret_cast<const float4*>(a.kept + int64_t(row) * a.H + c));
-        float f[4] = {sum.x, sum.y, sum.z, sum.w};
-        for (int m = row; m >= 0; m = ld_after_wait(a.next_of + m)) {
+        float4 f = __ldcg(reinterpret_cast<const float4*>(a.kept + int64_t(row) * a.H + c));
+        for (int m = row; m >= 0; m = m == row ? next : ld_after_wait(a.next_of + m)) {
             const float rest = ld_after_wait(a.rest + m);
             const uint2 x = *reinterpret_cast<const uint2*>(a.hidden + int64_t(m) * a.hidden_stride + c);
-            f[0] = fmaf(rest, __uint_as_float(x.x << 16), f[0]);
-            f[1] = fmaf(rest, __uint_as_float(x.x & 0xFFFF0000u), f[1]);
-            f[2] = fmaf(rest, __uint_as_float(x.y << 16), f[2]);
-            f[3] = fmaf(rest, __uint_as_float(x.y & 0xFFFF0000u), f[3]);
+            f.x = fmaf(rest, __uint_as_float(x.x << 16), f.x);
+            f.y = fmaf(rest, __uint_as_float(x.x & 0xFFFF0000u), f.y);
+            f.z = fmaf(rest, __uint_as_float(x.y << 16), f.z);
+            f.w = fmaf(rest, __uint_as_float(x.y & 0xFFFF0000u), f.w);
         }
-        if (a.bf16)
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.to) + target * a.to_stride + c) = make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]));
-        else
-            *reinterpret_cast<float4*>(static_cast<float*>(a.to) + target * a.to_stride + c) = make_float4(f[0], f[1], f[2], f[3]);
+        store_weight_targets(a, target, c, f);
+    }
+}
+// ... of the chains of many rows that begin in kTargetSlice rows from `first` on, kTargetCols columns from c0 on
+__device__ __forceinline__ void weight_targets_of_slice(const WeightTargetsArgs& a, int first, int c0) {
+    const int lane = int(threadIdx.x) & 31, mine = first + lane, target = lane < kTargetSlice && mine < a.N ? ld_after_wait(a.targets + mine) : -1;
+    uint32_t many = __ballot_sync(0xFFFFFFFFu, chain_of(a, mine, target) == kTargetMany);
+    for (; many; many &= many - 1) {
+        const int of = __ffs(many) - 1;
+        weight_targets_of_many(a, first + of, __shfl_sync(0xFFFFFFFFu, target, of), c0);
+        __syncthreads();
     }
 }
 
-// Both, one behind the other: the first `rows` blocks take a row's target each.
-__global__ void __launch_bounds__(256) k_head_targets_finish(const WeightTargetsArgs w, const RoundTargetsArgs r, int rows) {
+// Both, one behind the other: the first `ahead` blocks look for chains of many rows, for a number of columns each, `rows` blocks take a row's
+// target each.
+__global__ void __launch_bounds__(256, 8) k_head_targets_finish(const WeightTargetsArgs w, const RoundTargetsArgs r, int ahead, int slices, int rows) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (int(blockIdx.x) < rows)
-        weight_targets(w, int(blockIdx.x));
+    if (int(blockIdx.x) < ahead)
+        weight_targets_of_slice(w, int(blockIdx.x) % slices * kTargetSlice, int(blockIdx.x) / slices * kTargetCols);
+    else if (int(blockIdx.x) < ahead + rows)
+        weight_targets(w, int(blockIdx.x) - ahead);
     else
-        round_targets(r, int(blockIdx.x) - rows, int(gridDim.x) - rows);
+        round_targets(r, int(blockIdx.x) - ahead - rows, int(gridDim.x) - ahead - rows);
 }
 
 }  // namespace cfgzip
