@@ -72,7 +72,9 @@ __global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
     a.loss[row] = loss;
 }
 
-// The same for log probabilities and entropies. A state's reference is its largest score, kFew where it has none.
+// The same for log probabilities and entropies. A state's reference is its largest score, kFew where it has none. Differences of references are
+// bounded where their exponential is 0: a sum of many times one may be infinite, and the sum of exp(d) d with it NaN.
+constexpr float kNothing = -4096.f;
 struct LogprobsFinishArgs {
     const float4* sums;
     const float* of_target;
@@ -100,12 +102,12 @@ __global__ void __launch_bounds__(256) k_head_logprobs_finish(const LogprobsFini
             float next = m;
 #pragma unroll
             for (int k = 0; k < 5; ++k) next = fmaxf(next, p[k].x);
-            const float by = m - next, e = ex2f(by * kLog2e);
+            const float by = fmaxf(m - next, kNothing), e = ex2f(by * kLog2e);
             d = fmaf(by, s, d) * e;
             s *= e;
 #pragma unroll
             for (int k = 0; k < 5; ++k) {
-                const float of = p[k].x - next, f = ex2f(of * kLog2e);
+                const float of = fmaxf(p[k].x - next, kNothing), f = ex2f(of * kLog2e);
                 d = fmaf(fmaf(of, p[k].y, p[k].z), f, d);
                 s = fmaf(p[k].y, f, s);
             }
@@ -127,7 +129,7 @@ __global__ void __launch_bounds__(256) k_head_logprobs_finish(const LogprobsFini
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
         const float4 p = sh[8 * (lane >> 2) + w][lane & 3];
-        const float of = p.x - top, f = ex2f(of * kLog2e);
+        const float of = fmaxf(p.x - top, kNothing), f = ex2f(of * kLog2e);
         d = fmaf(fmaf(of, p.y, p.z), f, d);
         s = fmaf(p.y, f, s);
     }

@@ -86,3 +86,33 @@ def test_tokens_that_come_again_take_no_other_time():
             return min(times)
 
         assert least(torch.full_like(tokens, 7)) <= 4 * least(tokens)
+
+
+def scored(ctx, weight, hidden, tokens):
+    V, H, N = weight.shape[0], weight.shape[1], hidden.shape[0]
+    head = cz.cfgzip_head(weight, cz.BF16, V, H)
+    ws = torch.empty(cz.cfgzip_head_workspace(head, cz.HEAD_LOGPROBS, N), dtype=torch.uint8, device="cuda")
+    logp, entropy, lse = (torch.full((N,), 99.0, device="cuda") for _ in range(3))
+    cz.cfgzip_head_logprobs(ctx.h, head, hidden, H, N, None, 0, tokens, logp, entropy, lse, ws, ws.numel(), torch.cuda.current_stream())
+    return logp, entropy, lse
+
+
+@pytest.mark.parametrize("size", [1e35, 3e36, 2e37, 1.5e38])
+def test_scores_as_large_as_a_float_holds(size):
+    """One token's score, and whole tiles of tokens at 0 or at as much below it."""
+    V, H, N = 3000, 64, 300
+    weight = torch.zeros((V, H), dtype=torch.bfloat16, device="cuda")
+    weight[2500, 0], weight[600:900, 0] = 1.0, -1.0
+    hidden = torch.zeros((N, H), dtype=torch.bfloat16, device="cuda")
+    hidden[:, 0] = size
+    hidden[1::2, 0] = -size
+    tokens = torch.full((N,), 2500, dtype=torch.int32, device="cuda")
+    tokens[1::2] = 700
+    with Ctx([]) as ctx:
+        logp, entropy, lse = scored(ctx, weight, hidden, tokens)
+    of = hidden[:, 0].float().abs()
+    assert (lse == of).all()
+    log_n = torch.log(torch.tensor(300.0, dtype=torch.float64)).item()
+    assert (logp[::2] == 0).all() and (entropy[::2] == 0).all()
+    # three hundred equal scores, in exact arithmetic: the roundings of a logarithm
+    assert ((logp[1::2] + log_n).abs() <= 2.0 ** -20).all() and ((entropy[1::2] - log_n).abs() <= 2.0 ** -20).all()
