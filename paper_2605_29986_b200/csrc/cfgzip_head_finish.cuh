@@ -72,9 +72,18 @@ __global__ void __launch_bounds__(256) k_head_loss_finish(const FinishArgs a) {
     a.loss[row] = loss;
 }
 
-// The same for log probabilities and entropies. A state's reference is its largest score, kFew where it has none. Differences of references are
-// bounded where their exponential is 0: a sum of many times one may be infinite, and the sum of exp(d) d with it NaN.
+// The same for log probabilities and entropies. A state is its largest score, kFew where it has none, the sum of exp(d) without the scores that
+// are the largest, the sum of exp(d) d, and how many are the largest: of a row that has one probable token the sum is 1 and little, and the
+// little is what its log probability and entropy are. Differences of references are bounded where their exponential is 0: a sum of many times
+// one may be infinite, and the sum of exp(d) d with it NaN.
 constexpr float kNothing = -4096.f;
+__device__ __forceinline__ void add_state(const float4& p, float ref, float& n, float& s, float& d) {
+    const float of = fmaxf(p.x - ref, kNothing), f = ex2f(of * kLog2e);
+    const bool same = p.x == ref;
+    d = fmaf(fmaf(of, p.y + p.w, p.z), f, d);
+    n += same ? p.w : 0.f;
+    s = fmaf(same ? p.y : p.y + p.w, f, s);
+}
 struct LogprobsFinishArgs {
     const float4* sums;
     const float* of_target;
@@ -92,7 +101,7 @@ __global__ void __launch_bounds__(256) k_head_logprobs_finish(const LogprobsFini
     const bool ends = warp == 0 && lane < kFinishRows && row < a.rows;
     const int token = ends ? ld_after_wait(a.tokens + row) : -1;
     const float of_token = ends ? ld_after_wait(a.of_target + row) : 0.f;
-    float m = kFew, s = 0.f, d = 0.f;
+    float m = kFew, n = 0.f, s = 0.f, d = 0.f;
     if (row < a.rows)
         for (int t = warp * 8 + (lane >> 2); t < a.tiles; t += 320) {
             float4 p[5];
@@ -102,21 +111,17 @@ __global__ void __launch_bounds__(256) k_head_logprobs_finish(const LogprobsFini
             float next = m;
 #pragma unroll
             for (int k = 0; k < 5; ++k) next = fmaxf(next, p[k].x);
-            const float by = fmaxf(m - next, kNothing), e = ex2f(by * kLog2e);
-            d = fmaf(by, s, d) * e;
-            s *= e;
+            const float4 before = make_float4(m, s, d, n);
+            n = s = d = 0.f;
+            add_state(before, next, n, s, d);
 #pragma unroll
-            for (int k = 0; k < 5; ++k) {
-                const float of = fmaxf(p[k].x - next, kNothing), f = ex2f(of * kLog2e);
-                d = fmaf(fmaf(of, p[k].y, p[k].z), f, d);
-                s = fmaf(p[k].y, f, s);
-            }
+            for (int k = 0; k < 5; ++k) add_state(p[k], next, n, s, d);
             m = next;
         }
     bool has = token >= 0 && token < a.V;
     if (has && a.mask) has = (ld_after_wait(a.mask + int64_t(row) * a.mask_stride + (token >> 5)) >> (token & 31)) & 1u;
     __shared__ float4 sh[64][kFinishRows];
-    sh[warp * 8 + (lane >> 2)][lane & 3] = make_float4(m, s, d, 0.f);
+    sh[warp * 8 + (lane >> 2)][lane & 3] = make_float4(m, s, d, n);
     __syncthreads();
     if (warp) return;
     // eight threads a row, eight states each
@@ -125,23 +130,20 @@ __global__ void __launch_bounds__(256) k_head_logprobs_finish(const LogprobsFini
     for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[8 * (lane >> 2) + w][lane & 3].x);
 #pragma unroll
     for (int k = 4; k <= 16; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, k));
-    s = d = 0.f;
+    n = s = d = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) {
-        const float4 p = sh[8 * (lane >> 2) + w][lane & 3];
-        const float of = fmaxf(p.x - top, kNothing), f = ex2f(of * kLog2e);
-        d = fmaf(fmaf(of, p.y, p.z), f, d);
-        s = fmaf(p.y, f, s);
-    }
+    for (int w = 0; w < 8; ++w) add_state(sh[8 * (lane >> 2) + w][lane & 3], top, n, s, d);
 #pragma unroll
     for (int k = 4; k <= 16; k <<= 1) {
+        n += __shfl_xor_sync(0xFFFFFFFFu, n, k);
         s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
         d += __shfl_xor_sync(0xFFFFFFFFu, d, k);
     }
     if (!ends) return;
-    const float log_sum = logf(s);
-    if (a.lse) a.lse[row] = s > 0.f ? top + log_sum : -INFINITY;
-    if (a.entropy) a.entropy[row] = s > 0.f ? fmaxf(log_sum - d / s, 0.f) : 0.f;
+    // (n is 0 where nothing is allowed; 1 as a rule, whose logarithm is 0)
+    const float log_sum = logf(n) + log1pf(s / n);
+    if (a.lse) a.lse[row] = n > 0.f ? top + log_sum : -INFINITY;
+    if (a.entropy) a.entropy[row] = n > 0.f ? fmaxf(log_sum - d / (n + s), 0.f) : 0.f;
     if (token >= a.V) atomicAdd(a.status + 1, 1);
     float logp = 0.f;
     if (token >= 0) logp = has && of_token > kFew ? (of_token - top) - log_sum : -INFINITY;

@@ -55,7 +55,7 @@ struct MmaArgs {
     const float *lse, *d_loss;
     const float *entropy, *d_entropy;  // gradient of log probabilities (whose gradient is in d_loss, null where it is 0) and entropies
     float2* part;              // loss: [2 n_tiles, rows] largest score and sum of half a tile
-    float4* sums;              // log probabilities: [2 n_tiles, rows] the same with the sum of exp(d) d
+    float4* sums;              // log probabilities: [2 n_tiles, rows] largest score, sum of the others, of exp(d) d, how many are the largest
     float* of_target;          // loss, log probabilities: [rows]
     Partial* states;           // step: [2 n_tiles, rows] the same with the token
     // results
@@ -143,7 +143,18 @@ __device__ __forceinline__ void loss_epilogue(const MmaArgs& a, const MmaTile& t
     if (valid) a.part[int64_t(2 * t.n + half) * a.rows + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
 }
 
-// The same with the sum of exp(d) d, d = z - largest, which the entropy is made of.
+__device__ __forceinline__ float is_zero(float x) {  // 1 or 0
+    float y;
+    asm("set.eq.f32.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float sum_of(pair2 x) {
+    float a, b;
+    unpack2(x, a, b);
+    return a + b;
+}
+
+// The same with the sum of exp(d) d, d = z - largest, which the entropy is made of; the scores that are the largest are counted apart.
 __device__ __forceinline__ void logprobs_epilogue(const MmaArgs& a, const MmaTile& t, int half, int row, bool valid, float (&z)[128],
                                                   const uint32_t (&bits)[4]) {
     store_of_target(a, t, half, row, valid, z);
@@ -154,17 +165,18 @@ __device__ __forceinline__ void logprobs_epilogue(const MmaArgs& a, const MmaTil
         m[j & 3] = fmaxf(m[j & 3], z[j]);
     }
     const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), ref = fmaxf(top, kFew);
-    float s[4] = {}, d[4] = {};
+    pair2 s[2] = {}, d[2] = {}, n[2] = {};
 #pragma unroll
-    for (int j = 0; j < 128; ++j) {
-        const float x = fmaxf(z[j] - ref, 2.f * kNone), e = ex2f(x * kLog2e);
-        s[j & 3] += e;
-        d[j & 3] = fmaf(e, x, d[j & 3]);
+    for (int j = 0; j < 128; j += 2) {
+        float x0, x1;
+        unpack2(add2(pack2(z[j], z[j + 1]), both(-ref)), x0, x1);
+        const pair2 x = pack2(fmaxf(x0, 2.f * kNone), fmaxf(x1, 2.f * kNone)), e = ex2_pair(mul2(x, both(kLog2e)));
+        const pair2 largest = pack2(is_zero(x0), is_zero(x1));
+        n[j >> 1 & 1] = add2(n[j >> 1 & 1], largest);
+        s[j >> 1 & 1] = add2(s[j >> 1 & 1], fma2(largest, both(-1.f), e));
+        d[j >> 1 & 1] = fma2(e, x, d[j >> 1 & 1]);
     }
-    if (valid) {
-        const float s4 = (s[0] + s[1]) + (s[2] + s[3]), d4 = (d[0] + d[1]) + (d[2] + d[3]);
-        *reinterpret_cast<float4*>(&a.sums[int64_t(2 * t.n + half) * a.rows + row]) = make_float4(ref, s4, d4, 0.f);
-    }
+    if (valid) a.sums[int64_t(2 * t.n + half) * a.rows + row] = make_float4(ref, sum_of(add2(s[0], s[1])), sum_of(add2(d[0], d[1])), sum_of(add2(n[0], n[1])));
 }
 
 // Largest allowed score, its lowest token and the sum of exponentials, of one row and half a tile's tokens.

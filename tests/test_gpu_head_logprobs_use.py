@@ -116,3 +116,33 @@ def test_scores_as_large_as_a_float_holds(size):
     assert (logp[::2] == 0).all() and (entropy[::2] == 0).all()
     # three hundred equal scores, in exact arithmetic: the roundings of a logarithm
     assert ((logp[1::2] + log_n).abs() <= 2.0 ** -20).all() and ((entropy[1::2] - log_n).abs() <= 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("V,N", [(2000, 3), (50000, 3), (9000, 300)])
+def test_a_nearly_certain_token_keeps_what_the_others_have_together(V, N):
+    """Scores of small whole numbers, exact in 32 bits: what is left of the log probability is good to the bits of the others' sum, not of
+    the 1 beside it; the same of the entropy."""
+    H = 64
+    g = torch.Generator(device="cuda")
+    g.manual_seed(17)
+    weight = torch.zeros((V, H), device="cuda")
+    weight[:, :8] = torch.randint(-4, 5, (V, 8), generator=g, device="cuda") / 4
+    weight[5, :] = 0.0
+    weight[5, 8] = 1.0
+    hidden = torch.zeros((N, H), device="cuda")
+    hidden[:, :8] = torch.randint(-2, 3, (N, 8), generator=g, device="cuda") / 2
+    hidden[:, 8] = torch.tensor([20.0, 24.0, 28.0], device="cuda").repeat(N // 3)
+    weight, hidden = weight.to(torch.bfloat16), hidden.to(torch.bfloat16)
+    tokens = torch.full((N,), 5, dtype=torch.int32, device="cuda")
+    with Ctx([]) as ctx:
+        logp, entropy, _ = scored(ctx, weight, hidden, tokens)
+    z = hidden.double() @ weight.double().T
+    x = z - z[:, 5:6]
+    x[:, 5] = -float("inf")
+    rest = torch.exp(x).sum(dim=1)
+    want = -torch.log1p(rest)
+    want_entropy = torch.log1p(rest) - (torch.exp(x) * x).nan_to_num(0.0).sum(dim=1) / (1.0 + rest)
+    # the others' terms: an argument within 40 powers of two rounded twice (40 * 2^-23 ln 2), an exponential good to a few units, 32 additions
+    # in a row, some 30 where chains and tiles meet: below 2^-16 of the sum together; the entropy's terms are as many, with a product each
+    assert ((logp - want).abs() <= 2.0 ** -16 * want.abs()).all()
+    assert ((entropy - want_entropy).abs() <= 2.0 ** -15 * want_entropy).all()
