@@ -482,7 +482,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
                 const MmaTile t = mma_tile(a, i);
                 const int m = t.m * kMmaTile + int(rank) * 128, n = t.n * a.width + int(rank) * (a.width / 2);
                 const int k1 = a.expire ? min(t.k1, t.k0 + kStages) : t.k1;
-                const bool first_only = !A_MN && a.rows <= 128;
+                const bool first_only = !A_MN && a.rows <= 128, with_a = !first_only || rank == 0;
                 const uint32_t bytes = (A_MN ? 2 * kMmaHalf : uint32_t(a.box) * (first_only ? 1 : 2) * kMmaK * 2) + uint32_t(a.width) * kMmaK * 2;
                 for (int k = t.k0; k < k1; ++k) {
                     if (!ring_wait<true>(&empty[r.stage], r.phase ^ 1)) {
@@ -494,8 +494,8 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
                     if (A_MN) {
                         tma_load_pair(at, &map_a, m, k * kMmaK, bar);
                         tma_load_pair(at + kMmaHalf / 2, &map_a, m + 64, k * kMmaK, bar);
-                    } else if (!first_only || rank == 0) {
-                        tma_load_pair(at, &map_a, k * kMmaK, m, bar);
+                    } else {
+                        tma_load_pair_if(with_a, at, &map_a, k * kMmaK, m, bar);
                     }
                     if (B_MN) {
                         tma_load_pair(at + kMmaHalf, &map_b, n, k * kMmaK, bar);
