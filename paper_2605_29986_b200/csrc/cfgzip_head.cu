@@ -245,7 +245,7 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
         return CFGZIP_OK;
     }
     CUtensorMap x_k, x_mn, w_k, w_mn, g_k, g_mn;
-    if ((rc = tensor_map(ctx, &x_k, hidden, N, H, hidden_stride, a_box(N))) != CFGZIP_OK ||
+    if ((rc = tensor_map_a(ctx, &x_k, hidden, N, H, hidden_stride)) != CFGZIP_OK ||
         (rc = tensor_map(ctx, &x_mn, hidden, N, H, hidden_stride, 64)) != CFGZIP_OK)
         return rc;
     const int32_t* targets = of.d_loss ? of.targets : nullptr;
@@ -259,7 +259,7 @@ int head_gradient(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidden, 
         const int width = tile_width(N, n);
         if ((rc = tensor_map(ctx, &w_k, weights, n, H, head->row_stride, width / 2)) != CFGZIP_OK ||
             (rc = tensor_map(ctx, &w_mn, weights, n, H, head->row_stride, 64)) != CFGZIP_OK ||
-            (rc = tensor_map(ctx, &g_k, w.g, N, n, w.piece, a_box(N))) != CFGZIP_OK ||
+            (rc = tensor_map_a(ctx, &g_k, w.g, N, n, w.piece)) != CFGZIP_OK ||
             (rc = tensor_map(ctx, &g_mn, w.g, N, n, w.piece, 64)) != CFGZIP_OK)
             return rc;
         MmaArgs a{};
@@ -451,7 +451,7 @@ int cfgzip_head_step(cfgzip_ctx* ctx, cfgzip_part_id part0, const int32_t* row_p
     const int32_t most = head->dtype == CFGZIP_MXFP4 ? kStepRowsMx : kStepRows;
     if (tall) {
         CUtensorMap map_x, map_w;
-        if ((rc = tensor_map(ctx, &map_x, hidden, B, head->H, hidden_stride, 128)) != CFGZIP_OK ||
+        if ((rc = tensor_map_a(ctx, &map_x, hidden, B, head->H, hidden_stride)) != CFGZIP_OK ||
             (rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, tile_width(B, head->V) / 2)) != CFGZIP_OK)
             return rc;
         MmaArgs a{};
@@ -531,7 +531,7 @@ int cfgzip_head_loss(cfgzip_ctx* ctx, const cfgzip_head* head, const void* hidde
     if (!guard.ok) return CFGZIP_E_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     CUtensorMap map_x, map_w;
-    if ((rc = tensor_map(ctx, &map_x, hidden, N, head->H, hidden_stride, a_box(N))) != CFGZIP_OK ||
+    if ((rc = tensor_map_a(ctx, &map_x, hidden, N, head->H, hidden_stride)) != CFGZIP_OK ||
         (rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, tile_width(N, head->V) / 2)) != CFGZIP_OK)
         return rc;
     MmaArgs a{};
@@ -590,7 +590,7 @@ int cfgzip_head_logprobs(cfgzip_ctx* ctx, const cfgzip_head* head, const void* h
     CUtensorMap map_x, map_w;
     MmaArgs a{};
     a.width = tile_width(N, head->V);
-    if ((rc = tensor_map(ctx, &map_x, hidden, N, head->H, hidden_stride, a_box(N))) != CFGZIP_OK ||
+    if ((rc = tensor_map_a(ctx, &map_x, hidden, N, head->H, hidden_stride)) != CFGZIP_OK ||
         (rc = tensor_map(ctx, &map_w, head->weight, head->V, head->H, head->row_stride, a.width / 2)) != CFGZIP_OK)
         return rc;
     a.rows = N;

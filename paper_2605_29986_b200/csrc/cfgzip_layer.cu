@@ -198,7 +198,7 @@ int run_tall(cfgzip_ctx* ctx, const LayerProduct& p, cudaStream_t st) {
     a.has_slope = p.slope != nullptr;
     CUtensorMap map_a, map_b, map_y, map_slope;
     int rc;
-    if ((rc = tensor_map(ctx, &map_a, p.a, p.rows, p.k, p.a_stride, a_box(p.rows))) != CFGZIP_OK ||
+    if ((rc = tensor_map_a(ctx, &map_a, p.a, p.rows, p.k, p.a_stride)) != CFGZIP_OK ||
         (rc = p.turned ? tensor_map(ctx, &map_b, p.weight, p.k, p.features, p.weight_stride, 64)
                        : tensor_map(ctx, &map_b, p.weight, p.features, p.k, p.weight_stride, 128)) != CFGZIP_OK ||
         (rc = tensor_map_out(ctx, &map_y, a, true)) != CFGZIP_OK)

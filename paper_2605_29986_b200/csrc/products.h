@@ -109,7 +109,11 @@ inline int tensor_map_out(cfgzip_ctx* ctx, CUtensorMap* map, const MmaArgs& a, b
 
 // Rows of A, where its k is contiguous, in a block's copies: what lies behind the last one is not asked for (rows outside a map cost the
 // copies more than they seem: log probabilities of one row of 32000 x 2048 46 -> 31 us, of 128256 x 4096 221 -> 191).
+// (MmaArgs::box, and with it the bytes that a stage waits for, and the map are both made from it.)
 inline int a_box(int64_t rows) { return int(std::min<int64_t>(128, up(rows, 8))); }
+inline int tensor_map_a(cfgzip_ctx* ctx, CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t stride) {
+    return tensor_map(ctx, map, p, rows, cols, stride, a_box(rows));
+}
 
 template <bool A_MN, bool B_MN, int KIND, bool LONG = true>
 int run_mma(cfgzip_ctx* ctx, MmaArgs& a, const CUtensorMap& map_a, const CUtensorMap& map_b, cudaStream_t st) {
