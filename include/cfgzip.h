@@ -380,8 +380,9 @@ int cfgzip_head_loss_backward(cfgzip_ctx* ctx, const cfgzip_head* head, const vo
  *                id, lowest first. Where fewer have a probability the rest is token -1 with log probability -inf
  *   logp, entropy, lse : dev float [N], each nullable. A row with nothing allowed: lse -inf, entropy 0, logp -inf (0 where no token is given)
  *   top_tokens, top_logp : dev int32 and float [N, n_top] (not looked at where n_top is 0)
- * Allowed logits below -1e29 count as -inf; +inf and NaN among them, and zt that no float holds, are outside the contract. Statistics are held in 32 bits. The results
- * are the same from call to call.
+ * Allowed logits below -1e29 count as -inf; +inf and NaN among them, and zt that no float holds, are outside the contract. Sums are held in 32
+ * bits in a thread and in 64 between threads, log probabilities are taken of differences to the row's largest logit: they and the entropy lose
+ * nothing where a row is far from zero, of which lse keeps 24 bits. The results are the same from call to call.
  */
 int cfgzip_token_logprobs(cfgzip_ctx* ctx, const void* logits, int dtype, int64_t row_stride_elems, int32_t N, int32_t V,
                           const uint32_t* vocab_mask, int64_t vocab_stride_words, const int32_t* tokens, float inv_temperature,
@@ -391,8 +392,10 @@ int cfgzip_token_logprobs(cfgzip_ctx* ctx, const void* logits, int dtype, int64_
  * Its gradient with respect to the logits, for gradients d_logp and d_entropy of the two results:
  *   d_logits[n, t] = inv_temperature * (d_logp[n] * ([t = tokens[n]] - p) - d_entropy[n] * p * (log p + entropy[n]))
  * over the allowed tokens, and 0 for the others. d_logp has no part in rows whose logp is 0 or -inf as said above (no token given, one
- * that is not allowed); a row with nothing allowed is all 0. At the given token 1 - p is taken without its difference to 1, so that a
- * token the model is sure of keeps its gradient.
+ * that is not allowed); a row with nothing allowed is all 0. p = exp(zt - lse[n]) has in it what lse was rounded by, up to 2^-24 |lse| of
+ * itself: 1e-6 of rows around 20, all of it from |lse| = 2^24 on, where the gradient is finite and no more can be said of it. At the given
+ * token 1 - p is taken without its difference to 1 and is off by no more than that: a token that the model is sure of has its gradient
+ * down to a 1 - p of 2^-24 |lse|, and below it what the rounding left.
  *   logits .. inv_temperature : as given to cfgzip_token_logprobs
  *   lse, entropy : dev float [N], as it returned them (entropy NULL where d_entropy is)
  *   d_logp, d_entropy : dev float [N], one of them nullable
@@ -419,7 +422,8 @@ int cfgzip_head_logprobs(cfgzip_ctx* ctx, const cfgzip_head* head, const void* h
 
 /*
  * Its gradient. With g[n, t] = d_logp[n] * ([t = tokens[n]] - p) - d_entropy[n] * p * (log p + entropy[n]) over the allowed tokens (d_logp
- * has no part in rows whose logp is not a finite function of z, a row with nothing allowed has none):
+ * has no part in rows whose logp is not a finite function of z, a row with nothing allowed has none; the given token's score is -1e29 at the
+ * least, unless it is not allowed):
  *   d_hidden[n, :] = sum_t g[n, t] * weight[t, :],    d_weight[t, :] = sum_n g[n, t] * hidden[n, :]
  * The scores are computed again, the same to the last bit, and g is rounded to bf16, as in cfgzip_head_loss_backward; what is said there of
  * accuracy, and of weights and hidden states that have to be finite where g is 0, holds here. Only what the given token's g is rounded by,
