@@ -241,6 +241,19 @@ struct EntropySums {
     }
 };
 
+// The sum over `LANES` lanes of sums that each has, relative to a reference that is no lower (in every lane).
+template <int LANES>
+__device__ __forceinline__ double2 sum_at(const double2& p, const Reference& from, const Reference& to, const Powers& powers) {
+    const float by = from.to(to, powers), e = ex2f(by);
+    double2 t = make_double2(p.x * double(e), fma(double(by), p.x, p.y) * double(e));
+#pragma unroll
+    for (int k = LANES / 2; k >= 1; k >>= 1) {
+        t.x += __shfl_xor_sync(0xFFFFFFFFu, t.x, k);
+        t.y += __shfl_xor_sync(0xFFFFFFFFu, t.y, k);
+    }
+    return t;
+}
+
 // Numbers in the order of their values, both zeros alike, and behind it the lower token first.
 __device__ __forceinline__ unsigned long long candidate_key(float z, int token) {
     const uint32_t b = __float_as_uint(z + 0.f);
@@ -476,55 +489,43 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
         s_sum[warp] = t;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        float m = s_ref[0];
-#pragma unroll
-        for (int w = 1; w < WARPS; ++w) m = fmaxf(m, s_ref[w]);
-        const Reference to{m};
-        double s = 0.0, d = 0.0;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            const double2 p = s_sum[w];
-            const float by = Reference{s_ref[w]}.to(to, a.powers), e = ex2f(by);
-            s = fma(p.x, double(e), s);
-            d = fma(fma(double(by), p.x, p.y), double(e), d);
+    if (warp == 0) {
+        const float ref = lane < WARPS ? s_ref[lane] : kFew, m = redux_max(ref);
+        t = sum_at<WARPS>(lane < WARPS ? s_sum[lane] : make_double2(0.0, 0.0), Reference{ref}, Reference{m}, a.powers);
+        if (lane == 0) {
+            st_peer_u32(peer_shared(&s_block_ref[rank], 0), __float_as_uint(m));
+            const uint32_t at = peer_shared(&s_block[rank], 0);
+            st_peer_u32(at, uint32_t(__double2loint(t.x)));
+            st_peer_u32(at + 4, uint32_t(__double2hiint(t.x)));
+            st_peer_u32(at + 8, uint32_t(__double2loint(t.y)));
+            st_peer_u32(at + 12, uint32_t(__double2hiint(t.y)));
         }
-        st_peer_u32(peer_shared(&s_block_ref[rank], 0), __float_as_uint(m));
-        const uint32_t at = peer_shared(&s_block[rank], 0);
-        st_peer_u32(at, uint32_t(__double2loint(s)));
-        st_peer_u32(at + 4, uint32_t(__double2hiint(s)));
-        st_peer_u32(at + 8, uint32_t(__double2loint(d)));
-        st_peer_u32(at + 12, uint32_t(__double2hiint(d)));
     }
     __syncwarp();
     cluster_barrier();
     if (rank != 0) return;
 
-    if (threadIdx.x == 32) {  // (the second warp, while the first looks for the alternatives)
-        float m = kFew;
-        for (int b = 0; b < blocks; ++b) m = fmaxf(m, s_block_ref[b]);
+    if (warp == 1) {  // (the second warp, while the first looks for the alternatives)
+        const float ref = lane < blocks ? s_block_ref[lane] : kFew, m = redux_max(ref);
         const Reference to{m};
-        double s = 0.0, d = 0.0;
-        for (int b = 0; b < blocks; ++b) {
-            const double2 p = s_block[b];
-            const float by = Reference{s_block_ref[b]}.to(to, a.powers), e = ex2f(by);
-            s = fma(p.x, double(e), s);
-            d = fma(fma(double(by), p.x, p.y), double(e), d);
-        }
+        t = sum_at<kClusterMost>(lane < blocks ? s_block[lane] : make_double2(0.0, 0.0), Reference{ref}, to, a.powers);
+        const double s = t.x, d = t.y;
         // relative to the largest logit itself, whose exponential is taken off and divided out as it was added: a row's only token has log
         // probability 0, and one that is nearly certain keeps what the others have together
         const float of_most = to.power(m, a.powers), e_most = ex2f(of_most);
         const double rest = s - double(e_most);
         const float log_sum = log1pf(float(rest) / e_most);  // (-inf where nothing is allowed)
-        s_most = m;
-        s_log_sum = log_sum;
-        if (a.lse) a.lse[row] = s > 0.0 ? fmaf(m, a.inv_temperature, log_sum) : -INFINITY;
-        if (a.entropy) a.entropy[row] = s > 0.0 ? fmaxf(log_sum - kLn2 * (float(fma(-double(of_most), rest, d - double(e_most * of_most))) / float(s)), 0.f) : 0.f;
-        if (a.tokens) {
-            float logp = 0.f;
-            if (token >= 0) logp = of_token > kFew ? fmaf(of_token - m, a.inv_temperature, -log_sum) : -INFINITY;
-            a.logp[row] = logp;
-            if (token >= a.V) atomicAdd(a.status + 1, 1);
+        if (lane == 0) {
+            s_most = m;
+            s_log_sum = log_sum;
+            if (a.lse) a.lse[row] = s > 0.0 ? fmaf(m, a.inv_temperature, log_sum) : -INFINITY;
+            if (a.entropy) a.entropy[row] = s > 0.0 ? fmaxf(log_sum - kLn2 * (float(fma(-double(of_most), rest, d - double(e_most * of_most))) / float(s)), 0.f) : 0.f;
+            if (a.tokens) {
+                float logp = 0.f;
+                if (token >= 0) logp = of_token > kFew ? fmaf(of_token - m, a.inv_temperature, -log_sum) : -INFINITY;
+                a.logp[row] = logp;
+                if (token >= a.V) atomicAdd(a.status + 1, 1);
+            }
         }
     }
     if (!a.n_top) return;
