@@ -209,7 +209,8 @@ __device__ __forceinline__ void round_targets(const RoundTargetsArgs& a, int blo
 // The rows that have a token for a target as a chain in the order of the rows: the first row of each token that is a target, each row's next
 // one. A warp compares its four rows' targets with all others, 32 at a time; no order of arrival plays a part. Tokens that are no target keep
 // what the workspace held before: whoever asks for a token's first row looks whether that row has it (first_row), which spares writing, and
-// searching for, all of the vocabulary's. Nothing is left of the targets yet (rest 0). (4096 rows: 20 us of a gradient of 9 ms.)
+// searching for, all of the vocabulary's. Nothing is left of the targets yet (rest 0). (4096 rows: 10 us of a gradient of 9 ms;
+// it grows with the square of them.)
 constexpr int kTargetRows = 4;
 __global__ void __launch_bounds__(256) k_head_targets(const int32_t* targets, int N, int V, int32_t* first_of, int32_t* next_of, float* rest) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

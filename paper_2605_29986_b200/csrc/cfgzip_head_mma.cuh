@@ -423,8 +423,8 @@ __device__ __forceinline__ void layer_columns(const MmaArgs& a, const CUtensorMa
 // from tensor memory (100 tokens of 50021 x 1024: 26 us for d_weight against 38).
 //
 // A layer's sums stay in tensor memory to their end: their results are bf16, and what is cut off (1e-9 of a sum per element of k) is far
-// below that. (8192 rows of 4096 -> 4096 with bias, residual and derivative: 180 to 193 us, 1.42 to 1.53 PFLOP/s; of 512 -> 4096 56, bound by
-// what is done with the sums.)
+// below that. (8192 rows of 4096 -> 4096 with bias, residual and derivative: 180 to 227 us, 1.2 to 1.5 PFLOP/s by the power limit; of
+// 512 -> 4096 50 without a derivative, bound by what is done with the sums.)
 template <bool A_MN, bool B_MN, int KIND, bool LONG>
 __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_out,
                                              const CUtensorMap& map_slope) {
@@ -460,7 +460,7 @@ __device__ __forceinline__ void mma_products(const MmaArgs& a, const CUtensorMap
     if (warp == 2) tmem_alloc<2>(&s_tmem, 512);
     if (!A_MN && !kLayer && a.rows <= 128) {
         // Rows that no copy brings are zeros: whatever stands there would do, but is multiplied at the expense of the clocks (a second of
-        // losses of 16 rows of 128256 x 4096: 250 us each instead of 200).
+        // losses of 16 rows of 128256 x 4096: 250 us each instead of 225). It takes each launch 0.2 us.
         for (int i = 0; i < kStages; ++i)
             for (uint32_t at = (rank == 0 ? uint32_t(a.box) * 128 : 0u) + threadIdx.x * 16; at < kMmaHalf; at += blockDim.x * 16)
                 st_shared16(stages + uint32_t(i) * 2 * kMmaHalf + at, make_uint4(0, 0, 0, 0));

@@ -112,6 +112,7 @@ FewPlan few_plan(const cfgzip_ctx* ctx, const LayerProduct& p) {
         for (int s = 1; s <= kLayerBlocks && (s == 1 || 2 * s <= k_blocks); ++s) {
             const int steps = ceil_div(k_blocks, s), stages = std::max(std::min(most, steps), least);
             const int twice = 2 * (size_t(stages) * stage_bytes + 2560) <= size_t(ctx->smem_optin) ? 2 : 1;
+            // (of clusters with a block to an SM; those of 3 and 5 leave SMs over wherever they are placed)
             const int limit = s == 1 ? ctx->sm_count : ctx->cluster_limit[s] - (s == 3 || s == 5 ? 3 : 0);
             if (limit <= 0) continue;
             const double rounds = std::ceil(clusters / (double(limit) * twice)), beside = std::min(double(twice), std::ceil(clusters / limit));

@@ -106,7 +106,8 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const float* part
 // Sums stay in tensor memory over all of a block's k: what its additions cut off (1e-9 of the sum per element) is far below the rounding
 // of the result to bf16.
 //
-// Bound by latency (one row of 2048 x 2048: 4.7 us), then by the weights' way from memory (32 rows of 4096 x 4096: 8.4 us, 4 TB/s).
+// Bound by latency (one row of 2048 x 2048: 4.7 us), then by the weights' way from memory (32 rows of 4096 x 4096: 8.4 to 10.5 us, 3.2 to
+// 4 TB/s).
 template <bool A_MN, int ACT>
 __global__ void __launch_bounds__(kLayerThreads, 2)
     k_layer_few(const __grid_constant__ LayerArgs a, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x) {

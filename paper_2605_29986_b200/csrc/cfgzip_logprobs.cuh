@@ -359,9 +359,9 @@ __device__ __forceinline__ Picked pick_largest(float* values, int all, int n, in
 // Equal logits may put too many chunks above a bar. In the order (largest logit, then place) the first n chunks hold the first n tokens (n
 // chunks ahead of a token's own hold n tokens ahead of it), and can be picked one after the other: 0.5 us each.
 //
-// 4096 bf16 rows of 128256 take 175 us (6.0 TB/s), with 5 alternatives 190; 1000 of 100003 under masks 53, bound by instruction issue; 32 of
-// 128256 with 20 alternatives 9 to 10, and one of 32000 5, by latency. What is done in 64 bits, and eight logits added up first, are 1.5 % of
-// the large ones.
+// 4096 bf16 rows of 128256 take 177 to 185 us (5.7 to 5.9 TB/s), with 5 alternatives 192 to 203; 1000 of 100003 under masks 54 to 55, bound by
+// instruction issue; 32 of 128256 with 20 alternatives 9 to 10, and one of 32000 5, by latency. What is done in 64 bits, and eight logits added
+// up first, are 1.5 % of the large ones, references that hold far from zero 1 % (of short rows, 4096 of 2000, 6).
 template <int DT, bool MASKED, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const LogprobsArgs a, int blocks) {
     constexpr int kThreads = WARPS * 32;
@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_token_logprobs(const
 
     __syncwarp();
     cluster_wait();  // (the first block is there to be written to)
-    // (f32 rows under masks have no registers for it: 1000 of 100003 91 us instead of 74)
+    // (f32 rows under masks have no registers for it: 1000 of 100003 87 us instead of 70)
     constexpr bool kFirst = !(DT == kF32 && MASKED);
     EntropySums sums;
     float most = kNone;
@@ -722,7 +722,8 @@ constexpr int kLogprobsPiece = kLogprobsOctets<DT> * 2048;
 // An octet at a time from the gradient's own boundaries on. Logits whose rows start at another place relative to 16 bytes (TOGETHER false) are
 // read element by element. Rows without a gradient are written without being read. A block does its tokens in one go: masks and the row's numbers are asked
 // for, then the logits, then what the row's constants need of the given token, so that three latencies follow one another, and four or more
-// blocks of an SM share them. (4096 bf16 rows of 128256: 307 us, 6.8 TB/s; 500 f32 rows of 50021 under masks 35 to 40, 5.1 to 5.7.)
+// blocks of an SM share them. (4096 bf16 rows of 128256: 305 to 331 us, of which a copy takes 321; 500 f32 rows of 50021 under
+// masks 35 to 40, 5.1 to 5.7 TB/s.)
 template <int DT, bool MASKED, bool TOGETHER>
 __global__ void __launch_bounds__(256, 4) k_token_logprobs_backward(const LogprobsBackwardArgs a) {
     constexpr int kSize = DT == kBF16 ? 2 : 4, kAhead = kLogprobsOctets<DT>;
