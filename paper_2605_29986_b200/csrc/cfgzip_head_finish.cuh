@@ -255,9 +255,10 @@ __global__ void __launch_bounds__(256) k_head_targets(const int32_t* targets, in
 // The rows of the head's gradient that are targets, once more: their sums as they were kept, and what their rows' g was rounded by times the
 // hidden states. A block a row of the text; the first row of a chain does all of it. Each step along a chain is a load that waits for the one
 // before. Answers under a grammar repeat some tokens again and again: chains of more than kTargetSteps rows are listed by looking through the
-// targets, and have a block for every kTargetCols columns, in which four groups of threads add up every fourth row, four loads in flight
-// (gradient of 1000 tokens of 32000 x 2048, all the same: 775 us along the chain).
-constexpr int kTargetCols = 512, kTargetSteps = 8, kTargetList = 1024, kTargetSlice = 4;
+// targets, and have a block for every kTargetCols columns, in which eight groups of threads add up every eighth row, four loads in flight
+// (gradient of 4000 tokens of 2000 x 4096, all the same: 7300 us along the chain, 670 by 512 columns, 440; of twice as many tokens as there are
+// in the vocabulary 242, 228 without looking for long chains).
+constexpr int kTargetCols = 256, kTargetGroups = 8 * 256 / kTargetCols, kTargetSteps = 8, kTargetList = 1024, kTargetSlice = 8;
 struct WeightTargetsArgs {
     const int32_t *targets, *first_of, *next_of;
     const float *rest, *kept;
@@ -276,8 +277,8 @@ __device__ __forceinline__ void store_weight_targets(const WeightTargetsArgs& a,
 __device__ __forceinline__ void weight_targets_of_many(const WeightTargetsArgs& a, int row, int target, int c0) {
     __shared__ int s_row[kTargetList], s_count[32];
     __shared__ float s_rest[kTargetList];
-    __shared__ __align__(16) float s_sum[4][kTargetCols];
-    const int warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31, group = int(threadIdx.x) >> 6, mine = 8 * (int(threadIdx.x) & 63);
+    __shared__ __align__(16) float s_sum[kTargetGroups][kTargetCols];
+    const int warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31, group = int(threadIdx.x) / (kTargetCols / 8), mine = 8 * (int(threadIdx.x) % (kTargetCols / 8));
     const bool some = c0 + mine < a.H;
     float f[8] = {};
     for (int n0 = row; n0 < a.N; n0 += kTargetList) {  // 1024 targets at a time, those that are this one in the rows' order
@@ -309,7 +310,7 @@ __device__ __forceinline__ void weight_targets_of_many(const WeightTargetsArgs& 
         __syncthreads();
         if (some) {
 #pragma unroll 4
-            for (int i = group; i < all; i += 4) {
+            for (int i = group; i < all; i += kTargetGroups) {
                 float x[8];
                 bf16_values(ld_after_wait(reinterpret_cast<const uint4*>(a.hidden + int64_t(s_row[i]) * a.hidden_stride + c0 + mine)), x);
 #pragma unroll
@@ -327,7 +328,7 @@ __device__ __forceinline__ void weight_targets_of_many(const WeightTargetsArgs& 
     if (at >= kTargetCols || c0 + at >= a.H) return;
     float4 sum = __ldcg(reinterpret_cast<const float4*>(a.kept + int64_t(row) * a.H + c0 + at));
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
+    for (int g = 0; g < kTargetGroups; ++g) {
         const float4 x = *reinterpret_cast<const float4*>(&s_sum[g][at]);
         sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
     }
