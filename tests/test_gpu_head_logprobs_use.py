@@ -4,7 +4,7 @@ import torch
 
 from paper_2605_29986_b200 import binding as cz
 from _gpu_util import Ctx
-from test_gpu_head import close, loss_inputs
+from test_gpu_head import close, loss_inputs, run_loss
 from test_gpu_head_logprobs import gradient, run, run_gradient
 
 pytestmark = pytest.mark.gpu
@@ -146,3 +146,22 @@ def test_a_nearly_certain_token_keeps_what_the_others_have_together(V, N):
     # in a row, some 30 where chains and tiles meet: below 2^-16 of the sum together; the entropy's terms are as many, with a product each
     assert ((logp - want).abs() <= 2.0 ** -16 * want.abs()).all()
     assert ((entropy - want_entropy).abs() <= 2.0 ** -15 * want_entropy).all()
+
+
+@pytest.mark.parametrize("V,H,N", [(300, 64, 9), (2000, 1032, 1000)])
+def test_gradient_of_the_loss_in_the_place_of_the_hidden_states(V, H, N):
+    case, mask, packed, targets = loss_inputs(V, H, N, 0.5, 8, seed=22)
+    d_loss = torch.rand(N, generator=case.gen, device="cuda")
+    ws = case.workspace(cz.HEAD_LOSS_BACKWARD)
+    with Ctx([]) as ctx:
+        _, lse = run_loss(ctx, case, packed, targets)
+
+        def backward(d_hidden, d_weight):
+            cz.cfgzip_head_loss_backward(ctx.h, case.head, case.hidden, case.hidden.stride(0), N, packed, packed.shape[1], targets, lse, d_loss,
+                                         d_hidden, d_hidden.stride(0), d_weight, cz.F32, H, 0, ws, ws.numel(), torch.cuda.current_stream())
+
+        want, got = (torch.zeros((V, H), device="cuda") for _ in range(2))
+        d_hidden = torch.zeros((N, H), dtype=torch.bfloat16, device="cuda")
+        backward(d_hidden, want)
+        backward(case.hidden, got)
+        assert torch.equal(case.hidden, d_hidden) and torch.equal(got, want)
